@@ -179,7 +179,8 @@ def prepare(case, seed):
                 pos += list(range(lens[s], lens[s] + cnt[s]))
         st["pos"] = dev(pos, torch.int32)
         if case["tree"]:
-            st["mask"] = dev(np.concatenate(words), torch.int64)
+            behind = 3 if case["op"] == "attend" and S > 1 else 0
+            st["mask"] = dev(np.concatenate(words + [np.zeros((behind, W), dtype=np.int64)]), torch.int64)
     if case["op"] == "append":       # q, k and v of one projection, side by side
         st["qkv"] = torch.randn(n_rows, (H + 2 * Hk) * d, device="cuda", generator=gen).to(T)
         st["q_out"] = torch.empty(n_rows, H * d, dtype=T, device="cuda")
@@ -276,7 +277,7 @@ def _plain_attend(st):
     j = (key[None, :] - kv[:, None])                                                # [S, L]: number among the new rows
     see = (j[:, None, :] >= 0) & (j[:, None, :] <= row[None, :, None])              # [S, N, L]
     if st["mask"] is not None:
-        m = st["mask"][at.clamp(max=st["mask"].shape[0] - 1)]                       # [S, N, W]
+        m = st["mask"][at]                                                          # [S, N, W]
         jj = j.clamp(0, m.shape[2] * 64 - 1)[:, None, :].expand(S, N, L)
         see = see & (((m.gather(2, jj >> 6) >> (jj & 63)) & 1) == 1)
     see = (see | (j[:, None, :] < 0)) & (j[:, None, :] < cnt[:, None, None])
