@@ -281,6 +281,76 @@ ghd_status ghd_medusa_draft(ghd_ctx *ctx, const ghd_medusa_weights *w, const ghd
 ghd_status ghd_tree_fill_tokens(ghd_ctx *ctx, const int32_t *cand_dev, const ghd_accept_result *result_dev,
                                 const int32_t *level_dev, const int32_t *rank_dev, int32_t n, int32_t *tokens_dev);
 
+/* ---- A paged cache in 4 bits, for batches of sequences -----------------------------------------------------------
+ * (Paper Sec. II-A / III-B: a decode step reads every cached key and value once; with 4 bits a value it reads a
+ * quarter of the bytes, and pages let sequences of any length share one buffer.)
+ *
+ * A row of one head, x[d_head] (keys after the rotation, rounded to float), is held as codes with a scale and a minimum:
+ *   min = T(lowest x), scale = T((highest - lowest) / 15), code = (x - min) / scale rounded to the nearest (ties to
+ *   even) and held in [0, 15], 0 when scale is 0; the code stands for min + scale * code.
+ * A row with a NaN or an infinity, or one whose extremes leave T's range, reads back as NaN throughout.
+ * A pool (one per layer) is dev bytes [n_pages][n_kv_heads][block], 16-byte aligned; with R = page_rows a block is
+ *   K codes [R][d_head / 2] | V codes [R][d_head / 2] | K {scale, min} T [R][2] | V {scale, min} T [R][2],
+ * channel 2b in the low half of byte b, channel 2b + 1 in the high half.  Row t of sequence s is row t mod R of page
+ * page_table[s * max_pages + t / R].  Pages may be shared by sequences as long as nobody writes to them.
+ * The lengths live on the device: no call reads them on the host, so steps can be recorded into one CUDA graph.
+ * A length, row number or page id outside its range is skipped by the kernel that meets it (such keys count as not
+ * visible) and recorded in the status word: ghd_sync_status -> GHD_ENOSPACE (rows beyond the page table) or GHD_EINVAL
+ * (a page id outside [0, n_pages)). */
+typedef struct ghd_kv4 {
+    int32_t n_seqs;             /* 1 .. GHD_MAX_SEQS                                             */
+    int32_t n_pages;            /* pages of every pool                                           */
+    int32_t page_rows;          /* 16, 32, 64 or 128                                             */
+    int32_t max_pages;          /* columns of the page table: max_pages * page_rows < 2^31        */
+    int32_t n_kv_heads;         /* divides cfg.n_heads: query head h reads head h / (n_heads / n_kv_heads) */
+    const int32_t *page_table;  /* dev [n_seqs][max_pages]; entries past a sequence's rows are not read */
+    int32_t *kv_len;            /* dev [n_seqs]: rows in the cache                                */
+} ghd_kv4;
+#define GHD_MAX_SEQS 1024
+
+/* The new rows of a call, all sequences behind one another: sequence s has rows row_start[s] .. row_start[s + 1] - 1
+ * (none is allowed); its i-th new row is cache row kv_len[s] + i.  Rows from row_start[n_seqs] on belong to nobody:
+ * what the calls write there stays as it was.  pos: position ids, NULL = kv_len[s] + i.  mask: bit j (word j / 64, LSB
+ * first) of row i says whether the sequence's new row j is visible to its new row i, for j <= i (bits above i are not
+ * looked at; rows from 64 * mask_words on are not visible); NULL = every j <= i is.  A row that sees nothing gets zeros. */
+typedef struct ghd_kv4_rows {
+    int32_t n_rows;             /* rows of the buffers (0: the call does nothing)                 */
+    int32_t mask_words;
+    const int32_t *row_start;   /* dev [n_seqs + 1], not falling                                  */
+    const int32_t *pos;         /* dev [n_rows] or NULL                                           */
+    const uint64_t *mask;       /* dev [n_rows][mask_words] or NULL                               */
+} ghd_kv4_rows;
+
+/* Bytes of one pool (0 for a description that the calls refuse). */
+size_t ghd_kv4_pool_bytes(const ghd_ctx *ctx, const ghd_kv4 *kv);
+
+/* Appends the new rows (Sec. II-A): rotates q and k by the rows' positions (angles in 64 bits, rotate-half pairing,
+ * cfg.rope_theta), quantises k and v and writes them to cache rows kv_len[s] + i.  kv_len is not changed.
+ *   q: dev T [n_rows][n_heads * d_head], rows q_ld elements apart; q_out: dev T [n_rows][n_heads * d_head], contiguous
+ *   (may be q itself when q_ld is n_heads * d_head); both NULL: keys and values only.  k, v: dev T
+ *   [n_rows][n_kv_heads * d_head], rows kv_ld elements apart (q, k and v may be column blocks of one projection).
+ *   q_ld / kv_ld 0 = contiguous.  Pointers 16-byte aligned, leading dimensions multiples of 8. */
+ghd_status ghd_kv4_append(ghd_ctx *ctx, const ghd_kv4 *kv, const ghd_kv4_rows *rows, void *pool, const void *q, int64_t q_ld,
+                          const void *k, const void *v, int64_t kv_ld, void *q_out);
+
+/* Attention of the new rows over the cache (ghd_tree_attention over pages and 4 bits): row i of sequence s sees cache
+ * rows [0, kv_len[s]) and the new rows its mask shows, which ghd_kv4_append has already written.
+ * q (rotated), out: dev T [n_rows][n_heads * d_head], 16-byte aligned. */
+ghd_status ghd_kv4_attention(ghd_ctx *ctx, const ghd_kv4 *kv, const ghd_kv4_rows *rows, const void *pool, const void *q, void *out);
+
+/* Reads rows back: row i of sequence s is cache row first[s] + i (first: dev [n_seqs], NULL = kv_len), min + scale * code
+ * rounded once to T, into k_out and v_out, dev T [n_rows][n_kv_heads * d_head], 16-byte aligned (one of them may be NULL).
+ * rows->pos and rows->mask are not looked at. */
+ghd_status ghd_kv4_read(ghd_ctx *ctx, const ghd_kv4 *kv, const ghd_kv4_rows *rows, const void *pool, const int32_t *first,
+                        void *k_out, void *v_out);
+
+/* What a step keeps (ghd_kv_commit over pages): results_dev[s] is what ghd_accept wrote for sequence s; its accepted rows
+ * move from kv_len[s] + nodes[j] to kv_len[s] + j, j = 1 .. n_matched, in each of the n_layers pools (HOST array), and
+ * kv_len[s] grows by n_matched + 1.  A sequence without new rows keeps its length.  results_dev NULL: every new row is
+ * kept, kv_len[s] grows by the sequence's number of new rows (a prompt) and nothing moves (pools may be NULL). */
+ghd_status ghd_kv4_commit(ghd_ctx *ctx, const ghd_kv4 *kv, const ghd_kv4_rows *rows, void *const *pools, int32_t n_layers,
+                          const ghd_accept_result *results_dev);
+
 /* Building blocks of the layer, exposed for unit tests (same kernels the layer uses).
  * ghd_linear: y float [n][m] = x T[n][k] * w T[m][k]^T.
  * ghd_gate_up: u T [n][d_ffn] = SiLU(h Wg^T) * (h Wu^T) for h T [n][d_model], w_gate_up T [2*d_ffn][d_model]

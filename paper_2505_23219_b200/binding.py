@@ -18,6 +18,7 @@ __all__ = [
     "ghd_create", "ghd_destroy", "ghd_set_option", "ghd_tree_build", "ghd_tree_from_mask", "ghd_verify_layer",
     "ghd_verify_step", "ghd_accept", "ghd_linear", "ghd_rmsnorm", "ghd_tree_attention", "ghd_argmax",
     "ghd_sync_status", "ghd_launch_count", "pack_mask", "ghd_copy_hidden", "ghd_gate_up", "ghd_tree_attention_static", "ghd_path_count", "ghd_kv_commit", "ghd_medusa_draft", "ghd_tree_fill_tokens",
+    "Kv4Cache", "Kv4Rows", "ghd_kv4_pool_bytes", "ghd_kv4_pool", "ghd_kv4_append", "ghd_kv4_attention", "ghd_kv4_read", "ghd_kv4_commit", "GHD_MAX_SEQS",
     "ghd_kv_len_set", "ghd_kv_len_get", "KV_LEN_DEVICE", "MedusaWeights", "GHD_MAX_TOPK",
     "PATH_GEMM_TILE", "PATH_GEMM_SIMT", "PATH_ATTN_TC", "PATH_ATTN_SIMT", "PATH_ATTN_COO", "PATH_GEMM_PAIR", "OPT_GEMM_PAIR", "OPT_ATTN_ROWS", "OPT_GEMM_SKEW", "OPT_ATTN_SMALL",
     "GHD_F32", "GHD_F16", "GHD_MAX_NODES", "OPT_GEMM_PATH", "OPT_ATTN_SPLITS", "OPT_ATTN_PATH", "OPT_GRAPH",
@@ -27,6 +28,7 @@ __all__ = [
 GHD_F32, GHD_F16 = 0, 1
 GHD_MAX_NODES = 256
 GHD_MAX_TOPK = 16
+GHD_MAX_SEQS = 1024
 KV_LEN_DEVICE = -1      # "take the cache length from the context's device word"
 OPT_GEMM_PATH, OPT_ATTN_SPLITS, OPT_ATTN_PATH, OPT_GRAPH, OPT_GEMM_CTAS, OPT_GEMM_BURST, OPT_NO_PDL = 0, 1, 2, 3, 4, 5, 6
 OPT_GEMM_STAGES, OPT_GEMM_EPI, OPT_ATTN_SPARSE, OPT_CHAIN_CALLS, OPT_FUSED_NORM = 7, 8, 9, 10, 11
@@ -42,6 +44,7 @@ EXPORTS = [
     "ghd_tree_attention", "ghd_argmax", "ghd_sync_status", "ghd_status_str", "ghd_last_error", "ghd_launch_count",
     "ghd_tree_attention_static", "ghd_path_count", "ghd_kv_commit", "ghd_kv_len_set", "ghd_kv_len_get",
     "ghd_medusa_draft", "ghd_tree_fill_tokens", "ghd_copy_hidden", "ghd_gate_up",
+    "ghd_kv4_pool_bytes", "ghd_kv4_append", "ghd_kv4_attention", "ghd_kv4_read", "ghd_kv4_commit",
 ]
 
 
@@ -81,6 +84,15 @@ class _Tree(C.Structure):
                 ("rope", C.c_void_p), ("coo_ptr", C.c_void_p), ("coo_col", C.c_void_p), ("nnz", C.c_int32)]
 
 
+class _Kv4(C.Structure):
+    _fields_ = [(k, C.c_int32) for k in ("n_seqs", "n_pages", "page_rows", "max_pages", "n_kv_heads")] + \
+               [("page_table", C.c_void_p), ("kv_len", C.c_void_p)]
+
+
+class _Kv4Rows(C.Structure):
+    _fields_ = [("n_rows", C.c_int32), ("mask_words", C.c_int32), ("row_start", C.c_void_p), ("pos", C.c_void_p), ("mask", C.c_void_p)]
+
+
 _LIB = None
 
 
@@ -118,6 +130,11 @@ def load_library(path: str | Path | None = None):
         "ghd_gate_up": ([vp, vp, vp, i32, vp], C.c_int),
         "ghd_tree_attention": ([vp, vp, C.POINTER(_Kv), C.POINTER(_Tree), vp], C.c_int),
         "ghd_argmax": ([vp, vp, i32, i32, vp], C.c_int),
+        "ghd_kv4_pool_bytes": ([vp, C.POINTER(_Kv4)], C.c_size_t),
+        "ghd_kv4_append": ([vp, C.POINTER(_Kv4), C.POINTER(_Kv4Rows), vp, vp, C.c_int64, vp, vp, C.c_int64, vp], C.c_int),
+        "ghd_kv4_attention": ([vp, C.POINTER(_Kv4), C.POINTER(_Kv4Rows), vp, vp, vp], C.c_int),
+        "ghd_kv4_read": ([vp, C.POINTER(_Kv4), C.POINTER(_Kv4Rows), vp, vp, vp, vp], C.c_int),
+        "ghd_kv4_commit": ([vp, C.POINTER(_Kv4), C.POINTER(_Kv4Rows), vp, i32, vp], C.c_int),
         "ghd_sync_status": ([vp], C.c_int),
         "ghd_status_str": ([C.c_int], C.c_char_p),
         "ghd_last_error": ([vp], C.c_char_p),
@@ -180,6 +197,38 @@ class KvLayer:
     @property
     def c(self):
         return _Kv(_ptr(self.k), _ptr(self.v), self.len)
+
+
+def _need(t, dtype, what: str, numel: int):
+    """A contiguous device tensor of `dtype` with at least `numel` elements (its pointer); raises otherwise."""
+    if t.dtype != dtype or not t.is_cuda or not t.is_contiguous() or t.numel() < numel:
+        raise GhdError(1, f"{what}: want a contiguous {dtype} device tensor of at least {numel} elements, "
+                          f"got {tuple(t.shape)} {t.dtype} on {t.device}")
+    return t.data_ptr()
+
+
+class Kv4Cache:
+    """Paging of a 4-bit cache: page_table int32 [n_seqs][max_pages], kv_len int32 [n_seqs] (device tensors; the pools of
+    the layers come with each call).  The tensors are read when a kernel runs and have to stay alive until then."""
+
+    def __init__(self, page_table, kv_len, page_rows: int, n_kv_heads: int, n_pages: int):
+        self.page_table, self.kv_len = page_table, kv_len
+        if page_table.dim() != 2:
+            raise GhdError(1, "kv4: page_table is not [n_seqs][max_pages]")
+        n_seqs, max_pages = page_table.shape
+        self.c = _Kv4(n_seqs, n_pages, page_rows, max_pages, n_kv_heads, _need(page_table, torch.int32, "page_table", 0),
+                      _need(kv_len, torch.int32, "kv_len", n_seqs))
+
+
+class Kv4Rows:
+    """The new rows of a call: row_start int32 [n_seqs + 1]; optional pos int32 [n_rows]; optional mask int64
+    [n_rows][words], bit j of row i = the sequence's new row j is visible to it (device tensors)."""
+
+    def __init__(self, row_start, n_rows: int, pos=None, mask=None):
+        self.row_start, self.n_rows, self.pos, self.mask = row_start, int(n_rows), pos, mask
+        words = 0 if mask is None else int(mask.shape[-1])
+        self.c = _Kv4Rows(self.n_rows, words, _need(row_start, torch.int32, "row_start", 2), None if pos is None else _need(pos, torch.int32, "pos", self.n_rows),
+                          None if mask is None else _need(mask, torch.int64, "mask", self.n_rows * words))
 
 
 class Tree:
@@ -372,6 +421,78 @@ def ghd_tree_fill_tokens(ctx: Ctx, cand, result, level, rank, tokens=None):
     ctx._check(ctx.lib.ghd_tree_fill_tokens(ctx.handle, cand.data_ptr(), result.data_ptr(), level.data_ptr(), rank.data_ptr(), n,
                                             tokens.data_ptr()))
     return tokens
+
+
+def ghd_kv4_pool_bytes(ctx: Ctx, kv: Kv4Cache) -> int:
+    return int(ctx.lib.ghd_kv4_pool_bytes(ctx.handle, C.byref(kv.c)))
+
+
+def ghd_kv4_pool(ctx: Ctx, kv: Kv4Cache, n_layers: int = 1):
+    """A zeroed pool per layer, uint8 [n_layers][bytes]."""
+    return torch.zeros((n_layers, ghd_kv4_pool_bytes(ctx, kv)), dtype=torch.uint8, device=ctx.device)
+
+
+def _kv4_args(ctx: Ctx, kv: Kv4Cache, rows: Kv4Rows, pool):
+    if rows.row_start.numel() < kv.c.n_seqs + 1:
+        raise GhdError(1, "kv4: row_start has fewer than n_seqs + 1 entries")
+    return _need(pool, torch.uint8, "pool", ghd_kv4_pool_bytes(ctx, kv))
+
+
+def _kv4_strided(ctx: Ctx, t, n: int, width: int, what: str):
+    """Rows of `width` elements, contiguous inside a row -> (pointer, row stride)."""
+    if t.dtype != ctx.cfg.torch_dtype or not t.is_cuda or t.dim() != 2 or t.shape[0] < n or t.shape[1] != width or t.stride(1) != 1:
+        raise GhdError(1, f"{what}: want {ctx.cfg.torch_dtype} [{n}][{width}] with contiguous rows, got {tuple(t.shape)} {t.dtype}")
+    return t.data_ptr(), t.stride(0)
+
+
+def ghd_kv4_append(ctx: Ctx, kv: Kv4Cache, rows: Kv4Rows, pool, q, k, v, q_out=None):
+    """Rotates q and k, quantises k and v into the pool behind each sequence's cache rows.  q, k, v: [n_rows][heads * d_head], rows may
+    be strided (column blocks of one projection); q None: keys and values only.  -> rotated queries (q_out)."""
+    n, d = rows.n_rows, ctx.cfg.c.d_head
+    at = _kv4_args(ctx, kv, rows, pool)
+    kp, kld = _kv4_strided(ctx, k, n, kv.c.n_kv_heads * d, "k")
+    vp, vld = _kv4_strided(ctx, v, n, kv.c.n_kv_heads * d, "v")
+    if kld != vld:
+        raise GhdError(1, "kv4_append: k and v have different row strides")
+    qp, qld, op = None, 0, None
+    if q is not None:
+        qp, qld = _kv4_strided(ctx, q, n, ctx.cfg.c.n_heads * d, "q")
+        if q_out is None:
+            q_out = torch.empty((n, ctx.cfg.c.n_heads * d), dtype=ctx.cfg.torch_dtype, device=ctx.device)
+        op = _need(q_out, ctx.cfg.torch_dtype, "q_out", n * ctx.cfg.c.n_heads * d)
+    ctx._check(ctx.lib.ghd_kv4_append(ctx.handle, C.byref(kv.c), C.byref(rows.c), at, qp, qld, kp, vp, kld, op))
+    return q_out
+
+
+def ghd_kv4_attention(ctx: Ctx, kv: Kv4Cache, rows: Kv4Rows, pool, q, out=None):
+    """Attention of the new rows (rotated queries q [n_rows][n_heads * d_head]) over the paged 4-bit cache."""
+    numel = rows.n_rows * ctx.cfg.c.n_heads * ctx.cfg.c.d_head
+    at = _kv4_args(ctx, kv, rows, pool)
+    qp = _need(q, ctx.cfg.torch_dtype, "q", numel)
+    out = torch.zeros_like(q) if out is None else out
+    ctx._check(ctx.lib.ghd_kv4_attention(ctx.handle, C.byref(kv.c), C.byref(rows.c), at, qp, _need(out, ctx.cfg.torch_dtype, "out", numel)))
+    return out
+
+
+def ghd_kv4_read(ctx: Ctx, kv: Kv4Cache, pool, row_start, n_rows: int, first=None, k_out=None, v_out=None):
+    """Cache rows first[s] + i (first None: the new rows' places) in the storage type -> (k, v) [n_rows][n_kv_heads * d_head]."""
+    rows = Kv4Rows(row_start, n_rows)
+    at = _kv4_args(ctx, kv, rows, pool)
+    shape = (rows.n_rows, kv.c.n_kv_heads * ctx.cfg.c.d_head)
+    k_out = torch.empty(shape, dtype=ctx.cfg.torch_dtype, device=ctx.device) if k_out is None else k_out
+    v_out = torch.empty(shape, dtype=ctx.cfg.torch_dtype, device=ctx.device) if v_out is None else v_out
+    ctx._check(ctx.lib.ghd_kv4_read(ctx.handle, C.byref(kv.c), C.byref(rows.c), at, None if first is None else _need(first, torch.int32, "first", kv.c.n_seqs),
+                                    _need(k_out, ctx.cfg.torch_dtype, "k_out", shape[0] * shape[1]), _need(v_out, ctx.cfg.torch_dtype, "v_out", shape[0] * shape[1])))
+    return k_out, v_out
+
+
+def ghd_kv4_commit(ctx: Ctx, kv: Kv4Cache, rows: Kv4Rows, pools, results=None):
+    """Keeps the accepted rows of every sequence in all pools (a list, or one tensor [n_layers][...]) and advances kv.kv_len.
+    results: int32 [n_seqs][514] as ghd_accept writes them; None keeps every new row (pools are not touched)."""
+    ptrs = [] if results is None else [_kv4_args(ctx, kv, rows, p) for p in pools]
+    arr = (C.c_void_p * max(len(ptrs), 1))(*ptrs)
+    ctx._check(ctx.lib.ghd_kv4_commit(ctx.handle, C.byref(kv.c), C.byref(rows.c), arr, len(ptrs),
+                                      None if results is None else _need(results, torch.int32, "results", kv.c.n_seqs * (2 + 2 * GHD_MAX_NODES))))
 
 
 def ghd_linear(ctx: Ctx, x, w, y=None):

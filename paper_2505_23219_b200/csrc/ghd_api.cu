@@ -40,12 +40,12 @@ size_t carve_workspace(ghd_ctx* c, char* base) {
     return off;
 }
 
-static ghd_status fail(ghd_ctx* c, ghd_status s, const char* what) {
+ghd_status fail(ghd_ctx* c, ghd_status s, const char* what) {
     if (c) snprintf(c->err, sizeof(c->err), "%s", what);
     return s;
 }
 
-static ghd_status check_cuda(ghd_ctx* c, const char* where) {
+ghd_status check_cuda(ghd_ctx* c, const char* where) {
     const cudaError_t e = cudaGetLastError();
     if (e == cudaSuccess) return GHD_OK;
     snprintf(c->err, sizeof(c->err), "%s: %s", where, cudaGetErrorString(e));
@@ -597,6 +597,12 @@ ghd_status ghd_sync_status(ghd_ctx* c) {
         snprintf(c->err, sizeof(c->err), "the cache length on the device left [0, max_kv_len - n]");
         cudaMemset(c->status, 0, sizeof(int));
         return GHD_ENOSPACE;
+    }
+    if (st == DEV_KV4_ROWS || st == DEV_KV4_PAGE) {
+        snprintf(c->err, sizeof(c->err), st == DEV_KV4_ROWS ? "paged cache: a row beyond the page table, or a length or row start out of order"
+                                                            : "paged cache: a page id outside the pool");
+        cudaMemset(c->status, 0, sizeof(int));
+        return st == DEV_KV4_ROWS ? GHD_ENOSPACE : GHD_EINVAL;
     }
     if (st != DEV_OK) {
         snprintf(c->err, sizeof(c->err), "device wait expired (code %d)", st);

@@ -15,7 +15,7 @@
 namespace ghd {
 
 // Device status word values (first failure wins).
-enum : int { DEV_OK = 0, DEV_TIMEOUT_TMA = 1, DEV_TIMEOUT_MMA = 2, DEV_TIMEOUT_EPI = 3, DEV_TIMEOUT_TMEM = 4, DEV_TIMEOUT_GRID = 5, DEV_KV_RANGE = 6 };
+enum : int { DEV_OK = 0, DEV_TIMEOUT_TMA = 1, DEV_TIMEOUT_MMA = 2, DEV_TIMEOUT_EPI = 3, DEV_TIMEOUT_TMEM = 4, DEV_TIMEOUT_GRID = 5, DEV_KV_RANGE = 6, DEV_KV4_ROWS = 7, DEV_KV4_PAGE = 8 };
 
 // Epilogues of the projection GEMMs.
 enum Epilogue : int {
@@ -173,6 +173,8 @@ inline cudaError_t launch_k(ghd_ctx* c, bool pdl, void (*kernel)(KArgs...), dim3
     return launch_kc(c, pdl, 1, kernel, grid, block, smem, std::forward<Args>(args)...);
 }
 
+ghd_status fail(ghd_ctx* c, ghd_status s, const char* what);      // keeps the message for ghd_last_error
+ghd_status check_cuda(ghd_ctx* c, const char* where);             // status of the launches so far
 size_t carve_workspace(ghd_ctx* c, char* base);   // returns bytes needed; assigns pointers when base != nullptr
 
 // kernels_small.cu

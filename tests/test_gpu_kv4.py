@@ -1,0 +1,566 @@
+"""The paged 4-bit cache on the GPU against the double-precision oracle (oracle/kv4.py)."""
+import numpy as np
+import pytest
+
+import workloads as wl
+from oracle import kv4 as okv4
+
+pytestmark = pytest.mark.gpu
+
+THETA = 10000.0
+
+
+@pytest.fixture(scope="module")
+def ghd():
+    import paper_2505_23219_b200 as g
+    return g
+
+
+def make_ctx(ghd, H, d, dtype, max_nodes=64):
+    return ghd.ghd_create(ghd.ModelCfg(H * d, H, d, 256, 100, 1, 512, max_nodes, dtype, 1e-6, THETA))
+
+
+def dev(a):
+    import torch
+    return torch.from_numpy(np.ascontiguousarray(a)).cuda()
+
+
+class Setup:
+    """A cache with random rows, pages in random order, every other byte of the pool random too (NaN scales among it)."""
+
+    def __init__(self, ghd, H, Hk, d, dtype, R, lens, cnt, seed, spare=3, behind=0, garbage=True):
+        r = np.random.RandomState(seed)
+        self.H, self.Hk, self.d, self.dtype, self.R = H, Hk, d, dtype, R
+        self.np_t = np.float16 if dtype == "f16" else np.float32
+        S = len(lens)
+        self.lens, self.cnt = list(lens), list(cnt)
+        self.start = np.concatenate(([0], np.cumsum(cnt))).astype(np.int32)
+        self.n, self.n_rows = int(self.start[-1]), int(self.start[-1]) + behind
+        need = [-(-(a + b) // R) for a, b in zip(lens, cnt)]
+        n_pages = sum(need) + spare
+        order = r.permutation(n_pages)
+        self.table = np.full((S, max(need) + 1), -7, np.int32)              # entries past a sequence's rows are not ids
+        at = 0
+        for s in range(S):
+            self.table[s, :need[s]] = order[at:at + need[s]]
+            at += need[s]
+        self.pool = okv4.Pool(n_pages, Hk, R, d, dtype)
+        if garbage:
+            self.pool.data[:] = r.randint(0, 256, self.pool.data.shape)
+        strong = np.exp(0.6 * r.randn(d))
+        for s in range(S):
+            for t in range(lens[s] + cnt[s]):
+                page, row = okv4.slots(self.table, R, s, t)
+                for h in range(Hk):
+                    self.pool.put(0, page, row, h, *okv4.quantise((r.randn(d) * strong).astype(np.float32), dtype))
+                    self.pool.put(1, page, row, h, *okv4.quantise((r.randn(d) * 0.6 + 0.1).astype(np.float32), dtype))
+        self.r = r
+        self.ctx = make_ctx(ghd, H, d, dtype)
+        self.kv_len = dev(np.array(lens, np.int32))
+        self.kv = ghd.Kv4Cache(dev(self.table), self.kv_len, R, Hk, n_pages)
+        self.dpool = dev(self.pool.data.reshape(-1))
+        assert ghd.ghd_kv4_pool_bytes(self.ctx, self.kv) == self.pool.data.size
+
+    def trees(self, words=None):
+        vis = []
+        W = words or (max(max(self.cnt), 1) + 63) // 64
+        mask = np.zeros((max(self.n_rows, 1), W * 64), np.uint8)
+        for s, n in enumerate(self.cnt):
+            v = np.eye(n, dtype=bool)
+            for i in range(1, n):
+                v[i] |= v[self.r.randint(max(0, i - 7), i)]
+            vis.append(v)
+            mask[self.start[s]:self.start[s] + n, :n] = v
+        return vis, np.packbits(mask, axis=1, bitorder="little").view(np.int64).reshape(len(mask), W)
+
+
+def attention_tolerance(su, q):
+    """Absolute bound per output element, from the arithmetic (nothing measured).
+    Scores: q . c is summed in 32 bits over d products of |q_i| and at most 8, each of up to d additions off by 2^-23 of
+    the running sum (the tensor cores may truncate); scaled by scale / sqrt d; the minimum's term by 2^-22.  A score off by
+    e moves a weight by a factor 1 +- 2 e, hence the output by at most 4 e max |v|.  exp2 and the 32-bit weights: 2^-20.
+    Values: the weight times scale is rounded to half (2^-11, plus 2^-25 below the normal range) in f16, to 24 bits in
+    f32, and meets codes of at most 8; the sums run over L keys in 32 bits.  Output: half a step of its type."""
+    f16 = su.dtype == "f16"
+    K, V = su.pool_values
+    d, L = su.d, max(a + b for a, b in zip(su.lens, su.cnt))
+    par = np.array([np.abs(x).max() for x in (K, V)])
+    qsum = np.abs(q.astype(np.float64)).sum(-1).max()
+    s_k, s_v, m_k = su.max_scale[0], su.max_scale[1], par[0]
+    e = (d * 2.0 ** -23 * 8 * s_k * qsum + 2.0 ** -22 * 2 * m_k * qsum) / np.sqrt(d) + 2.0 ** -20
+    e += 2.0 ** -23 * 16 * par[0] * qsum / np.sqrt(d) if not f16 else 0.0            # q in three terms: 2^-24 each
+    w = 2.0 ** -11 if f16 else 2.0 ** -23
+    a = 8 * s_v * (w + L * 2.0 ** -23) + (8 * 2.0 ** -25 * L if f16 else 0.0) + 4 * e * par[1] + L * 2.0 ** -23 * par[1]
+    return lambda want: a + (2.0 ** -11 if f16 else 2.0 ** -23) * np.abs(want)
+
+
+def collect(su):
+    """Largest scales and all finite values of the sequences' rows, for the tolerance."""
+    K, V, sc = [], [], np.zeros(2)
+    for s in range(len(su.lens)):
+        k, v = okv4.rows(su.pool, su.table, s, 0, su.lens[s] + su.cnt[s])
+        K.append(k.reshape(-1)), V.append(v.reshape(-1))
+        for t in range(su.lens[s] + su.cnt[s]):
+            page, row = okv4.slots(su.table, su.R, s, t)
+            for w in (0, 1):
+                for h in range(su.Hk):
+                    x = float(su.pool.params(w, page, row, h)[0])
+                    sc[w] = max(sc[w], x) if np.isfinite(x) else sc[w]
+    K, V = np.concatenate(K), np.concatenate(V)
+    su.pool_values = (K[np.isfinite(K)], V[np.isfinite(V)])
+    su.max_scale = sc
+
+
+def run_attention(ghd, su, vis, words, want_status=True):
+    import torch
+    q = su.r.randn(su.n_rows, su.H, su.d).astype(su.np_t)
+    rows = ghd.Kv4Rows(dev(su.start), su.n_rows, mask=None if words is None else dev(words))
+    out = torch.full((su.n_rows, su.H * su.d), 7.0, dtype=su.ctx.cfg.torch_dtype, device="cuda")
+    ghd.ghd_kv4_attention(su.ctx, su.kv, rows, su.dpool, dev(q.reshape(su.n_rows, -1)), out=out)
+    if want_status:
+        ghd.ghd_sync_status(su.ctx)
+    got = out.float().cpu().numpy().astype(np.float64).reshape(su.n_rows, su.H, su.d)
+    assert (got[su.n:] == 7.0).all()                                      # rows behind the last sequence
+    want = okv4.attention(su.pool, su.table, su.lens, su.start, vis, q[: su.n])
+    return q, got[: su.n], want
+
+
+def check_attention(ghd, su, vis, words):
+    collect(su)
+    q, got, want = run_attention(ghd, su, vis, words)
+    tol = attention_tolerance(su, q)(want)
+    assert np.isfinite(got).all()
+    assert (np.abs(got - want) <= tol).all(), float((np.abs(got - want) / tol).max())
+
+
+CASES = [
+    # heads, kv heads, d, type, page rows, lengths, new rows
+    (4, 4, 128, "f16", 64, [130], [1]),
+    (4, 4, 128, "f16", 16, [0], [1]),
+    (4, 4, 128, "f16", 32, [63, 64, 65, 0], [1, 1, 1, 1]),
+    (8, 2, 128, "f16", 16, [200, 0, 17], [3, 0, 9]),
+    (7, 1, 64, "f16", 128, [255, 1], [5, 2]),
+    (4, 4, 64, "f16", 16, [90], [70]),
+    (4, 4, 128, "f16", 128, [300, 10], [33, 64]),
+    (4, 4, 128, "f16", 64, [40], [200]),
+    (4, 4, 64, "f32", 32, [129, 0, 3], [7, 5, 1]),
+    (6, 2, 128, "f32", 16, [50], [11]),
+    (4, 1, 128, "f16", 16, [700], [1]),
+]
+
+
+@pytest.mark.parametrize("tree", [True, False], ids=["tree", "causal"])
+@pytest.mark.parametrize("H,Hk,d,dtype,R,lens,cnt", CASES)
+def test_attention_against_the_oracle(ghd, H, Hk, d, dtype, R, lens, cnt, tree):
+    su = Setup(ghd, H, Hk, d, dtype, R, lens, cnt, 17 * H + R + len(lens), behind=2)
+    if tree:
+        vis, words = su.trees()
+    else:
+        vis, words = [np.ones((n, n), bool) for n in cnt], None
+    check_attention(ghd, su, vis, words)
+
+
+@pytest.mark.parametrize("dtype", ["f16", "f32"])
+def test_rows_that_see_nothing_get_zeros_and_bits_above_the_diagonal_count_for_nothing(ghd, dtype):
+    su = Setup(ghd, 4, 2, 64, dtype, 16, [0, 20], [6, 6], 5)
+    vis, words = su.trees()
+    words[2] = 0                                                          # row 2 of the first sequence: no cache, no node
+    words[4] |= 1 << 5                                                    # a later node
+    words[8] = 0                                                          # second sequence: only the cache is left
+    vis[0][2] = False
+    vis[1][2] = False
+    collect(su)
+    q, got, want = run_attention(ghd, su, vis, words)
+    assert (got[2] == 0).all() and (want[2] == 0).all()
+    assert (np.abs(got - want) <= attention_tolerance(su, q)(want)).all()
+
+
+@pytest.mark.parametrize("dtype", ["f16", "f32"])
+def test_nan_and_infinity_reach_only_the_rows_that_see_them(ghd, dtype):
+    """Node 1 of a tree has a NaN key row and node 2 an infinite value row; node 3 sees neither, 4 sees 1, 5 sees 2.
+    A query of NaN touches its own row alone.  What lies past the sequence's rows is random bytes."""
+    su = Setup(ghd, 4, 2, 128, dtype, 32, [37], [6], 9)
+    vis = [np.eye(6, dtype=bool)]
+    vis[0][:, 0] = True
+    vis[0][4, 1] = vis[0][5, 2] = True
+    mask = np.zeros((6, 64), np.uint8)
+    mask[:, :6] = vis[0]
+    words = np.packbits(mask, axis=1, bitorder="little").view(np.int64)
+    for node, which in ((1, 0), (2, 1)):
+        page, row = okv4.slots(su.table, su.R, 0, 37 + node)
+        for h in range(2):
+            su.pool.put(which, page, row, h, su.pool.codes(which, page, row, h), np.nan if which == 0 else np.inf, 0.5)
+    su.dpool.copy_(dev(su.pool.data.reshape(-1)))
+    collect(su)
+    with np.errstate(all="ignore"):
+        q, got, want = run_attention(ghd, su, vis, words)
+    bad = np.array([False, True, True, False, True, True])
+    assert np.isfinite(got[~bad]).all() and np.isnan(got[[1, 4]]).all() and (~np.isfinite(got[[2, 5]])).any(-1).all()
+    tol = attention_tolerance(su, q)
+    assert (np.abs(got - want)[~bad] <= tol(want)[~bad]).all()
+
+
+def test_a_nan_query_stays_in_its_row(ghd):
+    import torch
+    su = Setup(ghd, 4, 4, 128, "f16", 64, [100], [5], 10)
+    vis, words = su.trees()
+    collect(su)
+    q = su.r.randn(5, 4, 128).astype(np.float16)
+    q[3, 1, 17] = np.nan
+    out = ghd.ghd_kv4_attention(su.ctx, su.kv, ghd.Kv4Rows(dev(su.start), 5, mask=dev(words)), su.dpool, dev(q.reshape(5, -1)))
+    ghd.ghd_sync_status(su.ctx)
+    got = out.float().cpu().numpy().reshape(5, 4, 128)
+    assert np.isnan(got[3, 1]).all()
+    got[3, 1] = 0
+    q[3, 1] = 0
+    want = okv4.attention(su.pool, su.table, su.lens, su.start, vis, q)
+    want[3, 1] = 0
+    assert (np.abs(got - want) <= attention_tolerance(su, q)(want)).all()
+    assert torch.isfinite(torch.from_numpy(got)).all()
+
+
+def test_extreme_scales_of_values_and_scores(ghd):
+    """Values near the largest half, and scores that grow along the cache (the reference has to follow)."""
+    su = Setup(ghd, 2, 2, 128, "f16", 16, [150], [2], 11, garbage=False)
+    for t in range(152):
+        page, row = okv4.slots(su.table, 16, 0, t)
+        for h in range(2):
+            su.pool.put(1, page, row, h, su.pool.codes(1, page, row, h), 8000.0, -60000.0)
+            x = np.full(128, 0.02 * t, np.float32)
+            x[::2] += 0.5
+            su.pool.put(0, page, row, h, *okv4.quantise(x, "f16"))
+    su.dpool.copy_(dev(su.pool.data.reshape(-1)))
+    collect(su)
+    vis = [np.ones((2, 2), bool)]
+    q = np.abs(su.r.randn(2, 2, 128)).astype(np.float16)
+    out = ghd.ghd_kv4_attention(su.ctx, su.kv, ghd.Kv4Rows(dev(su.start), 2), su.dpool, dev(q.reshape(2, -1)))
+    ghd.ghd_sync_status(su.ctx)
+    got = out.double().cpu().numpy().reshape(2, 2, 128)
+    want = okv4.attention(su.pool, su.table, su.lens, su.start, vis, q)
+    tol = np.minimum(attention_tolerance(su, q)(want), 400.0)
+    assert np.isfinite(got).all() and (np.abs(got - want) <= tol).all()
+
+
+def test_the_same_call_gives_the_same_bits_and_leaves_its_scratch_clean(ghd):
+    su = Setup(ghd, 4, 4, 128, "f16", 64, [1500, 10], [9, 3], 12)
+    vis, words = su.trees()
+    q = dev(su.r.randn(12, 4 * 128).astype(np.float16))
+    rows = ghd.Kv4Rows(dev(su.start), 12, mask=dev(words))
+    first = ghd.ghd_kv4_attention(su.ctx, su.kv, rows, su.dpool, q).clone()
+    for _ in range(20):
+        assert bool((ghd.ghd_kv4_attention(su.ctx, su.kv, rows, su.dpool, q) == first).all())
+    ghd.ghd_sync_status(su.ctx)
+
+
+@pytest.mark.parametrize("H,Hk,d,dtype,R,lens,cnt", [
+    (4, 4, 128, "f16", 64, [130], [1]),
+    (8, 2, 128, "f16", 16, [0, 13, 40], [20, 0, 7]),
+    (4, 4, 64, "f16", 32, [31, 5], [2, 40]),
+    (4, 2, 64, "f32", 16, [0, 100000 % 97], [33, 3]),
+    (2, 2, 128, "f32", 128, [127], [130]),
+])
+@pytest.mark.parametrize("with_pos", [True, False], ids=["pos", "slots"])
+def test_append_and_read_back(ghd, H, Hk, d, dtype, R, lens, cnt, with_pos):
+    import torch
+    su = Setup(ghd, H, Hk, d, dtype, R, lens, cnt, 23 + H + R, behind=2)
+    n = su.n_rows
+    pos = su.r.randint(0, 200000, n).astype(np.int32) if with_pos else None
+    # q, k and v side by side in one buffer
+    qkv = su.r.randn(n, (H + 2 * Hk) * d).astype(su.np_t)
+    qkv[0, H * d: H * d + d] = 0.25                                          # a constant row: scale 0 after position 0, else a rotated one
+    x = dev(qkv)
+    q, k, v = x.split((H * d, Hk * d, Hk * d), 1)
+    before = su.dpool.clone()
+    q_out = torch.full((n, H * d), 9.0, dtype=x.dtype, device="cuda")
+    rows = ghd.Kv4Rows(dev(su.start), n, pos=None if pos is None else dev(pos))
+    ghd.ghd_kv4_append(su.ctx, su.kv, rows, su.dpool, q, k, v, q_out=q_out)
+    ghd.ghd_sync_status(su.ctx)
+    a = qkv[: su.n].reshape(su.n, H + 2 * Hk, d)
+    want_q = okv4.append(su.pool, su.table, su.lens, su.start, pos, a[:, :H], a[:, H:H + Hk], a[:, H + Hk:], THETA)
+    got_q = q_out.double().cpu().numpy().reshape(n, H, d)
+    assert (got_q[su.n:] == 9.0).all()
+    # rotated in 32 bits (angle's cosine and sine rounded, two products, one sum: 2^-22 of |a| + |b|), then rounded once
+    amp = np.abs(a[:, :H].astype(np.float64))
+    amp = amp + np.concatenate([amp[..., d // 2:], amp[..., : d // 2]], -1)
+    half = 2.0 ** -11 if dtype == "f16" else 2.0 ** -24
+    assert (np.abs(got_q[: su.n] - want_q) <= half * np.abs(want_q) + 2.0 ** -22 * amp + (2.0 ** -25 if dtype == "f16" else 0)).all()
+    # codes, scales and minima bit for bit, and not one other byte of the pool
+    assert np.array_equal(su.dpool.cpu().numpy(), su.pool.data.reshape(-1))
+    assert before.numel() == su.dpool.numel() and int(su.kv_len[0]) == lens[0]
+    # read back
+    kb, vb = ghd.ghd_kv4_read(su.ctx, su.kv, su.dpool, dev(su.start), n)
+    ghd.ghd_sync_status(su.ctx)
+    for w, got in ((0, kb), (1, vb)):
+        got = got.double().cpu().numpy()[: su.n].reshape(su.n, Hk, d)
+        want = np.concatenate([okv4.rows(su.pool, su.table, s, lens[s], cnt[s])[w] for s in range(len(lens))])
+        # one fused 32-bit operation, then the rounding to T
+        assert (np.abs(got - want) <= (half + 2.0 ** -24) * np.abs(want) + 2.0 ** -25).all()
+
+
+def test_append_of_keys_and_values_alone_and_in_place_queries(ghd):
+    su = Setup(ghd, 4, 4, 128, "f16", 16, [5], [9], 31)
+    k, v, q = (su.r.randn(9, 4 * 128).astype(np.float16) for _ in range(3))
+    rows = ghd.Kv4Rows(dev(su.start), 9)
+    assert ghd.ghd_kv4_append(su.ctx, su.kv, rows, su.dpool, None, dev(k), dev(v)) is None
+    r = lambda a: a.reshape(9, 4, 128)  # noqa: E731
+    want = okv4.append(su.pool, su.table, su.lens, su.start, None, r(q), r(k), r(v), THETA)
+    assert np.array_equal(su.dpool.cpu().numpy(), su.pool.data.reshape(-1))
+    qd = dev(q)
+    other = ghd.ghd_kv4_append(su.ctx, su.kv, rows, su.dpool, qd.clone(), dev(k), dev(v))
+    ghd.ghd_kv4_append(su.ctx, su.kv, rows, su.dpool, qd, dev(k), dev(v), q_out=qd)
+    assert bool((other == qd).all())
+    assert np.abs(qd.double().cpu().numpy().reshape(9, 4, 128) - want).max() <= 2.0 ** -11 * np.abs(want).max() + 2.0 ** -20 * 8
+    ghd.ghd_sync_status(su.ctx)
+
+
+@pytest.mark.parametrize("dtype", ["f16", "f32"])
+def test_append_of_rows_that_are_not_finite_reads_back_as_nan(ghd, dtype):
+    su = Setup(ghd, 2, 2, 64, dtype, 16, [3], [4], 33)
+    k, v, q = (su.r.randn(4, 2 * 64).astype(su.np_t) for _ in range(3))
+    v[0, 5], v[1, 70], v[2, 3], k[3, 9] = np.nan, np.inf, -np.inf, np.nan
+    rows = ghd.Kv4Rows(dev(su.start), 4)
+    ghd.ghd_kv4_append(su.ctx, su.kv, rows, su.dpool, dev(q), dev(k), dev(v))
+    kb, vb = (x.float().cpu().numpy().reshape(4, 2, 64) for x in ghd.ghd_kv4_read(su.ctx, su.kv, su.dpool, dev(su.start), 4))
+    ghd.ghd_sync_status(su.ctx)
+    bad_v = np.array([[1, 0], [0, 1], [1, 0], [0, 0]], bool)
+    bad_k = np.array([[0, 0], [0, 0], [0, 0], [1, 0]], bool)
+    assert np.isnan(vb[bad_v]).all() and np.isfinite(vb[~bad_v]).all()
+    assert np.isnan(kb[bad_k]).all() and np.isfinite(kb[~bad_k]).all()
+
+
+@pytest.mark.parametrize("dtype,d,R", [("f16", 128, 16), ("f16", 64, 64), ("f32", 64, 16), ("f32", 128, 32)])
+def test_commit_moves_the_accepted_rows(ghd, dtype, d, R):
+    import torch
+    lens, cnt = [30, 0, 5, 64], [12, 9, 0, 40]
+    su = Setup(ghd, 4, 2, d, dtype, R, lens, cnt, 41)
+    pools = torch.stack([su.dpool, torch.from_numpy(su.r.randint(0, 256, su.dpool.numel()).astype(np.uint8)).cuda()])
+    host = [okv4.Pool(su.pool.data.shape[0], 2, R, d, dtype, data=p.cpu().numpy().reshape(su.pool.data.shape)) for p in pools]
+    paths = [(3, [0, 1, 4, 11]), (0, [0]), (0, [0]), (5, [0, 2, 3, 9, 20, 39])]
+    res = np.zeros((4, 514), np.int32)
+    for s, (m, nodes) in enumerate(paths):
+        res[s, 0], res[s, 1], res[s, 2:3 + m] = m, m + 1, nodes
+    rows = ghd.Kv4Rows(dev(su.start), su.n)
+    ghd.ghd_kv4_commit(su.ctx, su.kv, rows, pools, dev(res))
+    ghd.ghd_sync_status(su.ctx)
+    new = okv4.commit(host, su.table, lens, su.start, paths)
+    assert su.kv_len.cpu().tolist() == new == [34, 1, 5, 70]
+    assert np.array_equal(pools.cpu().numpy(), np.stack([h.data.reshape(-1) for h in host]))
+    ghd.ghd_kv4_commit(su.ctx, su.kv, ghd.Kv4Rows(dev(np.array([0, 1, 3, 3, 4], np.int32)), 4), None)     # a prompt: all rows stay
+    assert su.kv_len.cpu().tolist() == [35, 3, 5, 71]
+    ghd.ghd_sync_status(su.ctx)
+
+
+def test_pages_behind_four_gigabytes(ghd):
+    """Page ids whose byte offsets pass 32 bits (signed and unsigned)."""
+    import torch
+    H, d, R = 32, 128, 128
+    ctx = make_ctx(ghd, H, d, "f16")
+    page_bytes = H * okv4.block_bytes(R, d, "f16")
+    n_pages = (1 << 32) // page_bytes + 40
+    pool = torch.zeros(n_pages * page_bytes, dtype=torch.uint8, device="cuda")
+    ids = [n_pages - 1, (1 << 31) // page_bytes + 1, 3]
+    kv = ghd.Kv4Cache(dev(np.array([ids], np.int32)), dev(np.array([0], np.int32)), R, H, n_pages)
+    small = torch.zeros(3 * page_bytes, dtype=torch.uint8, device="cuda")
+    kv2 = ghd.Kv4Cache(dev(np.array([[1, 0, 2]], np.int32)), dev(np.array([0], np.int32)), R, H, 3)
+    r = np.random.RandomState(3)
+    n = 300
+    q, k, v = (dev(r.randn(n, H * d).astype(np.float16)) for _ in range(3))
+    rows = ghd.Kv4Rows(dev(np.array([0, n], np.int32)), n)
+    outs = []
+    for c, p in ((kv, pool), (kv2, small)):
+        qr = ghd.ghd_kv4_append(ctx, c, rows, p, q, k, v)
+        ghd.ghd_kv4_commit(ctx, c, rows, None)
+        one = ghd.Kv4Rows(dev(np.array([0, 0], np.int32)), 0)
+        assert one.n_rows == 0
+        c.kv_len.sub_(5)
+        last = ghd.Kv4Rows(dev(np.array([0, 5], np.int32)), 5)
+        outs.append([ghd.ghd_kv4_attention(ctx, c, last, p, qr[-5:].contiguous()), *ghd.ghd_kv4_read(ctx, c, p, dev(np.array([0, n], np.int32)), n, first=dev(np.array([0], np.int32)))])
+    ghd.ghd_sync_status(ctx)
+    for a, b in zip(*outs):
+        assert bool((a == b).all()) and float(a.abs().max()) > 0
+
+
+def test_bad_pages_and_rows_are_skipped_and_reported(ghd):
+    import torch
+    su = Setup(ghd, 4, 4, 64, "f16", 16, [40, 20], [2, 2], 51, garbage=False)
+    rows = ghd.Kv4Rows(dev(su.start), 4)
+    q = dev(su.r.randn(4, 256).astype(np.float16))
+    k = dev(su.r.randn(4, 256).astype(np.float16))
+    good = ghd.ghd_kv4_attention(su.ctx, su.kv, rows, su.dpool, q).clone()
+    ghd.ghd_sync_status(su.ctx)
+    for bad in (-1, su.kv.c.n_pages, 2**31 - 1):
+        su.kv.page_table[0, 1] = bad
+        out = ghd.ghd_kv4_attention(su.ctx, su.kv, rows, su.dpool, q)
+        with pytest.raises(ghd.GhdError) as e:
+            ghd.ghd_sync_status(su.ctx)
+        assert e.value.name == "GHD_EINVAL" and "page id" in str(e.value)
+        assert bool(torch.isfinite(out).all()) and bool((out[2:] == good[2:]).all())
+        ghd.ghd_sync_status(su.ctx)                                       # reported once
+    su.kv.page_table[0, 1] = int(su.table[0, 1])
+    su.kv.page_table[1, 1] = -3                                           # where the second sequence's new rows go
+    before = su.dpool.clone()
+    ghd.ghd_kv4_append(su.ctx, su.kv, ghd.Kv4Rows(dev(np.array([0, 0, 4], np.int32)), 4), su.dpool, None, k, k)
+    with pytest.raises(ghd.GhdError):
+        ghd.ghd_sync_status(su.ctx)
+    assert bool((su.dpool == before).all())
+    su.kv.page_table[1, 1] = int(su.table[1, 1])
+    for bad_len in (-4, 16 * su.table.shape[1] - 1, 2**31 - 1):             # no room for two rows
+        su.kv_len[0] = bad_len
+        for call in (lambda: ghd.ghd_kv4_attention(su.ctx, su.kv, rows, su.dpool, q), lambda: ghd.ghd_kv4_append(su.ctx, su.kv, rows, su.dpool, q, k, k),
+                     lambda: ghd.ghd_kv4_commit(su.ctx, su.kv, rows, None)):
+            su.kv_len[0] = bad_len
+            call()
+            with pytest.raises(ghd.GhdError) as e:
+                ghd.ghd_sync_status(su.ctx)
+            assert e.value.name in ("GHD_ENOSPACE", "GHD_EINVAL")
+    su.kv_len.copy_(dev(np.array([40, 20], np.int32)))
+    with pytest.raises(ghd.GhdError):
+        ghd.ghd_kv4_read(su.ctx, su.kv, su.dpool, dev(su.start), 4, first=dev(np.array([0, 10**6], np.int32)))
+        ghd.ghd_sync_status(su.ctx)
+
+
+def test_refusals(ghd):
+    import torch
+    su = Setup(ghd, 4, 4, 64, "f16", 16, [4], [2], 61)
+    rows = ghd.Kv4Rows(dev(su.start), 2)
+    h = lambda *s: torch.zeros(s, dtype=torch.float16, device="cuda")  # noqa: E731
+    good = (su.kv.page_table, su.kv_len)
+
+    def refused(name, fn):
+        launches = ghd.ghd_launch_count(su.ctx)
+        with pytest.raises(ghd.GhdError) as e:
+            fn()
+        assert e.value.name == name
+        assert ghd.ghd_launch_count(su.ctx) == launches
+
+    att = lambda kv, rows_=rows, q=None: ghd.ghd_kv4_attention(su.ctx, kv, rows_, torch.zeros(1 << 20, dtype=torch.uint8, device="cuda"), h(2, 256) if q is None else q)  # noqa: E731
+    refused("GHD_EINVAL", lambda: att(ghd.Kv4Cache(*good, 24, 4, 4)))
+    refused("GHD_ESHAPE", lambda: att(ghd.Kv4Cache(*good, 16, 3, 4)))
+    refused("GHD_EINVAL", lambda: att(ghd.Kv4Cache(*good, 16, 4, 0)))
+    refused("GHD_EINVAL", lambda: att(su.kv, q=h(1, 256)))
+    refused("GHD_EINVAL", lambda: att(su.kv, q=torch.zeros(2, 256, device="cuda")))
+    refused("GHD_EINVAL", lambda: ghd.ghd_kv4_attention(su.ctx, su.kv, rows, su.dpool[1:], h(2, 256)))
+    refused("GHD_EINVAL", lambda: ghd.ghd_kv4_attention(su.ctx, su.kv, rows, su.dpool, h(3, 256).view(-1)[1:513].view(2, 256)))
+    refused("GHD_EINVAL", lambda: ghd.ghd_kv4_append(su.ctx, su.kv, rows, su.dpool, None, h(2, 256), h(2, 260)[:, :256]))
+    refused("GHD_EINVAL", lambda: ghd.ghd_kv4_append(su.ctx, su.kv, rows, su.dpool, h(2, 128), h(2, 256), h(2, 256)))
+    big = torch.zeros((1025, 1), dtype=torch.int32, device="cuda")
+    refused("GHD_EINVAL", lambda: ghd.ghd_kv4_attention(su.ctx, ghd.Kv4Cache(big, big.view(-1), 16, 4, 1), ghd.Kv4Rows(torch.zeros(1026, dtype=torch.int32, device="cuda"), 2),
+                                                        su.dpool, h(2, 256)))
+    refused("GHD_EINVAL", lambda: ghd.Kv4Rows(dev(su.start), 2, pos=torch.zeros(1, dtype=torch.int32, device="cuda")))
+    refused("GHD_EINVAL", lambda: ghd.Kv4Rows(dev(su.start), 2, mask=torch.zeros((1, 1), dtype=torch.int64, device="cuda")))
+    assert ghd.ghd_kv4_attention(su.ctx, su.kv, ghd.Kv4Rows(dev(su.start), 0), su.dpool, h(2, 256)).abs().sum() == 0      # no rows: nothing to do
+    ghd.ghd_sync_status(su.ctx)
+
+
+def test_steps_captured_in_one_graph_on_a_stream_of_their_own(ghd):
+    """append -> attention -> accept's result -> commit, three steps recorded once and replayed twice, against the same
+    steps called one by one: lengths, pools and outputs equal to the bit."""
+    import torch
+    H, Hk, d, R, S, n = 4, 2, 128, 16, 3, 9
+    r = np.random.RandomState(71)
+    stream = torch.cuda.Stream()
+    steps = 3
+    lens0 = np.array([0, 33, 200], np.int32)
+    paths = r.randint(1, 3, (steps, S))
+    res = np.zeros((steps, S, 514), np.int32)
+    for t in range(steps):
+        for s in range(S):
+            m = int(paths[t, s])
+            res[t, s, 0], res[t, s, 1] = m, m + 1
+            res[t, s, 3:3 + m] = np.sort(r.choice(np.arange(1, n), m, replace=False))
+    with torch.cuda.stream(stream):
+        ctx = make_ctx(ghd, H, d, "f16")
+        pages = 20
+        table = dev(np.arange(S * pages, dtype=np.int32).reshape(pages, S).T.copy())
+        kv_len = dev(lens0)
+        kv = ghd.Kv4Cache(table, kv_len, R, Hk, S * pages)
+        pool = ghd.ghd_kv4_pool(ctx, kv, 2)
+        rows = ghd.Kv4Rows(dev(np.arange(S + 1, dtype=np.int32) * n), S * n)
+        fill = ghd.Kv4Rows(dev(np.concatenate(([0], np.cumsum(lens0))).astype(np.int32)), int(lens0.sum()))
+        big = dev(r.randn(int(lens0.sum()), Hk * d).astype(np.float16))
+        kv_len.zero_()
+        for p in pool:
+            ghd.ghd_kv4_append(ctx, kv, fill, p, None, big, big)
+        ghd.ghd_kv4_commit(ctx, kv, fill, None)
+        assert kv_len.cpu().tolist() == lens0.tolist()
+        x = [[dev(r.randn(S * n, w * d).astype(np.float16)) for w in (H, Hk, Hk)] for _ in range(steps)]
+        resd = dev(res)
+        outs = torch.zeros((steps, 2, S * n, H * d), dtype=torch.float16, device="cuda")
+        qr = torch.zeros((S * n, H * d), dtype=torch.float16, device="cuda")
+        pool0 = pool.clone()
+
+        def go(t):
+            for l in range(2):
+                ghd.ghd_kv4_append(ctx, kv, rows, pool[l], *x[t], q_out=qr)
+                ghd.ghd_kv4_attention(ctx, kv, rows, pool[l], qr, out=outs[t, l])
+            ghd.ghd_kv4_commit(ctx, kv, rows, pool, resd[t])
+
+        for t in range(steps):
+            go(t)
+        ghd.ghd_sync_status(ctx)
+        want = (outs.clone(), pool.clone(), kv_len.clone())
+        assert want[2].cpu().tolist() == (lens0 + (paths + 1).sum(0)).tolist()
+        graph = torch.cuda.CUDAGraph()
+        kv_len.copy_(dev(lens0))
+        with torch.cuda.graph(graph, stream=stream):
+            for t in range(steps):
+                go(t)
+        for _ in range(2):
+            kv_len.copy_(dev(lens0))
+            pool.copy_(pool0)
+            outs.zero_()
+            graph.replay()
+            ghd.ghd_sync_status(ctx)
+            for a, b in zip((outs, pool, kv_len), want):
+                assert bool((a == b).all())
+
+
+def test_a_decode_loop_over_the_paged_cache_agrees_with_decoding_one_row_at_a_time(ghd):
+    """A chain of rows verified as one tree gives each row what decoding it alone gives (the same cache rows are read),
+    and the path accepted out of a branching tree leaves the cache that appending its rows in sequence leaves."""
+    import torch
+    H, Hk, d, R = 4, 2, 64, 16
+    ctx = make_ctx(ghd, H, d, "f32")
+    r = np.random.RandomState(81)
+    table = dev(np.array([[4, 2, 7, 0]], np.int32))
+    q, k, v = (dev(r.randn(30, w * d).astype(np.float32)) for w in (H, Hk, Hk))
+
+    def fresh():
+        kv = ghd.Kv4Cache(table, dev(np.array([0], np.int32)), R, Hk, 8)
+        return kv, ghd.ghd_kv4_pool(ctx, kv)
+
+    one_row = ghd.Kv4Rows(dev(np.array([0, 1], np.int32)), 1)
+    kv_a, pool_a = fresh()
+    alone = []
+    for i in range(30):
+        qr = ghd.ghd_kv4_append(ctx, kv_a, one_row, pool_a[0], q[i:i + 1], k[i:i + 1], v[i:i + 1])
+        alone.append(ghd.ghd_kv4_attention(ctx, kv_a, one_row, pool_a[0], qr))
+        ghd.ghd_kv4_commit(ctx, kv_a, one_row, None)
+    kv_b, pool_b = fresh()
+    rows = ghd.Kv4Rows(dev(np.array([0, 30], np.int32)), 30)
+    qr = ghd.ghd_kv4_append(ctx, kv_b, rows, pool_b[0], q, k, v)
+    chain = ghd.ghd_kv4_attention(ctx, kv_b, rows, pool_b[0], qr)
+    assert bool((pool_a == pool_b).all())
+    a, b = torch.cat(alone).double(), chain.double()
+    assert float((a - b).abs().max()) <= 2.0 ** -17 * float(a.abs().max())     # both within the bounds of the 32-bit sums
+    # tree: rows 0, 1, 2 are the accepted path at nodes 0, 3, 5; the others are alternatives
+    kv_c, pool_c = fresh()
+    pick = torch.tensor([0, 7, 8, 1, 9, 2], device="cuda")
+    pos = dev(np.array([0, 1, 1, 1, 2, 2], np.int32))
+    vis = np.eye(6, dtype=np.uint8)
+    vis[:, 0] = 1
+    vis[4, 1] = vis[5, 3] = 1
+    mask = np.zeros((6, 64), np.uint8)
+    mask[:, :6] = vis
+    rows = ghd.Kv4Rows(dev(np.array([0, 6], np.int32)), 6, pos=pos, mask=dev(np.packbits(mask, axis=1, bitorder="little").view(np.int64)))
+    qr = ghd.ghd_kv4_append(ctx, kv_c, rows, pool_c[0], q[pick], k[pick], v[pick])
+    out = ghd.ghd_kv4_attention(ctx, kv_c, rows, pool_c[0], qr)
+    assert float((out[[0, 3, 5]].double() - a[:3]).abs().max()) <= 2.0 ** -17 * float(a.abs().max())
+    res = np.zeros((1, 514), np.int32)
+    res[0, :5] = [2, 3, 0, 3, 5]
+    ghd.ghd_kv4_commit(ctx, kv_c, rows, pool_c, dev(res))
+    ghd.ghd_sync_status(ctx)
+    assert int(kv_c.kv_len[0]) == 3
+    three, first = dev(np.array([0, 3], np.int32)), dev(np.array([0], np.int32))
+    for x, y in zip(ghd.ghd_kv4_read(ctx, kv_c, pool_c[0], three, 3, first=first), ghd.ghd_kv4_read(ctx, kv_a, pool_a[0], three, 3, first=first)):
+        assert bool((x == y).all())
