@@ -16,7 +16,7 @@
 // an equal run of them (kv4_layout.h), so ragged batches and single long sequences fill the device alike.  An item cut by
 // a run's border leaves partial sums; the last of its CTAs to arrive adds them in CTA order (the result does not
 // depend on who was last).  Float contexts split q and p * scale into three bfloat16 terms (24 bits).
-#include "kv4.cuh"
+#include "attn_kv4_dev.cuh"
 
 #include <cuda_bf16.h>
 
@@ -27,26 +27,9 @@ namespace ghd {
 namespace {
 
 constexpr int WARPS = 4, CHUNK = 16 * WARPS;
-constexpr float LOG2E = 1.4426950408889634f;
 constexpr float RAISE = 2.f;
 
-struct Kv4AttnParams {
-    Kv4View w;
-    const uint8_t* pool;
-    const void* q;
-    void* out;
-    const uint64_t* mask;
-    int mask_words, q_heads, group, ctas;
-    float scale;                 // 1 / sqrt(d_head)
-    float* part;                 // [ctas][2] slots of [RT][D] sums, then [RT][2] (reference, sum of weights)
-    int* counters;               // [ctas], zero between launches
-};
-
-__device__ __forceinline__ float ex2(float x) {
-    float y;
-    asm("ex2.approx.ftz.f32 %0, %1;" : "=f"(y) : "f"(x));
-    return y;
-}
+using namespace kv4;
 
 // ---------------------------------------------------------------- operands of the two storage types
 template <typename T> struct Op;
@@ -57,13 +40,7 @@ template <> struct Op<__half> {
                      : "+f"(d[0]), "+f"(d[1]), "+f"(d[2]), "+f"(d[3]) : "r"(a0), "r"(a1), "r"(a2), "r"(a3), "r"(b0), "r"(b1));
     }
     // two codes (at bits SH .. SH + 3 of each half word) less 8
-    template <int SH> static __device__ __forceinline__ uint32_t centred(uint32_t w) {
-        constexpr uint32_t m = SH == 0 ? 0x000f000fu : 0x00f000f0u, e = SH == 0 ? 0x64006400u : 0x54005400u;   // 1024 + c, 64 + c
-        const uint32_t x = (w & m) | e;
-        const __half2 off = SH == 0 ? __floats2half2_rn(-1032.f, -1032.f) : __floats2half2_rn(-72.f, -72.f);
-        const __half2 r = __hadd2(*reinterpret_cast<const __half2*>(&x), off);
-        return *reinterpret_cast<const uint32_t*>(&r);
-    }
+    template <int SH> static __device__ __forceinline__ uint32_t centred(uint32_t w) { return centred_half<SH>(w); }
     // (a, b) as TERMS packed pairs whose sum is (a, b) to 11 bits
     static __device__ __forceinline__ void split(float a, float b, uint32_t (&t)[1]) {
         const __half2 h = __floats2half2_rn(a, b);
@@ -99,13 +76,6 @@ __device__ __forceinline__ uint32_t transpose8x8(uint32_t x) {
     return y;
 }
 
-template <typename T> __device__ __forceinline__ float2 load_params(const uint8_t* p);        // (scale, min)
-template <> __device__ __forceinline__ float2 load_params<__half>(const uint8_t* p) { return __half22float2(__ldg(reinterpret_cast<const __half2*>(p))); }
-template <> __device__ __forceinline__ float2 load_params<float>(const uint8_t* p) { return __ldg(reinterpret_cast<const float2*>(p)); }
-template <typename T> __device__ __forceinline__ float to_f(T v);
-template <> __device__ __forceinline__ float to_f<float>(float v) { return v; }
-template <> __device__ __forceinline__ float to_f<__half>(__half v) { return __half2float(v); }
-
 template <int N> struct Words { uint32_t w[N]; };
 template <int N> __device__ __forceinline__ Words<N> load_words(const uint8_t* p) {
     Words<N> r;
@@ -113,45 +83,6 @@ template <int N> __device__ __forceinline__ Words<N> load_words(const uint8_t* p
     else if constexpr (N == 2) { const uint2 v = __ldg(reinterpret_cast<const uint2*>(p)); r.w[0] = v.x; r.w[1] = v.y; }
     else r.w[0] = __ldg(reinterpret_cast<const uint32_t*>(p));
     return r;
-}
-
-template <typename T> __device__ __forceinline__ void store4(T* p, float a, float b, float c, float d);
-template <> __device__ __forceinline__ void store4<float>(float* p, float a, float b, float c, float d) { *reinterpret_cast<float4*>(p) = make_float4(a, b, c, d); }
-template <> __device__ __forceinline__ void store4<__half>(__half* p, float a, float b, float c, float d) {
-    const __half2 lo = __floats2half2_rn(a, b), hi = __floats2half2_rn(c, d);
-    *reinterpret_cast<uint2*>(p) = make_uint2(*reinterpret_cast<const uint32_t*>(&lo), *reinterpret_cast<const uint32_t*>(&hi));
-}
-
-// ---------------------------------------------------------------- the run of units of a CTA
-// Exclusive sums of the sequences' units in shared memory; -> all units.  Called by every thread of the block.
-__device__ __forceinline__ int64_t unit_sums(const Kv4View& w, const Kv4Tiling& t, int64_t* sums /* [n_seqs + 1] */, int64_t* scratch /* [32] */) {
-    const int nt = blockDim.x, each = (w.n_seqs + nt - 1) / nt, s0 = threadIdx.x * each;
-    int64_t mine = 0;
-    for (int s = s0; s < s0 + each && s < w.n_seqs; ++s) {
-        const Kv4Seq q = kv4_load_seq(w, s);
-        if (q.bad) atomicCAS(w.status, DEV_OK, DEV_KV4_ROWS);
-        const int64_t u = (int64_t)t.heads * kv4_head_units(t, q);
-        sums[s] = u;
-        mine += u;
-    }
-    const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
-    int64_t run = mine;
-    for (int o = 1; o < 32; o <<= 1) {
-        const int64_t v = __shfl_up_sync(0xffffffffu, run, o);
-        if (lane >= o) run += v;
-    }
-    if (lane == 31) scratch[warp] = run;
-    __syncthreads();
-    int64_t base = run - mine;
-    for (int i = 0; i < warp; ++i) base += scratch[i];
-    for (int s = s0; s < s0 + each && s < w.n_seqs; ++s) {
-        const int64_t u = sums[s];
-        sums[s] = base;
-        base += u;
-    }
-    if (s0 < w.n_seqs && s0 + each >= w.n_seqs) sums[w.n_seqs] = base;
-    __syncthreads();
-    return sums[w.n_seqs];
 }
 
 template <typename T, int D, int NT>
@@ -183,7 +114,7 @@ __global__ void __launch_bounds__(WARPS * 32, NT == 1 && sizeof(T) == 2 ? 4 : 2)
     const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5, g = lane >> 2, t = lane & 3;
     const int R = 1 << w.shift;
     constexpr int es = (int)sizeof(T);
-    const float sl2 = p.scale * LOG2E;
+    const float sl2 = p.scale * KV4_LOG2E;
 
     while (u < u_end) {
         const Kv4Item it = kv4_find_item(til, sums, w.n_seqs, [&](int s_) { return kv4_load_seq(w, s_); }, u, u_end);
@@ -290,12 +221,8 @@ __global__ void __launch_bounds__(WARPS * 32, NT == 1 && sizeof(T) == 2 ? 4 : 2)
                 for (int nt = 0; nt < NT; ++nt)
 #pragma unroll
                     for (int e = 0; e < 4; ++e) {
-                        const int j = key0 + g + 8 * (e >> 1) - it.q.len, i = node[nt][e & 1];
-                        bool ok = j < 0;
-                        if (!ok && j <= i && j < it.q.n_new && i < it.q.n) {
-                            ok = true;
-                            if (p.mask) ok = (j >> 6) < p.mask_words && ((__ldg(p.mask + (size_t)(it.q.row0 + i) * p.mask_words + (j >> 6)) >> (j & 63)) & 1ull);
-                        }
+                        const int j = key0 + g + 8 * (e >> 1) - it.q.len;
+                        const bool ok = j < 0 || sees_new(p, it.q, node[nt][e & 1], j);
                         vis[nt][e] = ok;
                         if (!ok) s[nt][e] = -INFINITY;
                     }
@@ -420,25 +347,7 @@ __global__ void __launch_bounds__(WARPS * 32, NT == 1 && sizeof(T) == 2 ? 4 : 2)
             }
             __syncthreads();
             if (arrived) {
-                for (int x = threadIdx.x; x < rows * (D / 4); x += WARPS * 32) {
-                    const int rl = x / (D / 4), c = 4 * (x % (D / 4));
-                    float m = -INFINITY, lsum = 0.f;
-                    float4 a = make_float4(0.f, 0.f, 0.f, 0.f);
-                    for (int64_t k = c0; k <= c1; ++k) {
-                        const float* sl = p.part + ((size_t)k * 2 + (k == c0 ? 1 : 0)) * N::SLOT;
-                        const float2 ml = __ldcg(reinterpret_cast<const float2*>(sl + (size_t)RT * D + 2 * rl));
-                        const float4 b = __ldcg(reinterpret_cast<const float4*>(sl + (size_t)rl * D + c));
-                        if (ml.x == -INFINITY && ml.y == 0.f) continue;
-                        const float mn = fmaxf(m, ml.x), fa = m == -INFINITY ? 0.f : ex2(m - mn), fb = ex2(ml.x - mn);
-                        a.x = a.x * fa + b.x * fb; a.y = a.y * fa + b.y * fb; a.z = a.z * fa + b.z * fb; a.w = a.w * fa + b.w * fb;
-                        lsum = lsum * fa + ml.y * fb;
-                        m = mn;
-                    }
-                    const int rr = it.tile * RT + rl;
-                    const float inv = lsum == 0.f ? 0.f : 1.f / lsum;
-                    T* dst = (T*)p.out + ((size_t)(it.q.row0 + rr / p.group) * p.q_heads + it.head * p.group + rr % p.group) * D + c;
-                    store4<T>(dst, a.x * inv, a.y * inv, a.z * inv, a.w * inv);
-                }
+                merge_item<T, D>(p, it, RT, rows, c0, c1, threadIdx.x, WARPS * 32);
             }
         }
         __syncthreads();                                                 // the exchange buffers are written again
@@ -466,10 +375,11 @@ ghd_status launch_attn_kv4(ghd_ctx* c, const Kv4View& w, const ghd_kv4_rows* row
     p.q_heads = m.n_heads; p.group = m.n_heads / w.heads;
     p.scale = 1.0f / sqrtf((float)m.d_head);
     p.part = c->gemm_part; p.counters = c->counters;
-    const bool one = (int64_t)rows->n_rows * p.group <= 8ll * w.n_seqs;  // eight query rows a sequence and head, on average
+    const int64_t avg = ((int64_t)rows->n_rows * p.group + w.n_seqs - 1) / w.n_seqs;      // query rows of a sequence and head, on average
     if (m.dtype == GHD_F32) return m.d_head == 64 ? launch_narrow<float, 64, 1>(c, p) : launch_narrow<float, 128, 1>(c, p);
-    if (m.d_head == 64) return one ? launch_narrow<__half, 64, 1>(c, p) : launch_narrow<__half, 64, 2>(c, p);
-    return one ? launch_narrow<__half, 128, 1>(c, p) : launch_narrow<__half, 128, 2>(c, p);
+    if (avg > 16) return launch_attn_kv4_tc(c, p, avg > 64 ? 128 : 64);
+    if (m.d_head == 64) return avg <= 8 ? launch_narrow<__half, 64, 1>(c, p) : launch_narrow<__half, 64, 2>(c, p);
+    return avg <= 8 ? launch_narrow<__half, 128, 1>(c, p) : launch_narrow<__half, 128, 2>(c, p);
 }
 
 }  // namespace ghd

@@ -1,0 +1,605 @@
+// Attention over the paged 4-bit cache for tiles of many query rows (trees, groups of heads): tcgen05 on sm_100a.
+//
+// As in attn_kv4.cu the scales stay out of the products and keys are the M side: S^T [128 keys x rows] = K Q^T,
+// O^T [d_head x rows] = V^T P^T.  With keys on the tensor-memory lanes a thread owns whole key rows:
+//   K   warps 8..11: one thread per key unpacks its 4-bit row in registers and stores it to tensor memory, from where
+//       the first product takes its A operand - the unpacked keys never touch shared memory;
+//   V   the same warps unpack V rows into a swizzled shared-memory tile (A operand of the second product, M-major);
+//   softmax  warps 0..7 read S^T in the 16x256b fragment form: a thread holds 4 keys x 8 (or 16) query rows, so a key's
+//       scale and minimum are four registers pairs and a row's running sums a register each; weights times V's scale
+//       go to shared memory by stmatrix as the B operand of the second product;
+//   warp 12 issues the first product, warp 13 the second.  O^T stays in tensor memory over all keys of an item.
+// Packed codes reach shared memory by cp.async, three units ahead (rows of unknown pages are filled with zeros).
+// Nibbles come out of a word in the order 0 4 1 5 2 6 3 7; the queries are stored in that order, and the output's
+// lanes are read back through it.
+//
+// Half range: weights are taken against a reference that is raised when a score passes it by 2^8, and V's scales are
+// divided by 2^e, e raised when a scale passes 2^7 of it, so the operand stays below 2^15.  Raising either rescales O^T
+// in place (rare after the first unit); the 128 threads that share query rows agree on it by one barrier a unit.
+//
+// Shared memory is what bounds it: per unit of 128 keys and 64 rows 32 KB of V written and read, 16 KB of weights
+// written and read, 16 KB of queries read, 16 KB of codes in and out.  Work is dealt as in attn_kv4.cu, one CTA an SM.
+#include <cstddef>
+#include <cstdio>
+
+#include "attn_kv4_dev.cuh"
+#include "tc_common.cuh"
+
+namespace ghd {
+
+namespace {
+
+using namespace tc;
+using namespace kv4;
+
+constexpr int UNIT = 128;                      // keys of a unit (MMA M of S^T, MMA K of O^T)
+constexpr int SOFT = 256, CONV = 128;          // threads of the softmax and of the unpacking warps
+constexpr int THREADS = SOFT + CONV + 64;
+constexpr float RAISE = 8.f;
+constexpr uint32_t V_SLAB = UNIT * 128;        // [128 keys x 64 channels] half
+
+template <int D, int N>
+struct Shape {
+    static constexpr int STAGES = 4 - (N == 128 ? 1 : 0);
+    static constexpr int SLABS = D / 64, PSLABS = N / 64;
+    static constexpr uint32_t Q_BYTES = SLABS * N * 128, V_BYTES = SLABS * V_SLAB, P_BYTES = PSLABS * UNIT * 128;
+    static constexpr uint32_t ST_BYTES = UNIT * D;                       // K then V codes of a unit, D / 2 bytes a row each
+    static constexpr uint32_t V_AT = Q_BYTES, P_AT = V_AT + 2 * V_BYTES, ST_AT = P_AT + 2 * P_BYTES, CTRL_AT = ST_AT + STAGES * ST_BYTES;
+    static constexpr uint32_t T_K = 0, T_S = 2 * (D / 2), T_O = T_S + 2 * N;      // tensor-memory columns
+    static_assert(T_O + N <= 512, "tensor memory");
+};
+
+struct Ctrl {
+    uint64_t q_full, k_full[2], k_empty[2], v_full[2], v_empty[2], s_full[2], s_empty[2], p_full[2], p_empty[2], drain, drain_pv;
+    uint32_t tmem_base;
+    int abort_flag, arrived;
+    alignas(16) float qs[128];       // sums of the tile's queries
+    alignas(16) float fac[128];      // factors of a rescale, by row
+    float x[4][128], y[4][128];      // exchange between the four warps that share rows
+    float vmax[2][4];                // largest of V's scales of a unit, by half and warp
+    int64_t scratch[32];
+    int64_t sums[GHD_MAX_SEQS + 1];
+};
+template <int D, int N> constexpr uint32_t smem_bytes() { return Shape<D, N>::CTRL_AT + (uint32_t)sizeof(Ctrl) + 1024; }
+static_assert(offsetof(Ctrl, qs) % 16 == 0 && offsetof(Ctrl, fac) % 16 == 0, "rows are read in pairs");
+static_assert(smem_bytes<128, 128>() <= 227 * 1024 && smem_bytes<128, 64>() <= 227 * 1024, "shared memory");
+
+__device__ __forceinline__ void ld_frag(uint32_t taddr, uint32_t (&r)[4]) {      // 16 lanes x 8 columns, as an mma accumulator
+    asm volatile("tcgen05.ld.sync.aligned.16x256b.x1.b32 {%0, %1, %2, %3}, [%4];" : "=r"(r[0]), "=r"(r[1]), "=r"(r[2]), "=r"(r[3]) : "r"(taddr) : "memory");
+}
+__device__ __forceinline__ void st16(uint32_t taddr, const uint32_t (&r)[16]) {
+    asm volatile("tcgen05.st.sync.aligned.32x32b.x16.b32 [%0], {%1, %2, %3, %4, %5, %6, %7, %8, %9, %10, %11, %12, %13, %14, %15, %16};"
+                 ::"r"(taddr), "r"(r[0]), "r"(r[1]), "r"(r[2]), "r"(r[3]), "r"(r[4]), "r"(r[5]), "r"(r[6]), "r"(r[7]), "r"(r[8]), "r"(r[9]), "r"(r[10]), "r"(r[11]),
+                   "r"(r[12]), "r"(r[13]), "r"(r[14]), "r"(r[15]) : "memory");
+}
+__device__ __forceinline__ void ld_wait() { asm volatile("tcgen05.wait::ld.sync.aligned;" ::: "memory"); }
+__device__ __forceinline__ void st_wait() { asm volatile("tcgen05.wait::st.sync.aligned;" ::: "memory"); }
+// D[tmem] (+)= A[tmem] * B[smem]
+__device__ __forceinline__ void mma_ts(uint32_t d_tmem, uint32_t a_tmem, uint64_t bdesc, uint32_t idesc, uint32_t accumulate) {
+    asm volatile(
+        "{\n\t.reg .pred p;\n\t"
+        "setp.ne.b32 p, %4, 0;\n\t"
+        "tcgen05.mma.cta_group::1.kind::f16 [%0], [%1], %2, %3, p;\n\t}"
+        ::"r"(d_tmem), "r"(a_tmem), "l"(bdesc), "r"(idesc), "r"(accumulate) : "memory");
+}
+__device__ __forceinline__ void cp16(uint32_t dst, const void* src, bool there) {     // zeros when the row is not there
+    asm volatile("cp.async.cg.shared.global [%0], [%1], 16, %2;" ::"r"(dst), "l"(src), "r"(there ? 16 : 0) : "memory");
+}
+__device__ __forceinline__ void stmatrix4(uint32_t addr, uint32_t a, uint32_t b, uint32_t c, uint32_t d) {
+    asm volatile("stmatrix.sync.aligned.m8n8.x4.shared.b16 [%0], {%1, %2, %3, %4};" ::"r"(addr), "r"(a), "r"(b), "r"(c), "r"(d) : "memory");
+}
+__device__ __forceinline__ uint4 lds128(uint32_t addr) {
+    uint4 v;
+    asm volatile("ld.shared.v4.u32 {%0, %1, %2, %3}, [%4];" : "=r"(v.x), "=r"(v.y), "=r"(v.z), "=r"(v.w) : "r"(addr) : "memory");
+    return v;
+}
+__device__ __forceinline__ void sts128(uint32_t addr, const uint32_t* r) {
+    asm volatile("st.shared.v4.u32 [%0], {%1, %2, %3, %4};" ::"r"(addr), "r"(r[0]), "r"(r[1]), "r"(r[2]), "r"(r[3]) : "memory");
+}
+template <int ID, int NT> __device__ __forceinline__ void named_sync() { asm volatile("bar.sync %0, %1;" ::"n"(ID), "n"(NT) : "memory"); }
+__device__ __forceinline__ void half_sync(int half) { asm volatile("bar.sync %0, 128;" ::"r"(2 + half) : "memory"); }
+__device__ __forceinline__ bool half_any(int half, bool v) {
+    uint32_t r;
+    asm volatile("{\n\t.reg .pred p, q;\n\tsetp.ne.u32 p, %1, 0;\n\tbar.red.or.pred q, %2, 128, p;\n\tselp.u32 %0, 1, 0, q;\n\t}" : "=r"(r) : "r"(v ? 1u : 0u), "r"(2 + half) : "memory");
+    return r != 0;
+}
+
+// eight codes -> four packed pairs, nibbles in the order 0 4 1 5 2 6 3 7
+__device__ __forceinline__ void unpack8(uint32_t w, uint32_t* r) {
+    const uint32_t x = w >> 8;
+    r[0] = centred_half<0>(w);
+    r[1] = centred_half<4>(w);
+    r[2] = centred_half<0>(x);
+    r[3] = centred_half<4>(x);
+}
+// place of 16-byte piece c of a packed row in its staging buffer: rows of D / 2 bytes, pieces swapped so that eight lanes
+// reading the same piece of eight rows hit eight different bank groups
+template <int D> __device__ __forceinline__ uint32_t piece_at(int row, int c) {
+    return D == 128 ? (uint32_t)(row * 64 + ((c ^ ((row >> 1) & 3)) << 4)) : (uint32_t)(row * 32 + ((c ^ ((row >> 2) & 1)) << 4));
+}
+
+template <int D, int N>
+__global__ void __launch_bounds__(THREADS, 1) k_attn_kv4_tc(const Kv4AttnParams p) {
+    using SH = Shape<D, N>;
+    constexpr int NB = N / 16;                       // blocks of eight query rows a softmax thread sees (it takes every other block)
+    constexpr int PIECES = D / 32;                   // 16-byte pieces of a packed row
+    extern __shared__ uint8_t smem_raw[];
+    const uint32_t raw_addr = smem_u32(smem_raw), pad = (1024u - (raw_addr & 1023u)) & 1023u;
+    uint8_t* base = smem_raw + pad;
+    const uint32_t base_a = smem_u32(base);
+    Ctrl* sm = reinterpret_cast<Ctrl*>(base + SH::CTRL_AT);
+    const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
+
+    if (threadIdx.x == 0) {
+        mbar_init(smem_u32(&sm->q_full), SOFT);
+        for (int b = 0; b < 2; ++b) {
+            mbar_init(smem_u32(&sm->k_full[b]), CONV); mbar_init(smem_u32(&sm->k_empty[b]), 1);
+            mbar_init(smem_u32(&sm->v_full[b]), CONV); mbar_init(smem_u32(&sm->v_empty[b]), 1);
+            mbar_init(smem_u32(&sm->s_full[b]), 1); mbar_init(smem_u32(&sm->s_empty[b]), SOFT);
+            mbar_init(smem_u32(&sm->p_full[b]), SOFT); mbar_init(smem_u32(&sm->p_empty[b]), 1);
+        }
+        mbar_init(smem_u32(&sm->drain), 1);
+        mbar_init(smem_u32(&sm->drain_pv), 1);
+        sm->abort_flag = 0;
+        asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
+    }
+    if (warp == 12) {
+        asm volatile("tcgen05.alloc.cta_group::1.sync.aligned.shared::cta.b32 [%0], %1;" ::"r"(smem_u32(&sm->tmem_base)), "r"(512u) : "memory");
+        asm volatile("tcgen05.relinquish_alloc_permit.cta_group::1.sync.aligned;" ::: "memory");
+    }
+    const Kv4View& w = p.w;
+    const Kv4Tiling til{w.heads, p.group, N, UNIT};
+    tc_fence_before();
+    const int64_t units = unit_sums(w, til, sm->sums, sm->scratch);      // two block barriers inside
+    tc_fence_after();
+    const uint32_t tmem = sm->tmem_base;
+    volatile int* abort_flag = &sm->abort_flag;
+    const int64_t per = kv4_units_per_cta(units, p.ctas);
+    const int64_t u_beg = per * blockIdx.x, u_end = u_beg + per < units ? u_beg + per : units;
+    auto item_at = [&](int64_t u) { return kv4_find_item(til, sm->sums, w.n_seqs, [&](int s_) { return kv4_load_seq(w, s_); }, u, u_end); };
+    auto rows_of = [&](const Kv4Item& it) { const int r = it.q.n * p.group - it.tile * N; return r < N ? r : N; };
+    auto cols_of = [&](int rows) { return (rows + 15) & ~15; };           // MMA N: a multiple of 16
+
+    if (warp >= 8 && warp < 12) {
+        // ------------------------------------------------ unpacking warps: thread = key
+        const int quad = warp - 8, key = quad * 32 + lane;
+        const uint32_t st0 = base_a + SH::ST_AT + quad * 32 * (D / 2);    // this warp's 32 rows of a stage (K; V UNIT rows further)
+        const int R = 1 << w.shift;
+        int64_t lu = u_beg;                                               // load cursor
+        Kv4Item it{};
+        int lch = 0, lend = 0, lkeys = 0;
+        auto load_next = [&](int i) {
+            if (lu < u_end) {
+                if (lch >= lend) { it = item_at(lu); lch = it.chunk0; lend = it.chunk0 + it.take; lkeys = kv4_tile_keys(til, it.q, it.tile); }
+                const uint32_t st = st0 + (uint32_t)(i % SH::STAGES) * SH::ST_BYTES;
+                const int key0 = lch * UNIT + quad * 32;
+                int page[2];                                              // of this warp's two groups of 16 keys
+#pragma unroll
+                for (int h = 0; h < 2; ++h) page[h] = key0 + 16 * h < lkeys ? kv4_page(w, it.seq, key0 + 16 * h) : -1;
+                constexpr int PER = 32 / PIECES;                          // rows a warp-wide copy covers
+#pragma unroll
+                for (int j = 0; j < PIECES; ++j) {
+                    const int row = lane / PIECES + PER * j, c = lane % PIECES;
+                    const int pg = row < 16 ? page[0] : page[1];
+                    const int r = (key0 + row) & (R - 1);
+                    const uint8_t* blk = p.pool + kv4_block_at(w, pg < 0 ? 0 : pg, it.head);
+                    cp16(st + piece_at<D>(row, c), blk + kv4_code_at(R, D, 0, r) + 16 * c, pg >= 0);
+                    cp16(st + UNIT * (D / 2) + piece_at<D>(row, c), blk + kv4_code_at(R, D, 1, r) + 16 * c, pg >= 0);
+                }
+                ++lch;
+                ++lu;
+            }
+            asm volatile("cp.async.commit_group;" ::: "memory");
+        };
+        const int n = (int)(u_end > u_beg ? u_end - u_beg : 0);
+#pragma unroll
+        for (int i = 0; i < SH::STAGES - 1; ++i) load_next(i);
+        for (int i = 0; i < n; ++i) {
+            const int b = i & 1;
+            const uint32_t st = st0 + (uint32_t)(i % SH::STAGES) * SH::ST_BYTES;
+            __syncwarp();                                                 // everybody has read the stage that is filled next
+            load_next(i + SH::STAGES - 1);
+            asm volatile("cp.async.wait_group %0;" ::"n"(SH::STAGES - 1) : "memory");
+            __syncwarp();
+            if (i >= 2) mbar_wait(smem_u32(&sm->k_empty[b]), ((i >> 1) - 1) & 1, abort_flag, w.status, DEV_TIMEOUT_TMEM);
+            tc_fence_after();
+#pragma unroll
+            for (int c = 0; c < PIECES; ++c) {
+                const uint4 x = lds128(st + piece_at<D>(lane, c));
+                uint32_t r[16];
+                unpack8(x.x, r); unpack8(x.y, r + 4); unpack8(x.z, r + 8); unpack8(x.w, r + 12);
+                st16(tmem + SH::T_K + b * (D / 2) + c * 16 + ((uint32_t)(quad * 32) << 16), r);
+            }
+            st_wait();
+            tc_fence_before();
+            mbar_arrive(smem_u32(&sm->k_full[b]));
+            if (i >= 2) mbar_wait(smem_u32(&sm->v_empty[b]), ((i >> 1) - 1) & 1, abort_flag, w.status, DEV_TIMEOUT_TMEM);
+            const uint32_t vt = base_a + SH::V_AT + b * SH::V_BYTES + key * 128;
+#pragma unroll
+            for (int c = 0; c < PIECES; ++c) {
+                const uint4 x = lds128(st + UNIT * (D / 2) + piece_at<D>(lane, c));
+                uint32_t r[16];
+                unpack8(x.x, r); unpack8(x.y, r + 4); unpack8(x.z, r + 8); unpack8(x.w, r + 12);
+#pragma unroll
+                for (int k = 0; k < 4; ++k) sts128(vt + (c >> 1) * V_SLAB + ((((c & 1) * 4 + k) ^ (key & 7)) << 4), r + 4 * k);
+            }
+            asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
+            mbar_arrive(smem_u32(&sm->v_full[b]));
+        }
+        asm volatile("cp.async.wait_all;" ::: "memory");
+    } else if (warp == 12) {
+        // ------------------------------------------------ issuer of S^T = K Q^T
+        if (lane == 0) {
+            const uint64_t q_desc = smem_desc_sw128(base_a);
+            bool ok = true;
+            int i = 0, items = 0;
+            for (int64_t u = u_beg; ok && u < u_end; ++items) {
+                const Kv4Item it = item_at(u);
+                const uint32_t idesc = instr_desc_f16(cols_of(rows_of(it)), false);
+                ok = mbar_wait(smem_u32(&sm->q_full), items & 1, abort_flag, w.status, DEV_TIMEOUT_MMA);
+                for (int k = 0; ok && k < it.take; ++k, ++i) {
+                    const int b = i & 1;
+                    ok = mbar_wait(smem_u32(&sm->k_full[b]), (i >> 1) & 1, abort_flag, w.status, DEV_TIMEOUT_MMA);
+                    if (ok && i >= 2) ok = mbar_wait(smem_u32(&sm->s_empty[b]), ((i >> 1) - 1) & 1, abort_flag, w.status, DEV_TIMEOUT_TMEM);
+                    if (!ok) break;
+                    tc_fence_after();
+#pragma unroll
+                    for (int ks = 0; ks < D / 16; ++ks)                  // 16 channels: 8 columns of K, 32 bytes along Q's rows
+                        mma_ts(tmem + SH::T_S + b * N, tmem + SH::T_K + b * (D / 2) + ks * 8,
+                               q_desc + (uint64_t)((((ks >> 2) * N * 128) >> 4) + (ks & 3) * 2), idesc, ks > 0 ? 1u : 0u);
+                    tc_commit(smem_u32(&sm->s_full[b]));
+                    tc_commit(smem_u32(&sm->k_empty[b]));
+                }
+                u += it.take;
+            }
+            if (!ok) {
+                tc_commit(smem_u32(&sm->drain));
+                for (uint32_t spin = 0; spin < SPIN_LIMIT && !mbar_try(smem_u32(&sm->drain), 0); ++spin) __nanosleep(64);
+            }
+        }
+    } else if (warp == 13) {
+        // ------------------------------------------------ issuer of O^T += V^T P^T
+        if (lane == 0) {
+            // both operands have the MMA's K dimension (keys) as rows of 128 bytes: 64 channels of V, 64 query rows of P
+            const uint64_t v_desc = smem_desc_sw128(base_a + SH::V_AT, D == 128 ? V_SLAB : 0);   // d_head 64: channels 64 .. 127 repeat 0 .. 63
+            const uint64_t p_desc = smem_desc_sw128(base_a + SH::P_AT, UNIT * 128);
+            bool ok = true;
+            int i = 0;
+            for (int64_t u = u_beg; ok && u < u_end;) {
+                const Kv4Item it = item_at(u);
+                const uint32_t idesc = instr_desc_f16(cols_of(rows_of(it)), true) | (1u << 15);
+                for (int k = 0; ok && k < it.take; ++k, ++i) {
+                    const int b = i & 1;
+                    ok = mbar_wait(smem_u32(&sm->v_full[b]), (i >> 1) & 1, abort_flag, w.status, DEV_TIMEOUT_MMA);
+                    if (ok) ok = mbar_wait(smem_u32(&sm->p_full[b]), (i >> 1) & 1, abort_flag, w.status, DEV_TIMEOUT_MMA);
+                    if (!ok) break;
+                    tc_fence_after();
+#pragma unroll
+                    for (int ks = 0; ks < UNIT / 16; ++ks)               // 16 keys: 16 rows of both tiles
+                        tc_mma_f16(tmem + SH::T_O, v_desc + (uint64_t)((b * SH::V_BYTES + ks * 2048) >> 4), p_desc + (uint64_t)((b * SH::P_BYTES + ks * 2048) >> 4),
+                                   idesc, (k > 0 || ks > 0) ? 1u : 0u);
+                    tc_commit(smem_u32(&sm->v_empty[b]));
+                    tc_commit(smem_u32(&sm->p_empty[b]));
+                }
+                u += it.take;
+            }
+            if (!ok) {
+                tc_commit(smem_u32(&sm->drain_pv));
+                for (uint32_t spin = 0; spin < SPIN_LIMIT && !mbar_try(smem_u32(&sm->drain_pv), 0); ++spin) __nanosleep(64);
+            }
+        }
+    } else if (warp < 8) {
+        // ------------------------------------------------ softmax warps
+        // half: which blocks of eight query rows (half, half + 2, ...); quad: which 32 keys (tensor-memory lanes)
+        const int half = warp >> 2, quad = warp & 3, g = lane >> 2, t = lane & 3, tid = threadIdx.x;
+        const int R = 1 << w.shift;
+        const float sl2 = p.scale * KV4_LOG2E;
+        int i = 0;                                                        // unit of this CTA
+        for (int64_t u = u_beg; u < u_end;) {
+            const Kv4Item it = item_at(u);
+            const int rows = rows_of(it), cols = cols_of(rows), keys = kv4_tile_keys(til, it.q, it.tile);
+            // ---- queries to shared memory, channels of a word in the order the nibbles come in; their sums
+            {
+                constexpr int C8 = D / 8;                                 // 16-byte pieces of a row
+                for (int x = tid; x < cols * C8; x += SOFT) {
+                    const int rl = x / C8, c = x % C8, rr = it.tile * N + rl;
+                    uint4 v = make_uint4(0, 0, 0, 0);
+                    if (rl < rows) v = __ldg(reinterpret_cast<const uint4*>((const __half*)p.q + ((size_t)(it.q.row0 + rr / p.group) * p.q_heads + it.head * p.group + rr % p.group) * D + 8 * c));
+                    const uint32_t r[4] = {__byte_perm(v.x, v.z, 0x5410), __byte_perm(v.x, v.z, 0x7632), __byte_perm(v.y, v.w, 0x5410), __byte_perm(v.y, v.w, 0x7632)};
+                    sts128(base_a + (c >> 3) * N * 128 + rl * 128 + (((c & 7) ^ (rl & 7)) << 4), r);
+                    float s = 0.f;
+#pragma unroll
+                    for (int e = 0; e < 4; ++e) { const float2 f = __half22float2(*reinterpret_cast<const __half2*>(&r[e])); s += f.x + f.y; }
+#pragma unroll
+                    for (int o = 1; o < C8; o <<= 1) s += __shfl_xor_sync(0xffffffffu, s, o);
+                    if (c == 0) sm->qs[rl] = s;
+                }
+                asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
+                mbar_arrive(smem_u32(&sm->q_full));
+                named_sync<1, SOFT>();                                    // the sums are read by everybody
+            }
+            float l[NB][2], ms[NB][2], ref[NB][2];
+#pragma unroll
+            for (int j = 0; j < NB; ++j)
+#pragma unroll
+                for (int e = 0; e < 2; ++e) { l[j][e] = 0.f; ms[j][e] = 0.f; ref[j][e] = -INFINITY; }
+            float vmul = 0x1p24f;                                         // 2^-e of V's scales
+            bool any_pv = false;                                          // O^T holds something of this item
+
+            float2 kp[4], vp[4];                                          // scale and minimum of this thread's four keys
+            bool there[4];
+            auto load_par = [&](int ch) {
+#pragma unroll
+                for (int x = 0; x < 4; ++x) {
+                    const int key = ch * UNIT + quad * 32 + g + 8 * x;
+                    kp[x] = vp[x] = make_float2(0.f, 0.f);
+                    there[x] = false;
+                    if (key < keys) {
+                        const int pg = kv4_page(w, it.seq, key);
+                        if (pg >= 0) {
+                            const uint8_t* blk = p.pool + kv4_block_at(w, pg, it.head);
+                            kp[x] = load_params<__half>(blk + kv4_param_at(R, D, 2, 0, key & (R - 1)));
+                            vp[x] = load_params<__half>(blk + kv4_param_at(R, D, 2, 1, key & (R - 1)));
+                            there[x] = true;
+                        }
+                    }
+                }
+            };
+            for (int k = 0; k < it.take; ++k, ++i) {
+                const int b = i & 1, ch = it.chunk0 + k, key0 = ch * UNIT + quad * 32 + g;
+                load_par(ch);
+                const bool all = ch * UNIT + UNIT <= it.q.len && there[0] && there[1] && there[2] && there[3];
+                float ks[4], km[4];
+#pragma unroll
+                for (int x = 0; x < 4; ++x) { ks[x] = kp[x].x * sl2; km[x] = fmaf(8.f, kp[x].x, kp[x].y) * sl2; vp[x].y = fmaf(8.f, vp[x].x, vp[x].y); }
+                mbar_wait(smem_u32(&sm->s_full[b]), (i >> 1) & 1, abort_flag, w.status, DEV_TIMEOUT_EPI);
+                tc_fence_after();
+                bool p_ready = false;
+#pragma unroll
+                for (int j0 = 0; j0 < NB; j0 += 4) {                      // 32 of this thread's scores at a time
+                    if (8 * (2 * j0 + half) >= cols) { if (j0 > 0) break; }
+                    uint32_t s[4][2][4];
+#pragma unroll
+                    for (int j = 0; j < 4; ++j)
+#pragma unroll
+                        for (int h = 0; h < 2; ++h) ld_frag(tmem + SH::T_S + b * N + 8 * (2 * (j0 + j) + half) + ((uint32_t)(quad * 32 + 16 * h) << 16), s[j][h]);
+                    ld_wait();
+                    uint32_t vis = 0xffffffffu;
+                    bool over = false;
+#pragma unroll
+                    for (int x = 0; x < 4; ++x) over = over || vp[x].x * vmul > 128.f;
+                    if (!all) {
+                        vis = 0u;
+#pragma unroll
+                        for (int j = 0; j < 4; ++j)
+#pragma unroll
+                            for (int e = 0; e < 2; ++e) {
+                                const int node = (it.tile * N + 8 * (2 * (j0 + j) + half) + 2 * t + e) / p.group;
+#pragma unroll
+                                for (int x = 0; x < 4; ++x) {
+                                    const int jj = key0 + 8 * x - it.q.len;
+                                    if (there[x] && (jj < 0 || sees_new(p, it.q, node, jj))) vis |= 1u << (8 * j + 4 * e + x);
+                                }
+                            }
+                    }
+#pragma unroll
+                    for (int j = 0; j < 4; ++j) if (8 * (2 * (j0 + j) + half) >= cols) vis &= ~(0xffu << (8 * j));      // no such rows
+                    // score of key x and row (j, e): register 2 (x & 1) + e of fragment x >> 1
+#pragma unroll
+                    for (int j = 0; j < 4; ++j) {
+                        const float2 q2 = *reinterpret_cast<const float2*>(&sm->qs[8 * (2 * (j0 + j) + half) + 2 * t]);
+#pragma unroll
+                        for (int e = 0; e < 2; ++e)
+#pragma unroll
+                            for (int x = 0; x < 4; ++x) {
+                                uint32_t& r = s[j][x >> 1][2 * (x & 1) + e];
+                                float v = fmaf(ks[x], __uint_as_float(r), km[x] * (e ? q2.y : q2.x));
+                                if (!((vis >> (8 * j + 4 * e + x)) & 1u)) v = -INFINITY;
+                                over = over || v - ref[j0 + j][e] > RAISE;
+                                r = __float_as_uint(v);
+                            }
+                    }
+                    if (half_any(half, over)) {
+                        // ---- the 128 threads of these rows agree on new references and a new exponent
+                        float vm = 0.f;
+#pragma unroll
+                        for (int x = 0; x < 4; ++x) if (vp[x].x <= 65504.f) vm = fmaxf(vm, vp[x].x);
+#pragma unroll
+                        for (int o = 4; o < 32; o <<= 1) vm = fmaxf(vm, __shfl_xor_sync(0xffffffffu, vm, o));
+                        if (lane == 0) sm->vmax[half][quad] = vm;
+#pragma unroll
+                        for (int j = 0; j < 4; ++j)
+#pragma unroll
+                            for (int e = 0; e < 2; ++e) {
+                                float m = -INFINITY;
+#pragma unroll
+                                for (int x = 0; x < 4; ++x) m = fmaxf(m, __uint_as_float(s[j][x >> 1][2 * (x & 1) + e]));
+#pragma unroll
+                                for (int o = 4; o < 32; o <<= 1) m = fmaxf(m, __shfl_xor_sync(0xffffffffu, m, o));
+                                if (g == 0) sm->x[quad][8 * (2 * (j0 + j) + half) + 2 * t + e] = m;
+                            }
+                        half_sync(half);
+                        vm = fmaxf(fmaxf(sm->vmax[half][0], sm->vmax[half][1]), fmaxf(sm->vmax[half][2], sm->vmax[half][3]));
+                        float vnew = vmul;                        // changes before the unit's first weights only
+                        if (j0 == 0 && vm * vnew > 1.f) vnew = exp2f(-ceilf(log2f(vm)));
+                        const float fv = vnew / vmul;
+#pragma unroll
+                        for (int j = 0; j < NB; ++j)
+#pragma unroll
+                            for (int e = 0; e < 2; ++e) {
+                                const int rl = 8 * (2 * j + half) + 2 * t + e;
+                                float f = 1.f;
+                                if (j >= j0 && j < j0 + 4) {
+                                    const float m = fmaxf(fmaxf(sm->x[0][rl], sm->x[1][rl]), fmaxf(sm->x[2][rl], sm->x[3][rl]));
+                                    if (m > ref[j][e]) {
+                                        f = ex2(ref[j][e] - m);
+                                        ref[j][e] = m;
+                                        l[j][e] *= f;
+                                        ms[j][e] *= f;
+                                    }
+                                }
+                                if (quad == 0 && g == 0) sm->fac[rl] = f * fv;
+                            }
+                        vmul = vnew;
+                        half_sync(half);
+                        if (any_pv) {
+                            // O^T holds the products of the units before once the last of them has completed (each P buffer's
+                            // release is waited for again two units later, so its phases are seen one by one)
+                            mbar_wait(smem_u32(&sm->p_empty[(i - 1) & 1]), ((i - 1) >> 1) & 1, abort_flag, w.status, DEV_TIMEOUT_EPI);
+                            tc_fence_after();
+#pragma unroll
+                            for (int j = 0; j < NB; ++j) {                // this half's blocks of eight columns, both groups of 16 lanes
+                                const int c0 = 8 * (2 * j + half);
+                                if (c0 >= cols) break;
+                                const float2 f = *reinterpret_cast<const float2*>(&sm->fac[c0 + 2 * t]);
+                                uint32_t o[2][4];
+#pragma unroll
+                                for (int h = 0; h < 2; ++h) ld_frag(tmem + SH::T_O + c0 + ((uint32_t)(quad * 32 + 16 * h) << 16), o[h]);
+                                ld_wait();
+#pragma unroll
+                                for (int h = 0; h < 2; ++h) {
+#pragma unroll
+                                    for (int e = 0; e < 4; ++e) o[h][e] = __float_as_uint(__uint_as_float(o[h][e]) * ((e & 1) ? f.y : f.x));
+                                    asm volatile("tcgen05.st.sync.aligned.16x256b.x1.b32 [%0], {%1, %2, %3, %4};"
+                                                 ::"r"(tmem + SH::T_O + c0 + ((uint32_t)(quad * 32 + 16 * h) << 16)), "r"(o[h][0]), "r"(o[h][1]), "r"(o[h][2]), "r"(o[h][3]) : "memory");
+                                }
+                            }
+                            st_wait();
+                            tc_fence_before();
+                        }
+                        half_sync(half);                                  // the exchange buffers may be written again
+                    }
+                    if (!p_ready) {
+                        if (i >= 2) mbar_wait(smem_u32(&sm->p_empty[b]), ((i >> 1) - 1) & 1, abort_flag, w.status, DEV_TIMEOUT_EPI);
+                        p_ready = true;
+                    }
+                    float vs[4];
+#pragma unroll
+                    for (int x = 0; x < 4; ++x) vs[x] = vp[x].x * vmul;
+#pragma unroll
+                    for (int j = 0; j < 4; ++j) {
+                        const int blk = 2 * (j0 + j) + half;
+                        float pv[2][4];
+#pragma unroll
+                        for (int e = 0; e < 2; ++e) {
+                            const float rf = ref[j0 + j][e] == -INFINITY ? 0.f : ref[j0 + j][e];
+#pragma unroll
+                            for (int x = 0; x < 4; ++x) {
+                                const bool ok = (vis >> (8 * j + 4 * e + x)) & 1u;
+                                const float pe = ex2(__uint_as_float(s[j][x >> 1][2 * (x & 1) + e]) - rf);
+                                l[j0 + j][e] += ok ? pe : 0.f;
+                                ms[j0 + j][e] += ok ? pe * vp[x].y : 0.f;
+                                pv[e][x] = ok ? pe * vs[x] : 0.f;
+                            }
+                        }
+                        uint32_t h4[4];
+#pragma unroll
+                        for (int x = 0; x < 4; ++x) {
+                            const __half2 h2 = __floats2half2_rn(pv[0][x], pv[1][x]);
+                            h4[x] = *reinterpret_cast<const uint32_t*>(&h2);
+                        }
+                        // lane's matrix row: key 32 quad + lane, query rows 8 blk .. 8 blk + 7
+                        if (8 * blk < cols)
+                            stmatrix4(base_a + SH::P_AT + b * SH::P_BYTES + (blk >> 3) * (UNIT * 128) + (quad * 32 + lane) * 128 + (((blk & 7) ^ (lane & 7)) << 4), h4[0], h4[1], h4[2], h4[3]);
+                    }
+                }
+                tc_fence_before();
+                mbar_arrive(smem_u32(&sm->s_empty[b]));
+                asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
+                mbar_arrive(smem_u32(&sm->p_full[b]));
+                any_pv = true;
+            }
+            // ---- sums of the rows over the four warps that share them
+#pragma unroll
+            for (int j = 0; j < NB; ++j)
+#pragma unroll
+                for (int e = 0; e < 2; ++e) {
+                    float a = l[j][e], c = ms[j][e];
+#pragma unroll
+                    for (int o = 4; o < 32; o <<= 1) { a += __shfl_xor_sync(0xffffffffu, a, o); c += __shfl_xor_sync(0xffffffffu, c, o); }
+                    const int rl = 8 * (2 * j + half) + 2 * t + e;
+                    if (g == 0) { sm->x[quad][rl] = a; sm->y[quad][rl] = c; if (quad == 0) sm->fac[rl] = ref[j][e]; }
+                }
+            named_sync<1, SOFT>();
+            mbar_wait(smem_u32(&sm->p_empty[(i - 1) & 1]), ((i - 1) >> 1) & 1, abort_flag, w.status, DEV_TIMEOUT_EPI);
+            tc_fence_after();
+            const int64_t c0 = it.first / per, c1 = (it.first + it.chunks - 1) / per;
+            const bool whole = c0 == c1;
+            float* slot = p.part + ((size_t)blockIdx.x * 2 + ((int64_t)blockIdx.x == c0 ? 1 : 0)) * ((size_t)N * (D + 2));
+            const float vinv = 1.f / vmul;
+            // lane (16 h + g or + 8) of this quad is channel ch_of(lane); columns of this half's blocks
+            auto ch_of = [](int m) { return (m & ~7) | ((m & 1) * 4) | ((m & 7) >> 1); };       // 0 4 1 5 2 6 3 7
+#pragma unroll
+            for (int j = 0; j < NB; ++j) {
+                const int blk = 2 * j + half;
+                if (8 * blk >= rows || quad * 32 >= D) break;
+                uint32_t o[2][4];
+#pragma unroll
+                for (int h = 0; h < 2; ++h) ld_frag(tmem + SH::T_O + 8 * blk + ((uint32_t)(quad * 32 + 16 * h) << 16), o[h]);
+                ld_wait();
+#pragma unroll
+                for (int e = 0; e < 2; ++e) {
+                    const int rl = 8 * blk + 2 * t + e;
+                    if (rl >= rows) continue;
+                    const float lsum = (sm->x[0][rl] + sm->x[1][rl]) + (sm->x[2][rl] + sm->x[3][rl]), mm = (sm->y[0][rl] + sm->y[1][rl]) + (sm->y[2][rl] + sm->y[3][rl]);
+                    const int rr = it.tile * N + rl;
+                    const float inv = lsum == 0.f ? 0.f : 1.f / lsum;
+                    __half* dst = (__half*)p.out + ((size_t)(it.q.row0 + rr / p.group) * p.q_heads + it.head * p.group + rr % p.group) * D;
+#pragma unroll
+                    for (int h = 0; h < 2; ++h)
+#pragma unroll
+                        for (int x = 0; x < 2; ++x) {
+                            const int chn = quad * 32 + ch_of(16 * h + 8 * x + g);
+                            const float v = fmaf(__uint_as_float(o[h][2 * x + e]), vinv, mm);
+                            if (whole) dst[chn] = __float2half_rn(v * inv);
+                            else __stcg(slot + (size_t)rl * D + chn, v);
+                        }
+                    if (!whole && g == 0 && quad == 0) __stcg(reinterpret_cast<float2*>(slot + (size_t)N * D + 2 * rl), make_float2(sm->fac[rl], lsum));
+                }
+            }
+            tc_fence_before();                                            // O^T has been read: the next item's first product may write it
+            if (!whole) {
+                __threadfence();
+                named_sync<1, SOFT>();
+                if (tid == 0) {
+                    const int want = (int)(c1 - c0), old = atomicAdd(p.counters + c0, 1);
+                    if (old == want) p.counters[c0] = 0;
+                    sm->arrived = old == want;
+                    __threadfence();
+                }
+                named_sync<1, SOFT>();
+                if (sm->arrived) merge_item<__half, D>(p, it, N, rows, c0, c1, tid, SOFT);
+            }
+            named_sync<1, SOFT>();                                        // queries' sums and exchange buffers are written again
+            u += it.take;
+        }
+    }
+
+    tc_fence_before();
+    __syncthreads();
+    if (warp == 12) {
+        tc_fence_after();
+        asm volatile("tcgen05.dealloc.cta_group::1.sync.aligned.b32 %0, %1;" ::"r"(tmem), "r"(512u) : "memory");
+    }
+}
+
+template <int D, int N>
+ghd_status launch_tc(ghd_ctx* c, Kv4AttnParams& p) {
+    if (cudaFuncSetAttribute(k_attn_kv4_tc<D, N>, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)smem_bytes<D, N>()) != cudaSuccess) {
+        cudaGetLastError();
+        return fail(c, GHD_ECUDA, "kv4_attention: cannot raise dynamic shared memory");
+    }
+    p.ctas = c->sm_count;
+    launch_k(c, false, k_attn_kv4_tc<D, N>, dim3(p.ctas), dim3(THREADS), smem_bytes<D, N>(), p);
+    return GHD_OK;
+}
+
+}  // namespace
+
+// partials: 2 slots of [tile_rows][d_head + 2] floats a CTA, within the tile scratch of 2 x 256 x 128 floats an SM
+ghd_status launch_attn_kv4_tc(ghd_ctx* c, Kv4AttnParams& p, int tile_rows) {
+    if (c->cfg.d_head == 64) return tile_rows == 64 ? launch_tc<64, 64>(c, p) : launch_tc<64, 128>(c, p);
+    return tile_rows == 64 ? launch_tc<128, 64>(c, p) : launch_tc<128, 128>(c, p);
+}
+
+}  // namespace ghd
