@@ -28,6 +28,7 @@ namespace {
 
 constexpr int WARPS = 4, CHUNK = 16 * WARPS;
 constexpr float RAISE = 2.f;
+constexpr int LEAD = 3;          // an item's fixed cost in chunks
 
 using namespace kv4;
 
@@ -70,20 +71,18 @@ template <> struct Op<float> {
     }
 };
 
+template <typename T> __device__ __forceinline__ float2 param_of(const uint8_t* p, int key);
+template <> __device__ __forceinline__ float2 param_of<__half>(const uint8_t* p, int key) { return __half22float2(reinterpret_cast<const __half2*>(p)[key]); }
+template <> __device__ __forceinline__ float2 param_of<float>(const uint8_t* p, int key) { return reinterpret_cast<const float2*>(p)[key]; }
 __device__ __forceinline__ uint32_t transpose8x8(uint32_t x) {
     uint32_t y;
     asm volatile("movmatrix.sync.aligned.m8n8.trans.b16 %0, %1;" : "=r"(y) : "r"(x));
     return y;
 }
 
-template <int N> struct Words { uint32_t w[N]; };
-template <int N> __device__ __forceinline__ Words<N> load_words(const uint8_t* p) {
-    Words<N> r;
-    if constexpr (N == 4) { const uint4 v = __ldg(reinterpret_cast<const uint4*>(p)); r.w[0] = v.x; r.w[1] = v.y; r.w[2] = v.z; r.w[3] = v.w; }
-    else if constexpr (N == 2) { const uint2 v = __ldg(reinterpret_cast<const uint2*>(p)); r.w[0] = v.x; r.w[1] = v.y; }
-    else r.w[0] = __ldg(reinterpret_cast<const uint32_t*>(p));
-    return r;
-}
+// Key rows of a block of 16 in operand order: operand rows 2 t and 2 t + 1 (and + 8) are keys 2 t + (t & 1) and the other of
+// the pair, so that eight lanes reading K and sixteen reading V from shared memory meet different banks.
+__device__ __forceinline__ int key_of(int k) { return (k & ~1) | ((k ^ (k >> 1)) & 1); }
 
 template <typename T, int D, int NT>
 struct Narrow {
@@ -92,32 +91,84 @@ struct Narrow {
     static constexpr int KS = D / 16;                          // k-steps of S^T
     static constexpr int MT = D / 16;                          // m-tiles of O^T
     static constexpr size_t SLOT = (size_t)RT * (D + 2);       // floats of a partial
+    static constexpr int ES = (int)sizeof(T), ROW = D / 2;     // bytes of a scale, of a packed row
+    // a warp's stage: K rows, V rows, K params, V params of 16 keys, and whether their page is there
+    static constexpr int K_AT = 0, V_AT = 16 * ROW, KP_AT = 32 * ROW, VP_AT = KP_AT + 32 * ES, FLAG_AT = VP_AT + 32 * ES, STAGE = FLAG_AT + 16;
+    static constexpr int STAGES = sizeof(T) == 2 ? 5 : 4;
+    static constexpr int XO = D + 4;                           // floats between rows of the exchange buffer
+    static constexpr int SMEM = WARPS * STAGES * STAGE + WARPS * RT * (XO + 3) * 4 + WARPS * (D + 2) * 4;
+    static constexpr int BLOCKS = NT == 1 && sizeof(T) == 2 ? (D == 64 ? 4 : 3) : 2;      // CTAs an SM
+    // place of 16-byte piece c of packed row r
+    static __device__ __forceinline__ int piece(int r, int c) { return D == 128 ? r * 64 + ((c ^ ((r >> 1) & 2)) << 4) : r * 32 + (c << 4); }
 };
 
 template <typename T, int D, int NT>
-__global__ void __launch_bounds__(WARPS * 32, NT == 1 && sizeof(T) == 2 ? 4 : 2) k_attn_kv4(const Kv4AttnParams p) {
+__global__ void __launch_bounds__(WARPS * 32, Narrow<T, D, NT>::BLOCKS) k_attn_kv4(const Kv4AttnParams p) {
     using N = Narrow<T, D, NT>;
     using O_ = Op<T>;
-    constexpr int RT = N::RT, KW = N::KW, VW = N::VW, KS = N::KS, MT = N::MT, TERMS = O_::TERMS;
-    __shared__ int64_t sums[GHD_MAX_SEQS + 1];
+    constexpr int RT = N::RT, KW = N::KW, VW = N::VW, KS = N::KS, MT = N::MT, TERMS = O_::TERMS, XO = N::XO, es = N::ES;
+    extern __shared__ __align__(16) uint8_t smem[];
     __shared__ int64_t scratch[32];
-    __shared__ __align__(16) float xo[WARPS][RT][D + 4];
-    __shared__ float xm[WARPS][RT], xl[WARPS][RT], xs[WARPS][RT];
     __shared__ int arrived;
+    float* xo = reinterpret_cast<float*>(smem + WARPS * N::STAGES * N::STAGE);       // [WARPS][RT][XO]
+    float* xm = xo + WARPS * RT * XO;                                                // reference, sum, minimum's sum: [WARPS][RT] each
+    float* xl = xm + WARPS * RT;
+    float* xs = xl + WARPS * RT;
+    float* xmerge = xs + WARPS * RT;                                                 // [WARPS][D + 2]
+    int64_t* sums = reinterpret_cast<int64_t*>(smem + ((N::SMEM + 15) & ~15));       // [n_seqs + 1]
 
     const Kv4View& w = p.w;
-    const Kv4Tiling til{w.heads, p.group, RT, CHUNK};
+    const Kv4Tiling til{w.heads, p.group, RT, CHUNK, LEAD};
     const int64_t units = unit_sums(w, til, sums, scratch);
     const int64_t per = kv4_units_per_cta(units, p.ctas);
     int64_t u = per * blockIdx.x;
     const int64_t u_end = u + per < units ? u + per : units;
     const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5, g = lane >> 2, t = lane & 3;
     const int R = 1 << w.shift;
-    constexpr int es = (int)sizeof(T);
     const float sl2 = p.scale * KV4_LOG2E;
+    auto item_at = [&](int64_t x) { return kv4_find_item(til, sums, w.n_seqs, [&](int s_) { return kv4_load_seq(w, s_); }, x, u_end); };
 
+    // ---- this warp's ring: 16 keys a stage, STAGES - 1 units ahead, over the borders of items
+    uint8_t* ring = smem + warp * N::STAGES * N::STAGE;
+    const uint32_t ring_a = (uint32_t)__cvta_generic_to_shared(ring);
+    int64_t lu = u;
+    int lch = 0, lend = 0, lkeys = 0, lseq = 0, lhead = 0;
+    auto load_next = [&](int i) {
+        while (lch >= lend && lu < u_end) {
+            const Kv4Item it = item_at(lu);
+            lch = it.chunk0; lend = it.chunk0 + it.take; lkeys = kv4_tile_keys(til, it.q, it.tile); lseq = it.seq; lhead = it.head;
+            lu = it.next;
+        }
+        if (lch < lend) {
+            const int key0 = lch * CHUNK + warp * 16, r0 = key0 & (R - 1);
+            const int page = key0 < lkeys ? kv4_page(w, lseq, key0) : -1;
+            const uint8_t* blk = p.pool + kv4_block_at(w, page < 0 ? 0 : page, lhead);
+            const uint32_t st = ring_a + (uint32_t)(i % N::STAGES) * N::STAGE;
+            constexpr int PIECES = N::ROW / 16, PER = 32 / PIECES;                   // pieces of a row, rows a warp-wide copy covers
+#pragma unroll
+            for (int j = 0; j < 16 / PER; ++j) {
+                const int r = lane / PIECES + PER * j, c = lane % PIECES;
+                cp16(st + N::K_AT + N::piece(r, c), blk + kv4_code_at(R, D, 0, r0 + r) + 16 * c, page >= 0);
+                cp16(st + N::V_AT + N::piece(r, c), blk + kv4_code_at(R, D, 1, r0 + r) + 16 * c, page >= 0);
+            }
+            constexpr int PP = 2 * es;                                               // 16-byte pieces of 16 keys' scales and minima
+            if (lane < 2 * PP) {
+                const int which = lane / PP, c = lane % PP;
+                cp16(st + (which ? N::VP_AT : N::KP_AT) + 16 * c, blk + kv4_param_at(R, D, es, which, r0) + 16 * c, page >= 0);
+            }
+            if (lane == 0) *reinterpret_cast<int*>(ring + (i % N::STAGES) * N::STAGE + N::FLAG_AT) = page >= 0;
+            ++lch;
+        }
+        cp_commit();
+    };
+#pragma unroll
+    for (int i = 0; i < N::STAGES - 1; ++i) load_next(i);
+
+    int i = 0;                                                          // unit of this CTA
     while (u < u_end) {
-        const Kv4Item it = kv4_find_item(til, sums, w.n_seqs, [&](int s_) { return kv4_load_seq(w, s_); }, u, u_end);
+        const Kv4Item it = item_at(u);
+        u = it.next;
+        if (it.take == 0) continue;
         const int rows = min(RT, it.q.n * p.group - it.tile * RT);      // query rows of this tile
         const int keys = kv4_tile_keys(til, it.q, it.tile);
 
@@ -152,11 +203,6 @@ __global__ void __launch_bounds__(WARPS * 32, NT == 1 && sizeof(T) == 2 ? 4 : 2)
                 for (int e = 0; e < TERMS; ++e) { bq[nt][ks][e][0] = a[e]; bq[nt][ks][e][1] = b[e]; }
             }
         }
-        int node[NT][2];                                                // new row of score columns 2 t, 2 t + 1
-#pragma unroll
-        for (int nt = 0; nt < NT; ++nt)
-#pragma unroll
-            for (int e = 0; e < 2; ++e) node[nt][e] = (it.tile * RT + nt * 8 + 2 * t + e) / p.group;
 
         float o[MT][NT][4];
         float ref[NT][2], l[NT][2], ms[NT][2];
@@ -170,68 +216,78 @@ __global__ void __launch_bounds__(WARPS * 32, NT == 1 && sizeof(T) == 2 ? 4 : 2)
                 for (int e = 0; e < 4; ++e) o[mt][nt][e] = 0.f;
         }
 
-        for (int ch = it.chunk0; ch < it.chunk0 + it.take; ++ch) {
+        for (int ch = it.chunk0; ch < it.chunk0 + it.take; ++ch, ++i) {
+            __syncwarp();                                               // everybody has read the stage that is filled next
+            load_next(i + N::STAGES - 1);
+            cp_wait<N::STAGES - 1>();
+            __syncwarp();
+            const uint8_t* st = ring + (i % N::STAGES) * N::STAGE;
             const int key0 = ch * CHUNK + warp * 16;
-            if (key0 >= keys) continue;
-            const int page = kv4_page(w, it.seq, key0);
-            if (page < 0) continue;                                     // such keys are not visible
-            const uint8_t* blk = p.pool + kv4_block_at(w, page, it.head);
-            const int r0 = key0 & (R - 1);
-            // A-operand rows g and g + 8 are keys r0 + g and r0 + g + 8; a lane's channels [t D/4, (t + 1) D/4)
-            const Words<KW> k0 = load_words<KW>(blk + kv4_code_at(R, D, 0, r0 + g) + t * (D / 8));
-            const Words<KW> k1 = load_words<KW>(blk + kv4_code_at(R, D, 0, r0 + g + 8) + t * (D / 8));
-            float2 kp0 = load_params<T>(blk + kv4_param_at(R, D, es, 0, r0 + g)), kp1 = load_params<T>(blk + kv4_param_at(R, D, es, 0, r0 + g + 8));
-            float2 vp0 = load_params<T>(blk + kv4_param_at(R, D, es, 1, r0 + g)), vp1 = load_params<T>(blk + kv4_param_at(R, D, es, 1, r0 + g + 8));
-            // V: keys 2 t, 2 t + 1, 2 t + 8, 2 t + 9, a lane's channels [g D/8, (g + 1) D/8)
-            Words<VW> v[4];
-#pragma unroll
-            for (int e = 0; e < 4; ++e) v[e] = load_words<VW>(blk + kv4_code_at(R, D, 1, r0 + 2 * t + (e & 1) + 8 * (e >> 1)) + g * (D / 16));
+            if (key0 >= keys || !*reinterpret_cast<const int*>(st + N::FLAG_AT)) continue;      // keys of an unknown page are not visible
+            const int ka = key_of(g);                                   // operand rows g and g + 8 are keys ka and ka + 8
+            const float2 kp0 = param_of<T>(st + N::KP_AT, ka), kp1 = param_of<T>(st + N::KP_AT, ka + 8);
 
             float s[NT][4];
 #pragma unroll
             for (int nt = 0; nt < NT; ++nt)
 #pragma unroll
                 for (int e = 0; e < 4; ++e) s[nt][e] = 0.f;
+            {
+                uint32_t k0[KW], k1[KW];
+                if constexpr (D == 128) {
+                    const uint4 x = *reinterpret_cast<const uint4*>(st + N::K_AT + N::piece(ka, t)), y = *reinterpret_cast<const uint4*>(st + N::K_AT + N::piece(ka + 8, t));
+                    k0[0] = x.x; k0[1] = x.y; k0[2] = x.z; k0[3] = x.w;
+                    k1[0] = y.x; k1[1] = y.y; k1[2] = y.z; k1[3] = y.w;
+                } else {
+                    const uint2 x = *reinterpret_cast<const uint2*>(st + N::K_AT + ka * 32 + 8 * t), y = *reinterpret_cast<const uint2*>(st + N::K_AT + (ka + 8) * 32 + 8 * t);
+                    k0[0] = x.x; k0[1] = x.y;
+                    k1[0] = y.x; k1[1] = y.y;
+                }
 #pragma unroll
-            for (int i = 0; i < KW; ++i) {
+                for (int j = 0; j < KW; ++j) {
 #pragma unroll
-                for (int hlf = 0; hlf < 2; ++hlf) {
-                    const uint32_t wa = k0.w[i] >> (8 * hlf), wb = k1.w[i] >> (8 * hlf);
-                    const uint32_t a0 = O_::template centred<0>(wa), a1 = O_::template centred<0>(wb);
-                    const uint32_t a2 = O_::template centred<4>(wa), a3 = O_::template centred<4>(wb);
+                    for (int hlf = 0; hlf < 2; ++hlf) {
+                        const uint32_t wa = k0[j] >> (8 * hlf), wb = k1[j] >> (8 * hlf);
+                        const uint32_t a0 = O_::template centred<0>(wa), a1 = O_::template centred<0>(wb);
+                        const uint32_t a2 = O_::template centred<4>(wa), a3 = O_::template centred<4>(wb);
 #pragma unroll
-                    for (int nt = 0; nt < NT; ++nt)
+                        for (int nt = 0; nt < NT; ++nt)
 #pragma unroll
-                        for (int e = 0; e < TERMS; ++e) O_::mma(s[nt], a0, a1, a2, a3, bq[nt][2 * i + hlf][e][0], bq[nt][2 * i + hlf][e][1]);
+                            for (int e = 0; e < TERMS; ++e) O_::mma(s[nt], a0, a1, a2, a3, bq[nt][2 * j + hlf][e][0], bq[nt][2 * j + hlf][e][1]);
+                    }
                 }
             }
-            const float ks0 = kp0.x * sl2, ks1 = kp1.x * sl2;
+            // scores (in powers of two): key g rows 2 t, 2 t + 1, then key g + 8; a pair of rows shares its key's scale
+            const F2 ks0 = f2(kp0.x * sl2, kp0.x * sl2), ks1 = f2(kp1.x * sl2, kp1.x * sl2);
             const float km0 = fmaf(8.f, kp0.x, kp0.y) * sl2, km1 = fmaf(8.f, kp1.x, kp1.y) * sl2;
-            bool vis[NT][4];
+#pragma unroll
+            for (int nt = 0; nt < NT; ++nt) {
+                const F2 q2 = f2(qs[nt][0], qs[nt][1]);
+                f2_get(f2_fma(ks0, f2(s[nt][0], s[nt][1]), f2_mul(f2(km0, km0), q2)), s[nt][0], s[nt][1]);
+                f2_get(f2_fma(ks1, f2(s[nt][2], s[nt][3]), f2_mul(f2(km1, km1), q2)), s[nt][2], s[nt][3]);
+            }
             const bool all = key0 + 16 <= it.q.len;
-#pragma unroll
-            for (int nt = 0; nt < NT; ++nt)
-#pragma unroll
-                for (int e = 0; e < 4; ++e) {
-                    s[nt][e] = (e < 2) ? fmaf(ks0, s[nt][e], km0 * qs[nt][e & 1]) : fmaf(ks1, s[nt][e], km1 * qs[nt][e & 1]);
-                    vis[nt][e] = true;
-                }
+            uint32_t vis = 0xffffffffu;
             if (!all) {
+                vis = 0u;
 #pragma unroll
                 for (int nt = 0; nt < NT; ++nt)
 #pragma unroll
-                    for (int e = 0; e < 4; ++e) {
-                        const int j = key0 + g + 8 * (e >> 1) - it.q.len;
-                        const bool ok = j < 0 || sees_new(p, it.q, node[nt][e & 1], j);
-                        vis[nt][e] = ok;
-                        if (!ok) s[nt][e] = -INFINITY;
+                    for (int e = 0; e < 2; ++e) {
+                        const uint32_t b = sees(p, it.q, (it.tile * RT + nt * 8 + 2 * t + e) / p.group, key0 + ka - it.q.len);
+                        vis |= ((b & 1u) << (4 * nt + e)) | (((b >> 8) & 1u) << (4 * nt + e + 2));
                     }
+#pragma unroll
+                for (int nt = 0; nt < NT; ++nt)
+#pragma unroll
+                    for (int e = 0; e < 4; ++e)
+                        if (!((vis >> (4 * nt + e)) & 1u)) s[nt][e] = -INFINITY;
             }
             bool over = false;
 #pragma unroll
             for (int nt = 0; nt < NT; ++nt)
 #pragma unroll
-                for (int e = 0; e < 4; ++e) over = over || (s[nt][e] - ref[nt][e & 1] > RAISE);
+                for (int e = 0; e < 2; ++e) over = over || (fmaxf(s[nt][e], s[nt][e + 2]) - ref[nt][e] > RAISE);
             if (__any_sync(0xffffffffu, over)) {
 #pragma unroll
                 for (int nt = 0; nt < NT; ++nt)
@@ -252,38 +308,55 @@ __global__ void __launch_bounds__(WARPS * 32, NT == 1 && sizeof(T) == 2 ? 4 : 2)
                     }
             }
             uint32_t bp[NT][TERMS][2];
+            const float2 vp0 = param_of<T>(st + N::VP_AT, ka), vp1 = param_of<T>(st + N::VP_AT, ka + 8);
             const float vm0 = fmaf(8.f, vp0.x, vp0.y), vm1 = fmaf(8.f, vp1.x, vp1.y);
 #pragma unroll
             for (int nt = 0; nt < NT; ++nt) {
-                float ps[4];
+                float ps[4], pm[4];
 #pragma unroll
                 for (int e = 0; e < 4; ++e) {
                     const float rf = ref[nt][e & 1];
-                    float pe = ex2(s[nt][e] - (rf == -INFINITY ? 0.f : rf));
-                    float a = pe * (e < 2 ? vp0.x : vp1.x), b = pe * (e < 2 ? vm0 : vm1);
-                    if (!all && !vis[nt][e]) pe = a = b = 0.f;
+                    const float pe = ex2(s[nt][e] - (rf == -INFINITY ? 0.f : rf));
                     l[nt][e & 1] += pe;
-                    ms[nt][e & 1] += b;
-                    ps[e] = a;
+                    ps[e] = pe * (e < 2 ? vp0.x : vp1.x);
+                    pm[e] = pe * (e < 2 ? vm0 : vm1);
                 }
+                if (!all) {                                             // by selection: what a key holds stays out of rows that do not see it
+#pragma unroll
+                    for (int e = 0; e < 4; ++e)
+                        if (!((vis >> (4 * nt + e)) & 1u)) ps[e] = pm[e] = 0.f;
+                }
+                ms[nt][0] += pm[0] + pm[2];
+                ms[nt][1] += pm[1] + pm[3];
                 uint32_t x[TERMS], y[TERMS];
                 O_::split(ps[0], ps[1], x);
                 O_::split(ps[2], ps[3], y);
 #pragma unroll
                 for (int e = 0; e < TERMS; ++e) { bp[nt][e][0] = transpose8x8(x[e]); bp[nt][e][1] = transpose8x8(y[e]); }
             }
-            // O^T: m-tile mt holds the lane's channels 2 mt (operand row g) and 2 mt + 1 (row g + 8)
+            // O^T: m-tile mt holds the lane's channels 2 mt (operand row g) and 2 mt + 1 (row g + 8) of the D/8 from g D/8 on
+            uint32_t v[4][VW];
 #pragma unroll
-            for (int i = 0; i < VW; ++i)
+            for (int e = 0; e < 4; ++e) {
+                const int r = key_of(2 * t + (e & 1)) + 8 * (e >> 1);
+                if constexpr (D == 128) {
+                    const uint2 x = *reinterpret_cast<const uint2*>(st + N::V_AT + N::piece(r, g >> 1) + 8 * (g & 1));
+                    v[e][0] = x.x; v[e][1] = x.y;
+                } else {
+                    v[e][0] = *reinterpret_cast<const uint32_t*>(st + N::V_AT + r * 32 + 4 * g);
+                }
+            }
+#pragma unroll
+            for (int j = 0; j < VW; ++j)
 #pragma unroll
                 for (int z = 0; z < 2; ++z) {                           // half words of the two keys of a pair side by side
-                    const uint32_t x = __byte_perm(v[0].w[i], v[1].w[i], z ? 0x7632 : 0x5410), y = __byte_perm(v[2].w[i], v[3].w[i], z ? 0x7632 : 0x5410);
+                    const uint32_t x = __byte_perm(v[0][j], v[1][j], z ? 0x7632 : 0x5410), y = __byte_perm(v[2][j], v[3][j], z ? 0x7632 : 0x5410);
 #pragma unroll
                     for (int hlf = 0; hlf < 2; ++hlf) {
                         const uint32_t xs_ = x >> (8 * hlf), ys_ = y >> (8 * hlf);
                         const uint32_t a0 = O_::template centred<0>(xs_), a1 = O_::template centred<4>(xs_);
                         const uint32_t a2 = O_::template centred<0>(ys_), a3 = O_::template centred<4>(ys_);
-                        const int mt = 4 * i + 2 * z + hlf;
+                        const int mt = 4 * j + 2 * z + hlf;
 #pragma unroll
                         for (int nt = 0; nt < NT; ++nt)
 #pragma unroll
@@ -301,10 +374,11 @@ __global__ void __launch_bounds__(WARPS * 32, NT == 1 && sizeof(T) == 2 ? 4 : 2)
 #pragma unroll
                 for (int x = 4; x < 32; x <<= 1) { a += __shfl_xor_sync(0xffffffffu, a, x); b += __shfl_xor_sync(0xffffffffu, b, x); }
                 const int rl = nt * 8 + 2 * t + e;
-                if (g == 0) { xm[warp][rl] = ref[nt][e]; xl[warp][rl] = a; xs[warp][rl] = b; }
+                if (rl >= rows) continue;
+                if (g == 0) { xm[warp * RT + rl] = ref[nt][e]; xl[warp * RT + rl] = a; xs[warp * RT + rl] = b; }
 #pragma unroll
                 for (int mt = 0; mt < MT; mt += 2)
-                    *reinterpret_cast<float4*>(&xo[warp][rl][g * (D / 8) + 2 * mt]) = make_float4(o[mt][nt][e], o[mt][nt][e + 2], o[mt + 1][nt][e], o[mt + 1][nt][e + 2]);
+                    *reinterpret_cast<float4*>(xo + (warp * RT + rl) * XO + g * (D / 8) + 2 * mt) = make_float4(o[mt][nt][e], o[mt][nt][e + 2], o[mt + 1][nt][e], o[mt + 1][nt][e + 2]);
             }
         __syncthreads();
         const int64_t c0 = it.first / per, c1 = (it.first + it.chunks - 1) / per;      // CTAs that share the item
@@ -312,19 +386,19 @@ __global__ void __launch_bounds__(WARPS * 32, NT == 1 && sizeof(T) == 2 ? 4 : 2)
         float* slot = p.part + ((size_t)blockIdx.x * 2 + ((int64_t)blockIdx.x == c0 ? 1 : 0)) * N::SLOT;
         for (int x = threadIdx.x; x < rows * (D / 4); x += WARPS * 32) {
             const int rl = x / (D / 4), c = 4 * (x % (D / 4));
-            float m = xm[0][rl];
+            float m = xm[rl];
 #pragma unroll
-            for (int k = 1; k < WARPS; ++k) m = fmaxf(m, xm[k][rl]);
+            for (int k = 1; k < WARPS; ++k) m = fmaxf(m, xm[k * RT + rl]);
             float4 a = make_float4(0.f, 0.f, 0.f, 0.f);
             float lsum = 0.f;
 #pragma unroll
             for (int k = 0; k < WARPS; ++k) {
-                if (xm[k][rl] == -INFINITY && xl[k][rl] == 0.f) continue;   // a warp that saw nothing (a NaN goes on)
-                const float f = ex2(xm[k][rl] - m);
-                const float4 b = *reinterpret_cast<const float4*>(&xo[k][rl][c]);
-                const float mm = xs[k][rl];
+                const int at = k * RT + rl;
+                if (xm[at] == -INFINITY && xl[at] == 0.f) continue;      // a warp that saw nothing (a NaN goes on)
+                const float f = ex2(xm[at] - m), mm = xs[at];
+                const float4 b = *reinterpret_cast<const float4*>(xo + at * XO + c);
                 a.x += f * (b.x + mm); a.y += f * (b.y + mm); a.z += f * (b.z + mm); a.w += f * (b.w + mm);
-                lsum += f * xl[k][rl];
+                lsum += f * xl[at];
             }
             if (whole) {
                 const int rr = it.tile * RT + rl;
@@ -346,21 +420,25 @@ __global__ void __launch_bounds__(WARPS * 32, NT == 1 && sizeof(T) == 2 ? 4 : 2)
                 __threadfence();
             }
             __syncthreads();
-            if (arrived) {
-                merge_item<T, D>(p, it, RT, rows, c0, c1, threadIdx.x, WARPS * 32);
-            }
+            if (arrived) merge_item<T, D, WARPS>(p, it, RT, rows, c0, c1, warp, xmerge, [] { __syncthreads(); });
         }
         __syncthreads();                                                 // the exchange buffers are written again
-        u += it.take;
     }
+    cp_wait<0>();
 }
 
 template <typename T, int D, int NT>
 ghd_status launch_narrow(ghd_ctx* c, Kv4AttnParams& p) {
-    p.ctas = c->sm_count * (NT == 1 && sizeof(T) == 2 ? 4 : 2);
+    using N = Narrow<T, D, NT>;
+    const int smem = ((N::SMEM + 15) & ~15) + (p.w.n_seqs + 1) * 8;
+    if (cudaFuncSetAttribute(k_attn_kv4<T, D, NT>, cudaFuncAttributeMaxDynamicSharedMemorySize, smem) != cudaSuccess) {
+        cudaGetLastError();
+        return fail(c, GHD_ECUDA, "kv4_attention: cannot raise dynamic shared memory");
+    }
+    p.ctas = c->sm_count * N::BLOCKS;
     const size_t have = (size_t)c->sm_count * 2 * 256 * 128;             // floats of the tile scratch (carve_workspace)
-    if ((size_t)p.ctas * 2 * Narrow<T, D, NT>::SLOT > have || p.ctas > 4096) return fail(c, GHD_ENOSPACE, "kv4_attention: workspace too small");
-    launch_k(c, false, k_attn_kv4<T, D, NT>, dim3(p.ctas), dim3(WARPS * 32), 0, p);
+    if ((size_t)p.ctas * 2 * N::SLOT > have || p.ctas > 4096) return fail(c, GHD_ENOSPACE, "kv4_attention: workspace too small");
+    launch_k(c, false, k_attn_kv4<T, D, NT>, dim3(p.ctas), dim3(WARPS * 32), smem, p);
     return GHD_OK;
 }
 

@@ -46,11 +46,29 @@ template <> __device__ __forceinline__ void store4<__half>(__half* p, float a, f
     *reinterpret_cast<uint2*>(p) = make_uint2(*reinterpret_cast<const uint32_t*>(&lo), *reinterpret_cast<const uint32_t*>(&hi));
 }
 
-// Whether new row i of a sequence sees the new row j >= 0 (j <= i, and the mask's bit when there is a mask).
-__device__ __forceinline__ bool sees_new(const Kv4AttnParams& p, const Kv4Seq& q, int i, int j) {
-    if (j > i || j >= q.n_new || i >= q.n) return false;
-    if (!p.mask) return true;
-    return (j >> 6) < p.mask_words && ((__ldg(p.mask + (size_t)(q.row0 + i) * p.mask_words + (j >> 6)) >> (j & 63)) & 1ull);
+template <typename T> __device__ __forceinline__ void store2(T* p, float a, float b);
+template <> __device__ __forceinline__ void store2<float>(float* p, float a, float b) { *reinterpret_cast<float2*>(p) = make_float2(a, b); }
+template <> __device__ __forceinline__ void store2<__half>(__half* p, float a, float b) { *reinterpret_cast<__half2*>(p) = __floats2half2_rn(a, b); }
+
+__device__ __forceinline__ void cp16(uint32_t dst, const void* src, bool there) {     // 16 bytes, or zeros when they are not there
+    asm volatile("cp.async.cg.shared.global [%0], [%1], 16, %2;" ::"r"(dst), "l"(src), "r"(there ? 16 : 0) : "memory");
+}
+__device__ __forceinline__ void cp_commit() { asm volatile("cp.async.commit_group;" ::: "memory"); }
+template <int N> __device__ __forceinline__ void cp_wait() { asm volatile("cp.async.wait_group %0;" ::"n"(N) : "memory"); }
+
+// Which of the keys j0 .. j0 + 31 (numbers among the sequence's new rows; below 0: cache rows) new row i sees: bit d for
+// j0 + d.  Cache rows are seen; new rows up to i itself, where the mask's bit is set (without a mask: all of them).
+// No branch depends on a load, so that the words of many rows are fetched together.
+__device__ __forceinline__ uint32_t sees(const Kv4AttnParams& p, const Kv4Seq& q, int i, int j0) {
+    auto low = [](int n) -> uint32_t { return n >= 32 ? 0xffffffffu : (n <= 0 ? 0u : (1u << n) - 1u); };
+    uint32_t w = 0xffffffffu;
+    if (p.mask) {
+        const int at = j0 >> 6, sh = j0 & 63;                    // floor: -1 and below are cache rows
+        const uint64_t* row = p.mask + (size_t)(q.row0 + min(i, q.n - 1)) * p.mask_words;
+        const uint64_t a = at >= 0 && at < p.mask_words ? __ldg(row + at) : 0ull, b = at + 1 >= 0 && at + 1 < p.mask_words ? __ldg(row + at + 1) : 0ull;
+        w = (uint32_t)(sh ? (a >> sh) | (b << (64 - sh)) : a);
+    }
+    return low(-j0) | (w & low(min(i, q.n_new - 1) + 1 - j0));
 }
 
 // Codes of half type, less 8, for the two nibbles at bits SH .. SH + 3 of the half words of w: (w & mask) | exponent is
@@ -94,28 +112,99 @@ __device__ __forceinline__ int64_t unit_sums(const Kv4View& w, const Kv4Tiling& 
     return sums[w.n_seqs];
 }
 
-// Adds the partial sums that CTAs c0 .. c1 left of one item, in that order, and writes its rows.  NT threads take part.
-template <typename T, int D>
-__device__ __forceinline__ void merge_item(const Kv4AttnParams& p, const Kv4Item& it, int tile_rows, int rows, int64_t c0, int64_t c1, int tid, int nt) {
+// Two 32-bit floats in one register pair, worked on by one instruction.
+struct F2 { uint64_t v; };
+__device__ __forceinline__ F2 f2(float a, float b) { F2 r; asm("mov.b64 %0, {%1, %2};" : "=l"(r.v) : "f"(a), "f"(b)); return r; }
+__device__ __forceinline__ void f2_get(F2 x, float& a, float& b) { asm("mov.b64 {%0, %1}, %2;" : "=f"(a), "=f"(b) : "l"(x.v)); }
+__device__ __forceinline__ F2 f2_fma(F2 a, F2 b, F2 c) { F2 r; asm("fma.rn.f32x2 %0, %1, %2, %3;" : "=l"(r.v) : "l"(a.v), "l"(b.v), "l"(c.v)); return r; }
+__device__ __forceinline__ F2 f2_add(F2 a, F2 b) { F2 r; asm("add.rn.f32x2 %0, %1, %2;" : "=l"(r.v) : "l"(a.v), "l"(b.v)); return r; }
+__device__ __forceinline__ F2 f2_mul(F2 a, F2 b) { F2 r; asm("mul.rn.f32x2 %0, %1, %2;" : "=l"(r.v) : "l"(a.v), "l"(b.v)); return r; }
+
+// Adds the partial sums that CTAs c0 .. c1 left of one item, in that order, and writes its rows.  A warp takes a row (the
+// lanes hold D / 32 channels each); with fewer rows than warps several warps share a row's contributors and meet in
+// `xch`, floats [warps][D + 2].  Loads run eight contributors ahead: their latency is what the merge would otherwise
+// cost.  `sync` is a barrier of the NW warps that take part.
+template <typename T, int D, int NW, typename Sync>
+__device__ __forceinline__ void merge_item(const Kv4AttnParams& p, const Kv4Item& it, int tile_rows, int rows, int64_t c0, int64_t c1, int warp, float* xch, Sync sync) {
+    constexpr int VL = D / 32;
     const size_t slot = (size_t)tile_rows * (D + 2);
-    for (int x = tid; x < rows * (D / 4); x += nt) {
-        const int rl = x / (D / 4), c = 4 * (x % (D / 4));
-        float m = -INFINITY, lsum = 0.f;
-        float4 a = make_float4(0.f, 0.f, 0.f, 0.f);
-        for (int64_t k = c0; k <= c1; ++k) {
-            const float* sl = p.part + ((size_t)k * 2 + (k == c0 ? 1 : 0)) * slot;
-            const float2 ml = __ldcg(reinterpret_cast<const float2*>(sl + (size_t)tile_rows * D + 2 * rl));
-            const float4 b = __ldcg(reinterpret_cast<const float4*>(sl + (size_t)rl * D + c));
-            if (ml.x == -INFINITY && ml.y == 0.f) continue;      // saw nothing (a NaN goes on)
-            const float mn = fmaxf(m, ml.x), fa = m == -INFINITY ? 0.f : ex2(m - mn), fb = ex2(ml.x - mn);
-            a.x = a.x * fa + b.x * fb; a.y = a.y * fa + b.y * fb; a.z = a.z * fa + b.z * fb; a.w = a.w * fa + b.w * fb;
-            lsum = lsum * fa + ml.y * fb;
-            m = mn;
+    const int lane = threadIdx.x & 31, n = (int)(c1 - c0) + 1;
+    int share = 1;                                               // warps a row: a power of two
+    while (share * 2 * rows <= NW && share * 16 <= n) share *= 2;
+    const int sub = warp % share;
+    const int k_beg = (int)((int64_t)n * sub / share), k_end = (int)((int64_t)n * (sub + 1) / share);
+    auto slot_of = [&](int k) { return p.part + ((size_t)(c0 + k) * 2 + (k == 0 ? 1 : 0)) * slot; };
+    for (int rl0 = 0; rl0 < rows; rl0 += NW / share) {
+        const int rl = rl0 + warp / share;
+        float m = -INFINITY, lsum = 0.f, a[VL];
+#pragma unroll
+        for (int e = 0; e < VL; ++e) a[e] = 0.f;
+        if (rl < rows) {
+            for (int kb = k_beg; kb < k_end; kb += 8) {
+                float2 ml[8];
+                float v[8][VL];
+#pragma unroll
+                for (int k = 0; k < 8; ++k) {
+                    ml[k] = make_float2(-INFINITY, 0.f);
+                    if (kb + k < k_end) {
+                        const float* sl = slot_of(kb + k);
+                        ml[k] = __ldcg(reinterpret_cast<const float2*>(sl + (size_t)tile_rows * D + 2 * rl));
+                        const float* src = sl + (size_t)rl * D + VL * lane;
+                        if constexpr (VL == 4) { const float4 x = __ldcg(reinterpret_cast<const float4*>(src)); v[k][0] = x.x; v[k][1] = x.y; v[k][2] = x.z; v[k][3] = x.w; }
+                        else { const float2 x = __ldcg(reinterpret_cast<const float2*>(src)); v[k][0] = x.x; v[k][1] = x.y; }
+                    }
+                }
+                float mn = m;
+#pragma unroll
+                for (int k = 0; k < 8; ++k) mn = fmaxf(mn, ml[k].x);
+                const float f = m == -INFINITY ? (lsum == 0.f ? 0.f : 1.f) : ex2(m - mn);     // keeps a NaN
+                lsum *= f;
+#pragma unroll
+                for (int e = 0; e < VL; ++e) a[e] *= f;
+#pragma unroll
+                for (int k = 0; k < 8; ++k) {
+                    if (ml[k].x == -INFINITY && ml[k].y == 0.f) continue;                     // not there, or saw nothing (a NaN goes on)
+                    const float g = ex2(ml[k].x - mn);
+                    lsum = fmaf(ml[k].y, g, lsum);
+#pragma unroll
+                    for (int e = 0; e < VL; ++e) a[e] = fmaf(v[k][e], g, a[e]);
+                }
+                m = mn;
+            }
         }
-        const int rr = it.tile * tile_rows + rl;
-        const float inv = lsum == 0.f ? 0.f : 1.f / lsum;
-        T* dst = (T*)p.out + ((size_t)(it.q.row0 + rr / p.group) * p.q_heads + it.head * p.group + rr % p.group) * D + c;
-        store4<T>(dst, a.x * inv, a.y * inv, a.z * inv, a.w * inv);
+        if (share > 1) {
+            float* mine = xch + (size_t)warp * (D + 2);
+#pragma unroll
+            for (int e = 0; e < VL; ++e) mine[VL * lane + e] = a[e];
+            if (lane == 0) { mine[D] = m; mine[D + 1] = lsum; }
+            sync();
+            if (sub == 0 && rl < rows) {
+                float mn = m;
+                for (int k = 1; k < share; ++k) mn = fmaxf(mn, mine[(size_t)k * (D + 2) + D]);
+                float ls = 0.f, b[VL];
+#pragma unroll
+                for (int e = 0; e < VL; ++e) b[e] = 0.f;
+                for (int k = 0; k < share; ++k) {
+                    const float* x = mine + (size_t)k * (D + 2);
+                    if (x[D] == -INFINITY && x[D + 1] == 0.f) continue;
+                    const float g = ex2(x[D] - mn);
+                    ls = fmaf(x[D + 1], g, ls);
+#pragma unroll
+                    for (int e = 0; e < VL; ++e) b[e] = fmaf(x[VL * lane + e], g, b[e]);
+                }
+                lsum = ls;
+#pragma unroll
+                for (int e = 0; e < VL; ++e) a[e] = b[e];
+            }
+            sync();                                              // xch is written again
+        }
+        if (rl < rows && sub == 0) {
+            const int rr = it.tile * tile_rows + rl;
+            const float inv = lsum == 0.f ? 0.f : 1.f / lsum;
+            T* dst = (T*)p.out + ((size_t)(it.q.row0 + rr / p.group) * p.q_heads + it.head * p.group + rr % p.group) * D + VL * lane;
+            if constexpr (VL == 4) store4<T>(dst, a[0] * inv, a[1] * inv, a[2] * inv, a[3] * inv);
+            else store2<T>(dst, a[0] * inv, a[1] * inv);
+        }
     }
 }
 

@@ -21,6 +21,7 @@
 // written and read, 16 KB of queries read, 16 KB of codes in and out.  Work is dealt as in attn_kv4.cu, one CTA an SM.
 #include <cstddef>
 #include <cstdio>
+#include <type_traits>
 
 #include "attn_kv4_dev.cuh"
 #include "tc_common.cuh"
@@ -34,8 +35,12 @@ using namespace kv4;
 
 constexpr int UNIT = 128;                      // keys of a unit (MMA M of S^T, MMA K of O^T)
 constexpr int SOFT = 256, CONV = 128;          // threads of the softmax and of the unpacking warps
-constexpr int THREADS = SOFT + CONV + 64;
+constexpr int THREADS = SOFT + CONV + 128;   // the last warpgroup: two issuers and two idle warps (register counts change by warpgroups)
+// registers a thread after the split: 256 x 176 + 128 x 96 + 128 x 56 = 64512 of the 512 x 128 = 65536 launched with
+constexpr int REGS_SOFT = 176, REGS_CONV = 96, REGS_ISSUE = 56;
+static_assert(SOFT * REGS_SOFT + CONV * REGS_CONV + 128 * REGS_ISSUE <= THREADS * 128, "register split");
 constexpr float RAISE = 8.f;
+constexpr int LEAD = 6;                        // an item's fixed cost in units
 constexpr uint32_t V_SLAB = UNIT * 128;        // [128 keys x 64 channels] half
 
 template <int D, int N>
@@ -56,6 +61,7 @@ struct Ctrl {
     alignas(16) float qs[128];       // sums of the tile's queries
     alignas(16) float fac[128];      // factors of a rescale, by row
     float x[4][128], y[4][128];      // exchange between the four warps that share rows
+    float merge[8 * 130];            // warps that share a row's partial sums
     float vmax[2][4];                // largest of V's scales of a unit, by half and warp
     int64_t scratch[32];
     int64_t sums[GHD_MAX_SEQS + 1];
@@ -82,8 +88,8 @@ __device__ __forceinline__ void mma_ts(uint32_t d_tmem, uint32_t a_tmem, uint64_
         "tcgen05.mma.cta_group::1.kind::f16 [%0], [%1], %2, %3, p;\n\t}"
         ::"r"(d_tmem), "r"(a_tmem), "l"(bdesc), "r"(idesc), "r"(accumulate) : "memory");
 }
-__device__ __forceinline__ void cp16(uint32_t dst, const void* src, bool there) {     // zeros when the row is not there
-    asm volatile("cp.async.cg.shared.global [%0], [%1], 16, %2;" ::"r"(dst), "l"(src), "r"(there ? 16 : 0) : "memory");
+__device__ __forceinline__ void st_frag(uint32_t taddr, const uint32_t (&r)[4]) {
+    asm volatile("tcgen05.st.sync.aligned.16x256b.x1.b32 [%0], {%1, %2, %3, %4};" ::"r"(taddr), "r"(r[0]), "r"(r[1]), "r"(r[2]), "r"(r[3]) : "memory");
 }
 __device__ __forceinline__ void stmatrix4(uint32_t addr, uint32_t a, uint32_t b, uint32_t c, uint32_t d) {
     asm volatile("stmatrix.sync.aligned.m8n8.x4.shared.b16 [%0], {%1, %2, %3, %4};" ::"r"(addr), "r"(a), "r"(b), "r"(c), "r"(d) : "memory");
@@ -148,7 +154,7 @@ __global__ void __launch_bounds__(THREADS, 1) k_attn_kv4_tc(const Kv4AttnParams 
         asm volatile("tcgen05.relinquish_alloc_permit.cta_group::1.sync.aligned;" ::: "memory");
     }
     const Kv4View& w = p.w;
-    const Kv4Tiling til{w.heads, p.group, N, UNIT};
+    const Kv4Tiling til{w.heads, p.group, N, UNIT, LEAD};
     tc_fence_before();
     const int64_t units = unit_sums(w, til, sm->sums, sm->scratch);      // two block barriers inside
     tc_fence_after();
@@ -161,16 +167,21 @@ __global__ void __launch_bounds__(THREADS, 1) k_attn_kv4_tc(const Kv4AttnParams 
     auto cols_of = [&](int rows) { return (rows + 15) & ~15; };           // MMA N: a multiple of 16
 
     if (warp >= 8 && warp < 12) {
+        asm volatile("setmaxnreg.dec.sync.aligned.u32 %0;" ::"n"(REGS_CONV));
         // ------------------------------------------------ unpacking warps: thread = key
         const int quad = warp - 8, key = quad * 32 + lane;
         const uint32_t st0 = base_a + SH::ST_AT + quad * 32 * (D / 2);    // this warp's 32 rows of a stage (K; V UNIT rows further)
         const int R = 1 << w.shift;
         int64_t lu = u_beg;                                               // load cursor
         Kv4Item it{};
-        int lch = 0, lend = 0, lkeys = 0;
+        int lch = 0, lend = 0, lkeys = 0, n = 0;                          // n: units asked for so far
         auto load_next = [&](int i) {
-            if (lu < u_end) {
-                if (lch >= lend) { it = item_at(lu); lch = it.chunk0; lend = it.chunk0 + it.take; lkeys = kv4_tile_keys(til, it.q, it.tile); }
+            while (lch >= lend && lu < u_end) {
+                it = item_at(lu);
+                lch = it.chunk0; lend = it.chunk0 + it.take; lkeys = kv4_tile_keys(til, it.q, it.tile);
+                lu = it.next;
+            }
+            if (lch < lend) {
                 const uint32_t st = st0 + (uint32_t)(i % SH::STAGES) * SH::ST_BYTES;
                 const int key0 = lch * UNIT + quad * 32;
                 int page[2];                                              // of this warp's two groups of 16 keys
@@ -187,19 +198,18 @@ __global__ void __launch_bounds__(THREADS, 1) k_attn_kv4_tc(const Kv4AttnParams 
                     cp16(st + UNIT * (D / 2) + piece_at<D>(row, c), blk + kv4_code_at(R, D, 1, r) + 16 * c, pg >= 0);
                 }
                 ++lch;
-                ++lu;
+                ++n;
             }
-            asm volatile("cp.async.commit_group;" ::: "memory");
+            cp_commit();
         };
-        const int n = (int)(u_end > u_beg ? u_end - u_beg : 0);
 #pragma unroll
         for (int i = 0; i < SH::STAGES - 1; ++i) load_next(i);
-        for (int i = 0; i < n; ++i) {
+        for (int i = 0; i < n; ++i) {                                     // (n runs ahead until the last unit has been asked for)
             const int b = i & 1;
             const uint32_t st = st0 + (uint32_t)(i % SH::STAGES) * SH::ST_BYTES;
             __syncwarp();                                                 // everybody has read the stage that is filled next
             load_next(i + SH::STAGES - 1);
-            asm volatile("cp.async.wait_group %0;" ::"n"(SH::STAGES - 1) : "memory");
+            cp_wait<SH::STAGES - 1>();
             __syncwarp();
             if (i >= 2) mbar_wait(smem_u32(&sm->k_empty[b]), ((i >> 1) - 1) & 1, abort_flag, w.status, DEV_TIMEOUT_TMEM);
             tc_fence_after();
@@ -226,17 +236,22 @@ __global__ void __launch_bounds__(THREADS, 1) k_attn_kv4_tc(const Kv4AttnParams 
             asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
             mbar_arrive(smem_u32(&sm->v_full[b]));
         }
-        asm volatile("cp.async.wait_all;" ::: "memory");
-    } else if (warp == 12) {
+        cp_wait<0>();
+    } else if (warp >= 12) {
+        asm volatile("setmaxnreg.dec.sync.aligned.u32 %0;" ::"n"(REGS_ISSUE));
+        if (warp == 12) {
         // ------------------------------------------------ issuer of S^T = K Q^T
         if (lane == 0) {
             const uint64_t q_desc = smem_desc_sw128(base_a);
             bool ok = true;
             int i = 0, items = 0;
-            for (int64_t u = u_beg; ok && u < u_end; ++items) {
+            for (int64_t u = u_beg; ok && u < u_end;) {
                 const Kv4Item it = item_at(u);
+                u = it.next;
+                if (it.take == 0) continue;
                 const uint32_t idesc = instr_desc_f16(cols_of(rows_of(it)), false);
                 ok = mbar_wait(smem_u32(&sm->q_full), items & 1, abort_flag, w.status, DEV_TIMEOUT_MMA);
+                ++items;
                 for (int k = 0; ok && k < it.take; ++k, ++i) {
                     const int b = i & 1;
                     ok = mbar_wait(smem_u32(&sm->k_full[b]), (i >> 1) & 1, abort_flag, w.status, DEV_TIMEOUT_MMA);
@@ -250,14 +265,13 @@ __global__ void __launch_bounds__(THREADS, 1) k_attn_kv4_tc(const Kv4AttnParams 
                     tc_commit(smem_u32(&sm->s_full[b]));
                     tc_commit(smem_u32(&sm->k_empty[b]));
                 }
-                u += it.take;
             }
             if (!ok) {
                 tc_commit(smem_u32(&sm->drain));
                 for (uint32_t spin = 0; spin < SPIN_LIMIT && !mbar_try(smem_u32(&sm->drain), 0); ++spin) __nanosleep(64);
             }
         }
-    } else if (warp == 13) {
+        } else if (warp == 13) {
         // ------------------------------------------------ issuer of O^T += V^T P^T
         if (lane == 0) {
             // both operands have the MMA's K dimension (keys) as rows of 128 bytes: 64 channels of V, 64 query rows of P
@@ -267,6 +281,7 @@ __global__ void __launch_bounds__(THREADS, 1) k_attn_kv4_tc(const Kv4AttnParams 
             int i = 0;
             for (int64_t u = u_beg; ok && u < u_end;) {
                 const Kv4Item it = item_at(u);
+                u = it.next;
                 const uint32_t idesc = instr_desc_f16(cols_of(rows_of(it)), true) | (1u << 15);
                 for (int k = 0; ok && k < it.take; ++k, ++i) {
                     const int b = i & 1;
@@ -281,14 +296,15 @@ __global__ void __launch_bounds__(THREADS, 1) k_attn_kv4_tc(const Kv4AttnParams 
                     tc_commit(smem_u32(&sm->v_empty[b]));
                     tc_commit(smem_u32(&sm->p_empty[b]));
                 }
-                u += it.take;
             }
             if (!ok) {
                 tc_commit(smem_u32(&sm->drain_pv));
                 for (uint32_t spin = 0; spin < SPIN_LIMIT && !mbar_try(smem_u32(&sm->drain_pv), 0); ++spin) __nanosleep(64);
             }
         }
-    } else if (warp < 8) {
+        }
+    } else {
+        asm volatile("setmaxnreg.inc.sync.aligned.u32 %0;" ::"n"(REGS_SOFT));
         // ------------------------------------------------ softmax warps
         // half: which blocks of eight query rows (half, half + 2, ...); quad: which 32 keys (tensor-memory lanes)
         const int half = warp >> 2, quad = warp & 3, g = lane >> 2, t = lane & 3, tid = threadIdx.x;
@@ -297,6 +313,8 @@ __global__ void __launch_bounds__(THREADS, 1) k_attn_kv4_tc(const Kv4AttnParams 
         int i = 0;                                                        // unit of this CTA
         for (int64_t u = u_beg; u < u_end;) {
             const Kv4Item it = item_at(u);
+            u = it.next;
+            if (it.take == 0) continue;
             const int rows = rows_of(it), cols = cols_of(rows), keys = kv4_tile_keys(til, it.q, it.tile);
             // ---- queries to shared memory, channels of a word in the order the nibbles come in; their sums
             {
@@ -318,95 +336,119 @@ __global__ void __launch_bounds__(THREADS, 1) k_attn_kv4_tc(const Kv4AttnParams 
                 mbar_arrive(smem_u32(&sm->q_full));
                 named_sync<1, SOFT>();                                    // the sums are read by everybody
             }
-            float l[NB][2], ms[NB][2], ref[NB][2];
+            // running sums and negated references of this thread's rows: rows 2 t and 2 t + 1 of a block side by side
+            F2 l[NB], ms[NB], nref[NB];
 #pragma unroll
-            for (int j = 0; j < NB; ++j)
-#pragma unroll
-                for (int e = 0; e < 2; ++e) { l[j][e] = 0.f; ms[j][e] = 0.f; ref[j][e] = -INFINITY; }
+            for (int j = 0; j < NB; ++j) { l[j] = ms[j] = f2(0.f, 0.f); nref[j] = f2(INFINITY, INFINITY); }
             float vmul = 0x1p24f;                                         // 2^-e of V's scales
-            bool any_pv = false;                                          // O^T holds something of this item
 
-            float2 kp[4], vp[4];                                          // scale and minimum of this thread's four keys
-            bool there[4];
+            // (scale, min) of K and V of this thread's four keys, loaded one unit ahead; `there`: which of them the tile has
+            uint32_t kn[4], vn[4], there_n = 0;
             auto load_par = [&](int ch) {
+                there_n = 0;
 #pragma unroll
-                for (int x = 0; x < 4; ++x) {
-                    const int key = ch * UNIT + quad * 32 + g + 8 * x;
-                    kp[x] = vp[x] = make_float2(0.f, 0.f);
-                    there[x] = false;
-                    if (key < keys) {
-                        const int pg = kv4_page(w, it.seq, key);
-                        if (pg >= 0) {
-                            const uint8_t* blk = p.pool + kv4_block_at(w, pg, it.head);
-                            kp[x] = load_params<__half>(blk + kv4_param_at(R, D, 2, 0, key & (R - 1)));
-                            vp[x] = load_params<__half>(blk + kv4_param_at(R, D, 2, 1, key & (R - 1)));
-                            there[x] = true;
+                for (int h = 0; h < 2; ++h) {                             // two groups of 16 keys, each in one page
+                    const int key = ch * UNIT + quad * 32 + 16 * h + g;
+                    const int pg = key - g < keys ? kv4_page(w, it.seq, key - g) : -1;
+                    const uint8_t* blk = p.pool + kv4_block_at(w, pg < 0 ? 0 : pg, it.head);
+#pragma unroll
+                    for (int x = 0; x < 2; ++x) {
+                        const int r = (key + 8 * x) & (R - 1);
+                        kn[2 * h + x] = vn[2 * h + x] = 0;
+                        if (pg >= 0 && key + 8 * x < keys) {
+                            kn[2 * h + x] = __ldg(reinterpret_cast<const uint32_t*>(blk + kv4_param_at(R, D, 2, 0, r)));
+                            vn[2 * h + x] = __ldg(reinterpret_cast<const uint32_t*>(blk + kv4_param_at(R, D, 2, 1, r)));
+                            there_n |= 1u << (2 * h + x);
                         }
                     }
                 }
             };
-            for (int k = 0; k < it.take; ++k, ++i) {
-                const int b = i & 1, ch = it.chunk0 + k, key0 = ch * UNIT + quad * 32 + g;
-                load_par(ch);
-                const bool all = ch * UNIT + UNIT <= it.q.len && there[0] && there[1] && there[2] && there[3];
-                float ks[4], km[4];
+            load_par(it.chunk0);
+
+            // One unit.  MASKED: some key may be invisible to some row (an item's last units); otherwise all are visible.
+            auto unit = [&](auto masked, int k) {
+                constexpr bool MASKED = decltype(masked)::value;
+                const int b = i & 1, key0 = (it.chunk0 + k) * UNIT + quad * 32 + g;
+                const uint32_t there = there_n;
+                float ks[4], km[4], vs[4], vm[4];
 #pragma unroll
-                for (int x = 0; x < 4; ++x) { ks[x] = kp[x].x * sl2; km[x] = fmaf(8.f, kp[x].x, kp[x].y) * sl2; vp[x].y = fmaf(8.f, vp[x].x, vp[x].y); }
+                for (int x = 0; x < 4; ++x) {
+                    const float2 a = __half22float2(*reinterpret_cast<const __half2*>(&kn[x])), c = __half22float2(*reinterpret_cast<const __half2*>(&vn[x]));
+                    ks[x] = a.x * sl2;
+                    km[x] = fmaf(8.f, a.x, a.y) * sl2;
+                    vs[x] = c.x;
+                    vm[x] = fmaf(8.f, c.x, c.y);
+                }
+                if (k + 1 < it.take) load_par(it.chunk0 + k + 1);
                 mbar_wait(smem_u32(&sm->s_full[b]), (i >> 1) & 1, abort_flag, w.status, DEV_TIMEOUT_EPI);
                 tc_fence_after();
-                bool p_ready = false;
 #pragma unroll
                 for (int j0 = 0; j0 < NB; j0 += 4) {                      // 32 of this thread's scores at a time
-                    if (8 * (2 * j0 + half) >= cols) { if (j0 > 0) break; }
-                    uint32_t s[4][2][4];
-#pragma unroll
-                    for (int j = 0; j < 4; ++j)
-#pragma unroll
-                        for (int h = 0; h < 2; ++h) ld_frag(tmem + SH::T_S + b * N + 8 * (2 * (j0 + j) + half) + ((uint32_t)(quad * 32 + 16 * h) << 16), s[j][h]);
-                    ld_wait();
+                    if (j0 > 0 && 8 * (2 * j0 + half) >= cols) break;
                     uint32_t vis = 0xffffffffu;
-                    bool over = false;
-#pragma unroll
-                    for (int x = 0; x < 4; ++x) over = over || vp[x].x * vmul > 128.f;
-                    if (!all) {
+                    if constexpr (MASKED) {
                         vis = 0u;
 #pragma unroll
                         for (int j = 0; j < 4; ++j)
 #pragma unroll
                             for (int e = 0; e < 2; ++e) {
                                 const int node = (it.tile * N + 8 * (2 * (j0 + j) + half) + 2 * t + e) / p.group;
+                                const uint32_t w32 = sees(p, it.q, node, key0 - it.q.len);
 #pragma unroll
-                                for (int x = 0; x < 4; ++x) {
-                                    const int jj = key0 + 8 * x - it.q.len;
-                                    if (there[x] && (jj < 0 || sees_new(p, it.q, node, jj))) vis |= 1u << (8 * j + 4 * e + x);
-                                }
+                                for (int x = 0; x < 4; ++x) vis |= ((w32 >> (8 * x)) & (there >> x) & 1u) << (8 * j + 4 * e + x);
                             }
                     }
+                    // Scores of key x and row e of block j (registers 2 (x & 1) + e of fragment x >> 1), in powers of two.
+                    // Pass 0 takes them against the rows' references; where one of the 128 threads of these rows finds a score
+                    // too far above, pass 1 takes them plain, new references are agreed on, and pass 2 is pass 0 again.
+                    uint32_t s[4][2][4];
+                    for (int pass = 0;; ++pass) {
 #pragma unroll
-                    for (int j = 0; j < 4; ++j) if (8 * (2 * (j0 + j) + half) >= cols) vis &= ~(0xffu << (8 * j));      // no such rows
-                    // score of key x and row (j, e): register 2 (x & 1) + e of fragment x >> 1
+                        for (int j = 0; j < 4; ++j)
 #pragma unroll
-                    for (int j = 0; j < 4; ++j) {
-                        const float2 q2 = *reinterpret_cast<const float2*>(&sm->qs[8 * (2 * (j0 + j) + half) + 2 * t]);
+                            for (int h = 0; h < 2; ++h) ld_frag(tmem + SH::T_S + b * N + 8 * (2 * (j0 + j) + half) + ((uint32_t)(quad * 32 + 16 * h) << 16), s[j][h]);
+                        ld_wait();
+                        bool over = false;
 #pragma unroll
-                        for (int e = 0; e < 2; ++e)
+                        for (int j = 0; j < 4; ++j) {
+                            const int c8 = 8 * (2 * (j0 + j) + half);
+                            const float2 qq = *reinterpret_cast<const float2*>(&sm->qs[c8 + 2 * t]);
+                            const F2 q2 = f2(qq.x, qq.y), base = pass == 1 ? f2(0.f, 0.f) : nref[j0 + j];
+                            float top = -INFINITY;
 #pragma unroll
                             for (int x = 0; x < 4; ++x) {
-                                uint32_t& r = s[j][x >> 1][2 * (x & 1) + e];
-                                float v = fmaf(ks[x], __uint_as_float(r), km[x] * (e ? q2.y : q2.x));
-                                if (!((vis >> (8 * j + 4 * e + x)) & 1u)) v = -INFINITY;
-                                over = over || v - ref[j0 + j][e] > RAISE;
-                                r = __float_as_uint(v);
+                                uint32_t &r0 = s[j][x >> 1][2 * (x & 1)], &r1 = s[j][x >> 1][2 * (x & 1) + 1];
+                                float a, c;
+                                f2_get(f2_fma(f2(ks[x], ks[x]), f2(__uint_as_float(r0), __uint_as_float(r1)), f2_fma(f2(km[x], km[x]), q2, base)), a, c);
+                                if constexpr (MASKED) {
+                                    if (!((vis >> (8 * j + x)) & 1u)) a = -INFINITY;
+                                    if (!((vis >> (8 * j + 4 + x)) & 1u)) c = -INFINITY;
+                                }
+                                r0 = __float_as_uint(a);
+                                r1 = __float_as_uint(c);
+                                top = fmaxf(top, fmaxf(a, c));
                             }
-                    }
-                    if (half_any(half, over)) {
-                        // ---- the 128 threads of these rows agree on new references and a new exponent
-                        float vm = 0.f;
+                            over = over || (c8 < cols && top > RAISE);    // (blocks behind the tile's rows hold anything)
+                        }
+                        if (pass == 2) break;
+                        if (pass == 0) {
+                            if (j0 == 0) {
 #pragma unroll
-                        for (int x = 0; x < 4; ++x) if (vp[x].x <= 65504.f) vm = fmaxf(vm, vp[x].x);
+                                for (int x = 0; x < 4; ++x) over = over || vs[x] * vmul > 128.f;
+                            }
+                            if (!half_any(half, over)) break;
+                            continue;
+                        }
+                        // the exponent changes before the unit's first weights only
+                        float vnew = vmul;
+                        if (j0 == 0) {
+                            float vx = 0.f;
 #pragma unroll
-                        for (int o = 4; o < 32; o <<= 1) vm = fmaxf(vm, __shfl_xor_sync(0xffffffffu, vm, o));
-                        if (lane == 0) sm->vmax[half][quad] = vm;
+                            for (int x = 0; x < 4; ++x) if (vs[x] <= 65504.f) vx = fmaxf(vx, vs[x]);
+#pragma unroll
+                            for (int o = 4; o < 32; o <<= 1) vx = fmaxf(vx, __shfl_xor_sync(0xffffffffu, vx, o));
+                            if (lane == 0) sm->vmax[half][quad] = vx;
+                        }
 #pragma unroll
                         for (int j = 0; j < 4; ++j)
 #pragma unroll
@@ -419,38 +461,40 @@ __global__ void __launch_bounds__(THREADS, 1) k_attn_kv4_tc(const Kv4AttnParams 
                                 if (g == 0) sm->x[quad][8 * (2 * (j0 + j) + half) + 2 * t + e] = m;
                             }
                         half_sync(half);
-                        vm = fmaxf(fmaxf(sm->vmax[half][0], sm->vmax[half][1]), fmaxf(sm->vmax[half][2], sm->vmax[half][3]));
-                        float vnew = vmul;                        // changes before the unit's first weights only
-                        if (j0 == 0 && vm * vnew > 1.f) vnew = exp2f(-ceilf(log2f(vm)));
+                        if (j0 == 0) {
+                            const float vx = fmaxf(fmaxf(sm->vmax[half][0], sm->vmax[half][1]), fmaxf(sm->vmax[half][2], sm->vmax[half][3]));
+                            if (vx * vmul > 1.f) vnew = exp2f(-ceilf(log2f(vx)));
+                        }
                         const float fv = vnew / vmul;
+                        vmul = vnew;
 #pragma unroll
-                        for (int j = 0; j < NB; ++j)
+                        for (int j = 0; j < NB; ++j) {
+                            float f[2] = {1.f, 1.f};
+                            const int rl = 8 * (2 * j + half) + 2 * t;
+                            if (j >= j0 && j < j0 + 4) {
+                                float n[2];
+                                f2_get(nref[j], n[0], n[1]);
 #pragma unroll
-                            for (int e = 0; e < 2; ++e) {
-                                const int rl = 8 * (2 * j + half) + 2 * t + e;
-                                float f = 1.f;
-                                if (j >= j0 && j < j0 + 4) {
-                                    const float m = fmaxf(fmaxf(sm->x[0][rl], sm->x[1][rl]), fmaxf(sm->x[2][rl], sm->x[3][rl]));
-                                    if (m > ref[j][e]) {
-                                        f = ex2(ref[j][e] - m);
-                                        ref[j][e] = m;
-                                        l[j][e] *= f;
-                                        ms[j][e] *= f;
+                                for (int e = 0; e < 2; ++e) {
+                                    const float m = fmaxf(fmaxf(sm->x[0][rl + e], sm->x[1][rl + e]), fmaxf(sm->x[2][rl + e], sm->x[3][rl + e]));
+                                    if (m > -n[e]) {
+                                        f[e] = ex2(-n[e] - m);            // 0 from a reference of -infinity
+                                        n[e] = -m;
                                     }
                                 }
-                                if (quad == 0 && g == 0) sm->fac[rl] = f * fv;
+                                nref[j] = f2(n[0], n[1]);
+                                l[j] = f2_mul(l[j], f2(f[0], f[1]));
+                                ms[j] = f2_mul(ms[j], f2(f[0], f[1]));
                             }
-                        vmul = vnew;
+                            if (quad == 0 && g == 0) { sm->fac[rl] = f[0] * fv; sm->fac[rl + 1] = f[1] * fv; }
+                        }
                         half_sync(half);
-                        if (any_pv) {
+                        if (k > 0) {
                             // O^T holds the products of the units before once the last of them has completed (each P buffer's
                             // release is waited for again two units later, so its phases are seen one by one)
                             mbar_wait(smem_u32(&sm->p_empty[(i - 1) & 1]), ((i - 1) >> 1) & 1, abort_flag, w.status, DEV_TIMEOUT_EPI);
                             tc_fence_after();
-#pragma unroll
-                            for (int j = 0; j < NB; ++j) {                // this half's blocks of eight columns, both groups of 16 lanes
-                                const int c0 = 8 * (2 * j + half);
-                                if (c0 >= cols) break;
+                            for (int c0 = 8 * half; c0 < cols; c0 += 16) {      // this half's blocks of eight columns, both groups of 16 lanes
                                 const float2 f = *reinterpret_cast<const float2*>(&sm->fac[c0 + 2 * t]);
                                 uint32_t o[2][4];
 #pragma unroll
@@ -460,8 +504,7 @@ __global__ void __launch_bounds__(THREADS, 1) k_attn_kv4_tc(const Kv4AttnParams 
                                 for (int h = 0; h < 2; ++h) {
 #pragma unroll
                                     for (int e = 0; e < 4; ++e) o[h][e] = __float_as_uint(__uint_as_float(o[h][e]) * ((e & 1) ? f.y : f.x));
-                                    asm volatile("tcgen05.st.sync.aligned.16x256b.x1.b32 [%0], {%1, %2, %3, %4};"
-                                                 ::"r"(tmem + SH::T_O + c0 + ((uint32_t)(quad * 32 + 16 * h) << 16)), "r"(o[h][0]), "r"(o[h][1]), "r"(o[h][2]), "r"(o[h][3]) : "memory");
+                                    st_frag(tmem + SH::T_O + c0 + ((uint32_t)(quad * 32 + 16 * h) << 16), o[h]);
                                 }
                             }
                             st_wait();
@@ -469,57 +512,63 @@ __global__ void __launch_bounds__(THREADS, 1) k_attn_kv4_tc(const Kv4AttnParams 
                         }
                         half_sync(half);                                  // the exchange buffers may be written again
                     }
-                    if (!p_ready) {
-                        if (i >= 2) mbar_wait(smem_u32(&sm->p_empty[b]), ((i >> 1) - 1) & 1, abort_flag, w.status, DEV_TIMEOUT_EPI);
-                        p_ready = true;
-                    }
-                    float vs[4];
+                    if (j0 == 0 && i >= 2) mbar_wait(smem_u32(&sm->p_empty[b]), ((i >> 1) - 1) & 1, abort_flag, w.status, DEV_TIMEOUT_EPI);
+                    float vsc[4];
 #pragma unroll
-                    for (int x = 0; x < 4; ++x) vs[x] = vp[x].x * vmul;
+                    for (int x = 0; x < 4; ++x) vsc[x] = vs[x] * vmul;
 #pragma unroll
                     for (int j = 0; j < 4; ++j) {
                         const int blk = 2 * (j0 + j) + half;
-                        float pv[2][4];
-#pragma unroll
-                        for (int e = 0; e < 2; ++e) {
-                            const float rf = ref[j0 + j][e] == -INFINITY ? 0.f : ref[j0 + j][e];
-#pragma unroll
-                            for (int x = 0; x < 4; ++x) {
-                                const bool ok = (vis >> (8 * j + 4 * e + x)) & 1u;
-                                const float pe = ex2(__uint_as_float(s[j][x >> 1][2 * (x & 1) + e]) - rf);
-                                l[j0 + j][e] += ok ? pe : 0.f;
-                                ms[j0 + j][e] += ok ? pe * vp[x].y : 0.f;
-                                pv[e][x] = ok ? pe * vs[x] : 0.f;
-                            }
-                        }
+                        if (8 * blk >= cols) break;
                         uint32_t h4[4];
 #pragma unroll
                         for (int x = 0; x < 4; ++x) {
-                            const __half2 h2 = __floats2half2_rn(pv[0][x], pv[1][x]);
+                            const F2 pe = f2(ex2(__uint_as_float(s[j][x >> 1][2 * (x & 1)])), ex2(__uint_as_float(s[j][x >> 1][2 * (x & 1) + 1])));
+                            l[j0 + j] = f2_add(l[j0 + j], pe);
+                            float a, c;
+                            f2_get(f2_mul(pe, f2(vsc[x], vsc[x])), a, c);
+                            if constexpr (MASKED) {                       // by selection: what a key holds stays out of rows that do not see it
+                                float d0, d1;
+                                f2_get(f2_mul(pe, f2(vm[x], vm[x])), d0, d1);
+                                if (!((vis >> (8 * j + x)) & 1u)) a = d0 = 0.f;
+                                if (!((vis >> (8 * j + 4 + x)) & 1u)) c = d1 = 0.f;
+                                ms[j0 + j] = f2_add(ms[j0 + j], f2(d0, d1));
+                            } else {
+                                ms[j0 + j] = f2_fma(pe, f2(vm[x], vm[x]), ms[j0 + j]);
+                            }
+                            const __half2 h2 = __floats2half2_rn(a, c);
                             h4[x] = *reinterpret_cast<const uint32_t*>(&h2);
                         }
                         // lane's matrix row: key 32 quad + lane, query rows 8 blk .. 8 blk + 7
-                        if (8 * blk < cols)
-                            stmatrix4(base_a + SH::P_AT + b * SH::P_BYTES + (blk >> 3) * (UNIT * 128) + (quad * 32 + lane) * 128 + (((blk & 7) ^ (lane & 7)) << 4), h4[0], h4[1], h4[2], h4[3]);
+                        stmatrix4(base_a + SH::P_AT + b * SH::P_BYTES + (blk >> 3) * (UNIT * 128) + (quad * 32 + lane) * 128 + (((blk & 7) ^ (lane & 7)) << 4), h4[0], h4[1], h4[2], h4[3]);
                     }
                 }
                 tc_fence_before();
                 mbar_arrive(smem_u32(&sm->s_empty[b]));
                 asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
                 mbar_arrive(smem_u32(&sm->p_full[b]));
-                any_pv = true;
+            };
+            for (int k = 0; k < it.take; ++k, ++i) {
+                // (the whole warp takes the same branch)
+                const bool all = (it.chunk0 + k + 1) * UNIT <= it.q.len && __all_sync(0xffffffffu, there_n == 15u);
+                if (all) unit(std::false_type{}, k);
+                else unit(std::true_type{}, k);
             }
             // ---- sums of the rows over the four warps that share them
 #pragma unroll
-            for (int j = 0; j < NB; ++j)
+            for (int j = 0; j < NB; ++j) {
+                float a[2], c[2], n[2];
+                f2_get(l[j], a[0], a[1]);
+                f2_get(ms[j], c[0], c[1]);
+                f2_get(nref[j], n[0], n[1]);
 #pragma unroll
                 for (int e = 0; e < 2; ++e) {
-                    float a = l[j][e], c = ms[j][e];
 #pragma unroll
-                    for (int o = 4; o < 32; o <<= 1) { a += __shfl_xor_sync(0xffffffffu, a, o); c += __shfl_xor_sync(0xffffffffu, c, o); }
+                    for (int o = 4; o < 32; o <<= 1) { a[e] += __shfl_xor_sync(0xffffffffu, a[e], o); c[e] += __shfl_xor_sync(0xffffffffu, c[e], o); }
                     const int rl = 8 * (2 * j + half) + 2 * t + e;
-                    if (g == 0) { sm->x[quad][rl] = a; sm->y[quad][rl] = c; if (quad == 0) sm->fac[rl] = ref[j][e]; }
+                    if (g == 0) { sm->x[quad][rl] = a[e]; sm->y[quad][rl] = c[e]; if (quad == 0) sm->fac[rl] = -n[e]; }
                 }
+            }
             named_sync<1, SOFT>();
             mbar_wait(smem_u32(&sm->p_empty[(i - 1) & 1]), ((i - 1) >> 1) & 1, abort_flag, w.status, DEV_TIMEOUT_EPI);
             tc_fence_after();
@@ -568,10 +617,9 @@ __global__ void __launch_bounds__(THREADS, 1) k_attn_kv4_tc(const Kv4AttnParams 
                     __threadfence();
                 }
                 named_sync<1, SOFT>();
-                if (sm->arrived) merge_item<__half, D>(p, it, N, rows, c0, c1, tid, SOFT);
+                if (sm->arrived) merge_item<__half, D, SOFT / 32>(p, it, N, rows, c0, c1, warp, sm->merge, [] { named_sync<1, SOFT>(); });
             }
             named_sync<1, SOFT>();                                        // queries' sums and exchange buffers are written again
-            u += it.take;
         }
     }
 

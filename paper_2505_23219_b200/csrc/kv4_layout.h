@@ -45,9 +45,10 @@ GHD_HD Kv4Seq kv4_seq(int start, int end, int n_rows, int kv_len, int64_t capaci
 // ---------------------------------------------------------------- the attention's work
 // An item is one (sequence, key/value head, tile of query rows); a query row of an item is (new row i, query head of
 // the group), numbered i * group + head.  Its keys are walked in chunks of `chunk` rows; a tile sees the cache and
-// the new rows up to its last one.  Units = chunks of all items in the order (sequence, head, tile, chunk).
+// the new rows up to its last one.  The work is numbered in units in the order (sequence, head, tile): an item has
+// `lead` units for what it costs whatever its length (queries in, sums out), then one for each chunk.
 struct Kv4Tiling {
-    int heads, group, tile_rows, chunk;
+    int heads, group, tile_rows, chunk, lead;
 };
 GHD_HD int kv4_tiles(const Kv4Tiling& t, int n) { return (int)(((int64_t)n * t.group + t.tile_rows - 1) / t.tile_rows); }
 // keys that the rows of a tile may see
@@ -62,17 +63,18 @@ GHD_HD int kv4_tile_chunks(const Kv4Tiling& t, const Kv4Seq& q, int tile) {
 // units of one head of a sequence
 GHD_HD int64_t kv4_head_units(const Kv4Tiling& t, const Kv4Seq& q) {
     int64_t u = 0;
-    for (int i = 0, n = kv4_tiles(t, q.n); i < n; ++i) u += kv4_tile_chunks(t, q, i);
+    for (int i = 0, n = kv4_tiles(t, q.n); i < n; ++i) u += t.lead + kv4_tile_chunks(t, q, i);
     return u;
 }
 // Every CTA takes `per` consecutive units (the last ones fewer or none), so a unit's CTA is unit / per.
 GHD_HD int64_t kv4_units_per_cta(int64_t units, int ctas) { return units > 0 ? (units + ctas - 1) / ctas : 1; }
 
-// The item that unit u belongs to, and how many of its chunks the run [u, u_end) takes.  sums: exclusive sums of the
-// sequences' units, n_seqs + 1 of them; seq_of(s) -> Kv4Seq; u < sums[n_seqs].
+// The item that unit u belongs to, and the chunks of it that the run [u, u_end) takes (none when the run ends before the
+// item's first chunk).  sums: exclusive sums of the sequences' units, n_seqs + 1 of them; seq_of(s) -> Kv4Seq;
+// u < sums[n_seqs].
 struct Kv4Item {
     int seq, head, tile, chunk0, chunks, take;
-    int64_t first;                  // number of the item's first unit
+    int64_t first, next;            // unit of the item's first chunk; unit where the run goes on behind this item
     Kv4Seq q;
 };
 template <typename SeqOf>
@@ -92,15 +94,15 @@ GHD_HD Kv4Item kv4_find_item(const Kv4Tiling& t, const int64_t* sums, int n_seqs
     it.tile = 0;
     for (;;) {
         it.chunks = kv4_tile_chunks(t, it.q, it.tile);
-        if (rem < it.chunks) break;
-        rem -= it.chunks;
+        if (rem < t.lead + it.chunks) break;
+        rem -= t.lead + it.chunks;
         ++it.tile;
     }
-    it.chunk0 = (int)rem;
-    it.first = u - rem;
-    const int64_t left = u_end - u;
-    it.take = it.chunks - it.chunk0;
-    if (it.take > left) it.take = (int)left;
+    it.first = u - rem + t.lead;
+    it.next = it.first + it.chunks < u_end ? it.first + it.chunks : u_end;
+    it.chunk0 = rem > t.lead ? (int)(rem - t.lead) : 0;
+    const int64_t take = it.next - (it.first + it.chunk0);
+    it.take = take > 0 ? (int)take : 0;
     return it;
 }
 

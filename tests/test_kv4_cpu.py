@@ -25,8 +25,8 @@ void seq(int start, int end, int n_rows, int len, long long cap, int* out) {
 }
 // Deals the units of a batch over `ctas` runs as the kernels do.  out: (seq, head, tile, chunk0, take, chunks, cta, first lo) per piece.
 long long deal(int n_seqs, const int* start, const int* len, int n_rows, long long cap, int heads, int group, int tile_rows, int chunk,
-               int ctas, long long* out, long long most) {
-    Kv4Tiling t{heads, group, tile_rows, chunk};
+               int lead, int ctas, long long* out, long long most) {
+    Kv4Tiling t{heads, group, tile_rows, chunk, lead};
     std::vector<int64_t> sums(n_seqs + 1, 0);
     auto seq_of = [&](int s) { return kv4_seq(start[s], start[s + 1], n_rows, len[s], cap); };
     for (int s = 0; s < n_seqs; ++s) sums[s + 1] = sums[s] + heads * kv4_head_units(t, seq_of(s));
@@ -37,10 +37,11 @@ long long deal(int n_seqs, const int* start, const int* len, int n_rows, long lo
         const int64_t e = u + per < units ? u + per : units;
         while (u < e) {
             Kv4Item it = kv4_find_item(t, sums.data(), n_seqs, seq_of, u, e);
-            if (n >= most || it.take < 1) return -1;
+            if (n >= most || it.next <= u || it.next > e) return -1;
+            u = it.next;
+            if (it.take == 0) continue;
             long long* o = out + 9 * n++;
             o[0] = it.seq; o[1] = it.head; o[2] = it.tile; o[3] = it.chunk0; o[4] = it.take; o[5] = it.chunks; o[6] = c; o[7] = it.first; o[8] = kv4_tile_keys(t, it.q, it.tile);
-            u += it.take;
         }
     }
     return n;
@@ -99,7 +100,8 @@ def test_numbers_out_of_range_are_held_inside_the_buffers(lay):
 
 
 @pytest.mark.parametrize("group,tile_rows,chunk", [(1, 8, 64), (1, 16, 64), (4, 8, 64), (7, 16, 64), (1, 64, 128), (5, 128, 128)])
-def test_the_work_split_takes_every_chunk_once(lay, group, tile_rows, chunk):
+@pytest.mark.parametrize("lead", [0, 3, 6])
+def test_the_work_split_takes_every_chunk_once(lay, group, tile_rows, chunk, lead):
     rng = np.random.RandomState(group * 100 + tile_rows)
     buf = (C.c_longlong * (9 * 200000))()
     for trial in range(25):
@@ -109,7 +111,7 @@ def test_the_work_split_takes_every_chunk_once(lay, group, tile_rows, chunk):
         start = np.concatenate(([0], np.cumsum(cnt))).astype(np.int32)
         heads, ctas = int(rng.choice([1, 3, 8])), int(rng.choice([1, 7, 148, 592]))
         n = lay.deal(n_seqs, start.ctypes.data_as(C.c_void_p), lens.ctypes.data_as(C.c_void_p), int(start[-1]), C.c_longlong(1 << 20), heads, group, tile_rows, chunk,
-                     ctas, buf, C.c_longlong(200000))
+                     lead, ctas, buf, C.c_longlong(200000))
         assert n >= 0
         pieces = np.array(buf[: 9 * n], np.int64).reshape(n, 9)
         seen = {}
@@ -123,7 +125,7 @@ def test_the_work_split_takes_every_chunk_once(lay, group, tile_rows, chunk):
             assert got[0] <= chunks
         items = {(s, h, tl) for s in range(n_seqs) for h in range(heads) for tl in range(-(-int(cnt[s]) * group // tile_rows))}
         assert set(seen) == items
-        units = sum(v[0] for v in seen.values())
+        units = sum(v[0] + lead for v in seen.values())
         per = max(1, -(-units // ctas))
         cont, begun = {}, {}
         for key, (total, first, ctas_of) in seen.items():
