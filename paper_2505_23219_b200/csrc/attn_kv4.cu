@@ -103,7 +103,7 @@ struct Narrow {
 };
 
 template <typename T, int D, int NT>
-__global__ void __launch_bounds__(WARPS * 32, Narrow<T, D, NT>::BLOCKS) k_attn_kv4(const Kv4AttnParams p) {
+__global__ void __launch_bounds__(WARPS * 32, Narrow<T, D, NT>::BLOCKS) k_attn_kv4(const __grid_constant__ Kv4AttnParams p) {
     using N = Narrow<T, D, NT>;
     using O_ = Op<T>;
     constexpr int RT = N::RT, KW = N::KW, VW = N::VW, KS = N::KS, MT = N::MT, TERMS = O_::TERMS, XO = N::XO, es = N::ES;
@@ -126,7 +126,7 @@ __global__ void __launch_bounds__(WARPS * 32, Narrow<T, D, NT>::BLOCKS) k_attn_k
     const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5, g = lane >> 2, t = lane & 3;
     const int R = 1 << w.shift;
     const float sl2 = p.scale * KV4_LOG2E;
-    auto item_at = [&](int64_t x) { return kv4_find_item(til, sums, w.n_seqs, [&](int s_) { return kv4_load_seq(w, s_); }, x, u_end); };
+    auto item_at = [&](int64_t x) { Kv4Item r; find_item(&w, &til, sums, x, u_end, &r); return r; };
 
     // ---- this warp's ring: 16 keys a stage, STAGES - 1 units ahead, over the borders of items
     uint8_t* ring = smem + warp * N::STAGES * N::STAGE;
@@ -161,7 +161,7 @@ __global__ void __launch_bounds__(WARPS * 32, Narrow<T, D, NT>::BLOCKS) k_attn_k
         }
         cp_commit();
     };
-#pragma unroll
+#pragma unroll 1
     for (int i = 0; i < N::STAGES - 1; ++i) load_next(i);
 
     int i = 0;                                                          // unit of this CTA
@@ -258,14 +258,11 @@ __global__ void __launch_bounds__(WARPS * 32, Narrow<T, D, NT>::BLOCKS) k_attn_k
                 }
             }
             // scores (in powers of two): key g rows 2 t, 2 t + 1, then key g + 8; a pair of rows shares its key's scale
-            const F2 ks0 = f2(kp0.x * sl2, kp0.x * sl2), ks1 = f2(kp1.x * sl2, kp1.x * sl2);
-            const float km0 = fmaf(8.f, kp0.x, kp0.y) * sl2, km1 = fmaf(8.f, kp1.x, kp1.y) * sl2;
+            const float ks0 = kp0.x * sl2, ks1 = kp1.x * sl2, km0 = fmaf(8.f, kp0.x, kp0.y) * sl2, km1 = fmaf(8.f, kp1.x, kp1.y) * sl2;
 #pragma unroll
-            for (int nt = 0; nt < NT; ++nt) {
-                const F2 q2 = f2(qs[nt][0], qs[nt][1]);
-                f2_get(f2_fma(ks0, f2(s[nt][0], s[nt][1]), f2_mul(f2(km0, km0), q2)), s[nt][0], s[nt][1]);
-                f2_get(f2_fma(ks1, f2(s[nt][2], s[nt][3]), f2_mul(f2(km1, km1), q2)), s[nt][2], s[nt][3]);
-            }
+            for (int nt = 0; nt < NT; ++nt)
+#pragma unroll
+                for (int e = 0; e < 4; ++e) s[nt][e] = e < 2 ? fmaf(ks0, s[nt][e], km0 * qs[nt][e & 1]) : fmaf(ks1, s[nt][e], km1 * qs[nt][e & 1]);
             const bool all = key0 + 16 <= it.q.len;
             uint32_t vis = 0xffffffffu;
             if (!all) {

@@ -112,13 +112,11 @@ __device__ __forceinline__ int64_t unit_sums(const Kv4View& w, const Kv4Tiling& 
     return sums[w.n_seqs];
 }
 
-// Two 32-bit floats in one register pair, worked on by one instruction.
-struct F2 { uint64_t v; };
-__device__ __forceinline__ F2 f2(float a, float b) { F2 r; asm("mov.b64 %0, {%1, %2};" : "=l"(r.v) : "f"(a), "f"(b)); return r; }
-__device__ __forceinline__ void f2_get(F2 x, float& a, float& b) { asm("mov.b64 {%0, %1}, %2;" : "=f"(a), "=f"(b) : "l"(x.v)); }
-__device__ __forceinline__ F2 f2_fma(F2 a, F2 b, F2 c) { F2 r; asm("fma.rn.f32x2 %0, %1, %2, %3;" : "=l"(r.v) : "l"(a.v), "l"(b.v), "l"(c.v)); return r; }
-__device__ __forceinline__ F2 f2_add(F2 a, F2 b) { F2 r; asm("add.rn.f32x2 %0, %1, %2;" : "=l"(r.v) : "l"(a.v), "l"(b.v)); return r; }
-__device__ __forceinline__ F2 f2_mul(F2 a, F2 b) { F2 r; asm("mul.rn.f32x2 %0, %1, %2;" : "=l"(r.v) : "l"(a.v), "l"(b.v)); return r; }
+// kv4_find_item out of line: it is called from several places and its code is long (instruction fetch is what short
+// calls wait for).
+static __device__ __noinline__ void find_item(const Kv4View* w, const Kv4Tiling* t, const int64_t* sums, int64_t u, int64_t u_end, Kv4Item* out) {
+    *out = kv4_find_item(*t, sums, w->n_seqs, [&](int s) { return kv4_load_seq(*w, s); }, u, u_end);
+}
 
 // Adds the partial sums that CTAs c0 .. c1 left of one item, in that order, and writes its rows.  A warp takes a row (the
 // lanes hold D / 32 channels each); with fewer rows than warps several warps share a row's contributors and meet in

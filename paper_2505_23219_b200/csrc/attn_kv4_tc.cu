@@ -8,7 +8,7 @@
 //   softmax  warps 0..7 read S^T in the 16x256b fragment form: a thread holds 4 keys x 8 (or 16) query rows, so a key's
 //       scale and minimum are four registers pairs and a row's running sums a register each; weights times V's scale
 //       go to shared memory by stmatrix as the B operand of the second product;
-//   warp 12 issues the first product, warp 13 the second.  O^T stays in tensor memory over all keys of an item.
+//   warp 12 issues the first product, warp 13 the second, warp 14 works out the CTA's items ahead of everybody.  O^T stays in tensor memory over all keys of an item.
 // Packed codes reach shared memory by cp.async, three units ahead (rows of unknown pages are filled with zeros).
 // Nibbles come out of a word in the order 0 4 1 5 2 6 3 7; the queries are stored in that order, and the output's
 // lanes are read back through it.
@@ -21,7 +21,6 @@
 // written and read, 16 KB of queries read, 16 KB of codes in and out.  Work is dealt as in attn_kv4.cu, one CTA an SM.
 #include <cstddef>
 #include <cstdio>
-#include <type_traits>
 
 #include "attn_kv4_dev.cuh"
 #include "tc_common.cuh"
@@ -41,6 +40,9 @@ constexpr int REGS_SOFT = 176, REGS_CONV = 96, REGS_ISSUE = 56;
 static_assert(SOFT * REGS_SOFT + CONV * REGS_CONV + 128 * REGS_ISSUE <= THREADS * 128, "register split");
 constexpr float RAISE = 8.f;
 constexpr int LEAD = 6;                        // an item's fixed cost in units
+// The scales and minima stay until the softmax warps have read them: when a unit's codes are asked for, at most 4 units
+// behind and 3 ahead of the unpacking are in use.
+constexpr int PAR_SLOTS = 8;
 constexpr uint32_t V_SLAB = UNIT * 128;        // [128 keys x 64 channels] half
 
 template <int D, int N>
@@ -54,21 +56,28 @@ struct Shape {
     static_assert(T_O + N <= 512, "tensor memory");
 };
 
+constexpr int ITEMS = 4;                       // items that the scheduler is ahead, at most
+
 struct Ctrl {
+    uint64_t item_full[ITEMS], item_empty[ITEMS];
+    Kv4Item item[ITEMS], cur;        // cur: the softmax warps' item
     uint64_t q_full, k_full[2], k_empty[2], v_full[2], v_empty[2], s_full[2], s_empty[2], p_full[2], p_empty[2], drain, drain_pv;
     uint32_t tmem_base;
     int abort_flag, arrived;
     alignas(16) float qs[128];       // sums of the tile's queries
     alignas(16) float fac[128];      // factors of a rescale, by row
     float x[4][128], y[4][128];      // exchange between the four warps that share rows
-    float merge[8 * 130];            // warps that share a row's partial sums
+    alignas(16) uint32_t par[PAR_SLOTS][2][UNIT];   // (scale, min) of K and of V by unit and key
+    uint32_t page_there[PAR_SLOTS][8];     // whether a group of 16 keys has a page
+    int rowix[128];                  // row of q and out, in d_head elements, of the tile's query rows
     float vmax[2][4];                // largest of V's scales of a unit, by half and warp
     int64_t scratch[32];
-    int64_t sums[GHD_MAX_SEQS + 1];
+    int64_t sums[1];                 // [n_seqs + 1]
 };
-template <int D, int N> constexpr uint32_t smem_bytes() { return Shape<D, N>::CTRL_AT + (uint32_t)sizeof(Ctrl) + 1024; }
+template <int D, int N> constexpr uint32_t smem_bytes(int n_seqs) { return Shape<D, N>::CTRL_AT + (uint32_t)sizeof(Ctrl) + 8 * (uint32_t)n_seqs + 1024; }
+constexpr int WIDE_SEQS = 400;                 // most sequences of a call with tiles of 128 rows (their sums share the memory)
 static_assert(offsetof(Ctrl, qs) % 16 == 0 && offsetof(Ctrl, fac) % 16 == 0, "rows are read in pairs");
-static_assert(smem_bytes<128, 128>() <= 227 * 1024 && smem_bytes<128, 64>() <= 227 * 1024, "shared memory");
+static_assert(smem_bytes<128, 128>(WIDE_SEQS) <= 227 * 1024 && smem_bytes<128, 64>(GHD_MAX_SEQS) <= 227 * 1024, "shared memory");
 
 __device__ __forceinline__ void ld_frag(uint32_t taddr, uint32_t (&r)[4]) {      // 16 lanes x 8 columns, as an mma accumulator
     asm volatile("tcgen05.ld.sync.aligned.16x256b.x1.b32 {%0, %1, %2, %3}, [%4];" : "=r"(r[0]), "=r"(r[1]), "=r"(r[2]), "=r"(r[3]) : "r"(taddr) : "memory");
@@ -125,7 +134,7 @@ template <int D> __device__ __forceinline__ uint32_t piece_at(int row, int c) {
 }
 
 template <int D, int N>
-__global__ void __launch_bounds__(THREADS, 1) k_attn_kv4_tc(const Kv4AttnParams p) {
+__global__ void __launch_bounds__(THREADS, 1) k_attn_kv4_tc(const __grid_constant__ Kv4AttnParams p) {
     using SH = Shape<D, N>;
     constexpr int NB = N / 16;                       // blocks of eight query rows a softmax thread sees (it takes every other block)
     constexpr int PIECES = D / 32;                   // 16-byte pieces of a packed row
@@ -146,6 +155,7 @@ __global__ void __launch_bounds__(THREADS, 1) k_attn_kv4_tc(const Kv4AttnParams 
         }
         mbar_init(smem_u32(&sm->drain), 1);
         mbar_init(smem_u32(&sm->drain_pv), 1);
+        for (int b = 0; b < ITEMS; ++b) { mbar_init(smem_u32(&sm->item_full[b]), 1); mbar_init(smem_u32(&sm->item_empty[b]), 1 + CONV / 32 + 2); }
         sm->abort_flag = 0;
         asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
     }
@@ -162,7 +172,14 @@ __global__ void __launch_bounds__(THREADS, 1) k_attn_kv4_tc(const Kv4AttnParams 
     volatile int* abort_flag = &sm->abort_flag;
     const int64_t per = kv4_units_per_cta(units, p.ctas);
     const int64_t u_beg = per * blockIdx.x, u_end = u_beg + per < units ? u_beg + per : units;
-    auto item_at = [&](int64_t u) { return kv4_find_item(til, sm->sums, w.n_seqs, [&](int s_) { return kv4_load_seq(w, s_); }, u, u_end); };
+    // The k-th item of this CTA (take = 0: there are no more, or a wait has run out).  One thread looks; who takes it together
+    // with others gets it from that thread, so that all of them go on or stop alike.
+    auto item_get = [&](int k) -> Kv4Item {
+        if (!mbar_wait(smem_u32(&sm->item_full[k % ITEMS]), (k / ITEMS) & 1, abort_flag, w.status, DEV_TIMEOUT_EPI)) { Kv4Item none{}; return none; }
+        const Kv4Item it = sm->item[k % ITEMS];
+        mbar_arrive(smem_u32(&sm->item_empty[k % ITEMS]));
+        return it;
+    };
     auto rows_of = [&](const Kv4Item& it) { const int r = it.q.n * p.group - it.tile * N; return r < N ? r : N; };
     auto cols_of = [&](int rows) { return (rows + 15) & ~15; };           // MMA N: a multiple of 16
 
@@ -172,37 +189,52 @@ __global__ void __launch_bounds__(THREADS, 1) k_attn_kv4_tc(const Kv4AttnParams 
         const int quad = warp - 8, key = quad * 32 + lane;
         const uint32_t st0 = base_a + SH::ST_AT + quad * 32 * (D / 2);    // this warp's 32 rows of a stage (K; V UNIT rows further)
         const int R = 1 << w.shift;
-        int64_t lu = u_beg;                                               // load cursor
-        Kv4Item it{};
-        int lch = 0, lend = 0, lkeys = 0, n = 0;                          // n: units asked for so far
+        int items = 0;                                                    // load cursor
+        bool more = true;
+        int lseq = 0, lhead = 0, lch = 0, lend = 0, lkeys = 0, n = 0;                          // n: units asked for so far
         auto load_next = [&](int i) {
-            while (lch >= lend && lu < u_end) {
-                it = item_at(lu);
-                lch = it.chunk0; lend = it.chunk0 + it.take; lkeys = kv4_tile_keys(til, it.q, it.tile);
-                lu = it.next;
+            if (lch >= lend && more) {
+                if (lane == 0) {
+                    const Kv4Item it = item_get(items);
+                    lseq = it.seq; lhead = it.head; lch = it.chunk0; lend = it.chunk0 + it.take; lkeys = it.keys;
+                }
+                ++items;
+                lseq = __shfl_sync(0xffffffffu, lseq, 0);
+                lhead = __shfl_sync(0xffffffffu, lhead, 0);
+                lch = __shfl_sync(0xffffffffu, lch, 0);
+                lend = __shfl_sync(0xffffffffu, lend, 0);
+                lkeys = __shfl_sync(0xffffffffu, lkeys, 0);
+                more = lend > lch;
             }
             if (lch < lend) {
                 const uint32_t st = st0 + (uint32_t)(i % SH::STAGES) * SH::ST_BYTES;
                 const int key0 = lch * UNIT + quad * 32;
                 int page[2];                                              // of this warp's two groups of 16 keys
 #pragma unroll
-                for (int h = 0; h < 2; ++h) page[h] = key0 + 16 * h < lkeys ? kv4_page(w, it.seq, key0 + 16 * h) : -1;
+                for (int h = 0; h < 2; ++h) page[h] = key0 + 16 * h < lkeys ? kv4_page(w, lseq, key0 + 16 * h) : -1;
                 constexpr int PER = 32 / PIECES;                          // rows a warp-wide copy covers
 #pragma unroll
                 for (int j = 0; j < PIECES; ++j) {
                     const int row = lane / PIECES + PER * j, c = lane % PIECES;
                     const int pg = row < 16 ? page[0] : page[1];
                     const int r = (key0 + row) & (R - 1);
-                    const uint8_t* blk = p.pool + kv4_block_at(w, pg < 0 ? 0 : pg, it.head);
+                    const uint8_t* blk = p.pool + kv4_block_at(w, pg < 0 ? 0 : pg, lhead);
                     cp16(st + piece_at<D>(row, c), blk + kv4_code_at(R, D, 0, r) + 16 * c, pg >= 0);
                     cp16(st + UNIT * (D / 2) + piece_at<D>(row, c), blk + kv4_code_at(R, D, 1, r) + 16 * c, pg >= 0);
+                }
+                if (lane < 16) {                                          // scales and minima: four keys a piece, K then V
+                    const int which = lane >> 3, row = (lane & 7) * 4, pg = row < 16 ? page[0] : page[1];
+                    const uint8_t* blk = p.pool + kv4_block_at(w, pg < 0 ? 0 : pg, lhead);
+                    cp16(smem_u32(&sm->par[i & (PAR_SLOTS - 1)][which][quad * 32 + row]), blk + kv4_param_at(R, D, 2, which, (key0 + row) & (R - 1)), pg >= 0);
+                } else if (lane < 18) {
+                    sm->page_there[i & (PAR_SLOTS - 1)][2 * quad + lane - 16] = (lane == 16 ? page[0] : page[1]) >= 0;
                 }
                 ++lch;
                 ++n;
             }
             cp_commit();
         };
-#pragma unroll
+#pragma unroll 1
         for (int i = 0; i < SH::STAGES - 1; ++i) load_next(i);
         for (int i = 0; i < n; ++i) {                                     // (n runs ahead until the last unit has been asked for)
             const int b = i & 1;
@@ -213,7 +245,7 @@ __global__ void __launch_bounds__(THREADS, 1) k_attn_kv4_tc(const Kv4AttnParams 
             __syncwarp();
             if (i >= 2) mbar_wait(smem_u32(&sm->k_empty[b]), ((i >> 1) - 1) & 1, abort_flag, w.status, DEV_TIMEOUT_TMEM);
             tc_fence_after();
-#pragma unroll
+#pragma unroll 1
             for (int c = 0; c < PIECES; ++c) {
                 const uint4 x = lds128(st + piece_at<D>(lane, c));
                 uint32_t r[16];
@@ -225,7 +257,7 @@ __global__ void __launch_bounds__(THREADS, 1) k_attn_kv4_tc(const Kv4AttnParams 
             mbar_arrive(smem_u32(&sm->k_full[b]));
             if (i >= 2) mbar_wait(smem_u32(&sm->v_empty[b]), ((i >> 1) - 1) & 1, abort_flag, w.status, DEV_TIMEOUT_TMEM);
             const uint32_t vt = base_a + SH::V_AT + b * SH::V_BYTES + key * 128;
-#pragma unroll
+#pragma unroll 1
             for (int c = 0; c < PIECES; ++c) {
                 const uint4 x = lds128(st + UNIT * (D / 2) + piece_at<D>(lane, c));
                 uint32_t r[16];
@@ -245,10 +277,9 @@ __global__ void __launch_bounds__(THREADS, 1) k_attn_kv4_tc(const Kv4AttnParams 
             const uint64_t q_desc = smem_desc_sw128(base_a);
             bool ok = true;
             int i = 0, items = 0;
-            for (int64_t u = u_beg; ok && u < u_end;) {
-                const Kv4Item it = item_at(u);
-                u = it.next;
-                if (it.take == 0) continue;
+            while (ok) {
+                const Kv4Item it = item_get(items);
+                if (it.take == 0) break;
                 const uint32_t idesc = instr_desc_f16(cols_of(rows_of(it)), false);
                 ok = mbar_wait(smem_u32(&sm->q_full), items & 1, abort_flag, w.status, DEV_TIMEOUT_MMA);
                 ++items;
@@ -278,10 +309,10 @@ __global__ void __launch_bounds__(THREADS, 1) k_attn_kv4_tc(const Kv4AttnParams 
             const uint64_t v_desc = smem_desc_sw128(base_a + SH::V_AT, D == 128 ? V_SLAB : 0);   // d_head 64: channels 64 .. 127 repeat 0 .. 63
             const uint64_t p_desc = smem_desc_sw128(base_a + SH::P_AT, UNIT * 128);
             bool ok = true;
-            int i = 0;
-            for (int64_t u = u_beg; ok && u < u_end;) {
-                const Kv4Item it = item_at(u);
-                u = it.next;
+            int i = 0, items = 0;
+            while (ok) {
+                const Kv4Item it = item_get(items++);
+                if (it.take == 0) break;
                 const uint32_t idesc = instr_desc_f16(cols_of(rows_of(it)), true) | (1u << 15);
                 for (int k = 0; ok && k < it.take; ++k, ++i) {
                     const int b = i & 1;
@@ -302,29 +333,58 @@ __global__ void __launch_bounds__(THREADS, 1) k_attn_kv4_tc(const Kv4AttnParams 
                 for (uint32_t spin = 0; spin < SPIN_LIMIT && !mbar_try(smem_u32(&sm->drain_pv), 0); ++spin) __nanosleep(64);
             }
         }
+        } else if (warp == 14) {
+        // ------------------------------------------------ scheduler
+        if (lane == 0) {
+            int k = 0;
+            bool ok = true;
+            for (int64_t u = u_beg; ok;) {
+                Kv4Item it{};
+                while (u < u_end && it.take == 0) {
+                    it = kv4_find_item(til, sm->sums, w.n_seqs, [&](int s_) { return kv4_load_seq(w, s_); }, u, u_end);
+                    u = it.next;
+                }
+                if (it.take > 0) it.keys = kv4_tile_keys(til, it.q, it.tile);
+                if (k >= ITEMS) ok = mbar_wait(smem_u32(&sm->item_empty[k % ITEMS]), ((k / ITEMS) - 1) & 1, abort_flag, w.status, DEV_TIMEOUT_EPI);
+                sm->item[k % ITEMS] = it;
+                mbar_arrive(smem_u32(&sm->item_full[k % ITEMS]));
+                ++k;
+                if (it.take == 0) break;
+            }
+        }
         }
     } else {
         asm volatile("setmaxnreg.inc.sync.aligned.u32 %0;" ::"n"(REGS_SOFT));
         // ------------------------------------------------ softmax warps
         // half: which blocks of eight query rows (half, half + 2, ...); quad: which 32 keys (tensor-memory lanes)
         const int half = warp >> 2, quad = warp & 3, g = lane >> 2, t = lane & 3, tid = threadIdx.x;
-        const int R = 1 << w.shift;
         const float sl2 = p.scale * KV4_LOG2E;
         int i = 0;                                                        // unit of this CTA
-        for (int64_t u = u_beg; u < u_end;) {
-            const Kv4Item it = item_at(u);
-            u = it.next;
-            if (it.take == 0) continue;
-            const int rows = rows_of(it), cols = cols_of(rows), keys = kv4_tile_keys(til, it.q, it.tile);
+        for (int items = 0;; ++items) {
+            if (tid == 0) sm->cur = item_get(items);
+            named_sync<1, SOFT>();
+            const Kv4Item it = sm->cur;
+            if (it.take == 0) break;
+            const int rows = rows_of(it), cols = cols_of(rows);
             // ---- queries to shared memory, channels of a word in the order the nibbles come in; their sums
             {
-                constexpr int C8 = D / 8;                                 // 16-byte pieces of a row
-                for (int x = tid; x < cols * C8; x += SOFT) {
-                    const int rl = x / C8, c = x % C8, rr = it.tile * N + rl;
-                    uint4 v = make_uint4(0, 0, 0, 0);
-                    if (rl < rows) v = __ldg(reinterpret_cast<const uint4*>((const __half*)p.q + ((size_t)(it.q.row0 + rr / p.group) * p.q_heads + it.head * p.group + rr % p.group) * D + 8 * c));
-                    const uint32_t r[4] = {__byte_perm(v.x, v.z, 0x5410), __byte_perm(v.x, v.z, 0x7632), __byte_perm(v.y, v.w, 0x5410), __byte_perm(v.y, v.w, 0x7632)};
-                    sts128(base_a + (c >> 3) * N * 128 + rl * 128 + (((c & 7) ^ (rl & 7)) << 4), r);
+                constexpr int C8 = D / 8, MOST = N * C8 / SOFT;           // 16-byte pieces of a row, and at most of a thread
+                uint4 v[MOST];
+#pragma unroll
+                for (int z = 0; z < MOST; ++z) {                          // all loads first
+                    const int x = tid + z * SOFT, rl = x / C8, c = x % C8, rr = it.tile * N + rl;
+                    v[z] = make_uint4(0, 0, 0, 0);
+                    if (rl < rows) {
+                        const int ix = (it.q.row0 + rr / p.group) * p.q_heads + it.head * p.group + rr % p.group;
+                        v[z] = __ldg(reinterpret_cast<const uint4*>((const __half*)p.q + (size_t)ix * D + 8 * c));
+                        if (c == 0) sm->rowix[rl] = ix;
+                    }
+                }
+#pragma unroll
+                for (int z = 0; z < MOST; ++z) {
+                    const int x = tid + z * SOFT, rl = x / C8, c = x % C8;
+                    const uint32_t r[4] = {__byte_perm(v[z].x, v[z].z, 0x5410), __byte_perm(v[z].x, v[z].z, 0x7632), __byte_perm(v[z].y, v[z].w, 0x5410), __byte_perm(v[z].y, v[z].w, 0x7632)};
+                    if (rl < cols) sts128(base_a + (c >> 3) * N * 128 + rl * 128 + (((c & 7) ^ (rl & 7)) << 4), r);
                     float s = 0.f;
 #pragma unroll
                     for (int e = 0; e < 4; ++e) { const float2 f = __half22float2(*reinterpret_cast<const __half2*>(&r[e])); s += f.x + f.y; }
@@ -336,57 +396,38 @@ __global__ void __launch_bounds__(THREADS, 1) k_attn_kv4_tc(const Kv4AttnParams 
                 mbar_arrive(smem_u32(&sm->q_full));
                 named_sync<1, SOFT>();                                    // the sums are read by everybody
             }
-            // running sums and negated references of this thread's rows: rows 2 t and 2 t + 1 of a block side by side
-            F2 l[NB], ms[NB], nref[NB];
+            // running sums and references of this thread's rows: rows 2 t + e of its blocks
+            float l[NB][2], ms[NB][2], ref[NB][2];
 #pragma unroll
-            for (int j = 0; j < NB; ++j) { l[j] = ms[j] = f2(0.f, 0.f); nref[j] = f2(INFINITY, INFINITY); }
+            for (int j = 0; j < NB; ++j)
+#pragma unroll
+                for (int e = 0; e < 2; ++e) { l[j][e] = ms[j][e] = 0.f; ref[j][e] = -INFINITY; }
             float vmul = 0x1p24f;                                         // 2^-e of V's scales
-
-            // (scale, min) of K and V of this thread's four keys, loaded one unit ahead; `there`: which of them the tile has
-            uint32_t kn[4], vn[4], there_n = 0;
-            auto load_par = [&](int ch) {
-                there_n = 0;
-#pragma unroll
-                for (int h = 0; h < 2; ++h) {                             // two groups of 16 keys, each in one page
-                    const int key = ch * UNIT + quad * 32 + 16 * h + g;
-                    const int pg = key - g < keys ? kv4_page(w, it.seq, key - g) : -1;
-                    const uint8_t* blk = p.pool + kv4_block_at(w, pg < 0 ? 0 : pg, it.head);
-#pragma unroll
-                    for (int x = 0; x < 2; ++x) {
-                        const int r = (key + 8 * x) & (R - 1);
-                        kn[2 * h + x] = vn[2 * h + x] = 0;
-                        if (pg >= 0 && key + 8 * x < keys) {
-                            kn[2 * h + x] = __ldg(reinterpret_cast<const uint32_t*>(blk + kv4_param_at(R, D, 2, 0, r)));
-                            vn[2 * h + x] = __ldg(reinterpret_cast<const uint32_t*>(blk + kv4_param_at(R, D, 2, 1, r)));
-                            there_n |= 1u << (2 * h + x);
-                        }
-                    }
-                }
-            };
-            load_par(it.chunk0);
-
-            // One unit.  MASKED: some key may be invisible to some row (an item's last units); otherwise all are visible.
-            auto unit = [&](auto masked, int k) {
-                constexpr bool MASKED = decltype(masked)::value;
+            for (int k = 0; k < it.take; ++k, ++i) {
                 const int b = i & 1, key0 = (it.chunk0 + k) * UNIT + quad * 32 + g;
-                const uint32_t there = there_n;
+                mbar_wait(smem_u32(&sm->s_full[b]), (i >> 1) & 1, abort_flag, w.status, DEV_TIMEOUT_EPI);
+                tc_fence_after();
+                // (the scales were in place before the unit's keys were: the same threads wrote them)
+                uint32_t there = 0;                                       // which of this thread's keys have a page
                 float ks[4], km[4], vs[4], vm[4];
 #pragma unroll
                 for (int x = 0; x < 4; ++x) {
-                    const float2 a = __half22float2(*reinterpret_cast<const __half2*>(&kn[x])), c = __half22float2(*reinterpret_cast<const __half2*>(&vn[x]));
+                    const int slot = i & (PAR_SLOTS - 1), key = quad * 32 + g + 8 * x;
+                    const float2 a = __half22float2(*reinterpret_cast<const __half2*>(&sm->par[slot][0][key])), c = __half22float2(*reinterpret_cast<const __half2*>(&sm->par[slot][1][key]));
                     ks[x] = a.x * sl2;
                     km[x] = fmaf(8.f, a.x, a.y) * sl2;
                     vs[x] = c.x;
                     vm[x] = fmaf(8.f, c.x, c.y);
+                    if (sm->page_there[slot][key >> 4]) there |= 1u << x;
                 }
-                if (k + 1 < it.take) load_par(it.chunk0 + k + 1);
-                mbar_wait(smem_u32(&sm->s_full[b]), (i >> 1) & 1, abort_flag, w.status, DEV_TIMEOUT_EPI);
-                tc_fence_after();
+                // (the whole warp takes the same branches on `all`: every key of the unit is visible to every row)
+                const bool all = (it.chunk0 + k + 1) * UNIT <= it.q.len && __all_sync(0xffffffffu, there == 15u);
 #pragma unroll
                 for (int j0 = 0; j0 < NB; j0 += 4) {                      // 32 of this thread's scores at a time
                     if (j0 > 0 && 8 * (2 * j0 + half) >= cols) break;
-                    uint32_t vis = 0xffffffffu;
-                    if constexpr (MASKED) {
+                    const uint32_t ts = tmem + SH::T_S + b * N + 8 * (2 * j0 + half) + ((uint32_t)(quad * 32) << 16);
+                    uint32_t vis = 0xffffffffu;                           // bit 8 j + 4 e + x: row e of block j sees key x
+                    if (!all) {
                         vis = 0u;
 #pragma unroll
                         for (int j = 0; j < 4; ++j)
@@ -398,73 +439,83 @@ __global__ void __launch_bounds__(THREADS, 1) k_attn_kv4_tc(const Kv4AttnParams 
                                 for (int x = 0; x < 4; ++x) vis |= ((w32 >> (8 * x)) & (there >> x) & 1u) << (8 * j + 4 * e + x);
                             }
                     }
-                    // Scores of key x and row e of block j (registers 2 (x & 1) + e of fragment x >> 1), in powers of two.
-                    // Pass 0 takes them against the rows' references; where one of the 128 threads of these rows finds a score
-                    // too far above, pass 1 takes them plain, new references are agreed on, and pass 2 is pass 0 again.
+                    // Scores of key x and row e of block j (registers 2 (x & 1) + e of fragment x >> 1), in powers of two, against
+                    // the rows' references.  Where one of the 128 threads of these rows finds a score too far above, they agree on
+                    // new references and look again.
                     uint32_t s[4][2][4];
-                    for (int pass = 0;; ++pass) {
+                    bool settled = false;
+#pragma unroll 1
+                    for (;;) {
 #pragma unroll
                         for (int j = 0; j < 4; ++j)
 #pragma unroll
-                            for (int h = 0; h < 2; ++h) ld_frag(tmem + SH::T_S + b * N + 8 * (2 * (j0 + j) + half) + ((uint32_t)(quad * 32 + 16 * h) << 16), s[j][h]);
+                            for (int h = 0; h < 2; ++h) ld_frag(ts + 16 * j + ((uint32_t)(16 * h) << 16), s[j][h]);
                         ld_wait();
-                        bool over = false;
+                        float top = -INFINITY;
 #pragma unroll
                         for (int j = 0; j < 4; ++j) {
                             const int c8 = 8 * (2 * (j0 + j) + half);
                             const float2 qq = *reinterpret_cast<const float2*>(&sm->qs[c8 + 2 * t]);
-                            const F2 q2 = f2(qq.x, qq.y), base = pass == 1 ? f2(0.f, 0.f) : nref[j0 + j];
-                            float top = -INFINITY;
+                            float tj = -INFINITY;
 #pragma unroll
                             for (int x = 0; x < 4; ++x) {
                                 uint32_t &r0 = s[j][x >> 1][2 * (x & 1)], &r1 = s[j][x >> 1][2 * (x & 1) + 1];
-                                float a, c;
-                                f2_get(f2_fma(f2(ks[x], ks[x]), f2(__uint_as_float(r0), __uint_as_float(r1)), f2_fma(f2(km[x], km[x]), q2, base)), a, c);
-                                if constexpr (MASKED) {
-                                    if (!((vis >> (8 * j + x)) & 1u)) a = -INFINITY;
-                                    if (!((vis >> (8 * j + 4 + x)) & 1u)) c = -INFINITY;
-                                }
+                                const float a = fmaf(ks[x], __uint_as_float(r0), fmaf(km[x], qq.x, -ref[j0 + j][0]));
+                                const float c = fmaf(ks[x], __uint_as_float(r1), fmaf(km[x], qq.y, -ref[j0 + j][1]));
                                 r0 = __float_as_uint(a);
                                 r1 = __float_as_uint(c);
-                                top = fmaxf(top, fmaxf(a, c));
+                                tj = fmaxf(tj, fmaxf(a, c));
                             }
-                            over = over || (c8 < cols && top > RAISE);    // (blocks behind the tile's rows hold anything)
+                            if (c8 < cols) top = fmaxf(top, tj);          // (blocks behind the tile's rows hold anything)
                         }
-                        if (pass == 2) break;
-                        if (pass == 0) {
-                            if (j0 == 0) {
+                        if (!all) {
+                            top = -INFINITY;
 #pragma unroll
-                                for (int x = 0; x < 4; ++x) over = over || vs[x] * vmul > 128.f;
-                            }
-                            if (!half_any(half, over)) break;
-                            continue;
+                            for (int j = 0; j < 4; ++j)
+#pragma unroll
+                                for (int e = 0; e < 2; ++e)
+#pragma unroll
+                                    for (int x = 0; x < 4; ++x) {
+                                        uint32_t& r = s[j][x >> 1][2 * (x & 1) + e];
+                                        if (!((vis >> (8 * j + 4 * e + x)) & 1u)) r = __float_as_uint(-INFINITY);
+                                        if (8 * (2 * (j0 + j) + half) < cols) top = fmaxf(top, __uint_as_float(r));
+                                    }
                         }
-                        // the exponent changes before the unit's first weights only
-                        float vnew = vmul;
-                        if (j0 == 0) {
-                            float vx = 0.f;
-#pragma unroll
-                            for (int x = 0; x < 4; ++x) if (vs[x] <= 65504.f) vx = fmaxf(vx, vs[x]);
-#pragma unroll
-                            for (int o = 4; o < 32; o <<= 1) vx = fmaxf(vx, __shfl_xor_sync(0xffffffffu, vx, o));
-                            if (lane == 0) sm->vmax[half][quad] = vx;
-                        }
-#pragma unroll
-                        for (int j = 0; j < 4; ++j)
+                        bool over = top > RAISE;
+                        if (j0 == 0) over = over || fmaxf(fmaxf(vs[0], vs[1]), fmaxf(vs[2], vs[3])) * vmul > 128.f;
+                        if (settled || !half_any(half, over)) break;
+                        settled = true;
+                        // plain scores of the unit, their maxima by row, and the largest of V's scales
+#pragma unroll 1
+                        for (int j = 0; j < 4; ++j) {
+                            const int c8 = 8 * (2 * (j0 + j) + half);
+                            const float2 qq = *reinterpret_cast<const float2*>(&sm->qs[c8 + 2 * t]);
+                            uint32_t o[2][4];
+                            ld_frag(ts + 16 * j, o[0]);
+                            ld_frag(ts + 16 * j + (16u << 16), o[1]);
+                            ld_wait();
 #pragma unroll
                             for (int e = 0; e < 2; ++e) {
                                 float m = -INFINITY;
 #pragma unroll
-                                for (int x = 0; x < 4; ++x) m = fmaxf(m, __uint_as_float(s[j][x >> 1][2 * (x & 1) + e]));
+                                for (int x = 0; x < 4; ++x)
+                                    if ((vis >> (8 * j + 4 * e + x)) & 1u) m = fmaxf(m, fmaf(ks[x], __uint_as_float(o[x >> 1][2 * (x & 1) + e]), km[x] * (e ? qq.y : qq.x)));
 #pragma unroll
-                                for (int o = 4; o < 32; o <<= 1) m = fmaxf(m, __shfl_xor_sync(0xffffffffu, m, o));
-                                if (g == 0) sm->x[quad][8 * (2 * (j0 + j) + half) + 2 * t + e] = m;
+                                for (int sh = 4; sh < 32; sh <<= 1) m = fmaxf(m, __shfl_xor_sync(0xffffffffu, m, sh));
+                                if (g == 0) sm->x[quad][c8 + 2 * t + e] = m;
                             }
-                        half_sync(half);
-                        if (j0 == 0) {
-                            const float vx = fmaxf(fmaxf(sm->vmax[half][0], sm->vmax[half][1]), fmaxf(sm->vmax[half][2], sm->vmax[half][3]));
-                            if (vx * vmul > 1.f) vnew = exp2f(-ceilf(log2f(vx)));
                         }
+                        float vx = 0.f;
+#pragma unroll
+                        for (int x = 0; x < 4; ++x) if (vs[x] <= 65504.f) vx = fmaxf(vx, vs[x]);
+#pragma unroll
+                        for (int sh = 4; sh < 32; sh <<= 1) vx = fmaxf(vx, __shfl_xor_sync(0xffffffffu, vx, sh));
+                        if (lane == 0) sm->vmax[half][quad] = vx;
+                        half_sync(half);
+                        // the exponent changes before the unit's first weights only
+                        float vnew = vmul;
+                        vx = fmaxf(fmaxf(sm->vmax[half][0], sm->vmax[half][1]), fmaxf(sm->vmax[half][2], sm->vmax[half][3]));
+                        if (j0 == 0 && vx * vmul > 1.f) vnew = exp2f(-ceilf(log2f(vx)));
                         const float fv = vnew / vmul;
                         vmul = vnew;
 #pragma unroll
@@ -472,19 +523,16 @@ __global__ void __launch_bounds__(THREADS, 1) k_attn_kv4_tc(const Kv4AttnParams 
                             float f[2] = {1.f, 1.f};
                             const int rl = 8 * (2 * j + half) + 2 * t;
                             if (j >= j0 && j < j0 + 4) {
-                                float n[2];
-                                f2_get(nref[j], n[0], n[1]);
 #pragma unroll
                                 for (int e = 0; e < 2; ++e) {
                                     const float m = fmaxf(fmaxf(sm->x[0][rl + e], sm->x[1][rl + e]), fmaxf(sm->x[2][rl + e], sm->x[3][rl + e]));
-                                    if (m > -n[e]) {
-                                        f[e] = ex2(-n[e] - m);            // 0 from a reference of -infinity
-                                        n[e] = -m;
+                                    if (m > ref[j][e]) {
+                                        f[e] = ex2(ref[j][e] - m);        // 0 from a reference of -infinity
+                                        ref[j][e] = m;
+                                        l[j][e] *= f[e];
+                                        ms[j][e] *= f[e];
                                     }
                                 }
-                                nref[j] = f2(n[0], n[1]);
-                                l[j] = f2_mul(l[j], f2(f[0], f[1]));
-                                ms[j] = f2_mul(ms[j], f2(f[0], f[1]));
                             }
                             if (quad == 0 && g == 0) { sm->fac[rl] = f[0] * fv; sm->fac[rl + 1] = f[1] * fv; }
                         }
@@ -494,17 +542,19 @@ __global__ void __launch_bounds__(THREADS, 1) k_attn_kv4_tc(const Kv4AttnParams 
                             // release is waited for again two units later, so its phases are seen one by one)
                             mbar_wait(smem_u32(&sm->p_empty[(i - 1) & 1]), ((i - 1) >> 1) & 1, abort_flag, w.status, DEV_TIMEOUT_EPI);
                             tc_fence_after();
+#pragma unroll 1
                             for (int c0 = 8 * half; c0 < cols; c0 += 16) {      // this half's blocks of eight columns, both groups of 16 lanes
                                 const float2 f = *reinterpret_cast<const float2*>(&sm->fac[c0 + 2 * t]);
+                                const uint32_t to = tmem + SH::T_O + c0 + ((uint32_t)(quad * 32) << 16);
                                 uint32_t o[2][4];
-#pragma unroll
-                                for (int h = 0; h < 2; ++h) ld_frag(tmem + SH::T_O + c0 + ((uint32_t)(quad * 32 + 16 * h) << 16), o[h]);
+                                ld_frag(to, o[0]);
+                                ld_frag(to + (16u << 16), o[1]);
                                 ld_wait();
 #pragma unroll
                                 for (int h = 0; h < 2; ++h) {
 #pragma unroll
                                     for (int e = 0; e < 4; ++e) o[h][e] = __float_as_uint(__uint_as_float(o[h][e]) * ((e & 1) ? f.y : f.x));
-                                    st_frag(tmem + SH::T_O + c0 + ((uint32_t)(quad * 32 + 16 * h) << 16), o[h]);
+                                    st_frag(to + ((uint32_t)(16 * h) << 16), o[h]);
                                 }
                             }
                             st_wait();
@@ -523,20 +573,22 @@ __global__ void __launch_bounds__(THREADS, 1) k_attn_kv4_tc(const Kv4AttnParams 
                         uint32_t h4[4];
 #pragma unroll
                         for (int x = 0; x < 4; ++x) {
-                            const F2 pe = f2(ex2(__uint_as_float(s[j][x >> 1][2 * (x & 1)])), ex2(__uint_as_float(s[j][x >> 1][2 * (x & 1) + 1])));
-                            l[j0 + j] = f2_add(l[j0 + j], pe);
-                            float a, c;
-                            f2_get(f2_mul(pe, f2(vsc[x], vsc[x])), a, c);
-                            if constexpr (MASKED) {                       // by selection: what a key holds stays out of rows that do not see it
-                                float d0, d1;
-                                f2_get(f2_mul(pe, f2(vm[x], vm[x])), d0, d1);
-                                if (!((vis >> (8 * j + x)) & 1u)) a = d0 = 0.f;
-                                if (!((vis >> (8 * j + 4 + x)) & 1u)) c = d1 = 0.f;
-                                ms[j0 + j] = f2_add(ms[j0 + j], f2(d0, d1));
-                            } else {
-                                ms[j0 + j] = f2_fma(pe, f2(vm[x], vm[x]), ms[j0 + j]);
+                            float pe[2], pv[2], pm[2];
+#pragma unroll
+                            for (int e = 0; e < 2; ++e) {
+                                pe[e] = ex2(__uint_as_float(s[j][x >> 1][2 * (x & 1) + e]));
+                                l[j0 + j][e] += pe[e];
+                                pv[e] = pe[e] * vsc[x];
+                                pm[e] = pe[e] * vm[x];
                             }
-                            const __half2 h2 = __floats2half2_rn(a, c);
+                            if (!all) {                                   // by selection: what a key holds stays out of rows that do not see it
+#pragma unroll
+                                for (int e = 0; e < 2; ++e)
+                                    if (!((vis >> (8 * j + 4 * e + x)) & 1u)) pv[e] = pm[e] = 0.f;
+                            }
+                            ms[j0 + j][0] += pm[0];
+                            ms[j0 + j][1] += pm[1];
+                            const __half2 h2 = __floats2half2_rn(pv[0], pv[1]);
                             h4[x] = *reinterpret_cast<const uint32_t*>(&h2);
                         }
                         // lane's matrix row: key 32 quad + lane, query rows 8 blk .. 8 blk + 7
@@ -547,26 +599,17 @@ __global__ void __launch_bounds__(THREADS, 1) k_attn_kv4_tc(const Kv4AttnParams 
                 mbar_arrive(smem_u32(&sm->s_empty[b]));
                 asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
                 mbar_arrive(smem_u32(&sm->p_full[b]));
-            };
-            for (int k = 0; k < it.take; ++k, ++i) {
-                // (the whole warp takes the same branch)
-                const bool all = (it.chunk0 + k + 1) * UNIT <= it.q.len && __all_sync(0xffffffffu, there_n == 15u);
-                if (all) unit(std::false_type{}, k);
-                else unit(std::true_type{}, k);
             }
             // ---- sums of the rows over the four warps that share them
 #pragma unroll
             for (int j = 0; j < NB; ++j) {
-                float a[2], c[2], n[2];
-                f2_get(l[j], a[0], a[1]);
-                f2_get(ms[j], c[0], c[1]);
-                f2_get(nref[j], n[0], n[1]);
 #pragma unroll
                 for (int e = 0; e < 2; ++e) {
+                    float a = l[j][e], c = ms[j][e];
 #pragma unroll
-                    for (int o = 4; o < 32; o <<= 1) { a[e] += __shfl_xor_sync(0xffffffffu, a[e], o); c[e] += __shfl_xor_sync(0xffffffffu, c[e], o); }
+                    for (int o = 4; o < 32; o <<= 1) { a += __shfl_xor_sync(0xffffffffu, a, o); c += __shfl_xor_sync(0xffffffffu, c, o); }
                     const int rl = 8 * (2 * j + half) + 2 * t + e;
-                    if (g == 0) { sm->x[quad][rl] = a[e]; sm->y[quad][rl] = c[e]; if (quad == 0) sm->fac[rl] = -n[e]; }
+                    if (g == 0) { sm->x[quad][rl] = a; sm->y[quad][rl] = c; if (quad == 0) sm->fac[rl] = ref[j][e]; }
                 }
             }
             named_sync<1, SOFT>();
@@ -578,30 +621,28 @@ __global__ void __launch_bounds__(THREADS, 1) k_attn_kv4_tc(const Kv4AttnParams 
             const float vinv = 1.f / vmul;
             // lane (16 h + g or + 8) of this quad is channel ch_of(lane); columns of this half's blocks
             auto ch_of = [](int m) { return (m & ~7) | ((m & 1) * 4) | ((m & 7) >> 1); };       // 0 4 1 5 2 6 3 7
-#pragma unroll
-            for (int j = 0; j < NB; ++j) {
-                const int blk = 2 * j + half;
-                if (8 * blk >= rows || quad * 32 >= D) break;
+#pragma unroll 1
+            for (int blk = half; 8 * blk < rows && quad * 32 < D; blk += 2) {
                 uint32_t o[2][4];
-#pragma unroll
-                for (int h = 0; h < 2; ++h) ld_frag(tmem + SH::T_O + 8 * blk + ((uint32_t)(quad * 32 + 16 * h) << 16), o[h]);
+                const uint32_t to = tmem + SH::T_O + 8 * blk + ((uint32_t)(quad * 32) << 16);
+                ld_frag(to, o[0]);
+                ld_frag(to + (16u << 16), o[1]);
                 ld_wait();
 #pragma unroll
                 for (int e = 0; e < 2; ++e) {
                     const int rl = 8 * blk + 2 * t + e;
                     if (rl >= rows) continue;
                     const float lsum = (sm->x[0][rl] + sm->x[1][rl]) + (sm->x[2][rl] + sm->x[3][rl]), mm = (sm->y[0][rl] + sm->y[1][rl]) + (sm->y[2][rl] + sm->y[3][rl]);
-                    const int rr = it.tile * N + rl;
                     const float inv = lsum == 0.f ? 0.f : 1.f / lsum;
-                    __half* dst = (__half*)p.out + ((size_t)(it.q.row0 + rr / p.group) * p.q_heads + it.head * p.group + rr % p.group) * D;
+                    __half* dst = (__half*)p.out + (size_t)sm->rowix[rl] * D + quad * 32 + ch_of(g);
+                    float* part = slot + (size_t)rl * D + quad * 32 + ch_of(g);
 #pragma unroll
                     for (int h = 0; h < 2; ++h)
 #pragma unroll
                         for (int x = 0; x < 2; ++x) {
-                            const int chn = quad * 32 + ch_of(16 * h + 8 * x + g);
                             const float v = fmaf(__uint_as_float(o[h][2 * x + e]), vinv, mm);
-                            if (whole) dst[chn] = __float2half_rn(v * inv);
-                            else __stcg(slot + (size_t)rl * D + chn, v);
+                            if (whole) dst[16 * h + 8 * x] = __float2half_rn(v * inv);
+                            else __stcg(part + 16 * h + 8 * x, v);
                         }
                     if (!whole && g == 0 && quad == 0) __stcg(reinterpret_cast<float2*>(slot + (size_t)N * D + 2 * rl), make_float2(sm->fac[rl], lsum));
                 }
@@ -617,7 +658,7 @@ __global__ void __launch_bounds__(THREADS, 1) k_attn_kv4_tc(const Kv4AttnParams 
                     __threadfence();
                 }
                 named_sync<1, SOFT>();
-                if (sm->arrived) merge_item<__half, D, SOFT / 32>(p, it, N, rows, c0, c1, warp, sm->merge, [] { named_sync<1, SOFT>(); });
+                if (sm->arrived) merge_item<__half, D, SOFT / 32>(p, it, N, rows, c0, c1, warp, reinterpret_cast<float*>(base + SH::P_AT), [] { named_sync<1, SOFT>(); });
             }
             named_sync<1, SOFT>();                                        // queries' sums and exchange buffers are written again
         }
@@ -633,12 +674,12 @@ __global__ void __launch_bounds__(THREADS, 1) k_attn_kv4_tc(const Kv4AttnParams 
 
 template <int D, int N>
 ghd_status launch_tc(ghd_ctx* c, Kv4AttnParams& p) {
-    if (cudaFuncSetAttribute(k_attn_kv4_tc<D, N>, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)smem_bytes<D, N>()) != cudaSuccess) {
+    if (cudaFuncSetAttribute(k_attn_kv4_tc<D, N>, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)smem_bytes<D, N>(p.w.n_seqs)) != cudaSuccess) {
         cudaGetLastError();
         return fail(c, GHD_ECUDA, "kv4_attention: cannot raise dynamic shared memory");
     }
     p.ctas = c->sm_count;
-    launch_k(c, false, k_attn_kv4_tc<D, N>, dim3(p.ctas), dim3(THREADS), smem_bytes<D, N>(), p);
+    launch_k(c, false, k_attn_kv4_tc<D, N>, dim3(p.ctas), dim3(THREADS), smem_bytes<D, N>(p.w.n_seqs), p);
     return GHD_OK;
 }
 
@@ -646,6 +687,7 @@ ghd_status launch_tc(ghd_ctx* c, Kv4AttnParams& p) {
 
 // partials: 2 slots of [tile_rows][d_head + 2] floats a CTA, within the tile scratch of 2 x 256 x 128 floats an SM
 ghd_status launch_attn_kv4_tc(ghd_ctx* c, Kv4AttnParams& p, int tile_rows) {
+    if (p.w.n_seqs > WIDE_SEQS) tile_rows = 64;
     if (c->cfg.d_head == 64) return tile_rows == 64 ? launch_tc<64, 64>(c, p) : launch_tc<64, 128>(c, p);
     return tile_rows == 64 ? launch_tc<128, 64>(c, p) : launch_tc<128, 128>(c, p);
 }

@@ -50,14 +50,15 @@ GHD_HD Kv4Seq kv4_seq(int start, int end, int n_rows, int kv_len, int64_t capaci
 struct Kv4Tiling {
     int heads, group, tile_rows, chunk, lead;
 };
-GHD_HD int kv4_tiles(const Kv4Tiling& t, int n) { return (int)(((int64_t)n * t.group + t.tile_rows - 1) / t.tile_rows); }
+GHD_HD int kv4_div(int64_t a, int b) { return a <= 0x7fffffff ? (int)((uint32_t)a / (uint32_t)b) : (int)(a / b); }     // a >= 0, b > 0
+GHD_HD int kv4_tiles(const Kv4Tiling& t, int n) { return kv4_div((int64_t)n * t.group + t.tile_rows - 1, t.tile_rows); }
 // keys that the rows of a tile may see
 GHD_HD int kv4_tile_keys(const Kv4Tiling& t, const Kv4Seq& q, int tile) {
-    const int64_t last = ((int64_t)(tile + 1) * t.tile_rows - 1) / t.group;        // number of the tile's last new row
-    return q.len + (last + 1 < q.n_new ? (int)(last + 1) : q.n_new);
+    const int last = kv4_div((int64_t)(tile + 1) * t.tile_rows - 1, t.group);        // number of the tile's last new row
+    return q.len + (last < q.n_new ? last + 1 : q.n_new);
 }
 GHD_HD int kv4_tile_chunks(const Kv4Tiling& t, const Kv4Seq& q, int tile) {
-    const int c = (int)(((int64_t)kv4_tile_keys(t, q, tile) + t.chunk - 1) / t.chunk);
+    const int c = kv4_div((int64_t)kv4_tile_keys(t, q, tile) + t.chunk - 1, t.chunk);
     return c > 0 ? c : 1;               // a row that sees nothing still gets its zeros
 }
 // units of one head of a sequence
@@ -74,6 +75,7 @@ GHD_HD int64_t kv4_units_per_cta(int64_t units, int ctas) { return units > 0 ? (
 // u < sums[n_seqs].
 struct Kv4Item {
     int seq, head, tile, chunk0, chunks, take;
+    int keys;                       // keys the tile may see (filled in by who needs it)
     int64_t first, next;            // unit of the item's first chunk; unit where the run goes on behind this item
     Kv4Seq q;
 };
@@ -88,8 +90,15 @@ GHD_HD Kv4Item kv4_find_item(const Kv4Tiling& t, const int64_t* sums, int n_seqs
     it.seq = lo;
     it.q = seq_of(lo);
     int64_t rem = u - sums[lo];
-    const int64_t head_units = (sums[lo + 1] - sums[lo]) / t.heads;
-    it.head = (int)(rem / head_units);
+    const int64_t seq_units = sums[lo + 1] - sums[lo];
+    int64_t head_units;
+    if (seq_units <= 0x7fffffff) {  // 64-bit divisions are long on the device
+        head_units = (uint32_t)seq_units / (uint32_t)t.heads;
+        it.head = (int)((uint32_t)rem / (uint32_t)head_units);
+    } else {
+        head_units = seq_units / t.heads;
+        it.head = (int)(rem / head_units);
+    }
     rem -= it.head * head_units;
     it.tile = 0;
     for (;;) {
@@ -103,6 +112,7 @@ GHD_HD Kv4Item kv4_find_item(const Kv4Tiling& t, const int64_t* sums, int n_seqs
     it.chunk0 = rem > t.lead ? (int)(rem - t.lead) : 0;
     const int64_t take = it.next - (it.first + it.chunk0);
     it.take = take > 0 ? (int)take : 0;
+    it.keys = 0;
     return it;
 }
 
