@@ -85,6 +85,7 @@ template <int SH> __device__ __forceinline__ uint32_t centred_half(uint32_t w) {
 __device__ __forceinline__ int64_t unit_sums(const Kv4View& w, const Kv4Tiling& t, int64_t* sums /* [n_seqs + 1] */, int64_t* scratch /* [32] */) {
     const int nt = blockDim.x, each = (w.n_seqs + nt - 1) / nt, s0 = threadIdx.x * each;
     int64_t mine = 0;
+#pragma unroll 1
     for (int s = s0; s < s0 + each && s < w.n_seqs; ++s) {
         const Kv4Seq q = kv4_load_seq(w, s);
         if (q.bad) atomicCAS(w.status, DEV_OK, DEV_KV4_ROWS);
@@ -101,7 +102,9 @@ __device__ __forceinline__ int64_t unit_sums(const Kv4View& w, const Kv4Tiling& 
     if (lane == 31) scratch[warp] = run;
     __syncthreads();
     int64_t base = run - mine;
+#pragma unroll 1
     for (int i = 0; i < warp; ++i) base += scratch[i];
+#pragma unroll 1
     for (int s = s0; s < s0 + each && s < w.n_seqs; ++s) {
         const int64_t u = sums[s];
         sums[s] = base;
@@ -128,16 +131,19 @@ __device__ __forceinline__ void merge_item(const Kv4AttnParams& p, const Kv4Item
     const size_t slot = (size_t)tile_rows * (D + 2);
     const int lane = threadIdx.x & 31, n = (int)(c1 - c0) + 1;
     int share = 1;                                               // warps a row: a power of two
+#pragma unroll 1
     while (share * 2 * rows <= NW && share * 16 <= n) share *= 2;
     const int sub = warp % share;
     const int k_beg = (int)((int64_t)n * sub / share), k_end = (int)((int64_t)n * (sub + 1) / share);
     auto slot_of = [&](int k) { return p.part + ((size_t)(c0 + k) * 2 + (k == 0 ? 1 : 0)) * slot; };
+#pragma unroll 1
     for (int rl0 = 0; rl0 < rows; rl0 += NW / share) {
         const int rl = rl0 + warp / share;
         float m = -INFINITY, lsum = 0.f, a[VL];
 #pragma unroll
         for (int e = 0; e < VL; ++e) a[e] = 0.f;
         if (rl < rows) {
+#pragma unroll 1
             for (int kb = k_beg; kb < k_end; kb += 8) {
                 float2 ml[8];
                 float v[8][VL];
@@ -178,10 +184,12 @@ __device__ __forceinline__ void merge_item(const Kv4AttnParams& p, const Kv4Item
             sync();
             if (sub == 0 && rl < rows) {
                 float mn = m;
+#pragma unroll 1
                 for (int k = 1; k < share; ++k) mn = fmaxf(mn, mine[(size_t)k * (D + 2) + D]);
                 float ls = 0.f, b[VL];
 #pragma unroll
                 for (int e = 0; e < VL; ++e) b[e] = 0.f;
+#pragma unroll 1
                 for (int k = 0; k < share; ++k) {
                     const float* x = mine + (size_t)k * (D + 2);
                     if (x[D] == -INFINITY && x[D + 1] == 0.f) continue;

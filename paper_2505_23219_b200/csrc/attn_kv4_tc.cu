@@ -2,23 +2,22 @@
 //
 // As in attn_kv4.cu the scales stay out of the products and keys are the M side: S^T [128 keys x rows] = K Q^T,
 // O^T [d_head x rows] = V^T P^T.  With keys on the tensor-memory lanes a thread owns whole key rows:
-//   K   warps 8..11: one thread per key unpacks its 4-bit row in registers and stores it to tensor memory, from where
-//       the first product takes its A operand - the unpacked keys never touch shared memory;
-//   V   the same warps unpack V rows into a swizzled shared-memory tile (A operand of the second product, M-major);
-//   softmax  warps 0..7 read S^T in the 16x256b fragment form: a thread holds 4 keys x 8 (or 16) query rows, so a key's
-//       scale and minimum are four registers pairs and a row's running sums a register each; weights times V's scale
-//       go to shared memory by stmatrix as the B operand of the second product;
-//   warp 12 issues the first product, warp 13 the second, warp 14 works out the CTA's items ahead of everybody.  O^T stays in tensor memory over all keys of an item.
-// Packed codes reach shared memory by cp.async, three units ahead (rows of unknown pages are filled with zeros).
-// Nibbles come out of a word in the order 0 4 1 5 2 6 3 7; the queries are stored in that order, and the output's
-// lanes are read back through it.
+//   K        warps 16..19: one thread per key unpacks its 4-bit row in registers and stores it to tensor memory, from where
+//            the first product takes its A operand - the unpacked keys never touch shared memory;
+//   V        warps 20..23 unpack V rows into a swizzled shared-memory tile (A operand of the second product, M-major);
+//   softmax  warps 0..15 read S^T in the 16x256b fragment form: a thread holds 4 keys x 4 (or 8) query rows, so a key's
+//            scales and minima are a few registers and a row's running sums one each; weights times V's scale go to
+//            shared memory by stmatrix as the B operand of the second product;
+//   warp 24 issues the first product, 25 the second, 26 works out the CTA's items ahead of everybody, 27 asks for the packed
+//            rows: one bulk copy per group of 16 keys and kind, a ring of units ahead.
+// O^T stays in tensor memory over all keys of an item.  Nibbles come out of a word in the order 0 4 1 5 2 6 3 7; the
+// queries are stored in that order, and the output's lanes are read back through it.
 //
 // Half range: weights are taken against a reference that is raised when a score passes it by 2^8, and V's scales are
 // divided by 2^e, e raised when a scale passes 2^7 of it, so the operand stays below 2^15.  Raising either rescales O^T
 // in place (rare after the first unit); the 128 threads that share query rows agree on it by one barrier a unit.
 //
-// Shared memory is what bounds it: per unit of 128 keys and 64 rows 32 KB of V written and read, 16 KB of weights
-// written and read, 16 KB of queries read, 16 KB of codes in and out.  Work is dealt as in attn_kv4.cu, one CTA an SM.
+// Work is dealt as in attn_kv4.cu, one CTA an SM.
 #include <cstddef>
 #include <cstdio>
 
@@ -33,21 +32,22 @@ using namespace tc;
 using namespace kv4;
 
 constexpr int UNIT = 128;                      // keys of a unit (MMA M of S^T, MMA K of O^T)
-constexpr int SOFT = 256, CONV = 128;          // threads of the softmax and of the unpacking warps
-constexpr int THREADS = SOFT + CONV + 128;   // the last warpgroup: two issuers and two idle warps (register counts change by warpgroups)
-// registers a thread after the split: 256 x 176 + 128 x 96 + 128 x 56 = 64512 of the 512 x 128 = 65536 launched with
-constexpr int REGS_SOFT = 176, REGS_CONV = 96, REGS_ISSUE = 56;
-static_assert(SOFT * REGS_SOFT + CONV * REGS_CONV + 128 * REGS_ISSUE <= THREADS * 128, "register split");
+constexpr int SOFT = 512, CONV = 256;          // threads of the softmax and of the unpacking warps
+constexpr int PARTS = SOFT / 128;              // 128 threads (one a key of four) share query rows: blocks part, part + PARTS, ... of eight
+constexpr int THREADS = SOFT + CONV + 128;
+// registers a thread after the split by warpgroups: 512 x 80 + 256 x 56 + 128 x 56 = 62464 of the 896 x 72 = 64512 launched with
+constexpr int REGS_LAUNCH = 72, REGS_SOFT = 80, REGS_CONV = 56, REGS_ISSUE = 56;
+static_assert(SOFT * REGS_SOFT + CONV * REGS_CONV + 128 * REGS_ISSUE <= THREADS * REGS_LAUNCH && THREADS * REGS_LAUNCH <= 65536, "register split");
 constexpr float RAISE = 8.f;
 constexpr int LEAD = 6;                        // an item's fixed cost in units
-// The scales and minima stay until the softmax warps have read them: when a unit's codes are asked for, at most 4 units
-// behind and 3 ahead of the unpacking are in use.
+// The scales and minima stay until the softmax warps have read them.  Unit j is asked for when unit j - 4 has been
+// unpacked, that is when the first product of unit j - 6 was complete and the softmax warps were done with unit j - 8.
 constexpr int PAR_SLOTS = 8;
 constexpr uint32_t V_SLAB = UNIT * 128;        // [128 keys x 64 channels] half
 
 template <int D, int N>
 struct Shape {
-    static constexpr int STAGES = 4 - (N == 128 ? 1 : 0);
+    static constexpr int STAGES = N == 128 ? 3 : 4;
     static constexpr int SLABS = D / 64, PSLABS = N / 64;
     static constexpr uint32_t Q_BYTES = SLABS * N * 128, V_BYTES = SLABS * V_SLAB, P_BYTES = PSLABS * UNIT * 128;
     static constexpr uint32_t ST_BYTES = UNIT * D;                       // K then V codes of a unit, D / 2 bytes a row each
@@ -61,6 +61,7 @@ constexpr int ITEMS = 4;                       // items that the scheduler is ah
 struct Ctrl {
     uint64_t item_full[ITEMS], item_empty[ITEMS];
     Kv4Item item[ITEMS], cur;        // cur: the softmax warps' item
+    uint64_t c_full[4], c_empty[4];  // packed codes of a unit
     uint64_t q_full, k_full[2], k_empty[2], v_full[2], v_empty[2], s_full[2], s_empty[2], p_full[2], p_empty[2], drain, drain_pv;
     uint32_t tmem_base;
     int abort_flag, arrived;
@@ -68,9 +69,10 @@ struct Ctrl {
     alignas(16) float fac[128];      // factors of a rescale, by row
     float x[4][128], y[4][128];      // exchange between the four warps that share rows
     alignas(16) uint32_t par[PAR_SLOTS][2][UNIT];   // (scale, min) of K and of V by unit and key
+    int unit_there[4];               // 0 in the stage behind the last unit
     uint32_t page_there[PAR_SLOTS][8];     // whether a group of 16 keys has a page
     int rowix[128];                  // row of q and out, in d_head elements, of the tile's query rows
-    float vmax[2][4];                // largest of V's scales of a unit, by half and warp
+    float vmax[PARTS][4];            // largest of V's scales of a unit, by part and warp
     int64_t scratch[32];
     int64_t sums[1];                 // [n_seqs + 1]
 };
@@ -111,12 +113,39 @@ __device__ __forceinline__ uint4 lds128(uint32_t addr) {
 __device__ __forceinline__ void sts128(uint32_t addr, const uint32_t* r) {
     asm volatile("st.shared.v4.u32 [%0], {%1, %2, %3, %4};" ::"r"(addr), "r"(r[0]), "r"(r[1]), "r"(r[2]), "r"(r[3]) : "memory");
 }
+// mbar_wait in few instructions: this kernel has many waits, and what it executes has to fit the instruction cache.
+__device__ __forceinline__ bool wait(uint32_t bar, uint32_t parity, volatile int* abort_flag, int* status, int code) {
+#pragma unroll 1
+    for (uint32_t spin = 0; spin < SPIN_LIMIT; ++spin) {
+        if (mbar_try(bar, parity)) return true;
+        if (__builtin_expect((spin & 63) == 63, 0)) {
+            if (*abort_flag) return false;
+            __nanosleep(64);
+        }
+    }
+    *abort_flag = 1;
+    atomicCAS(status, DEV_OK, code);
+    return false;
+}
+__device__ __forceinline__ void wait_drain(uint32_t bar, uint32_t parity) {
+#pragma unroll 1
+    for (uint32_t spin = 0; spin < SPIN_LIMIT && !mbar_try(bar, parity); ++spin) __nanosleep(64);
+}
+// One arrival for the whole warp: arrivals on one barrier are taken one by one, five cycles each.
+__device__ __forceinline__ void warp_arrive(uint32_t bar) {
+    __syncwarp();
+    if ((threadIdx.x & 31) == 0) mbar_arrive(bar);
+}
 template <int ID, int NT> __device__ __forceinline__ void named_sync() { asm volatile("bar.sync %0, %1;" ::"n"(ID), "n"(NT) : "memory"); }
-__device__ __forceinline__ void half_sync(int half) { asm volatile("bar.sync %0, 128;" ::"r"(2 + half) : "memory"); }
-__device__ __forceinline__ bool half_any(int half, bool v) {
+__device__ __forceinline__ void part_sync(int part) { asm volatile("bar.sync %0, 128;" ::"r"(2 + part) : "memory"); }
+__device__ __forceinline__ bool part_any(int part, bool v) {
     uint32_t r;
-    asm volatile("{\n\t.reg .pred p, q;\n\tsetp.ne.u32 p, %1, 0;\n\tbar.red.or.pred q, %2, 128, p;\n\tselp.u32 %0, 1, 0, q;\n\t}" : "=r"(r) : "r"(v ? 1u : 0u), "r"(2 + half) : "memory");
+    asm volatile("{\n\t.reg .pred p, q;\n\tsetp.ne.u32 p, %1, 0;\n\tbar.red.or.pred q, %2, 128, p;\n\tselp.u32 %0, 1, 0, q;\n\t}" : "=r"(r) : "r"(v ? 1u : 0u), "r"(2 + part) : "memory");
     return r != 0;
+}
+// untiled copy to shared memory, counted on an mbarrier
+__device__ __forceinline__ void bulk_load(uint32_t dst, const void* src, uint32_t bytes, uint32_t bar) {
+    asm volatile("cp.async.bulk.shared::cluster.global.mbarrier::complete_tx::bytes [%0], [%1], %2, [%3];" ::"r"(dst), "l"(src), "r"(bytes), "r"(bar) : "memory");
 }
 
 // eight codes -> four packed pairs, nibbles in the order 0 4 1 5 2 6 3 7
@@ -127,17 +156,13 @@ __device__ __forceinline__ void unpack8(uint32_t w, uint32_t* r) {
     r[2] = centred_half<0>(x);
     r[3] = centred_half<4>(x);
 }
-// place of 16-byte piece c of a packed row in its staging buffer: rows of D / 2 bytes, pieces swapped so that eight lanes
-// reading the same piece of eight rows hit eight different bank groups
-template <int D> __device__ __forceinline__ uint32_t piece_at(int row, int c) {
-    return D == 128 ? (uint32_t)(row * 64 + ((c ^ ((row >> 1) & 3)) << 4)) : (uint32_t)(row * 32 + ((c ^ ((row >> 2) & 1)) << 4));
-}
-
 template <int D, int N>
 __global__ void __launch_bounds__(THREADS, 1) k_attn_kv4_tc(const __grid_constant__ Kv4AttnParams p) {
     using SH = Shape<D, N>;
-    constexpr int NB = N / 16;                       // blocks of eight query rows a softmax thread sees (it takes every other block)
+    constexpr int NB = N / 8 / PARTS;                // blocks of eight query rows of a softmax thread
+    constexpr int JB = 2;                            // ... and at a time
     constexpr int PIECES = D / 32;                   // 16-byte pieces of a packed row
+    constexpr uint32_t ROW = D / 2;                  // bytes of a packed row
     extern __shared__ uint8_t smem_raw[];
     const uint32_t raw_addr = smem_u32(smem_raw), pad = (1024u - (raw_addr & 1023u)) & 1023u;
     uint8_t* base = smem_raw + pad;
@@ -146,20 +171,21 @@ __global__ void __launch_bounds__(THREADS, 1) k_attn_kv4_tc(const __grid_constan
     const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
 
     if (threadIdx.x == 0) {
-        mbar_init(smem_u32(&sm->q_full), SOFT);
+        mbar_init(smem_u32(&sm->q_full), SOFT / 32);
         for (int b = 0; b < 2; ++b) {
-            mbar_init(smem_u32(&sm->k_full[b]), CONV); mbar_init(smem_u32(&sm->k_empty[b]), 1);
-            mbar_init(smem_u32(&sm->v_full[b]), CONV); mbar_init(smem_u32(&sm->v_empty[b]), 1);
-            mbar_init(smem_u32(&sm->s_full[b]), 1); mbar_init(smem_u32(&sm->s_empty[b]), SOFT);
-            mbar_init(smem_u32(&sm->p_full[b]), SOFT); mbar_init(smem_u32(&sm->p_empty[b]), 1);
+            mbar_init(smem_u32(&sm->k_full[b]), CONV / 64); mbar_init(smem_u32(&sm->k_empty[b]), 1);
+            mbar_init(smem_u32(&sm->v_full[b]), CONV / 64); mbar_init(smem_u32(&sm->v_empty[b]), 1);
+            mbar_init(smem_u32(&sm->s_full[b]), 1); mbar_init(smem_u32(&sm->s_empty[b]), SOFT / 32);
+            mbar_init(smem_u32(&sm->p_full[b]), SOFT / 32); mbar_init(smem_u32(&sm->p_empty[b]), 1);
         }
         mbar_init(smem_u32(&sm->drain), 1);
         mbar_init(smem_u32(&sm->drain_pv), 1);
-        for (int b = 0; b < ITEMS; ++b) { mbar_init(smem_u32(&sm->item_full[b]), 1); mbar_init(smem_u32(&sm->item_empty[b]), 1 + CONV / 32 + 2); }
+        for (int b = 0; b < 4; ++b) { mbar_init(smem_u32(&sm->c_full[b]), 1); mbar_init(smem_u32(&sm->c_empty[b]), CONV / 32); }
+        for (int b = 0; b < ITEMS; ++b) { mbar_init(smem_u32(&sm->item_full[b]), 1); mbar_init(smem_u32(&sm->item_empty[b]), 4); }      // softmax, both issuers, loader
         sm->abort_flag = 0;
         asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
     }
-    if (warp == 12) {
+    if (warp == 24) {
         asm volatile("tcgen05.alloc.cta_group::1.sync.aligned.shared::cta.b32 [%0], %1;" ::"r"(smem_u32(&sm->tmem_base)), "r"(512u) : "memory");
         asm volatile("tcgen05.relinquish_alloc_permit.cta_group::1.sync.aligned;" ::: "memory");
     }
@@ -175,7 +201,7 @@ __global__ void __launch_bounds__(THREADS, 1) k_attn_kv4_tc(const __grid_constan
     // The k-th item of this CTA (take = 0: there are no more, or a wait has run out).  One thread looks; who takes it together
     // with others gets it from that thread, so that all of them go on or stop alike.
     auto item_get = [&](int k) -> Kv4Item {
-        if (!mbar_wait(smem_u32(&sm->item_full[k % ITEMS]), (k / ITEMS) & 1, abort_flag, w.status, DEV_TIMEOUT_EPI)) { Kv4Item none{}; return none; }
+        if (!wait(smem_u32(&sm->item_full[k % ITEMS]), (k / ITEMS) & 1, abort_flag, w.status, DEV_TIMEOUT_EPI)) { Kv4Item none{}; return none; }
         const Kv4Item it = sm->item[k % ITEMS];
         mbar_arrive(smem_u32(&sm->item_empty[k % ITEMS]));
         return it;
@@ -183,113 +209,90 @@ __global__ void __launch_bounds__(THREADS, 1) k_attn_kv4_tc(const __grid_constan
     auto rows_of = [&](const Kv4Item& it) { const int r = it.q.n * p.group - it.tile * N; return r < N ? r : N; };
     auto cols_of = [&](int rows) { return (rows + 15) & ~15; };           // MMA N: a multiple of 16
 
-    if (warp >= 8 && warp < 12) {
+    if (warp >= 16 && warp < 24) {
         asm volatile("setmaxnreg.dec.sync.aligned.u32 %0;" ::"n"(REGS_CONV));
-        // ------------------------------------------------ unpacking warps: thread = key
-        const int quad = warp - 8, key = quad * 32 + lane;
-        const uint32_t st0 = base_a + SH::ST_AT + quad * 32 * (D / 2);    // this warp's 32 rows of a stage (K; V UNIT rows further)
-        const int R = 1 << w.shift;
-        int items = 0;                                                    // load cursor
-        bool more = true;
-        int lseq = 0, lhead = 0, lch = 0, lend = 0, lkeys = 0, n = 0;                          // n: units asked for so far
-        auto load_next = [&](int i) {
-            if (lch >= lend && more) {
-                if (lane == 0) {
-                    const Kv4Item it = item_get(items);
-                    lseq = it.seq; lhead = it.head; lch = it.chunk0; lend = it.chunk0 + it.take; lkeys = it.keys;
-                }
-                ++items;
-                lseq = __shfl_sync(0xffffffffu, lseq, 0);
-                lhead = __shfl_sync(0xffffffffu, lhead, 0);
-                lch = __shfl_sync(0xffffffffu, lch, 0);
-                lend = __shfl_sync(0xffffffffu, lend, 0);
-                lkeys = __shfl_sync(0xffffffffu, lkeys, 0);
-                more = lend > lch;
-            }
-            if (lch < lend) {
-                const uint32_t st = st0 + (uint32_t)(i % SH::STAGES) * SH::ST_BYTES;
-                const int key0 = lch * UNIT + quad * 32;
-                int page[2];                                              // of this warp's two groups of 16 keys
-#pragma unroll
-                for (int h = 0; h < 2; ++h) page[h] = key0 + 16 * h < lkeys ? kv4_page(w, lseq, key0 + 16 * h) : -1;
-                constexpr int PER = 32 / PIECES;                          // rows a warp-wide copy covers
-#pragma unroll
-                for (int j = 0; j < PIECES; ++j) {
-                    const int row = lane / PIECES + PER * j, c = lane % PIECES;
-                    const int pg = row < 16 ? page[0] : page[1];
-                    const int r = (key0 + row) & (R - 1);
-                    const uint8_t* blk = p.pool + kv4_block_at(w, pg < 0 ? 0 : pg, lhead);
-                    cp16(st + piece_at<D>(row, c), blk + kv4_code_at(R, D, 0, r) + 16 * c, pg >= 0);
-                    cp16(st + UNIT * (D / 2) + piece_at<D>(row, c), blk + kv4_code_at(R, D, 1, r) + 16 * c, pg >= 0);
-                }
-                if (lane < 16) {                                          // scales and minima: four keys a piece, K then V
-                    const int which = lane >> 3, row = (lane & 7) * 4, pg = row < 16 ? page[0] : page[1];
-                    const uint8_t* blk = p.pool + kv4_block_at(w, pg < 0 ? 0 : pg, lhead);
-                    cp16(smem_u32(&sm->par[i & (PAR_SLOTS - 1)][which][quad * 32 + row]), blk + kv4_param_at(R, D, 2, which, (key0 + row) & (R - 1)), pg >= 0);
-                } else if (lane < 18) {
-                    sm->page_there[i & (PAR_SLOTS - 1)][2 * quad + lane - 16] = (lane == 16 ? page[0] : page[1]) >= 0;
-                }
-                ++lch;
-                ++n;
-            }
-            cp_commit();
+        const int quad = warp & 3;                                        // this warp's 32 keys of a unit
+        // units come until the loader says that there are no more (an empty stage)
+        auto unit_there = [&](int i) -> bool {
+            bool ok = false;
+            if (lane == 0) ok = wait(smem_u32(&sm->c_full[i % SH::STAGES]), (i / SH::STAGES) & 1, abort_flag, w.status, DEV_TIMEOUT_TMA) && sm->unit_there[i % SH::STAGES];
+            ok = __shfl_sync(0xffffffffu, ok, 0);
+            return ok;
         };
+        if (warp < 20) {
+            // ------------------------------------------------ K: thread = key = tensor-memory lane
 #pragma unroll 1
-        for (int i = 0; i < SH::STAGES - 1; ++i) load_next(i);
-        for (int i = 0; i < n; ++i) {                                     // (n runs ahead until the last unit has been asked for)
-            const int b = i & 1;
-            const uint32_t st = st0 + (uint32_t)(i % SH::STAGES) * SH::ST_BYTES;
-            __syncwarp();                                                 // everybody has read the stage that is filled next
-            load_next(i + SH::STAGES - 1);
-            cp_wait<SH::STAGES - 1>();
-            __syncwarp();
-            if (i >= 2) mbar_wait(smem_u32(&sm->k_empty[b]), ((i >> 1) - 1) & 1, abort_flag, w.status, DEV_TIMEOUT_TMEM);
-            tc_fence_after();
+            for (int i = 0; unit_there(i); ++i) {
+                const int b = i & 1;
+                const uint32_t st = base_a + SH::ST_AT + (uint32_t)(i % SH::STAGES) * SH::ST_BYTES + (quad * 32 + lane) * ROW;
+                if (i >= 2) wait(smem_u32(&sm->k_empty[b]), ((i >> 1) - 1) & 1, abort_flag, w.status, DEV_TIMEOUT_TMEM);
+                tc_fence_after();
+                const uint32_t tk = tmem + SH::T_K + b * ROW + ((uint32_t)(quad * 32) << 16);
+                uint4 x = lds128(st);
 #pragma unroll 1
-            for (int c = 0; c < PIECES; ++c) {
-                const uint4 x = lds128(st + piece_at<D>(lane, c));
-                uint32_t r[16];
-                unpack8(x.x, r); unpack8(x.y, r + 4); unpack8(x.z, r + 8); unpack8(x.w, r + 12);
-                st16(tmem + SH::T_K + b * (D / 2) + c * 16 + ((uint32_t)(quad * 32) << 16), r);
+                for (int c = 0; c < PIECES; ++c) {
+                    uint32_t r[16];
+                    unpack8(x.x, r); unpack8(x.y, r + 4); unpack8(x.z, r + 8); unpack8(x.w, r + 12);
+                    if (c + 1 < PIECES) x = lds128(st + 16 * (c + 1));
+                    st16(tk + c * 16, r);
+                }
+                warp_arrive(smem_u32(&sm->c_empty[i % SH::STAGES]));
+                st_wait();
+                tc_fence_before();
+                warp_arrive(smem_u32(&sm->k_full[b]));
             }
-            st_wait();
-            tc_fence_before();
-            mbar_arrive(smem_u32(&sm->k_full[b]));
-            if (i >= 2) mbar_wait(smem_u32(&sm->v_empty[b]), ((i >> 1) - 1) & 1, abort_flag, w.status, DEV_TIMEOUT_TMEM);
-            const uint32_t vt = base_a + SH::V_AT + b * SH::V_BYTES + key * 128;
+        } else {
+            // ------------------------------------------------ V: a lane takes one 16-byte piece of a row at a time; eight lanes read 128
+            // bytes in a row, and their four stores go to eight different bank groups
+            const int row0 = quad * 32 + lane / PIECES, c = lane % PIECES, turn = D == 128 ? (c >> 1) << 1 : 0;
+            constexpr int PER = 32 / PIECES;
 #pragma unroll 1
-            for (int c = 0; c < PIECES; ++c) {
-                const uint4 x = lds128(st + UNIT * (D / 2) + piece_at<D>(lane, c));
-                uint32_t r[16];
-                unpack8(x.x, r); unpack8(x.y, r + 4); unpack8(x.z, r + 8); unpack8(x.w, r + 12);
+            for (int i = 0; unit_there(i); ++i) {
+                const int b = i & 1;
+                const uint32_t st = base_a + SH::ST_AT + (uint32_t)(i % SH::STAGES) * SH::ST_BYTES + UNIT * ROW + row0 * ROW + 16 * c;
+                if (i >= 2) wait(smem_u32(&sm->v_empty[b]), ((i >> 1) - 1) & 1, abort_flag, w.status, DEV_TIMEOUT_TMEM);
+                uint4 x = lds128(st);
+#pragma unroll 1
+                for (int j = 0; j < PIECES; ++j) {
+                    const int key = row0 + j * PER;
+                    const uint32_t vt = base_a + SH::V_AT + b * SH::V_BYTES + (c >> 1) * V_SLAB + key * 128;
+                    const uint32_t wd[4] = {turn ? x.z : x.x, turn ? x.w : x.y, turn ? x.x : x.z, turn ? x.y : x.w};
+                    if (j + 1 < PIECES) x = lds128(st + (j + 1) * PER * ROW);
 #pragma unroll
-                for (int k = 0; k < 4; ++k) sts128(vt + (c >> 1) * V_SLAB + ((((c & 1) * 4 + k) ^ (key & 7)) << 4), r + 4 * k);
+                    for (int k = 0; k < 4; ++k) {
+                        uint32_t r[4];
+                        unpack8(wd[k], r);
+                        sts128(vt + ((((c & 1) * 4 + (k ^ turn)) ^ (key & 7)) << 4), r);
+                    }
+                }
+                warp_arrive(smem_u32(&sm->c_empty[i % SH::STAGES]));
+                asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
+                warp_arrive(smem_u32(&sm->v_full[b]));
             }
-            asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
-            mbar_arrive(smem_u32(&sm->v_full[b]));
         }
-        cp_wait<0>();
-    } else if (warp >= 12) {
+    } else if (warp >= 24) {
         asm volatile("setmaxnreg.dec.sync.aligned.u32 %0;" ::"n"(REGS_ISSUE));
-        if (warp == 12) {
+        if (warp == 24) {
         // ------------------------------------------------ issuer of S^T = K Q^T
         if (lane == 0) {
             const uint64_t q_desc = smem_desc_sw128(base_a);
             bool ok = true;
             int i = 0, items = 0;
+#pragma unroll 1
             while (ok) {
                 const Kv4Item it = item_get(items);
                 if (it.take == 0) break;
                 const uint32_t idesc = instr_desc_f16(cols_of(rows_of(it)), false);
-                ok = mbar_wait(smem_u32(&sm->q_full), items & 1, abort_flag, w.status, DEV_TIMEOUT_MMA);
+                ok = wait(smem_u32(&sm->q_full), items & 1, abort_flag, w.status, DEV_TIMEOUT_MMA);
                 ++items;
+#pragma unroll 1
                 for (int k = 0; ok && k < it.take; ++k, ++i) {
                     const int b = i & 1;
-                    ok = mbar_wait(smem_u32(&sm->k_full[b]), (i >> 1) & 1, abort_flag, w.status, DEV_TIMEOUT_MMA);
-                    if (ok && i >= 2) ok = mbar_wait(smem_u32(&sm->s_empty[b]), ((i >> 1) - 1) & 1, abort_flag, w.status, DEV_TIMEOUT_TMEM);
+                    ok = wait(smem_u32(&sm->k_full[b]), (i >> 1) & 1, abort_flag, w.status, DEV_TIMEOUT_MMA);
+                    if (ok && i >= 2) ok = wait(smem_u32(&sm->s_empty[b]), ((i >> 1) - 1) & 1, abort_flag, w.status, DEV_TIMEOUT_TMEM);
                     if (!ok) break;
                     tc_fence_after();
-#pragma unroll
+#pragma unroll 1
                     for (int ks = 0; ks < D / 16; ++ks)                  // 16 channels: 8 columns of K, 32 bytes along Q's rows
                         mma_ts(tmem + SH::T_S + b * N, tmem + SH::T_K + b * (D / 2) + ks * 8,
                                q_desc + (uint64_t)((((ks >> 2) * N * 128) >> 4) + (ks & 3) * 2), idesc, ks > 0 ? 1u : 0u);
@@ -299,10 +302,10 @@ __global__ void __launch_bounds__(THREADS, 1) k_attn_kv4_tc(const __grid_constan
             }
             if (!ok) {
                 tc_commit(smem_u32(&sm->drain));
-                for (uint32_t spin = 0; spin < SPIN_LIMIT && !mbar_try(smem_u32(&sm->drain), 0); ++spin) __nanosleep(64);
+                wait_drain(smem_u32(&sm->drain), 0);
             }
         }
-        } else if (warp == 13) {
+        } else if (warp == 25) {
         // ------------------------------------------------ issuer of O^T += V^T P^T
         if (lane == 0) {
             // both operands have the MMA's K dimension (keys) as rows of 128 bytes: 64 channels of V, 64 query rows of P
@@ -310,17 +313,19 @@ __global__ void __launch_bounds__(THREADS, 1) k_attn_kv4_tc(const __grid_constan
             const uint64_t p_desc = smem_desc_sw128(base_a + SH::P_AT, UNIT * 128);
             bool ok = true;
             int i = 0, items = 0;
+#pragma unroll 1
             while (ok) {
                 const Kv4Item it = item_get(items++);
                 if (it.take == 0) break;
                 const uint32_t idesc = instr_desc_f16(cols_of(rows_of(it)), true) | (1u << 15);
+#pragma unroll 1
                 for (int k = 0; ok && k < it.take; ++k, ++i) {
                     const int b = i & 1;
-                    ok = mbar_wait(smem_u32(&sm->v_full[b]), (i >> 1) & 1, abort_flag, w.status, DEV_TIMEOUT_MMA);
-                    if (ok) ok = mbar_wait(smem_u32(&sm->p_full[b]), (i >> 1) & 1, abort_flag, w.status, DEV_TIMEOUT_MMA);
+                    ok = wait(smem_u32(&sm->v_full[b]), (i >> 1) & 1, abort_flag, w.status, DEV_TIMEOUT_MMA);
+                    if (ok) ok = wait(smem_u32(&sm->p_full[b]), (i >> 1) & 1, abort_flag, w.status, DEV_TIMEOUT_MMA);
                     if (!ok) break;
                     tc_fence_after();
-#pragma unroll
+#pragma unroll 1
                     for (int ks = 0; ks < UNIT / 16; ++ks)               // 16 keys: 16 rows of both tiles
                         tc_mma_f16(tmem + SH::T_O, v_desc + (uint64_t)((b * SH::V_BYTES + ks * 2048) >> 4), p_desc + (uint64_t)((b * SH::P_BYTES + ks * 2048) >> 4),
                                    idesc, (k > 0 || ks > 0) ? 1u : 0u);
@@ -330,45 +335,93 @@ __global__ void __launch_bounds__(THREADS, 1) k_attn_kv4_tc(const __grid_constan
             }
             if (!ok) {
                 tc_commit(smem_u32(&sm->drain_pv));
-                for (uint32_t spin = 0; spin < SPIN_LIMIT && !mbar_try(smem_u32(&sm->drain_pv), 0); ++spin) __nanosleep(64);
+                wait_drain(smem_u32(&sm->drain_pv), 0);
             }
         }
-        } else if (warp == 14) {
+        } else if (warp == 26) {
         // ------------------------------------------------ scheduler
         if (lane == 0) {
             int k = 0;
             bool ok = true;
+#pragma unroll 1
             for (int64_t u = u_beg; ok;) {
                 Kv4Item it{};
+#pragma unroll 1
                 while (u < u_end && it.take == 0) {
                     it = kv4_find_item(til, sm->sums, w.n_seqs, [&](int s_) { return kv4_load_seq(w, s_); }, u, u_end);
                     u = it.next;
                 }
                 if (it.take > 0) it.keys = kv4_tile_keys(til, it.q, it.tile);
-                if (k >= ITEMS) ok = mbar_wait(smem_u32(&sm->item_empty[k % ITEMS]), ((k / ITEMS) - 1) & 1, abort_flag, w.status, DEV_TIMEOUT_EPI);
+                if (k >= ITEMS) ok = wait(smem_u32(&sm->item_empty[k % ITEMS]), ((k / ITEMS) - 1) & 1, abort_flag, w.status, DEV_TIMEOUT_EPI);
                 sm->item[k % ITEMS] = it;
                 mbar_arrive(smem_u32(&sm->item_full[k % ITEMS]));
                 ++k;
                 if (it.take == 0) break;
             }
         }
+        } else if (warp == 27) {
+        // ------------------------------------------------ loader: lane = (kind, group of 16 keys): K codes, V codes, K and V scales
+        const int kind = lane >> 3, grp = lane & 7, R = 1 << w.shift;
+        const uint32_t bytes = kind < 2 ? 16 * ROW : 64;
+        int i = 0;
+#pragma unroll 1
+        for (int items = 0;; ++items) {
+            Kv4Item it{};
+            if (lane == 0) it = item_get(items);
+            const int take = __shfl_sync(0xffffffffu, it.take, 0), chunk0 = __shfl_sync(0xffffffffu, it.chunk0, 0), keys = __shfl_sync(0xffffffffu, it.keys, 0);
+            const int seq = __shfl_sync(0xffffffffu, it.seq, 0), head = __shfl_sync(0xffffffffu, it.head, 0);
+            // (a page's id is looked up one unit ahead)
+            auto look = [&](int k) { const int key0 = (chunk0 + k) * UNIT + 16 * grp; return k < take && key0 < keys ? __ldg(w.table + (size_t)seq * w.max_pages + (key0 >> w.shift)) : -1; };
+            int next = look(0);
+#pragma unroll 1
+            for (int k = 0; k < (take > 0 ? take : 1); ++k, ++i) {
+                const int page = next, key0 = (chunk0 + k) * UNIT + 16 * grp, s_ = i % SH::STAGES, slot = i & (PAR_SLOTS - 1);
+                next = look(k + 1);
+                const bool there = take > 0 && key0 < keys && (unsigned)page < (unsigned)w.n_pages;
+                if (take > 0 && key0 < keys && !there) atomicCAS(w.status, DEV_OK, DEV_KV4_PAGE);
+                if (i >= SH::STAGES) wait(smem_u32(&sm->c_empty[s_]), ((i / SH::STAGES) - 1) & 1, abort_flag, w.status, DEV_TIMEOUT_TMA);
+                const uint32_t full = smem_u32(&sm->c_full[s_]);
+                uint32_t total = there ? bytes : 0u;
+#pragma unroll
+                for (int o = 16; o > 0; o >>= 1) total += __shfl_xor_sync(0xffffffffu, total, o);
+                if (kind == 0) sm->page_there[slot][grp] = there;
+                if (lane == 0) sm->unit_there[s_] = take > 0;
+                __syncwarp();
+                if (lane == 0) { if (total) mbar_expect_tx(full, total); else mbar_arrive(full); }
+                __syncwarp();
+                if (there) {
+                    const uint8_t* blk = p.pool + kv4_block_at(w, page, head);
+                    const int r = key0 & (R - 1);
+                    const uint32_t dst = kind < 2 ? base_a + SH::ST_AT + (uint32_t)s_ * SH::ST_BYTES + kind * UNIT * ROW + 16 * grp * ROW
+                                                  : smem_u32(&sm->par[slot][kind - 2][16 * grp]);
+                    bulk_load(dst, blk + (kind < 2 ? kv4_code_at(R, D, kind, r) : kv4_param_at(R, D, 2, kind - 2, r)), bytes, full);
+                }
+            }
+            if (take == 0) break;
+        }
+        // no copy is in flight when the block ends, whatever the others have given up
+        if (lane == 0)
+#pragma unroll 1
+            for (int k = i > SH::STAGES ? i - SH::STAGES : 0; k < i; ++k)
+                wait_drain(smem_u32(&sm->c_full[k % SH::STAGES]), (k / SH::STAGES) & 1);
         }
     } else {
         asm volatile("setmaxnreg.inc.sync.aligned.u32 %0;" ::"n"(REGS_SOFT));
         // ------------------------------------------------ softmax warps
-        // half: which blocks of eight query rows (half, half + 2, ...); quad: which 32 keys (tensor-memory lanes)
-        const int half = warp >> 2, quad = warp & 3, g = lane >> 2, t = lane & 3, tid = threadIdx.x;
+        // part: which blocks of eight query rows (part, part + PARTS, ...); quad: which 32 keys (tensor-memory lanes)
+        const int part = warp >> 2, quad = warp & 3, g = lane >> 2, t = lane & 3, tid = threadIdx.x;
         const float sl2 = p.scale * KV4_LOG2E;
         int i = 0;                                                        // unit of this CTA
+#pragma unroll 1
         for (int items = 0;; ++items) {
             if (tid == 0) sm->cur = item_get(items);
             named_sync<1, SOFT>();
-            const Kv4Item it = sm->cur;
+            const Kv4Item& it = sm->cur;                                  // stays until the barrier at the item's end
             if (it.take == 0) break;
             const int rows = rows_of(it), cols = cols_of(rows);
             // ---- queries to shared memory, channels of a word in the order the nibbles come in; their sums
             {
-                constexpr int C8 = D / 8, MOST = N * C8 / SOFT;           // 16-byte pieces of a row, and at most of a thread
+                constexpr int C8 = D / 8, MOST = (N * C8 + SOFT - 1) / SOFT;      // 16-byte pieces of a row, and at most of a thread
                 uint4 v[MOST];
 #pragma unroll
                 for (int z = 0; z < MOST; ++z) {                          // all loads first
@@ -393,7 +446,7 @@ __global__ void __launch_bounds__(THREADS, 1) k_attn_kv4_tc(const __grid_constan
                     if (c == 0) sm->qs[rl] = s;
                 }
                 asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
-                mbar_arrive(smem_u32(&sm->q_full));
+                warp_arrive(smem_u32(&sm->q_full));
                 named_sync<1, SOFT>();                                    // the sums are read by everybody
             }
             // running sums and references of this thread's rows: rows 2 t + e of its blocks
@@ -403,9 +456,10 @@ __global__ void __launch_bounds__(THREADS, 1) k_attn_kv4_tc(const __grid_constan
 #pragma unroll
                 for (int e = 0; e < 2; ++e) { l[j][e] = ms[j][e] = 0.f; ref[j][e] = -INFINITY; }
             float vmul = 0x1p24f;                                         // 2^-e of V's scales
+#pragma unroll 1
             for (int k = 0; k < it.take; ++k, ++i) {
                 const int b = i & 1, key0 = (it.chunk0 + k) * UNIT + quad * 32 + g;
-                mbar_wait(smem_u32(&sm->s_full[b]), (i >> 1) & 1, abort_flag, w.status, DEV_TIMEOUT_EPI);
+                wait(smem_u32(&sm->s_full[b]), (i >> 1) & 1, abort_flag, w.status, DEV_TIMEOUT_EPI);
                 tc_fence_after();
                 // (the scales were in place before the unit's keys were: the same threads wrote them)
                 uint32_t there = 0;                                       // which of this thread's keys have a page
@@ -423,17 +477,17 @@ __global__ void __launch_bounds__(THREADS, 1) k_attn_kv4_tc(const __grid_constan
                 // (the whole warp takes the same branches on `all`: every key of the unit is visible to every row)
                 const bool all = (it.chunk0 + k + 1) * UNIT <= it.q.len && __all_sync(0xffffffffu, there == 15u);
 #pragma unroll
-                for (int j0 = 0; j0 < NB; j0 += 4) {                      // 32 of this thread's scores at a time
-                    if (j0 > 0 && 8 * (2 * j0 + half) >= cols) break;
-                    const uint32_t ts = tmem + SH::T_S + b * N + 8 * (2 * j0 + half) + ((uint32_t)(quad * 32) << 16);
+                for (int j0 = 0; j0 < NB; j0 += JB) {                     // 16 of this thread's scores at a time
+                    if (8 * (PARTS * j0 + part) >= cols) break;           // (whole parts have nothing when the tile has few rows)
+                    const uint32_t ts = tmem + SH::T_S + b * N + 8 * (PARTS * j0 + part) + ((uint32_t)(quad * 32) << 16);
                     uint32_t vis = 0xffffffffu;                           // bit 8 j + 4 e + x: row e of block j sees key x
-                    if (!all) {
+                    if (__builtin_expect(!all, 0)) {
                         vis = 0u;
 #pragma unroll
-                        for (int j = 0; j < 4; ++j)
+                        for (int j = 0; j < JB; ++j)
 #pragma unroll
                             for (int e = 0; e < 2; ++e) {
-                                const int node = (it.tile * N + 8 * (2 * (j0 + j) + half) + 2 * t + e) / p.group;
+                                const int node = (it.tile * N + 8 * (PARTS * (j0 + j) + part) + 2 * t + e) / p.group;
                                 const uint32_t w32 = sees(p, it.q, node, key0 - it.q.len);
 #pragma unroll
                                 for (int x = 0; x < 4; ++x) vis |= ((w32 >> (8 * x)) & (there >> x) & 1u) << (8 * j + 4 * e + x);
@@ -442,19 +496,19 @@ __global__ void __launch_bounds__(THREADS, 1) k_attn_kv4_tc(const __grid_constan
                     // Scores of key x and row e of block j (registers 2 (x & 1) + e of fragment x >> 1), in powers of two, against
                     // the rows' references.  Where one of the 128 threads of these rows finds a score too far above, they agree on
                     // new references and look again.
-                    uint32_t s[4][2][4];
+                    uint32_t s[JB][2][4];
                     bool settled = false;
 #pragma unroll 1
                     for (;;) {
 #pragma unroll
-                        for (int j = 0; j < 4; ++j)
+                        for (int j = 0; j < JB; ++j)
 #pragma unroll
-                            for (int h = 0; h < 2; ++h) ld_frag(ts + 16 * j + ((uint32_t)(16 * h) << 16), s[j][h]);
+                            for (int h = 0; h < 2; ++h) ld_frag(ts + 8 * PARTS * j + ((uint32_t)(16 * h) << 16), s[j][h]);
                         ld_wait();
                         float top = -INFINITY;
 #pragma unroll
-                        for (int j = 0; j < 4; ++j) {
-                            const int c8 = 8 * (2 * (j0 + j) + half);
+                        for (int j = 0; j < JB; ++j) {
+                            const int c8 = 8 * (PARTS * (j0 + j) + part);
                             const float2 qq = *reinterpret_cast<const float2*>(&sm->qs[c8 + 2 * t]);
                             float tj = -INFINITY;
 #pragma unroll
@@ -468,31 +522,31 @@ __global__ void __launch_bounds__(THREADS, 1) k_attn_kv4_tc(const __grid_constan
                             }
                             if (c8 < cols) top = fmaxf(top, tj);          // (blocks behind the tile's rows hold anything)
                         }
-                        if (!all) {
+                        if (__builtin_expect(!all, 0)) {
                             top = -INFINITY;
 #pragma unroll
-                            for (int j = 0; j < 4; ++j)
+                            for (int j = 0; j < JB; ++j)
 #pragma unroll
                                 for (int e = 0; e < 2; ++e)
 #pragma unroll
                                     for (int x = 0; x < 4; ++x) {
                                         uint32_t& r = s[j][x >> 1][2 * (x & 1) + e];
                                         if (!((vis >> (8 * j + 4 * e + x)) & 1u)) r = __float_as_uint(-INFINITY);
-                                        if (8 * (2 * (j0 + j) + half) < cols) top = fmaxf(top, __uint_as_float(r));
+                                        if (8 * (PARTS * (j0 + j) + part) < cols) top = fmaxf(top, __uint_as_float(r));
                                     }
                         }
                         bool over = top > RAISE;
                         if (j0 == 0) over = over || fmaxf(fmaxf(vs[0], vs[1]), fmaxf(vs[2], vs[3])) * vmul > 128.f;
-                        if (settled || !half_any(half, over)) break;
+                        if (settled || __builtin_expect(!part_any(part, over), 1)) break;
                         settled = true;
                         // plain scores of the unit, their maxima by row, and the largest of V's scales
 #pragma unroll 1
-                        for (int j = 0; j < 4; ++j) {
-                            const int c8 = 8 * (2 * (j0 + j) + half);
+                        for (int j = 0; j < JB; ++j) {
+                            const int c8 = 8 * (PARTS * (j0 + j) + part);
                             const float2 qq = *reinterpret_cast<const float2*>(&sm->qs[c8 + 2 * t]);
                             uint32_t o[2][4];
-                            ld_frag(ts + 16 * j, o[0]);
-                            ld_frag(ts + 16 * j + (16u << 16), o[1]);
+                            ld_frag(ts + 8 * PARTS * j, o[0]);
+                            ld_frag(ts + 8 * PARTS * j + (16u << 16), o[1]);
                             ld_wait();
 #pragma unroll
                             for (int e = 0; e < 2; ++e) {
@@ -510,19 +564,19 @@ __global__ void __launch_bounds__(THREADS, 1) k_attn_kv4_tc(const __grid_constan
                         for (int x = 0; x < 4; ++x) if (vs[x] <= 65504.f) vx = fmaxf(vx, vs[x]);
 #pragma unroll
                         for (int sh = 4; sh < 32; sh <<= 1) vx = fmaxf(vx, __shfl_xor_sync(0xffffffffu, vx, sh));
-                        if (lane == 0) sm->vmax[half][quad] = vx;
-                        half_sync(half);
+                        if (lane == 0) sm->vmax[part][quad] = vx;
+                        part_sync(part);
                         // the exponent changes before the unit's first weights only
                         float vnew = vmul;
-                        vx = fmaxf(fmaxf(sm->vmax[half][0], sm->vmax[half][1]), fmaxf(sm->vmax[half][2], sm->vmax[half][3]));
+                        vx = fmaxf(fmaxf(sm->vmax[part][0], sm->vmax[part][1]), fmaxf(sm->vmax[part][2], sm->vmax[part][3]));
                         if (j0 == 0 && vx * vmul > 1.f) vnew = exp2f(-ceilf(log2f(vx)));
                         const float fv = vnew / vmul;
                         vmul = vnew;
 #pragma unroll
                         for (int j = 0; j < NB; ++j) {
                             float f[2] = {1.f, 1.f};
-                            const int rl = 8 * (2 * j + half) + 2 * t;
-                            if (j >= j0 && j < j0 + 4) {
+                            const int rl = 8 * (PARTS * j + part) + 2 * t;
+                            if (j >= j0 && j < j0 + JB) {
 #pragma unroll
                                 for (int e = 0; e < 2; ++e) {
                                     const float m = fmaxf(fmaxf(sm->x[0][rl + e], sm->x[1][rl + e]), fmaxf(sm->x[2][rl + e], sm->x[3][rl + e]));
@@ -536,14 +590,14 @@ __global__ void __launch_bounds__(THREADS, 1) k_attn_kv4_tc(const __grid_constan
                             }
                             if (quad == 0 && g == 0) { sm->fac[rl] = f[0] * fv; sm->fac[rl + 1] = f[1] * fv; }
                         }
-                        half_sync(half);
+                        part_sync(part);
                         if (k > 0) {
                             // O^T holds the products of the units before once the last of them has completed (each P buffer's
                             // release is waited for again two units later, so its phases are seen one by one)
-                            mbar_wait(smem_u32(&sm->p_empty[(i - 1) & 1]), ((i - 1) >> 1) & 1, abort_flag, w.status, DEV_TIMEOUT_EPI);
+                            wait(smem_u32(&sm->p_empty[(i - 1) & 1]), ((i - 1) >> 1) & 1, abort_flag, w.status, DEV_TIMEOUT_EPI);
                             tc_fence_after();
 #pragma unroll 1
-                            for (int c0 = 8 * half; c0 < cols; c0 += 16) {      // this half's blocks of eight columns, both groups of 16 lanes
+                            for (int c0 = 8 * part; c0 < cols; c0 += 8 * PARTS) {      // this part's blocks of eight columns, both groups of 16 lanes
                                 const float2 f = *reinterpret_cast<const float2*>(&sm->fac[c0 + 2 * t]);
                                 const uint32_t to = tmem + SH::T_O + c0 + ((uint32_t)(quad * 32) << 16);
                                 uint32_t o[2][4];
@@ -560,35 +614,39 @@ __global__ void __launch_bounds__(THREADS, 1) k_attn_kv4_tc(const __grid_constan
                             st_wait();
                             tc_fence_before();
                         }
-                        half_sync(half);                                  // the exchange buffers may be written again
+                        part_sync(part);                                  // the exchange buffers may be written again
                     }
-                    if (j0 == 0 && i >= 2) mbar_wait(smem_u32(&sm->p_empty[b]), ((i >> 1) - 1) & 1, abort_flag, w.status, DEV_TIMEOUT_EPI);
+                    if (j0 == 0 && i >= 2) wait(smem_u32(&sm->p_empty[b]), ((i >> 1) - 1) & 1, abort_flag, w.status, DEV_TIMEOUT_EPI);
                     float vsc[4];
 #pragma unroll
                     for (int x = 0; x < 4; ++x) vsc[x] = vs[x] * vmul;
 #pragma unroll
-                    for (int j = 0; j < 4; ++j) {
-                        const int blk = 2 * (j0 + j) + half;
+                    for (int j = 0; j < JB; ++j) {
+                        const int blk = PARTS * (j0 + j) + part;
                         if (8 * blk >= cols) break;
+                        float pv[4][2], pm[4][2];
+#pragma unroll
+                        for (int x = 0; x < 4; ++x)
+#pragma unroll
+                            for (int e = 0; e < 2; ++e) {
+                                const float pe = ex2(__uint_as_float(s[j][x >> 1][2 * (x & 1) + e]));
+                                l[j0 + j][e] += pe;
+                                pv[x][e] = pe * vsc[x];
+                                pm[x][e] = pe * vm[x];
+                            }
+                        if (__builtin_expect(!all, 0)) {                                       // by selection: what a key holds stays out of rows that do not see it
+#pragma unroll
+                            for (int x = 0; x < 4; ++x)
+#pragma unroll
+                                for (int e = 0; e < 2; ++e)
+                                    if (!((vis >> (8 * j + 4 * e + x)) & 1u)) pv[x][e] = pm[x][e] = 0.f;
+                        }
                         uint32_t h4[4];
 #pragma unroll
                         for (int x = 0; x < 4; ++x) {
-                            float pe[2], pv[2], pm[2];
-#pragma unroll
-                            for (int e = 0; e < 2; ++e) {
-                                pe[e] = ex2(__uint_as_float(s[j][x >> 1][2 * (x & 1) + e]));
-                                l[j0 + j][e] += pe[e];
-                                pv[e] = pe[e] * vsc[x];
-                                pm[e] = pe[e] * vm[x];
-                            }
-                            if (!all) {                                   // by selection: what a key holds stays out of rows that do not see it
-#pragma unroll
-                                for (int e = 0; e < 2; ++e)
-                                    if (!((vis >> (8 * j + 4 * e + x)) & 1u)) pv[e] = pm[e] = 0.f;
-                            }
-                            ms[j0 + j][0] += pm[0];
-                            ms[j0 + j][1] += pm[1];
-                            const __half2 h2 = __floats2half2_rn(pv[0], pv[1]);
+                            ms[j0 + j][0] += pm[x][0];
+                            ms[j0 + j][1] += pm[x][1];
+                            const __half2 h2 = __floats2half2_rn(pv[x][0], pv[x][1]);
                             h4[x] = *reinterpret_cast<const uint32_t*>(&h2);
                         }
                         // lane's matrix row: key 32 quad + lane, query rows 8 blk .. 8 blk + 7
@@ -596,9 +654,9 @@ __global__ void __launch_bounds__(THREADS, 1) k_attn_kv4_tc(const __grid_constan
                     }
                 }
                 tc_fence_before();
-                mbar_arrive(smem_u32(&sm->s_empty[b]));
+                warp_arrive(smem_u32(&sm->s_empty[b]));
                 asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
-                mbar_arrive(smem_u32(&sm->p_full[b]));
+                warp_arrive(smem_u32(&sm->p_full[b]));
             }
             // ---- sums of the rows over the four warps that share them
 #pragma unroll
@@ -608,21 +666,21 @@ __global__ void __launch_bounds__(THREADS, 1) k_attn_kv4_tc(const __grid_constan
                     float a = l[j][e], c = ms[j][e];
 #pragma unroll
                     for (int o = 4; o < 32; o <<= 1) { a += __shfl_xor_sync(0xffffffffu, a, o); c += __shfl_xor_sync(0xffffffffu, c, o); }
-                    const int rl = 8 * (2 * j + half) + 2 * t + e;
+                    const int rl = 8 * (PARTS * j + part) + 2 * t + e;
                     if (g == 0) { sm->x[quad][rl] = a; sm->y[quad][rl] = c; if (quad == 0) sm->fac[rl] = ref[j][e]; }
                 }
             }
             named_sync<1, SOFT>();
-            mbar_wait(smem_u32(&sm->p_empty[(i - 1) & 1]), ((i - 1) >> 1) & 1, abort_flag, w.status, DEV_TIMEOUT_EPI);
+            wait(smem_u32(&sm->p_empty[(i - 1) & 1]), ((i - 1) >> 1) & 1, abort_flag, w.status, DEV_TIMEOUT_EPI);
             tc_fence_after();
             const int64_t c0 = it.first / per, c1 = (it.first + it.chunks - 1) / per;
             const bool whole = c0 == c1;
             float* slot = p.part + ((size_t)blockIdx.x * 2 + ((int64_t)blockIdx.x == c0 ? 1 : 0)) * ((size_t)N * (D + 2));
             const float vinv = 1.f / vmul;
-            // lane (16 h + g or + 8) of this quad is channel ch_of(lane); columns of this half's blocks
+            // lane (16 h + g or + 8) of this quad is channel ch_of(lane); columns of this part's blocks
             auto ch_of = [](int m) { return (m & ~7) | ((m & 1) * 4) | ((m & 7) >> 1); };       // 0 4 1 5 2 6 3 7
 #pragma unroll 1
-            for (int blk = half; 8 * blk < rows && quad * 32 < D; blk += 2) {
+            for (int blk = part; 8 * blk < rows && quad * 32 < D; blk += PARTS) {
                 uint32_t o[2][4];
                 const uint32_t to = tmem + SH::T_O + 8 * blk + ((uint32_t)(quad * 32) << 16);
                 ld_frag(to, o[0]);
@@ -666,7 +724,7 @@ __global__ void __launch_bounds__(THREADS, 1) k_attn_kv4_tc(const __grid_constan
 
     tc_fence_before();
     __syncthreads();
-    if (warp == 12) {
+    if (warp == 24) {
         tc_fence_after();
         asm volatile("tcgen05.dealloc.cta_group::1.sync.aligned.b32 %0, %1;" ::"r"(tmem), "r"(512u) : "memory");
     }

@@ -7,8 +7,10 @@
 
 #ifdef __CUDACC__
 #define GHD_HD __host__ __device__ __forceinline__
+#define GHD_ROLLED _Pragma("unroll 1")      // these loops run once an item: short code matters, not their speed
 #else
 #define GHD_HD inline
+#define GHD_ROLLED
 #endif
 
 namespace ghd {
@@ -64,6 +66,7 @@ GHD_HD int kv4_tile_chunks(const Kv4Tiling& t, const Kv4Seq& q, int tile) {
 // units of one head of a sequence
 GHD_HD int64_t kv4_head_units(const Kv4Tiling& t, const Kv4Seq& q) {
     int64_t u = 0;
+    GHD_ROLLED
     for (int i = 0, n = kv4_tiles(t, q.n); i < n; ++i) u += t.lead + kv4_tile_chunks(t, q, i);
     return u;
 }
@@ -83,6 +86,7 @@ template <typename SeqOf>
 GHD_HD Kv4Item kv4_find_item(const Kv4Tiling& t, const int64_t* sums, int n_seqs, SeqOf seq_of, int64_t u, int64_t u_end) {
     Kv4Item it;
     int lo = 0, hi = n_seqs - 1;    // the last sequence that starts at or before u: it has units, u is one of them
+    GHD_ROLLED
     while (lo < hi) {
         const int mid = (lo + hi + 1) >> 1;
         if (sums[mid] <= u) lo = mid; else hi = mid - 1;
@@ -101,6 +105,7 @@ GHD_HD Kv4Item kv4_find_item(const Kv4Tiling& t, const int64_t* sums, int n_seqs
     }
     rem -= it.head * head_units;
     it.tile = 0;
+    GHD_ROLLED
     for (;;) {
         it.chunks = kv4_tile_chunks(t, it.q, it.tile);
         if (rem < t.lead + it.chunks) break;
