@@ -41,7 +41,8 @@ template <> struct Op<__half> {
                      : "+f"(d[0]), "+f"(d[1]), "+f"(d[2]), "+f"(d[3]) : "r"(a0), "r"(a1), "r"(a2), "r"(a3), "r"(b0), "r"(b1));
     }
     // two codes (at bits SH .. SH + 3 of each half word) less 8
-    template <int SH> static __device__ __forceinline__ uint32_t centred(uint32_t w) { return centred_half<SH>(w); }
+    typedef HalfMagic Magic;
+    template <int SH> static __device__ __forceinline__ uint32_t centred(uint32_t w, const Magic& m) { return centred_half<SH>(w, m); }
     // (a, b) as TERMS packed pairs whose sum is (a, b) to 11 bits
     static __device__ __forceinline__ void split(float a, float b, uint32_t (&t)[1]) {
         const __half2 h = __floats2half2_rn(a, b);
@@ -54,8 +55,13 @@ template <> struct Op<float> {
         asm volatile("mma.sync.aligned.m16n8k16.row.col.f32.bf16.bf16.f32 {%0,%1,%2,%3}, {%4,%5,%6,%7}, {%8,%9}, {%0,%1,%2,%3};"
                      : "+f"(d[0]), "+f"(d[1]), "+f"(d[2]), "+f"(d[3]) : "r"(a0), "r"(a1), "r"(a2), "r"(a3), "r"(b0), "r"(b1));
     }
-    template <int SH> static __device__ __forceinline__ uint32_t centred(uint32_t w) {
-        const uint32_t x = ((w >> SH) & 0x000f000fu) | 0x43004300u;                  // 128 + c
+    struct Magic {
+        uint32_t e;
+        __device__ __forceinline__ Magic() : e(0x43004300u) { asm volatile("" : "+r"(e)); }
+    };
+    template <int SH> static __device__ __forceinline__ uint32_t centred(uint32_t w, const Magic& m) {
+        uint32_t x;                                                                  // 128 + c
+        asm("lop3.b32 %0, %1, 0x000f000f, %2, 0xea;" : "=r"(x) : "r"(w >> SH), "r"(m.e));
         const __nv_bfloat162 r = __hsub2(*reinterpret_cast<const __nv_bfloat162*>(&x), __floats2bfloat162_rn(136.f, 136.f));
         return *reinterpret_cast<const uint32_t*>(&r);
     }
@@ -126,6 +132,7 @@ __global__ void __launch_bounds__(WARPS * 32, Narrow<T, D, NT>::BLOCKS) k_attn_k
     const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5, g = lane >> 2, t = lane & 3;
     const int R = 1 << w.shift;
     const float sl2 = p.scale * KV4_LOG2E;
+    const typename O_::Magic magic;
     auto item_at = [&](int64_t x) { Kv4Item r; find_item(&w, &til, sums, x, u_end, &r); return r; };
 
     // ---- this warp's ring: 16 keys a stage, STAGES - 1 units ahead, over the borders of items
@@ -248,8 +255,8 @@ __global__ void __launch_bounds__(WARPS * 32, Narrow<T, D, NT>::BLOCKS) k_attn_k
 #pragma unroll
                     for (int hlf = 0; hlf < 2; ++hlf) {
                         const uint32_t wa = k0[j] >> (8 * hlf), wb = k1[j] >> (8 * hlf);
-                        const uint32_t a0 = O_::template centred<0>(wa), a1 = O_::template centred<0>(wb);
-                        const uint32_t a2 = O_::template centred<4>(wa), a3 = O_::template centred<4>(wb);
+                        const uint32_t a0 = O_::template centred<0>(wa, magic), a1 = O_::template centred<0>(wb, magic);
+                        const uint32_t a2 = O_::template centred<4>(wa, magic), a3 = O_::template centred<4>(wb, magic);
 #pragma unroll
                         for (int nt = 0; nt < NT; ++nt)
 #pragma unroll
@@ -351,8 +358,8 @@ __global__ void __launch_bounds__(WARPS * 32, Narrow<T, D, NT>::BLOCKS) k_attn_k
 #pragma unroll
                     for (int hlf = 0; hlf < 2; ++hlf) {
                         const uint32_t xs_ = x >> (8 * hlf), ys_ = y >> (8 * hlf);
-                        const uint32_t a0 = O_::template centred<0>(xs_), a1 = O_::template centred<4>(xs_);
-                        const uint32_t a2 = O_::template centred<0>(ys_), a3 = O_::template centred<4>(ys_);
+                        const uint32_t a0 = O_::template centred<0>(xs_, magic), a1 = O_::template centred<4>(xs_, magic);
+                        const uint32_t a2 = O_::template centred<0>(ys_, magic), a3 = O_::template centred<4>(ys_, magic);
                         const int mt = 4 * j + 2 * z + hlf;
 #pragma unroll
                         for (int nt = 0; nt < NT; ++nt)

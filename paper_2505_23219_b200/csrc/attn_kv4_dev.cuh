@@ -72,10 +72,16 @@ __device__ __forceinline__ uint32_t sees(const Kv4AttnParams& p, const Kv4Seq& q
 }
 
 // Codes of half type, less 8, for the two nibbles at bits SH .. SH + 3 of the half words of w: (w & mask) | exponent is
-// 1024 + c or 64 + c.
-template <int SH> __device__ __forceinline__ uint32_t centred_half(uint32_t w) {
-    constexpr uint32_t m = SH == 0 ? 0x000f000fu : 0x00f000f0u, e = SH == 0 ? 0x64006400u : 0x54005400u;
-    const uint32_t x = (w & m) | e;
+// 1024 + c or 64 + c.  The exponents come in registers the compiler does not see through, so that the two operations
+// stay one instruction.
+struct HalfMagic {
+    uint32_t e0, e4;
+    __device__ __forceinline__ HalfMagic() : e0(0x64006400u), e4(0x54005400u) { asm volatile("" : "+r"(e0), "+r"(e4)); }
+};
+template <int SH> __device__ __forceinline__ uint32_t centred_half(uint32_t w, const HalfMagic& m) {
+    uint32_t x;
+    if constexpr (SH == 0) asm("lop3.b32 %0, %1, 0x000f000f, %2, 0xea;" : "=r"(x) : "r"(w), "r"(m.e0));
+    else asm("lop3.b32 %0, %1, 0x00f000f0, %2, 0xea;" : "=r"(x) : "r"(w), "r"(m.e4));
     const __half2 off = SH == 0 ? __floats2half2_rn(-1032.f, -1032.f) : __floats2half2_rn(-72.f, -72.f);
     const __half2 r = __hadd2(*reinterpret_cast<const __half2*>(&x), off);
     return *reinterpret_cast<const uint32_t*>(&r);

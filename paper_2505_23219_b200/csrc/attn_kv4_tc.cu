@@ -2,14 +2,14 @@
 //
 // As in attn_kv4.cu the scales stay out of the products and keys are the M side: S^T [128 keys x rows] = K Q^T,
 // O^T [d_head x rows] = V^T P^T.  With keys on the tensor-memory lanes a thread owns whole key rows:
-//   K        warps 16..19: one thread per key unpacks its 4-bit row in registers and stores it to tensor memory, from where
+//   K        four warps: one thread per key unpacks its 4-bit row in registers and stores it to tensor memory, from where
 //            the first product takes its A operand - the unpacked keys never touch shared memory;
-//   V        warps 20..23 unpack V rows into a swizzled shared-memory tile (A operand of the second product, M-major);
-//   softmax  warps 0..15 read S^T in the 16x256b fragment form: a thread holds 4 keys x 4 (or 8) query rows, so a key's
+//   V        four warps unpack V rows into a swizzled shared-memory tile (A operand of the second product, M-major);
+//   softmax  warps read S^T in the 16x256b fragment form: a thread holds 4 keys x 4 (or 8) query rows, so a key's
 //            scales and minima are a few registers and a row's running sums one each; weights times V's scale go to
 //            shared memory by stmatrix as the B operand of the second product;
-//   warp 24 issues the first product, 25 the second, 26 works out the CTA's items ahead of everybody, 27 asks for the packed
-//            rows: one bulk copy per group of 16 keys and kind, a ring of units ahead.
+//   one warp each issues the first and the second product, works out the CTA's items ahead of everybody, and asks for the
+//            packed rows: one bulk copy per group of 16 keys and kind, a ring of units ahead.
 // O^T stays in tensor memory over all keys of an item.  Nibbles come out of a word in the order 0 4 1 5 2 6 3 7; the
 // queries are stored in that order, and the output's lanes are read back through it.
 //
@@ -32,25 +32,30 @@ using namespace tc;
 using namespace kv4;
 
 constexpr int UNIT = 128;                      // keys of a unit (MMA M of S^T, MMA K of O^T)
-constexpr int SOFT = 512, CONV = 256;          // threads of the softmax and of the unpacking warps
-constexpr int PARTS = SOFT / 128;              // 128 threads (one a key of four) share query rows: blocks part, part + PARTS, ... of eight
-constexpr int THREADS = SOFT + CONV + 128;
-// registers a thread after the split by warpgroups: 512 x 80 + 256 x 56 + 128 x 56 = 62464 of the 896 x 72 = 64512 launched with
-constexpr int REGS_LAUNCH = 72, REGS_SOFT = 80, REGS_CONV = 56, REGS_ISSUE = 56;
+#ifndef KV4_SOFT
+#define KV4_SOFT 256
+#endif
+constexpr int SOFT = KV4_SOFT, CONV = 256;     // threads of the softmax and of the unpacking warps
+constexpr int PARTS = SOFT / 128;              // 128 threads (one a key of four) share query rows, as pairs of blocks of eight: pair part, part + PARTS, ...
+constexpr int THREADS = SOFT + CONV + 128, SW = SOFT / 32, CW = SW + CONV / 32;      // first unpacking warp, first of the others
+// registers a thread after the split by warpgroups, within those launched with
+constexpr int REGS_LAUNCH = SOFT == 512 ? 72 : 96, REGS_SOFT = SOFT == 512 ? 80 : 152, REGS_CONV = 56, REGS_ISSUE = 56;
 static_assert(SOFT * REGS_SOFT + CONV * REGS_CONV + 128 * REGS_ISSUE <= THREADS * REGS_LAUNCH && THREADS * REGS_LAUNCH <= 65536, "register split");
 constexpr float RAISE = 8.f;
 constexpr int LEAD = 6;                        // an item's fixed cost in units
-// The scales and minima stay until the softmax warps have read them.  Unit j is asked for when unit j - 4 has been
-// unpacked, that is when the first product of unit j - 6 was complete and the softmax warps were done with unit j - 8.
-constexpr int PAR_SLOTS = 8;
+// What the softmax warps need of a unit's keys is ready when its keys are: the K warps are two units ahead of the first
+// product, which is two ahead of the softmax warps.
+constexpr int PAR_SLOTS = 4;
+// The loader is at most four units ahead of the unpacking warps.
+constexpr int GROUP_SLOTS = 8;
 constexpr uint32_t V_SLAB = UNIT * 128;        // [128 keys x 64 channels] half
 
 template <int D, int N>
 struct Shape {
-    static constexpr int STAGES = N == 128 ? 3 : 4;
+    static constexpr int STAGES = N == 128 ? 2 : 4;
     static constexpr int SLABS = D / 64, PSLABS = N / 64;
     static constexpr uint32_t Q_BYTES = SLABS * N * 128, V_BYTES = SLABS * V_SLAB, P_BYTES = PSLABS * UNIT * 128;
-    static constexpr uint32_t ST_BYTES = UNIT * D;                       // K then V codes of a unit, D / 2 bytes a row each
+    static constexpr uint32_t ST_BYTES = UNIT * (D + 8);                 // codes of a unit, D / 2 bytes a row, K then V; then K's and V's (scale, min)
     static constexpr uint32_t V_AT = Q_BYTES, P_AT = V_AT + 2 * V_BYTES, ST_AT = P_AT + 2 * P_BYTES, CTRL_AT = ST_AT + STAGES * ST_BYTES;
     static constexpr uint32_t T_K = 0, T_S = 2 * (D / 2), T_O = T_S + 2 * N;      // tensor-memory columns
     static_assert(T_O + N <= 512, "tensor memory");
@@ -68,9 +73,9 @@ struct Ctrl {
     alignas(16) float qs[128];       // sums of the tile's queries
     alignas(16) float fac[128];      // factors of a rescale, by row
     float x[4][128], y[4][128];      // exchange between the four warps that share rows
-    alignas(16) uint32_t par[PAR_SLOTS][2][UNIT];   // (scale, min) of K and of V by unit and key
+    float4 par[PAR_SLOTS][UNIT];     // by unit and key: K's scale and middle (min + 8 scale) times log2(e) / sqrt(d_head), V's scale and middle
     int unit_there[4];               // 0 in the stage behind the last unit
-    uint32_t page_there[PAR_SLOTS][8];     // whether a group of 16 keys has a page
+    uint32_t groups[GROUP_SLOTS];    // which groups of 16 keys have a page, by unit
     int rowix[128];                  // row of q and out, in d_head elements, of the tile's query rows
     float vmax[PARTS][4];            // largest of V's scales of a unit, by part and warp
     int64_t scratch[32];
@@ -83,6 +88,10 @@ static_assert(smem_bytes<128, 128>(WIDE_SEQS) <= 227 * 1024 && smem_bytes<128, 6
 
 __device__ __forceinline__ void ld_frag(uint32_t taddr, uint32_t (&r)[4]) {      // 16 lanes x 8 columns, as an mma accumulator
     asm volatile("tcgen05.ld.sync.aligned.16x256b.x1.b32 {%0, %1, %2, %3}, [%4];" : "=r"(r[0]), "=r"(r[1]), "=r"(r[2]), "=r"(r[3]) : "r"(taddr) : "memory");
+}
+__device__ __forceinline__ void ld_frag2(uint32_t taddr, uint32_t (&a)[4], uint32_t (&b)[4]) {      // ... x 16 columns
+    asm volatile("tcgen05.ld.sync.aligned.16x256b.x2.b32 {%0, %1, %2, %3, %4, %5, %6, %7}, [%8];"
+                 : "=r"(a[0]), "=r"(a[1]), "=r"(a[2]), "=r"(a[3]), "=r"(b[0]), "=r"(b[1]), "=r"(b[2]), "=r"(b[3]) : "r"(taddr) : "memory");
 }
 __device__ __forceinline__ void st16(uint32_t taddr, const uint32_t (&r)[16]) {
     asm volatile("tcgen05.st.sync.aligned.32x32b.x16.b32 [%0], {%1, %2, %3, %4, %5, %6, %7, %8, %9, %10, %11, %12, %13, %14, %15, %16};"
@@ -113,15 +122,20 @@ __device__ __forceinline__ uint4 lds128(uint32_t addr) {
 __device__ __forceinline__ void sts128(uint32_t addr, const uint32_t* r) {
     asm volatile("st.shared.v4.u32 [%0], {%1, %2, %3, %4};" ::"r"(addr), "r"(r[0]), "r"(r[1]), "r"(r[2]), "r"(r[3]) : "memory");
 }
-// mbar_wait in few instructions: this kernel has many waits, and what it executes has to fit the instruction cache.
+// mbar_wait in few instructions (this kernel has many waits, and what it executes has to fit the instruction cache), asleep
+// until the phase is over or 20 us have passed: threads that poll take issue slots from those that work.
+constexpr uint32_t WAITS = 1u << 16;
+__device__ __forceinline__ bool try_long(uint32_t bar, uint32_t parity) {
+    uint32_t ok;
+    asm volatile("{\n\t.reg .pred p;\n\tmbarrier.try_wait.parity.shared::cta.b64 p, [%1], %2, %3;\n\tselp.u32 %0, 1, 0, p;\n\t}" : "=r"(ok) : "r"(bar), "r"(parity), "r"(20000u) : "memory");
+    return ok != 0;
+}
 __device__ __forceinline__ bool wait(uint32_t bar, uint32_t parity, volatile int* abort_flag, int* status, int code) {
+    if (__builtin_expect(try_long(bar, parity), 1)) return true;
 #pragma unroll 1
-    for (uint32_t spin = 0; spin < SPIN_LIMIT; ++spin) {
-        if (mbar_try(bar, parity)) return true;
-        if (__builtin_expect((spin & 63) == 63, 0)) {
-            if (*abort_flag) return false;
-            __nanosleep(64);
-        }
+    for (uint32_t spin = 0; spin < WAITS; ++spin) {
+        if (*abort_flag) return false;
+        if (try_long(bar, parity)) return true;
     }
     *abort_flag = 1;
     atomicCAS(status, DEV_OK, code);
@@ -129,7 +143,7 @@ __device__ __forceinline__ bool wait(uint32_t bar, uint32_t parity, volatile int
 }
 __device__ __forceinline__ void wait_drain(uint32_t bar, uint32_t parity) {
 #pragma unroll 1
-    for (uint32_t spin = 0; spin < SPIN_LIMIT && !mbar_try(bar, parity); ++spin) __nanosleep(64);
+    for (uint32_t spin = 0; spin < WAITS && !try_long(bar, parity); ++spin) {}
 }
 // One arrival for the whole warp: arrivals on one barrier are taken one by one, five cycles each.
 __device__ __forceinline__ void warp_arrive(uint32_t bar) {
@@ -149,18 +163,18 @@ __device__ __forceinline__ void bulk_load(uint32_t dst, const void* src, uint32_
 }
 
 // eight codes -> four packed pairs, nibbles in the order 0 4 1 5 2 6 3 7
-__device__ __forceinline__ void unpack8(uint32_t w, uint32_t* r) {
+__device__ __forceinline__ void unpack8(uint32_t w, uint32_t* r, const HalfMagic& m) {
     const uint32_t x = w >> 8;
-    r[0] = centred_half<0>(w);
-    r[1] = centred_half<4>(w);
-    r[2] = centred_half<0>(x);
-    r[3] = centred_half<4>(x);
+    r[0] = centred_half<0>(w, m);
+    r[1] = centred_half<4>(w, m);
+    r[2] = centred_half<0>(x, m);
+    r[3] = centred_half<4>(x, m);
 }
 template <int D, int N>
 __global__ void __launch_bounds__(THREADS, 1) k_attn_kv4_tc(const __grid_constant__ Kv4AttnParams p) {
     using SH = Shape<D, N>;
     constexpr int NB = N / 8 / PARTS;                // blocks of eight query rows of a softmax thread
-    constexpr int JB = 2;                            // ... and at a time
+    constexpr int JB = NB < 4 ? NB : 4;              // ... and at a time
     constexpr int PIECES = D / 32;                   // 16-byte pieces of a packed row
     constexpr uint32_t ROW = D / 2;                  // bytes of a packed row
     extern __shared__ uint8_t smem_raw[];
@@ -168,7 +182,7 @@ __global__ void __launch_bounds__(THREADS, 1) k_attn_kv4_tc(const __grid_constan
     uint8_t* base = smem_raw + pad;
     const uint32_t base_a = smem_u32(base);
     Ctrl* sm = reinterpret_cast<Ctrl*>(base + SH::CTRL_AT);
-    const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
+    const int warp = __shfl_sync(0xffffffffu, (int)threadIdx.x >> 5, 0), lane = threadIdx.x & 31;      // (the compiler sees that a warp has one number)
 
     if (threadIdx.x == 0) {
         mbar_init(smem_u32(&sm->q_full), SOFT / 32);
@@ -185,7 +199,7 @@ __global__ void __launch_bounds__(THREADS, 1) k_attn_kv4_tc(const __grid_constan
         sm->abort_flag = 0;
         asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
     }
-    if (warp == 24) {
+    if (warp == CW) {
         asm volatile("tcgen05.alloc.cta_group::1.sync.aligned.shared::cta.b32 [%0], %1;" ::"r"(smem_u32(&sm->tmem_base)), "r"(512u) : "memory");
         asm volatile("tcgen05.relinquish_alloc_permit.cta_group::1.sync.aligned;" ::: "memory");
     }
@@ -209,9 +223,11 @@ __global__ void __launch_bounds__(THREADS, 1) k_attn_kv4_tc(const __grid_constan
     auto rows_of = [&](const Kv4Item& it) { const int r = it.q.n * p.group - it.tile * N; return r < N ? r : N; };
     auto cols_of = [&](int rows) { return (rows + 15) & ~15; };           // MMA N: a multiple of 16
 
-    if (warp >= 16 && warp < 24) {
+    if (warp >= SW && warp < CW) {
         asm volatile("setmaxnreg.dec.sync.aligned.u32 %0;" ::"n"(REGS_CONV));
         const int quad = warp & 3;                                        // this warp's 32 keys of a unit
+        const float sl2 = p.scale * KV4_LOG2E;
+        const HalfMagic magic;
         // units come until the loader says that there are no more (an empty stage)
         auto unit_there = [&](int i) -> bool {
             bool ok = false;
@@ -219,7 +235,7 @@ __global__ void __launch_bounds__(THREADS, 1) k_attn_kv4_tc(const __grid_constan
             ok = __shfl_sync(0xffffffffu, ok, 0);
             return ok;
         };
-        if (warp < 20) {
+        if (warp < SW + 4) {
             // ------------------------------------------------ K: thread = key = tensor-memory lane
 #pragma unroll 1
             for (int i = 0; unit_there(i); ++i) {
@@ -227,12 +243,20 @@ __global__ void __launch_bounds__(THREADS, 1) k_attn_kv4_tc(const __grid_constan
                 const uint32_t st = base_a + SH::ST_AT + (uint32_t)(i % SH::STAGES) * SH::ST_BYTES + (quad * 32 + lane) * ROW;
                 if (i >= 2) wait(smem_u32(&sm->k_empty[b]), ((i >> 1) - 1) & 1, abort_flag, w.status, DEV_TIMEOUT_TMEM);
                 tc_fence_after();
+                {
+                    const uint32_t at = base_a + SH::ST_AT + (uint32_t)(i % SH::STAGES) * SH::ST_BYTES + 2 * UNIT * ROW + 4 * (quad * 32 + lane);
+                    uint32_t kr, vr;
+                    asm volatile("ld.shared.u32 %0, [%1];" : "=r"(kr) : "r"(at) : "memory");
+                    asm volatile("ld.shared.u32 %0, [%1];" : "=r"(vr) : "r"(at + 4 * UNIT) : "memory");
+                    const float2 kf = __half22float2(*reinterpret_cast<const __half2*>(&kr)), vf = __half22float2(*reinterpret_cast<const __half2*>(&vr));
+                    sm->par[i & (PAR_SLOTS - 1)][quad * 32 + lane] = make_float4(kf.x * sl2, fmaf(8.f, kf.x, kf.y) * sl2, vf.x, fmaf(8.f, vf.x, vf.y));
+                }
                 const uint32_t tk = tmem + SH::T_K + b * ROW + ((uint32_t)(quad * 32) << 16);
                 uint4 x = lds128(st);
 #pragma unroll 1
                 for (int c = 0; c < PIECES; ++c) {
                     uint32_t r[16];
-                    unpack8(x.x, r); unpack8(x.y, r + 4); unpack8(x.z, r + 8); unpack8(x.w, r + 12);
+                    unpack8(x.x, r, magic); unpack8(x.y, r + 4, magic); unpack8(x.z, r + 8, magic); unpack8(x.w, r + 12, magic);
                     if (c + 1 < PIECES) x = lds128(st + 16 * (c + 1));
                     st16(tk + c * 16, r);
                 }
@@ -261,7 +285,7 @@ __global__ void __launch_bounds__(THREADS, 1) k_attn_kv4_tc(const __grid_constan
 #pragma unroll
                     for (int k = 0; k < 4; ++k) {
                         uint32_t r[4];
-                        unpack8(wd[k], r);
+                        unpack8(wd[k], r, magic);
                         sts128(vt + ((((c & 1) * 4 + (k ^ turn)) ^ (key & 7)) << 4), r);
                     }
                 }
@@ -270,9 +294,9 @@ __global__ void __launch_bounds__(THREADS, 1) k_attn_kv4_tc(const __grid_constan
                 warp_arrive(smem_u32(&sm->v_full[b]));
             }
         }
-    } else if (warp >= 24) {
+    } else if (warp >= CW) {
         asm volatile("setmaxnreg.dec.sync.aligned.u32 %0;" ::"n"(REGS_ISSUE));
-        if (warp == 24) {
+        if (warp == CW) {
         // ------------------------------------------------ issuer of S^T = K Q^T
         if (lane == 0) {
             const uint64_t q_desc = smem_desc_sw128(base_a);
@@ -305,7 +329,7 @@ __global__ void __launch_bounds__(THREADS, 1) k_attn_kv4_tc(const __grid_constan
                 wait_drain(smem_u32(&sm->drain), 0);
             }
         }
-        } else if (warp == 25) {
+        } else if (warp == CW + 1) {
         // ------------------------------------------------ issuer of O^T += V^T P^T
         if (lane == 0) {
             // both operands have the MMA's K dimension (keys) as rows of 128 bytes: 64 channels of V, 64 query rows of P
@@ -338,7 +362,7 @@ __global__ void __launch_bounds__(THREADS, 1) k_attn_kv4_tc(const __grid_constan
                 wait_drain(smem_u32(&sm->drain_pv), 0);
             }
         }
-        } else if (warp == 26) {
+        } else if (warp == CW + 2) {
         // ------------------------------------------------ scheduler
         if (lane == 0) {
             int k = 0;
@@ -359,7 +383,7 @@ __global__ void __launch_bounds__(THREADS, 1) k_attn_kv4_tc(const __grid_constan
                 if (it.take == 0) break;
             }
         }
-        } else if (warp == 27) {
+        } else if (warp == CW + 3) {
         // ------------------------------------------------ loader: lane = (kind, group of 16 keys): K codes, V codes, K and V scales
         const int kind = lane >> 3, grp = lane & 7, R = 1 << w.shift;
         const uint32_t bytes = kind < 2 ? 16 * ROW : 64;
@@ -375,7 +399,7 @@ __global__ void __launch_bounds__(THREADS, 1) k_attn_kv4_tc(const __grid_constan
             int next = look(0);
 #pragma unroll 1
             for (int k = 0; k < (take > 0 ? take : 1); ++k, ++i) {
-                const int page = next, key0 = (chunk0 + k) * UNIT + 16 * grp, s_ = i % SH::STAGES, slot = i & (PAR_SLOTS - 1);
+                const int page = next, key0 = (chunk0 + k) * UNIT + 16 * grp, s_ = i % SH::STAGES;
                 next = look(k + 1);
                 const bool there = take > 0 && key0 < keys && (unsigned)page < (unsigned)w.n_pages;
                 if (take > 0 && key0 < keys && !there) atomicCAS(w.status, DEV_OK, DEV_KV4_PAGE);
@@ -384,8 +408,8 @@ __global__ void __launch_bounds__(THREADS, 1) k_attn_kv4_tc(const __grid_constan
                 uint32_t total = there ? bytes : 0u;
 #pragma unroll
                 for (int o = 16; o > 0; o >>= 1) total += __shfl_xor_sync(0xffffffffu, total, o);
-                if (kind == 0) sm->page_there[slot][grp] = there;
-                if (lane == 0) sm->unit_there[s_] = take > 0;
+                const uint32_t groups = __ballot_sync(0xffffffffu, there) & 0xffu;
+                if (lane == 0) { sm->groups[i & (GROUP_SLOTS - 1)] = groups; sm->unit_there[s_] = take > 0; }
                 __syncwarp();
                 if (lane == 0) { if (total) mbar_expect_tx(full, total); else mbar_arrive(full); }
                 __syncwarp();
@@ -393,7 +417,7 @@ __global__ void __launch_bounds__(THREADS, 1) k_attn_kv4_tc(const __grid_constan
                     const uint8_t* blk = p.pool + kv4_block_at(w, page, head);
                     const int r = key0 & (R - 1);
                     const uint32_t dst = kind < 2 ? base_a + SH::ST_AT + (uint32_t)s_ * SH::ST_BYTES + kind * UNIT * ROW + 16 * grp * ROW
-                                                  : smem_u32(&sm->par[slot][kind - 2][16 * grp]);
+                                                  : base_a + SH::ST_AT + (uint32_t)s_ * SH::ST_BYTES + 2 * UNIT * ROW + (kind - 2) * 4 * UNIT + 64 * grp;
                     bulk_load(dst, blk + (kind < 2 ? kv4_code_at(R, D, kind, r) : kv4_param_at(R, D, 2, kind - 2, r)), bytes, full);
                 }
             }
@@ -408,9 +432,9 @@ __global__ void __launch_bounds__(THREADS, 1) k_attn_kv4_tc(const __grid_constan
     } else {
         asm volatile("setmaxnreg.inc.sync.aligned.u32 %0;" ::"n"(REGS_SOFT));
         // ------------------------------------------------ softmax warps
-        // part: which blocks of eight query rows (part, part + PARTS, ...); quad: which 32 keys (tensor-memory lanes)
+        // part: which pairs of blocks of eight query rows (part, part + PARTS, ...); quad: which 32 keys (tensor-memory lanes)
         const int part = warp >> 2, quad = warp & 3, g = lane >> 2, t = lane & 3, tid = threadIdx.x;
-        const float sl2 = p.scale * KV4_LOG2E;
+        auto col8 = [&](int j) { return 16 * (PARTS * (j >> 1) + part) + 8 * (j & 1); };      // first query row of this thread's block j
         int i = 0;                                                        // unit of this CTA
 #pragma unroll 1
         for (int items = 0;; ++items) {
@@ -461,25 +485,18 @@ __global__ void __launch_bounds__(THREADS, 1) k_attn_kv4_tc(const __grid_constan
                 const int b = i & 1, key0 = (it.chunk0 + k) * UNIT + quad * 32 + g;
                 wait(smem_u32(&sm->s_full[b]), (i >> 1) & 1, abort_flag, w.status, DEV_TIMEOUT_EPI);
                 tc_fence_after();
-                // (the scales were in place before the unit's keys were: the same threads wrote them)
-                uint32_t there = 0;                                       // which of this thread's keys have a page
                 float ks[4], km[4], vs[4], vm[4];
 #pragma unroll
                 for (int x = 0; x < 4; ++x) {
-                    const int slot = i & (PAR_SLOTS - 1), key = quad * 32 + g + 8 * x;
-                    const float2 a = __half22float2(*reinterpret_cast<const __half2*>(&sm->par[slot][0][key])), c = __half22float2(*reinterpret_cast<const __half2*>(&sm->par[slot][1][key]));
-                    ks[x] = a.x * sl2;
-                    km[x] = fmaf(8.f, a.x, a.y) * sl2;
-                    vs[x] = c.x;
-                    vm[x] = fmaf(8.f, c.x, c.y);
-                    if (sm->page_there[slot][key >> 4]) there |= 1u << x;
+                    const float4 f = sm->par[i & (PAR_SLOTS - 1)][quad * 32 + g + 8 * x];
+                    ks[x] = f.x; km[x] = f.y; vs[x] = f.z; vm[x] = f.w;
                 }
-                // (the whole warp takes the same branches on `all`: every key of the unit is visible to every row)
-                const bool all = (it.chunk0 + k + 1) * UNIT <= it.q.len && __all_sync(0xffffffffu, there == 15u);
+                const uint32_t groups = sm->groups[i & (GROUP_SLOTS - 1)];
+                const bool all = (it.chunk0 + k + 1) * UNIT <= it.q.len && groups == 0xffu;      // every key of the unit is visible to every row
 #pragma unroll
-                for (int j0 = 0; j0 < NB; j0 += JB) {                     // 16 of this thread's scores at a time
-                    if (8 * (PARTS * j0 + part) >= cols) break;           // (whole parts have nothing when the tile has few rows)
-                    const uint32_t ts = tmem + SH::T_S + b * N + 8 * (PARTS * j0 + part) + ((uint32_t)(quad * 32) << 16);
+                for (int j0 = 0; j0 < NB; j0 += JB) {                     // up to 32 of this thread's scores at a time
+                    if (col8(j0) >= cols) break;           // (whole parts have nothing when the tile has few rows)
+                    const uint32_t ts = tmem + SH::T_S + b * N + ((uint32_t)(quad * 32) << 16);
                     uint32_t vis = 0xffffffffu;                           // bit 8 j + 4 e + x: row e of block j sees key x
                     if (__builtin_expect(!all, 0)) {
                         vis = 0u;
@@ -487,10 +504,10 @@ __global__ void __launch_bounds__(THREADS, 1) k_attn_kv4_tc(const __grid_constan
                         for (int j = 0; j < JB; ++j)
 #pragma unroll
                             for (int e = 0; e < 2; ++e) {
-                                const int node = (it.tile * N + 8 * (PARTS * (j0 + j) + part) + 2 * t + e) / p.group;
+                                const int node = (it.tile * N + col8(j0 + j) + 2 * t + e) / p.group;
                                 const uint32_t w32 = sees(p, it.q, node, key0 - it.q.len);
 #pragma unroll
-                                for (int x = 0; x < 4; ++x) vis |= ((w32 >> (8 * x)) & (there >> x) & 1u) << (8 * j + 4 * e + x);
+                                for (int x = 0; x < 4; ++x) vis |= ((w32 >> (8 * x)) & (groups >> (2 * quad + (x >> 1))) & 1u) << (8 * j + 4 * e + x);
                             }
                     }
                     // Scores of key x and row e of block j (registers 2 (x & 1) + e of fragment x >> 1), in powers of two, against
@@ -501,14 +518,14 @@ __global__ void __launch_bounds__(THREADS, 1) k_attn_kv4_tc(const __grid_constan
 #pragma unroll 1
                     for (;;) {
 #pragma unroll
-                        for (int j = 0; j < JB; ++j)
+                        for (int j = 0; j < JB; j += 2)
 #pragma unroll
-                            for (int h = 0; h < 2; ++h) ld_frag(ts + 8 * PARTS * j + ((uint32_t)(16 * h) << 16), s[j][h]);
+                            for (int h = 0; h < 2; ++h) ld_frag2(ts + col8(j0 + j) + ((uint32_t)(16 * h) << 16), s[j][h], s[j + 1][h]);
                         ld_wait();
                         float top = -INFINITY;
 #pragma unroll
                         for (int j = 0; j < JB; ++j) {
-                            const int c8 = 8 * (PARTS * (j0 + j) + part);
+                            const int c8 = col8(j0 + j);
                             const float2 qq = *reinterpret_cast<const float2*>(&sm->qs[c8 + 2 * t]);
                             float tj = -INFINITY;
 #pragma unroll
@@ -532,7 +549,7 @@ __global__ void __launch_bounds__(THREADS, 1) k_attn_kv4_tc(const __grid_constan
                                     for (int x = 0; x < 4; ++x) {
                                         uint32_t& r = s[j][x >> 1][2 * (x & 1) + e];
                                         if (!((vis >> (8 * j + 4 * e + x)) & 1u)) r = __float_as_uint(-INFINITY);
-                                        if (8 * (PARTS * (j0 + j) + part) < cols) top = fmaxf(top, __uint_as_float(r));
+                                        if (col8(j0 + j) < cols) top = fmaxf(top, __uint_as_float(r));
                                     }
                         }
                         bool over = top > RAISE;
@@ -542,11 +559,11 @@ __global__ void __launch_bounds__(THREADS, 1) k_attn_kv4_tc(const __grid_constan
                         // plain scores of the unit, their maxima by row, and the largest of V's scales
 #pragma unroll 1
                         for (int j = 0; j < JB; ++j) {
-                            const int c8 = 8 * (PARTS * (j0 + j) + part);
+                            const int c8 = col8(j0 + j);
                             const float2 qq = *reinterpret_cast<const float2*>(&sm->qs[c8 + 2 * t]);
                             uint32_t o[2][4];
-                            ld_frag(ts + 8 * PARTS * j, o[0]);
-                            ld_frag(ts + 8 * PARTS * j + (16u << 16), o[1]);
+                            ld_frag(ts + c8, o[0]);
+                            ld_frag(ts + c8 + (16u << 16), o[1]);
                             ld_wait();
 #pragma unroll
                             for (int e = 0; e < 2; ++e) {
@@ -575,7 +592,7 @@ __global__ void __launch_bounds__(THREADS, 1) k_attn_kv4_tc(const __grid_constan
 #pragma unroll
                         for (int j = 0; j < NB; ++j) {
                             float f[2] = {1.f, 1.f};
-                            const int rl = 8 * (PARTS * j + part) + 2 * t;
+                            const int rl = col8(j) + 2 * t;
                             if (j >= j0 && j < j0 + JB) {
 #pragma unroll
                                 for (int e = 0; e < 2; ++e) {
@@ -597,7 +614,8 @@ __global__ void __launch_bounds__(THREADS, 1) k_attn_kv4_tc(const __grid_constan
                             wait(smem_u32(&sm->p_empty[(i - 1) & 1]), ((i - 1) >> 1) & 1, abort_flag, w.status, DEV_TIMEOUT_EPI);
                             tc_fence_after();
 #pragma unroll 1
-                            for (int c0 = 8 * part; c0 < cols; c0 += 8 * PARTS) {      // this part's blocks of eight columns, both groups of 16 lanes
+                            for (int j = 0; j < NB && col8(j) < cols; ++j) {      // this part's blocks of eight columns, both groups of 16 lanes
+                                const int c0 = col8(j);
                                 const float2 f = *reinterpret_cast<const float2*>(&sm->fac[c0 + 2 * t]);
                                 const uint32_t to = tmem + SH::T_O + c0 + ((uint32_t)(quad * 32) << 16);
                                 uint32_t o[2][4];
@@ -622,30 +640,34 @@ __global__ void __launch_bounds__(THREADS, 1) k_attn_kv4_tc(const __grid_constan
                     for (int x = 0; x < 4; ++x) vsc[x] = vs[x] * vmul;
 #pragma unroll
                     for (int j = 0; j < JB; ++j) {
-                        const int blk = PARTS * (j0 + j) + part;
+                        const int blk = col8(j0 + j) >> 3;
                         if (8 * blk >= cols) break;
-                        float pv[4][2], pm[4][2];
+                        float pe[4][2], pv[4][2];
 #pragma unroll
                         for (int x = 0; x < 4; ++x)
 #pragma unroll
                             for (int e = 0; e < 2; ++e) {
-                                const float pe = ex2(__uint_as_float(s[j][x >> 1][2 * (x & 1) + e]));
-                                l[j0 + j][e] += pe;
-                                pv[x][e] = pe * vsc[x];
-                                pm[x][e] = pe * vm[x];
+                                pe[x][e] = ex2(__uint_as_float(s[j][x >> 1][2 * (x & 1) + e]));
+                                l[j0 + j][e] += pe[x][e];
+                                pv[x][e] = pe[x][e] * vsc[x];
                             }
-                        if (__builtin_expect(!all, 0)) {                                       // by selection: what a key holds stays out of rows that do not see it
+                        if (__builtin_expect(all, 1)) {
 #pragma unroll
                             for (int x = 0; x < 4; ++x)
 #pragma unroll
-                                for (int e = 0; e < 2; ++e)
-                                    if (!((vis >> (8 * j + 4 * e + x)) & 1u)) pv[x][e] = pm[x][e] = 0.f;
+                                for (int e = 0; e < 2; ++e) ms[j0 + j][e] = fmaf(pe[x][e], vm[x], ms[j0 + j][e]);
+                        } else {                                          // by selection: what a key holds stays out of rows that do not see it
+#pragma unroll
+                            for (int x = 0; x < 4; ++x)
+#pragma unroll
+                                for (int e = 0; e < 2; ++e) {
+                                    if (!((vis >> (8 * j + 4 * e + x)) & 1u)) pv[x][e] = 0.f;
+                                    else ms[j0 + j][e] = fmaf(pe[x][e], vm[x], ms[j0 + j][e]);
+                                }
                         }
                         uint32_t h4[4];
 #pragma unroll
                         for (int x = 0; x < 4; ++x) {
-                            ms[j0 + j][0] += pm[x][0];
-                            ms[j0 + j][1] += pm[x][1];
                             const __half2 h2 = __floats2half2_rn(pv[x][0], pv[x][1]);
                             h4[x] = *reinterpret_cast<const uint32_t*>(&h2);
                         }
@@ -666,7 +688,7 @@ __global__ void __launch_bounds__(THREADS, 1) k_attn_kv4_tc(const __grid_constan
                     float a = l[j][e], c = ms[j][e];
 #pragma unroll
                     for (int o = 4; o < 32; o <<= 1) { a += __shfl_xor_sync(0xffffffffu, a, o); c += __shfl_xor_sync(0xffffffffu, c, o); }
-                    const int rl = 8 * (PARTS * j + part) + 2 * t + e;
+                    const int rl = col8(j) + 2 * t + e;
                     if (g == 0) { sm->x[quad][rl] = a; sm->y[quad][rl] = c; if (quad == 0) sm->fac[rl] = ref[j][e]; }
                 }
             }
@@ -680,7 +702,8 @@ __global__ void __launch_bounds__(THREADS, 1) k_attn_kv4_tc(const __grid_constan
             // lane (16 h + g or + 8) of this quad is channel ch_of(lane); columns of this part's blocks
             auto ch_of = [](int m) { return (m & ~7) | ((m & 1) * 4) | ((m & 7) >> 1); };       // 0 4 1 5 2 6 3 7
 #pragma unroll 1
-            for (int blk = part; 8 * blk < rows && quad * 32 < D; blk += PARTS) {
+            for (int j = 0; j < NB && col8(j) < rows && quad * 32 < D; ++j) {
+                const int blk = col8(j) >> 3;
                 uint32_t o[2][4];
                 const uint32_t to = tmem + SH::T_O + 8 * blk + ((uint32_t)(quad * 32) << 16);
                 ld_frag(to, o[0]);
@@ -724,7 +747,7 @@ __global__ void __launch_bounds__(THREADS, 1) k_attn_kv4_tc(const __grid_constan
 
     tc_fence_before();
     __syncthreads();
-    if (warp == 24) {
+    if (warp == CW) {
         tc_fence_after();
         asm volatile("tcgen05.dealloc.cta_group::1.sync.aligned.b32 %0, %1;" ::"r"(tmem), "r"(512u) : "memory");
     }
