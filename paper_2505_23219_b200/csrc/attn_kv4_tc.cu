@@ -8,8 +8,8 @@
 //   softmax  warps read S^T in the 16x256b fragment form: a thread holds 4 keys x 4 (or 8) query rows, so a key's
 //            scales and minima are a few registers and a row's running sums one each; weights times V's scale go to
 //            shared memory by stmatrix as the B operand of the second product;
-//   one warp each issues the first and the second product, works out the CTA's items ahead of everybody, and asks for the
-//            packed rows: one bulk copy per group of 16 keys and kind, a ring of units ahead.
+//   one warp each issues the first and the second product, and works out the CTA's items ahead of
+//            everybody.
 // O^T stays in tensor memory over all keys of an item.  Nibbles come out of a word in the order 0 4 1 5 2 6 3 7; the
 // queries are stored in that order, and the output's lanes are read back through it.
 //
@@ -20,6 +20,7 @@
 // Work is dealt as in attn_kv4.cu, one CTA an SM.
 #include <cstddef>
 #include <cstdio>
+#include <type_traits>
 
 #include "attn_kv4_dev.cuh"
 #include "tc_common.cuh"
@@ -66,7 +67,7 @@ constexpr int ITEMS = 4;                       // items that the scheduler is ah
 struct Ctrl {
     uint64_t item_full[ITEMS], item_empty[ITEMS];
     Kv4Item item[ITEMS], cur;        // cur: the softmax warps' item
-    uint64_t c_full[4], c_empty[4];  // packed codes of a unit
+    uint64_t c_full[CONV / 32][4];   // packed rows of a unit, by unpacking warp and stage
     uint64_t q_full, k_full[2], k_empty[2], v_full[2], v_empty[2], s_full[2], s_empty[2], p_full[2], p_empty[2], drain, drain_pv;
     uint32_t tmem_base;
     int abort_flag, arrived;
@@ -74,8 +75,7 @@ struct Ctrl {
     alignas(16) float fac[128];      // factors of a rescale, by row
     float x[4][128], y[4][128];      // exchange between the four warps that share rows
     float4 par[PAR_SLOTS][UNIT];     // by unit and key: K's scale and middle (min + 8 scale) times log2(e) / sqrt(d_head), V's scale and middle
-    int unit_there[4];               // 0 in the stage behind the last unit
-    uint32_t groups[GROUP_SLOTS];    // which groups of 16 keys have a page, by unit
+    alignas(4) uint8_t groups[GROUP_SLOTS][4];      // which of a quarter's two groups of 16 keys have a page, by unit
     int rowix[128];                  // row of q and out, in d_head elements, of the tile's query rows
     float vmax[PARTS][4];            // largest of V's scales of a unit, by part and warp
     int64_t scratch[32];
@@ -122,20 +122,17 @@ __device__ __forceinline__ uint4 lds128(uint32_t addr) {
 __device__ __forceinline__ void sts128(uint32_t addr, const uint32_t* r) {
     asm volatile("st.shared.v4.u32 [%0], {%1, %2, %3, %4};" ::"r"(addr), "r"(r[0]), "r"(r[1]), "r"(r[2]), "r"(r[3]) : "memory");
 }
-// mbar_wait in few instructions (this kernel has many waits, and what it executes has to fit the instruction cache), asleep
-// until the phase is over or 20 us have passed: threads that poll take issue slots from those that work.
-constexpr uint32_t WAITS = 1u << 16;
-__device__ __forceinline__ bool try_long(uint32_t bar, uint32_t parity) {
-    uint32_t ok;
-    asm volatile("{\n\t.reg .pred p;\n\tmbarrier.try_wait.parity.shared::cta.b64 p, [%1], %2, %3;\n\tselp.u32 %0, 1, 0, p;\n\t}" : "=r"(ok) : "r"(bar), "r"(parity), "r"(20000u) : "memory");
-    return ok != 0;
-}
+// mbar_wait in few instructions (this kernel has many waits, and what it executes has to fit the instruction cache).  NAP:
+// nanoseconds between two looks, for warps that are ahead of what they wait for: polling takes issue slots from the
+// warps that work (it was 40 % of all instructions).
+constexpr uint32_t WAITS = 1u << 22;
+template <int NAP = 0>
 __device__ __forceinline__ bool wait(uint32_t bar, uint32_t parity, volatile int* abort_flag, int* status, int code) {
-    if (__builtin_expect(try_long(bar, parity), 1)) return true;
 #pragma unroll 1
     for (uint32_t spin = 0; spin < WAITS; ++spin) {
-        if (*abort_flag) return false;
-        if (try_long(bar, parity)) return true;
+        if (__builtin_expect(mbar_try(bar, parity), 1)) return true;
+        if (NAP > 0) __nanosleep(NAP);
+        if (__builtin_expect((spin & 31) == 31, 0)) { if (*abort_flag) return false; }
     }
     *abort_flag = 1;
     atomicCAS(status, DEV_OK, code);
@@ -143,7 +140,7 @@ __device__ __forceinline__ bool wait(uint32_t bar, uint32_t parity, volatile int
 }
 __device__ __forceinline__ void wait_drain(uint32_t bar, uint32_t parity) {
 #pragma unroll 1
-    for (uint32_t spin = 0; spin < WAITS && !try_long(bar, parity); ++spin) {}
+    for (uint32_t spin = 0; spin < WAITS && !mbar_try(bar, parity); ++spin) __nanosleep(64);
 }
 // One arrival for the whole warp: arrivals on one barrier are taken one by one, five cycles each.
 __device__ __forceinline__ void warp_arrive(uint32_t bar) {
@@ -194,8 +191,8 @@ __global__ void __launch_bounds__(THREADS, 1) k_attn_kv4_tc(const __grid_constan
         }
         mbar_init(smem_u32(&sm->drain), 1);
         mbar_init(smem_u32(&sm->drain_pv), 1);
-        for (int b = 0; b < 4; ++b) { mbar_init(smem_u32(&sm->c_full[b]), 1); mbar_init(smem_u32(&sm->c_empty[b]), CONV / 32); }
-        for (int b = 0; b < ITEMS; ++b) { mbar_init(smem_u32(&sm->item_full[b]), 1); mbar_init(smem_u32(&sm->item_empty[b]), 4); }      // softmax, both issuers, loader
+        for (int b = 0; b < 4 * (CONV / 32); ++b) mbar_init(smem_u32(&sm->c_full[b >> 2][b & 3]), 1);
+        for (int b = 0; b < ITEMS; ++b) { mbar_init(smem_u32(&sm->item_full[b]), 1); mbar_init(smem_u32(&sm->item_empty[b]), CONV / 32 + 3); }      // unpacking warps, softmax, both issuers
         sm->abort_flag = 0;
         asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
     }
@@ -215,7 +212,7 @@ __global__ void __launch_bounds__(THREADS, 1) k_attn_kv4_tc(const __grid_constan
     // The k-th item of this CTA (take = 0: there are no more, or a wait has run out).  One thread looks; who takes it together
     // with others gets it from that thread, so that all of them go on or stop alike.
     auto item_get = [&](int k) -> Kv4Item {
-        if (!wait(smem_u32(&sm->item_full[k % ITEMS]), (k / ITEMS) & 1, abort_flag, w.status, DEV_TIMEOUT_EPI)) { Kv4Item none{}; return none; }
+        if (!wait<100>(smem_u32(&sm->item_full[k % ITEMS]), (k / ITEMS) & 1, abort_flag, w.status, DEV_TIMEOUT_EPI)) { Kv4Item none{}; return none; }
         const Kv4Item it = sm->item[k % ITEMS];
         mbar_arrive(smem_u32(&sm->item_empty[k % ITEMS]));
         return it;
@@ -228,23 +225,82 @@ __global__ void __launch_bounds__(THREADS, 1) k_attn_kv4_tc(const __grid_constan
         const int quad = warp & 3;                                        // this warp's 32 keys of a unit
         const float sl2 = p.scale * KV4_LOG2E;
         const HalfMagic magic;
-        // units come until the loader says that there are no more (an empty stage)
-        auto unit_there = [&](int i) -> bool {
-            bool ok = false;
-            if (lane == 0) ok = wait(smem_u32(&sm->c_full[i % SH::STAGES]), (i / SH::STAGES) & 1, abort_flag, w.status, DEV_TIMEOUT_TMA) && sm->unit_there[i % SH::STAGES];
-            ok = __shfl_sync(0xffffffffu, ok, 0);
-            return ok;
+        // Every warp asks for its own rows by bulk copies into a ring of its own, STAGES - 1 units ahead and over the borders of
+        // items: K's or V's codes (which), and the K warps the scales and minima of both.
+        const int which = warp < SW + 4 ? 0 : 1, own = warp - SW, R = 1 << w.shift;
+        const uint32_t ring = base_a + SH::ST_AT + which * UNIT * ROW + quad * 32 * ROW, pring = base_a + SH::ST_AT + 2 * UNIT * ROW + quad * 32 * 4;
+        int items = 0, lseq = 0, lhead = 0, lch = 0, lend = 0, lkeys = 0, n = 0;      // load cursor; units asked for so far
+        bool more = true;
+        auto page_of = [&](int key) { return key < lkeys ? __ldg(w.table + (size_t)lseq * w.max_pages + (key >> w.shift)) : -1; };
+        int page[2] = {-1, -1};                                           // of the next unit's two groups of 16 keys, looked up one unit ahead
+        auto ask = [&]() {
+            if (lch >= lend && more) {
+                if (lane == 0) {
+                    const Kv4Item it = item_get(items);
+                    lseq = it.seq; lhead = it.head; lch = it.chunk0; lend = it.chunk0 + it.take; lkeys = it.keys;
+                }
+                ++items;
+                lseq = __shfl_sync(0xffffffffu, lseq, 0);
+                lhead = __shfl_sync(0xffffffffu, lhead, 0);
+                lch = __shfl_sync(0xffffffffu, lch, 0);
+                lend = __shfl_sync(0xffffffffu, lend, 0);
+                lkeys = __shfl_sync(0xffffffffu, lkeys, 0);
+                more = lend > lch;
+#pragma unroll
+                for (int h = 0; h < 2; ++h) page[h] = page_of(lch * UNIT + quad * 32 + 16 * h);
+            }
+            if (lch >= lend) return;
+            if (lane == 0) {
+                const int key0 = lch * UNIT + quad * 32, s_ = n % SH::STAGES;
+                const uint32_t full = smem_u32(&sm->c_full[own][s_]);
+                uint32_t there = 0;
+#pragma unroll
+                for (int h = 0; h < 2; ++h) {
+                    if ((unsigned)page[h] < (unsigned)w.n_pages) there |= 1u << h;
+                    else if (key0 + 16 * h < lkeys) atomicCAS(w.status, DEV_OK, DEV_KV4_PAGE);
+                }
+                if (which == 0) sm->groups[n & (GROUP_SLOTS - 1)][quad] = (uint8_t)there;
+                if (there) mbar_expect_tx(full, (there == 3u ? 2u : 1u) * 16 * (ROW + (which ? 0 : 8)));
+                else mbar_arrive(full);
+                const bool one = there == 3u && R >= 32;                  // 32 rows of one page: one copy of each kind
+#pragma unroll 1
+                for (int h = 0; h < 2; ++h) {
+                    if (!((there >> h) & 1u) || (one && h)) continue;
+                    const int r = (key0 + 16 * h) & (R - 1), rows = one ? 32 : 16;
+                    const uint8_t* blk = p.pool + kv4_block_at(w, page[h], lhead);
+                    bulk_load(ring + s_ * SH::ST_BYTES + 16 * h * ROW, blk + kv4_code_at(R, D, which, r), rows * ROW, full);
+                    if (which == 0) {
+                        bulk_load(pring + s_ * SH::ST_BYTES + 64 * h, blk + kv4_param_at(R, D, 2, 0, r), rows * 4, full);
+                        bulk_load(pring + s_ * SH::ST_BYTES + 4 * UNIT + 64 * h, blk + kv4_param_at(R, D, 2, 1, r), rows * 4, full);
+                    }
+                }
+            }
+            ++lch;
+            ++n;
+            if (lch < lend) {
+#pragma unroll
+                for (int h = 0; h < 2; ++h) page[h] = page_of(lch * UNIT + quad * 32 + 16 * h);
+            }
         };
+        auto landed = [&](int i) {
+            if (lane == 0) wait<100>(smem_u32(&sm->c_full[own][i % SH::STAGES]), (i / SH::STAGES) & 1, abort_flag, w.status, DEV_TIMEOUT_TMA);
+            __syncwarp();
+        };
+#pragma unroll 1
+        for (int i = 0; i < SH::STAGES - 1; ++i) ask();
         if (warp < SW + 4) {
             // ------------------------------------------------ K: thread = key = tensor-memory lane
 #pragma unroll 1
-            for (int i = 0; unit_there(i); ++i) {
+            for (int i = 0; i < n; ++i) {                                 // (n runs ahead until the last unit has been asked for)
                 const int b = i & 1;
+                __syncwarp();                                             // everybody has read the stage that is filled next
+                ask();
+                landed(i);
                 const uint32_t st = base_a + SH::ST_AT + (uint32_t)(i % SH::STAGES) * SH::ST_BYTES + (quad * 32 + lane) * ROW;
-                if (i >= 2) wait(smem_u32(&sm->k_empty[b]), ((i >> 1) - 1) & 1, abort_flag, w.status, DEV_TIMEOUT_TMEM);
+                if (i >= 2) wait<100>(smem_u32(&sm->k_empty[b]), ((i >> 1) - 1) & 1, abort_flag, w.status, DEV_TIMEOUT_TMEM);
                 tc_fence_after();
                 {
-                    const uint32_t at = base_a + SH::ST_AT + (uint32_t)(i % SH::STAGES) * SH::ST_BYTES + 2 * UNIT * ROW + 4 * (quad * 32 + lane);
+                    const uint32_t at = pring + (uint32_t)(i % SH::STAGES) * SH::ST_BYTES + 4 * lane;
                     uint32_t kr, vr;
                     asm volatile("ld.shared.u32 %0, [%1];" : "=r"(kr) : "r"(at) : "memory");
                     asm volatile("ld.shared.u32 %0, [%1];" : "=r"(vr) : "r"(at + 4 * UNIT) : "memory");
@@ -260,7 +316,6 @@ __global__ void __launch_bounds__(THREADS, 1) k_attn_kv4_tc(const __grid_constan
                     if (c + 1 < PIECES) x = lds128(st + 16 * (c + 1));
                     st16(tk + c * 16, r);
                 }
-                warp_arrive(smem_u32(&sm->c_empty[i % SH::STAGES]));
                 st_wait();
                 tc_fence_before();
                 warp_arrive(smem_u32(&sm->k_full[b]));
@@ -271,10 +326,13 @@ __global__ void __launch_bounds__(THREADS, 1) k_attn_kv4_tc(const __grid_constan
             const int row0 = quad * 32 + lane / PIECES, c = lane % PIECES, turn = D == 128 ? (c >> 1) << 1 : 0;
             constexpr int PER = 32 / PIECES;
 #pragma unroll 1
-            for (int i = 0; unit_there(i); ++i) {
+            for (int i = 0; i < n; ++i) {                                 // (n runs ahead until the last unit has been asked for)
                 const int b = i & 1;
+                __syncwarp();                                             // everybody has read the stage that is filled next
+                ask();
+                landed(i);
                 const uint32_t st = base_a + SH::ST_AT + (uint32_t)(i % SH::STAGES) * SH::ST_BYTES + UNIT * ROW + row0 * ROW + 16 * c;
-                if (i >= 2) wait(smem_u32(&sm->v_empty[b]), ((i >> 1) - 1) & 1, abort_flag, w.status, DEV_TIMEOUT_TMEM);
+                if (i >= 2) wait<100>(smem_u32(&sm->v_empty[b]), ((i >> 1) - 1) & 1, abort_flag, w.status, DEV_TIMEOUT_TMEM);
                 uint4 x = lds128(st);
 #pragma unroll 1
                 for (int j = 0; j < PIECES; ++j) {
@@ -289,11 +347,14 @@ __global__ void __launch_bounds__(THREADS, 1) k_attn_kv4_tc(const __grid_constan
                         sts128(vt + ((((c & 1) * 4 + (k ^ turn)) ^ (key & 7)) << 4), r);
                     }
                 }
-                warp_arrive(smem_u32(&sm->c_empty[i % SH::STAGES]));
                 asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
                 warp_arrive(smem_u32(&sm->v_full[b]));
             }
         }
+        // no copy is in flight when the block ends, whatever the others have given up
+        if (lane == 0)
+#pragma unroll 1
+            for (int k = n > SH::STAGES ? n - SH::STAGES : 0; k < n; ++k) wait_drain(smem_u32(&sm->c_full[own][k % SH::STAGES]), (k / SH::STAGES) & 1);
     } else if (warp >= CW) {
         asm volatile("setmaxnreg.dec.sync.aligned.u32 %0;" ::"n"(REGS_ISSUE));
         if (warp == CW) {
@@ -376,58 +437,13 @@ __global__ void __launch_bounds__(THREADS, 1) k_attn_kv4_tc(const __grid_constan
                     u = it.next;
                 }
                 if (it.take > 0) it.keys = kv4_tile_keys(til, it.q, it.tile);
-                if (k >= ITEMS) ok = wait(smem_u32(&sm->item_empty[k % ITEMS]), ((k / ITEMS) - 1) & 1, abort_flag, w.status, DEV_TIMEOUT_EPI);
+                if (k >= ITEMS) ok = wait<500>(smem_u32(&sm->item_empty[k % ITEMS]), ((k / ITEMS) - 1) & 1, abort_flag, w.status, DEV_TIMEOUT_EPI);
                 sm->item[k % ITEMS] = it;
                 mbar_arrive(smem_u32(&sm->item_full[k % ITEMS]));
                 ++k;
                 if (it.take == 0) break;
             }
         }
-        } else if (warp == CW + 3) {
-        // ------------------------------------------------ loader: lane = (kind, group of 16 keys): K codes, V codes, K and V scales
-        const int kind = lane >> 3, grp = lane & 7, R = 1 << w.shift;
-        const uint32_t bytes = kind < 2 ? 16 * ROW : 64;
-        int i = 0;
-#pragma unroll 1
-        for (int items = 0;; ++items) {
-            Kv4Item it{};
-            if (lane == 0) it = item_get(items);
-            const int take = __shfl_sync(0xffffffffu, it.take, 0), chunk0 = __shfl_sync(0xffffffffu, it.chunk0, 0), keys = __shfl_sync(0xffffffffu, it.keys, 0);
-            const int seq = __shfl_sync(0xffffffffu, it.seq, 0), head = __shfl_sync(0xffffffffu, it.head, 0);
-            // (a page's id is looked up one unit ahead)
-            auto look = [&](int k) { const int key0 = (chunk0 + k) * UNIT + 16 * grp; return k < take && key0 < keys ? __ldg(w.table + (size_t)seq * w.max_pages + (key0 >> w.shift)) : -1; };
-            int next = look(0);
-#pragma unroll 1
-            for (int k = 0; k < (take > 0 ? take : 1); ++k, ++i) {
-                const int page = next, key0 = (chunk0 + k) * UNIT + 16 * grp, s_ = i % SH::STAGES;
-                next = look(k + 1);
-                const bool there = take > 0 && key0 < keys && (unsigned)page < (unsigned)w.n_pages;
-                if (take > 0 && key0 < keys && !there) atomicCAS(w.status, DEV_OK, DEV_KV4_PAGE);
-                if (i >= SH::STAGES) wait(smem_u32(&sm->c_empty[s_]), ((i / SH::STAGES) - 1) & 1, abort_flag, w.status, DEV_TIMEOUT_TMA);
-                const uint32_t full = smem_u32(&sm->c_full[s_]);
-                uint32_t total = there ? bytes : 0u;
-#pragma unroll
-                for (int o = 16; o > 0; o >>= 1) total += __shfl_xor_sync(0xffffffffu, total, o);
-                const uint32_t groups = __ballot_sync(0xffffffffu, there) & 0xffu;
-                if (lane == 0) { sm->groups[i & (GROUP_SLOTS - 1)] = groups; sm->unit_there[s_] = take > 0; }
-                __syncwarp();
-                if (lane == 0) { if (total) mbar_expect_tx(full, total); else mbar_arrive(full); }
-                __syncwarp();
-                if (there) {
-                    const uint8_t* blk = p.pool + kv4_block_at(w, page, head);
-                    const int r = key0 & (R - 1);
-                    const uint32_t dst = kind < 2 ? base_a + SH::ST_AT + (uint32_t)s_ * SH::ST_BYTES + kind * UNIT * ROW + 16 * grp * ROW
-                                                  : base_a + SH::ST_AT + (uint32_t)s_ * SH::ST_BYTES + 2 * UNIT * ROW + (kind - 2) * 4 * UNIT + 64 * grp;
-                    bulk_load(dst, blk + (kind < 2 ? kv4_code_at(R, D, kind, r) : kv4_param_at(R, D, 2, kind - 2, r)), bytes, full);
-                }
-            }
-            if (take == 0) break;
-        }
-        // no copy is in flight when the block ends, whatever the others have given up
-        if (lane == 0)
-#pragma unroll 1
-            for (int k = i > SH::STAGES ? i - SH::STAGES : 0; k < i; ++k)
-                wait_drain(smem_u32(&sm->c_full[k % SH::STAGES]), (k / SH::STAGES) & 1);
         }
     } else {
         asm volatile("setmaxnreg.inc.sync.aligned.u32 %0;" ::"n"(REGS_SOFT));
@@ -491,8 +507,8 @@ __global__ void __launch_bounds__(THREADS, 1) k_attn_kv4_tc(const __grid_constan
                     const float4 f = sm->par[i & (PAR_SLOTS - 1)][quad * 32 + g + 8 * x];
                     ks[x] = f.x; km[x] = f.y; vs[x] = f.z; vm[x] = f.w;
                 }
-                const uint32_t groups = sm->groups[i & (GROUP_SLOTS - 1)];
-                const bool all = (it.chunk0 + k + 1) * UNIT <= it.q.len && groups == 0xffu;      // every key of the unit is visible to every row
+                const uint32_t groups = *reinterpret_cast<const uint32_t*>(sm->groups[i & (GROUP_SLOTS - 1)]);
+                const bool all = (it.chunk0 + k + 1) * UNIT <= it.q.len && groups == 0x03030303u;      // every key of the unit is visible to every row
 #pragma unroll
                 for (int j0 = 0; j0 < NB; j0 += JB) {                     // up to 32 of this thread's scores at a time
                     if (col8(j0) >= cols) break;           // (whole parts have nothing when the tile has few rows)
@@ -507,7 +523,7 @@ __global__ void __launch_bounds__(THREADS, 1) k_attn_kv4_tc(const __grid_constan
                                 const int node = (it.tile * N + col8(j0 + j) + 2 * t + e) / p.group;
                                 const uint32_t w32 = sees(p, it.q, node, key0 - it.q.len);
 #pragma unroll
-                                for (int x = 0; x < 4; ++x) vis |= ((w32 >> (8 * x)) & (groups >> (2 * quad + (x >> 1))) & 1u) << (8 * j + 4 * e + x);
+                                for (int x = 0; x < 4; ++x) vis |= ((w32 >> (8 * x)) & (groups >> (8 * quad + (x >> 1))) & 1u) << (8 * j + 4 * e + x);
                             }
                     }
                     // Scores of key x and row e of block j (registers 2 (x & 1) + e of fragment x >> 1), in powers of two, against
@@ -638,42 +654,34 @@ __global__ void __launch_bounds__(THREADS, 1) k_attn_kv4_tc(const __grid_constan
                     float vsc[4];
 #pragma unroll
                     for (int x = 0; x < 4; ++x) vsc[x] = vs[x] * vmul;
+                    // (one straight run of instructions for the units that matter, where nothing is masked and every block has rows)
+                    auto weights = [&](auto plain) {
+                        constexpr bool PLAIN = decltype(plain)::value;
 #pragma unroll
-                    for (int j = 0; j < JB; ++j) {
-                        const int blk = col8(j0 + j) >> 3;
-                        if (8 * blk >= cols) break;
-                        float pe[4][2], pv[4][2];
+                        for (int j = 0; j < JB; ++j) {
+                            const int blk = col8(j0 + j) >> 3;
+                            if (!PLAIN && 8 * blk >= cols) break;
+                            uint32_t h4[4];
 #pragma unroll
-                        for (int x = 0; x < 4; ++x)
-#pragma unroll
-                            for (int e = 0; e < 2; ++e) {
-                                pe[x][e] = ex2(__uint_as_float(s[j][x >> 1][2 * (x & 1) + e]));
-                                l[j0 + j][e] += pe[x][e];
-                                pv[x][e] = pe[x][e] * vsc[x];
-                            }
-                        if (__builtin_expect(all, 1)) {
-#pragma unroll
-                            for (int x = 0; x < 4; ++x)
-#pragma unroll
-                                for (int e = 0; e < 2; ++e) ms[j0 + j][e] = fmaf(pe[x][e], vm[x], ms[j0 + j][e]);
-                        } else {                                          // by selection: what a key holds stays out of rows that do not see it
-#pragma unroll
-                            for (int x = 0; x < 4; ++x)
+                            for (int x = 0; x < 4; ++x) {
+                                float pv[2];
 #pragma unroll
                                 for (int e = 0; e < 2; ++e) {
-                                    if (!((vis >> (8 * j + 4 * e + x)) & 1u)) pv[x][e] = 0.f;
-                                    else ms[j0 + j][e] = fmaf(pe[x][e], vm[x], ms[j0 + j][e]);
+                                    const float pe = ex2(__uint_as_float(s[j][x >> 1][2 * (x & 1) + e]));
+                                    l[j0 + j][e] += pe;
+                                    pv[e] = pe * vsc[x];
+                                    if (PLAIN || ((vis >> (8 * j + 4 * e + x)) & 1u)) ms[j0 + j][e] = fmaf(pe, vm[x], ms[j0 + j][e]);
+                                    else pv[e] = 0.f;                     // by selection: what a key holds stays out of rows that do not see it
                                 }
+                                const __half2 h2 = __floats2half2_rn(pv[0], pv[1]);
+                                h4[x] = *reinterpret_cast<const uint32_t*>(&h2);
+                            }
+                            // lane's matrix row: key 32 quad + lane, query rows 8 blk .. 8 blk + 7
+                            stmatrix4(base_a + SH::P_AT + b * SH::P_BYTES + (blk >> 3) * (UNIT * 128) + (quad * 32 + lane) * 128 + (((blk & 7) ^ (lane & 7)) << 4), h4[0], h4[1], h4[2], h4[3]);
                         }
-                        uint32_t h4[4];
-#pragma unroll
-                        for (int x = 0; x < 4; ++x) {
-                            const __half2 h2 = __floats2half2_rn(pv[x][0], pv[x][1]);
-                            h4[x] = *reinterpret_cast<const uint32_t*>(&h2);
-                        }
-                        // lane's matrix row: key 32 quad + lane, query rows 8 blk .. 8 blk + 7
-                        stmatrix4(base_a + SH::P_AT + b * SH::P_BYTES + (blk >> 3) * (UNIT * 128) + (quad * 32 + lane) * 128 + (((blk & 7) ^ (lane & 7)) << 4), h4[0], h4[1], h4[2], h4[3]);
-                    }
+                    };
+                    if (__builtin_expect(all && col8(j0 + JB - 1) < cols, 1)) weights(std::true_type{});
+                    else weights(std::false_type{});
                 }
                 tc_fence_before();
                 warp_arrive(smem_u32(&sm->s_empty[b]));
