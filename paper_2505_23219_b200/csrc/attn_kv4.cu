@@ -424,7 +424,7 @@ __global__ void __launch_bounds__(WARPS * 32, Narrow<T, D, NT>::BLOCKS) k_attn_k
                 __threadfence();
             }
             __syncthreads();
-            if (arrived) merge_item<T, D, WARPS>(p, it, RT, rows, c0, c1, warp, xmerge, [] { __syncthreads(); });
+            if (arrived) merge_item<T, D, 1>(p, it, RT, rows, c0, c1, warp, WARPS, xmerge, [] { __syncthreads(); });
         }
         __syncthreads();                                                 // the exchange buffers are written again
     }
@@ -459,7 +459,7 @@ ghd_status launch_attn_kv4(ghd_ctx* c, const Kv4View& w, const ghd_kv4_rows* row
     p.part = c->gemm_part; p.counters = c->counters;
     const int64_t avg = ((int64_t)rows->n_rows * p.group + w.n_seqs - 1) / w.n_seqs;      // query rows of a sequence and head, on average
     if (m.dtype == GHD_F32) return m.d_head == 64 ? launch_narrow<float, 64, 1>(c, p) : launch_narrow<float, 128, 1>(c, p);
-    if (avg > 16) return launch_attn_kv4_tc(c, p, avg > 64 ? 128 : 64);
+    if (avg > 16) return launch_attn_kv4_tc(c, p, 64);
     if (m.d_head == 64) return avg <= 8 ? launch_narrow<__half, 64, 1>(c, p) : launch_narrow<__half, 64, 2>(c, p);
     return avg <= 8 ? launch_narrow<__half, 128, 1>(c, p) : launch_narrow<__half, 128, 2>(c, p);
 }

@@ -127,95 +127,110 @@ static __device__ __noinline__ void find_item(const Kv4View* w, const Kv4Tiling*
     *out = kv4_find_item(*t, sums, w->n_seqs, [&](int s) { return kv4_load_seq(*w, s); }, u, u_end);
 }
 
-// Adds the partial sums that CTAs c0 .. c1 left of one item, in that order, and writes its rows.  A warp takes a row (the
-// lanes hold D / 32 channels each); with fewer rows than warps several warps share a row's contributors and meet in
-// `xch`, floats [warps][D + 2].  Loads run eight contributors ahead: their latency is what the merge would otherwise
-// cost.  `sync` is a barrier of the NW warps that take part.
-template <typename T, int D, int NW, typename Sync>
-__device__ __forceinline__ void merge_item(const Kv4AttnParams& p, const Kv4Item& it, int tile_rows, int rows, int64_t c0, int64_t c1, int warp, float* xch, Sync sync) {
-    constexpr int VL = D / 32;
+// Adds the partial sums that CTAs c0 .. c1 left of one item, in that order, and writes its rows.  A warp takes RB rows at a
+// time (the lanes hold D / 32 channels each) and KB contributors of each: what the merge costs is the latency of its loads,
+// so 16 rows of sums are on the way together.  With few rows several warps share the contributors and meet in `xch`,
+// floats [warps][D + 2].  `sync` is a barrier of the NW warps that take part.
+template <typename T, int D, int RB, typename Sync>
+__device__ __forceinline__ void merge_item(const Kv4AttnParams& p, const Kv4Item& it, int tile_rows, int rows, int64_t c0, int64_t c1, int warp, int nw, float* xch, Sync sync) {
+    constexpr int VL = D / 32, KB = 16 / RB;
     const size_t slot = (size_t)tile_rows * (D + 2);
     const int lane = threadIdx.x & 31, n = (int)(c1 - c0) + 1;
-    int share = 1;                                               // warps a row: a power of two
+    int share = 1;                                               // warps a row: a power of two (only where a warp takes one row at a time)
+    if (RB == 1) {
 #pragma unroll 1
-    while (share * 2 * rows <= NW && share * 16 <= n) share *= 2;
-    const int sub = warp % share;
-    const int k_beg = (int)((int64_t)n * sub / share), k_end = (int)((int64_t)n * (sub + 1) / share);
-    auto slot_of = [&](int k) { return p.part + ((size_t)(c0 + k) * 2 + (k == 0 ? 1 : 0)) * slot; };
+        while (share * 2 * rows <= nw && share * 2 * KB < n) share *= 2;
+    }
+    const int sub = warp & (share - 1), team = warp / share, teams = nw / share;
+    const int k_beg = n * sub / share, k_end = n * (sub + 1) / share;
+    // contributor 0 has begun the item (its second slot), the others have gone on with it (their first)
+    const float* first = p.part + ((size_t)c0 * 2 + 1) * slot;
+    const float* rest = p.part + (size_t)c0 * 2 * slot;
 #pragma unroll 1
-    for (int rl0 = 0; rl0 < rows; rl0 += NW / share) {
-        const int rl = rl0 + warp / share;
-        float m = -INFINITY, lsum = 0.f, a[VL];
+    for (int r0 = 0; r0 < rows; r0 += teams * RB) {
+        float m[RB], lsum[RB], a[RB][VL];
 #pragma unroll
-        for (int e = 0; e < VL; ++e) a[e] = 0.f;
-        if (rl < rows) {
-#pragma unroll 1
-            for (int kb = k_beg; kb < k_end; kb += 8) {
-                float2 ml[8];
-                float v[8][VL];
+        for (int r = 0; r < RB; ++r) {
+            m[r] = -INFINITY;
+            lsum[r] = 0.f;
 #pragma unroll
-                for (int k = 0; k < 8; ++k) {
-                    ml[k] = make_float2(-INFINITY, 0.f);
-                    if (kb + k < k_end) {
-                        const float* sl = slot_of(kb + k);
-                        ml[k] = __ldcg(reinterpret_cast<const float2*>(sl + (size_t)tile_rows * D + 2 * rl));
-                        const float* src = sl + (size_t)rl * D + VL * lane;
-                        if constexpr (VL == 4) { const float4 x = __ldcg(reinterpret_cast<const float4*>(src)); v[k][0] = x.x; v[k][1] = x.y; v[k][2] = x.z; v[k][3] = x.w; }
-                        else { const float2 x = __ldcg(reinterpret_cast<const float2*>(src)); v[k][0] = x.x; v[k][1] = x.y; }
+            for (int e = 0; e < VL; ++e) a[r][e] = 0.f;
+        }
+#pragma unroll 1
+        for (int kb = k_beg; kb < k_end; kb += KB) {
+            float2 ml[KB][RB];
+            float v[KB][RB][VL];
+#pragma unroll
+            for (int k = 0; k < KB; ++k) {
+                const float* sl = kb + k == 0 ? first : rest + (size_t)(kb + k) * 2 * slot;
+#pragma unroll
+                for (int r = 0; r < RB; ++r) {
+                    const int rl = r0 + team * RB + r;
+                    ml[k][r] = make_float2(-INFINITY, 0.f);
+#pragma unroll
+                    for (int e = 0; e < VL; ++e) v[k][r][e] = 0.f;
+                    if (kb + k < k_end && rl < rows) {
+                        ml[k][r] = __ldcg(reinterpret_cast<const float2*>(sl + tile_rows * D + 2 * rl));
+                        const float* src = sl + rl * D + VL * lane;
+                        if constexpr (VL == 4) { const float4 x = __ldcg(reinterpret_cast<const float4*>(src)); v[k][r][0] = x.x; v[k][r][1] = x.y; v[k][r][2] = x.z; v[k][r][3] = x.w; }
+                        else { const float2 x = __ldcg(reinterpret_cast<const float2*>(src)); v[k][r][0] = x.x; v[k][r][1] = x.y; }
                     }
                 }
-                float mn = m;
+            }
 #pragma unroll
-                for (int k = 0; k < 8; ++k) mn = fmaxf(mn, ml[k].x);
-                const float f = m == -INFINITY ? (lsum == 0.f ? 0.f : 1.f) : ex2(m - mn);     // keeps a NaN
-                lsum *= f;
+            for (int r = 0; r < RB; ++r) {
+                float mn = m[r];
 #pragma unroll
-                for (int e = 0; e < VL; ++e) a[e] *= f;
+                for (int k = 0; k < KB; ++k) mn = fmaxf(mn, ml[k][r].x);
+                const float f = m[r] == -INFINITY ? (lsum[r] == 0.f ? 0.f : 1.f) : ex2(m[r] - mn);      // keeps a NaN
+                lsum[r] *= f;
 #pragma unroll
-                for (int k = 0; k < 8; ++k) {
-                    if (ml[k].x == -INFINITY && ml[k].y == 0.f) continue;                     // not there, or saw nothing (a NaN goes on)
-                    const float g = ex2(ml[k].x - mn);
-                    lsum = fmaf(ml[k].y, g, lsum);
+                for (int e = 0; e < VL; ++e) a[r][e] *= f;
 #pragma unroll
-                    for (int e = 0; e < VL; ++e) a[e] = fmaf(v[k][e], g, a[e]);
+                for (int k = 0; k < KB; ++k) {
+                    // (not there, or saw nothing: weight 0; a NaN goes on)
+                    const float g = ml[k][r].x == -INFINITY && ml[k][r].y == 0.f ? 0.f : ex2(ml[k][r].x - mn);
+                    lsum[r] = fmaf(ml[k][r].y, g, lsum[r]);
+#pragma unroll
+                    for (int e = 0; e < VL; ++e) a[r][e] = fmaf(v[k][r][e], g, a[r][e]);
                 }
-                m = mn;
+                m[r] = mn;
             }
         }
-        if (share > 1) {
-            float* mine = xch + (size_t)warp * (D + 2);
+        if (RB == 1 && share > 1) {
+            float* mine = xch + warp * (D + 2);
 #pragma unroll
-            for (int e = 0; e < VL; ++e) mine[VL * lane + e] = a[e];
-            if (lane == 0) { mine[D] = m; mine[D + 1] = lsum; }
+            for (int e = 0; e < VL; ++e) mine[VL * lane + e] = a[0][e];
+            if (lane == 0) { mine[D] = m[0]; mine[D + 1] = lsum[0]; }
             sync();
-            if (sub == 0 && rl < rows) {
-                float mn = m;
+            if (sub == 0) {
+                float mn = m[0];
 #pragma unroll 1
-                for (int k = 1; k < share; ++k) mn = fmaxf(mn, mine[(size_t)k * (D + 2) + D]);
-                float ls = 0.f, b[VL];
+                for (int k = 1; k < share; ++k) mn = fmaxf(mn, mine[k * (D + 2) + D]);
+                lsum[0] = 0.f;
 #pragma unroll
-                for (int e = 0; e < VL; ++e) b[e] = 0.f;
+                for (int e = 0; e < VL; ++e) a[0][e] = 0.f;
 #pragma unroll 1
                 for (int k = 0; k < share; ++k) {
-                    const float* x = mine + (size_t)k * (D + 2);
+                    const float* x = mine + k * (D + 2);
                     if (x[D] == -INFINITY && x[D + 1] == 0.f) continue;
                     const float g = ex2(x[D] - mn);
-                    ls = fmaf(x[D + 1], g, ls);
+                    lsum[0] = fmaf(x[D + 1], g, lsum[0]);
 #pragma unroll
-                    for (int e = 0; e < VL; ++e) b[e] = fmaf(x[VL * lane + e], g, b[e]);
+                    for (int e = 0; e < VL; ++e) a[0][e] = fmaf(x[VL * lane + e], g, a[0][e]);
                 }
-                lsum = ls;
-#pragma unroll
-                for (int e = 0; e < VL; ++e) a[e] = b[e];
             }
             sync();                                              // xch is written again
         }
-        if (rl < rows && sub == 0) {
+#pragma unroll
+        for (int r = 0; r < RB; ++r) {
+            const int rl = r0 + team * RB + r;
+            if (rl >= rows || sub != 0) continue;
             const int rr = it.tile * tile_rows + rl;
-            const float inv = lsum == 0.f ? 0.f : 1.f / lsum;
+            const float inv = lsum[r] == 0.f ? 0.f : 1.f / lsum[r];
             T* dst = (T*)p.out + ((size_t)(it.q.row0 + rr / p.group) * p.q_heads + it.head * p.group + rr % p.group) * D + VL * lane;
-            if constexpr (VL == 4) store4<T>(dst, a[0] * inv, a[1] * inv, a[2] * inv, a[3] * inv);
-            else store2<T>(dst, a[0] * inv, a[1] * inv);
+            if constexpr (VL == 4) store4<T>(dst, a[r][0] * inv, a[r][1] * inv, a[r][2] * inv, a[r][3] * inv);
+            else store2<T>(dst, a[r][0] * inv, a[r][1] * inv);
         }
     }
 }

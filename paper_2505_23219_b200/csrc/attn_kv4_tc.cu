@@ -73,6 +73,7 @@ struct Ctrl {
     int abort_flag, arrived;
     alignas(16) float qs[128];       // sums of the tile's queries
     alignas(16) float fac[128];      // factors of a rescale, by row
+    float2 tot[128];                 // a row's sum of weights and of weighted minima
     float x[4][128], y[4][128];      // exchange between the four warps that share rows
     float4 par[PAR_SLOTS][UNIT];     // by unit and key: K's scale and middle (min + 8 scale) times log2(e) / sqrt(d_head), V's scale and middle
     alignas(4) uint8_t groups[GROUP_SLOTS][4];      // which of a quarter's two groups of 16 keys have a page, by unit
@@ -83,11 +84,15 @@ struct Ctrl {
 };
 template <int D, int N> constexpr uint32_t smem_bytes(int n_seqs) { return Shape<D, N>::CTRL_AT + (uint32_t)sizeof(Ctrl) + 8 * (uint32_t)n_seqs + 1024; }
 constexpr int WIDE_SEQS = 400;                 // most sequences of a call with tiles of 128 rows (their sums share the memory)
-static_assert(offsetof(Ctrl, qs) % 16 == 0 && offsetof(Ctrl, fac) % 16 == 0, "rows are read in pairs");
+static_assert(offsetof(Ctrl, qs) % 16 == 0 && offsetof(Ctrl, fac) % 16 == 0 && offsetof(Ctrl, par) % 16 == 0, "rows are read in pairs");
 static_assert(smem_bytes<128, 128>(WIDE_SEQS) <= 227 * 1024 && smem_bytes<128, 64>(GHD_MAX_SEQS) <= 227 * 1024, "shared memory");
 
 __device__ __forceinline__ void ld_frag(uint32_t taddr, uint32_t (&r)[4]) {      // 16 lanes x 8 columns, as an mma accumulator
     asm volatile("tcgen05.ld.sync.aligned.16x256b.x1.b32 {%0, %1, %2, %3}, [%4];" : "=r"(r[0]), "=r"(r[1]), "=r"(r[2]), "=r"(r[3]) : "r"(taddr) : "memory");
+}
+__device__ __forceinline__ void ld_cols8(uint32_t taddr, uint32_t (&r)[8]) {     // 32 lanes x 8 columns, a lane a thread
+    asm volatile("tcgen05.ld.sync.aligned.32x32b.x8.b32 {%0, %1, %2, %3, %4, %5, %6, %7}, [%8];"
+                 : "=r"(r[0]), "=r"(r[1]), "=r"(r[2]), "=r"(r[3]), "=r"(r[4]), "=r"(r[5]), "=r"(r[6]), "=r"(r[7]) : "r"(taddr) : "memory");
 }
 __device__ __forceinline__ void ld_frag2(uint32_t taddr, uint32_t (&a)[4], uint32_t (&b)[4]) {      // ... x 16 columns
     asm volatile("tcgen05.ld.sync.aligned.16x256b.x2.b32 {%0, %1, %2, %3, %4, %5, %6, %7}, [%8];"
@@ -212,7 +217,7 @@ __global__ void __launch_bounds__(THREADS, 1) k_attn_kv4_tc(const __grid_constan
     // The k-th item of this CTA (take = 0: there are no more, or a wait has run out).  One thread looks; who takes it together
     // with others gets it from that thread, so that all of them go on or stop alike.
     auto item_get = [&](int k) -> Kv4Item {
-        if (!wait<100>(smem_u32(&sm->item_full[k % ITEMS]), (k / ITEMS) & 1, abort_flag, w.status, DEV_TIMEOUT_EPI)) { Kv4Item none{}; return none; }
+        if (!wait<20>(smem_u32(&sm->item_full[k % ITEMS]), (k / ITEMS) & 1, abort_flag, w.status, DEV_TIMEOUT_EPI)) { Kv4Item none{}; return none; }
         const Kv4Item it = sm->item[k % ITEMS];
         mbar_arrive(smem_u32(&sm->item_empty[k % ITEMS]));
         return it;
@@ -231,8 +236,13 @@ __global__ void __launch_bounds__(THREADS, 1) k_attn_kv4_tc(const __grid_constan
         const uint32_t ring = base_a + SH::ST_AT + which * UNIT * ROW + quad * 32 * ROW, pring = base_a + SH::ST_AT + 2 * UNIT * ROW + quad * 32 * 4;
         int items = 0, lseq = 0, lhead = 0, lch = 0, lend = 0, lkeys = 0, n = 0;      // load cursor; units asked for so far
         bool more = true;
-        auto page_of = [&](int key) { return key < lkeys ? __ldg(w.table + (size_t)lseq * w.max_pages + (key >> w.shift)) : -1; };
-        int page[2] = {-1, -1};                                           // of the next unit's two groups of 16 keys, looked up one unit ahead
+        // page ids of the next sixteen units' two groups of 16 keys: lane 2 u + h has unit pbase + u
+        int pages = -1, pbase = 0;
+        auto look = [&]() {
+            const int key = (lch + (lane >> 1)) * UNIT + quad * 32 + 16 * (lane & 1);
+            pbase = lch;
+            pages = lch + (lane >> 1) < lend && key < lkeys ? __ldg(w.table + (size_t)lseq * w.max_pages + (key >> w.shift)) : -1;
+        };
         auto ask = [&]() {
             if (lch >= lend && more) {
                 if (lane == 0) {
@@ -246,10 +256,11 @@ __global__ void __launch_bounds__(THREADS, 1) k_attn_kv4_tc(const __grid_constan
                 lend = __shfl_sync(0xffffffffu, lend, 0);
                 lkeys = __shfl_sync(0xffffffffu, lkeys, 0);
                 more = lend > lch;
-#pragma unroll
-                for (int h = 0; h < 2; ++h) page[h] = page_of(lch * UNIT + quad * 32 + 16 * h);
+                look();
             }
             if (lch >= lend) return;
+            if (lch >= pbase + 16) look();
+            const int page[2] = {__shfl_sync(0xffffffffu, pages, 2 * (lch - pbase)), __shfl_sync(0xffffffffu, pages, 2 * (lch - pbase) + 1)};
             if (lane == 0) {
                 const int key0 = lch * UNIT + quad * 32, s_ = n % SH::STAGES;
                 const uint32_t full = smem_u32(&sm->c_full[own][s_]);
@@ -277,13 +288,9 @@ __global__ void __launch_bounds__(THREADS, 1) k_attn_kv4_tc(const __grid_constan
             }
             ++lch;
             ++n;
-            if (lch < lend) {
-#pragma unroll
-                for (int h = 0; h < 2; ++h) page[h] = page_of(lch * UNIT + quad * 32 + 16 * h);
-            }
         };
         auto landed = [&](int i) {
-            if (lane == 0) wait<100>(smem_u32(&sm->c_full[own][i % SH::STAGES]), (i / SH::STAGES) & 1, abort_flag, w.status, DEV_TIMEOUT_TMA);
+            if (lane == 0) wait<40>(smem_u32(&sm->c_full[own][i % SH::STAGES]), (i / SH::STAGES) & 1, abort_flag, w.status, DEV_TIMEOUT_TMA);
             __syncwarp();
         };
 #pragma unroll 1
@@ -526,72 +533,60 @@ __global__ void __launch_bounds__(THREADS, 1) k_attn_kv4_tc(const __grid_constan
                                 for (int x = 0; x < 4; ++x) vis |= ((w32 >> (8 * x)) & (groups >> (8 * quad + (x >> 1))) & 1u) << (8 * j + 4 * e + x);
                             }
                     }
-                    // Scores of key x and row e of block j (registers 2 (x & 1) + e of fragment x >> 1), in powers of two, against
-                    // the rows' references.  Where one of the 128 threads of these rows finds a score too far above, they agree on
-                    // new references and look again.
+                    // Scores of key x and row e of block j (registers 2 (x & 1) + e of fragment x >> 1), in powers of two, less the row's
+                    // reference (0 while it has none).
                     uint32_t s[JB][2][4];
-                    bool settled = false;
-#pragma unroll 1
-                    for (;;) {
 #pragma unroll
-                        for (int j = 0; j < JB; j += 2)
+                    for (int j = 0; j < JB; j += 2)
 #pragma unroll
-                            for (int h = 0; h < 2; ++h) ld_frag2(ts + col8(j0 + j) + ((uint32_t)(16 * h) << 16), s[j][h], s[j + 1][h]);
-                        ld_wait();
-                        float top = -INFINITY;
+                        for (int h = 0; h < 2; ++h) ld_frag2(ts + col8(j0 + j) + ((uint32_t)(16 * h) << 16), s[j][h], s[j + 1][h]);
+                    ld_wait();
+                    float top = -INFINITY;
 #pragma unroll
-                        for (int j = 0; j < JB; ++j) {
-                            const int c8 = col8(j0 + j);
-                            const float2 qq = *reinterpret_cast<const float2*>(&sm->qs[c8 + 2 * t]);
-                            float tj = -INFINITY;
+                    for (int j = 0; j < JB; ++j) {
+                        const float2 qq = *reinterpret_cast<const float2*>(&sm->qs[col8(j0 + j) + 2 * t]);
+                        const float b0 = ref[j0 + j][0] == -INFINITY ? 0.f : ref[j0 + j][0], b1 = ref[j0 + j][1] == -INFINITY ? 0.f : ref[j0 + j][1];
+                        float tj = -INFINITY;
 #pragma unroll
-                            for (int x = 0; x < 4; ++x) {
-                                uint32_t &r0 = s[j][x >> 1][2 * (x & 1)], &r1 = s[j][x >> 1][2 * (x & 1) + 1];
-                                const float a = fmaf(ks[x], __uint_as_float(r0), fmaf(km[x], qq.x, -ref[j0 + j][0]));
-                                const float c = fmaf(ks[x], __uint_as_float(r1), fmaf(km[x], qq.y, -ref[j0 + j][1]));
-                                r0 = __float_as_uint(a);
-                                r1 = __float_as_uint(c);
-                                tj = fmaxf(tj, fmaxf(a, c));
-                            }
-                            if (c8 < cols) top = fmaxf(top, tj);          // (blocks behind the tile's rows hold anything)
+                        for (int x = 0; x < 4; ++x) {
+                            uint32_t &r0 = s[j][x >> 1][2 * (x & 1)], &r1 = s[j][x >> 1][2 * (x & 1) + 1];
+                            const float a = fmaf(ks[x], __uint_as_float(r0), fmaf(km[x], qq.x, -b0));
+                            const float c = fmaf(ks[x], __uint_as_float(r1), fmaf(km[x], qq.y, -b1));
+                            r0 = __float_as_uint(a);
+                            r1 = __float_as_uint(c);
+                            tj = fmaxf(tj, fmaxf(a, c));
                         }
-                        if (__builtin_expect(!all, 0)) {
-                            top = -INFINITY;
+                        if (col8(j0 + j) < cols) top = fmaxf(top, tj);    // (blocks behind the tile's rows hold anything)
+                    }
+                    bool over = top > RAISE || k == 0;
+                    if (__builtin_expect(!all, 0)) {
+                        over = k == 0;
 #pragma unroll
-                            for (int j = 0; j < JB; ++j)
+                        for (int j = 0; j < JB; ++j)
 #pragma unroll
-                                for (int e = 0; e < 2; ++e)
+                            for (int e = 0; e < 2; ++e)
 #pragma unroll
-                                    for (int x = 0; x < 4; ++x) {
-                                        uint32_t& r = s[j][x >> 1][2 * (x & 1) + e];
-                                        if (!((vis >> (8 * j + 4 * e + x)) & 1u)) r = __float_as_uint(-INFINITY);
-                                        if (col8(j0 + j) < cols) top = fmaxf(top, __uint_as_float(r));
-                                    }
-                        }
-                        bool over = top > RAISE;
-                        if (j0 == 0) over = over || fmaxf(fmaxf(vs[0], vs[1]), fmaxf(vs[2], vs[3])) * vmul > 128.f;
-                        if (settled || __builtin_expect(!part_any(part, over), 1)) break;
-                        settled = true;
-                        // plain scores of the unit, their maxima by row, and the largest of V's scales
-#pragma unroll 1
-                        for (int j = 0; j < JB; ++j) {
-                            const int c8 = col8(j0 + j);
-                            const float2 qq = *reinterpret_cast<const float2*>(&sm->qs[c8 + 2 * t]);
-                            uint32_t o[2][4];
-                            ld_frag(ts + c8, o[0]);
-                            ld_frag(ts + c8 + (16u << 16), o[1]);
-                            ld_wait();
+                                for (int x = 0; x < 4; ++x) {
+                                    uint32_t& r = s[j][x >> 1][2 * (x & 1) + e];
+                                    if (!((vis >> (8 * j + 4 * e + x)) & 1u)) r = __float_as_uint(-INFINITY);
+                                    over = over || (col8(j0 + j) < cols && __uint_as_float(r) > (ref[j0 + j][e] == -INFINITY ? -INFINITY : RAISE));
+                                }
+                    }
+                    if (j0 == 0) over = over || fmaxf(fmaxf(vs[0], vs[1]), fmaxf(vs[2], vs[3])) * vmul > 128.f;
+                    // Where one of the 128 threads of these rows finds a score too far above (and in an item's first unit), they agree
+                    // on new references.
+                    if (__builtin_expect(part_any(part, over), 0)) {
+#pragma unroll
+                        for (int j = 0; j < JB; ++j)
 #pragma unroll
                             for (int e = 0; e < 2; ++e) {
                                 float m = -INFINITY;
 #pragma unroll
-                                for (int x = 0; x < 4; ++x)
-                                    if ((vis >> (8 * j + 4 * e + x)) & 1u) m = fmaxf(m, fmaf(ks[x], __uint_as_float(o[x >> 1][2 * (x & 1) + e]), km[x] * (e ? qq.y : qq.x)));
+                                for (int x = 0; x < 4; ++x) m = fmaxf(m, __uint_as_float(s[j][x >> 1][2 * (x & 1) + e]));
 #pragma unroll
                                 for (int sh = 4; sh < 32; sh <<= 1) m = fmaxf(m, __shfl_xor_sync(0xffffffffu, m, sh));
-                                if (g == 0) sm->x[quad][c8 + 2 * t + e] = m;
+                                if (g == 0) sm->x[quad][col8(j0 + j) + 2 * t + e] = m;
                             }
-                        }
                         float vx = 0.f;
 #pragma unroll
                         for (int x = 0; x < 4; ++x) if (vs[x] <= 65504.f) vx = fmaxf(vx, vs[x]);
@@ -612,12 +607,18 @@ __global__ void __launch_bounds__(THREADS, 1) k_attn_kv4_tc(const __grid_constan
                             if (j >= j0 && j < j0 + JB) {
 #pragma unroll
                                 for (int e = 0; e < 2; ++e) {
-                                    const float m = fmaxf(fmaxf(sm->x[0][rl + e], sm->x[1][rl + e]), fmaxf(sm->x[2][rl + e], sm->x[3][rl + e]));
-                                    if (m > ref[j][e]) {
-                                        f[e] = ex2(ref[j][e] - m);        // 0 from a reference of -infinity
-                                        ref[j][e] = m;
+                                    const float old = ref[j][e] == -INFINITY ? 0.f : ref[j][e];
+                                    const float up = fmaxf(fmaxf(sm->x[0][rl + e], sm->x[1][rl + e]), fmaxf(sm->x[2][rl + e], sm->x[3][rl + e]));
+                                    if (up > (ref[j][e] == -INFINITY ? -INFINITY : 0.f)) {     // the new reference is `up` above the old one
+                                        f[e] = ref[j][e] == -INFINITY ? 0.f : ex2(-up);
+                                        ref[j][e] = old + up;
                                         l[j][e] *= f[e];
                                         ms[j][e] *= f[e];
+#pragma unroll
+                                        for (int x = 0; x < 4; ++x) {
+                                            uint32_t& r = s[j - j0][x >> 1][2 * (x & 1) + e];
+                                            r = __float_as_uint(__uint_as_float(r) - up);
+                                        }
                                     }
                                 }
                             }
@@ -701,41 +702,38 @@ __global__ void __launch_bounds__(THREADS, 1) k_attn_kv4_tc(const __grid_constan
                 }
             }
             named_sync<1, SOFT>();
+            if (tid < rows) {                                             // (sum of weights, minima's sum) of a row; qs has been read for the last time
+                const float lsum = (sm->x[0][tid] + sm->x[1][tid]) + (sm->x[2][tid] + sm->x[3][tid]), mm = (sm->y[0][tid] + sm->y[1][tid]) + (sm->y[2][tid] + sm->y[3][tid]);
+                sm->tot[tid] = make_float2(lsum, mm);
+            }
+            named_sync<1, SOFT>();
             wait(smem_u32(&sm->p_empty[(i - 1) & 1]), ((i - 1) >> 1) & 1, abort_flag, w.status, DEV_TIMEOUT_EPI);
             tc_fence_after();
             const int64_t c0 = it.first / per, c1 = (it.first + it.chunks - 1) / per;
             const bool whole = c0 == c1;
             float* slot = p.part + ((size_t)blockIdx.x * 2 + ((int64_t)blockIdx.x == c0 ? 1 : 0)) * ((size_t)N * (D + 2));
-            const float vinv = 1.f / vmul;
-            // lane (16 h + g or + 8) of this quad is channel ch_of(lane); columns of this part's blocks
-            auto ch_of = [](int m) { return (m & ~7) | ((m & 1) * 4) | ((m & 7) >> 1); };       // 0 4 1 5 2 6 3 7
+            const float vinv = 1.f / vmul;                                // (of this part's rows: the same in its four warps)
+            // lane m of the accumulator is channel (m & ~7) | {0 4 1 5 2 6 3 7}[m & 7]; a row's channels of this quarter are one store of the warp
+            const int chn = quad * 32 + ((lane & ~7) | ((lane & 1) * 4) | ((lane & 7) >> 1));
+            if (quad * 32 < D) {
 #pragma unroll 1
-            for (int j = 0; j < NB && col8(j) < rows && quad * 32 < D; ++j) {
-                const int blk = col8(j) >> 3;
-                uint32_t o[2][4];
-                const uint32_t to = tmem + SH::T_O + 8 * blk + ((uint32_t)(quad * 32) << 16);
-                ld_frag(to, o[0]);
-                ld_frag(to + (16u << 16), o[1]);
-                ld_wait();
+                for (int j = 0; j < NB && col8(j) < rows; ++j) {
+                    uint32_t o[8];
+                    const int r0 = col8(j);
+                    ld_cols8(tmem + SH::T_O + r0 + ((uint32_t)(quad * 32) << 16), o);
+                    ld_wait();
 #pragma unroll
-                for (int e = 0; e < 2; ++e) {
-                    const int rl = 8 * blk + 2 * t + e;
-                    if (rl >= rows) continue;
-                    const float lsum = (sm->x[0][rl] + sm->x[1][rl]) + (sm->x[2][rl] + sm->x[3][rl]), mm = (sm->y[0][rl] + sm->y[1][rl]) + (sm->y[2][rl] + sm->y[3][rl]);
-                    const float inv = lsum == 0.f ? 0.f : 1.f / lsum;
-                    __half* dst = (__half*)p.out + (size_t)sm->rowix[rl] * D + quad * 32 + ch_of(g);
-                    float* part = slot + (size_t)rl * D + quad * 32 + ch_of(g);
-#pragma unroll
-                    for (int h = 0; h < 2; ++h)
-#pragma unroll
-                        for (int x = 0; x < 2; ++x) {
-                            const float v = fmaf(__uint_as_float(o[h][2 * x + e]), vinv, mm);
-                            if (whole) dst[16 * h + 8 * x] = __float2half_rn(v * inv);
-                            else __stcg(part + 16 * h + 8 * x, v);
-                        }
-                    if (!whole && g == 0 && quad == 0) __stcg(reinterpret_cast<float2*>(slot + (size_t)N * D + 2 * rl), make_float2(sm->fac[rl], lsum));
+                    for (int x = 0; x < 8; ++x) {
+                        const int rl = r0 + x;
+                        if (rl >= rows) break;
+                        const float2 tm = sm->tot[rl];
+                        const float v = fmaf(__uint_as_float(o[x]), vinv, tm.y);
+                        if (whole) ((__half*)p.out)[(size_t)sm->rowix[rl] * D + chn] = __float2half_rn(tm.x == 0.f ? 0.f : v / tm.x);
+                        else __stcg(slot + (size_t)rl * D + chn, v);
+                    }
                 }
             }
+            if (!whole && tid < rows) __stcg(reinterpret_cast<float2*>(slot + (size_t)N * D + 2 * tid), make_float2(sm->fac[tid], sm->tot[tid].x));
             tc_fence_before();                                            // O^T has been read: the next item's first product may write it
             if (!whole) {
                 __threadfence();
@@ -747,7 +745,7 @@ __global__ void __launch_bounds__(THREADS, 1) k_attn_kv4_tc(const __grid_constan
                     __threadfence();
                 }
                 named_sync<1, SOFT>();
-                if (sm->arrived) merge_item<__half, D, SOFT / 32>(p, it, N, rows, c0, c1, warp, reinterpret_cast<float*>(base + SH::P_AT), [] { named_sync<1, SOFT>(); });
+                if (sm->arrived) merge_item<__half, D, 4>(p, it, N, rows, c0, c1, warp, SW, nullptr, [] {});
             }
             named_sync<1, SOFT>();                                        // queries' sums and exchange buffers are written again
         }
