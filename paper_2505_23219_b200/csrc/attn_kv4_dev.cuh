@@ -20,7 +20,7 @@ struct Kv4AttnParams {
 constexpr float KV4_LOG2E = 1.4426950408889634f;
 
 // attn_kv4_tc.cu: tiles of many query rows on the tcgen05 tensor cores (GHD_F16)
-ghd_status launch_attn_kv4_tc(ghd_ctx* c, Kv4AttnParams& p, int tile_rows);
+ghd_status launch_attn_kv4_tc(ghd_ctx* c, Kv4AttnParams& p);
 
 #ifdef __CUDACC__
 namespace kv4 {

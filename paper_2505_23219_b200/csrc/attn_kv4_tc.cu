@@ -33,6 +33,8 @@ using namespace tc;
 using namespace kv4;
 
 constexpr int UNIT = 128;                      // keys of a unit (MMA M of S^T, MMA K of O^T)
+constexpr int N = 64;                          // query rows of a tile; tiles of 128 rows unpack each key half as often and measured slower
+                                               // (256 nodes, 13B shape, 4096 rows: 108 us against 90): their code does not fit the cache
 #ifndef KV4_SOFT
 #define KV4_SOFT 256
 #endif
@@ -44,18 +46,17 @@ constexpr int REGS_LAUNCH = SOFT == 512 ? 72 : 96, REGS_SOFT = SOFT == 512 ? 80 
 static_assert(SOFT * REGS_SOFT + CONV * REGS_CONV + 128 * REGS_ISSUE <= THREADS * REGS_LAUNCH && THREADS * REGS_LAUNCH <= 65536, "register split");
 constexpr float RAISE = 8.f;
 constexpr int LEAD = 6;                        // an item's fixed cost in units
-// What the softmax warps need of a unit's keys is ready when its keys are: the K warps are two units ahead of the first
-// product, which is two ahead of the softmax warps.
-constexpr int PAR_SLOTS = 4;
-// The loader is at most four units ahead of the unpacking warps.
-constexpr int GROUP_SLOTS = 8;
+// What the softmax warps need of a unit's keys is ready when its keys are.  The K warps are two units ahead of the first
+// product, that is two ahead of the scores being fetched, and those one ahead of what the softmax warps work on: five in use.
+constexpr int PAR_SLOTS = 8;
+// The copies are asked for three units ahead of the unpacking.
+constexpr int GROUP_SLOTS = 16;
 constexpr uint32_t V_SLAB = UNIT * 128;        // [128 keys x 64 channels] half
 
-template <int D, int N>
+template <int D>
 struct Shape {
-    static constexpr int STAGES = N == 128 ? 2 : 4;
-    static constexpr int SLABS = D / 64, PSLABS = N / 64;
-    static constexpr uint32_t Q_BYTES = SLABS * N * 128, V_BYTES = SLABS * V_SLAB, P_BYTES = PSLABS * UNIT * 128;
+    static constexpr int STAGES = 4, SLABS = D / 64;
+    static constexpr uint32_t Q_BYTES = SLABS * N * 128, V_BYTES = SLABS * V_SLAB, P_BYTES = UNIT * 128;
     static constexpr uint32_t ST_BYTES = UNIT * (D + 8);                 // codes of a unit, D / 2 bytes a row, K then V; then K's and V's (scale, min)
     static constexpr uint32_t V_AT = Q_BYTES, P_AT = V_AT + 2 * V_BYTES, ST_AT = P_AT + 2 * P_BYTES, CTRL_AT = ST_AT + STAGES * ST_BYTES;
     static constexpr uint32_t T_K = 0, T_S = 2 * (D / 2), T_O = T_S + 2 * N;      // tensor-memory columns
@@ -71,21 +72,20 @@ struct Ctrl {
     uint64_t q_full, k_full[2], k_empty[2], v_full[2], v_empty[2], s_full[2], s_empty[2], p_full[2], p_empty[2], drain, drain_pv;
     uint32_t tmem_base;
     int abort_flag, arrived;
-    alignas(16) float qs[128];       // sums of the tile's queries
-    alignas(16) float fac[128];      // factors of a rescale, by row
-    float2 tot[128];                 // a row's sum of weights and of weighted minima
-    float x[4][128], y[4][128];      // exchange between the four warps that share rows
+    alignas(16) float qs[N];       // sums of the tile's queries
+    alignas(16) float fac[N];      // factors of a rescale, by row
+    float4 tot[N];                   // a row's sum of weights, its inverse, sum of weighted middles
+    float x[4][N], y[4][N];      // exchange between the four warps that share rows
     float4 par[PAR_SLOTS][UNIT];     // by unit and key: K's scale and middle (min + 8 scale) times log2(e) / sqrt(d_head), V's scale and middle
     alignas(4) uint8_t groups[GROUP_SLOTS][4];      // which of a quarter's two groups of 16 keys have a page, by unit
-    int rowix[128];                  // row of q and out, in d_head elements, of the tile's query rows
+    int rowix[N];                  // row of q and out, in d_head elements, of the tile's query rows
     float vmax[PARTS][4];            // largest of V's scales of a unit, by part and warp
     int64_t scratch[32];
     int64_t sums[1];                 // [n_seqs + 1]
 };
-template <int D, int N> constexpr uint32_t smem_bytes(int n_seqs) { return Shape<D, N>::CTRL_AT + (uint32_t)sizeof(Ctrl) + 8 * (uint32_t)n_seqs + 1024; }
-constexpr int WIDE_SEQS = 400;                 // most sequences of a call with tiles of 128 rows (their sums share the memory)
+template <int D> constexpr uint32_t smem_bytes(int n_seqs) { return Shape<D>::CTRL_AT + (uint32_t)sizeof(Ctrl) + 8 * (uint32_t)n_seqs + 1024; }
 static_assert(offsetof(Ctrl, qs) % 16 == 0 && offsetof(Ctrl, fac) % 16 == 0 && offsetof(Ctrl, par) % 16 == 0, "rows are read in pairs");
-static_assert(smem_bytes<128, 128>(WIDE_SEQS) <= 227 * 1024 && smem_bytes<128, 64>(GHD_MAX_SEQS) <= 227 * 1024, "shared memory");
+static_assert(smem_bytes<128>(GHD_MAX_SEQS) <= 227 * 1024, "shared memory");
 
 __device__ __forceinline__ void ld_frag(uint32_t taddr, uint32_t (&r)[4]) {      // 16 lanes x 8 columns, as an mma accumulator
     asm volatile("tcgen05.ld.sync.aligned.16x256b.x1.b32 {%0, %1, %2, %3}, [%4];" : "=r"(r[0]), "=r"(r[1]), "=r"(r[2]), "=r"(r[3]) : "r"(taddr) : "memory");
@@ -172,11 +172,10 @@ __device__ __forceinline__ void unpack8(uint32_t w, uint32_t* r, const HalfMagic
     r[2] = centred_half<0>(x, m);
     r[3] = centred_half<4>(x, m);
 }
-template <int D, int N>
+template <int D>
 __global__ void __launch_bounds__(THREADS, 1) k_attn_kv4_tc(const __grid_constant__ Kv4AttnParams p) {
-    using SH = Shape<D, N>;
+    using SH = Shape<D>;
     constexpr int NB = N / 8 / PARTS;                // blocks of eight query rows of a softmax thread
-    constexpr int JB = NB < 4 ? NB : 4;              // ... and at a time
     constexpr int PIECES = D / 32;                   // 16-byte pieces of a packed row
     constexpr uint32_t ROW = D / 2;                  // bytes of a packed row
     extern __shared__ uint8_t smem_raw[];
@@ -304,7 +303,7 @@ __global__ void __launch_bounds__(THREADS, 1) k_attn_kv4_tc(const __grid_constan
                 ask();
                 landed(i);
                 const uint32_t st = base_a + SH::ST_AT + (uint32_t)(i % SH::STAGES) * SH::ST_BYTES + (quad * 32 + lane) * ROW;
-                if (i >= 2) wait<100>(smem_u32(&sm->k_empty[b]), ((i >> 1) - 1) & 1, abort_flag, w.status, DEV_TIMEOUT_TMEM);
+                if (i >= 2) wait<200>(smem_u32(&sm->k_empty[b]), ((i >> 1) - 1) & 1, abort_flag, w.status, DEV_TIMEOUT_TMEM);
                 tc_fence_after();
                 {
                     const uint32_t at = pring + (uint32_t)(i % SH::STAGES) * SH::ST_BYTES + 4 * lane;
@@ -331,7 +330,11 @@ __global__ void __launch_bounds__(THREADS, 1) k_attn_kv4_tc(const __grid_constan
             // ------------------------------------------------ V: a lane takes one 16-byte piece of a row at a time; eight lanes read 128
             // bytes in a row, and their four stores go to eight different bank groups
             const int row0 = quad * 32 + lane / PIECES, c = lane % PIECES, turn = D == 128 ? (c >> 1) << 1 : 0;
-            constexpr int PER = 32 / PIECES;
+            constexpr int PER = 32 / PIECES;                              // rows a step: a multiple of 8, so the swizzle of a lane's rows is one
+            const uint32_t vt0 = base_a + SH::V_AT + (c >> 1) * V_SLAB + row0 * 128;
+            uint32_t off[4];
+#pragma unroll
+            for (int k = 0; k < 4; ++k) off[k] = (((c & 1) * 4 + (k ^ turn)) ^ (row0 & 7)) << 4;
 #pragma unroll 1
             for (int i = 0; i < n; ++i) {                                 // (n runs ahead until the last unit has been asked for)
                 const int b = i & 1;
@@ -341,17 +344,16 @@ __global__ void __launch_bounds__(THREADS, 1) k_attn_kv4_tc(const __grid_constan
                 const uint32_t st = base_a + SH::ST_AT + (uint32_t)(i % SH::STAGES) * SH::ST_BYTES + UNIT * ROW + row0 * ROW + 16 * c;
                 if (i >= 2) wait<100>(smem_u32(&sm->v_empty[b]), ((i >> 1) - 1) & 1, abort_flag, w.status, DEV_TIMEOUT_TMEM);
                 uint4 x = lds128(st);
+                uint32_t vt = vt0 + b * SH::V_BYTES;
 #pragma unroll 1
-                for (int j = 0; j < PIECES; ++j) {
-                    const int key = row0 + j * PER;
-                    const uint32_t vt = base_a + SH::V_AT + b * SH::V_BYTES + (c >> 1) * V_SLAB + key * 128;
+                for (int j = 0; j < PIECES; ++j, vt += PER * 128) {
                     const uint32_t wd[4] = {turn ? x.z : x.x, turn ? x.w : x.y, turn ? x.x : x.z, turn ? x.y : x.w};
                     if (j + 1 < PIECES) x = lds128(st + (j + 1) * PER * ROW);
 #pragma unroll
                     for (int k = 0; k < 4; ++k) {
                         uint32_t r[4];
                         unpack8(wd[k], r, magic);
-                        sts128(vt + ((((c & 1) * 4 + (k ^ turn)) ^ (key & 7)) << 4), r);
+                        sts128(vt + off[k], r);
                     }
                 }
                 asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
@@ -380,8 +382,8 @@ __global__ void __launch_bounds__(THREADS, 1) k_attn_kv4_tc(const __grid_constan
 #pragma unroll 1
                 for (int k = 0; ok && k < it.take; ++k, ++i) {
                     const int b = i & 1;
-                    ok = wait(smem_u32(&sm->k_full[b]), (i >> 1) & 1, abort_flag, w.status, DEV_TIMEOUT_MMA);
-                    if (ok && i >= 2) ok = wait(smem_u32(&sm->s_empty[b]), ((i >> 1) - 1) & 1, abort_flag, w.status, DEV_TIMEOUT_TMEM);
+                    ok = wait<30>(smem_u32(&sm->k_full[b]), (i >> 1) & 1, abort_flag, w.status, DEV_TIMEOUT_MMA);
+                    if (ok && i >= 2) ok = wait<30>(smem_u32(&sm->s_empty[b]), ((i >> 1) - 1) & 1, abort_flag, w.status, DEV_TIMEOUT_TMEM);
                     if (!ok) break;
                     tc_fence_after();
 #pragma unroll 1
@@ -413,8 +415,8 @@ __global__ void __launch_bounds__(THREADS, 1) k_attn_kv4_tc(const __grid_constan
 #pragma unroll 1
                 for (int k = 0; ok && k < it.take; ++k, ++i) {
                     const int b = i & 1;
-                    ok = wait(smem_u32(&sm->v_full[b]), (i >> 1) & 1, abort_flag, w.status, DEV_TIMEOUT_MMA);
-                    if (ok) ok = wait(smem_u32(&sm->p_full[b]), (i >> 1) & 1, abort_flag, w.status, DEV_TIMEOUT_MMA);
+                    ok = wait<30>(smem_u32(&sm->v_full[b]), (i >> 1) & 1, abort_flag, w.status, DEV_TIMEOUT_MMA);
+                    if (ok) ok = wait<30>(smem_u32(&sm->p_full[b]), (i >> 1) & 1, abort_flag, w.status, DEV_TIMEOUT_MMA);
                     if (!ok) break;
                     tc_fence_after();
 #pragma unroll 1
@@ -497,17 +499,36 @@ __global__ void __launch_bounds__(THREADS, 1) k_attn_kv4_tc(const __grid_constan
                 named_sync<1, SOFT>();                                    // the sums are read by everybody
             }
             // running sums and references of this thread's rows: rows 2 t + e of its blocks
-            float l[NB][2], ms[NB][2], ref[NB][2];
+            // `base`: what a row's scores are taken against, its reference, or 0 while it has none (its bit 2 j + e of `none`)
+            float l[NB][2], ms[NB][2], base[NB][2];
+            uint32_t none = (1u << 2 * NB) - 1u;
 #pragma unroll
             for (int j = 0; j < NB; ++j)
 #pragma unroll
-                for (int e = 0; e < 2; ++e) { l[j][e] = ms[j][e] = 0.f; ref[j][e] = -INFINITY; }
+                for (int e = 0; e < 2; ++e) l[j][e] = ms[j][e] = base[j][e] = 0.f;
             float vmul = 0x1p24f;                                         // 2^-e of V's scales
+            // The scores of a unit are fetched while the one before is worked on: s[j][h] has the 16 keys 16 h of block j.
+            uint32_t s[NB][2][4];
+            auto fetch = [&](int u) {
+                const int b = u & 1;
+                wait(smem_u32(&sm->s_full[b]), (u >> 1) & 1, abort_flag, w.status, DEV_TIMEOUT_EPI);
+                tc_fence_after();
+                const uint32_t ts = tmem + SH::T_S + b * N + ((uint32_t)(quad * 32) << 16);
+#pragma unroll
+                for (int j = 0; j < NB; j += 2)
+#pragma unroll
+                    for (int h = 0; h < 2; ++h) ld_frag2(ts + col8(j) + ((uint32_t)(16 * h) << 16), s[j][h], s[j + 1][h]);
+            };
+            auto fetched = [&](int u) {
+                ld_wait();
+                tc_fence_before();
+                warp_arrive(smem_u32(&sm->s_empty[u & 1]));
+            };
+            fetch(i);
+            fetched(i);
 #pragma unroll 1
             for (int k = 0; k < it.take; ++k, ++i) {
                 const int b = i & 1, key0 = (it.chunk0 + k) * UNIT + quad * 32 + g;
-                wait(smem_u32(&sm->s_full[b]), (i >> 1) & 1, abort_flag, w.status, DEV_TIMEOUT_EPI);
-                tc_fence_after();
                 float ks[4], km[4], vs[4], vm[4];
 #pragma unroll
                 for (int x = 0; x < 4; ++x) {
@@ -516,195 +537,160 @@ __global__ void __launch_bounds__(THREADS, 1) k_attn_kv4_tc(const __grid_constan
                 }
                 const uint32_t groups = *reinterpret_cast<const uint32_t*>(sm->groups[i & (GROUP_SLOTS - 1)]);
                 const bool all = (it.chunk0 + k + 1) * UNIT <= it.q.len && groups == 0x03030303u;      // every key of the unit is visible to every row
+                // Scores of key x and row e of block j (registers 2 (x & 1) + e of fragment x >> 1), in powers of two, less the base.
+                float sc[NB][4][2], top = -INFINITY;
 #pragma unroll
-                for (int j0 = 0; j0 < NB; j0 += JB) {                     // up to 32 of this thread's scores at a time
-                    if (col8(j0) >= cols) break;           // (whole parts have nothing when the tile has few rows)
-                    const uint32_t ts = tmem + SH::T_S + b * N + ((uint32_t)(quad * 32) << 16);
-                    uint32_t vis = 0xffffffffu;                           // bit 8 j + 4 e + x: row e of block j sees key x
-                    if (__builtin_expect(!all, 0)) {
-                        vis = 0u;
+                for (int j = 0; j < NB; ++j) {
+                    const float2 qq = *reinterpret_cast<const float2*>(&sm->qs[col8(j) + 2 * t]);
+                    float tj = -INFINITY;
 #pragma unroll
-                        for (int j = 0; j < JB; ++j)
-#pragma unroll
-                            for (int e = 0; e < 2; ++e) {
-                                const int node = (it.tile * N + col8(j0 + j) + 2 * t + e) / p.group;
-                                const uint32_t w32 = sees(p, it.q, node, key0 - it.q.len);
-#pragma unroll
-                                for (int x = 0; x < 4; ++x) vis |= ((w32 >> (8 * x)) & (groups >> (8 * quad + (x >> 1))) & 1u) << (8 * j + 4 * e + x);
-                            }
+                    for (int x = 0; x < 4; ++x) {
+                        sc[j][x][0] = fmaf(ks[x], __uint_as_float(s[j][x >> 1][2 * (x & 1)]), fmaf(km[x], qq.x, -base[j][0]));
+                        sc[j][x][1] = fmaf(ks[x], __uint_as_float(s[j][x >> 1][2 * (x & 1) + 1]), fmaf(km[x], qq.y, -base[j][1]));
+                        tj = fmaxf(tj, fmaxf(sc[j][x][0], sc[j][x][1]));
                     }
-                    // Scores of key x and row e of block j (registers 2 (x & 1) + e of fragment x >> 1), in powers of two, less the row's
-                    // reference (0 while it has none).
-                    uint32_t s[JB][2][4];
+                    if (col8(j) < cols) top = fmaxf(top, tj);             // (blocks behind the tile's rows hold anything)
+                }
+                bool over = top > RAISE || k == 0;
+                uint32_t vis = 0xffffffffu;                               // bit 8 j + 4 e + x: row e of block j sees key x
+                if (__builtin_expect(!all, 0)) {
+                    vis = 0u;
+                    over = k == 0;
 #pragma unroll
-                    for (int j = 0; j < JB; j += 2)
+                    for (int j = 0; j < NB; ++j)
 #pragma unroll
-                        for (int h = 0; h < 2; ++h) ld_frag2(ts + col8(j0 + j) + ((uint32_t)(16 * h) << 16), s[j][h], s[j + 1][h]);
-                    ld_wait();
-                    float top = -INFINITY;
-#pragma unroll
-                    for (int j = 0; j < JB; ++j) {
-                        const float2 qq = *reinterpret_cast<const float2*>(&sm->qs[col8(j0 + j) + 2 * t]);
-                        const float b0 = ref[j0 + j][0] == -INFINITY ? 0.f : ref[j0 + j][0], b1 = ref[j0 + j][1] == -INFINITY ? 0.f : ref[j0 + j][1];
-                        float tj = -INFINITY;
-#pragma unroll
-                        for (int x = 0; x < 4; ++x) {
-                            uint32_t &r0 = s[j][x >> 1][2 * (x & 1)], &r1 = s[j][x >> 1][2 * (x & 1) + 1];
-                            const float a = fmaf(ks[x], __uint_as_float(r0), fmaf(km[x], qq.x, -b0));
-                            const float c = fmaf(ks[x], __uint_as_float(r1), fmaf(km[x], qq.y, -b1));
-                            r0 = __float_as_uint(a);
-                            r1 = __float_as_uint(c);
-                            tj = fmaxf(tj, fmaxf(a, c));
-                        }
-                        if (col8(j0 + j) < cols) top = fmaxf(top, tj);    // (blocks behind the tile's rows hold anything)
-                    }
-                    bool over = top > RAISE || k == 0;
-                    if (__builtin_expect(!all, 0)) {
-                        over = k == 0;
-#pragma unroll
-                        for (int j = 0; j < JB; ++j)
-#pragma unroll
-                            for (int e = 0; e < 2; ++e)
-#pragma unroll
-                                for (int x = 0; x < 4; ++x) {
-                                    uint32_t& r = s[j][x >> 1][2 * (x & 1) + e];
-                                    if (!((vis >> (8 * j + 4 * e + x)) & 1u)) r = __float_as_uint(-INFINITY);
-                                    over = over || (col8(j0 + j) < cols && __uint_as_float(r) > (ref[j0 + j][e] == -INFINITY ? -INFINITY : RAISE));
-                                }
-                    }
-                    if (j0 == 0) over = over || fmaxf(fmaxf(vs[0], vs[1]), fmaxf(vs[2], vs[3])) * vmul > 128.f;
-                    // Where one of the 128 threads of these rows finds a score too far above (and in an item's first unit), they agree
-                    // on new references.
-                    if (__builtin_expect(part_any(part, over), 0)) {
-#pragma unroll
-                        for (int j = 0; j < JB; ++j)
-#pragma unroll
-                            for (int e = 0; e < 2; ++e) {
-                                float m = -INFINITY;
-#pragma unroll
-                                for (int x = 0; x < 4; ++x) m = fmaxf(m, __uint_as_float(s[j][x >> 1][2 * (x & 1) + e]));
-#pragma unroll
-                                for (int sh = 4; sh < 32; sh <<= 1) m = fmaxf(m, __shfl_xor_sync(0xffffffffu, m, sh));
-                                if (g == 0) sm->x[quad][col8(j0 + j) + 2 * t + e] = m;
-                            }
-                        float vx = 0.f;
-#pragma unroll
-                        for (int x = 0; x < 4; ++x) if (vs[x] <= 65504.f) vx = fmaxf(vx, vs[x]);
-#pragma unroll
-                        for (int sh = 4; sh < 32; sh <<= 1) vx = fmaxf(vx, __shfl_xor_sync(0xffffffffu, vx, sh));
-                        if (lane == 0) sm->vmax[part][quad] = vx;
-                        part_sync(part);
-                        // the exponent changes before the unit's first weights only
-                        float vnew = vmul;
-                        vx = fmaxf(fmaxf(sm->vmax[part][0], sm->vmax[part][1]), fmaxf(sm->vmax[part][2], sm->vmax[part][3]));
-                        if (j0 == 0 && vx * vmul > 1.f) vnew = exp2f(-ceilf(log2f(vx)));
-                        const float fv = vnew / vmul;
-                        vmul = vnew;
-#pragma unroll
-                        for (int j = 0; j < NB; ++j) {
-                            float f[2] = {1.f, 1.f};
-                            const int rl = col8(j) + 2 * t;
-                            if (j >= j0 && j < j0 + JB) {
-#pragma unroll
-                                for (int e = 0; e < 2; ++e) {
-                                    const float old = ref[j][e] == -INFINITY ? 0.f : ref[j][e];
-                                    const float up = fmaxf(fmaxf(sm->x[0][rl + e], sm->x[1][rl + e]), fmaxf(sm->x[2][rl + e], sm->x[3][rl + e]));
-                                    if (up > (ref[j][e] == -INFINITY ? -INFINITY : 0.f)) {     // the new reference is `up` above the old one
-                                        f[e] = ref[j][e] == -INFINITY ? 0.f : ex2(-up);
-                                        ref[j][e] = old + up;
-                                        l[j][e] *= f[e];
-                                        ms[j][e] *= f[e];
-#pragma unroll
-                                        for (int x = 0; x < 4; ++x) {
-                                            uint32_t& r = s[j - j0][x >> 1][2 * (x & 1) + e];
-                                            r = __float_as_uint(__uint_as_float(r) - up);
-                                        }
-                                    }
-                                }
-                            }
-                            if (quad == 0 && g == 0) { sm->fac[rl] = f[0] * fv; sm->fac[rl + 1] = f[1] * fv; }
-                        }
-                        part_sync(part);
-                        if (k > 0) {
-                            // O^T holds the products of the units before once the last of them has completed (each P buffer's
-                            // release is waited for again two units later, so its phases are seen one by one)
-                            wait(smem_u32(&sm->p_empty[(i - 1) & 1]), ((i - 1) >> 1) & 1, abort_flag, w.status, DEV_TIMEOUT_EPI);
-                            tc_fence_after();
-#pragma unroll 1
-                            for (int j = 0; j < NB && col8(j) < cols; ++j) {      // this part's blocks of eight columns, both groups of 16 lanes
-                                const int c0 = col8(j);
-                                const float2 f = *reinterpret_cast<const float2*>(&sm->fac[c0 + 2 * t]);
-                                const uint32_t to = tmem + SH::T_O + c0 + ((uint32_t)(quad * 32) << 16);
-                                uint32_t o[2][4];
-                                ld_frag(to, o[0]);
-                                ld_frag(to + (16u << 16), o[1]);
-                                ld_wait();
-#pragma unroll
-                                for (int h = 0; h < 2; ++h) {
-#pragma unroll
-                                    for (int e = 0; e < 4; ++e) o[h][e] = __float_as_uint(__uint_as_float(o[h][e]) * ((e & 1) ? f.y : f.x));
-                                    st_frag(to + ((uint32_t)(16 * h) << 16), o[h]);
-                                }
-                            }
-                            st_wait();
-                            tc_fence_before();
-                        }
-                        part_sync(part);                                  // the exchange buffers may be written again
-                    }
-                    if (j0 == 0 && i >= 2) wait(smem_u32(&sm->p_empty[b]), ((i >> 1) - 1) & 1, abort_flag, w.status, DEV_TIMEOUT_EPI);
-                    float vsc[4];
-#pragma unroll
-                    for (int x = 0; x < 4; ++x) vsc[x] = vs[x] * vmul;
-                    // (one straight run of instructions for the units that matter, where nothing is masked and every block has rows)
-                    auto weights = [&](auto plain) {
-                        constexpr bool PLAIN = decltype(plain)::value;
-#pragma unroll
-                        for (int j = 0; j < JB; ++j) {
-                            const int blk = col8(j0 + j) >> 3;
-                            if (!PLAIN && 8 * blk >= cols) break;
-                            uint32_t h4[4];
+                        for (int e = 0; e < 2; ++e) {
+                            const uint32_t w32 = sees(p, it.q, (it.tile * N + col8(j) + 2 * t + e) / p.group, key0 - it.q.len);
 #pragma unroll
                             for (int x = 0; x < 4; ++x) {
-                                float pv[2];
-#pragma unroll
-                                for (int e = 0; e < 2; ++e) {
-                                    const float pe = ex2(__uint_as_float(s[j][x >> 1][2 * (x & 1) + e]));
-                                    l[j0 + j][e] += pe;
-                                    pv[e] = pe * vsc[x];
-                                    if (PLAIN || ((vis >> (8 * j + 4 * e + x)) & 1u)) ms[j0 + j][e] = fmaf(pe, vm[x], ms[j0 + j][e]);
-                                    else pv[e] = 0.f;                     // by selection: what a key holds stays out of rows that do not see it
-                                }
-                                const __half2 h2 = __floats2half2_rn(pv[0], pv[1]);
-                                h4[x] = *reinterpret_cast<const uint32_t*>(&h2);
+                                const bool ok = (w32 >> (8 * x)) & (groups >> (8 * quad + (x >> 1))) & 1u;
+                                if (ok) vis |= 1u << (8 * j + 4 * e + x);
+                                else sc[j][x][e] = -INFINITY;
+                                over = over || (col8(j) < cols && sc[j][x][e] > ((none >> (2 * j + e)) & 1u ? -INFINITY : RAISE));
                             }
-                            // lane's matrix row: key 32 quad + lane, query rows 8 blk .. 8 blk + 7
-                            stmatrix4(base_a + SH::P_AT + b * SH::P_BYTES + (blk >> 3) * (UNIT * 128) + (quad * 32 + lane) * 128 + (((blk & 7) ^ (lane & 7)) << 4), h4[0], h4[1], h4[2], h4[3]);
                         }
-                    };
-                    if (__builtin_expect(all && col8(j0 + JB - 1) < cols, 1)) weights(std::true_type{});
-                    else weights(std::false_type{});
                 }
-                tc_fence_before();
-                warp_arrive(smem_u32(&sm->s_empty[b]));
+                over = over || fmaxf(fmaxf(vs[0], vs[1]), fmaxf(vs[2], vs[3])) * vmul > 128.f;
+                // Where one of the 128 threads of these rows finds a score too far above (and in an item's first unit), they agree
+                // on new references.
+                if (__builtin_expect(part_any(part, over), 0)) {
+#pragma unroll
+                    for (int j = 0; j < NB; ++j)
+#pragma unroll
+                        for (int e = 0; e < 2; ++e) {
+                            float m = fmaxf(fmaxf(sc[j][0][e], sc[j][1][e]), fmaxf(sc[j][2][e], sc[j][3][e]));
+#pragma unroll
+                            for (int sh = 4; sh < 32; sh <<= 1) m = fmaxf(m, __shfl_xor_sync(0xffffffffu, m, sh));
+                            if (g == 0) sm->x[quad][col8(j) + 2 * t + e] = m;
+                        }
+                    float vx = 0.f;
+#pragma unroll
+                    for (int x = 0; x < 4; ++x) if (vs[x] <= 65504.f) vx = fmaxf(vx, vs[x]);
+#pragma unroll
+                    for (int sh = 4; sh < 32; sh <<= 1) vx = fmaxf(vx, __shfl_xor_sync(0xffffffffu, vx, sh));
+                    if (lane == 0) sm->vmax[part][quad] = vx;
+                    part_sync(part);
+                    vx = fmaxf(fmaxf(sm->vmax[part][0], sm->vmax[part][1]), fmaxf(sm->vmax[part][2], sm->vmax[part][3]));
+                    const float vnew = vx * vmul > 1.f ? exp2f(-ceilf(log2f(vx))) : vmul, fv = vnew / vmul;
+                    vmul = vnew;
+#pragma unroll
+                    for (int j = 0; j < NB; ++j)
+#pragma unroll
+                        for (int e = 0; e < 2; ++e) {
+                            const int rl = col8(j) + 2 * t + e;
+                            const bool had = !((none >> (2 * j + e)) & 1u);
+                            const float up = fmaxf(fmaxf(sm->x[0][rl], sm->x[1][rl]), fmaxf(sm->x[2][rl], sm->x[3][rl]));
+                            float f = 1.f;
+                            if (up > (had ? 0.f : -INFINITY)) {           // the new reference is `up` above the base
+                                f = had ? ex2(-up) : 0.f;
+                                none &= ~(1u << (2 * j + e));
+                                base[j][e] += up;
+                                l[j][e] *= f;
+                                ms[j][e] *= f;
+#pragma unroll
+                                for (int x = 0; x < 4; ++x) sc[j][x][e] -= up;
+                            }
+                            if (quad == 0 && g == 0) sm->fac[rl] = f * fv;
+                        }
+                    part_sync(part);
+                    if (k > 0) {
+                        // O^T holds the products of the units before once the last of them has completed (each P buffer's release
+                        // is waited for again two units later, so its phases are seen one by one)
+                        wait(smem_u32(&sm->p_empty[(i - 1) & 1]), ((i - 1) >> 1) & 1, abort_flag, w.status, DEV_TIMEOUT_EPI);
+                        tc_fence_after();
+#pragma unroll 1
+                        for (int j = 0; j < NB && col8(j) < cols; ++j) {  // this part's blocks of eight columns, both groups of 16 lanes
+                            const float2 f = *reinterpret_cast<const float2*>(&sm->fac[col8(j) + 2 * t]);
+                            const uint32_t to = tmem + SH::T_O + col8(j) + ((uint32_t)(quad * 32) << 16);
+                            uint32_t o[2][4];
+                            ld_frag(to, o[0]);
+                            ld_frag(to + (16u << 16), o[1]);
+                            ld_wait();
+#pragma unroll
+                            for (int h = 0; h < 2; ++h) {
+#pragma unroll
+                                for (int e = 0; e < 4; ++e) o[h][e] = __float_as_uint(__uint_as_float(o[h][e]) * ((e & 1) ? f.y : f.x));
+                                st_frag(to + ((uint32_t)(16 * h) << 16), o[h]);
+                            }
+                        }
+                        st_wait();
+                        tc_fence_before();
+                    }
+                    part_sync(part);                                      // the exchange buffers may be written again
+                }
+                const bool more = k + 1 < it.take;
+                if (more) fetch(i + 1);
+                if (i >= 2) wait(smem_u32(&sm->p_empty[b]), ((i >> 1) - 1) & 1, abort_flag, w.status, DEV_TIMEOUT_EPI);
+#pragma unroll
+                for (int x = 0; x < 4; ++x) vs[x] *= vmul;
+                // (one straight run of instructions for the units that matter, where nothing is masked and every block has rows)
+                auto weights = [&](auto plain) {
+                    constexpr bool PLAIN = decltype(plain)::value;
+#pragma unroll
+                    for (int j = 0; j < NB; ++j) {
+                        const int blk = col8(j) >> 3;
+                        if (!PLAIN && 8 * blk >= cols) break;
+                        uint32_t h4[4];
+#pragma unroll
+                        for (int x = 0; x < 4; ++x) {
+                            float pv[2];
+#pragma unroll
+                            for (int e = 0; e < 2; ++e) {
+                                const float pe = ex2(sc[j][x][e]);
+                                l[j][e] += pe;
+                                pv[e] = pe * vs[x];
+                                if (PLAIN || ((vis >> (8 * j + 4 * e + x)) & 1u)) ms[j][e] = fmaf(pe, vm[x], ms[j][e]);
+                                else pv[e] = 0.f;                         // by selection: what a key holds stays out of rows that do not see it
+                            }
+                            const __half2 h2 = __floats2half2_rn(pv[0], pv[1]);
+                            h4[x] = *reinterpret_cast<const uint32_t*>(&h2);
+                        }
+                        // lane's matrix row: key 32 quad + lane, query rows 8 blk .. 8 blk + 7
+                        stmatrix4(base_a + SH::P_AT + b * SH::P_BYTES + (quad * 32 + lane) * 128 + ((blk ^ (lane & 7)) << 4), h4[0], h4[1], h4[2], h4[3]);
+                    }
+                };
+                if (__builtin_expect(all && col8(NB - 1) < cols, 1)) weights(std::true_type{});
+                else weights(std::false_type{});
                 asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
+                tc_fence_before();
                 warp_arrive(smem_u32(&sm->p_full[b]));
+                if (more) fetched(i + 1);
             }
             // ---- sums of the rows over the four warps that share them
 #pragma unroll
-            for (int j = 0; j < NB; ++j) {
+            for (int j = 0; j < NB; ++j)
 #pragma unroll
                 for (int e = 0; e < 2; ++e) {
                     float a = l[j][e], c = ms[j][e];
 #pragma unroll
                     for (int o = 4; o < 32; o <<= 1) { a += __shfl_xor_sync(0xffffffffu, a, o); c += __shfl_xor_sync(0xffffffffu, c, o); }
                     const int rl = col8(j) + 2 * t + e;
-                    if (g == 0) { sm->x[quad][rl] = a; sm->y[quad][rl] = c; if (quad == 0) sm->fac[rl] = ref[j][e]; }
+                    if (g == 0) { sm->x[quad][rl] = a; sm->y[quad][rl] = c; if (quad == 0) sm->fac[rl] = (none >> (2 * j + e)) & 1u ? -INFINITY : base[j][e]; }
                 }
-            }
             named_sync<1, SOFT>();
-            if (tid < rows) {                                             // (sum of weights, minima's sum) of a row; qs has been read for the last time
+            if (tid < N) {
                 const float lsum = (sm->x[0][tid] + sm->x[1][tid]) + (sm->x[2][tid] + sm->x[3][tid]), mm = (sm->y[0][tid] + sm->y[1][tid]) + (sm->y[2][tid] + sm->y[3][tid]);
-                sm->tot[tid] = make_float2(lsum, mm);
+                sm->tot[tid] = make_float4(lsum, lsum == 0.f ? 0.f : 1.f / lsum, mm, 0.f);
             }
             named_sync<1, SOFT>();
             wait(smem_u32(&sm->p_empty[(i - 1) & 1]), ((i - 1) >> 1) & 1, abort_flag, w.status, DEV_TIMEOUT_EPI);
@@ -725,15 +711,16 @@ __global__ void __launch_bounds__(THREADS, 1) k_attn_kv4_tc(const __grid_constan
 #pragma unroll
                     for (int x = 0; x < 8; ++x) {
                         const int rl = r0 + x;
-                        if (rl >= rows) break;
-                        const float2 tm = sm->tot[rl];
-                        const float v = fmaf(__uint_as_float(o[x]), vinv, tm.y);
-                        if (whole) ((__half*)p.out)[(size_t)sm->rowix[rl] * D + chn] = __float2half_rn(tm.x == 0.f ? 0.f : v / tm.x);
-                        else __stcg(slot + (size_t)rl * D + chn, v);
+                        const float4 tm = sm->tot[rl];
+                        const float v = fmaf(__uint_as_float(o[x]), vinv, tm.z);
+                        if (rl < rows) {
+                            if (whole) ((__half*)p.out)[(size_t)sm->rowix[rl] * D + chn] = __float2half_rn(v * tm.y);
+                            else __stcg(slot + rl * D + chn, v);
+                        }
                     }
                 }
             }
-            if (!whole && tid < rows) __stcg(reinterpret_cast<float2*>(slot + (size_t)N * D + 2 * tid), make_float2(sm->fac[tid], sm->tot[tid].x));
+            if (!whole && tid < rows) __stcg(reinterpret_cast<float2*>(slot + N * D + 2 * tid), make_float2(sm->fac[tid], sm->tot[tid].x));
             tc_fence_before();                                            // O^T has been read: the next item's first product may write it
             if (!whole) {
                 __threadfence();
@@ -759,24 +746,23 @@ __global__ void __launch_bounds__(THREADS, 1) k_attn_kv4_tc(const __grid_constan
     }
 }
 
-template <int D, int N>
+template <int D>
 ghd_status launch_tc(ghd_ctx* c, Kv4AttnParams& p) {
-    if (cudaFuncSetAttribute(k_attn_kv4_tc<D, N>, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)smem_bytes<D, N>(p.w.n_seqs)) != cudaSuccess) {
+    if (cudaFuncSetAttribute(k_attn_kv4_tc<D>, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)smem_bytes<D>(p.w.n_seqs)) != cudaSuccess) {
         cudaGetLastError();
         return fail(c, GHD_ECUDA, "kv4_attention: cannot raise dynamic shared memory");
     }
     p.ctas = c->sm_count;
-    launch_k(c, false, k_attn_kv4_tc<D, N>, dim3(p.ctas), dim3(THREADS), smem_bytes<D, N>(p.w.n_seqs), p);
+    launch_k(c, false, k_attn_kv4_tc<D>, dim3(p.ctas), dim3(THREADS), smem_bytes<D>(p.w.n_seqs), p);
     return GHD_OK;
 }
 
 }  // namespace
 
-// partials: 2 slots of [tile_rows][d_head + 2] floats a CTA, within the tile scratch of 2 x 256 x 128 floats an SM
-ghd_status launch_attn_kv4_tc(ghd_ctx* c, Kv4AttnParams& p, int tile_rows) {
-    if (p.w.n_seqs > WIDE_SEQS) tile_rows = 64;
-    if (c->cfg.d_head == 64) return tile_rows == 64 ? launch_tc<64, 64>(c, p) : launch_tc<64, 128>(c, p);
-    return tile_rows == 64 ? launch_tc<128, 64>(c, p) : launch_tc<128, 128>(c, p);
+// partials: 2 slots of [64][d_head + 2] floats a CTA, within the tile scratch of 2 x 256 x 128 floats an SM
+ghd_status launch_attn_kv4_tc(ghd_ctx* c, Kv4AttnParams& p) {
+    return c->cfg.d_head == 64 ? launch_tc<64>(c, p) : launch_tc<128>(c, p);
 }
 
 }  // namespace ghd
+
