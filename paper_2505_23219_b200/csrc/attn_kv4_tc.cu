@@ -71,7 +71,8 @@ struct Ctrl {
     uint64_t c_full[CONV / 32][4];   // packed rows of a unit, by unpacking warp and stage
     uint64_t q_full, k_full[2], k_empty[2], v_full[2], v_empty[2], s_full[2], s_empty[2], p_full[2], p_empty[2], drain, drain_pv;
     uint32_t tmem_base;
-    int abort_flag, arrived;
+    uint32_t looks;                  // how often a wait looks before it gives up
+    int arrived;
     alignas(16) float qs[N];       // sums of the tile's queries
     alignas(16) float fac[N];      // factors of a rescale, by row
     float4 tot[N];                   // a row's sum of weights, its inverse, sum of weighted middles
@@ -127,25 +128,28 @@ __device__ __forceinline__ uint4 lds128(uint32_t addr) {
 __device__ __forceinline__ void sts128(uint32_t addr, const uint32_t* r) {
     asm volatile("st.shared.v4.u32 [%0], {%1, %2, %3, %4};" ::"r"(addr), "r"(r[0]), "r"(r[1]), "r"(r[2]), "r"(r[3]) : "memory");
 }
-// mbar_wait in few instructions (this kernel has many waits, and what it executes has to fit the instruction cache).  NAP:
-// nanoseconds between two looks, for warps that are ahead of what they wait for: polling takes issue slots from the
-// warps that work (it was 40 % of all instructions).
-constexpr uint32_t WAITS = 1u << 22;
+// mbar_wait in few instructions: what this kernel executes over and over has to fit the instruction cache.  A wait takes at
+// most *left looks (2^22, about a second); one that runs out sets it to 1, so that all later ones are short.  NAP:
+// nanoseconds between two looks, for warps that are ahead of what they wait for.
+constexpr uint32_t LOOKS = 1u << 22;
 template <int NAP = 0>
-__device__ __forceinline__ bool wait(uint32_t bar, uint32_t parity, volatile int* abort_flag, int* status, int code) {
-#pragma unroll 1
-    for (uint32_t spin = 0; spin < WAITS; ++spin) {
-        if (__builtin_expect(mbar_try(bar, parity), 1)) return true;
-        if (NAP > 0) __nanosleep(NAP);
-        if (__builtin_expect((spin & 31) == 31, 0)) { if (*abort_flag) return false; }
+__device__ __forceinline__ bool wait(uint32_t bar, uint32_t parity, volatile uint32_t* left, int* status, int code) {
+    uint32_t ok, n = *left;
+    if (NAP > 0)
+        asm volatile("{\n\t.reg .pred p, q;\n\tWAIT_%=:\n\tmbarrier.try_wait.parity.shared::cta.b64 p, [%2], %3;\n\t@p bra DONE_%=;\n\tnanosleep.u32 %4;\n\t"
+                     "sub.u32 %1, %1, 1;\n\tsetp.ne.u32 q, %1, 0;\n\t@q bra WAIT_%=;\n\tDONE_%=:\n\tselp.u32 %0, 1, 0, p;\n\t}" : "=r"(ok), "+r"(n) : "r"(bar), "r"(parity), "n"(NAP) : "memory");
+    else
+        asm volatile("{\n\t.reg .pred p, q;\n\tWAIT_%=:\n\tmbarrier.try_wait.parity.shared::cta.b64 p, [%2], %3;\n\t@p bra DONE_%=;\n\t"
+                     "sub.u32 %1, %1, 1;\n\tsetp.ne.u32 q, %1, 0;\n\t@q bra WAIT_%=;\n\tDONE_%=:\n\tselp.u32 %0, 1, 0, p;\n\t}" : "=r"(ok), "+r"(n) : "r"(bar), "r"(parity) : "memory");
+    if (__builtin_expect(!ok, 0)) {
+        *left = 1;
+        atomicCAS(status, DEV_OK, code);
     }
-    *abort_flag = 1;
-    atomicCAS(status, DEV_OK, code);
-    return false;
+    return ok != 0;
 }
 __device__ __forceinline__ void wait_drain(uint32_t bar, uint32_t parity) {
 #pragma unroll 1
-    for (uint32_t spin = 0; spin < WAITS && !mbar_try(bar, parity); ++spin) __nanosleep(64);
+    for (uint32_t spin = 0; spin < LOOKS && !mbar_try(bar, parity); ++spin) __nanosleep(64);
 }
 // One arrival for the whole warp: arrivals on one barrier are taken one by one, five cycles each.
 __device__ __forceinline__ void warp_arrive(uint32_t bar) {
@@ -197,7 +201,7 @@ __global__ void __launch_bounds__(THREADS, 1) k_attn_kv4_tc(const __grid_constan
         mbar_init(smem_u32(&sm->drain_pv), 1);
         for (int b = 0; b < 4 * (CONV / 32); ++b) mbar_init(smem_u32(&sm->c_full[b >> 2][b & 3]), 1);
         for (int b = 0; b < ITEMS; ++b) { mbar_init(smem_u32(&sm->item_full[b]), 1); mbar_init(smem_u32(&sm->item_empty[b]), CONV / 32 + 3); }      // unpacking warps, softmax, both issuers
-        sm->abort_flag = 0;
+        sm->looks = LOOKS;
         asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
     }
     if (warp == CW) {
@@ -210,13 +214,13 @@ __global__ void __launch_bounds__(THREADS, 1) k_attn_kv4_tc(const __grid_constan
     const int64_t units = unit_sums(w, til, sm->sums, sm->scratch);      // two block barriers inside
     tc_fence_after();
     const uint32_t tmem = sm->tmem_base;
-    volatile int* abort_flag = &sm->abort_flag;
+    volatile uint32_t* looks = &sm->looks;
     const int64_t per = kv4_units_per_cta(units, p.ctas);
     const int64_t u_beg = per * blockIdx.x, u_end = u_beg + per < units ? u_beg + per : units;
     // The k-th item of this CTA (take = 0: there are no more, or a wait has run out).  One thread looks; who takes it together
     // with others gets it from that thread, so that all of them go on or stop alike.
     auto item_get = [&](int k) -> Kv4Item {
-        if (!wait<20>(smem_u32(&sm->item_full[k % ITEMS]), (k / ITEMS) & 1, abort_flag, w.status, DEV_TIMEOUT_EPI)) { Kv4Item none{}; return none; }
+        if (!wait<20>(smem_u32(&sm->item_full[k % ITEMS]), (k / ITEMS) & 1, looks, w.status, DEV_TIMEOUT_EPI)) { Kv4Item none{}; return none; }
         const Kv4Item it = sm->item[k % ITEMS];
         mbar_arrive(smem_u32(&sm->item_empty[k % ITEMS]));
         return it;
@@ -288,77 +292,61 @@ __global__ void __launch_bounds__(THREADS, 1) k_attn_kv4_tc(const __grid_constan
             ++lch;
             ++n;
         };
-        auto landed = [&](int i) {
-            if (lane == 0) wait<40>(smem_u32(&sm->c_full[own][i % SH::STAGES]), (i / SH::STAGES) & 1, abort_flag, w.status, DEV_TIMEOUT_TMA);
-            __syncwarp();
-        };
 #pragma unroll 1
         for (int i = 0; i < SH::STAGES - 1; ++i) ask();
-        if (warp < SW + 4) {
-            // ------------------------------------------------ K: thread = key = tensor-memory lane
+        // K: thread = key = tensor-memory lane.  V: a lane takes one 16-byte piece of a row at a time; eight lanes read 128 bytes in
+        // a row, and their four stores go to eight different bank groups.
+        const int row0 = quad * 32 + lane / PIECES, c = lane % PIECES, turn = D == 128 ? (c >> 1) << 1 : 0;
+        constexpr int PER = 32 / PIECES;                                  // rows a step: a multiple of 8, so the swizzle of a lane's rows is one
+        const uint32_t from = which == 0 ? ring + lane * ROW : ring + (lane / PIECES) * ROW + 16 * c, step = which == 0 ? 16 : PER * ROW;
+        const uint32_t vt0 = base_a + SH::V_AT + (c >> 1) * V_SLAB + row0 * 128;
+        uint32_t off[4];
+#pragma unroll
+        for (int k = 0; k < 4; ++k) off[k] = (((c & 1) * 4 + (k ^ turn)) ^ (row0 & 7)) << 4;
+        // what the unpacked rows go to (a tensor-memory block, a V tile), when it is free and when it is full
+        const uint32_t empty = which == 0 ? smem_u32(&sm->k_empty[0]) : smem_u32(&sm->v_empty[0]), full = which == 0 ? smem_u32(&sm->k_full[0]) : smem_u32(&sm->v_full[0]);
 #pragma unroll 1
-            for (int i = 0; i < n; ++i) {                                 // (n runs ahead until the last unit has been asked for)
-                const int b = i & 1;
-                __syncwarp();                                             // everybody has read the stage that is filled next
-                ask();
-                landed(i);
-                const uint32_t st = base_a + SH::ST_AT + (uint32_t)(i % SH::STAGES) * SH::ST_BYTES + (quad * 32 + lane) * ROW;
-                if (i >= 2) wait<200>(smem_u32(&sm->k_empty[b]), ((i >> 1) - 1) & 1, abort_flag, w.status, DEV_TIMEOUT_TMEM);
-                tc_fence_after();
-                {
-                    const uint32_t at = pring + (uint32_t)(i % SH::STAGES) * SH::ST_BYTES + 4 * lane;
-                    uint32_t kr, vr;
-                    asm volatile("ld.shared.u32 %0, [%1];" : "=r"(kr) : "r"(at) : "memory");
-                    asm volatile("ld.shared.u32 %0, [%1];" : "=r"(vr) : "r"(at + 4 * UNIT) : "memory");
-                    const float2 kf = __half22float2(*reinterpret_cast<const __half2*>(&kr)), vf = __half22float2(*reinterpret_cast<const __half2*>(&vr));
-                    sm->par[i & (PAR_SLOTS - 1)][quad * 32 + lane] = make_float4(kf.x * sl2, fmaf(8.f, kf.x, kf.y) * sl2, vf.x, fmaf(8.f, vf.x, vf.y));
-                }
-                const uint32_t tk = tmem + SH::T_K + b * ROW + ((uint32_t)(quad * 32) << 16);
-                uint4 x = lds128(st);
+        for (int i = 0; i < n; ++i) {                                     // (n runs ahead until the last unit has been asked for)
+            const int b = i & 1, s_ = i % SH::STAGES;
+            __syncwarp();                                                 // everybody has read the stage that is filled next
+            ask();
+            wait<40>(smem_u32(&sm->c_full[own][s_]), (i / SH::STAGES) & 1, looks, w.status, DEV_TIMEOUT_TMA);
+            if (i >= 2) wait<100>(empty + 8 * b, ((i >> 1) - 1) & 1, looks, w.status, DEV_TIMEOUT_TMEM);
+            uint32_t st = from + s_ * SH::ST_BYTES;
+            uint4 x = lds128(st);
+            if (which == 0) {
+                const uint32_t at = pring + s_ * SH::ST_BYTES + 4 * lane;
+                uint32_t kr, vr;
+                asm volatile("ld.shared.u32 %0, [%1];" : "=r"(kr) : "r"(at) : "memory");
+                asm volatile("ld.shared.u32 %0, [%1];" : "=r"(vr) : "r"(at + 4 * UNIT) : "memory");
+                const float2 kf = __half22float2(*reinterpret_cast<const __half2*>(&kr)), vf = __half22float2(*reinterpret_cast<const __half2*>(&vr));
+                sm->par[i & (PAR_SLOTS - 1)][quad * 32 + lane] = make_float4(kf.x * sl2, fmaf(8.f, kf.x, kf.y) * sl2, vf.x, fmaf(8.f, vf.x, vf.y));
+            }
+            tc_fence_after();
+            uint32_t to = which == 0 ? tmem + SH::T_K + b * ROW + ((uint32_t)(quad * 32) << 16) : vt0 + b * SH::V_BYTES;
 #pragma unroll 1
-                for (int c = 0; c < PIECES; ++c) {
-                    uint32_t r[16];
-                    unpack8(x.x, r, magic); unpack8(x.y, r + 4, magic); unpack8(x.z, r + 8, magic); unpack8(x.w, r + 12, magic);
-                    if (c + 1 < PIECES) x = lds128(st + 16 * (c + 1));
-                    st16(tk + c * 16, r);
+            for (int j = 0; j < PIECES; ++j) {
+                uint32_t r[16];
+                const bool swap = which != 0 && turn != 0;
+                unpack8(swap ? x.z : x.x, r, magic); unpack8(swap ? x.w : x.y, r + 4, magic); unpack8(swap ? x.x : x.z, r + 8, magic); unpack8(swap ? x.y : x.w, r + 12, magic);
+                st += step;
+                if (j + 1 < PIECES) x = lds128(st);
+                if (which == 0) {
+                    st16(to, r);
+                    to += 16;
+                } else {
+#pragma unroll
+                    for (int k = 0; k < 4; ++k) sts128(to + off[k], r + 4 * k);
+                    to += PER * 128;
                 }
+            }
+            if (which == 0) {
                 st_wait();
                 tc_fence_before();
-                warp_arrive(smem_u32(&sm->k_full[b]));
-            }
-        } else {
-            // ------------------------------------------------ V: a lane takes one 16-byte piece of a row at a time; eight lanes read 128
-            // bytes in a row, and their four stores go to eight different bank groups
-            const int row0 = quad * 32 + lane / PIECES, c = lane % PIECES, turn = D == 128 ? (c >> 1) << 1 : 0;
-            constexpr int PER = 32 / PIECES;                              // rows a step: a multiple of 8, so the swizzle of a lane's rows is one
-            const uint32_t vt0 = base_a + SH::V_AT + (c >> 1) * V_SLAB + row0 * 128;
-            uint32_t off[4];
-#pragma unroll
-            for (int k = 0; k < 4; ++k) off[k] = (((c & 1) * 4 + (k ^ turn)) ^ (row0 & 7)) << 4;
-#pragma unroll 1
-            for (int i = 0; i < n; ++i) {                                 // (n runs ahead until the last unit has been asked for)
-                const int b = i & 1;
-                __syncwarp();                                             // everybody has read the stage that is filled next
-                ask();
-                landed(i);
-                const uint32_t st = base_a + SH::ST_AT + (uint32_t)(i % SH::STAGES) * SH::ST_BYTES + UNIT * ROW + row0 * ROW + 16 * c;
-                if (i >= 2) wait<100>(smem_u32(&sm->v_empty[b]), ((i >> 1) - 1) & 1, abort_flag, w.status, DEV_TIMEOUT_TMEM);
-                uint4 x = lds128(st);
-                uint32_t vt = vt0 + b * SH::V_BYTES;
-#pragma unroll 1
-                for (int j = 0; j < PIECES; ++j, vt += PER * 128) {
-                    const uint32_t wd[4] = {turn ? x.z : x.x, turn ? x.w : x.y, turn ? x.x : x.z, turn ? x.y : x.w};
-                    if (j + 1 < PIECES) x = lds128(st + (j + 1) * PER * ROW);
-#pragma unroll
-                    for (int k = 0; k < 4; ++k) {
-                        uint32_t r[4];
-                        unpack8(wd[k], r, magic);
-                        sts128(vt + off[k], r);
-                    }
-                }
+            } else {
                 asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
-                warp_arrive(smem_u32(&sm->v_full[b]));
             }
+            warp_arrive(full + 8 * b);
         }
         // no copy is in flight when the block ends, whatever the others have given up
         if (lane == 0)
@@ -377,13 +365,13 @@ __global__ void __launch_bounds__(THREADS, 1) k_attn_kv4_tc(const __grid_constan
                 const Kv4Item it = item_get(items);
                 if (it.take == 0) break;
                 const uint32_t idesc = instr_desc_f16(cols_of(rows_of(it)), false);
-                ok = wait(smem_u32(&sm->q_full), items & 1, abort_flag, w.status, DEV_TIMEOUT_MMA);
+                ok = wait(smem_u32(&sm->q_full), items & 1, looks, w.status, DEV_TIMEOUT_MMA);
                 ++items;
 #pragma unroll 1
                 for (int k = 0; ok && k < it.take; ++k, ++i) {
                     const int b = i & 1;
-                    ok = wait<30>(smem_u32(&sm->k_full[b]), (i >> 1) & 1, abort_flag, w.status, DEV_TIMEOUT_MMA);
-                    if (ok && i >= 2) ok = wait<30>(smem_u32(&sm->s_empty[b]), ((i >> 1) - 1) & 1, abort_flag, w.status, DEV_TIMEOUT_TMEM);
+                    ok = wait<30>(smem_u32(&sm->k_full[b]), (i >> 1) & 1, looks, w.status, DEV_TIMEOUT_MMA);
+                    if (ok && i >= 2) ok = wait<30>(smem_u32(&sm->s_empty[b]), ((i >> 1) - 1) & 1, looks, w.status, DEV_TIMEOUT_TMEM);
                     if (!ok) break;
                     tc_fence_after();
 #pragma unroll 1
@@ -415,8 +403,8 @@ __global__ void __launch_bounds__(THREADS, 1) k_attn_kv4_tc(const __grid_constan
 #pragma unroll 1
                 for (int k = 0; ok && k < it.take; ++k, ++i) {
                     const int b = i & 1;
-                    ok = wait<30>(smem_u32(&sm->v_full[b]), (i >> 1) & 1, abort_flag, w.status, DEV_TIMEOUT_MMA);
-                    if (ok) ok = wait<30>(smem_u32(&sm->p_full[b]), (i >> 1) & 1, abort_flag, w.status, DEV_TIMEOUT_MMA);
+                    ok = wait<30>(smem_u32(&sm->v_full[b]), (i >> 1) & 1, looks, w.status, DEV_TIMEOUT_MMA);
+                    if (ok) ok = wait<30>(smem_u32(&sm->p_full[b]), (i >> 1) & 1, looks, w.status, DEV_TIMEOUT_MMA);
                     if (!ok) break;
                     tc_fence_after();
 #pragma unroll 1
@@ -446,7 +434,7 @@ __global__ void __launch_bounds__(THREADS, 1) k_attn_kv4_tc(const __grid_constan
                     u = it.next;
                 }
                 if (it.take > 0) it.keys = kv4_tile_keys(til, it.q, it.tile);
-                if (k >= ITEMS) ok = wait<500>(smem_u32(&sm->item_empty[k % ITEMS]), ((k / ITEMS) - 1) & 1, abort_flag, w.status, DEV_TIMEOUT_EPI);
+                if (k >= ITEMS) ok = wait<500>(smem_u32(&sm->item_empty[k % ITEMS]), ((k / ITEMS) - 1) & 1, looks, w.status, DEV_TIMEOUT_EPI);
                 sm->item[k % ITEMS] = it;
                 mbar_arrive(smem_u32(&sm->item_full[k % ITEMS]));
                 ++k;
@@ -511,7 +499,7 @@ __global__ void __launch_bounds__(THREADS, 1) k_attn_kv4_tc(const __grid_constan
             uint32_t s[NB][2][4];
             auto fetch = [&](int u) {
                 const int b = u & 1;
-                wait(smem_u32(&sm->s_full[b]), (u >> 1) & 1, abort_flag, w.status, DEV_TIMEOUT_EPI);
+                wait(smem_u32(&sm->s_full[b]), (u >> 1) & 1, looks, w.status, DEV_TIMEOUT_EPI);
                 tc_fence_after();
                 const uint32_t ts = tmem + SH::T_S + b * N + ((uint32_t)(quad * 32) << 16);
 #pragma unroll
@@ -616,7 +604,7 @@ __global__ void __launch_bounds__(THREADS, 1) k_attn_kv4_tc(const __grid_constan
                     if (k > 0) {
                         // O^T holds the products of the units before once the last of them has completed (each P buffer's release
                         // is waited for again two units later, so its phases are seen one by one)
-                        wait(smem_u32(&sm->p_empty[(i - 1) & 1]), ((i - 1) >> 1) & 1, abort_flag, w.status, DEV_TIMEOUT_EPI);
+                        wait(smem_u32(&sm->p_empty[(i - 1) & 1]), ((i - 1) >> 1) & 1, looks, w.status, DEV_TIMEOUT_EPI);
                         tc_fence_after();
 #pragma unroll 1
                         for (int j = 0; j < NB && col8(j) < cols; ++j) {  // this part's blocks of eight columns, both groups of 16 lanes
@@ -640,7 +628,7 @@ __global__ void __launch_bounds__(THREADS, 1) k_attn_kv4_tc(const __grid_constan
                 }
                 const bool more = k + 1 < it.take;
                 if (more) fetch(i + 1);
-                if (i >= 2) wait(smem_u32(&sm->p_empty[b]), ((i >> 1) - 1) & 1, abort_flag, w.status, DEV_TIMEOUT_EPI);
+                if (i >= 2) wait(smem_u32(&sm->p_empty[b]), ((i >> 1) - 1) & 1, looks, w.status, DEV_TIMEOUT_EPI);
 #pragma unroll
                 for (int x = 0; x < 4; ++x) vs[x] *= vmul;
                 // (one straight run of instructions for the units that matter, where nothing is masked and every block has rows)
@@ -693,7 +681,7 @@ __global__ void __launch_bounds__(THREADS, 1) k_attn_kv4_tc(const __grid_constan
                 sm->tot[tid] = make_float4(lsum, lsum == 0.f ? 0.f : 1.f / lsum, mm, 0.f);
             }
             named_sync<1, SOFT>();
-            wait(smem_u32(&sm->p_empty[(i - 1) & 1]), ((i - 1) >> 1) & 1, abort_flag, w.status, DEV_TIMEOUT_EPI);
+            wait(smem_u32(&sm->p_empty[(i - 1) & 1]), ((i - 1) >> 1) & 1, looks, w.status, DEV_TIMEOUT_EPI);
             tc_fence_after();
             const int64_t c0 = it.first / per, c1 = (it.first + it.chunks - 1) / per;
             const bool whole = c0 == c1;
