@@ -8,7 +8,7 @@
 //
 // Keys are the M side of both products: S^T [16 keys x 8 rows] = K Q^T and O^T [16 channels x 8 rows] = V^T P^T
 // (mma.sync m16n8k16), so one to eight rows cost one n-tile.  The lanes' channels are permuted so that a lane's codes are
-// consecutive bytes of a row; nibbles become operands in registers.  A warp takes 16 keys of every chunk of 64 and keeps
+// consecutive bytes of a row; nibbles become operands in registers.  A warp takes 32 keys of every chunk of 128 and keeps
 // its own running reference (raised when a score exceeds it by 2^2: p * scale then fits half for every scale) and sums;
 // the warps meet in shared memory.
 //
@@ -26,9 +26,9 @@ namespace ghd {
 
 namespace {
 
-constexpr int WARPS = 4, CHUNK = 16 * WARPS;
+constexpr int WARPS = 4, WKEYS = 32, CHUNK = WKEYS * WARPS;      // a warp takes 32 keys of every chunk
 constexpr float RAISE = 2.f;
-constexpr int LEAD = 3;          // an item's fixed cost in chunks
+constexpr int LEAD = 2;          // an item's fixed cost in chunks
 
 using namespace kv4;
 
@@ -86,6 +86,20 @@ __device__ __forceinline__ uint32_t transpose8x8(uint32_t x) {
     return y;
 }
 
+// N consecutive values of a row in 16-byte loads (zeros for no row)
+template <typename T, int N>
+__device__ __forceinline__ void load_row(const T* src, float (&x)[N]) {
+    constexpr int E = 16 / (int)sizeof(T);
+#pragma unroll
+    for (int c = 0; c < N; c += E) {
+        uint4 v = make_uint4(0, 0, 0, 0);
+        if (src) v = __ldg(reinterpret_cast<const uint4*>(src + c));
+        const T* e = reinterpret_cast<const T*>(&v);
+#pragma unroll
+        for (int k = 0; k < E; ++k) x[c + k] = to_f<T>(e[k]);
+    }
+}
+
 // Key rows of a block of 16 in operand order: operand rows 2 t and 2 t + 1 (and + 8) are keys 2 t + (t & 1) and the other of
 // the pair, so that eight lanes reading K and sixteen reading V from shared memory meet different banks.
 __device__ __forceinline__ int key_of(int k) { return (k & ~1) | ((k ^ (k >> 1)) & 1); }
@@ -98,9 +112,9 @@ struct Narrow {
     static constexpr int MT = D / 16;                          // m-tiles of O^T
     static constexpr size_t SLOT = (size_t)RT * (D + 2);       // floats of a partial
     static constexpr int ES = (int)sizeof(T), ROW = D / 2;     // bytes of a scale, of a packed row
-    // a warp's stage: K rows, V rows, K params, V params of 16 keys, and whether their page is there
-    static constexpr int K_AT = 0, V_AT = 16 * ROW, KP_AT = 32 * ROW, VP_AT = KP_AT + 32 * ES, FLAG_AT = VP_AT + 32 * ES, STAGE = FLAG_AT + 16;
-    static constexpr int STAGES = sizeof(T) == 2 ? 5 : 4;
+    // a warp's stage: K rows, V rows, K and V (scale, min) of 32 keys, and which of the two groups of 16 have a page
+    static constexpr int V_AT = WKEYS * ROW, P_AT = 2 * WKEYS * ROW, VP_AT = P_AT + 2 * WKEYS * ES, FLAG_AT = VP_AT + 2 * WKEYS * ES, STAGE = FLAG_AT + 16;
+    static constexpr int STAGES = 3;
     static constexpr int XO = D + 4;                           // floats between rows of the exchange buffer
     static constexpr int SMEM = WARPS * STAGES * STAGE + WARPS * RT * (XO + 3) * 4 + WARPS * (D + 2) * 4;
     static constexpr int BLOCKS = NT == 1 && sizeof(T) == 2 ? (D == 64 ? 4 : 3) : 2;      // CTAs an SM
@@ -117,7 +131,7 @@ __global__ void __launch_bounds__(WARPS * 32, Narrow<T, D, NT>::BLOCKS) k_attn_k
     __shared__ int64_t scratch[32];
     __shared__ int arrived;
     float* xo = reinterpret_cast<float*>(smem + WARPS * N::STAGES * N::STAGE);       // [WARPS][RT][XO]
-    float* xm = xo + WARPS * RT * XO;                                                // reference, sum, minimum's sum: [WARPS][RT] each
+    float* xm = xo + WARPS * RT * XO;                                                // reference, sum, middles' sum: [WARPS][RT] each
     float* xl = xm + WARPS * RT;
     float* xs = xl + WARPS * RT;
     float* xmerge = xs + WARPS * RT;                                                 // [WARPS][D + 2]
@@ -129,41 +143,56 @@ __global__ void __launch_bounds__(WARPS * 32, Narrow<T, D, NT>::BLOCKS) k_attn_k
     const int64_t per = kv4_units_per_cta(units, p.ctas);
     int64_t u = per * blockIdx.x;
     const int64_t u_end = u + per < units ? u + per : units;
-    const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5, g = lane >> 2, t = lane & 3;
+    const int warp = __shfl_sync(0xffffffffu, (int)threadIdx.x >> 5, 0), lane = threadIdx.x & 31, g = lane >> 2, t = lane & 3;
     const int R = 1 << w.shift;
     const float sl2 = p.scale * KV4_LOG2E;
     const typename O_::Magic magic;
     auto item_at = [&](int64_t x) { Kv4Item r; find_item(&w, &til, sums, x, u_end, &r); return r; };
 
-    // ---- this warp's ring: 16 keys a stage, STAGES - 1 units ahead, over the borders of items
+    // ---- this warp's ring: 32 keys a stage, STAGES - 1 units ahead, over the borders of items
     uint8_t* ring = smem + warp * N::STAGES * N::STAGE;
     const uint32_t ring_a = (uint32_t)__cvta_generic_to_shared(ring);
     int64_t lu = u;
-    int lch = 0, lend = 0, lkeys = 0, lseq = 0, lhead = 0;
+    int lch = 0, lend = 0, lkeys = 0, lseq = 0, lhead = 0, pages = -1, pbase = 0;
+    // 16 rows are contiguous: lane's piece of them, and its place; lane (which, group, piece) of the scales
+    constexpr int PIECES = N::ROW / 16, PER = 32 / PIECES, PP = es * 2;              // pieces of a row, rows a warp-wide copy covers, pieces of 16 keys' scales
+    const uint32_t put = N::piece(lane / PIECES, lane % PIECES);
+    const int pwhich = lane / (2 * PP), pgrp = lane / PP & 1, pc = lane % PP;
+    const uint32_t pput = (pwhich ? N::VP_AT : N::P_AT) + pgrp * 32 * es + 16 * pc;
     auto load_next = [&](int i) {
         while (lch >= lend && lu < u_end) {
             const Kv4Item it = item_at(lu);
             lch = it.chunk0; lend = it.chunk0 + it.take; lkeys = kv4_tile_keys(til, it.q, it.tile); lseq = it.seq; lhead = it.head;
             lu = it.next;
+            pbase = lch - 16;
         }
         if (lch < lend) {
-            const int key0 = lch * CHUNK + warp * 16, r0 = key0 & (R - 1);
-            const int page = key0 < lkeys ? kv4_page(w, lseq, key0) : -1;
-            const uint8_t* blk = p.pool + kv4_block_at(w, page < 0 ? 0 : page, lhead);
+            if (lch >= pbase + 16) {                                                 // page ids of sixteen units: lane 2 u + h has unit pbase + u, keys 16 h on
+                const int key = (lch + (lane >> 1)) * CHUNK + warp * WKEYS + 16 * (lane & 1);
+                pbase = lch;
+                pages = lch + (lane >> 1) < lend && key < lkeys ? __ldg(w.table + (size_t)lseq * w.max_pages + (key >> w.shift)) : -1;
+                if ((unsigned)pages >= (unsigned)w.n_pages) {
+                    if (lch + (lane >> 1) < lend && key < lkeys) atomicCAS(w.status, DEV_OK, DEV_KV4_PAGE);
+                    pages = -1;                                                      // such keys are not visible
+                }
+            }
+            const int pg[2] = {__shfl_sync(0xffffffffu, pages, 2 * (lch - pbase)), __shfl_sync(0xffffffffu, pages, 2 * (lch - pbase) + 1)};
+            const int r0 = (lch * CHUNK + warp * WKEYS) & (R - 1);
             const uint32_t st = ring_a + (uint32_t)(i % N::STAGES) * N::STAGE;
-            constexpr int PIECES = N::ROW / 16, PER = 32 / PIECES;                   // pieces of a row, rows a warp-wide copy covers
 #pragma unroll
-            for (int j = 0; j < 16 / PER; ++j) {
-                const int r = lane / PIECES + PER * j, c = lane % PIECES;
-                cp16(st + N::K_AT + N::piece(r, c), blk + kv4_code_at(R, D, 0, r0 + r) + 16 * c, page >= 0);
-                cp16(st + N::V_AT + N::piece(r, c), blk + kv4_code_at(R, D, 1, r0 + r) + 16 * c, page >= 0);
+            for (int h = 0; h < 2; ++h) {
+                const uint8_t* src = p.pool + kv4_block_at(w, pg[h] < 0 ? 0 : pg[h], lhead) + (((r0 + 16 * h) & (R - 1)) * N::ROW + 16 * lane);
+#pragma unroll
+                for (int which = 0; which < 2; ++which)
+#pragma unroll
+                    for (int j = 0; j < 16 / PER; ++j)
+                        cp16(st + (which ? N::V_AT : 0) + h * 16 * N::ROW + j * 512 + put, src + which * R * N::ROW + j * 512, pg[h] >= 0);
             }
-            constexpr int PP = 2 * es;                                               // 16-byte pieces of 16 keys' scales and minima
-            if (lane < 2 * PP) {
-                const int which = lane / PP, c = lane % PP;
-                cp16(st + (which ? N::VP_AT : N::KP_AT) + 16 * c, blk + kv4_param_at(R, D, es, which, r0) + 16 * c, page >= 0);
+            if (lane < 4 * PP) {
+                const int page = pgrp ? pg[1] : pg[0];
+                cp16(st + pput, p.pool + kv4_block_at(w, page < 0 ? 0 : page, lhead) + kv4_param_at(R, D, es, pwhich, (r0 + 16 * pgrp) & (R - 1)) + 16 * pc, page >= 0);
             }
-            if (lane == 0) *reinterpret_cast<int*>(ring + (i % N::STAGES) * N::STAGE + N::FLAG_AT) = page >= 0;
+            if (lane == 0) *reinterpret_cast<int*>(ring + (i % N::STAGES) * N::STAGE + N::FLAG_AT) = (pg[0] >= 0 ? 1 : 0) | (pg[1] >= 0 ? 2 : 0);
             ++lch;
         }
         cp_commit();
@@ -171,13 +200,21 @@ __global__ void __launch_bounds__(WARPS * 32, Narrow<T, D, NT>::BLOCKS) k_attn_k
 #pragma unroll 1
     for (int i = 0; i < N::STAGES - 1; ++i) load_next(i);
 
+    const int ka = key_of(g);                                           // operand rows g and g + 8 of a block of 16 are its keys ka and ka + 8
+    const uint32_t kat = D == 128 ? N::piece(ka, t) : ka * 32 + 8 * t;
+    uint32_t vat[2];                                                    // of keys 2 t and 2 t + 1 in operand order; + 8 rows for the other two
+#pragma unroll
+    for (int e = 0; e < 2; ++e) {
+        const int r = key_of(2 * t + e);
+        vat[e] = N::V_AT + (D == 128 ? N::piece(r, g >> 1) + 8 * (g & 1) : r * 32 + 4 * g);
+    }
     int i = 0;                                                          // unit of this CTA
+#pragma unroll 1
     while (u < u_end) {
         const Kv4Item it = item_at(u);
         u = it.next;
         if (it.take == 0) continue;
         const int rows = min(RT, it.q.n * p.group - it.tile * RT);      // query rows of this tile
-        const int keys = kv4_tile_keys(til, it.q, it.tile);
 
         // ---- queries: lane (g, t) holds row 8 nt + g, channels [t D/4, (t + 1) D/4), pairs in the order the codes come in
         uint32_t bq[NT][KS][TERMS][2];
@@ -186,13 +223,7 @@ __global__ void __launch_bounds__(WARPS * 32, Narrow<T, D, NT>::BLOCKS) k_attn_k
         for (int nt = 0; nt < NT; ++nt) {
             const int rl = nt * 8 + g, rr = it.tile * RT + rl;
             float x[D / 4];
-#pragma unroll
-            for (int c = 0; c < D / 4; ++c) x[c] = 0.f;
-            if (rl < rows) {
-                const T* src = (const T*)p.q + ((size_t)(it.q.row0 + rr / p.group) * p.q_heads + it.head * p.group + rr % p.group) * D + t * (D / 4);
-#pragma unroll
-                for (int c = 0; c < D / 4; ++c) x[c] = to_f<T>(src[c]);
-            }
+            load_row<T, D / 4>(rl < rows ? (const T*)p.q + ((size_t)(it.q.row0 + rr / p.group) * p.q_heads + it.head * p.group + rr % p.group) * D + t * (D / 4) : nullptr, x);
             float sum = 0.f;
 #pragma unroll
             for (int c = 0; c < D / 4; ++c) sum += x[c];
@@ -211,42 +242,47 @@ __global__ void __launch_bounds__(WARPS * 32, Narrow<T, D, NT>::BLOCKS) k_attn_k
             }
         }
 
+        // base: what a row's scores are taken against, its reference, or 0 while it has none (its bit of `none`)
         float o[MT][NT][4];
-        float ref[NT][2], l[NT][2], ms[NT][2];
+        float base[NT][2], l[NT][2], ms[NT][2];
+        uint32_t none = (1u << 2 * NT) - 1u;
 #pragma unroll
         for (int nt = 0; nt < NT; ++nt) {
 #pragma unroll
-            for (int e = 0; e < 2; ++e) { ref[nt][e] = -INFINITY; l[nt][e] = 0.f; ms[nt][e] = 0.f; }
+            for (int e = 0; e < 2; ++e) { base[nt][e] = 0.f; l[nt][e] = 0.f; ms[nt][e] = 0.f; }
 #pragma unroll
             for (int mt = 0; mt < MT; ++mt)
 #pragma unroll
                 for (int e = 0; e < 4; ++e) o[mt][nt][e] = 0.f;
         }
 
+#pragma unroll 1
         for (int ch = it.chunk0; ch < it.chunk0 + it.take; ++ch, ++i) {
             __syncwarp();                                               // everybody has read the stage that is filled next
             load_next(i + N::STAGES - 1);
             cp_wait<N::STAGES - 1>();
             __syncwarp();
             const uint8_t* st = ring + (i % N::STAGES) * N::STAGE;
-            const int key0 = ch * CHUNK + warp * 16;
-            if (key0 >= keys || !*reinterpret_cast<const int*>(st + N::FLAG_AT)) continue;      // keys of an unknown page are not visible
-            const int ka = key_of(g);                                   // operand rows g and g + 8 are keys ka and ka + 8
-            const float2 kp0 = param_of<T>(st + N::KP_AT, ka), kp1 = param_of<T>(st + N::KP_AT, ka + 8);
+            const int key0 = ch * CHUNK + warp * WKEYS;
+            const int there = *reinterpret_cast<const int*>(st + N::FLAG_AT);
+            if (there == 0) continue;
+            const bool all = key0 + WKEYS <= it.q.len && there == 3;   // every key is visible to every row
 
-            float s[NT][4];
+            float s[2][NT][4];                                          // block z: key ka rows 2 t, 2 t + 1, then key ka + 8
 #pragma unroll
-            for (int nt = 0; nt < NT; ++nt)
+            for (int z = 0; z < 2; ++z) {
 #pragma unroll
-                for (int e = 0; e < 4; ++e) s[nt][e] = 0.f;
-            {
+                for (int nt = 0; nt < NT; ++nt)
+#pragma unroll
+                    for (int e = 0; e < 4; ++e) s[z][nt][e] = 0.f;
                 uint32_t k0[KW], k1[KW];
+                const uint8_t* kp = st + z * 16 * N::ROW + kat;
                 if constexpr (D == 128) {
-                    const uint4 x = *reinterpret_cast<const uint4*>(st + N::K_AT + N::piece(ka, t)), y = *reinterpret_cast<const uint4*>(st + N::K_AT + N::piece(ka + 8, t));
+                    const uint4 x = *reinterpret_cast<const uint4*>(kp), y = *reinterpret_cast<const uint4*>(kp + 8 * N::ROW);
                     k0[0] = x.x; k0[1] = x.y; k0[2] = x.z; k0[3] = x.w;
                     k1[0] = y.x; k1[1] = y.y; k1[2] = y.z; k1[3] = y.w;
                 } else {
-                    const uint2 x = *reinterpret_cast<const uint2*>(st + N::K_AT + ka * 32 + 8 * t), y = *reinterpret_cast<const uint2*>(st + N::K_AT + (ka + 8) * 32 + 8 * t);
+                    const uint2 x = *reinterpret_cast<const uint2*>(kp), y = *reinterpret_cast<const uint2*>(kp + 8 * N::ROW);
                     k0[0] = x.x; k0[1] = x.y;
                     k1[0] = y.x; k1[1] = y.y;
                 }
@@ -260,113 +296,125 @@ __global__ void __launch_bounds__(WARPS * 32, Narrow<T, D, NT>::BLOCKS) k_attn_k
 #pragma unroll
                         for (int nt = 0; nt < NT; ++nt)
 #pragma unroll
-                            for (int e = 0; e < TERMS; ++e) O_::mma(s[nt], a0, a1, a2, a3, bq[nt][2 * j + hlf][e][0], bq[nt][2 * j + hlf][e][1]);
+                            for (int e = 0; e < TERMS; ++e) O_::mma(s[z][nt], a0, a1, a2, a3, bq[nt][2 * j + hlf][e][0], bq[nt][2 * j + hlf][e][1]);
                     }
                 }
             }
-            // scores (in powers of two): key g rows 2 t, 2 t + 1, then key g + 8; a pair of rows shares its key's scale
-            const float ks0 = kp0.x * sl2, ks1 = kp1.x * sl2, km0 = fmaf(8.f, kp0.x, kp0.y) * sl2, km1 = fmaf(8.f, kp1.x, kp1.y) * sl2;
+            // scores in powers of two, less the base
+            bool over = ch == it.chunk0;
 #pragma unroll
-            for (int nt = 0; nt < NT; ++nt)
+            for (int z = 0; z < 2; ++z)
 #pragma unroll
-                for (int e = 0; e < 4; ++e) s[nt][e] = e < 2 ? fmaf(ks0, s[nt][e], km0 * qs[nt][e & 1]) : fmaf(ks1, s[nt][e], km1 * qs[nt][e & 1]);
-            const bool all = key0 + 16 <= it.q.len;
-            uint32_t vis = 0xffffffffu;
-            if (!all) {
+                for (int h = 0; h < 2; ++h) {
+                    const float2 kp = param_of<T>(st + N::P_AT, 16 * z + ka + 8 * h);
+                    const float ks = kp.x * sl2, km = fmaf(8.f, kp.x, kp.y) * sl2;
+#pragma unroll
+                    for (int nt = 0; nt < NT; ++nt)
+#pragma unroll
+                        for (int e = 0; e < 2; ++e) {
+                            float& v = s[z][nt][2 * h + e];
+                            v = fmaf(ks, v, fmaf(km, qs[nt][e], -base[nt][e]));
+                            over = over || v > RAISE;
+                        }
+                }
+            uint32_t vis = 0xffffffffu;                                 // bit 8 nt + 4 z + e: score s[z][nt][e] counts
+            if (__builtin_expect(!all, 0)) {
                 vis = 0u;
+                over = ch == it.chunk0;
 #pragma unroll
                 for (int nt = 0; nt < NT; ++nt)
 #pragma unroll
                     for (int e = 0; e < 2; ++e) {
                         const uint32_t b = sees(p, it.q, (it.tile * RT + nt * 8 + 2 * t + e) / p.group, key0 + ka - it.q.len);
-                        vis |= ((b & 1u) << (4 * nt + e)) | (((b >> 8) & 1u) << (4 * nt + e + 2));
+#pragma unroll
+                        for (int z = 0; z < 2; ++z)
+#pragma unroll
+                            for (int h = 0; h < 2; ++h) {
+                                float& v = s[z][nt][2 * h + e];
+                                if ((b >> (16 * z + 8 * h)) & (there >> z) & 1u) vis |= 1u << (8 * nt + 4 * z + 2 * h + e);
+                                else v = -INFINITY;
+                                over = over || v > ((none >> (2 * nt + e)) & 1u ? -INFINITY : RAISE);
+                            }
                     }
-#pragma unroll
-                for (int nt = 0; nt < NT; ++nt)
-#pragma unroll
-                    for (int e = 0; e < 4; ++e)
-                        if (!((vis >> (4 * nt + e)) & 1u)) s[nt][e] = -INFINITY;
             }
-            bool over = false;
-#pragma unroll
-            for (int nt = 0; nt < NT; ++nt)
-#pragma unroll
-                for (int e = 0; e < 2; ++e) over = over || (fmaxf(s[nt][e], s[nt][e + 2]) - ref[nt][e] > RAISE);
             if (__any_sync(0xffffffffu, over)) {
 #pragma unroll
                 for (int nt = 0; nt < NT; ++nt)
 #pragma unroll
                     for (int e = 0; e < 2; ++e) {
-                        float mx = fmaxf(s[nt][e], s[nt][e + 2]);
-                        mx = fmaxf(mx, __shfl_xor_sync(0xffffffffu, mx, 4));
-                        mx = fmaxf(mx, __shfl_xor_sync(0xffffffffu, mx, 8));
-                        mx = fmaxf(mx, __shfl_xor_sync(0xffffffffu, mx, 16));
-                        if (mx > ref[nt][e]) {
-                            const float f = ex2(ref[nt][e] - mx);       // 0 from a reference of -infinity
-                            ref[nt][e] = mx;
+                        float up = fmaxf(fmaxf(s[0][nt][e], s[0][nt][e + 2]), fmaxf(s[1][nt][e], s[1][nt][e + 2]));
+                        up = fmaxf(up, __shfl_xor_sync(0xffffffffu, up, 4));
+                        up = fmaxf(up, __shfl_xor_sync(0xffffffffu, up, 8));
+                        up = fmaxf(up, __shfl_xor_sync(0xffffffffu, up, 16));
+                        const bool had = !((none >> (2 * nt + e)) & 1u);
+                        if (up > (had ? 0.f : -INFINITY)) {             // the new reference is `up` above the base
+                            const float f = had ? ex2(-up) : 0.f;
+                            none &= ~(1u << (2 * nt + e));
+                            base[nt][e] += up;
                             l[nt][e] *= f;
                             ms[nt][e] *= f;
+#pragma unroll
+                            for (int z = 0; z < 2; ++z) { s[z][nt][e] -= up; s[z][nt][e + 2] -= up; }
 #pragma unroll
                             for (int mt = 0; mt < MT; ++mt) { o[mt][nt][e] *= f; o[mt][nt][e + 2] *= f; }
                         }
                     }
             }
-            uint32_t bp[NT][TERMS][2];
-            const float2 vp0 = param_of<T>(st + N::VP_AT, ka), vp1 = param_of<T>(st + N::VP_AT, ka + 8);
-            const float vm0 = fmaf(8.f, vp0.x, vp0.y), vm1 = fmaf(8.f, vp1.x, vp1.y);
+            uint32_t bp[2][NT][TERMS][2];
 #pragma unroll
-            for (int nt = 0; nt < NT; ++nt) {
-                float ps[4], pm[4];
+            for (int z = 0; z < 2; ++z) {
+                const float2 vp0 = param_of<T>(st + N::VP_AT, 16 * z + ka), vp1 = param_of<T>(st + N::VP_AT, 16 * z + ka + 8);
+                const float vm0 = fmaf(8.f, vp0.x, vp0.y), vm1 = fmaf(8.f, vp1.x, vp1.y);
 #pragma unroll
-                for (int e = 0; e < 4; ++e) {
-                    const float rf = ref[nt][e & 1];
-                    const float pe = ex2(s[nt][e] - (rf == -INFINITY ? 0.f : rf));
-                    l[nt][e & 1] += pe;
-                    ps[e] = pe * (e < 2 ? vp0.x : vp1.x);
-                    pm[e] = pe * (e < 2 ? vm0 : vm1);
+                for (int nt = 0; nt < NT; ++nt) {
+                    float ps[4];
+#pragma unroll
+                    for (int e = 0; e < 4; ++e) {
+                        const float pe = ex2(s[z][nt][e]);
+                        l[nt][e & 1] += pe;
+                        ps[e] = pe * (e < 2 ? vp0.x : vp1.x);
+                        if (__builtin_expect(all, 1) || ((vis >> (8 * nt + 4 * z + e)) & 1u)) ms[nt][e & 1] = fmaf(pe, e < 2 ? vm0 : vm1, ms[nt][e & 1]);
+                        else ps[e] = 0.f;                               // by selection: what a key holds stays out of rows that do not see it
+                    }
+                    uint32_t x[TERMS], y[TERMS];
+                    O_::split(ps[0], ps[1], x);
+                    O_::split(ps[2], ps[3], y);
+#pragma unroll
+                    for (int e = 0; e < TERMS; ++e) { bp[z][nt][e][0] = transpose8x8(x[e]); bp[z][nt][e][1] = transpose8x8(y[e]); }
                 }
-                if (!all) {                                             // by selection: what a key holds stays out of rows that do not see it
-#pragma unroll
-                    for (int e = 0; e < 4; ++e)
-                        if (!((vis >> (4 * nt + e)) & 1u)) ps[e] = pm[e] = 0.f;
-                }
-                ms[nt][0] += pm[0] + pm[2];
-                ms[nt][1] += pm[1] + pm[3];
-                uint32_t x[TERMS], y[TERMS];
-                O_::split(ps[0], ps[1], x);
-                O_::split(ps[2], ps[3], y);
-#pragma unroll
-                for (int e = 0; e < TERMS; ++e) { bp[nt][e][0] = transpose8x8(x[e]); bp[nt][e][1] = transpose8x8(y[e]); }
             }
             // O^T: m-tile mt holds the lane's channels 2 mt (operand row g) and 2 mt + 1 (row g + 8) of the D/8 from g D/8 on
-            uint32_t v[4][VW];
 #pragma unroll
-            for (int e = 0; e < 4; ++e) {
-                const int r = key_of(2 * t + (e & 1)) + 8 * (e >> 1);
-                if constexpr (D == 128) {
-                    const uint2 x = *reinterpret_cast<const uint2*>(st + N::V_AT + N::piece(r, g >> 1) + 8 * (g & 1));
-                    v[e][0] = x.x; v[e][1] = x.y;
-                } else {
-                    v[e][0] = *reinterpret_cast<const uint32_t*>(st + N::V_AT + r * 32 + 4 * g);
-                }
-            }
+            for (int z = 0; z < 2; ++z) {
+                uint32_t v[4][VW];
 #pragma unroll
-            for (int j = 0; j < VW; ++j)
-#pragma unroll
-                for (int z = 0; z < 2; ++z) {                           // half words of the two keys of a pair side by side
-                    const uint32_t x = __byte_perm(v[0][j], v[1][j], z ? 0x7632 : 0x5410), y = __byte_perm(v[2][j], v[3][j], z ? 0x7632 : 0x5410);
-#pragma unroll
-                    for (int hlf = 0; hlf < 2; ++hlf) {
-                        const uint32_t xs_ = x >> (8 * hlf), ys_ = y >> (8 * hlf);
-                        const uint32_t a0 = O_::template centred<0>(xs_, magic), a1 = O_::template centred<4>(xs_, magic);
-                        const uint32_t a2 = O_::template centred<0>(ys_, magic), a3 = O_::template centred<4>(ys_, magic);
-                        const int mt = 4 * j + 2 * z + hlf;
-#pragma unroll
-                        for (int nt = 0; nt < NT; ++nt)
-#pragma unroll
-                            for (int e = 0; e < TERMS; ++e) O_::mma(o[mt][nt], a0, a1, a2, a3, bp[nt][e][0], bp[nt][e][1]);
+                for (int e = 0; e < 4; ++e) {
+                    const uint8_t* vp = st + z * 16 * N::ROW + vat[e & 1] + (e >> 1) * 8 * N::ROW;
+                    if constexpr (D == 128) {
+                        const uint2 x = *reinterpret_cast<const uint2*>(vp);
+                        v[e][0] = x.x; v[e][1] = x.y;
+                    } else {
+                        v[e][0] = *reinterpret_cast<const uint32_t*>(vp);
                     }
                 }
+#pragma unroll
+                for (int j = 0; j < VW; ++j)
+#pragma unroll
+                    for (int y = 0; y < 2; ++y) {                       // half words of the two keys of a pair side by side
+                        const uint32_t a = __byte_perm(v[0][j], v[1][j], y ? 0x7632 : 0x5410), b = __byte_perm(v[2][j], v[3][j], y ? 0x7632 : 0x5410);
+#pragma unroll
+                        for (int hlf = 0; hlf < 2; ++hlf) {
+                            const uint32_t as = a >> (8 * hlf), bs = b >> (8 * hlf);
+                            const uint32_t a0 = O_::template centred<0>(as, magic), a1 = O_::template centred<4>(as, magic);
+                            const uint32_t a2 = O_::template centred<0>(bs, magic), a3 = O_::template centred<4>(bs, magic);
+                            const int mt = 4 * j + 2 * y + hlf;
+#pragma unroll
+                            for (int nt = 0; nt < NT; ++nt)
+#pragma unroll
+                                for (int e = 0; e < TERMS; ++e) O_::mma(o[mt][nt], a0, a1, a2, a3, bp[z][nt][e][0], bp[z][nt][e][1]);
+                        }
+                    }
+            }
         }
 
         // ---- the warps' sums meet
@@ -379,7 +427,7 @@ __global__ void __launch_bounds__(WARPS * 32, Narrow<T, D, NT>::BLOCKS) k_attn_k
                 for (int x = 4; x < 32; x <<= 1) { a += __shfl_xor_sync(0xffffffffu, a, x); b += __shfl_xor_sync(0xffffffffu, b, x); }
                 const int rl = nt * 8 + 2 * t + e;
                 if (rl >= rows) continue;
-                if (g == 0) { xm[warp * RT + rl] = ref[nt][e]; xl[warp * RT + rl] = a; xs[warp * RT + rl] = b; }
+                if (g == 0) { xm[warp * RT + rl] = (none >> (2 * nt + e)) & 1u ? -INFINITY : base[nt][e]; xl[warp * RT + rl] = a; xs[warp * RT + rl] = b; }
 #pragma unroll
                 for (int mt = 0; mt < MT; mt += 2)
                     *reinterpret_cast<float4*>(xo + (warp * RT + rl) * XO + g * (D / 8) + 2 * mt) = make_float4(o[mt][nt][e], o[mt][nt][e + 2], o[mt + 1][nt][e], o[mt + 1][nt][e + 2]);
@@ -388,6 +436,7 @@ __global__ void __launch_bounds__(WARPS * 32, Narrow<T, D, NT>::BLOCKS) k_attn_k
         const int64_t c0 = it.first / per, c1 = (it.first + it.chunks - 1) / per;      // CTAs that share the item
         const bool whole = c0 == c1;
         float* slot = p.part + ((size_t)blockIdx.x * 2 + ((int64_t)blockIdx.x == c0 ? 1 : 0)) * N::SLOT;
+#pragma unroll 1
         for (int x = threadIdx.x; x < rows * (D / 4); x += WARPS * 32) {
             const int rl = x / (D / 4), c = 4 * (x % (D / 4));
             float m = xm[rl];
@@ -398,8 +447,7 @@ __global__ void __launch_bounds__(WARPS * 32, Narrow<T, D, NT>::BLOCKS) k_attn_k
 #pragma unroll
             for (int k = 0; k < WARPS; ++k) {
                 const int at = k * RT + rl;
-                if (xm[at] == -INFINITY && xl[at] == 0.f) continue;      // a warp that saw nothing (a NaN goes on)
-                const float f = ex2(xm[at] - m), mm = xs[at];
+                const float f = xm[at] == -INFINITY && xl[at] == 0.f ? 0.f : ex2(xm[at] - m), mm = xs[at];      // (saw nothing: 0; a NaN goes on)
                 const float4 b = *reinterpret_cast<const float4*>(xo + at * XO + c);
                 a.x += f * (b.x + mm); a.y += f * (b.y + mm); a.z += f * (b.z + mm); a.w += f * (b.w + mm);
                 lsum += f * xl[at];
