@@ -19,158 +19,283 @@ template <> __device__ __forceinline__ __half from_f<__half>(float v) { return _
 struct RopeFreq { double f[64]; };
 
 // min and max that keep a NaN (fminf and fmaxf drop it)
-__device__ __forceinline__ float min_nan(float a, float b) { return (a != a) ? a : ((b != b) ? b : fminf(a, b)); }
-__device__ __forceinline__ float max_nan(float a, float b) { return (a != a) ? a : ((b != b) ? b : fmaxf(a, b)); }
+__device__ __forceinline__ float min_nan(float a, float b) { float r; asm("min.NaN.f32 %0, %1, %2;" : "=f"(r) : "f"(a), "f"(b)); return r; }
+__device__ __forceinline__ float max_nan(float a, float b) { float r; asm("max.NaN.f32 %0, %1, %2;" : "=f"(r) : "f"(a), "f"(b)); return r; }
 
-// Scale and minimum of a row whose D values a warp holds, D / 32 a lane.
-template <typename T, int N>
-__device__ __forceinline__ void row_params(const float (&x)[N], T& scale, T& mn) {
-    float lo = x[0], hi = x[0];
+// 8 consecutive values, 16-byte aligned, as they come and as floats
+template <typename T> struct Raw8 { uint4 u[sizeof(T) / 2]; };
+template <typename T> __device__ __forceinline__ Raw8<T> load8(const T* p) {
+    Raw8<T> r;
 #pragma unroll
-    for (int i = 1; i < N; ++i) { lo = min_nan(lo, x[i]); hi = max_nan(hi, x[i]); }
-    for (int o = 16; o > 0; o >>= 1) {
-        lo = min_nan(lo, __shfl_xor_sync(0xffffffffu, lo, o));
-        hi = max_nan(hi, __shfl_xor_sync(0xffffffffu, hi, o));
+    for (int i = 0; i < (int)sizeof(T) / 2; ++i) r.u[i] = reinterpret_cast<const uint4*>(p)[i];
+    return r;
+}
+template <typename T> __device__ __forceinline__ void floats(const Raw8<T>& r, float (&x)[8]);
+template <> __device__ __forceinline__ void floats<float>(const Raw8<float>& w, float (&x)[8]) {
+#pragma unroll
+    for (int i = 0; i < 2; ++i) {
+        x[4 * i] = __uint_as_float(w.u[i].x); x[4 * i + 1] = __uint_as_float(w.u[i].y);
+        x[4 * i + 2] = __uint_as_float(w.u[i].z); x[4 * i + 3] = __uint_as_float(w.u[i].w);
     }
-    mn = from_f<T>(lo);
-    scale = from_f<T>((float)(((double)hi - (double)lo) / 15.0));
+}
+template <> __device__ __forceinline__ void floats<__half>(const Raw8<__half>& w, float (&x)[8]) {
+    const uint32_t r[4] = {w.u[0].x, w.u[0].y, w.u[0].z, w.u[0].w};
+#pragma unroll
+    for (int e = 0; e < 4; ++e) {
+        const float2 f = __half22float2(*reinterpret_cast<const __half2*>(&r[e]));
+        x[2 * e] = f.x;
+        x[2 * e + 1] = f.y;
+    }
+}
+template <typename T> __device__ __forceinline__ void store8(T* p, const float (&x)[8]);
+template <> __device__ __forceinline__ void store8<float>(float* p, const float (&x)[8]) {
+    *reinterpret_cast<float4*>(p) = make_float4(x[0], x[1], x[2], x[3]);
+    *reinterpret_cast<float4*>(p + 4) = make_float4(x[4], x[5], x[6], x[7]);
+}
+template <> __device__ __forceinline__ void store8<__half>(__half* p, const float (&x)[8]) {
+    uint32_t r[4];
+#pragma unroll
+    for (int e = 0; e < 4; ++e) {
+        const __half2 h = __floats2half2_rn(x[2 * e], x[2 * e + 1]);
+        r[e] = *reinterpret_cast<const uint32_t*>(&h);
+    }
+    *reinterpret_cast<uint4*>(p) = make_uint4(r[0], r[1], r[2], r[3]);
+}
+template <typename T> __device__ __forceinline__ float2 load_pair(const uint8_t* p);
+template <> __device__ __forceinline__ float2 load_pair<float>(const uint8_t* p) { return *reinterpret_cast<const float2*>(p); }
+template <> __device__ __forceinline__ float2 load_pair<__half>(const uint8_t* p) { return __half22float2(*reinterpret_cast<const __half2*>(p)); }
+
+// Codes of 16 values, x[0 .. 7] in c[0] from the low end.  The quotient decides between two codes, so it is taken in 64 bits
+// where 32 could fall on the other side of a half: 32-bit subtraction and multiplication by a reciprocal are off by less
+// than 2^-20 of the quotient (three roundings of 2^-24 and the reciprocal's own), which is below 16; where one of the 16 is
+// nearer than 2^-15 to a half (or the reciprocal is none) they are redone.  Adding 1.5 * 2^23 rounds to a whole number, ties to
+// even, and leaves it in the low bits.
+__device__ __forceinline__ void codes_of(const float (&x)[16], float mn, float scale, uint32_t (&c)[2]) {
+    constexpr float MAGIC = 12582912.f;                             // bits 0x4b400000
+    const float inv = scale == 0.f ? 0.f : 1.f / scale;
+    float far = 0.f;
+    c[0] = c[1] = 0u;
+#pragma unroll
+    for (int i = 0; i < 16; ++i) {
+        const float t = fminf(fmaxf((x[i] - mn) * inv, 0.f), 15.f);
+        const float r = t + MAGIC;
+        far = fmaxf(far, fabsf(t - (r - MAGIC)));
+        c[i >> 3] += (__float_as_uint(r) - 0x4b400000u) << (4 * (i & 7));
+    }
+    if (far > 0.5f - 0x1p-15f || !(inv < INFINITY)) {
+        c[0] = c[1] = 0u;
+#pragma unroll 1
+        for (int i = 0; i < 16; ++i) {
+            float y = x[0];
+#pragma unroll
+            for (int k = 1; k < 16; ++k) if (k == i) y = x[k];
+            const float r = fminf(fmaxf((float)rint(((double)y - (double)mn) / (double)scale), 0.f), 15.f);
+            c[i >> 3] |= (uint32_t)r << (4 * (i & 7));
+        }
+    }
 }
 
-// Code of x.  The quotient decides between two codes, so it is taken in 64 bits where 32 could fall on the other
-// side of a half: 32-bit subtraction and multiplication by a reciprocal are off by less than 2^-20 of the quotient
-// (three roundings of 2^-24 and the reciprocal's own), which is below 16; nearer than 2^-15 to a half is redone.
-__device__ __forceinline__ uint32_t code_of(float x, float mn, float scale, float inv) {
-    if (scale == 0.f) return 0u;
-    const float t = (x - mn) * inv;
-    float r = rintf(t);
-    if (!(fabsf(fabsf(t - r) - 0.5f) > 0x1p-15f) || !(fabsf(t) < 32.f)) r = (float)rint(((double)x - (double)mn) / (double)scale);
-    r = fminf(fmaxf(r, 0.f), 15.f);
-    return (uint32_t)r;
+// Rows of the call that one warp works through, and their sequence: found by the lanes together when a row leaves the
+// sequence of the one before.
+struct RowOwner {
+    int seq, end;       // -1: nobody's; rows up to `end` (excluded) have the same answer
+    Kv4Seq q;
+};
+__device__ __forceinline__ void find_owner(const Kv4View& w, int row, bool lengths, RowOwner& o) {      // lengths: the rows go behind kv_len
+    const int lane = threadIdx.x & 31;
+    int seq = -1;
+    for (int s0 = 0; s0 < w.n_seqs && seq < 0; s0 += 32) {
+        const int s = s0 + lane;
+        const bool mine = s < w.n_seqs && __ldg(w.row_start + s) <= row && row < __ldg(w.row_start + s + 1);
+        const uint32_t b = __ballot_sync(0xffffffffu, mine);
+        if (b) seq = s0 + __ffs(b) - 1;
+    }
+    o.seq = seq;
+    o.end = row + 1;
+    if (seq >= 0) {
+        o.q = lengths ? kv4_load_seq(w, seq) : kv4_seq(__ldg(w.row_start + seq), __ldg(w.row_start + seq + 1), w.n_rows, 0, 0x7fffffffll);
+        if (o.q.bad && lane == 0) atomicCAS(w.status, DEV_OK, DEV_KV4_ROWS);
+        if (row < o.q.row0 || row >= o.q.row0 + o.q.n) o.seq = -1;      // starts out of order
+        else o.end = o.q.row0 + o.q.n;
+    }
 }
 
-// One row of the call per grid column; the warps of its blocks (blockIdx.y, then warp) share the row's heads: first the K
-// heads, then V, then q.  Lane l of a K or q head holds the pairs t = l P .. l P + P - 1 with both halves (P = D / 64), so
-// the rotation needs no exchange; of a V head the 2 P channels from 2 P l on.
-// The angles of the row (64-bit sincos, D / 2 of them) are worked out once per block.
+constexpr int ROW_WARPS = 4;       // warps of a block; each has rows of its own
+
+// Blocks of blockIdx.y 0 append, those of 1 rotate the queries.  A warp takes a row and every `slices`-th of its jobs: a job is
+// the K, V or q rows of HPW heads, D / 16 lanes each.  Lane j of a head holds the pairs t = 8 j .. 8 j + 7 with both halves (K, q),
+// so the rotation needs no exchange and its codes are two words; of V the 16 channels from 16 j on.  What the next two jobs
+// read is asked for ahead.  The row's angles (64-bit sincos, D / 2 of them) are shared out over the lanes and passed round by
+// shuffles.  Bytes bound it when there are many rows (q in and out, k and v in, 4.25 bits a value out), latency when few.
 template <typename T, int D>
-__global__ void k_kv4_append(Kv4View w, RopeFreq fr, uint8_t* __restrict__ pool, const int32_t* __restrict__ pos, const T* q, int64_t q_ld,
-                             const T* __restrict__ k, const T* __restrict__ v, int64_t kv_ld, T* q_out, int q_heads) {
-    constexpr int P = D / 64, R2 = D / 2;
-    __shared__ double cs[R2], sn[R2];
-    __shared__ int owner;
-    const int row = blockIdx.x;
-    Kv4Seq sq;
-    const int s = kv4_owner(w, row, &owner, &sq);
-    if (s < 0) return;
-    const int i = row - sq.row0, slot = sq.len + i;
-    if (sq.bad && threadIdx.x == 0) atomicCAS(w.status, DEV_OK, DEV_KV4_ROWS);
-    if (i < 0 || i >= sq.n) return;
-    const bool stored = i < sq.n_new;
-    const int p0 = pos ? __ldg(pos + row) : slot;
-    for (int t = threadIdx.x; t < R2; t += blockDim.x) {
-        double a, b;
-        sincos((double)p0 * fr.f[t], &b, &a);
-        cs[t] = a;
-        sn[t] = b;
-    }
-    int page = -1;
-    if (stored) page = kv4_page(w, s, slot);
-    __syncthreads();
-    const int warps = blockDim.x >> 5, lane = threadIdx.x & 31;
-    const int R = 1 << w.shift, r = slot & (R - 1);
-    constexpr int es = (int)sizeof(T);
-    const int jobs = 2 * w.heads + (q ? q_heads : 0);
-    for (int job = blockIdx.y * warps + (threadIdx.x >> 5); job < jobs; job += gridDim.y * warps) {
-        if (job >= 2 * w.heads) {                                   // q: rotated in 32 bits, rounded once
-            const int h = job - 2 * w.heads;
-            const T* x = q + (int64_t)row * q_ld + (int64_t)h * D;
-            T* y = q_out + ((int64_t)row * q_heads + h) * D;
+__global__ void __launch_bounds__(ROW_WARPS * 32) k_kv4_append(const __grid_constant__ Kv4View w, const __grid_constant__ RopeFreq fr, uint8_t* __restrict__ pool,
+                                                               const int32_t* __restrict__ pos, const T* q, int64_t q_ld, const T* __restrict__ k,
+                                                               const T* __restrict__ v, int64_t kv_ld, T* q_out, int q_heads, int slices, int rows_each) {
+    constexpr int R2 = D / 2, LPH = D / 16, HPW = 32 / LPH, ANG = R2 / 32, es = (int)sizeof(T);
+    const int lane = threadIdx.x & 31, j = lane % LPH, sub = lane / LPH;
+    const int wid = blockIdx.x * ROW_WARPS + (threadIdx.x >> 5), slice = wid % slices;
+    const int R = 1 << w.shift, kv_jobs = (w.heads + HPW - 1) / HPW, q_jobs = (q_heads + HPW - 1) / HPW;
+    const bool queries = blockIdx.y != 0;
+    struct Pair { Raw8<T> a, b; };
+    RowOwner o;
+    o.end = -1;
+    const int64_t first = (int64_t)(wid / slices) * rows_each;
+#pragma unroll 1
+    for (int64_t row_ = first; row_ < first + rows_each && row_ < w.n_rows; ++row_) {
+        const int row = (int)row_;
+        if (row >= o.end) find_owner(w, row, true, o);
+        if (o.seq < 0) continue;
+        const int slot = o.q.len + (row - o.q.row0);
+        const int p0 = pos ? __ldg(pos + row) : slot;
+        // 16 values a lane of a job; which: 0 K, 1 V, 2 q
+        auto ask = [&](int job) {
+            Pair x{};
+            const int which = queries ? 2 : job >= kv_jobs, h = (which == 1 ? job - kv_jobs : job) * HPW + sub;
+            if (job < (queries ? q_jobs : 2 * kv_jobs) && h < (queries ? q_heads : w.heads)) {
+                const T* src = (which == 2 ? q + (int64_t)row * q_ld : (which ? v : k) + (int64_t)row * kv_ld) + (int64_t)h * D + (which == 1 ? 16 : 8) * j;
+                x.a = load8<T>(src);
+                x.b = load8<T>(src + (which == 1 ? 8 : R2));
+            }
+            return x;
+        };
+        Pair next = ask(slice), after = ask(slice + slices);
+        double mc[ANG], msn[ANG];                                   // angles ANG lane + i
 #pragma unroll
-            for (int e = 0; e < P; ++e) {
-                const int t = lane * P + e;
-                const float c0 = (float)cs[t], s0 = (float)sn[t], a = to_f<T>(x[t]), b = to_f<T>(x[t + R2]);
-                y[t] = from_f<T>(a * c0 - b * s0);
-                y[t + R2] = from_f<T>(b * c0 + a * s0);
+        for (int i = 0; i < ANG; ++i) sincos((double)p0 * fr.f[ANG * lane + i], &msn[i], &mc[i]);
+        if (queries) {                                              // rotated in 32 bits, rounded once
+            float cs[8], sn[8];                                     // angles 8 j + i
+#pragma unroll
+            for (int i = 0; i < 8; ++i) {
+                cs[i] = __shfl_sync(0xffffffffu, (float)mc[i % ANG], (8 * j + i) / ANG);
+                sn[i] = __shfl_sync(0xffffffffu, (float)msn[i % ANG], (8 * j + i) / ANG);
+            }
+#pragma unroll 1
+            for (int job = slice; job < q_jobs; job += slices) {
+                const Pair now = next;
+                next = after;
+                after = ask(job + 2 * slices);
+                float a[8], b[8], c[8], d[8];
+                floats<T>(now.a, a);
+                floats<T>(now.b, b);
+#pragma unroll
+                for (int i = 0; i < 8; ++i) {
+                    c[i] = a[i] * cs[i] - b[i] * sn[i];
+                    d[i] = b[i] * cs[i] + a[i] * sn[i];
+                }
+                const int h = job * HPW + sub;
+                if (h < q_heads) {
+                    T* y = q_out + ((int64_t)row * q_heads + h) * D + 8 * j;
+                    store8<T>(y, c);
+                    store8<T>(y + R2, d);
+                }
             }
             continue;
         }
+        const int page = row - o.q.row0 < o.q.n_new ? kv4_page(w, o.seq, slot) : -1;
         if (page < 0) continue;
-        const int which = job >= w.heads, h = which ? job - w.heads : job;
-        float x[2 * P];
-        const T* src = (which ? v : k) + (int64_t)row * kv_ld + (int64_t)h * D;
-        if (which) {
+        const int r = slot & (R - 1);
+        double cs[8], sn[8];
 #pragma unroll
-            for (int e = 0; e < 2 * P; ++e) x[e] = to_f<T>(src[2 * P * lane + e]);
-        } else {
-#pragma unroll
-            for (int e = 0; e < P; ++e) {
-                const int t = lane * P + e;
-                const double a = (double)to_f<T>(src[t]), b = (double)to_f<T>(src[t + R2]);
-                x[e] = (float)(a * cs[t] - b * sn[t]);
-                x[P + e] = (float)(b * cs[t] + a * sn[t]);
-            }
+        for (int i = 0; i < 8; ++i) {
+            cs[i] = __shfl_sync(0xffffffffu, mc[i % ANG], (8 * j + i) / ANG);
+            sn[i] = __shfl_sync(0xffffffffu, msn[i % ANG], (8 * j + i) / ANG);
         }
-        T scale, mn;
-        row_params<T>(x, scale, mn);
-        const float sf = to_f<T>(scale), mf = to_f<T>(mn), inv = 1.f / sf;
-        uint8_t* blk = pool + kv4_block_at(w, page, h);
-        uint8_t* codes = blk + kv4_code_at(R, D, which, r);
-        uint32_t c[2 * P];
+#pragma unroll 1
+        for (int job = slice; job < 2 * kv_jobs; job += slices) {
+            const Pair now = next;
+            next = after;
+            after = ask(job + 2 * slices);
+            const int which = job >= kv_jobs, h = (which ? job - kv_jobs : job) * HPW + sub;
+            float a[8], b[8], x[16];
+            floats<T>(now.a, a);
+            floats<T>(now.b, b);
+            if (which) {
 #pragma unroll
-        for (int e = 0; e < 2 * P; ++e) c[e] = code_of(x[e], mf, sf, inv);
-        if (which) {                                                // P consecutive bytes a lane
+                for (int i = 0; i < 8; ++i) { x[i] = a[i]; x[8 + i] = b[i]; }
+            } else {                                                // rotated in 64 bits, then rounded to 32
 #pragma unroll
-            for (int e = 0; e < P; ++e) codes[P * lane + e] = (uint8_t)(c[2 * e] | (c[2 * e + 1] << 4));
-        } else if constexpr (P == 2) {                              // channels 2l, 2l + 1 and 64 + 2l, 64 + 2l + 1
-            codes[lane] = (uint8_t)(c[0] | (c[1] << 4));
-            codes[32 + lane] = (uint8_t)(c[2] | (c[3] << 4));
-        } else {                                                    // channel l and 32 + l: the odd lane's code is the high half
-            const uint32_t o0 = __shfl_down_sync(0xffffffffu, c[0], 1), o1 = __shfl_down_sync(0xffffffffu, c[1], 1);
-            if (!(lane & 1)) {
-                codes[lane / 2] = (uint8_t)(c[0] | (o0 << 4));
-                codes[16 + lane / 2] = (uint8_t)(c[1] | (o1 << 4));
+                for (int i = 0; i < 8; ++i) {
+                    x[i] = (float)((double)a[i] * cs[i] - (double)b[i] * sn[i]);
+                    x[8 + i] = (float)((double)b[i] * cs[i] + (double)a[i] * sn[i]);
+                }
             }
-        }
-        if (lane == 0) {
-            T* par = reinterpret_cast<T*>(blk + kv4_param_at(R, D, es, which, r));
-            par[0] = scale;
-            par[1] = mn;
+            float lo = x[0], hi = x[0];
+#pragma unroll
+            for (int i = 1; i < 16; ++i) { lo = min_nan(lo, x[i]); hi = max_nan(hi, x[i]); }
+#pragma unroll
+            for (int s = 1; s < LPH; s <<= 1) {
+                lo = min_nan(lo, __shfl_xor_sync(0xffffffffu, lo, s));
+                hi = max_nan(hi, __shfl_xor_sync(0xffffffffu, hi, s));
+            }
+            const T mn = from_f<T>(lo), scale = from_f<T>((float)(((double)hi - (double)lo) / 15.0));
+            uint32_t c[2];
+            codes_of(x, to_f<T>(mn), to_f<T>(scale), c);
+            if (h >= w.heads) continue;
+            uint8_t* blk = pool + kv4_block_at(w, page, h);
+            uint8_t* codes = blk + kv4_code_at(R, D, which, r);
+            if (which) {
+                *reinterpret_cast<uint2*>(codes + 8 * j) = make_uint2(c[0], c[1]);
+            } else {
+                *reinterpret_cast<uint32_t*>(codes + 4 * j) = c[0];
+                *reinterpret_cast<uint32_t*>(codes + D / 4 + 4 * j) = c[1];
+            }
+            if (j == 0) {
+                T* par = reinterpret_cast<T*>(blk + kv4_param_at(R, D, es, which, r));
+                par[0] = scale;
+                par[1] = mn;
+            }
         }
     }
 }
 
-// One row of the call per grid column, a warp per (head, K or V): lane l decodes D / 32 consecutive channels.
+// A warp takes a row; a lane decodes eight channels of a head at a time (4 bytes in, 16 or 32 out), D / 8 lanes a head.
 template <typename T, int D>
-__global__ void k_kv4_read(Kv4View w, const uint8_t* __restrict__ pool, const int32_t* __restrict__ first, T* __restrict__ k_out,
-                           T* __restrict__ v_out) {
-    constexpr int N = D / 32;
-    __shared__ int owner;
-    const int row = blockIdx.x;
-    Kv4Seq sq;
-    const int s = kv4_owner(w, row, &owner, &sq);
-    if (s < 0 || row < sq.row0) return;
-    const int64_t slot = (int64_t)(first ? __ldg(first + s) : sq.len) + (row - sq.row0);
-    if (slot < 0 || slot >= kv4_capacity(w)) {
-        if (threadIdx.x == 0) atomicCAS(w.status, DEV_OK, DEV_KV4_ROWS);
-        return;
-    }
-    const int page = kv4_page(w, s, (int)slot);
-    if (page < 0) return;
-    const int R = 1 << w.shift, r = (int)slot & (R - 1), lane = threadIdx.x & 31, warps = blockDim.x >> 5;
-    for (int job = blockIdx.y * warps + (threadIdx.x >> 5); job < 2 * w.heads; job += gridDim.y * warps) {
-        const int which = job >= w.heads, h = which ? job - w.heads : job;
-        T* out = which ? v_out : k_out;
-        if (!out) continue;
-        const uint8_t* blk = pool + kv4_block_at(w, page, h);
-        const T* par = reinterpret_cast<const T*>(blk + kv4_param_at(R, D, (int)sizeof(T), which, r));
-        const float sc = to_f<T>(par[0]), mn = to_f<T>(par[1]);
-        const uint8_t* codes = blk + kv4_code_at(R, D, which, r) + lane * (N / 2);
-        T* y = out + ((int64_t)row * w.heads + h) * D + lane * N;
+__global__ void __launch_bounds__(ROW_WARPS * 32) k_kv4_read(const __grid_constant__ Kv4View w, const uint8_t* __restrict__ pool, const int32_t* __restrict__ first,
+                                                             T* __restrict__ k_out, T* __restrict__ v_out, int slices, int rows_each) {
+    constexpr int LPH = D / 8, HPW = 32 / LPH, AHEAD = 4, es = (int)sizeof(T);
+    const int lane = threadIdx.x & 31, j = lane % LPH, sub = lane / LPH;
+    const int wid = blockIdx.x * ROW_WARPS + (threadIdx.x >> 5), slice = wid % slices;
+    const int R = 1 << w.shift, half = (w.heads + HPW - 1) / HPW, jobs = 2 * half;
+    RowOwner o;
+    o.end = -1;
+    const int64_t begin = (int64_t)(wid / slices) * rows_each;
+    for (int64_t row_ = begin; row_ < begin + rows_each && row_ < w.n_rows; ++row_) {
+        const int row = (int)row_;
+        if (row >= o.end) find_owner(w, row, !first, o);
+        if (o.seq < 0) continue;
+        const int64_t slot = (int64_t)(first ? __ldg(first + o.seq) : o.q.len) + (row - o.q.row0);
+        if (slot < 0 || slot >= kv4_capacity(w)) {
+            if (lane == 0) atomicCAS(w.status, DEV_OK, DEV_KV4_ROWS);
+            continue;
+        }
+        const int page = kv4_page(w, o.seq, (int)slot);
+        if (page < 0) continue;
+        const int r = (int)slot & (R - 1);
+        const uint8_t* base = pool + kv4_block_at(w, page, 0);
+        for (int job0 = slice; job0 < jobs; job0 += AHEAD * slices) {       // several jobs' loads under way together
+            uint32_t c[AHEAD];
+            float2 f[AHEAD];
 #pragma unroll
-        for (int e = 0; e < N / 2; ++e) {
-            const uint32_t b = codes[e];
-            y[2 * e] = from_f<T>(fmaf(sc, (float)(b & 15u), mn));
-            y[2 * e + 1] = from_f<T>(fmaf(sc, (float)(b >> 4), mn));
+            for (int a = 0; a < AHEAD; ++a) {
+                const int job = job0 + a * slices, which = job >= half, h = (which ? job - half : job) * HPW + sub;
+                c[a] = 0;
+                f[a] = make_float2(0.f, 0.f);
+                if (job < jobs && h < w.heads) {
+                    const uint8_t* blk = base + (size_t)h * w.block;
+                    c[a] = __ldg(reinterpret_cast<const uint32_t*>(blk + kv4_code_at(R, D, which, r) + 4 * j));
+                    f[a] = load_pair<T>(blk + kv4_param_at(R, D, es, which, r));
+                }
+            }
+#pragma unroll
+            for (int a = 0; a < AHEAD; ++a) {
+                const int job = job0 + a * slices, which = job >= half, h = (which ? job - half : job) * HPW + sub;
+                T* out = which ? v_out : k_out;
+                if (job >= jobs || h >= w.heads || !out) continue;
+                float x[8];
+#pragma unroll
+                for (int i = 0; i < 8; ++i) x[i] = fmaf(f[a].x, (float)((c[a] >> (4 * i)) & 15u), f[a].y);
+                store8<T>(out + ((int64_t)row * w.heads + h) * D + 8 * j, x);
+            }
         }
     }
 }
@@ -234,12 +359,18 @@ __global__ void k_kv4_advance(Kv4View w, int32_t* kv_len, const ghd_accept_resul
     kv_len[s] = sq.len + add;
 }
 
-// Blocks per row so that a few rows still spread over the device: one warp's job is short, a block start is not.
-int row_blocks(const ghd_ctx* c, int n_rows, int jobs, int warps) {
-    int y = (4 * c->sm_count) / (n_rows > 0 ? n_rows : 1);
-    const int most = (jobs + warps - 1) / warps;
-    if (y > most) y = most;
-    return y < 1 ? 1 : y;
+// Warps of a call over rows: as many as the device holds at a time and a few times that.  Few rows: their jobs are dealt to
+// several warps (slices); many: a warp takes several rows in turn, whose sequence it then looks up once.
+struct RowGrid { int slices, rows_each, blocks; };
+RowGrid row_grid(const ghd_ctx* c, int n_rows, int jobs) {
+    const int64_t want = (int64_t)c->sm_count * 64;
+    RowGrid g;
+    int64_t s = want / n_rows;
+    g.slices = (int)(s < 1 ? 1 : (s > jobs ? jobs : s));
+    g.rows_each = (int)((n_rows + 4 * want - 1) / (4 * want));
+    const int64_t warps = ((int64_t)n_rows + g.rows_each - 1) / g.rows_each * g.slices;
+    g.blocks = (int)((warps + ROW_WARPS - 1) / ROW_WARPS);
+    return g;
 }
 
 // A call works on its context's device whatever the current one is.
@@ -312,9 +443,10 @@ ghd_status ghd_kv4_append(ghd_ctx* c, const ghd_kv4* kv, const ghd_kv4_rows* row
     RopeFreq fr;
     for (int t = 0; t < D / 2; ++t) fr.f[t] = pow((double)m.rope_theta, -2.0 * t / D);
     const Kv4View w = kv4_view(c, kv, rows);
-    constexpr int WARPS = 8;
-    const dim3 grid(rows->n_rows, row_blocks(c, rows->n_rows, 2 * kv->n_kv_heads + (q ? m.n_heads : 0), WARPS));
-#define GHD_APPEND(T, DH) k_kv4_append<T, DH><<<grid, WARPS * 32, 0, c->cur>>>(w, fr, (uint8_t*)pool, rows->pos, (const T*)q, q_ld, (const T*)k, (const T*)v, kv_ld, (T*)q_out, m.n_heads)
+    const int hpw = 32 / (D / 16);
+    const RowGrid g = row_grid(c, rows->n_rows, ((q ? m.n_heads : 2 * kv->n_kv_heads) + hpw - 1) / hpw);
+    const dim3 grid(g.blocks, q ? 2 : 1);
+#define GHD_APPEND(T, DH) k_kv4_append<T, DH><<<grid, ROW_WARPS * 32, 0, c->cur>>>(w, fr, (uint8_t*)pool, rows->pos, (const T*)q, q_ld, (const T*)k, (const T*)v, kv_ld, (T*)q_out, m.n_heads, g.slices, g.rows_each)
     if (m.dtype == GHD_F32) { if (D == 64) GHD_APPEND(float, 64); else GHD_APPEND(float, 128); }
     else { if (D == 64) GHD_APPEND(__half, 64); else GHD_APPEND(__half, 128); }
 #undef GHD_APPEND
@@ -344,9 +476,9 @@ ghd_status ghd_kv4_read(ghd_ctx* c, const ghd_kv4* kv, const ghd_kv4_rows* rows,
     if (rows->n_rows == 0) return GHD_OK;
     OnDevice dev(c);
     const Kv4View w = kv4_view(c, kv, rows);
-    constexpr int WARPS = 8;
-    const dim3 grid(rows->n_rows, row_blocks(c, rows->n_rows, 2 * kv->n_kv_heads, WARPS));
-#define GHD_READ(T, DH) k_kv4_read<T, DH><<<grid, WARPS * 32, 0, c->cur>>>(w, (const uint8_t*)pool, first, (T*)k_out, (T*)v_out)
+    const int hpw = 32 / (c->cfg.d_head / 8);
+    const RowGrid g = row_grid(c, rows->n_rows, 2 * ((kv->n_kv_heads + hpw - 1) / hpw));
+#define GHD_READ(T, DH) k_kv4_read<T, DH><<<g.blocks, ROW_WARPS * 32, 0, c->cur>>>(w, (const uint8_t*)pool, first, (T*)k_out, (T*)v_out, g.slices, g.rows_each)
     if (c->cfg.dtype == GHD_F32) { if (c->cfg.d_head == 64) GHD_READ(float, 64); else GHD_READ(float, 128); }
     else { if (c->cfg.d_head == 64) GHD_READ(__half, 64); else GHD_READ(__half, 128); }
 #undef GHD_READ

@@ -29,20 +29,6 @@ __device__ __forceinline__ int kv4_page(const Kv4View& w, int seq, int row) {
 }
 __device__ __forceinline__ size_t kv4_block_at(const Kv4View& w, int page, int head) { return ((size_t)page * w.heads + head) * w.block; }
 
-// Sequence that owns row `row`, found by all threads of the block together (-1: nobody's); its numbers in *q.
-// scratch: one shared int.
-__device__ __forceinline__ int kv4_owner(const Kv4View& w, int row, int* scratch, Kv4Seq* q) {
-    if (threadIdx.x == 0) *scratch = -1;
-    __syncthreads();
-    for (int s = threadIdx.x; s < w.n_seqs; s += blockDim.x) {
-        const int a = __ldg(w.row_start + s), b = __ldg(w.row_start + s + 1);
-        if (a <= row && row < b) *scratch = s;          // one sequence at most when the starts do not fall
-    }
-    __syncthreads();
-    const int s = *scratch;
-    if (s >= 0) *q = kv4_load_seq(w, s);
-    return s;
-}
 #endif
 
 Kv4View kv4_view(const ghd_ctx* c, const ghd_kv4* kv, const ghd_kv4_rows* rows);
