@@ -199,11 +199,12 @@ class KvLayer:
         return _Kv(_ptr(self.k), _ptr(self.v), self.len)
 
 
-def _need(t, dtype, what: str, numel: int):
-    """A contiguous device tensor of `dtype` with at least `numel` elements (its pointer); raises otherwise."""
-    if t.dtype != dtype or not t.is_cuda or not t.is_contiguous() or t.numel() < numel:
-        raise GhdError(1, f"{what}: want a contiguous {dtype} device tensor of at least {numel} elements, "
-                          f"got {tuple(t.shape)} {t.dtype} on {t.device}")
+def _need(t, dtype, what: str, numel: int, dev: int | None = None):
+    """A contiguous device tensor of `dtype` with at least `numel` elements (its pointer), on device `dev` if that is given;
+    raises otherwise."""
+    if t.dtype != dtype or not t.is_cuda or not t.is_contiguous() or t.numel() < numel or (dev is not None and t.get_device() != dev):
+        raise GhdError(1, f"{what}: want a contiguous {dtype} device tensor of at least {numel} elements"
+                          f"{'' if dev is None else f' on cuda:{dev}'}, got {tuple(t.shape)} {t.dtype} on {t.device}")
     return t.data_ptr()
 
 
@@ -216,8 +217,11 @@ class Kv4Cache:
         if page_table.dim() != 2:
             raise GhdError(1, "kv4: page_table is not [n_seqs][max_pages]")
         n_seqs, max_pages = page_table.shape
-        self.c = _Kv4(n_seqs, n_pages, page_rows, max_pages, n_kv_heads, _need(page_table, torch.int32, "page_table", 0),
-                      _need(kv_len, torch.int32, "kv_len", n_seqs))
+        table = _need(page_table, torch.int32, "page_table", 0)
+        self.dev = page_table.get_device()
+        self.n_seqs, self.n_kv_heads, self.n_rows = n_seqs, n_kv_heads, n_pages * n_kv_heads * page_rows
+        self.c = _Kv4(n_seqs, n_pages, page_rows, max_pages, n_kv_heads, table, _need(kv_len, torch.int32, "kv_len", n_seqs, self.dev))
+        self.ref = C.byref(self.c)
 
 
 class Kv4Rows:
@@ -226,9 +230,12 @@ class Kv4Rows:
 
     def __init__(self, row_start, n_rows: int, pos=None, mask=None):
         self.row_start, self.n_rows, self.pos, self.mask = row_start, int(n_rows), pos, mask
+        start = _need(row_start, torch.int32, "row_start", 2)
+        self.dev = row_start.get_device()
         words = 0 if mask is None else int(mask.shape[-1])
-        self.c = _Kv4Rows(self.n_rows, words, _need(row_start, torch.int32, "row_start", 2), None if pos is None else _need(pos, torch.int32, "pos", self.n_rows),
-                          None if mask is None else _need(mask, torch.int64, "mask", self.n_rows * words))
+        self.c = _Kv4Rows(self.n_rows, words, start, None if pos is None else _need(pos, torch.int32, "pos", self.n_rows, self.dev),
+                          None if mask is None else _need(mask, torch.int64, "mask", self.n_rows * words, self.dev))
+        self.ref = C.byref(self.c)
 
 
 class Tree:
@@ -266,9 +273,11 @@ class Ctx:
     def __init__(self, cfg: ModelCfg, device="cuda:0"):
         self.lib = load_library()
         self.cfg = cfg
+        self.dtype, self.d_head, self.n_heads = cfg.torch_dtype, cfg.c.d_head, cfg.c.n_heads
         self.device = torch.device(device)
         self.handle = C.c_void_p()
         with torch.cuda.device(self.device):
+            self.dev = torch.cuda.current_device()
             self.stream = torch.cuda.current_stream(self.device)
             st = self.lib.ghd_create(C.byref(cfg.c), C.c_void_p(self.stream.cuda_stream), C.byref(self.handle))
             if st != 0:
@@ -432,45 +441,54 @@ def ghd_kv4_pool(ctx: Ctx, kv: Kv4Cache, n_layers: int = 1):
     return torch.zeros((n_layers, ghd_kv4_pool_bytes(ctx, kv)), dtype=torch.uint8, device=ctx.device)
 
 
-def _kv4_args(ctx: Ctx, kv: Kv4Cache, rows: Kv4Rows, pool):
-    if rows.row_start.numel() < kv.c.n_seqs + 1:
+def _kv4_match(ctx: Ctx, kv: Kv4Cache, rows: Kv4Rows):
+    """Refuses descriptions that do not belong together or to the context's device."""
+    if rows.row_start.numel() <= kv.n_seqs:
         raise GhdError(1, "kv4: row_start has fewer than n_seqs + 1 entries")
-    return _need(pool, torch.uint8, "pool", ghd_kv4_pool_bytes(ctx, kv))
+    if kv.dev != ctx.dev or rows.dev != ctx.dev:
+        raise GhdError(1, f"kv4: page table on cuda:{kv.dev}, rows on cuda:{rows.dev}, context on cuda:{ctx.dev}")
+
+
+def _kv4_args(ctx: Ctx, kv: Kv4Cache, rows: Kv4Rows, pool):
+    """Checks what a call's tensors have to be for its context -> pointer of the pool."""
+    _kv4_match(ctx, kv, rows)
+    return _need(pool, torch.uint8, "pool", kv.n_rows * (ctx.d_head + 4 * ctx.dtype.itemsize), ctx.dev)
 
 
 def _kv4_strided(ctx: Ctx, t, n: int, width: int, what: str):
     """Rows of `width` elements, contiguous inside a row -> (pointer, row stride)."""
-    if t.dtype != ctx.cfg.torch_dtype or not t.is_cuda or t.dim() != 2 or t.shape[0] < n or t.shape[1] != width or t.stride(1) != 1:
-        raise GhdError(1, f"{what}: want {ctx.cfg.torch_dtype} [{n}][{width}] with contiguous rows, got {tuple(t.shape)} {t.dtype}")
+    if t.dim() != 2 or t.shape[0] < n or t.shape[1] != width or t.stride(1) != 1 or t.dtype != ctx.dtype or t.get_device() != ctx.dev:
+        raise GhdError(1, f"{what}: want {ctx.dtype} [{n}][{width}] with contiguous rows on cuda:{ctx.dev}, got {tuple(t.shape)} {t.dtype} on {t.device}")
     return t.data_ptr(), t.stride(0)
 
 
 def ghd_kv4_append(ctx: Ctx, kv: Kv4Cache, rows: Kv4Rows, pool, q, k, v, q_out=None):
     """Rotates q and k, quantises k and v into the pool behind each sequence's cache rows.  q, k, v: [n_rows][heads * d_head], rows may
     be strided (column blocks of one projection); q None: keys and values only.  -> rotated queries (q_out)."""
-    n, d = rows.n_rows, ctx.cfg.c.d_head
+    n, width = rows.n_rows, kv.n_kv_heads * ctx.d_head
     at = _kv4_args(ctx, kv, rows, pool)
-    kp, kld = _kv4_strided(ctx, k, n, kv.c.n_kv_heads * d, "k")
-    vp, vld = _kv4_strided(ctx, v, n, kv.c.n_kv_heads * d, "v")
+    kp, kld = _kv4_strided(ctx, k, n, width, "k")
+    vp, vld = _kv4_strided(ctx, v, n, width, "v")
     if kld != vld:
         raise GhdError(1, "kv4_append: k and v have different row strides")
     qp, qld, op = None, 0, None
     if q is not None:
-        qp, qld = _kv4_strided(ctx, q, n, ctx.cfg.c.n_heads * d, "q")
+        width = ctx.n_heads * ctx.d_head
+        qp, qld = _kv4_strided(ctx, q, n, width, "q")
         if q_out is None:
-            q_out = torch.empty((n, ctx.cfg.c.n_heads * d), dtype=ctx.cfg.torch_dtype, device=ctx.device)
-        op = _need(q_out, ctx.cfg.torch_dtype, "q_out", n * ctx.cfg.c.n_heads * d)
-    ctx._check(ctx.lib.ghd_kv4_append(ctx.handle, C.byref(kv.c), C.byref(rows.c), at, qp, qld, kp, vp, kld, op))
+            q_out = torch.empty((n, width), dtype=ctx.dtype, device=ctx.device)
+        op = _need(q_out, ctx.dtype, "q_out", n * width, ctx.dev)
+    ctx._check(ctx.lib.ghd_kv4_append(ctx.handle, kv.ref, rows.ref, at, qp, qld, kp, vp, kld, op))
     return q_out
 
 
 def ghd_kv4_attention(ctx: Ctx, kv: Kv4Cache, rows: Kv4Rows, pool, q, out=None):
     """Attention of the new rows (rotated queries q [n_rows][n_heads * d_head]) over the paged 4-bit cache."""
-    numel = rows.n_rows * ctx.cfg.c.n_heads * ctx.cfg.c.d_head
+    numel = rows.n_rows * ctx.n_heads * ctx.d_head
     at = _kv4_args(ctx, kv, rows, pool)
-    qp = _need(q, ctx.cfg.torch_dtype, "q", numel)
+    qp = _need(q, ctx.dtype, "q", numel, ctx.dev)
     out = torch.zeros_like(q) if out is None else out
-    ctx._check(ctx.lib.ghd_kv4_attention(ctx.handle, C.byref(kv.c), C.byref(rows.c), at, qp, _need(out, ctx.cfg.torch_dtype, "out", numel)))
+    ctx._check(ctx.lib.ghd_kv4_attention(ctx.handle, kv.ref, rows.ref, at, qp, _need(out, ctx.dtype, "out", numel, ctx.dev)))
     return out
 
 
@@ -478,21 +496,24 @@ def ghd_kv4_read(ctx: Ctx, kv: Kv4Cache, pool, row_start, n_rows: int, first=Non
     """Cache rows first[s] + i (first None: the new rows' places) in the storage type -> (k, v) [n_rows][n_kv_heads * d_head]."""
     rows = Kv4Rows(row_start, n_rows)
     at = _kv4_args(ctx, kv, rows, pool)
-    shape = (rows.n_rows, kv.c.n_kv_heads * ctx.cfg.c.d_head)
-    k_out = torch.empty(shape, dtype=ctx.cfg.torch_dtype, device=ctx.device) if k_out is None else k_out
-    v_out = torch.empty(shape, dtype=ctx.cfg.torch_dtype, device=ctx.device) if v_out is None else v_out
-    ctx._check(ctx.lib.ghd_kv4_read(ctx.handle, C.byref(kv.c), C.byref(rows.c), at, None if first is None else _need(first, torch.int32, "first", kv.c.n_seqs),
-                                    _need(k_out, ctx.cfg.torch_dtype, "k_out", shape[0] * shape[1]), _need(v_out, ctx.cfg.torch_dtype, "v_out", shape[0] * shape[1])))
+    n, width = rows.n_rows, kv.n_kv_heads * ctx.d_head
+    if k_out is None and v_out is None:
+        k_out, v_out = torch.empty((2, max(n, 0), width), dtype=ctx.dtype, device=ctx.device).unbind()
+    k_out = torch.empty((n, width), dtype=ctx.dtype, device=ctx.device) if k_out is None else k_out
+    v_out = torch.empty((n, width), dtype=ctx.dtype, device=ctx.device) if v_out is None else v_out
+    ctx._check(ctx.lib.ghd_kv4_read(ctx.handle, kv.ref, rows.ref, at, None if first is None else _need(first, torch.int32, "first", kv.n_seqs, ctx.dev),
+                                    _need(k_out, ctx.dtype, "k_out", n * width, ctx.dev), _need(v_out, ctx.dtype, "v_out", n * width, ctx.dev)))
     return k_out, v_out
 
 
 def ghd_kv4_commit(ctx: Ctx, kv: Kv4Cache, rows: Kv4Rows, pools, results=None):
     """Keeps the accepted rows of every sequence in all pools (a list, or one tensor [n_layers][...]) and advances kv.kv_len.
     results: int32 [n_seqs][514] as ghd_accept writes them; None keeps every new row (pools are not touched)."""
+    _kv4_match(ctx, kv, rows)
     ptrs = [] if results is None else [_kv4_args(ctx, kv, rows, p) for p in pools]
     arr = (C.c_void_p * max(len(ptrs), 1))(*ptrs)
-    ctx._check(ctx.lib.ghd_kv4_commit(ctx.handle, C.byref(kv.c), C.byref(rows.c), arr, len(ptrs),
-                                      None if results is None else _need(results, torch.int32, "results", kv.c.n_seqs * (2 + 2 * GHD_MAX_NODES))))
+    ctx._check(ctx.lib.ghd_kv4_commit(ctx.handle, kv.ref, rows.ref, arr, len(ptrs),
+                                      None if results is None else _need(results, torch.int32, "results", kv.n_seqs * (2 + 2 * GHD_MAX_NODES), ctx.dev)))
 
 
 def ghd_linear(ctx: Ctx, x, w, y=None):

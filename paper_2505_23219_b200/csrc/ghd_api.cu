@@ -1,5 +1,6 @@
 // C-ABI entry points of libghd: argument validation, workspace layout, and the
 // order in which the kernels of a layer / a step are enqueued.
+#include <cmath>
 #include <cstdio>
 #include <cstring>
 #include <new>
@@ -245,6 +246,7 @@ ghd_status ghd_create(const ghd_model_cfg* cfg, void* cuda_stream, ghd_ctx** out
     c->cap_stream = nullptr;
     c->device = dev;
     c->sm_count = sms;
+    for (int t = 0; t < 64; ++t) c->rope_freq[t] = t < cfg->d_head / 2 ? pow((double)cfg->rope_theta, -2.0 * t / cfg->d_head) : 0.0;
     c->opt_gemm_path = c->opt_attn_splits = c->opt_attn_path = c->opt_graph = c->opt_gemm_ctas = c->opt_gemm_burst = c->opt_no_pdl = c->opt_gemm_stages = c->opt_gemm_epi = c->opt_attn_sparse = c->opt_chain_calls = c->opt_fused_norm = c->opt_gemm_pair = c->opt_attn_rows = c->opt_gemm_skew = c->opt_attn_small = 0;
     c->ws = nullptr;
     c->ws_bytes = 0;

@@ -82,6 +82,7 @@ struct ghd_ctx {
     cudaStream_t cur;         // where launches go: `stream`, or `cap_stream` while a graph is being captured
     cudaStream_t cap_stream;  // library-owned stream used only for graph capture (nothing ever runs on it)
     int device, sm_count;
+    double rope_freq[64];     // rope_theta^(-2 t / d_head) for every pair of channels
     // options
     int opt_gemm_path, opt_attn_splits, opt_attn_path, opt_graph, opt_gemm_ctas, opt_gemm_burst, opt_no_pdl, opt_gemm_stages, opt_gemm_epi, opt_attn_sparse, opt_chain_calls, opt_fused_norm, opt_gemm_pair, opt_attn_rows, opt_gemm_skew, opt_attn_small;
     // workspace carve (all device pointers into the caller's buffer)

@@ -1,6 +1,6 @@
 // The paged cache in 4 bits: append (rotation and quantisation on the way), read back, commit, and the C entry points.
-#include <cmath>
 #include <cstdio>
+#include <cstring>
 
 #include "kv4.cuh"
 
@@ -17,6 +17,30 @@ template <> __device__ __forceinline__ __half from_f<__half>(float v) { return _
 
 // theta^(-2 t / d) for every pair of channels, worked out on the host in 64 bits
 struct RopeFreq { double f[64]; };
+
+// Sine and cosine in 64 bits of |x| < 2^31: x less a whole number of quarter turns (pi / 2 in two parts, the second below
+// 2^-53 of the first, so the remainder is off by about 2^-53), then the power series, whose first term left out is below 2^-54
+// on [-pi / 4, pi / 4].  The library's function takes any argument and three times the instructions, and keeps a local array.
+__device__ __forceinline__ void sincos_turns(double x, double& sn, double& cs) {
+    constexpr double HALF_PI_HI = 1.57079632679489655800, HALF_PI_LO = 6.12323399573676603587e-17;
+    const double n = rint(x * 0.63661977236758134308);
+    double r = fma(-n, HALF_PI_HI, x);
+    r = fma(-n, HALF_PI_LO, r);
+    const double z = r * r;
+    constexpr double F[7] = {1.0 / 6, 1.0 / 120, 1.0 / 5040, 1.0 / 362880, 1.0 / 39916800, 1.0 / 6227020800.0, 1.0 / 1307674368000.0};      // 1 / (2 k + 3)!
+    constexpr double G[8] = {0.5, 1.0 / 24, 1.0 / 720, 1.0 / 40320, 1.0 / 3628800, 1.0 / 479001600, 1.0 / 87178291200.0, 1.0 / 20922789888000.0};   // 1 / (2 k + 2)!
+    double a = F[6], b = G[7];
+#pragma unroll
+    for (int k = 5; k >= 0; --k) a = fma(-a, z, F[k]);
+#pragma unroll
+    for (int k = 6; k >= 0; --k) b = fma(-b, z, G[k]);
+    a = fma(-a * z, r, r);               // r - r^3 / 6 + ...
+    b = fma(-b, z, 1.0);                 // 1 - r^2 / 2 + ...
+    const int quarter = (int)(long long)n & 3;
+    const double u = quarter & 1 ? b : a, w = quarter & 1 ? a : b;
+    sn = quarter & 2 ? -u : u;
+    cs = (quarter == 1 || quarter == 2) ? -w : w;
+}
 
 // min and max that keep a NaN (fminf and fmaxf drop it)
 __device__ __forceinline__ float min_nan(float a, float b) { float r; asm("min.NaN.f32 %0, %1, %2;" : "=f"(r) : "f"(a), "f"(b)); return r; }
@@ -66,12 +90,12 @@ template <> __device__ __forceinline__ float2 load_pair<float>(const uint8_t* p)
 template <> __device__ __forceinline__ float2 load_pair<__half>(const uint8_t* p) { return __half22float2(*reinterpret_cast<const __half2*>(p)); }
 
 // Codes of 16 values, x[0 .. 7] in c[0] from the low end.  The quotient decides between two codes, so it is taken in 64 bits
-// where 32 could fall on the other side of a half: 32-bit subtraction and multiplication by a reciprocal are off by less
-// than 2^-20 of the quotient (three roundings of 2^-24 and the reciprocal's own), which is below 16; where one of the 16 is
-// nearer than 2^-15 to a half (or the reciprocal is none) they are redone.  Adding 1.5 * 2^23 rounds to a whole number, ties to
-// even, and leaves it in the low bits.
+// where 32 could fall on the other side of a half: a 32-bit difference, reciprocal and product, rounded once each, are off by
+// less than 2^-22 of the quotient, which the clamp keeps below 16, so values within 2^-18 of a half are done again, and all of
+// them where the reciprocal is none or the differences could leave the range of 32 bits.  Such values are common: differences of halves lie on a grid and many are ties.  Adding
+// 1.5 * 2^23 rounds to a whole number, ties to even, and leaves it in the low bits.
 __device__ __forceinline__ void codes_of(const float (&x)[16], float mn, float scale, uint32_t (&c)[2]) {
-    constexpr float MAGIC = 12582912.f;                             // bits 0x4b400000
+    constexpr float MAGIC = 12582912.f, NEAR = 0.5f - 0x1p-18f;     // MAGIC has the bits 0x4b400000
     const float inv = scale == 0.f ? 0.f : 1.f / scale;
     float far = 0.f;
     c[0] = c[1] = 0u;
@@ -82,16 +106,25 @@ __device__ __forceinline__ void codes_of(const float (&x)[16], float mn, float s
         far = fmaxf(far, fabsf(t - (r - MAGIC)));
         c[i >> 3] += (__float_as_uint(r) - 0x4b400000u) << (4 * (i & 7));
     }
-    if (far > 0.5f - 0x1p-15f || !(inv < INFINITY)) {
-        c[0] = c[1] = 0u;
-#pragma unroll 1
-        for (int i = 0; i < 16; ++i) {
-            float y = x[0];
+    uint32_t again = 0;
+    if (far > NEAR) {
 #pragma unroll
-            for (int k = 1; k < 16; ++k) if (k == i) y = x[k];
-            const float r = fminf(fmaxf((float)rint(((double)y - (double)mn) / (double)scale), 0.f), 15.f);
-            c[i >> 3] |= (uint32_t)r << (4 * (i & 7));
+        for (int i = 0; i < 16; ++i) {
+            const float t = fminf(fmaxf((x[i] - mn) * inv, 0.f), 15.f);
+            again |= (uint32_t)(fabsf(t - (t + MAGIC - MAGIC)) > NEAR) << i;
         }
+    }
+    if (!(inv < INFINITY) || scale > 0x1p123f) again = 0xffffu;
+    while (again) {
+        const int i = __ffs(again) - 1;
+        again &= again - 1;
+        float y = x[0];
+#pragma unroll
+        for (int k = 1; k < 16; ++k) if (k == i) y = x[k];
+        const float r = fminf(fmaxf((float)rint(((double)y - (double)mn) / (double)scale), 0.f), 15.f);
+        const int at = 4 * (i & 7);
+        if (i < 8) c[0] = (c[0] & ~(15u << at)) | (uint32_t)r << at;
+        else c[1] = (c[1] & ~(15u << at)) | (uint32_t)r << at;
     }
 }
 
@@ -128,7 +161,7 @@ constexpr int ROW_WARPS = 4;       // warps of a block; each has rows of its own
 // read is asked for ahead.  The row's angles (64-bit sincos, D / 2 of them) are shared out over the lanes and passed round by
 // shuffles.  Bytes bound it when there are many rows (q in and out, k and v in, 4.25 bits a value out), latency when few.
 template <typename T, int D>
-__global__ void __launch_bounds__(ROW_WARPS * 32) k_kv4_append(const __grid_constant__ Kv4View w, const __grid_constant__ RopeFreq fr, uint8_t* __restrict__ pool,
+__global__ void __launch_bounds__(ROW_WARPS * 32, 4) k_kv4_append(const __grid_constant__ Kv4View w, const __grid_constant__ RopeFreq fr, uint8_t* __restrict__ pool,
                                                                const int32_t* __restrict__ pos, const T* q, int64_t q_ld, const T* __restrict__ k,
                                                                const T* __restrict__ v, int64_t kv_ld, T* q_out, int q_heads, int slices, int rows_each) {
     constexpr int R2 = D / 2, LPH = D / 16, HPW = 32 / LPH, ANG = R2 / 32, es = (int)sizeof(T);
@@ -161,7 +194,7 @@ __global__ void __launch_bounds__(ROW_WARPS * 32) k_kv4_append(const __grid_cons
         Pair next = ask(slice), after = ask(slice + slices);
         double mc[ANG], msn[ANG];                                   // angles ANG lane + i
 #pragma unroll
-        for (int i = 0; i < ANG; ++i) sincos((double)p0 * fr.f[ANG * lane + i], &msn[i], &mc[i]);
+        for (int i = 0; i < ANG; ++i) sincos_turns((double)p0 * fr.f[ANG * lane + i], msn[i], mc[i]);
         if (queries) {                                              // rotated in 32 bits, rounded once
             float cs[8], sn[8];                                     // angles 8 j + i
 #pragma unroll
@@ -441,7 +474,7 @@ ghd_status ghd_kv4_append(ghd_ctx* c, const ghd_kv4* kv, const ghd_kv4_rows* row
     if (rows->n_rows == 0) return GHD_OK;
     OnDevice dev(c);
     RopeFreq fr;
-    for (int t = 0; t < D / 2; ++t) fr.f[t] = pow((double)m.rope_theta, -2.0 * t / D);
+    memcpy(fr.f, c->rope_freq, sizeof(fr.f));
     const Kv4View w = kv4_view(c, kv, rows);
     const int hpw = 32 / (D / 16);
     const RowGrid g = row_grid(c, rows->n_rows, ((q ? m.n_heads : 2 * kv->n_kv_heads) + hpw - 1) / hpw);
@@ -493,6 +526,9 @@ ghd_status ghd_kv4_commit(ghd_ctx* c, const ghd_kv4* kv, const ghd_kv4_rows* row
     if (n_layers < 0 || (results && (n_layers < 1 || !pools))) return fail(c, GHD_EINVAL, "kv4_commit: no pools");
     for (int l = 0; results && l < n_layers; ++l)
         if (!pools[l] || !aligned16(pools[l])) return fail(c, GHD_EINVAL, "kv4_commit: a pool is null or not 16-byte aligned");
+    for (int l = 1; results && l < n_layers; ++l)
+        for (int e = 0; e < l; ++e)
+            if (pools[e] == pools[l]) return fail(c, GHD_EINVAL, "kv4_commit: the same pool twice");
     if (rows->n_rows == 0) return GHD_OK;
     OnDevice dev(c);
     const Kv4View w = kv4_view(c, kv, rows);
