@@ -85,10 +85,6 @@ template <> __device__ __forceinline__ void store8<__half>(__half* p, const floa
     }
     *reinterpret_cast<uint4*>(p) = make_uint4(r[0], r[1], r[2], r[3]);
 }
-template <typename T> __device__ __forceinline__ float2 load_pair(const uint8_t* p);
-template <> __device__ __forceinline__ float2 load_pair<float>(const uint8_t* p) { return *reinterpret_cast<const float2*>(p); }
-template <> __device__ __forceinline__ float2 load_pair<__half>(const uint8_t* p) { return __half22float2(*reinterpret_cast<const __half2*>(p)); }
-
 // Codes of 16 values, x[0 .. 7] in c[0] from the low end.  The quotient decides between two codes, so it is taken in 64 bits
 // where 32 could fall on the other side of a half: a 32-bit difference, reciprocal and product, rounded once each, are off by
 // less than 2^-22 of the quotient, which the clamp keeps below 16, so values within 2^-18 of a half are done again, and all of
@@ -281,14 +277,40 @@ __global__ void __launch_bounds__(ROW_WARPS * 32, 4) k_kv4_append(const __grid_c
     }
 }
 
-// A warp takes a row; a lane decodes eight channels of a head at a time (4 bytes in, 16 or 32 out), D / 8 lanes a head.
+// min + scale * code of 8 channels, rounded once, and stored.  fp16: a byte of two codes goes to both halves of a register under
+// the exponent of 1024 (1024 + c and 1024 + 16 c), one fma makes both c exactly and one more is the value: a fused product and
+// sum of halves rounds once.
+template <typename T> struct RowPar;
+template <> struct RowPar<float> { float2 v; };
+template <> struct RowPar<__half> { __half2 v; };
+__device__ __forceinline__ void decode8(uint32_t c, RowPar<float> f, float* y) {
+    float x[8];
+#pragma unroll
+    for (int i = 0; i < 8; ++i) x[i] = fmaf(f.v.x, (float)((c >> (4 * i)) & 15u), f.v.y);
+    store8<float>(y, x);
+}
+__device__ __forceinline__ void decode8(uint32_t c, RowPar<__half> f, __half* y) {
+    const __half2 one = __floats2half2_rn(1.f, 0.0625f), off = __floats2half2_rn(-1024.f, -64.f);
+    const __half2 scale = __low2half2(f.v), mn = __high2half2(f.v);
+    uint32_t r[4];
+#pragma unroll
+    for (int b = 0; b < 4; ++b) {
+        const uint32_t w = (__byte_perm(c, 0u, b | b << 8) & 0x00f0000fu) | 0x64006400u;
+        const __half2 v = __hfma2(scale, __hfma2(*reinterpret_cast<const __half2*>(&w), one, off), mn);
+        r[b] = *reinterpret_cast<const uint32_t*>(&v);
+    }
+    *reinterpret_cast<uint4*>(y) = make_uint4(r[0], r[1], r[2], r[3]);
+}
+
+// A warp takes a row and every `slices`-th of its jobs: K and V of HPW heads, D / 8 lanes each; a lane decodes eight channels of
+// both (4 bytes in, 16 or 32 out).  AHEAD jobs' loads are under way together.  The bytes written bound it when there are many rows.
 template <typename T, int D>
 __global__ void __launch_bounds__(ROW_WARPS * 32) k_kv4_read(const __grid_constant__ Kv4View w, const uint8_t* __restrict__ pool, const int32_t* __restrict__ first,
                                                              T* __restrict__ k_out, T* __restrict__ v_out, int slices, int rows_each) {
     constexpr int LPH = D / 8, HPW = 32 / LPH, AHEAD = 4, es = (int)sizeof(T);
     const int lane = threadIdx.x & 31, j = lane % LPH, sub = lane / LPH;
     const int wid = blockIdx.x * ROW_WARPS + (threadIdx.x >> 5), slice = wid % slices;
-    const int R = 1 << w.shift, half = (w.heads + HPW - 1) / HPW, jobs = 2 * half;
+    const int R = 1 << w.shift;
     RowOwner o;
     o.end = -1;
     const int64_t begin = (int64_t)(wid / slices) * rows_each;
@@ -304,30 +326,31 @@ __global__ void __launch_bounds__(ROW_WARPS * 32) k_kv4_read(const __grid_consta
         const int page = kv4_page(w, o.seq, (int)slot);
         if (page < 0) continue;
         const int r = (int)slot & (R - 1);
-        const uint8_t* base = pool + kv4_block_at(w, page, 0);
-        for (int job0 = slice; job0 < jobs; job0 += AHEAD * slices) {       // several jobs' loads under way together
-            uint32_t c[AHEAD];
-            float2 f[AHEAD];
+        const uint8_t* codes = pool + kv4_block_at(w, page, 0) + kv4_code_at(R, D, 0, r) + 4 * j;
+        const uint8_t* pars = pool + kv4_block_at(w, page, 0) + kv4_param_at(R, D, es, 0, r);
+        const size_t codes_v = kv4_code_at(R, D, 1, 0) - kv4_code_at(R, D, 0, 0), pars_v = kv4_param_at(R, D, es, 1, 0) - kv4_param_at(R, D, es, 0, 0);
+        const int64_t out = (int64_t)row * w.heads * D + 8 * j;
+#pragma unroll 1
+        for (int h0 = slice * HPW + sub; h0 - sub < w.heads; h0 += AHEAD * slices * HPW) {
+            uint32_t c[AHEAD][2];
+            RowPar<T> f[AHEAD][2];
 #pragma unroll
             for (int a = 0; a < AHEAD; ++a) {
-                const int job = job0 + a * slices, which = job >= half, h = (which ? job - half : job) * HPW + sub;
-                c[a] = 0;
-                f[a] = make_float2(0.f, 0.f);
-                if (job < jobs && h < w.heads) {
-                    const uint8_t* blk = base + (size_t)h * w.block;
-                    c[a] = __ldg(reinterpret_cast<const uint32_t*>(blk + kv4_code_at(R, D, which, r) + 4 * j));
-                    f[a] = load_pair<T>(blk + kv4_param_at(R, D, es, which, r));
+                const int h = h0 + a * slices * HPW;
+                if (h < w.heads) {
+                    const uint8_t *pc = codes + (size_t)h * w.block, *pp = pars + (size_t)h * w.block;
+                    c[a][0] = __ldg(reinterpret_cast<const uint32_t*>(pc));
+                    c[a][1] = __ldg(reinterpret_cast<const uint32_t*>(pc + codes_v));
+                    f[a][0] = *reinterpret_cast<const RowPar<T>*>(pp);
+                    f[a][1] = *reinterpret_cast<const RowPar<T>*>(pp + pars_v);
                 }
             }
 #pragma unroll
             for (int a = 0; a < AHEAD; ++a) {
-                const int job = job0 + a * slices, which = job >= half, h = (which ? job - half : job) * HPW + sub;
-                T* out = which ? v_out : k_out;
-                if (job >= jobs || h >= w.heads || !out) continue;
-                float x[8];
-#pragma unroll
-                for (int i = 0; i < 8; ++i) x[i] = fmaf(f[a].x, (float)((c[a] >> (4 * i)) & 15u), f[a].y);
-                store8<T>(out + ((int64_t)row * w.heads + h) * D + 8 * j, x);
+                const int h = h0 + a * slices * HPW;
+                if (h >= w.heads) break;
+                if (k_out) decode8(c[a][0], f[a][0], k_out + out + (int64_t)h * D);
+                if (v_out) decode8(c[a][1], f[a][1], v_out + out + (int64_t)h * D);
             }
         }
     }
@@ -510,7 +533,7 @@ ghd_status ghd_kv4_read(ghd_ctx* c, const ghd_kv4* kv, const ghd_kv4_rows* rows,
     OnDevice dev(c);
     const Kv4View w = kv4_view(c, kv, rows);
     const int hpw = 32 / (c->cfg.d_head / 8);
-    const RowGrid g = row_grid(c, rows->n_rows, 2 * ((kv->n_kv_heads + hpw - 1) / hpw));
+    const RowGrid g = row_grid(c, rows->n_rows, (kv->n_kv_heads + hpw - 1) / hpw);
 #define GHD_READ(T, DH) k_kv4_read<T, DH><<<g.blocks, ROW_WARPS * 32, 0, c->cur>>>(w, (const uint8_t*)pool, first, (T*)k_out, (T*)v_out, g.slices, g.rows_each)
     if (c->cfg.dtype == GHD_F32) { if (c->cfg.d_head == 64) GHD_READ(float, 64); else GHD_READ(float, 128); }
     else { if (c->cfg.d_head == 64) GHD_READ(__half, 64); else GHD_READ(__half, 128); }
