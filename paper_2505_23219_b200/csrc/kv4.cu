@@ -86,31 +86,34 @@ template <> __device__ __forceinline__ void store8<__half>(__half* p, const floa
     *reinterpret_cast<uint4*>(p) = make_uint4(r[0], r[1], r[2], r[3]);
 }
 // Codes of 16 values, x[0 .. 7] in c[0] from the low end.  The quotient decides between two codes, so it is taken in 64 bits
-// where 32 could fall on the other side of a half: a 32-bit difference, reciprocal and product, rounded once each, are off by
-// less than 2^-22 of the quotient, which the clamp keeps below 16, so values within 2^-18 of a half are done again, and all of
-// them where the reciprocal is none or the differences could leave the range of 32 bits.  Such values are common: differences of halves lie on a grid and many are ties.  Adding
-// 1.5 * 2^23 rounds to a whole number, ties to even, and leaves it in the low bits.
+// where 32 could fall on the other side of a half: the difference, 15 scale, its reciprocal and the product, rounded once each, are
+// off by less than 2^-22 of the quotient, which is held in [0, 15] (as 15 times a number that the product clamps to [0, 1]), so
+// values within 2^-18 of a half are done again, and all of them where the reciprocal is none or the differences could leave the
+// range of 32 bits.  Such values are common: differences of halves lie on a grid and many are ties.  Adding 1.5 * 2^23 rounds
+// to a whole number, ties to even, and leaves it in the low bits.
 __device__ __forceinline__ void codes_of(const float (&x)[16], float mn, float scale, uint32_t (&c)[2]) {
-    constexpr float MAGIC = 12582912.f, NEAR = 0.5f - 0x1p-18f;     // MAGIC has the bits 0x4b400000
-    const float inv = scale == 0.f ? 0.f : 1.f / scale;
+    constexpr float MAGIC = 12582912.f, NEAR = 0.5f - 0x1p-18f;
+    constexpr uint32_t BITS = 0x4b400000u * 0x11111111u;            // MAGIC's bits, shifted and added up as the codes are
+    const float inv = scale == 0.f ? 0.f : 1.f / (15.f * scale);
+    auto share = [&](int i) { return __saturatef((x[i] - mn) * inv); };
+    auto off = [&](float t, float r) { return fabsf(fmaf(t, 15.f, MAGIC - r)); };
     float far = 0.f;
-    c[0] = c[1] = 0u;
+    c[0] = c[1] = 0u - BITS;
 #pragma unroll
     for (int i = 0; i < 16; ++i) {
-        const float t = fminf(fmaxf((x[i] - mn) * inv, 0.f), 15.f);
-        const float r = t + MAGIC;
-        far = fmaxf(far, fabsf(t - (r - MAGIC)));
-        c[i >> 3] += (__float_as_uint(r) - 0x4b400000u) << (4 * (i & 7));
+        const float t = share(i), r = fmaf(t, 15.f, MAGIC);
+        far = fmaxf(far, off(t, r));
+        c[i >> 3] += __float_as_uint(r) << (4 * (i & 7));
     }
     uint32_t again = 0;
     if (far > NEAR) {
 #pragma unroll
         for (int i = 0; i < 16; ++i) {
-            const float t = fminf(fmaxf((x[i] - mn) * inv, 0.f), 15.f);
-            again |= (uint32_t)(fabsf(t - (t + MAGIC - MAGIC)) > NEAR) << i;
+            const float t = share(i);
+            again |= (uint32_t)(off(t, fmaf(t, 15.f, MAGIC)) > NEAR) << i;
         }
     }
-    if (!(inv < INFINITY) || scale > 0x1p123f) again = 0xffffu;
+    if (!(inv < INFINITY) || scale > 0x1p121f) again = 0xffffu;
     while (again) {
         const int i = __ffs(again) - 1;
         again &= again - 1;
