@@ -545,6 +545,9 @@ __global__ void __launch_bounds__(THREADS, 1) k_attn_kv4_tc(const __grid_constan
                     vis = 0u;
                     over = k == 0;
 #pragma unroll
+                    for (int x = 0; x < 4; ++x)                           // what lies behind the rows has no say in the exponent
+                        if (key0 + 8 * x >= it.keys || !((groups >> (8 * quad + (x >> 1))) & 1u)) vs[x] = 0.f;
+#pragma unroll
                     for (int j = 0; j < NB; ++j)
 #pragma unroll
                         for (int e = 0; e < 2; ++e) {

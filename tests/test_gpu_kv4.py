@@ -241,6 +241,28 @@ def test_extreme_scales_of_values_and_scores(ghd):
     assert np.isfinite(got).all() and (np.abs(got - want) <= tol).all()
 
 
+@pytest.mark.parametrize("H,Hk,n", [(2, 2, 1), (4, 1, 9), (2, 2, 32), (2, 2, 70)])
+def test_scales_behind_the_rows_cost_no_precision(ghd, H, Hk, n):
+    """The page's rows behind a sequence hold the largest scales there are.  All scores are equal, so the tolerance is that of
+    the weights alone."""
+    su = Setup(ghd, H, Hk, 128, "f16", 128, [0, 3], [n, n], 13, garbage=False)
+    collect(su)
+    for s in range(2):
+        for t in range(su.lens[s] + n, -(-(su.lens[s] + n) // 128) * 128):
+            page, row = okv4.slots(su.table, 128, s, t)
+            for h in range(Hk):
+                for which in (0, 1):
+                    su.pool.put(which, page, row, h, su.pool.codes(which, page, row, h), 65504.0, -65504.0)
+    su.dpool.copy_(dev(su.pool.data.reshape(-1)))
+    vis, words = su.trees()
+    q = np.zeros((2 * n, H, 128), np.float16)
+    out = ghd.ghd_kv4_attention(su.ctx, su.kv, ghd.Kv4Rows(dev(su.start), 2 * n, mask=dev(words)), su.dpool, dev(q.reshape(2 * n, -1)))
+    ghd.ghd_sync_status(su.ctx)
+    got = out.double().cpu().numpy().reshape(2 * n, H, 128)
+    want = okv4.attention(su.pool, su.table, su.lens, su.start, vis, q)
+    assert (np.abs(got - want) <= attention_tolerance(su, q)(want)).all()
+
+
 def test_the_same_call_gives_the_same_bits_and_leaves_its_scratch_clean(ghd):
     su = Setup(ghd, 4, 4, 128, "f16", 64, [1500, 10], [9, 3], 12)
     vis, words = su.trees()
