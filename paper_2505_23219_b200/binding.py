@@ -202,7 +202,7 @@ class KvLayer:
 def _need(t, dtype, what: str, numel: int, dev: int | None = None):
     """A contiguous device tensor of `dtype` with at least `numel` elements (its pointer), on device `dev` if that is given;
     raises otherwise."""
-    if t.dtype != dtype or not t.is_cuda or not t.is_contiguous() or t.numel() < numel or (dev is not None and t.get_device() != dev):
+    if (not t.is_cuda if dev is None else t.get_device() != dev) or t.dtype is not dtype or t.numel() < numel or not t.is_contiguous():
         raise GhdError(1, f"{what}: want a contiguous {dtype} device tensor of at least {numel} elements"
                           f"{'' if dev is None else f' on cuda:{dev}'}, got {tuple(t.shape)} {t.dtype} on {t.device}")
     return t.data_ptr()
@@ -231,6 +231,7 @@ class Kv4Rows:
     def __init__(self, row_start, n_rows: int, pos=None, mask=None):
         self.row_start, self.n_rows, self.pos, self.mask = row_start, int(n_rows), pos, mask
         start = _need(row_start, torch.int32, "row_start", 2)
+        self.n_starts = row_start.numel()
         self.dev = row_start.get_device()
         words = 0 if mask is None else int(mask.shape[-1])
         self.c = _Kv4Rows(self.n_rows, words, start, None if pos is None else _need(pos, torch.int32, "pos", self.n_rows, self.dev),
@@ -274,6 +275,7 @@ class Ctx:
         self.lib = load_library()
         self.cfg = cfg
         self.dtype, self.d_head, self.n_heads = cfg.torch_dtype, cfg.c.d_head, cfg.c.n_heads
+        self.kv4_row = self.d_head + 4 * self.dtype.itemsize      # bytes of a row of one head in the 4-bit cache
         self.device = torch.device(device)
         self.handle = C.c_void_p()
         with torch.cuda.device(self.device):
@@ -443,16 +445,14 @@ def ghd_kv4_pool(ctx: Ctx, kv: Kv4Cache, n_layers: int = 1):
 
 def _kv4_match(ctx: Ctx, kv: Kv4Cache, rows: Kv4Rows):
     """Refuses descriptions that do not belong together or to the context's device."""
-    if rows.row_start.numel() <= kv.n_seqs:
+    if rows.n_starts <= kv.n_seqs:
         raise GhdError(1, "kv4: row_start has fewer than n_seqs + 1 entries")
     if kv.dev != ctx.dev or rows.dev != ctx.dev:
         raise GhdError(1, f"kv4: page table on cuda:{kv.dev}, rows on cuda:{rows.dev}, context on cuda:{ctx.dev}")
 
 
-def _kv4_args(ctx: Ctx, kv: Kv4Cache, rows: Kv4Rows, pool):
-    """Checks what a call's tensors have to be for its context -> pointer of the pool."""
-    _kv4_match(ctx, kv, rows)
-    return _need(pool, torch.uint8, "pool", kv.n_rows * (ctx.d_head + 4 * ctx.dtype.itemsize), ctx.dev)
+def _kv4_pool(ctx: Ctx, kv: Kv4Cache, pool):
+    return _need(pool, torch.uint8, "pool", kv.n_rows * ctx.kv4_row, ctx.dev)
 
 
 def _kv4_strided(ctx: Ctx, t, n: int, width: int, what: str):
@@ -466,7 +466,8 @@ def ghd_kv4_append(ctx: Ctx, kv: Kv4Cache, rows: Kv4Rows, pool, q, k, v, q_out=N
     """Rotates q and k, quantises k and v into the pool behind each sequence's cache rows.  q, k, v: [n_rows][heads * d_head], rows may
     be strided (column blocks of one projection); q None: keys and values only.  -> rotated queries (q_out)."""
     n, width = rows.n_rows, kv.n_kv_heads * ctx.d_head
-    at = _kv4_args(ctx, kv, rows, pool)
+    _kv4_match(ctx, kv, rows)
+    at = _kv4_pool(ctx, kv, pool)
     kp, kld = _kv4_strided(ctx, k, n, width, "k")
     vp, vld = _kv4_strided(ctx, v, n, width, "v")
     if kld != vld:
@@ -485,7 +486,8 @@ def ghd_kv4_append(ctx: Ctx, kv: Kv4Cache, rows: Kv4Rows, pool, q, k, v, q_out=N
 def ghd_kv4_attention(ctx: Ctx, kv: Kv4Cache, rows: Kv4Rows, pool, q, out=None):
     """Attention of the new rows (rotated queries q [n_rows][n_heads * d_head]) over the paged 4-bit cache."""
     numel = rows.n_rows * ctx.n_heads * ctx.d_head
-    at = _kv4_args(ctx, kv, rows, pool)
+    _kv4_match(ctx, kv, rows)
+    at = _kv4_pool(ctx, kv, pool)
     qp = _need(q, ctx.dtype, "q", numel, ctx.dev)
     out = torch.zeros_like(q) if out is None else out
     ctx._check(ctx.lib.ghd_kv4_attention(ctx.handle, kv.ref, rows.ref, at, qp, _need(out, ctx.dtype, "out", numel, ctx.dev)))
@@ -495,14 +497,19 @@ def ghd_kv4_attention(ctx: Ctx, kv: Kv4Cache, rows: Kv4Rows, pool, q, out=None):
 def ghd_kv4_read(ctx: Ctx, kv: Kv4Cache, pool, row_start, n_rows: int, first=None, k_out=None, v_out=None):
     """Cache rows first[s] + i (first None: the new rows' places) in the storage type -> (k, v) [n_rows][n_kv_heads * d_head]."""
     rows = Kv4Rows(row_start, n_rows)
-    at = _kv4_args(ctx, kv, rows, pool)
-    n, width = rows.n_rows, kv.n_kv_heads * ctx.d_head
-    if k_out is None and v_out is None:
-        k_out, v_out = torch.empty((2, max(n, 0), width), dtype=ctx.dtype, device=ctx.device).unbind()
-    k_out = torch.empty((n, width), dtype=ctx.dtype, device=ctx.device) if k_out is None else k_out
-    v_out = torch.empty((n, width), dtype=ctx.dtype, device=ctx.device) if v_out is None else v_out
-    ctx._check(ctx.lib.ghd_kv4_read(ctx.handle, kv.ref, rows.ref, at, None if first is None else _need(first, torch.int32, "first", kv.n_seqs, ctx.dev),
-                                    _need(k_out, ctx.dtype, "k_out", n * width, ctx.dev), _need(v_out, ctx.dtype, "v_out", n * width, ctx.dev)))
+    _kv4_match(ctx, kv, rows)
+    at = _kv4_pool(ctx, kv, pool)
+    n, width, kp, vp = rows.n_rows, kv.n_kv_heads * ctx.d_head, None, None
+    if k_out is None and v_out is None and n >= 0:
+        k_out, v_out = torch.empty((2, n, width), dtype=ctx.dtype, device=ctx.device).unbind()
+        kp, vp = k_out.data_ptr(), v_out.data_ptr()
+    else:
+        k_out = torch.empty((n, width), dtype=ctx.dtype, device=ctx.device) if k_out is None else k_out
+        v_out = torch.empty((n, width), dtype=ctx.dtype, device=ctx.device) if v_out is None else v_out
+        kp, vp = _need(k_out, ctx.dtype, "k_out", n * width, ctx.dev), _need(v_out, ctx.dtype, "v_out", n * width, ctx.dev)
+    st = ctx.lib.ghd_kv4_read(ctx.handle, kv.ref, rows.ref, at, None if first is None else _need(first, torch.int32, "first", kv.n_seqs, ctx.dev), kp, vp)
+    if st:
+        ctx._check(st)
     return k_out, v_out
 
 
@@ -510,7 +517,7 @@ def ghd_kv4_commit(ctx: Ctx, kv: Kv4Cache, rows: Kv4Rows, pools, results=None):
     """Keeps the accepted rows of every sequence in all pools (a list, or one tensor [n_layers][...]) and advances kv.kv_len.
     results: int32 [n_seqs][514] as ghd_accept writes them; None keeps every new row (pools are not touched)."""
     _kv4_match(ctx, kv, rows)
-    ptrs = [] if results is None else [_kv4_args(ctx, kv, rows, p) for p in pools]
+    ptrs = [] if results is None else [_kv4_pool(ctx, kv, p) for p in pools]
     arr = (C.c_void_p * max(len(ptrs), 1))(*ptrs)
     ctx._check(ctx.lib.ghd_kv4_commit(ctx.handle, kv.ref, rows.ref, arr, len(ptrs),
                                       None if results is None else _need(results, torch.int32, "results", kv.n_seqs * (2 + 2 * GHD_MAX_NODES), ctx.dev)))
