@@ -51,7 +51,8 @@ typedef enum ghd_dtype { GHD_F32 = 0, GHD_F16 = 1 } ghd_dtype;
 typedef enum ghd_option {
     GHD_OPT_GEMM_PATH = 0,    /* 0 auto, 1 SIMT kernels, 2 tcgen05 kernels (GHD_F16 only)   */
     GHD_OPT_ATTN_SPLITS = 1,  /* number of KV splits of the attention (>= 1), 0 auto         */
-    GHD_OPT_ATTN_PATH = 2,    /* 0 auto, 1 SIMT kernel, 2 tcgen05 kernel (GHD_F16 only)      */
+    GHD_OPT_ATTN_PATH = 2,    /* 0 auto, 1 SIMT kernel, 2 tcgen05 kernel (GHD_F16 only); ghd_kv4_attention: 1 the
+                                 kernel with tiles of at most 16 query rows, 2 the tcgen05 kernel (GHD_F16 only) */
     GHD_OPT_GRAPH = 3,        /* ghd_verify_step: 0/1 = launch kernels directly, 2 = replay a
                                  CUDA graph captured on first use for the same arguments    */
     GHD_OPT_GEMM_CTAS = 4,    /* CTAs of the tcgen05 GEMM (0 = one per SM)                   */
@@ -301,7 +302,7 @@ typedef struct ghd_kv4 {
     int32_t n_seqs;             /* 1 .. GHD_MAX_SEQS                                             */
     int32_t n_pages;            /* pages of every pool                                           */
     int32_t page_rows;          /* 16, 32, 64 or 128                                             */
-    int32_t max_pages;          /* columns of the page table: max_pages * page_rows < 2^31        */
+    int32_t max_pages;          /* columns of the page table: max_pages * page_rows <= 2^30       */
     int32_t n_kv_heads;         /* divides cfg.n_heads: query head h reads head h / (n_heads / n_kv_heads) */
     const int32_t *page_table;  /* dev [n_seqs][max_pages]; entries past a sequence's rows are not read */
     int32_t *kv_len;            /* dev [n_seqs]: rows in the cache                                */
@@ -345,7 +346,7 @@ ghd_status ghd_kv4_read(ghd_ctx *ctx, const ghd_kv4 *kv, const ghd_kv4_rows *row
                         void *k_out, void *v_out);
 
 /* What a step keeps (ghd_kv_commit over pages): results_dev[s] is what ghd_accept wrote for sequence s; its accepted rows
- * move from kv_len[s] + nodes[j] to kv_len[s] + j, j = 1 .. n_matched, in each of the n_layers pools (HOST array), and
+ * move from kv_len[s] + nodes[j] to kv_len[s] + j, j = 1 .. n_matched, in each of the n_layers pools (HOST array; no pool twice), and
  * kv_len[s] grows by n_matched + 1.  A sequence without new rows keeps its length.  results_dev NULL: every new row is
  * kept, kv_len[s] grows by the sequence's number of new rows (a prompt) and nothing moves (pools may be NULL). */
 ghd_status ghd_kv4_commit(ghd_ctx *ctx, const ghd_kv4 *kv, const ghd_kv4_rows *rows, void *const *pools, int32_t n_layers,

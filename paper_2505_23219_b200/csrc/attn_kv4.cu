@@ -513,8 +513,16 @@ ghd_status launch_attn_kv4(ghd_ctx* c, const Kv4View& w, const ghd_kv4_rows* row
     p.scale = 1.0f / sqrtf((float)m.d_head);
     p.part = c->gemm_part; p.counters = c->counters;
     const int64_t avg = ((int64_t)rows->n_rows * p.group + w.n_seqs - 1) / w.n_seqs;      // query rows of a sequence and head, on average
-    if (m.dtype == GHD_F32) return m.d_head == 64 ? launch_narrow<float, 64, 1>(c, p) : launch_narrow<float, 128, 1>(c, p);
-    if (avg > 16) return launch_attn_kv4_tc(c, p);
+    if (m.dtype == GHD_F32) {
+        if (c->opt_attn_path == 2) return fail(c, GHD_EUNSUPPORTED, "kv4_attention: the tcgen05 kernel takes GHD_F16 only");
+        return m.d_head == 64 ? launch_narrow<float, 64, 1>(c, p) : launch_narrow<float, 128, 1>(c, p);
+    }
+    // The tcgen05 kernel for tiles of many rows.  Up to 32 rows two tiles of this file's kernel cost the same a key and start sooner (8
+    // sequences, 32 heads, 32 rows over 512 / 1024 / 2048 keys: 33 / 39 / 60 us here, 37 / 43 / 62 there; over none 23 and 26); up to 64
+    // while its tiles leave half of the SMs free (32 tiles over 256 / 2048 keys: 16 / 19 us here, 20 / 26 there; 128 tiles over 1024: 30 and
+    // 28); 128 rows: 24 / 43 / 53 us over 512 .. 2048 keys here, 22 / 32 / 37 there.
+    const int64_t tiles = (avg + 15) / 16 * w.heads * w.n_seqs;
+    if (c->opt_attn_path == 2 || (c->opt_attn_path == 0 && avg > 32 && (avg > 64 || 2 * tiles > c->sm_count))) return launch_attn_kv4_tc(c, p);
     if (m.d_head == 64) return avg <= 8 ? launch_narrow<__half, 64, 1>(c, p) : launch_narrow<__half, 64, 2>(c, p);
     return avg <= 8 ? launch_narrow<__half, 128, 1>(c, p) : launch_narrow<__half, 128, 2>(c, p);
 }

@@ -35,14 +35,11 @@ using namespace kv4;
 constexpr int UNIT = 128;                      // keys of a unit (MMA M of S^T, MMA K of O^T)
 constexpr int N = 64;                          // query rows of a tile; tiles of 128 rows unpack each key half as often and measured slower
                                                // (256 nodes, 13B shape, 4096 rows: 108 us against 90): their code does not fit the cache
-#ifndef KV4_SOFT
-#define KV4_SOFT 256
-#endif
-constexpr int SOFT = KV4_SOFT, CONV = 256;     // threads of the softmax and of the unpacking warps
+constexpr int SOFT = 256, CONV = 256;          // threads of the softmax and of the unpacking warps
 constexpr int PARTS = SOFT / 128;              // 128 threads (one a key of four) share query rows, as pairs of blocks of eight: pair part, part + PARTS, ...
 constexpr int THREADS = SOFT + CONV + 128, SW = SOFT / 32, CW = SW + CONV / 32;      // first unpacking warp, first of the others
 // registers a thread after the split by warpgroups, within those launched with
-constexpr int REGS_LAUNCH = SOFT == 512 ? 72 : 96, REGS_SOFT = SOFT == 512 ? 80 : 152, REGS_CONV = 56, REGS_ISSUE = 56;
+constexpr int REGS_LAUNCH = 96, REGS_SOFT = 152, REGS_CONV = 56, REGS_ISSUE = 56;
 static_assert(SOFT * REGS_SOFT + CONV * REGS_CONV + 128 * REGS_ISSUE <= THREADS * REGS_LAUNCH && THREADS * REGS_LAUNCH <= 65536, "register split");
 constexpr float RAISE = 8.f;
 constexpr int LEAD = 6;                        // an item's fixed cost in units (8 ragged trees: 0: 410 us, 4: 147, 6: 133, 10: 136, 16: 142)

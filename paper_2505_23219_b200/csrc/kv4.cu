@@ -449,7 +449,7 @@ ghd_status check_kv4(ghd_ctx* c, const ghd_kv4* kv, const ghd_kv4_rows* rows) {
     if (kv->n_seqs < 1 || kv->n_seqs > GHD_MAX_SEQS) return fail(c, GHD_EINVAL, "kv4: n_seqs outside [1, GHD_MAX_SEQS]");
     if (kv->page_rows != 16 && kv->page_rows != 32 && kv->page_rows != 64 && kv->page_rows != 128)
         return fail(c, GHD_EINVAL, "kv4: page_rows is not 16, 32, 64 or 128");
-    if (kv->n_pages < 1 || kv->max_pages < 1 || (int64_t)kv->max_pages * kv->page_rows > 0x7fffffffll) return fail(c, GHD_EINVAL, "kv4: bad page counts");
+    if (kv->n_pages < 1 || kv->max_pages < 1 || (int64_t)kv->max_pages * kv->page_rows > (1ll << 30)) return fail(c, GHD_EINVAL, "kv4: bad page counts");
     if (kv->n_kv_heads < 1 || c->cfg.n_heads % kv->n_kv_heads) return fail(c, GHD_ESHAPE, "kv4: n_kv_heads does not divide n_heads");
     if (!kv->page_table || !kv->kv_len || !rows->row_start) return fail(c, GHD_EINVAL, "kv4: null page table, lengths or row starts");
     if (rows->n_rows < 0) return fail(c, GHD_EINVAL, "kv4: negative n_rows");

@@ -160,6 +160,41 @@ def test_attention_against_the_oracle(ghd, H, Hk, d, dtype, R, lens, cnt, tree):
     check_attention(ghd, su, vis, words)
 
 
+TILED = [
+    (4, 4, 128, "f16", 64, [130], [1]),
+    (2, 2, 128, "f16", 128, [0, 1], [17, 64]),
+    (2, 2, 64, "f16", 16, [127, 0, 128, 129, 5], [63, 64, 0, 65, 1]),
+    (6, 2, 128, "f16", 32, [300, 0], [21, 22]),               # 63 and 66 rows of a head: tiles that end inside a node's group
+    (5, 1, 64, "f16", 128, [640, 383], [1, 30]),
+    (2, 1, 128, "f16", 16, [33], [256]),
+    (3, 3, 64, "f16", 64, [1100], [40]),                      # a head's keys over several blocks
+    (16, 16, 128, "f16", 32, [0, 3, 90, 0, 31], [2, 1, 9, 33, 70]),
+]
+
+
+@pytest.mark.parametrize("path", [1, 2], ids=["rows", "tcgen05"])
+@pytest.mark.parametrize("tree", [True, False], ids=["tree", "causal"])
+@pytest.mark.parametrize("H,Hk,d,dtype,R,lens,cnt", TILED)
+def test_both_kernels_on_tiles_of_many_rows(ghd, H, Hk, d, dtype, R, lens, cnt, tree, path):
+    su = Setup(ghd, H, Hk, d, dtype, R, lens, cnt, 29 * H + R + len(lens), behind=3)
+    ghd.ghd_set_option(su.ctx, 2, path)
+    if tree:
+        vis, words = su.trees()
+    else:
+        vis, words = [np.ones((n, n), bool) for n in cnt], None
+    check_attention(ghd, su, vis, words)
+
+
+def test_more_sequences_than_blocks(ghd):
+    """1024 sequences, the most a call takes, of no, one or a few rows each."""
+    r = np.random.RandomState(3)
+    lens, cnt = r.randint(0, 40, 1024).tolist(), r.randint(0, 4, 1024).tolist()
+    for path in (1, 2):
+        su = Setup(ghd, 2, 1, 64, "f16", 16, lens, cnt, 37, behind=1)
+        ghd.ghd_set_option(su.ctx, 2, path)
+        check_attention(ghd, su, [np.ones((n, n), bool) for n in cnt], None)
+
+
 @pytest.mark.parametrize("dtype", ["f16", "f32"])
 def test_rows_that_see_nothing_get_zeros_and_bits_above_the_diagonal_count_for_nothing(ghd, dtype):
     su = Setup(ghd, 4, 2, 64, dtype, 16, [0, 20], [6, 6], 5)
@@ -586,3 +621,167 @@ def test_a_decode_loop_over_the_paged_cache_agrees_with_decoding_one_row_at_a_ti
     three, first = dev(np.array([0, 3], np.int32)), dev(np.array([0], np.int32))
     for x, y in zip(ghd.ghd_kv4_read(ctx, kv_c, pool_c[0], three, 3, first=first), ghd.ghd_kv4_read(ctx, kv_a, pool_a[0], three, 3, first=first)):
         assert bool((x == y).all())
+
+
+def on_path(ghd, ctx, path):
+    ghd.ghd_set_option(ctx, 2, path)
+
+
+def test_special_rows_in_the_tcgen05_kernel(ghd):
+    """A row that sees nothing, one that sees the cache alone, a key of NaN, a value of infinity and a query of NaN, among 40 rows."""
+    su = Setup(ghd, 4, 2, 128, "f16", 32, [0, 37], [40, 40], 91)
+    on_path(ghd, su.ctx, 2)
+    vis, words = su.trees()
+    words[7] = 0
+    vis[0][7] = False
+    words[40 + 11] = 0
+    vis[1][11] = False
+    for node, which in ((1, 0), (2, 1)):
+        page, row = okv4.slots(su.table, su.R, 1, 37 + node)
+        for h in range(2):
+            su.pool.put(which, page, row, h, su.pool.codes(which, page, row, h), np.nan if which == 0 else np.inf, 0.5)
+    su.dpool.copy_(dev(su.pool.data.reshape(-1)))
+    collect(su)
+    q = su.r.randn(80, 4, 128).astype(np.float16)
+    q[20, 1, 5] = np.nan
+    out = ghd.ghd_kv4_attention(su.ctx, su.kv, ghd.Kv4Rows(dev(su.start), 80, mask=dev(words)), su.dpool, dev(q.reshape(80, -1)))
+    ghd.ghd_sync_status(su.ctx)
+    got = out.double().cpu().numpy().reshape(80, 4, 128)
+    assert (got[7] == 0).all() and np.isnan(got[20, 1]).all()
+    clean = np.ones((80, 4), bool)
+    clean[20, 1] = False
+    sees_nan = np.tril(vis[1])[:, 1] | np.tril(vis[1])[:, 2]
+    clean[40:][sees_nan] = False
+    assert not np.isfinite(got[40:][sees_nan]).all(-1).any() and clean.sum() > 200
+    q[20, 1] = 0
+    with np.errstate(all="ignore"):
+        want = okv4.attention(su.pool, su.table, su.lens, su.start, vis, q)
+    assert (np.abs(got - want) <= attention_tolerance(su, np.nan_to_num(q))(want))[clean].all()
+
+
+@pytest.mark.parametrize("path", [1, 2], ids=["rows", "tcgen05"])
+def test_scores_and_scales_that_grow_along_the_cache(ghd, path):
+    """Scores rise by far more than the reference's slack every few keys, and V's scales by a factor of 10^4: references and the
+    exponent have to follow.  Late keys carry nearly all weight, so the output is close to their values."""
+    su = Setup(ghd, 2, 2, 128, "f16", 16, [700], [70], 93, garbage=False)
+    on_path(ghd, su.ctx, path)
+    for t in range(770):
+        page, row = okv4.slots(su.table, 16, 0, t)
+        for h in range(2):
+            x = np.full(128, 0.004 * t, np.float32)
+            x[::2] += 0.5
+            su.pool.put(0, page, row, h, *okv4.quantise(x, "f16"))
+            su.pool.put(1, page, row, h, su.pool.codes(1, page, row, h), 0.01 * 10 ** (4 * t / 770), -0.07 * 10 ** (4 * t / 770))
+    su.dpool.copy_(dev(su.pool.data.reshape(-1)))
+    collect(su)
+    vis = [np.tril(np.ones((70, 70), bool))]
+    q = np.abs(su.r.randn(70, 2, 128)).astype(np.float16)
+    out = ghd.ghd_kv4_attention(su.ctx, su.kv, ghd.Kv4Rows(dev(su.start), 70), su.dpool, dev(q.reshape(70, -1)))
+    ghd.ghd_sync_status(su.ctx)
+    got = out.double().cpu().numpy().reshape(70, 2, 128)
+    want = okv4.attention(su.pool, su.table, su.lens, su.start, vis, q)
+    assert np.isfinite(got).all() and (np.abs(got - want) <= attention_tolerance(su, q)(want)).all()
+
+
+@pytest.mark.parametrize("path", [1, 2], ids=["rows", "tcgen05"])
+def test_the_same_bits_every_time_over_many_blocks(ghd, path):
+    su = Setup(ghd, 4, 4, 128, "f16", 64, [900, 10, 0, 333], [33, 64, 5, 0], 95)
+    on_path(ghd, su.ctx, path)
+    vis, words = su.trees()
+    n = su.n
+    q = dev(su.r.randn(n, 4 * 128).astype(np.float16))
+    rows = ghd.Kv4Rows(dev(su.start), n, mask=dev(words))
+    first = ghd.ghd_kv4_attention(su.ctx, su.kv, rows, su.dpool, q).clone()
+    for _ in range(20):
+        assert bool((ghd.ghd_kv4_attention(su.ctx, su.kv, rows, su.dpool, q) == first).all())
+    ghd.ghd_sync_status(su.ctx)
+
+
+def test_two_contexts_on_two_streams_at_once(ghd):
+    """Each context has its own workspace, so calls of two of them may overlap."""
+    import torch
+    sets = []
+    for i in range(2):
+        stream = torch.cuda.Stream()
+        with torch.cuda.stream(stream):
+            su = Setup(ghd, 4, 4, 128, "f16", 64, [800 + 100 * i, 10], [70, 3], 96 + i)
+            vis, words = su.trees()
+            q = dev(su.r.randn(su.n, 4 * 128).astype(np.float16))
+            rows = ghd.Kv4Rows(dev(su.start), su.n, mask=dev(words))
+            alone = ghd.ghd_kv4_attention(su.ctx, su.kv, rows, su.dpool, q).clone()
+            stream.synchronize()
+            sets.append((stream, su, q, rows, alone, torch.empty_like(q)))
+    for _ in range(10):
+        for stream, su, q, rows, alone, out in sets:
+            with torch.cuda.stream(stream):
+                ghd.ghd_kv4_attention(su.ctx, su.kv, rows, su.dpool, q, out=out)
+    torch.cuda.synchronize()
+    for stream, su, q, rows, alone, out in sets:
+        ghd.ghd_sync_status(su.ctx)
+        assert bool((out == alone).all())
+
+
+@pytest.mark.parametrize("dtype,d", [("f16", 64), ("f16", 128), ("f32", 64), ("f32", 128)])
+def test_append_of_ties_and_of_the_ends_of_the_range(ghd, dtype, d):
+    """Quotients that are exactly a half, rows of one value, of the largest and of the smallest values: codes bit for bit."""
+    su = Setup(ghd, 2, 2, d, dtype, 16, [0], [9], 97, garbage=False)
+    r = np.random.RandomState(5)
+    top = 60000.0 if dtype == "f16" else 3.0e38
+    tiny = 6e-8 if dtype == "f16" else 1.4e-45
+    v = np.zeros((9, 2, d), np.float64)
+    v[0] = r.randint(0, 31, (2, d)) * 0.5                          # with ends 0 and 15: scale 1, halves
+    v[0, :, 0], v[0, :, 1] = 0, 15
+    v[1] = -v[0] * 0.25 - 3
+    v[2] = 0.75
+    v[3] = r.uniform(-top, top, (2, d))
+    v[3, :, 0], v[3, :, 1] = -top, top
+    v[4] = r.randint(0, 40, (2, d)) * tiny                         # below the normal range
+    v[5] = r.randint(0, 2, (2, d)) * tiny                          # the scale rounds to 0
+    v[6] = 1000 + r.randint(0, 3, (2, d))                          # the minimum's rounding against a small scale
+    v[7] = np.where(r.rand(2, d) < 0.5, -0.0, 0.0)
+    v[8] = r.randn(2, d) * np.exp2(r.randint(-12, 12, (2, d)))
+    v = v.astype(su.np_t)
+    rows = ghd.Kv4Rows(dev(su.start), 9)
+    flat = dev(v.reshape(9, -1))
+    pos = dev(np.zeros(9, np.int32))                               # no rotation: K gets the same rows
+    ghd.ghd_kv4_append(su.ctx, su.kv, ghd.Kv4Rows(dev(su.start), 9, pos=pos), su.dpool, None, flat, flat)
+    ghd.ghd_sync_status(su.ctx)
+    okv4.append(su.pool, su.table, su.lens, su.start, np.zeros(9, np.int32), v, v, v, THETA)
+    got = okv4.Pool(su.pool.data.shape[0], 2, 16, d, dtype, data=su.dpool.cpu().numpy().reshape(su.pool.data.shape))
+    page, row = okv4.slots(su.table, 16, 0, 7)
+    for which in (0, 1):
+        for h in (0, 1):                                           # of zeros of both signs either is the lowest: equal, but not the same bits
+            scale, mn = got.params(which, page, row, h)
+            assert scale == 0 and mn == 0
+            su.pool.put(which, page, row, h, su.pool.codes(which, page, row, h), scale, mn)
+    assert np.array_equal(got.data, su.pool.data)
+
+
+def test_more_refusals(ghd):
+    import torch
+    su = Setup(ghd, 4, 4, 64, "f32", 16, [4], [2], 98)
+    rows = ghd.Kv4Rows(dev(su.start), 2)
+    q = torch.zeros((2, 256), device="cuda")
+
+    def refused(name, fn):
+        launches = ghd.ghd_launch_count(su.ctx)
+        with pytest.raises(ghd.GhdError) as e:
+            fn()
+        assert e.value.name == name and ghd.ghd_launch_count(su.ctx) == launches
+
+    on_path(ghd, su.ctx, 2)
+    refused("GHD_EUNSUPPORTED", lambda: ghd.ghd_kv4_attention(su.ctx, su.kv, rows, su.dpool, q))
+    on_path(ghd, su.ctx, 0)
+    res = torch.zeros((1, 514), dtype=torch.int32, device="cuda")
+    refused("GHD_EINVAL", lambda: ghd.ghd_kv4_commit(su.ctx, su.kv, rows, [su.dpool, su.dpool], res))
+    refused("GHD_EINVAL", lambda: ghd.ghd_kv4_commit(su.ctx, su.kv, rows, [], res))
+    long = ghd.Kv4Cache(torch.zeros((1, (1 << 23) + 1), dtype=torch.int32, device="cuda"), su.kv_len, 128, 4, 1)
+    refused("GHD_EINVAL", lambda: ghd.ghd_kv4_attention(su.ctx, long, rows, su.dpool, q))
+    refused("GHD_EINVAL", lambda: ghd.ghd_kv4_attention(su.ctx, su.kv, rows, su.dpool.cpu(), q))
+    refused("GHD_EINVAL", lambda: ghd.ghd_kv4_attention(su.ctx, su.kv, rows, su.dpool, q, out=q.cpu()))
+    refused("GHD_EINVAL", lambda: ghd.ghd_kv4_read(su.ctx, su.kv, su.dpool, dev(su.start), 2, k_out=q[:1]))
+    refused("GHD_EINVAL", lambda: ghd.ghd_kv4_commit(su.ctx, su.kv, ghd.Kv4Rows(dev(su.start), -1), None))
+    with pytest.raises(ghd.GhdError):
+        ghd.Kv4Rows(torch.zeros(2, dtype=torch.int32), 2)
+    with pytest.raises(ghd.GhdError):
+        ghd.Kv4Rows(dev(np.zeros(4, np.int32))[::2], 2)
