@@ -285,6 +285,7 @@ class Ctx:
             if st != 0:
                 raise GhdError(st, "ghd_create")
             nbytes = self.lib.ghd_workspace_bytes(self.handle)
+            self.blank = torch.empty(0, dtype=self.dtype, device=self.device)      # outputs are made like it
             self.workspace = torch.empty(nbytes, dtype=torch.uint8, device=self.device)
             self._check(self.lib.ghd_set_workspace(self.handle, self.workspace.data_ptr(), nbytes))
 
@@ -477,7 +478,7 @@ def ghd_kv4_append(ctx: Ctx, kv: Kv4Cache, rows: Kv4Rows, pool, q, k, v, q_out=N
         width = ctx.n_heads * ctx.d_head
         qp, qld = _kv4_strided(ctx, q, n, width, "q")
         if q_out is None:
-            q_out = torch.empty((n, width), dtype=ctx.dtype, device=ctx.device)
+            q_out = ctx.blank.new_empty((n, width))
         op = _need(q_out, ctx.dtype, "q_out", n * width, ctx.dev)
     ctx._check(ctx.lib.ghd_kv4_append(ctx.handle, kv.ref, rows.ref, at, qp, qld, kp, vp, kld, op))
     return q_out
@@ -499,14 +500,14 @@ def ghd_kv4_read(ctx: Ctx, kv: Kv4Cache, pool, row_start, n_rows: int, first=Non
     rows = Kv4Rows(row_start, n_rows)
     _kv4_match(ctx, kv, rows)
     at = _kv4_pool(ctx, kv, pool)
-    n, width, kp, vp = rows.n_rows, kv.n_kv_heads * ctx.d_head, None, None
-    if k_out is None and v_out is None and n >= 0:
-        k_out, v_out = torch.empty((2, n, width), dtype=ctx.dtype, device=ctx.device).unbind()
-        kp, vp = k_out.data_ptr(), v_out.data_ptr()
-    else:
-        k_out = torch.empty((n, width), dtype=ctx.dtype, device=ctx.device) if k_out is None else k_out
-        v_out = torch.empty((n, width), dtype=ctx.dtype, device=ctx.device) if v_out is None else v_out
-        kp, vp = _need(k_out, ctx.dtype, "k_out", n * width, ctx.dev), _need(v_out, ctx.dtype, "v_out", n * width, ctx.dev)
+    shape = (rows.n_rows, kv.n_kv_heads * ctx.d_head)
+    if rows.n_rows < 0:
+        raise GhdError(1, "kv4_read: negative n_rows")
+    if k_out is None:
+        k_out = ctx.blank.new_empty(shape)
+    if v_out is None:
+        v_out = ctx.blank.new_empty(shape)
+    kp, vp = _need(k_out, ctx.dtype, "k_out", shape[0] * shape[1], ctx.dev), _need(v_out, ctx.dtype, "v_out", shape[0] * shape[1], ctx.dev)
     st = ctx.lib.ghd_kv4_read(ctx.handle, kv.ref, rows.ref, at, None if first is None else _need(first, torch.int32, "first", kv.n_seqs, ctx.dev), kp, vp)
     if st:
         ctx._check(st)

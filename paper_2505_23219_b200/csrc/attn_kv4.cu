@@ -515,6 +515,9 @@ ghd_status launch_attn_kv4(ghd_ctx* c, const Kv4View& w, const ghd_kv4_rows* row
     const int64_t avg = ((int64_t)rows->n_rows * p.group + w.n_seqs - 1) / w.n_seqs;      // query rows of a sequence and head, on average
     if (m.dtype == GHD_F32) {
         if (c->opt_attn_path == 2) return fail(c, GHD_EUNSUPPORTED, "kv4_attention: the tcgen05 kernel takes GHD_F16 only");
+        // two tiles of eight rows at a time where there are many (28 heads on 4, 5 sequences over 2048 keys: 2 x 7 rows 17 us in ones, 24 in
+        // twos; 8 x 7: 26 and 29; 16 x 7: 42 and 38; 88 x 7: 350 and 161)
+        if (avg > 64) return m.d_head == 64 ? launch_narrow<float, 64, 2>(c, p) : launch_narrow<float, 128, 2>(c, p);
         return m.d_head == 64 ? launch_narrow<float, 64, 1>(c, p) : launch_narrow<float, 128, 1>(c, p);
     }
     // The tcgen05 kernel for tiles of many rows.  Up to 32 rows two tiles of this file's kernel cost the same a key and start sooner (8

@@ -185,6 +185,14 @@ def test_both_kernels_on_tiles_of_many_rows(ghd, H, Hk, d, dtype, R, lens, cnt, 
     check_attention(ghd, su, vis, words)
 
 
+@pytest.mark.parametrize("tree", [True, False], ids=["tree", "causal"])
+@pytest.mark.parametrize("H,Hk,d,R,lens,cnt", [(4, 1, 64, 16, [100, 0], [30, 20]), (2, 2, 128, 32, [200], [90]), (3, 1, 128, 128, [129, 5, 0], [64, 1, 33]), (2, 2, 64, 64, [900], [70])])
+def test_many_rows_in_float_mode(ghd, H, Hk, d, R, lens, cnt, tree):
+    su = Setup(ghd, H, Hk, d, "f32", R, lens, cnt, 31 * H + R + len(lens), behind=3)
+    vis, words = su.trees() if tree else ([np.ones((n, n), bool) for n in cnt], None)
+    check_attention(ghd, su, vis, words)
+
+
 def test_more_sequences_than_blocks(ghd):
     """1024 sequences, the most a call takes, of no, one or a few rows each."""
     r = np.random.RandomState(3)
