@@ -165,6 +165,26 @@ __device__ __forceinline__ void bulk_load(uint32_t dst, const void* src, uint32_
     asm volatile("cp.async.bulk.shared::cluster.global.mbarrier::complete_tx::bytes [%0], [%1], %2, [%3];" ::"r"(dst), "l"(src), "r"(bytes), "r"(bar) : "memory");
 }
 
+// two 32-bit products and sums in one instruction
+__device__ __forceinline__ uint64_t bits2(float2 a) { return (uint64_t)__float_as_uint(a.x) | (uint64_t)__float_as_uint(a.y) << 32; }
+__device__ __forceinline__ float2 pair2(uint64_t a) { return make_float2(__uint_as_float((uint32_t)a), __uint_as_float((uint32_t)(a >> 32))); }
+__device__ __forceinline__ float2 fma2(float2 a, float2 b, float2 c) {
+    uint64_t r;
+    asm("fma.rn.f32x2 %0, %1, %2, %3;" : "=l"(r) : "l"(bits2(a)), "l"(bits2(b)), "l"(bits2(c)));
+    return pair2(r);
+}
+__device__ __forceinline__ float2 mul2(float2 a, float2 b) {
+    uint64_t r;
+    asm("mul.rn.f32x2 %0, %1, %2;" : "=l"(r) : "l"(bits2(a)), "l"(bits2(b)));
+    return pair2(r);
+}
+__device__ __forceinline__ float2 add2(float2 a, float2 b) {
+    uint64_t r;
+    asm("add.rn.f32x2 %0, %1, %2;" : "=l"(r) : "l"(bits2(a)), "l"(bits2(b)));
+    return pair2(r);
+}
+__device__ __forceinline__ float2 both(float a) { return make_float2(a, a); }
+
 // eight codes -> four packed pairs, nibbles in the order 0 4 1 5 2 6 3 7
 __device__ __forceinline__ void unpack8(uint32_t w, uint32_t* r, const HalfMagic& m) {
     const uint32_t x = w >> 8;
@@ -484,13 +504,12 @@ __global__ void __launch_bounds__(THREADS, 1) k_attn_kv4_tc(const __grid_constan
                 named_sync<1, SOFT>();                                    // the sums are read by everybody
             }
             // running sums and references of this thread's rows: rows 2 t + e of its blocks
-            // `base`: what a row's scores are taken against, its reference, or 0 while it has none (its bit 2 j + e of `none`)
-            float l[NB][2], ms[NB][2], base[NB][2];
+            // `neg`: less what a row's scores are taken against, its reference, or 0 while it has none (its bit 2 j + e of `none`)
+            float2 l[NB], ms[NB], neg[NB];
             uint32_t none = (1u << 2 * NB) - 1u;
 #pragma unroll
             for (int j = 0; j < NB; ++j)
-#pragma unroll
-                for (int e = 0; e < 2; ++e) l[j][e] = ms[j][e] = base[j][e] = 0.f;
+                l[j] = ms[j] = neg[j] = make_float2(0.f, 0.f);
             float vmul = 0x1p24f;                                         // 2^-e of V's scales
             // The scores of a unit are fetched while the one before is worked on: s[j][h] has the 16 keys 16 h of block j.
             uint32_t s[NB][2][4];
@@ -530,8 +549,10 @@ __global__ void __launch_bounds__(THREADS, 1) k_attn_kv4_tc(const __grid_constan
                     float tj = -INFINITY;
 #pragma unroll
                     for (int x = 0; x < 4; ++x) {
-                        sc[j][x][0] = fmaf(ks[x], __uint_as_float(s[j][x >> 1][2 * (x & 1)]), fmaf(km[x], qq.x, -base[j][0]));
-                        sc[j][x][1] = fmaf(ks[x], __uint_as_float(s[j][x >> 1][2 * (x & 1) + 1]), fmaf(km[x], qq.y, -base[j][1]));
+                        const float2 dot = make_float2(__uint_as_float(s[j][x >> 1][2 * (x & 1)]), __uint_as_float(s[j][x >> 1][2 * (x & 1) + 1]));
+                        const float2 v = fma2(both(ks[x]), dot, fma2(both(km[x]), qq, neg[j]));
+                        sc[j][x][0] = v.x;
+                        sc[j][x][1] = v.y;
                         tj = fmaxf(tj, fmaxf(sc[j][x][0], sc[j][x][1]));
                     }
                     if (col8(j) < cols) top = fmaxf(top, tj);             // (blocks behind the tile's rows hold anything)
@@ -592,9 +613,9 @@ __global__ void __launch_bounds__(THREADS, 1) k_attn_kv4_tc(const __grid_constan
                             if (up > (had ? 0.f : -INFINITY)) {           // the new reference is `up` above the base
                                 f = had ? ex2(-up) : 0.f;
                                 none &= ~(1u << (2 * j + e));
-                                base[j][e] += up;
-                                l[j][e] *= f;
-                                ms[j][e] *= f;
+                                (e ? neg[j].y : neg[j].x) -= up;
+                                (e ? l[j].y : l[j].x) *= f;
+                                (e ? ms[j].y : ms[j].x) *= f;
 #pragma unroll
                                 for (int x = 0; x < 4; ++x) sc[j][x][e] -= up;
                             }
@@ -641,16 +662,16 @@ __global__ void __launch_bounds__(THREADS, 1) k_attn_kv4_tc(const __grid_constan
                         uint32_t h4[4];
 #pragma unroll
                         for (int x = 0; x < 4; ++x) {
-                            float pv[2];
-#pragma unroll
-                            for (int e = 0; e < 2; ++e) {
-                                const float pe = ex2(sc[j][x][e]);
-                                l[j][e] += pe;
-                                pv[e] = pe * vs[x];
-                                if (PLAIN || ((vis >> (8 * j + 4 * e + x)) & 1u)) ms[j][e] = fmaf(pe, vm[x], ms[j][e]);
-                                else pv[e] = 0.f;                         // by selection: what a key holds stays out of rows that do not see it
+                            const float2 pe = make_float2(ex2(sc[j][x][0]), ex2(sc[j][x][1]));
+                            l[j] = add2(l[j], pe);
+                            float2 pv = mul2(pe, both(vs[x])), m2 = fma2(pe, both(vm[x]), ms[j]);
+                            if (!PLAIN) {                                 // by selection: what a key holds stays out of rows that do not see it
+                                const uint32_t at = vis >> (8 * j + x);
+                                if (!(at & 1u)) { pv.x = 0.f; m2.x = ms[j].x; }
+                                if (!(at & 16u)) { pv.y = 0.f; m2.y = ms[j].y; }
                             }
-                            const __half2 h2 = __floats2half2_rn(pv[0], pv[1]);
+                            ms[j] = m2;
+                            const __half2 h2 = __floats2half2_rn(pv.x, pv.y);
                             h4[x] = *reinterpret_cast<const uint32_t*>(&h2);
                         }
                         // lane's matrix row: key 32 quad + lane, query rows 8 blk .. 8 blk + 7
@@ -669,11 +690,11 @@ __global__ void __launch_bounds__(THREADS, 1) k_attn_kv4_tc(const __grid_constan
             for (int j = 0; j < NB; ++j)
 #pragma unroll
                 for (int e = 0; e < 2; ++e) {
-                    float a = l[j][e], c = ms[j][e];
+                    float a = e ? l[j].y : l[j].x, c = e ? ms[j].y : ms[j].x;
 #pragma unroll
                     for (int o = 4; o < 32; o <<= 1) { a += __shfl_xor_sync(0xffffffffu, a, o); c += __shfl_xor_sync(0xffffffffu, c, o); }
                     const int rl = col8(j) + 2 * t + e;
-                    if (g == 0) { sm->x[quad][rl] = a; sm->y[quad][rl] = c; if (quad == 0) sm->fac[rl] = (none >> (2 * j + e)) & 1u ? -INFINITY : base[j][e]; }
+                    if (g == 0) { sm->x[quad][rl] = a; sm->y[quad][rl] = c; if (quad == 0) sm->fac[rl] = (none >> (2 * j + e)) & 1u ? -INFINITY : -(e ? neg[j].y : neg[j].x); }
                 }
             named_sync<1, SOFT>();
             if (tid < N) {
