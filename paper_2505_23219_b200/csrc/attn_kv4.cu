@@ -318,11 +318,11 @@ __global__ void __launch_bounds__(WARPS * 32, Narrow<T, D, NT>::BLOCKS) k_attn_k
                             top = fmaxf(top, v);
                         }
                 }
-            bool over = ch == it.chunk0 || top > RAISE;
+            bool over = none != 0u || top > RAISE;                      // (a row's first keys may have had no page)
             uint32_t vis = 0xffffffffu;                                 // bit 8 nt + 4 z + e: score s[z][nt][e] counts
             if (__builtin_expect(!all, 0)) {
                 vis = 0u;
-                over = ch == it.chunk0;
+                over = false;
 #pragma unroll
                 for (int nt = 0; nt < NT; ++nt)
 #pragma unroll

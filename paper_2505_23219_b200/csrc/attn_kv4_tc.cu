@@ -506,7 +506,9 @@ __global__ void __launch_bounds__(THREADS, 1) k_attn_kv4_tc(const __grid_constan
             // running sums and references of this thread's rows: rows 2 t + e of its blocks
             // `neg`: less what a row's scores are taken against, its reference, or 0 while it has none (its bit 2 j + e of `none`)
             float2 l[NB], ms[NB], neg[NB];
-            uint32_t none = (1u << 2 * NB) - 1u;
+            uint32_t none = 0u;                                           // (no bits for blocks without rows)
+#pragma unroll
+            for (int j = 0; j < NB; ++j) if (col8(j) < cols) none |= 3u << 2 * j;
 #pragma unroll
             for (int j = 0; j < NB; ++j)
                 l[j] = ms[j] = neg[j] = make_float2(0.f, 0.f);
@@ -557,7 +559,7 @@ __global__ void __launch_bounds__(THREADS, 1) k_attn_kv4_tc(const __grid_constan
                     }
                     if (col8(j) < cols) top = fmaxf(top, tj);             // (blocks behind the tile's rows hold anything)
                 }
-                bool over = top > RAISE || k == 0;
+                bool over = top > RAISE || none != 0u;                    // (a row's first keys may have had no page)
                 uint32_t vis = 0xffffffffu;                               // bit 8 j + 4 e + x: row e of block j sees key x
                 if (__builtin_expect(!all, 0)) {
                     vis = 0u;

@@ -705,6 +705,36 @@ def test_the_same_bits_every_time_over_many_blocks(ghd, path):
     ghd.ghd_sync_status(su.ctx)
 
 
+@pytest.mark.parametrize("offset", [-8.0, 0.01, 8.0])
+@pytest.mark.parametrize("dtype,path,n", [("f16", 1, 3), ("f16", 1, 12), ("f16", 2, 40), ("f32", 0, 3)])
+def test_keys_without_a_page_before_those_with_one(ghd, dtype, path, n, offset):
+    """The first 320 rows have page ids that no pool has: the call reports it, and gives what the other rows alone give, whether
+    their scores are far below 0, near it or far above.  64 sequences share the pages, so that a block walks on from rows without
+    a page to rows with one."""
+    H, d, R, gone, S = 2, 128, 32, 10, 64
+    su = Setup(ghd, H, H, d, dtype, R, [1000], [n], 99, garbage=False)
+    for t in range(1000 + n):
+        page, row = okv4.slots(su.table, R, 0, t)
+        for h in range(H):
+            su.pool.put(0, page, row, h, *okv4.quantise((offset + 0.1 * su.r.randn(d)).astype(np.float32), dtype))
+    su.dpool.copy_(dev(su.pool.data.reshape(-1)))
+    on_path(ghd, su.ctx, path)
+    table = np.repeat(su.table, S, 0)
+    table[:, :gone] = -1
+    kv = ghd.Kv4Cache(dev(table), dev(np.full(S, 1000, np.int32)), R, H, su.kv.c.n_pages)
+    q = (1.0 + 0.2 * su.r.randn(n, H, d)).astype(su.np_t)
+    vis, words = su.trees()
+    rows = ghd.Kv4Rows(dev(np.arange(S + 1, dtype=np.int32) * n), S * n, mask=dev(np.tile(words[:n], (S, 1))))
+    out = ghd.ghd_kv4_attention(su.ctx, kv, rows, su.dpool, dev(np.tile(q.reshape(n, -1), (S, 1))))
+    with pytest.raises(ghd.GhdError):
+        ghd.ghd_sync_status(su.ctx)
+    su.table, su.lens = su.table[:, gone:].copy(), [1000 - gone * R]
+    collect(su)
+    want = okv4.attention(su.pool, su.table, su.lens, su.start, vis, q)
+    got = out.double().cpu().numpy().reshape(S, n, H, d)
+    assert (np.abs(got - want) <= attention_tolerance(su, q)(want)).all()
+
+
 def test_two_contexts_on_two_streams_at_once(ghd):
     """Each context has its own workspace, so calls of two of them may overlap."""
     import torch
