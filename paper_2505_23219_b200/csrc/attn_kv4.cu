@@ -489,10 +489,14 @@ __global__ void __launch_bounds__(WARPS * 32, Narrow<T, D, NT>::BLOCKS) k_attn_k
 template <typename T, int D, int NT>
 ghd_status launch_narrow(ghd_ctx* c, Kv4AttnParams& p) {
     using N = Narrow<T, D, NT>;
-    const int smem = ((N::SMEM + 15) & ~15) + (p.w.n_seqs + 1) * 8;
-    if (cudaFuncSetAttribute(k_attn_kv4<T, D, NT>, cudaFuncAttributeMaxDynamicSharedMemorySize, smem) != cudaSuccess) {
-        cudaGetLastError();
-        return fail(c, GHD_ECUDA, "kv4_attention: cannot raise dynamic shared memory");
+    constexpr int FIXED = (N::SMEM + 15) & ~15, VARIANT = (sizeof(T) == 2 ? 0 : 4) + (D == 64 ? 0 : 2) + NT - 1;
+    const int smem = FIXED + (p.w.n_seqs + 1) * 8;
+    if (!(c->attr_kv4 >> VARIANT & 1)) {                                 // once a context, for as many sequences as a call takes
+        if (cudaFuncSetAttribute(k_attn_kv4<T, D, NT>, cudaFuncAttributeMaxDynamicSharedMemorySize, FIXED + (GHD_MAX_SEQS + 1) * 8) != cudaSuccess) {
+            cudaGetLastError();
+            return fail(c, GHD_ECUDA, "kv4_attention: cannot raise dynamic shared memory");
+        }
+        c->attr_kv4 |= 1u << VARIANT;
     }
     p.ctas = c->sm_count * N::BLOCKS;
     const size_t have = (size_t)c->sm_count * 2 * 256 * 128;             // floats of the tile scratch (carve_workspace)

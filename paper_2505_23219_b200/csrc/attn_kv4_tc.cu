@@ -759,9 +759,13 @@ __global__ void __launch_bounds__(THREADS, 1) k_attn_kv4_tc(const __grid_constan
 
 template <int D>
 ghd_status launch_tc(ghd_ctx* c, Kv4AttnParams& p) {
-    if (cudaFuncSetAttribute(k_attn_kv4_tc<D>, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)smem_bytes<D>(p.w.n_seqs)) != cudaSuccess) {
-        cudaGetLastError();
-        return fail(c, GHD_ECUDA, "kv4_attention: cannot raise dynamic shared memory");
+    constexpr int VARIANT = 8 + (D == 64 ? 0 : 1);
+    if (!(c->attr_kv4 >> VARIANT & 1)) {                                 // once a context, for as many sequences as a call takes
+        if (cudaFuncSetAttribute(k_attn_kv4_tc<D>, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)smem_bytes<D>(GHD_MAX_SEQS)) != cudaSuccess) {
+            cudaGetLastError();
+            return fail(c, GHD_ECUDA, "kv4_attention: cannot raise dynamic shared memory");
+        }
+        c->attr_kv4 |= 1u << VARIANT;
     }
     p.ctas = c->sm_count;
     launch_k(c, false, k_attn_kv4_tc<D>, dim3(p.ctas), dim3(THREADS), smem_bytes<D>(p.w.n_seqs), p);

@@ -256,6 +256,7 @@ ghd_status ghd_create(const ghd_model_cfg* cfg, void* cuda_stream, ghd_ctx** out
     c->kv_len_hint = 0;
     c->entry_fresh = c->opt_chain_calls ? 0 : 1;
     c->attr_gemm = c->attr_attn = c->attr_attn_small = false;
+    c->attr_kv4 = 0u;
     c->launches = 0;
     memset(c->path_count, 0, sizeof(c->path_count));
     c->tmaps = new std::map<TmapKey, std::vector<uint64_t>>();

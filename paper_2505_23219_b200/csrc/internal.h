@@ -111,6 +111,7 @@ struct ghd_ctx {
     // bookkeeping
     int entry_fresh;          // 1 until the first launch of a public call: that launch is fully serialised (see launch_k)
     bool attr_gemm, attr_attn, attr_attn_small;  // dynamic shared memory limits raised on this context's device
+    unsigned attr_kv4;        // ... of the 4-bit cache's attention kernels, a bit each
     int64_t launches;
     int64_t path_count[8];   // launches per kernel family (ghd_path)
     char err[256];

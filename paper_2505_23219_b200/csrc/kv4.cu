@@ -452,6 +452,8 @@ ghd_status check_kv4(ghd_ctx* c, const ghd_kv4* kv, const ghd_kv4_rows* rows) {
     if (kv->n_pages < 1 || kv->max_pages < 1 || (int64_t)kv->max_pages * kv->page_rows > (1ll << 30)) return fail(c, GHD_EINVAL, "kv4: bad page counts");
     if (kv->n_kv_heads < 1 || c->cfg.n_heads % kv->n_kv_heads) return fail(c, GHD_ESHAPE, "kv4: n_kv_heads does not divide n_heads");
     if (!kv->page_table || !kv->kv_len || !rows->row_start) return fail(c, GHD_EINVAL, "kv4: null page table, lengths or row starts");
+    if ((((uintptr_t)kv->page_table | (uintptr_t)kv->kv_len | (uintptr_t)rows->row_start | (uintptr_t)rows->pos) & 3) || ((uintptr_t)rows->mask & 7))
+        return fail(c, GHD_EINVAL, "kv4: a table, length, row start, position or mask that is not aligned to its type");
     if (rows->n_rows < 0) return fail(c, GHD_EINVAL, "kv4: negative n_rows");
     if (rows->mask && rows->mask_words < 1) return fail(c, GHD_EINVAL, "kv4: a mask needs mask_words >= 1");
     if (!c->ws) return fail(c, GHD_ENOSPACE, "no workspace set");
@@ -519,6 +521,7 @@ ghd_status ghd_kv4_attention(ghd_ctx* c, const ghd_kv4* kv, const ghd_kv4_rows* 
     if (st != GHD_OK) return st;
     if (!pool || !q || !out) return fail(c, GHD_EINVAL, "kv4_attention: null pool, q or out");
     if (!aligned16(pool) || !aligned16(q) || !aligned16(out)) return fail(c, GHD_EINVAL, "kv4_attention: pointers must be 16-byte aligned");
+    if (q == out) return fail(c, GHD_EINVAL, "kv4_attention: out may not be q");
     if (rows->n_rows == 0) return GHD_OK;
     OnDevice dev(c);
     c->entry_fresh = c->opt_chain_calls ? 0 : 1;
@@ -531,7 +534,8 @@ ghd_status ghd_kv4_read(ghd_ctx* c, const ghd_kv4* kv, const ghd_kv4_rows* rows,
     ghd_status st = check_kv4(c, kv, rows);
     if (st != GHD_OK) return st;
     if (!pool || (!k_out && !v_out)) return fail(c, GHD_EINVAL, "kv4_read: null pool, or neither output");
-    if (!aligned16(pool) || !aligned16(k_out) || !aligned16(v_out)) return fail(c, GHD_EINVAL, "kv4_read: pointers must be 16-byte aligned");
+    if (!aligned16(pool) || !aligned16(k_out) || !aligned16(v_out) || ((uintptr_t)first & 3)) return fail(c, GHD_EINVAL, "kv4_read: pointers must be 16-byte aligned (first: 4)");
+    if (k_out == v_out) return fail(c, GHD_EINVAL, "kv4_read: k_out and v_out are the same");
     if (rows->n_rows == 0) return GHD_OK;
     OnDevice dev(c);
     const Kv4View w = kv4_view(c, kv, rows);
@@ -549,6 +553,7 @@ ghd_status ghd_kv4_commit(ghd_ctx* c, const ghd_kv4* kv, const ghd_kv4_rows* row
     if (!c) return GHD_EINVAL;
     ghd_status st = check_kv4(c, kv, rows);
     if (st != GHD_OK) return st;
+    if ((uintptr_t)results & 3) return fail(c, GHD_EINVAL, "kv4_commit: results are not aligned");
     if (n_layers < 0 || (results && (n_layers < 1 || !pools))) return fail(c, GHD_EINVAL, "kv4_commit: no pools");
     for (int l = 0; results && l < n_layers; ++l)
         if (!pools[l] || !aligned16(pools[l])) return fail(c, GHD_EINVAL, "kv4_commit: a pool is null or not 16-byte aligned");

@@ -819,6 +819,11 @@ def test_more_refusals(ghd):
     refused("GHD_EINVAL", lambda: ghd.ghd_kv4_attention(su.ctx, su.kv, rows, su.dpool, q, out=q.cpu()))
     refused("GHD_EINVAL", lambda: ghd.ghd_kv4_read(su.ctx, su.kv, su.dpool, dev(su.start), 2, k_out=q[:1]))
     refused("GHD_EINVAL", lambda: ghd.ghd_kv4_commit(su.ctx, su.kv, ghd.Kv4Rows(dev(su.start), -1), None))
+    refused("GHD_EINVAL", lambda: ghd.ghd_kv4_attention(su.ctx, su.kv, rows, su.dpool, q, out=q))
+    refused("GHD_EINVAL", lambda: ghd.ghd_kv4_read(su.ctx, su.kv, su.dpool, dev(su.start), 2, k_out=q, v_out=q))
+    odd = ghd.Kv4Rows(dev(su.start), 2, mask=torch.ones((2, 1), dtype=torch.int64, device="cuda"))
+    odd.c.mask += 4                                                # what only a C caller can pass
+    refused("GHD_EINVAL", lambda: ghd.ghd_kv4_attention(su.ctx, su.kv, odd, su.dpool, q))
     with pytest.raises(ghd.GhdError):
         ghd.Kv4Rows(torch.zeros(2, dtype=torch.int32), 2)
     with pytest.raises(ghd.GhdError):
