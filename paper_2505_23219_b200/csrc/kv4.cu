@@ -158,7 +158,11 @@ constexpr int ROW_WARPS = 4;       // warps of a block; each has rows of its own
 // the K, V or q rows of HPW heads, D / 16 lanes each.  Lane j of a head holds the pairs t = 8 j .. 8 j + 7 with both halves (K, q),
 // so the rotation needs no exchange and its codes are two words; of V the 16 channels from 16 j on.  What the next two jobs
 // read is asked for ahead.  The row's angles (64-bit sincos, D / 2 of them) are shared out over the lanes and passed round by
-// shuffles.  Bytes bound it when there are many rows (q in and out, k and v in, 4.25 bits a value out), latency when few.
+// shuffles.  One row of 32 heads takes 4.3 us, a launch and a chain of loads.  8 ragged prompts of up to 2048 rows (32 heads on 8;
+// q in and out, k and v in, codes out: 277 MB) take 85 us, 3.3 TB/s: 43 M instructions at 1.8 an SM a clock, half of them the
+// codes of K and V, on 16 warps an SM (125 registers).  More warps with spills: 79 us, but one row 5.2; the queries in a launch
+// of their own, with half the registers: 76, but up to half as long again for 512 to 2048 rows in all.  32 bits instead of 64 for the
+// rotation or the angles would save 2 us.
 template <typename T, int D>
 __global__ void __launch_bounds__(ROW_WARPS * 32, 4) k_kv4_append(const __grid_constant__ Kv4View w, const __grid_constant__ RopeFreq fr, uint8_t* __restrict__ pool,
                                                                const int32_t* __restrict__ pos, const T* q, int64_t q_ld, const T* __restrict__ k,
@@ -306,7 +310,8 @@ __device__ __forceinline__ void decode8(uint32_t c, RowPar<__half> f, __half* y)
 }
 
 // A warp takes a row and every `slices`-th of its jobs: K and V of HPW heads, D / 8 lanes each; a lane decodes eight channels of
-// both (4 bytes in, 16 or 32 out).  AHEAD jobs' loads are under way together.  The bytes written bound it when there are many rows.
+// both (4 bytes in, 16 or 32 out).  AHEAD jobs' loads are under way together.  The bytes written bound it when there are many rows:
+// 8 sequences of up to 2048 rows, 32 heads (177 MB): 36 us, 4.8 TB/s (59 us with codes converted to 32 bits one by one).  13 rows: 2.6 us.
 template <typename T, int D>
 __global__ void __launch_bounds__(ROW_WARPS * 32) k_kv4_read(const __grid_constant__ Kv4View w, const uint8_t* __restrict__ pool, const int32_t* __restrict__ first,
                                                              T* __restrict__ k_out, T* __restrict__ v_out, int slices, int rows_each) {
@@ -360,12 +365,13 @@ __global__ void __launch_bounds__(ROW_WARPS * 32) k_kv4_read(const __grid_consta
 }
 
 // Block = one (pool, sequence, head); a lane owns one piece of a row: 16 bytes of K or V codes, or the scale and minimum
-// of K or V.  Accepted nodes rise and nodes[j] >= j, so a lane that moves its piece in ascending j never reads a piece it
-// has overwritten, and lanes own disjoint pieces: no synchronisation.
-constexpr int COMMIT_POOLS = 64;
+// of K or V.  Lanes own disjoint pieces: no synchronisation.  Eight rows of the path are read together and then written: what a
+// call costs is the latency of node, page and piece, one behind the other (16 sequences, paths of 5, 8 layers, both launches:
+// 6.2 us row by row, 5.0 so).  Accepted nodes rise and nodes[j] >= j, so no row is written before it has been read.
+constexpr int COMMIT_POOLS = 64, COMMIT_ROWS = 8;
 struct CommitPools { uint8_t* p[COMMIT_POOLS]; };
 
-__global__ void k_kv4_commit(Kv4View w, CommitPools pools, int es, const ghd_accept_result* __restrict__ results) {
+__global__ void __launch_bounds__(32) k_kv4_commit(const __grid_constant__ Kv4View w, const __grid_constant__ CommitPools pools, int es, const ghd_accept_result* __restrict__ results) {
     const int s = blockIdx.y, head = blockIdx.x % w.heads, layer = blockIdx.x / w.heads, lane = threadIdx.x;
     const Kv4Seq sq = kv4_load_seq(w, s);
     if (sq.n <= 0) return;
@@ -375,27 +381,40 @@ __global__ void k_kv4_commit(Kv4View w, CommitPools pools, int es, const ghd_acc
     const int R = 1 << w.shift, D = w.d_head, half = D / 32;         // 16-byte pieces of a row's codes
     if (lane >= 2 * half + 2) return;
     uint8_t* pool = pools.p[layer];
-    const int which = lane < half ? 0 : (lane < 2 * half ? 1 : lane - 2 * half);
-    for (int j = 1; j <= m; ++j) {
-        const int src = res->nodes[j];
-        if (src == j) continue;
-        if (src < j || src >= sq.n_new) {
-            atomicCAS(w.status, DEV_OK, DEV_KV4_ROWS);
-            continue;
+    const int which = lane < half ? 0 : (lane < 2 * half ? 1 : lane - 2 * half), bytes = lane < 2 * half ? 16 : 2 * es;
+    auto piece = [&](int page, int row) {
+        return pool + kv4_block_at(w, page, head) + (bytes == 16 ? kv4_code_at(R, D, which, row) + 16 * (lane - which * half) : kv4_param_at(R, D, es, which, row));
+    };
+#pragma unroll 1
+    for (int j0 = 1; j0 <= m; j0 += COMMIT_ROWS) {
+        uint4 v[COMMIT_ROWS];
+        int src[COMMIT_ROWS], pf[COMMIT_ROWS], pt[COMMIT_ROWS];
+#pragma unroll
+        for (int k = 0; k < COMMIT_ROWS; ++k) src[k] = j0 + k <= m ? res->nodes[j0 + k] : j0 + k;
+#pragma unroll
+        for (int k = 0; k < COMMIT_ROWS; ++k) {
+            const int j = j0 + k;
+            const bool moves = src[k] > j && src[k] < sq.n_new;
+            if (src[k] != j && !moves) atomicCAS(w.status, DEV_OK, DEV_KV4_ROWS);
+            pf[k] = moves ? kv4_page(w, s, sq.len + src[k]) : -1;
+            pt[k] = moves ? kv4_page(w, s, sq.len + j) : -1;
         }
-        const int from = sq.len + src, to = sq.len + j;
-        const int pf = kv4_page(w, s, from), pt = kv4_page(w, s, to);
-        if (pf < 0 || pt < 0) continue;
-        const uint8_t* a = pool + kv4_block_at(w, pf, head);
-        uint8_t* b = pool + kv4_block_at(w, pt, head);
-        const int rf = from & (R - 1), rt = to & (R - 1);
-        if (lane < 2 * half) {
-            const int at = 16 * (lane - which * half);
-            *reinterpret_cast<uint4*>(b + kv4_code_at(R, D, which, rt) + at) = *reinterpret_cast<const uint4*>(a + kv4_code_at(R, D, which, rf) + at);
-        } else if (es == 2) {
-            *reinterpret_cast<uint32_t*>(b + kv4_param_at(R, D, es, which, rt)) = *reinterpret_cast<const uint32_t*>(a + kv4_param_at(R, D, es, which, rf));
-        } else {
-            *reinterpret_cast<uint2*>(b + kv4_param_at(R, D, es, which, rt)) = *reinterpret_cast<const uint2*>(a + kv4_param_at(R, D, es, which, rf));
+#pragma unroll
+        for (int k = 0; k < COMMIT_ROWS; ++k) {
+            v[k] = make_uint4(0, 0, 0, 0);
+            if (pf[k] < 0 || pt[k] < 0) continue;
+            const uint8_t* a = piece(pf[k], (sq.len + src[k]) & (R - 1));
+            if (bytes == 16) v[k] = *reinterpret_cast<const uint4*>(a);
+            else if (bytes == 8) { const uint2 x = *reinterpret_cast<const uint2*>(a); v[k].x = x.x; v[k].y = x.y; }
+            else v[k].x = *reinterpret_cast<const uint32_t*>(a);
+        }
+#pragma unroll
+        for (int k = 0; k < COMMIT_ROWS; ++k) {
+            if (pf[k] < 0 || pt[k] < 0) continue;
+            uint8_t* b = piece(pt[k], (sq.len + j0 + k) & (R - 1));
+            if (bytes == 16) *reinterpret_cast<uint4*>(b) = v[k];
+            else if (bytes == 8) *reinterpret_cast<uint2*>(b) = make_uint2(v[k].x, v[k].y);
+            else *reinterpret_cast<uint32_t*>(b) = v[k].x;
         }
     }
 }

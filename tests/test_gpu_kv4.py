@@ -828,3 +828,19 @@ def test_more_refusals(ghd):
         ghd.Kv4Rows(torch.zeros(2, dtype=torch.int32), 2)
     with pytest.raises(ghd.GhdError):
         ghd.Kv4Rows(dev(np.zeros(4, np.int32))[::2], 2)
+
+
+@pytest.mark.parametrize("dtype,d", [("f16", 128), ("f32", 64)])
+def test_commit_of_long_paths_that_overlap_themselves(ghd, dtype, d):
+    """Paths of 8, 9 and 70 rows whose sources are the places of rows moved earlier, over page borders."""
+    lens, cnt = [13, 0, 100], [10, 40, 80]
+    su = Setup(ghd, 2, 1, d, dtype, 16, lens, cnt, 43)
+    paths = [(8, [0] + list(range(2, 10))), (9, [0] + sorted(np.random.RandomState(4).choice(np.arange(9, 40), 9, replace=False).tolist())), (70, [0] + list(range(9, 79)))]
+    host = [okv4.Pool(su.pool.data.shape[0], 1, 16, d, dtype, data=su.pool.data.copy())]
+    res = np.zeros((3, 514), np.int32)
+    for s, (m, nodes) in enumerate(paths):
+        res[s, 0], res[s, 1], res[s, 2:3 + m] = m, m + 1, nodes
+    ghd.ghd_kv4_commit(su.ctx, su.kv, ghd.Kv4Rows(dev(su.start), su.n), [su.dpool], dev(res))
+    ghd.ghd_sync_status(su.ctx)
+    assert su.kv_len.cpu().tolist() == okv4.commit(host, su.table, lens, su.start, paths) == [22, 10, 171]
+    assert np.array_equal(su.dpool.cpu().numpy(), host[0].data.reshape(-1))
