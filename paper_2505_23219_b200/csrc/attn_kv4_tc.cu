@@ -24,7 +24,7 @@
 // exponentials 500: the softmax warps' chain (fetch, scores, agreement on references, wait for a P buffer, weights, hand-over), at
 // 2.0 instructions an SM a clock; K and V are two units ahead.  An item costs about six units besides (queries in, filling and
 // draining, sums out, merge), a launch 6 us before the first.  Measured and dropped: 16 softmax warps on one unit, two groups of eight
-// on units in turn (142 us: 88 registers a thread spill), scores fetched a unit ahead of need by more than one, tiles of 128 rows.
+// on units in turn (142 us: 88 registers a thread spill), tiles of 128 rows.
 #include <cstddef>
 #include <cstdio>
 #include <type_traits>
