@@ -147,30 +147,46 @@ __global__ void __launch_bounds__(WARPS * 32, Narrow<T, D, NT>::BLOCKS) k_attn_k
     const Kv4Tiling til{w.heads, p.group, RT, CHUNK, LEAD};
     const int64_t units = unit_sums(w, til, sums, scratch);
     const int64_t per = kv4_units_per_cta(units, p.ctas);
-    int64_t u = per * blockIdx.x;
-    const int64_t u_end = u + per < units ? u + per : units;
+    const int64_t u_beg = per * blockIdx.x, u_end = u_beg + per < units ? u_beg + per : units;
+    if (u_beg >= u_end) return;                                                      // (the whole block)
     const int warp = __shfl_sync(0xffffffffu, (int)threadIdx.x >> 5, 0), lane = threadIdx.x & 31, g = lane >> 2, t = lane & 3;
     const int R = 1 << w.shift;
     const float sl2 = p.scale * KV4_LOG2E;
     const typename O_::Magic magic;
-    auto item_at = [&](int64_t x) { Kv4Item r; find_item(&w, &til, sums, x, u_end, &r); return r; };
+    // the block's item, and by warp the one that it loads rows of
+    __shared__ Kv4Item cur, ahead[WARPS];
+    if (threadIdx.x == 0) {
+        Kv4Item it = kv4_find_item(til, sums, w.n_seqs, [&](int s) { return kv4_load_seq(w, s); }, u_beg, u_end);
+        it.keys = kv4_tile_keys(til, it.q, it.tile);
+        cur = it;
+#pragma unroll
+        for (int k = 0; k < WARPS; ++k) ahead[k] = it;
+    }
+    __syncthreads();
 
     // ---- this warp's ring: 32 keys a stage, STAGES - 1 units ahead, over the borders of items
     uint8_t* ring = smem + warp * N::STAGES * N::STAGE;
     const uint32_t ring_a = (uint32_t)__cvta_generic_to_shared(ring);
-    int64_t lu = u;
-    int lch = 0, lend = 0, lkeys = 0, lseq = 0, lhead = 0, pages = -1, pbase = 0;
+    int lch, lend, lkeys, lseq, lhead, pages = -1, pbase;
+    bool lmore;
+    auto look_ahead = [&]() {
+        const Kv4Item& it = ahead[warp];
+        lch = it.chunk0; lend = it.chunk0 + it.take; lkeys = it.keys; lseq = it.seq; lhead = it.head;
+        lmore = it.next < u_end;
+        pbase = lch - 16;
+    };
+    look_ahead();
     // 16 rows are contiguous: lane's piece of them, and its place; lane (which, group, piece) of the scales
     constexpr int PIECES = N::ROW / 16, PER = 32 / PIECES, PP = es * 2;              // pieces of a row, rows a warp-wide copy covers, pieces of 16 keys' scales
     const uint32_t put = N::piece(lane / PIECES, lane % PIECES);
     const int pwhich = lane / (2 * PP), pgrp = lane / PP & 1, pc = lane % PP;
     const uint32_t pput = (pwhich ? N::VP_AT : N::P_AT) + pgrp * 32 * es + 16 * pc;
     auto load_next = [&](int i) {
-        while (lch >= lend && lu < u_end) {
-            const Kv4Item it = item_at(lu);
-            lch = it.chunk0; lend = it.chunk0 + it.take; lkeys = kv4_tile_keys(til, it.q, it.tile); lseq = it.seq; lhead = it.head;
-            lu = it.next;
-            pbase = lch - 16;
+        if (lch >= lend && lmore) {
+            __syncwarp();
+            if (lane == 0) advance_item<RT, CHUNK, LEAD>(&w, p.group, &ahead[warp], u_end);
+            __syncwarp();
+            look_ahead();
         }
         if (lch < lend) {
             if (lch >= pbase + 16) {                                                 // page ids of sixteen units: lane 2 u + h has unit pbase + u, keys 16 h on
@@ -216,10 +232,9 @@ __global__ void __launch_bounds__(WARPS * 32, Narrow<T, D, NT>::BLOCKS) k_attn_k
     }
     int i = 0;                                                          // unit of this CTA
 #pragma unroll 1
-    while (u < u_end) {
-        const Kv4Item it = item_at(u);
-        u = it.next;
-        if (it.take == 0) continue;
+    for (;;) {
+        const Kv4Item it = cur;
+        if (it.take == 0) break;                                        // (the run ends before the item's first chunk)
         const int rows = min(RT, it.q.n * p.group - it.tile * RT);      // query rows of this tile
 
         // ---- queries: lane (g, t) holds row 8 nt + g, channels [t D/4, (t + 1) D/4), pairs in the order the codes come in
@@ -486,7 +501,10 @@ __global__ void __launch_bounds__(WARPS * 32, Narrow<T, D, NT>::BLOCKS) k_attn_k
             __syncthreads();
             if (arrived) merge_item<T, D, 1>(p, it, RT, rows, c0, c1, warp, WARPS, xmerge, [] { __syncthreads(); });
         }
-        __syncthreads();                                                 // the exchange buffers are written again
+        if (it.next >= u_end) break;
+        __syncthreads();                                                 // everybody has the item, and the exchange buffers are written again
+        if (threadIdx.x == 0) advance_item<RT, CHUNK, LEAD>(&w, p.group, &cur, u_end);
+        __syncthreads();
     }
     cp_wait<0>();
 }

@@ -121,10 +121,15 @@ __device__ __forceinline__ int64_t unit_sums(const Kv4View& w, const Kv4Tiling& 
     return sums[w.n_seqs];
 }
 
-// kv4_find_item out of line: it is called from several places and its code is long (instruction fetch is what short
-// calls wait for).
-static __device__ __noinline__ void find_item(const Kv4View* w, const Kv4Tiling* t, const int64_t* sums, int64_t u, int64_t u_end, Kv4Item* out) {
-    *out = kv4_find_item(*t, sums, w->n_seqs, [&](int s) { return kv4_load_seq(*w, s); }, u, u_end);
+// An item in shared memory becomes the one behind it, by one thread.  Out of line: it is called from several places, and
+// instruction fetch is what short calls wait for.
+template <int TILE_ROWS, int CHUNK, int LEAD>
+__device__ __noinline__ void advance_item(const Kv4View* w, int group, Kv4Item* it, int64_t u_end) {
+    const Kv4Tiling t{w->heads, group, TILE_ROWS, CHUNK, LEAD};
+    Kv4Item x = *it;
+    kv4_next_item(t, [&](int s) { return kv4_load_seq(*w, s); }, x, u_end);
+    x.keys = kv4_tile_keys(t, x.q, x.tile);
+    *it = x;
 }
 
 // Adds the partial sums that CTAs c0 .. c1 left of one item, in that order, and writes its rows.  A warp takes RB rows at a

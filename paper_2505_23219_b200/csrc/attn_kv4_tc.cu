@@ -450,13 +450,11 @@ __global__ void __launch_bounds__(THREADS, 1) k_attn_kv4_tc(const __grid_constan
             int k = 0;
             bool ok = true;
 #pragma unroll 1
-            for (int64_t u = u_beg; ok;) {
-                Kv4Item it{};
-#pragma unroll 1
-                while (u < u_end && it.take == 0) {
-                    it = kv4_find_item(til, sm->sums, w.n_seqs, [&](int s_) { return kv4_load_seq(w, s_); }, u, u_end);
-                    u = it.next;
-                }
+            for (Kv4Item it{}; ok;) {
+                const auto seq_of = [&](int s_) { return kv4_load_seq(w, s_); };
+                if (k == 0 && u_beg < u_end) it = kv4_find_item(til, sm->sums, w.n_seqs, seq_of, u_beg, u_end);
+                else if (k > 0 && it.next < u_end) kv4_next_item(til, seq_of, it, u_end);
+                else it.take = 0;
                 if (it.take > 0) it.keys = kv4_tile_keys(til, it.q, it.tile);
                 if (k >= ITEMS) ok = wait<500>(smem_u32(&sm->item_empty[k % ITEMS]), ((k / ITEMS) - 1) & 1, looks, w.status, DEV_TIMEOUT_EPI);
                 sm->item[k % ITEMS] = it;

@@ -121,4 +121,24 @@ GHD_HD Kv4Item kv4_find_item(const Kv4Tiling& t, const int64_t* sums, int n_seqs
     return it;
 }
 
+// The item behind `it` in the same run, where the run goes on (it.next < u_end): no search and no division by what only the
+// launch knows.
+template <typename SeqOf>
+GHD_HD void kv4_next_item(const Kv4Tiling& t, SeqOf seq_of, Kv4Item& it, int64_t u_end) {
+    if (++it.tile >= kv4_tiles(t, it.q.n)) {
+        it.tile = 0;
+        if (++it.head == t.heads) {
+            it.head = 0;
+            GHD_ROLLED
+            do it.q = seq_of(++it.seq); while (it.q.n == 0);        // there are units left, so there is one with rows
+        }
+    }
+    it.chunks = kv4_tile_chunks(t, it.q, it.tile);
+    it.first = it.next + t.lead;
+    it.next = it.first + it.chunks < u_end ? it.first + it.chunks : u_end;
+    it.chunk0 = 0;
+    it.take = it.next > it.first ? (int)(it.next - it.first) : 0;
+    it.keys = 0;
+}
+
 }  // namespace ghd

@@ -46,6 +46,30 @@ long long deal(int n_seqs, const int* start, const int* len, int n_rows, long lo
     }
     return n;
 }
+// Walks every run item by item: by a search for each and by going on from the one before.  -> items, or -1 where the two differ
+long long walk(int n_seqs, const int* start, const int* len, int n_rows, long long cap, int heads, int group, int tile_rows, int chunk, int lead, int ctas) {
+    Kv4Tiling t{heads, group, tile_rows, chunk, lead};
+    std::vector<int64_t> sums(n_seqs + 1, 0);
+    auto seq_of = [&](int s) { return kv4_seq(start[s], start[s + 1], n_rows, len[s], cap); };
+    for (int s = 0; s < n_seqs; ++s) sums[s + 1] = sums[s] + heads * kv4_head_units(t, seq_of(s));
+    const int64_t units = sums[n_seqs], per = kv4_units_per_cta(units, ctas);
+    long long n = 0;
+    for (int c = 0; c < ctas; ++c) {
+        const int64_t u = per * c, e = u + per < units ? u + per : units;
+        if (u >= e) continue;
+        Kv4Item b = kv4_find_item(t, sums.data(), n_seqs, seq_of, u, e);
+        for (;;) {
+            ++n;
+            if (b.take == 0 && b.next < e) return -1;             // only a run's last item may be without chunks
+            if (b.next >= e) break;
+            const Kv4Item a = kv4_find_item(t, sums.data(), n_seqs, seq_of, b.next, e);
+            kv4_next_item(t, seq_of, b, e);
+            if (a.seq != b.seq || a.head != b.head || a.tile != b.tile || a.chunk0 != b.chunk0 || a.chunks != b.chunks || a.take != b.take ||
+                a.first != b.first || a.next != b.next || a.q.row0 != b.q.row0 || a.q.n != b.q.n || a.q.len != b.q.len || a.q.n_new != b.q.n_new) return -1;
+        }
+    }
+    return n;
+}
 }
 """
 
@@ -56,7 +80,7 @@ def lay(tmp_path_factory):
     (d / "h.cpp").write_text(_HARNESS)
     subprocess.check_call(["g++", "-O1", "-std=c++17", "-shared", "-fPIC", f"-I{ROOT}/paper_2505_23219_b200/csrc", "-o", str(d / "h.so"), str(d / "h.cpp")])
     lib = C.CDLL(str(d / "h.so"))
-    lib.deal.restype = C.c_longlong
+    lib.deal.restype = lib.walk.restype = C.c_longlong
     return lib
 
 
@@ -206,3 +230,17 @@ def test_null_contexts_are_refused_without_a_gpu():
     assert lib.ghd_kv4_pool_bytes(None, None) == 0
     n = [None] * 12
     assert lib.ghd_kv4_append(*n[:10]) == 1 and lib.ghd_kv4_attention(*n[:6]) == 1 and lib.ghd_kv4_read(*n[:7]) == 1 and lib.ghd_kv4_commit(*n[:6]) == 1
+
+
+@pytest.mark.parametrize("seed", range(8))
+def test_going_on_to_the_next_item_is_the_search_for_it(lay, seed):
+    r = np.random.RandomState(seed)
+    for _ in range(8):
+        S = r.randint(1, 9)
+        cnt = np.where(r.rand(S) < 0.3, 0, r.randint(1, 90, S))
+        start = np.concatenate(([0], np.cumsum(cnt))).astype(np.int32)
+        ln = np.where(r.rand(S) < 0.2, 0, r.randint(1, 3000, S)).astype(np.int32)
+        heads, group, rows, lead, ctas = int(r.randint(1, 6)), int(r.randint(1, 9)), int(r.choice([8, 16, 64])), int(r.randint(0, 8)), int(r.choice([1, 3, 148, 444]))
+        p = lambda a: a.ctypes.data_as(C.c_void_p)  # noqa: E731
+        n = lay.walk(S, p(start), p(ln), int(start[-1]), C.c_longlong(4000), heads, group, rows, 128, lead, ctas)
+        assert n >= 0 and (n > 0) == (start[-1] > 0)
