@@ -460,7 +460,7 @@ __global__ void __launch_bounds__(WARPS * 32, Narrow<T, D, NT>::BLOCKS) k_attn_k
                     *reinterpret_cast<float4*>(xo + (warp * RT + rl) * XO + g * (D / 8) + 2 * mt) = make_float4(o[mt][nt][e], o[mt][nt][e + 2], o[mt + 1][nt][e], o[mt + 1][nt][e + 2]);
             }
         __syncthreads();
-        const int64_t c0 = it.first / per, c1 = (it.first + it.chunks - 1) / per;      // CTAs that share the item
+        const int64_t c0 = kv4_cta_of(it.first, per), c1 = kv4_cta_of(it.first + it.chunks - 1, per);      // CTAs that share the item
         const bool whole = c0 == c1;
         float* slot = p.part + ((size_t)blockIdx.x * 2 + ((int64_t)blockIdx.x == c0 ? 1 : 0)) * N::SLOT;
 #pragma unroll 1
@@ -490,13 +490,11 @@ __global__ void __launch_bounds__(WARPS * 32, Narrow<T, D, NT>::BLOCKS) k_attn_k
             }
         }
         if (!whole) {
-            __threadfence();
             __syncthreads();
             if (threadIdx.x == 0) {
-                const int want = (int)(c1 - c0), old = atomicAdd(p.counters + c0, 1);
+                const int want = (int)(c1 - c0), old = arrive_at(p.counters + c0);
                 if (old == want) p.counters[c0] = 0;                     // everybody has arrived: ready for the next launch
                 arrived = old == want;
-                __threadfence();
             }
             __syncthreads();
             if (arrived) merge_item<T, D, 1>(p, it, RT, rows, c0, c1, warp, WARPS, xmerge, [] { __syncthreads(); });

@@ -132,19 +132,27 @@ __device__ __noinline__ void advance_item(const Kv4View* w, int group, Kv4Item* 
     *it = x;
 }
 
+// Counts a CTA in, after a barrier of its threads: what they wrote before goes before the count, and who finds all counted sees
+// what the others wrote.
+__device__ __forceinline__ int arrive_at(int* counter) {
+    int old;
+    asm volatile("atom.add.acq_rel.gpu.global.s32 %0, [%1], 1;" : "=r"(old) : "l"(counter) : "memory");
+    return old;
+}
+
 // Adds the partial sums that CTAs c0 .. c1 left of one item, in that order, and writes its rows.  A warp takes RB rows at a
 // time (the lanes hold D / 32 channels each) and KB contributors of each: what the merge costs is the latency of its loads,
 // so 16 rows of sums are on the way together.  With few rows several warps share the contributors and meet in `xch`,
 // floats [warps][D + 2].  `sync` is a barrier of the NW warps that take part.
 template <typename T, int D, int RB, typename Sync>
 __device__ __forceinline__ void merge_item(const Kv4AttnParams& p, const Kv4Item& it, int tile_rows, int rows, int64_t c0, int64_t c1, int warp, int nw, float* xch, Sync sync) {
-    constexpr int VL = D / 32, KB = 16 / RB;
+    constexpr int VL = D / 32, KB = RB == 1 ? 8 : 16 / RB;
     const size_t slot = (size_t)tile_rows * (D + 2);
     const int lane = threadIdx.x & 31, n = (int)(c1 - c0) + 1;
     int share = 1;                                               // warps a row: a power of two (only where a warp takes one row at a time)
     if (RB == 1) {
 #pragma unroll 1
-        while (share * 2 * rows <= nw && share * 2 * KB < n) share *= 2;
+        while (share * 2 * rows <= nw && share * KB < n) share *= 2;
     }
     const int sub = warp & (share - 1), team = warp / share, teams = nw / share;
     const int k_beg = n * sub / share, k_end = n * (sub + 1) / share;

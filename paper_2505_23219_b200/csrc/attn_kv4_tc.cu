@@ -711,7 +711,7 @@ __global__ void __launch_bounds__(THREADS, 1) k_attn_kv4_tc(const __grid_constan
             named_sync<1, SOFT>();
             wait(smem_u32(&sm->p_empty[(i - 1) & 1]), ((i - 1) >> 1) & 1, looks, w.status, DEV_TIMEOUT_EPI);
             tc_fence_after();
-            const int64_t c0 = it.first / per, c1 = (it.first + it.chunks - 1) / per;
+            const int64_t c0 = kv4_cta_of(it.first, per), c1 = kv4_cta_of(it.first + it.chunks - 1, per);
             const bool whole = c0 == c1;
             float* slot = p.part + ((size_t)blockIdx.x * 2 + ((int64_t)blockIdx.x == c0 ? 1 : 0)) * ((size_t)N * (D + 2));
             const float vinv = 1.f / vmul;                                // (of this part's rows: the same in its four warps)
@@ -739,13 +739,11 @@ __global__ void __launch_bounds__(THREADS, 1) k_attn_kv4_tc(const __grid_constan
             if (!whole && tid < rows) __stcg(reinterpret_cast<float2*>(slot + N * D + 2 * tid), make_float2(sm->fac[tid], sm->tot[tid].x));
             tc_fence_before();                                            // O^T has been read: the next item's first product may write it
             if (!whole) {
-                __threadfence();
                 named_sync<1, SOFT>();
                 if (tid == 0) {
-                    const int want = (int)(c1 - c0), old = atomicAdd(p.counters + c0, 1);
+                    const int want = (int)(c1 - c0), old = arrive_at(p.counters + c0);
                     if (old == want) p.counters[c0] = 0;
                     sm->arrived = old == want;
-                    __threadfence();
                 }
                 named_sync<1, SOFT>();
                 if (sm->arrived) merge_item<__half, D, 4>(p, it, N, rows, c0, c1, warp, SW, nullptr, [] {});

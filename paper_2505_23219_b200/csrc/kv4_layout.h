@@ -70,8 +70,10 @@ GHD_HD int64_t kv4_head_units(const Kv4Tiling& t, const Kv4Seq& q) {
     for (int i = 0, n = kv4_tiles(t, q.n); i < n; ++i) u += t.lead + kv4_tile_chunks(t, q, i);
     return u;
 }
+// a / b for what is mostly below 2^32 (64-bit divisions are long on the device)
+GHD_HD int64_t kv4_cta_of(int64_t unit, int64_t per) { return ((uint64_t)unit | (uint64_t)per) <= 0xffffffffull ? (uint32_t)unit / (uint32_t)per : unit / per; }
 // Every CTA takes `per` consecutive units (the last ones fewer or none), so a unit's CTA is unit / per.
-GHD_HD int64_t kv4_units_per_cta(int64_t units, int ctas) { return units > 0 ? (units + ctas - 1) / ctas : 1; }
+GHD_HD int64_t kv4_units_per_cta(int64_t units, int ctas) { return units > 0 ? kv4_cta_of(units + ctas - 1, ctas) : 1; }
 
 // The item that unit u belongs to, and the chunks of it that the run [u, u_end) takes (none when the run ends before the
 // item's first chunk).  sums: exclusive sums of the sequences' units, n_seqs + 1 of them; seq_of(s) -> Kv4Seq;
