@@ -17,9 +17,9 @@
 // a run's border leaves partial sums; the last of its CTAs to arrive adds them in CTA order (the result does not
 // depend on who was last).  Float contexts split q and p * scale into three bfloat16 terms (24 bits).
 //
-// What it costs.  One token over 2048 rows of 32 heads (8.9 MB): 13.8 us, a chain of latencies (lengths, item, page ids, rows, weights,
-// partial sums, arrival, merge); over 16384 rows 30 us, 2.4 TB/s.  One token each of 32 ragged sequences of up to 8192 rows, 32 heads
-// on 8 (174.5 MB): 59 us, 2.9 TB/s.  That is instructions: 750 a warp for 32 keys (9 for a word of eight codes, 32 words a lane; the
+// What it costs.  One token over 2048 rows of 32 heads (8.9 MB): 11.3 us, a chain of latencies (in clocks: lengths and prefix sums 2300,
+// item 2000, page ids and first rows 2200, queries 1200, two chunks 4000, sums 1500, arrival 2000, merge 2500); over 16384 rows 27 us,
+// 2.6 TB/s.  One token each of 32 ragged sequences of up to 8192 rows, 32 heads on 8 (174.5 MB): 53 us, 3.3 TB/s.  That is instructions: 750 a warp for 32 keys (9 for a word of eight codes, 32 words a lane; the
 // products are 32), 2.2 an SM a clock out of 12 warps (163 registers a thread).  Four CTAs an SM spill, deeper rings take CTAs away.
 #include "attn_kv4_dev.cuh"
 
@@ -34,7 +34,7 @@ namespace {
 
 constexpr int WARPS = 4, WKEYS = 32, CHUNK = WKEYS * WARPS;      // a warp takes 32 keys of every chunk
 constexpr float RAISE = 2.f;
-constexpr int LEAD = 4;          // an item's fixed cost in chunks (0: 18.3 us for one token over 2048 rows of 32 heads, 2: 14.2, 4: 13.5, 8: 13.8)
+constexpr int LEAD = 4;          // an item's fixed cost in chunks (one token of 32 heads over 2048 and 16384 rows: 2: 11.6 and 28.4 us, 3: 11.2 and 27.3, 4: 11.3 and 27.0)
 
 using namespace kv4;
 
@@ -540,15 +540,15 @@ ghd_status launch_attn_kv4(ghd_ctx* c, const Kv4View& w, const ghd_kv4_rows* row
     const int64_t avg = ((int64_t)rows->n_rows * p.group + w.n_seqs - 1) / w.n_seqs;      // query rows of a sequence and head, on average
     if (m.dtype == GHD_F32) {
         if (c->opt_attn_path == 2) return fail(c, GHD_EUNSUPPORTED, "kv4_attention: the tcgen05 kernel takes GHD_F16 only");
-        // two tiles of eight rows at a time where there are many (28 heads on 4, 5 sequences over 2048 keys: 2 x 7 rows 17 us in ones, 24 in
-        // twos; 8 x 7: 26 and 29; 16 x 7: 42 and 38; 88 x 7: 350 and 161)
+        // Two tiles of eight rows at a time where there are many (5 sequences over 2048 keys; 28 heads on 4: 2 x 7 rows 15 us in ones, 22 in
+        // twos; 8 x 7: 20 and 24; 16 x 7: 31 and 33; 88 x 7: 130 and 106; 32 heads, 88 rows: 133 and 121).
         if (avg > 64) return m.d_head == 64 ? launch_narrow<float, 64, 2>(c, p) : launch_narrow<float, 128, 2>(c, p);
         return m.d_head == 64 ? launch_narrow<float, 64, 1>(c, p) : launch_narrow<float, 128, 1>(c, p);
     }
-    // The tcgen05 kernel for tiles of many rows.  Up to 32 rows two tiles of this file's kernel cost the same a key and start sooner (8
-    // sequences, 32 heads, 32 rows over 512 / 1024 / 2048 keys: 33 / 39 / 60 us here, 37 / 43 / 62 there; over none 23 and 26); up to 64
-    // while its tiles leave half of the SMs free (32 tiles over 256 / 2048 keys: 16 / 19 us here, 20 / 26 there; 128 tiles over 1024: 30 and
-    // 28); 128 rows: 24 / 43 / 53 us over 512 .. 2048 keys here, 22 / 32 / 37 there.
+    // The tcgen05 kernel for tiles of many rows.  Up to 32 rows two tiles of this file's kernel start sooner and cost a key no more (8
+    // sequences, 32 heads, 32 rows over 0 / 512 / 2048 / 8192 keys: 19 / 29 / 53 / 99 us here, 26 / 38 / 62 / 110 there).  Up to 64 rows
+    // they do while its tiles leave half of the SMs free (32 tiles over 256 / 2048 keys: 13 / 16 us here, 20 / 26 there; but 128 tiles over
+    // 1024 / 4096: 23 / 39 here, 27 / 36 there).  128 rows, 32 heads over 512 / 1024 / 2048 keys: 26 / 33 / 43 here, 27 / 32 / 37 there.
     const int64_t tiles = (avg + 15) / 16 * w.heads * w.n_seqs;
     if (c->opt_attn_path == 2 || (c->opt_attn_path == 0 && avg > 32 && (avg > 64 || 2 * tiles > c->sm_count))) return launch_attn_kv4_tc(c, p);
     if (m.d_head == 64) return avg <= 8 ? launch_narrow<__half, 64, 1>(c, p) : launch_narrow<__half, 64, 2>(c, p);

@@ -19,8 +19,8 @@
 //
 // Work is dealt as in attn_kv4.cu, one CTA an SM.
 //
-// What it costs.  8 ragged trees of up to 64 nodes over up to 8192 rows, 32 heads (148 MB, 30 GFLOP): 129 us; one tree of 256 nodes over
-// 4096 rows, 40 heads (22 GFLOP): 90 us.  A unit of 128 keys x 64 rows takes about 2700 clocks where its products take 900 and its
+// What it costs.  8 ragged trees of up to 64 nodes over up to 8192 rows, 32 heads (148 MB, 30 GFLOP): 130 us; one tree of 256 nodes over
+// 4096 rows, 40 heads (22 GFLOP): 89 us.  A unit of 128 keys x 64 rows takes about 2700 clocks where its products take 900 and its
 // exponentials 500: the softmax warps' chain (fetch, scores, agreement on references, wait for a P buffer, weights, hand-over), at
 // 2.0 instructions an SM a clock; K and V are two units ahead.  An item costs about six units besides (queries in, filling and
 // draining, sums out, merge), a launch 6 us before the first.  Measured and dropped: 16 softmax warps on one unit, two groups of eight
