@@ -71,7 +71,7 @@ constexpr int ITEMS = 4;                       // items that the scheduler is ah
 
 struct Ctrl {
     uint64_t item_full[ITEMS], item_empty[ITEMS];
-    Kv4Item item[ITEMS], cur;        // cur: the softmax warps' item
+    Kv4Item item[ITEMS], cur[3];     // cur: the softmax warps' items: the one being finished, the next, and a slot for who is behind
     uint64_t c_full[CONV / 32][4];   // packed rows of a unit, by unpacking warp and stage
     uint64_t q_full, k_full[2], k_empty[2], v_full[2], v_empty[2], s_full[2], s_empty[2], p_full[2], p_empty[2], drain, drain_pv;
     uint32_t tmem_base;
@@ -83,7 +83,7 @@ struct Ctrl {
     float x[4][N], y[4][N];      // exchange between the four warps that share rows
     float4 par[PAR_SLOTS][UNIT];     // by unit and key: K's scale and middle (min + 8 scale) times log2(e) / sqrt(d_head), V's scale and middle
     alignas(4) uint8_t groups[GROUP_SLOTS][4];      // which of a quarter's two groups of 16 keys have a page, by unit
-    int rowix[N];                  // row of q and out, in d_head elements, of the tile's query rows
+    int rowix[2][N];               // row of q and out, in d_head elements, of the query rows of an item and the next
     float vmax[PARTS][4];            // largest of V's scales of a unit, by part and warp
     int64_t scratch[32];
     int64_t sums[1];                 // [n_seqs + 1]
@@ -471,17 +471,37 @@ __global__ void __launch_bounds__(THREADS, 1) k_attn_kv4_tc(const __grid_constan
         const int part = warp >> 2, quad = warp & 3, g = lane >> 2, t = lane & 3, tid = threadIdx.x;
         auto col8 = [&](int j) { return 16 * (PARTS * (j >> 1) + part) + 8 * (j & 1); };      // first query row of this thread's block j
         int i = 0;                                                        // unit of this CTA
+        // running sums and references of this thread's rows: rows 2 t + e of its blocks
+        // `neg`: less what a row's scores are taken against, its reference, or 0 while it has none (its bit 2 j + e of `none`)
+        float2 l[NB], ms[NB], neg[NB];
+        uint32_t none = 0u;
+        float vmul = 0x1p24f;                                             // 2^-e of V's scales
+        // Pass n finishes item n - 1 and begins item n: its queries are in place, and its first scores on the way, before the sums of
+        // the one before go out.  (Shared words are double: a warp that is still writing sums out meets others in the next item.)
 #pragma unroll 1
-        for (int items = 0;; ++items) {
-            if (tid == 0) sm->cur = item_get(items);
+        for (int n = 0;; ++n) {
+            if (n > 0) {
+                // ---- sums of the rows over the four warps that share them
+#pragma unroll
+                for (int j = 0; j < NB; ++j)
+#pragma unroll
+                    for (int e = 0; e < 2; ++e) {
+                        float a = e ? l[j].y : l[j].x, c = e ? ms[j].y : ms[j].x;
+#pragma unroll
+                        for (int o = 4; o < 32; o <<= 1) { a += __shfl_xor_sync(0xffffffffu, a, o); c += __shfl_xor_sync(0xffffffffu, c, o); }
+                        const int rl = col8(j) + 2 * t + e;
+                        if (g == 0) { sm->x[quad][rl] = a; sm->y[quad][rl] = c; if (quad == 0) sm->fac[rl] = (none >> (2 * j + e)) & 1u ? -INFINITY : -(e ? neg[j].y : neg[j].x); }
+                    }
+            }
+            if (tid == 0) sm->cur[n % 3] = item_get(n);
             named_sync<1, SOFT>();
-            const Kv4Item& it = sm->cur;                                  // stays until the barrier at the item's end
-            if (it.take == 0) break;
+            const Kv4Item& it = sm->cur[n % 3];                           // stays until the pass after the next
+            const bool go = it.take > 0;
             const int rows = rows_of(it), cols = cols_of(rows);
             // ---- queries to shared memory, channels of a word in the order the nibbles come in; their sums
-            {
-                constexpr int C8 = D / 8, MOST = (N * C8 + SOFT - 1) / SOFT;      // 16-byte pieces of a row, and at most of a thread
-                uint4 v[MOST];
+            constexpr int C8 = D / 8, MOST = (N * C8 + SOFT - 1) / SOFT;  // 16-byte pieces of a row, and at most of a thread
+            uint4 v[MOST];
+            if (go) {
 #pragma unroll
                 for (int z = 0; z < MOST; ++z) {                          // all loads first
                     const int x = tid + z * SOFT, rl = x / C8, c = x % C8, rr = it.tile * N + rl;
@@ -489,9 +509,15 @@ __global__ void __launch_bounds__(THREADS, 1) k_attn_kv4_tc(const __grid_constan
                     if (rl < rows) {
                         const int ix = (it.q.row0 + rr / p.group) * p.q_heads + it.head * p.group + rr % p.group;
                         v[z] = __ldg(reinterpret_cast<const uint4*>((const __half*)p.q + (size_t)ix * D + 8 * c));
-                        if (c == 0) sm->rowix[rl] = ix;
+                        if (c == 0) sm->rowix[n & 1][rl] = ix;
                     }
                 }
+            }
+            if (n > 0 && tid < N) {
+                const float lsum = (sm->x[0][tid] + sm->x[1][tid]) + (sm->x[2][tid] + sm->x[3][tid]), mm = (sm->y[0][tid] + sm->y[1][tid]) + (sm->y[2][tid] + sm->y[3][tid]);
+                sm->tot[tid] = make_float4(lsum, lsum == 0.f ? 0.f : 1.f / lsum, mm, sm->fac[tid]);
+            }
+            if (go) {
 #pragma unroll
                 for (int z = 0; z < MOST; ++z) {
                     const int x = tid + z * SOFT, rl = x / C8, c = x % C8;
@@ -506,18 +532,59 @@ __global__ void __launch_bounds__(THREADS, 1) k_attn_kv4_tc(const __grid_constan
                 }
                 asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
                 warp_arrive(smem_u32(&sm->q_full));
-                named_sync<1, SOFT>();                                    // the sums are read by everybody
             }
-            // running sums and references of this thread's rows: rows 2 t + e of its blocks
-            // `neg`: less what a row's scores are taken against, its reference, or 0 while it has none (its bit 2 j + e of `none`)
-            float2 l[NB], ms[NB], neg[NB];
-            uint32_t none = 0u;                                           // (no bits for blocks without rows)
+            named_sync<1, SOFT>();                                        // totals and the queries' sums are read by everybody
+            if (n > 0) {
+            wait(smem_u32(&sm->p_empty[(i - 1) & 1]), ((i - 1) >> 1) & 1, looks, w.status, DEV_TIMEOUT_EPI);
+            tc_fence_after();
+            const Kv4Item& last = sm->cur[(n - 1) % 3];
+            const int lrows = rows_of(last);
+            const int64_t c0 = kv4_cta_of(last.first, per), c1 = kv4_cta_of(last.first + last.chunks - 1, per);
+            const bool whole = c0 == c1;
+            float* slot = p.part + ((size_t)blockIdx.x * 2 + ((int64_t)blockIdx.x == c0 ? 1 : 0)) * ((size_t)N * (D + 2));
+            const float vinv = 1.f / vmul;                                // (of this part's rows: the same in its four warps)
+            // lane m of the accumulator is channel (m & ~7) | {0 4 1 5 2 6 3 7}[m & 7]; a row's channels of this quarter are one store of the warp
+            const int chn = quad * 32 + ((lane & ~7) | ((lane & 1) * 4) | ((lane & 7) >> 1));
+            if (quad * 32 < D) {
+#pragma unroll 1
+                for (int j = 0; j < NB && col8(j) < lrows; ++j) {
+                    uint32_t o[8];
+                    const int r0 = col8(j);
+                    ld_cols8(tmem + SH::T_O + r0 + ((uint32_t)(quad * 32) << 16), o);
+                    ld_wait();
 #pragma unroll
-            for (int j = 0; j < NB; ++j) if (col8(j) < cols) none |= 3u << 2 * j;
+                    for (int x = 0; x < 8; ++x) {
+                        const int rl = r0 + x;
+                        const float4 tm = sm->tot[rl];
+                        const float v = fmaf(__uint_as_float(o[x]), vinv, tm.z);
+                        if (rl < lrows) {
+                            if (whole) ((__half*)p.out)[(size_t)sm->rowix[(n - 1) & 1][rl] * D + chn] = __float2half_rn(v * tm.y);
+                            else __stcg(slot + rl * D + chn, v);
+                        }
+                    }
+                }
+            }
+            if (!whole && tid < lrows) __stcg(reinterpret_cast<float2*>(slot + N * D + 2 * tid), make_float2(sm->tot[tid].w, sm->tot[tid].x));
+            tc_fence_before();                                            // O^T has been read: the next item's first product may write it
+            if (!whole) {
+                named_sync<1, SOFT>();
+                if (tid == 0) {
+                    const int want = (int)(c1 - c0), old = arrive_at(p.counters + c0);
+                    if (old == want) p.counters[c0] = 0;
+                    sm->arrived = old == want;
+                }
+                named_sync<1, SOFT>();
+                if (sm->arrived) merge_item<__half, D, 4>(p, last, N, lrows, c0, c1, warp, SW, nullptr, [] {});
+            }
+            }
+            if (!go) break;
+            none = 0u;                                                    // (no bits for blocks without rows)
+            vmul = 0x1p24f;
 #pragma unroll
-            for (int j = 0; j < NB; ++j)
+            for (int j = 0; j < NB; ++j) {
                 l[j] = ms[j] = neg[j] = make_float2(0.f, 0.f);
-            float vmul = 0x1p24f;                                         // 2^-e of V's scales
+                if (col8(j) < cols) none |= 3u << 2 * j;
+            }
             // The scores of a unit are fetched while the one before is worked on: s[j][h] has the 16 keys 16 h of block j.
             uint32_t s[NB][2][4];
             auto fetch = [&](int u) {
@@ -692,63 +759,6 @@ __global__ void __launch_bounds__(THREADS, 1) k_attn_kv4_tc(const __grid_constan
                 warp_arrive(smem_u32(&sm->p_full[b]));
                 if (more) fetched(i + 1);
             }
-            // ---- sums of the rows over the four warps that share them
-#pragma unroll
-            for (int j = 0; j < NB; ++j)
-#pragma unroll
-                for (int e = 0; e < 2; ++e) {
-                    float a = e ? l[j].y : l[j].x, c = e ? ms[j].y : ms[j].x;
-#pragma unroll
-                    for (int o = 4; o < 32; o <<= 1) { a += __shfl_xor_sync(0xffffffffu, a, o); c += __shfl_xor_sync(0xffffffffu, c, o); }
-                    const int rl = col8(j) + 2 * t + e;
-                    if (g == 0) { sm->x[quad][rl] = a; sm->y[quad][rl] = c; if (quad == 0) sm->fac[rl] = (none >> (2 * j + e)) & 1u ? -INFINITY : -(e ? neg[j].y : neg[j].x); }
-                }
-            named_sync<1, SOFT>();
-            if (tid < N) {
-                const float lsum = (sm->x[0][tid] + sm->x[1][tid]) + (sm->x[2][tid] + sm->x[3][tid]), mm = (sm->y[0][tid] + sm->y[1][tid]) + (sm->y[2][tid] + sm->y[3][tid]);
-                sm->tot[tid] = make_float4(lsum, lsum == 0.f ? 0.f : 1.f / lsum, mm, 0.f);
-            }
-            named_sync<1, SOFT>();
-            wait(smem_u32(&sm->p_empty[(i - 1) & 1]), ((i - 1) >> 1) & 1, looks, w.status, DEV_TIMEOUT_EPI);
-            tc_fence_after();
-            const int64_t c0 = kv4_cta_of(it.first, per), c1 = kv4_cta_of(it.first + it.chunks - 1, per);
-            const bool whole = c0 == c1;
-            float* slot = p.part + ((size_t)blockIdx.x * 2 + ((int64_t)blockIdx.x == c0 ? 1 : 0)) * ((size_t)N * (D + 2));
-            const float vinv = 1.f / vmul;                                // (of this part's rows: the same in its four warps)
-            // lane m of the accumulator is channel (m & ~7) | {0 4 1 5 2 6 3 7}[m & 7]; a row's channels of this quarter are one store of the warp
-            const int chn = quad * 32 + ((lane & ~7) | ((lane & 1) * 4) | ((lane & 7) >> 1));
-            if (quad * 32 < D) {
-#pragma unroll 1
-                for (int j = 0; j < NB && col8(j) < rows; ++j) {
-                    uint32_t o[8];
-                    const int r0 = col8(j);
-                    ld_cols8(tmem + SH::T_O + r0 + ((uint32_t)(quad * 32) << 16), o);
-                    ld_wait();
-#pragma unroll
-                    for (int x = 0; x < 8; ++x) {
-                        const int rl = r0 + x;
-                        const float4 tm = sm->tot[rl];
-                        const float v = fmaf(__uint_as_float(o[x]), vinv, tm.z);
-                        if (rl < rows) {
-                            if (whole) ((__half*)p.out)[(size_t)sm->rowix[rl] * D + chn] = __float2half_rn(v * tm.y);
-                            else __stcg(slot + rl * D + chn, v);
-                        }
-                    }
-                }
-            }
-            if (!whole && tid < rows) __stcg(reinterpret_cast<float2*>(slot + N * D + 2 * tid), make_float2(sm->fac[tid], sm->tot[tid].x));
-            tc_fence_before();                                            // O^T has been read: the next item's first product may write it
-            if (!whole) {
-                named_sync<1, SOFT>();
-                if (tid == 0) {
-                    const int want = (int)(c1 - c0), old = arrive_at(p.counters + c0);
-                    if (old == want) p.counters[c0] = 0;
-                    sm->arrived = old == want;
-                }
-                named_sync<1, SOFT>();
-                if (sm->arrived) merge_item<__half, D, 4>(p, it, N, rows, c0, c1, warp, SW, nullptr, [] {});
-            }
-            named_sync<1, SOFT>();                                        // queries' sums and exchange buffers are written again
         }
     }
 
