@@ -341,19 +341,22 @@ __global__ void __launch_bounds__(WARPS * 32, Narrow<T, D, NT>::BLOCKS) k_attn_k
             bool over = none != 0u || top > RAISE;                      // (a row's first keys may have had no page)
             uint32_t vis = 0xffffffffu;                                 // bit 8 nt + 4 z + e: score s[z][nt][e] counts
             if (__builtin_expect(!all, 0)) {
+                // a lane looks up the warp's 32 keys for one of the tile's rows; the others get the word by shuffle
+                uint32_t word = sees(p, it.q, (it.tile * RT + min(lane, RT - 1)) / p.group, key0 - it.q.len);
+                word &= (there & 1 ? 0x0000ffffu : 0u) | (there & 2 ? 0xffff0000u : 0u);
                 vis = 0u;
                 over = false;
 #pragma unroll
                 for (int nt = 0; nt < NT; ++nt)
 #pragma unroll
                     for (int e = 0; e < 2; ++e) {
-                        const uint32_t b = sees(p, it.q, (it.tile * RT + nt * 8 + 2 * t + e) / p.group, key0 + ka - it.q.len);
+                        const uint32_t b = __shfl_sync(0xffffffffu, word, 8 * nt + 2 * t + e) >> ka;
 #pragma unroll
                         for (int z = 0; z < 2; ++z)
 #pragma unroll
                             for (int h = 0; h < 2; ++h) {
                                 float& v = s[z][nt][2 * h + e];
-                                if ((b >> (16 * z + 8 * h)) & (there >> z) & 1u) vis |= 1u << (8 * nt + 4 * z + 2 * h + e);
+                                if ((b >> (16 * z + 8 * h)) & 1u) vis |= 1u << (8 * nt + 4 * z + 2 * h + e);
                                 else v = -INFINITY;
                                 over = over || v > ((none >> (2 * nt + e)) & 1u ? -INFINITY : RAISE);
                             }

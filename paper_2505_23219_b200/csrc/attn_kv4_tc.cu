@@ -634,6 +634,9 @@ __global__ void __launch_bounds__(THREADS, 1) k_attn_kv4_tc(const __grid_constan
                 bool over = top > RAISE || none != 0u;                    // (a row's first keys may have had no page)
                 uint32_t vis = 0xffffffffu;                               // bit 8 j + 4 e + x: row e of block j sees key x
                 if (__builtin_expect(!all, 0)) {
+                    // a lane looks up the warp's 32 keys for one of the part's 32 rows; the others get the word by shuffle
+                    uint32_t word = sees(p, it.q, (it.tile * N + col8(lane >> 3) + (lane & 7)) / p.group, key0 - g - it.q.len);
+                    word &= ((groups >> (8 * quad)) & 1u ? 0x0000ffffu : 0u) | ((groups >> (8 * quad)) & 2u ? 0xffff0000u : 0u);
                     vis = 0u;
                     over = k == 0;
 #pragma unroll
@@ -643,10 +646,10 @@ __global__ void __launch_bounds__(THREADS, 1) k_attn_kv4_tc(const __grid_constan
                     for (int j = 0; j < NB; ++j)
 #pragma unroll
                         for (int e = 0; e < 2; ++e) {
-                            const uint32_t w32 = sees(p, it.q, (it.tile * N + col8(j) + 2 * t + e) / p.group, key0 - it.q.len);
+                            const uint32_t w32 = __shfl_sync(0xffffffffu, word, 8 * j + 2 * t + e) >> g;
 #pragma unroll
                             for (int x = 0; x < 4; ++x) {
-                                const bool ok = (w32 >> (8 * x)) & (groups >> (8 * quad + (x >> 1))) & 1u;
+                                const bool ok = (w32 >> (8 * x)) & 1u;
                                 if (ok) vis |= 1u << (8 * j + 4 * e + x);
                                 else sc[j][x][e] = -INFINITY;
                                 over = over || (col8(j) < cols && sc[j][x][e] > ((none >> (2 * j + e)) & 1u ? -INFINITY : RAISE));
