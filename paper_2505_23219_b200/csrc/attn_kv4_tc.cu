@@ -46,6 +46,7 @@ constexpr int SOFT = 256, CONV = 256;          // threads of the softmax and of 
 constexpr int PARTS = SOFT / 128;              // 128 threads (one a key of four) share query rows, as pairs of blocks of eight: pair part, part + PARTS, ...
 constexpr int THREADS = SOFT + CONV + 128, SW = SOFT / 32, CW = SW + CONV / 32;      // first unpacking warp, first of the others
 // registers a thread after the split by warpgroups, within those launched with
+static_assert(N / 8 / PARTS == 4, "a lane of eight ends up with one of 4 + 4 blocks' sums");
 constexpr int REGS_LAUNCH = 96, REGS_SOFT = 152, REGS_CONV = 56, REGS_ISSUE = 56;
 static_assert(SOFT * REGS_SOFT + CONV * REGS_CONV + 128 * REGS_ISSUE <= THREADS * REGS_LAUNCH && THREADS * REGS_LAUNCH <= 65536, "register split");
 constexpr float RAISE = 8.f;
@@ -80,10 +81,10 @@ struct Ctrl {
     alignas(16) float qs[N];       // sums of the tile's queries
     alignas(16) float fac[N];      // factors of a rescale, by row
     float4 tot[N];                   // a row's sum of weights, its inverse, sum of weighted middles
-    float x[4][N], y[4][N];      // exchange between the four warps that share rows
+    alignas(16) float x[4][N], y[4][N];      // exchange between the four warps that share rows
     float4 par[PAR_SLOTS][UNIT];     // by unit and key: K's scale and middle (min + 8 scale) times log2(e) / sqrt(d_head), V's scale and middle
     alignas(4) uint8_t groups[GROUP_SLOTS][4];      // which of a quarter's two groups of 16 keys have a page, by unit
-    int rowix[2][N];               // row of q and out, in d_head elements, of the query rows of an item and the next
+    alignas(16) int rowix[2][N];               // row of q and out, in d_head elements, of the query rows of an item and the next
     float vmax[PARTS][4];            // largest of V's scales of a unit, by part and warp
     int64_t scratch[32];
     int64_t sums[1];                 // [n_seqs + 1]
@@ -482,16 +483,27 @@ __global__ void __launch_bounds__(THREADS, 1) k_attn_kv4_tc(const __grid_constan
         for (int n = 0;; ++n) {
             if (n > 0) {
                 // ---- sums of the rows over the four warps that share them
+                // (eight lanes have parts of 16 sums: every exchange halves the sums that a lane still has, until lane g has those of
+                // block g % 4, of weights or of middles)
+                float2 a[2 * NB];
 #pragma unroll
-                for (int j = 0; j < NB; ++j)
+                for (int j = 0; j < NB; ++j) {
+                    a[j] = l[j];
+                    a[NB + j] = ms[j];
+                }
 #pragma unroll
-                    for (int e = 0; e < 2; ++e) {
-                        float a = e ? l[j].y : l[j].x, c = e ? ms[j].y : ms[j].x;
+                for (int h = NB, bit = 4; h >= 1; h >>= 1, bit >>= 1)
 #pragma unroll
-                        for (int o = 4; o < 32; o <<= 1) { a += __shfl_xor_sync(0xffffffffu, a, o); c += __shfl_xor_sync(0xffffffffu, c, o); }
-                        const int rl = col8(j) + 2 * t + e;
-                        if (g == 0) { sm->x[quad][rl] = a; sm->y[quad][rl] = c; if (quad == 0) sm->fac[rl] = (none >> (2 * j + e)) & 1u ? -INFINITY : -(e ? neg[j].y : neg[j].x); }
+                    for (int k = 0; k < h; ++k) {
+                        const float2 keep = g & bit ? a[k + h] : a[k], send = g & bit ? a[k] : a[k + h];
+                        a[k] = add2(keep, make_float2(__shfl_xor_sync(0xffffffffu, send.x, 4 * bit), __shfl_xor_sync(0xffffffffu, send.y, 4 * bit)));
                     }
+                *reinterpret_cast<float2*>(&(g & 4 ? sm->y : sm->x)[quad][col8(g & 3) + 2 * t]) = a[0];
+                if (quad == 0 && g == 0) {
+#pragma unroll
+                    for (int j = 0; j < NB; ++j)
+                        *reinterpret_cast<float2*>(&sm->fac[col8(j) + 2 * t]) = make_float2((none >> (2 * j)) & 1u ? -INFINITY : -neg[j].x, (none >> (2 * j + 1)) & 1u ? -INFINITY : -neg[j].y);
+                }
             }
             if (tid == 0) sm->cur[n % 3] = item_get(n);
             named_sync<1, SOFT>();
@@ -549,18 +561,24 @@ __global__ void __launch_bounds__(THREADS, 1) k_attn_kv4_tc(const __grid_constan
 #pragma unroll 1
                 for (int j = 0; j < NB && col8(j) < lrows; ++j) {
                     uint32_t o[8];
-                    const int r0 = col8(j);
+                    const int r0 = col8(j), left = lrows - r0;
                     ld_cols8(tmem + SH::T_O + r0 + ((uint32_t)(quad * 32) << 16), o);
-                    ld_wait();
+                    float4 tm[8];
 #pragma unroll
-                    for (int x = 0; x < 8; ++x) {
-                        const int rl = r0 + x;
-                        const float4 tm = sm->tot[rl];
-                        const float v = fmaf(__uint_as_float(o[x]), vinv, tm.z);
-                        if (rl < lrows) {
-                            if (whole) ((__half*)p.out)[(size_t)sm->rowix[(n - 1) & 1][rl] * D + chn] = __float2half_rn(v * tm.y);
-                            else __stcg(slot + rl * D + chn, v);
-                        }
+                    for (int x = 0; x < 8; ++x) tm[x] = sm->tot[r0 + x];
+                    const int4 ia = *reinterpret_cast<const int4*>(&sm->rowix[(n - 1) & 1][r0]), ib = *reinterpret_cast<const int4*>(&sm->rowix[(n - 1) & 1][r0 + 4]);
+                    const int ix[8] = {ia.x, ia.y, ia.z, ia.w, ib.x, ib.y, ib.z, ib.w};
+                    ld_wait();
+                    if (whole) {
+                        __half* out = (__half*)p.out + chn;
+#pragma unroll
+                        for (int x = 0; x < 8; ++x)
+                            if (x < left) out[(size_t)ix[x] * D] = __float2half_rn(fmaf(__uint_as_float(o[x]), vinv, tm[x].z) * tm[x].y);
+                    } else {
+                        float* out = slot + r0 * D + chn;
+#pragma unroll
+                        for (int x = 0; x < 8; ++x)
+                            if (x < left) __stcg(out + x * D, fmaf(__uint_as_float(o[x]), vinv, tm[x].z));
                     }
                 }
             }
