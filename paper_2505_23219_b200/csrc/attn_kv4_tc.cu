@@ -19,12 +19,13 @@
 //
 // Work is dealt as in attn_kv4.cu, one CTA an SM.
 //
-// What it costs.  8 ragged trees of up to 64 nodes over up to 8192 rows, 32 heads (148 MB, 30 GFLOP): 130 us; one tree of 256 nodes over
-// 4096 rows, 40 heads (22 GFLOP): 89 us.  A unit of 128 keys x 64 rows takes about 2700 clocks where its products take 900 and its
-// exponentials 500: the softmax warps' chain (fetch, scores, agreement on references, wait for a P buffer, weights, hand-over), at
-// 2.0 instructions an SM a clock; K and V are two units ahead.  An item costs about six units besides (queries in, filling and
-// draining, sums out, merge), a launch 6 us before the first.  Measured and dropped: 16 softmax warps on one unit, two groups of eight
-// on units in turn (142 us: 88 registers a thread spill), tiles of 128 rows.
+// What it costs.  8 ragged trees of up to 64 nodes over up to 8192 rows, 32 heads (148 MB, 30 GFLOP): 120 us; one tree of 256 nodes over
+// 4096 rows, 40 heads (22 GFLOP): 83 us.  A unit of 128 keys x 64 rows takes about 2700 clocks where its products take 900 and its
+// exponentials 500: the softmax warps' chain (in clocks: scores 550, agreement on references 270, fetch of the next scores 700, wait
+// for a P buffer 350 though it is free, weights 900, hand-over 250), at 2 instructions an SM a clock; K and V are two units ahead.  A unit
+// with masked keys costs 2000 more, raising references 1700.  An item costs about 9000 besides (queries 3000, sums 900, sums out
+// 2500, arrival and merge 2400 where it is split), a launch 11000 before the first scores.  Measured and dropped: 16 softmax warps on
+// one unit, two groups of eight on units in turn (142 us against 132: 88 registers a thread spill), tiles of 128 rows.
 #include <cstddef>
 #include <cstdio>
 #include <type_traits>
@@ -50,7 +51,7 @@ static_assert(N / 8 / PARTS == 4, "a lane of eight ends up with one of 4 + 4 blo
 constexpr int REGS_LAUNCH = 96, REGS_SOFT = 152, REGS_CONV = 56, REGS_ISSUE = 56;
 static_assert(SOFT * REGS_SOFT + CONV * REGS_CONV + 128 * REGS_ISSUE <= THREADS * REGS_LAUNCH && THREADS * REGS_LAUNCH <= 65536, "register split");
 constexpr float RAISE = 8.f;
-constexpr int LEAD = 6;                        // an item's fixed cost in units (8 ragged trees: 0: 410 us, 4: 147, 6: 133, 10: 136, 16: 142)
+constexpr int LEAD = 4;                        // an item's fixed cost in units (8 ragged trees: 3: 124 us, 4: 120, 5: 120, 6: 122; one of 64 nodes over 512 rows: 20.5, 20.5, 21.9, 22.0)
 // What the softmax warps need of a unit's keys is ready when its keys are.  The K warps are two units ahead of the first
 // product, that is two ahead of the scores being fetched, and those one ahead of what the softmax warps work on: five in use.
 constexpr int PAR_SLOTS = 8;
