@@ -505,9 +505,14 @@ def ghd_kv4_read(ctx: Ctx, kv: Kv4Cache, pool, row_start, n_rows: int, first=Non
         raise GhdError(1, "kv4_read: negative n_rows")
     if k_out is None:
         k_out = ctx.blank.new_empty(shape)
+        kp = k_out.data_ptr()
+    else:
+        kp = _need(k_out, ctx.dtype, "k_out", shape[0] * shape[1], ctx.dev)
     if v_out is None:
-        v_out = ctx.blank.new_empty(shape)
-    kp, vp = _need(k_out, ctx.dtype, "k_out", shape[0] * shape[1], ctx.dev), _need(v_out, ctx.dtype, "v_out", shape[0] * shape[1], ctx.dev)
+        v_out = torch.empty_like(k_out) if k_out.shape == shape else ctx.blank.new_empty(shape)
+        vp = v_out.data_ptr()
+    else:
+        vp = _need(v_out, ctx.dtype, "v_out", shape[0] * shape[1], ctx.dev)
     st = ctx.lib.ghd_kv4_read(ctx.handle, kv.ref, rows.ref, at, None if first is None else _need(first, torch.int32, "first", kv.n_seqs, ctx.dev), kp, vp)
     if st:
         ctx._check(st)

@@ -19,8 +19,8 @@
 //
 // What it costs.  One token over 2048 rows of 32 heads (8.9 MB): 11.3 us, a chain of latencies (in clocks: lengths and prefix sums 2300,
 // item 2000, page ids and first rows 2200, queries 1200, two chunks 4000, sums 1500, arrival 2000, merge 2500); over 16384 rows 27 us,
-// 2.6 TB/s.  One token each of 32 ragged sequences of up to 8192 rows, 32 heads on 8 (174.5 MB): 53 us, 3.3 TB/s.  That is instructions: 750 a warp for 32 keys (9 for a word of eight codes, 32 words a lane; the
-// products are 32), 2.2 an SM a clock out of 12 warps (163 registers a thread).  Four CTAs an SM spill, deeper rings take CTAs away.
+// 2.6 TB/s.  One token each of 32 ragged sequences of up to 8192 rows, 32 heads on 8 (174.5 MB): 53 us, 3.3 TB/s.  That is instructions: 690 a warp for 32 keys (9 for a word of eight codes, 32 words a lane; the
+// products are 32), 2.2 an SM a clock out of 12 warps (162 registers a thread).  Four CTAs an SM spill, deeper rings take CTAs away.
 #include "attn_kv4_dev.cuh"
 
 #include <cuda_bf16.h>
