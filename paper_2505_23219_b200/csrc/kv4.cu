@@ -171,7 +171,7 @@ __global__ void __launch_bounds__(ROW_WARPS * 32, 4) k_kv4_append(const __grid_c
     const int lane = threadIdx.x & 31, j = lane % LPH, sub = lane / LPH;
     const int wid = blockIdx.x * ROW_WARPS + (threadIdx.x >> 5), slice = wid % slices;
     const int R = 1 << w.shift, kv_jobs = (w.heads + HPW - 1) / HPW, q_jobs = (q_heads + HPW - 1) / HPW;
-    const bool queries = blockIdx.y != 0;
+    const bool do_q = q && (gridDim.y == 1 || blockIdx.y != 0), do_kv = blockIdx.y == 0;
     struct Pair { Raw8<T> a, b; };
     RowOwner o;
     o.end = -1;
@@ -184,7 +184,7 @@ __global__ void __launch_bounds__(ROW_WARPS * 32, 4) k_kv4_append(const __grid_c
         const int slot = o.q.len + (row - o.q.row0);
         const int p0 = pos ? __ldg(pos + row) : slot;
         // 16 values a lane of a job; which: 0 K, 1 V, 2 q
-        auto ask = [&](int job) {
+        auto ask = [&](int job, bool queries) {
             Pair x{};
             const int which = queries ? 2 : job >= kv_jobs, h = (which == 1 ? job - kv_jobs : job) * HPW + sub;
             if (job < (queries ? q_jobs : 2 * kv_jobs) && h < (queries ? q_heads : w.heads)) {
@@ -194,11 +194,11 @@ __global__ void __launch_bounds__(ROW_WARPS * 32, 4) k_kv4_append(const __grid_c
             }
             return x;
         };
-        Pair next = ask(slice), after = ask(slice + slices);
+        Pair next = ask(slice, do_q), after = ask(slice + slices, do_q);
         double mc[ANG], msn[ANG];                                   // angles ANG lane + i
 #pragma unroll
         for (int i = 0; i < ANG; ++i) sincos_turns((double)p0 * fr.f[ANG * lane + i], msn[i], mc[i]);
-        if (queries) {                                              // rotated in 32 bits, rounded once
+        if (do_q) {                                                 // rotated in 32 bits, rounded once
             float cs[8], sn[8];                                     // angles 8 j + i
 #pragma unroll
             for (int i = 0; i < 8; ++i) {
@@ -209,7 +209,7 @@ __global__ void __launch_bounds__(ROW_WARPS * 32, 4) k_kv4_append(const __grid_c
             for (int job = slice; job < q_jobs; job += slices) {
                 const Pair now = next;
                 next = after;
-                after = ask(job + 2 * slices);
+                after = ask(job + 2 * slices, true);
                 float a[8], b[8], c[8], d[8];
                 floats<T>(now.a, a);
                 floats<T>(now.b, b);
@@ -225,7 +225,9 @@ __global__ void __launch_bounds__(ROW_WARPS * 32, 4) k_kv4_append(const __grid_c
                     store8<T>(y + R2, d);
                 }
             }
-            continue;
+            if (!do_kv) continue;
+            next = ask(slice, false);
+            after = ask(slice + slices, false);
         }
         const int page = row - o.q.row0 < o.q.n_new ? kv4_page(w, o.seq, slot) : -1;
         if (page < 0) continue;
@@ -240,7 +242,7 @@ __global__ void __launch_bounds__(ROW_WARPS * 32, 4) k_kv4_append(const __grid_c
         for (int job = slice; job < 2 * kv_jobs; job += slices) {
             const Pair now = next;
             next = after;
-            after = ask(job + 2 * slices);
+            after = ask(job + 2 * slices, false);
             const int which = job >= kv_jobs, h = (which ? job - kv_jobs : job) * HPW + sub;
             float a[8], b[8], x[16];
             floats<T>(now.a, a);
@@ -525,7 +527,7 @@ ghd_status ghd_kv4_append(ghd_ctx* c, const ghd_kv4* kv, const ghd_kv4_rows* row
     const Kv4View w = kv4_view(c, kv, rows);
     const int hpw = 32 / (D / 16);
     const RowGrid g = row_grid(c, rows->n_rows, ((q ? m.n_heads : 2 * kv->n_kv_heads) + hpw - 1) / hpw);
-    const dim3 grid(g.blocks, q ? 2 : 1);
+    const dim3 grid(g.blocks, q && g.slices > 1 ? 2 : 1);
 #define GHD_APPEND(T, DH) k_kv4_append<T, DH><<<grid, ROW_WARPS * 32, 0, c->cur>>>(w, fr, (uint8_t*)pool, rows->pos, (const T*)q, q_ld, (const T*)k, (const T*)v, kv_ld, (T*)q_out, m.n_heads, g.slices, g.rows_each)
     if (m.dtype == GHD_F32) { if (D == 64) GHD_APPEND(float, 64); else GHD_APPEND(float, 128); }
     else { if (D == 64) GHD_APPEND(__half, 64); else GHD_APPEND(__half, 128); }
