@@ -153,18 +153,19 @@ __device__ __forceinline__ void find_owner(const Kv4View& w, int row, bool lengt
 }
 
 constexpr int ROW_WARPS = 4;       // warps of a block; each has rows of its own
+constexpr int APPEND_RESIDENT = 16;     // warps of k_kv4_append on an SM at a time
 
-// Blocks of blockIdx.y 0 append, those of 1 rotate the queries.  A warp takes a row and every `slices`-th of its jobs: a job is
-// the K, V or q rows of HPW heads, D / 16 lanes each.  Lane j of a head holds the pairs t = 8 j .. 8 j + 7 with both halves (K, q),
-// so the rotation needs no exchange and its codes are two words; of V the 16 channels from 16 j on.  What the next two jobs
-// read is asked for ahead.  The row's angles (64-bit sincos, D / 2 of them) are shared out over the lanes and passed round by
-// shuffles.  One row of 32 heads takes 4.3 us, a launch and a chain of loads.  8 ragged prompts of up to 2048 rows (32 heads on 8;
-// q in and out, k and v in, codes out: 277 MB) take 85 us, 3.3 TB/s: 43 M instructions at 1.8 an SM a clock, half of them the
-// codes of K and V, on 16 warps an SM (125 registers).  More warps with spills: 79 us, but one row 5.2; the queries in a launch
-// of their own, with half the registers: 76, but up to half as long again for 512 to 2048 rows in all.  32 bits instead of 64 for the
-// rotation or the angles would save 2 us.
+// Rotates the queries and appends keys and values; in a grid of two rows blockIdx.y 0 does the latter and 1 the former.  A warp
+// takes a row and every `slices`-th of its jobs: a job is the K, V or q rows of HPW heads, D / 16 lanes each.  Lane j of a head holds
+// the pairs t = 8 j .. 8 j + 7 with both halves (K, q), so the rotation needs no exchange and its codes are two words; of V the 16
+// channels from 16 j on.  What the next two jobs read is asked for ahead.  The row's angles (64-bit sincos, D / 2 of them) are
+// shared out over the lanes and passed round by shuffles.
+// One row of 32 heads takes 4.0 us, a launch and a chain of loads; 2048 rows, 32 heads on 8, 12.6.  8 ragged prompts of up to 2048 rows
+// (q in and out, k and v in, codes out: 277 MB) take 75 us, 3.7 TB/s, of which the queries are 37; 16 warps an SM (125 registers) wait
+// for loads and for one another's results.  More warps with spills: 79 us when this took 85, but one row 5.2 instead of 4.3; quotients
+// in paired instructions: slower.  32 bits instead of 64 for the rotation or the angles would save 2 us.
 template <typename T, int D>
-__global__ void __launch_bounds__(ROW_WARPS * 32, 4) k_kv4_append(const __grid_constant__ Kv4View w, const __grid_constant__ RopeFreq fr, uint8_t* __restrict__ pool,
+__global__ void __launch_bounds__(ROW_WARPS * 32, APPEND_RESIDENT / ROW_WARPS) k_kv4_append(const __grid_constant__ Kv4View w, const __grid_constant__ RopeFreq fr, uint8_t* __restrict__ pool,
                                                                const int32_t* __restrict__ pos, const T* q, int64_t q_ld, const T* __restrict__ k,
                                                                const T* __restrict__ v, int64_t kv_ld, T* q_out, int q_heads, int slices, int rows_each) {
     constexpr int R2 = D / 2, LPH = D / 16, HPW = 32 / LPH, ANG = R2 / 32, es = (int)sizeof(T);
@@ -439,11 +440,13 @@ __global__ void k_kv4_advance(Kv4View w, int32_t* kv_len, const ghd_accept_resul
     kv_len[s] = sq.len + add;
 }
 
-// Warps of a call over rows: as many as the device holds at a time and a few times that.  Few rows: their jobs are dealt to
-// several warps (slices); many: a warp takes several rows in turn, whose sequence it then looks up once.
+// Warps of a call over rows; `resident`: those that an SM holds at a time.  Few rows: their jobs are dealt to several warps
+// (slices) until the device is full once, and no further, since every warp of a row works out its angles (append with four
+// times as many: 512 / 1024 / 2048 rows of 32 heads on 8 took 11.6 / 20.0 / 23.1 us, now 8.2 / 10.0 / 12.6).  Many rows: a warp takes
+// several in turn, whose sequence it then looks up once.
 struct RowGrid { int slices, rows_each, blocks; };
-RowGrid row_grid(const ghd_ctx* c, int n_rows, int jobs) {
-    const int64_t want = (int64_t)c->sm_count * 64;
+RowGrid row_grid(const ghd_ctx* c, int n_rows, int jobs, int resident) {
+    const int64_t want = (int64_t)c->sm_count * resident;
     RowGrid g;
     int64_t s = want / n_rows;
     g.slices = (int)(s < 1 ? 1 : (s > jobs ? jobs : s));
@@ -526,8 +529,12 @@ ghd_status ghd_kv4_append(ghd_ctx* c, const ghd_kv4* kv, const ghd_kv4_rows* row
     memcpy(fr.f, c->rope_freq, sizeof(fr.f));
     const Kv4View w = kv4_view(c, kv, rows);
     const int hpw = 32 / (D / 16);
-    const RowGrid g = row_grid(c, rows->n_rows, ((q ? m.n_heads : 2 * kv->n_kv_heads) + hpw - 1) / hpw);
-    const dim3 grid(g.blocks, q && g.slices > 1 ? 2 : 1);
+    const int q_jobs = (m.n_heads + hpw - 1) / hpw, kv_jobs = 2 * ((kv->n_kv_heads + hpw - 1) / hpw);
+    const RowGrid g = row_grid(c, rows->n_rows, q ? q_jobs : kv_jobs, APPEND_RESIDENT);
+    // Blocks of their own for the queries while all fit the device at once (one row 4.0 us, 64 rows 4.7); else a warp does both, with
+    // one set of angles (512 / 1024 rows of 32 heads on 8: 8.2 / 9.9 us apart, 6.5 / 8.6 together).
+    const bool apart = q && 2 * (int64_t)rows->n_rows * q_jobs <= (int64_t)c->sm_count * APPEND_RESIDENT;
+    const dim3 grid(g.blocks, apart ? 2 : 1);
 #define GHD_APPEND(T, DH) k_kv4_append<T, DH><<<grid, ROW_WARPS * 32, 0, c->cur>>>(w, fr, (uint8_t*)pool, rows->pos, (const T*)q, q_ld, (const T*)k, (const T*)v, kv_ld, (T*)q_out, m.n_heads, g.slices, g.rows_each)
     if (m.dtype == GHD_F32) { if (D == 64) GHD_APPEND(float, 64); else GHD_APPEND(float, 128); }
     else { if (D == 64) GHD_APPEND(__half, 64); else GHD_APPEND(__half, 128); }
@@ -561,7 +568,7 @@ ghd_status ghd_kv4_read(ghd_ctx* c, const ghd_kv4* kv, const ghd_kv4_rows* rows,
     OnDevice dev(c);
     const Kv4View w = kv4_view(c, kv, rows);
     const int hpw = 32 / (c->cfg.d_head / 8);
-    const RowGrid g = row_grid(c, rows->n_rows, (kv->n_kv_heads + hpw - 1) / hpw);
+    const RowGrid g = row_grid(c, rows->n_rows, (kv->n_kv_heads + hpw - 1) / hpw, 64);
 #define GHD_READ(T, DH) k_kv4_read<T, DH><<<g.blocks, ROW_WARPS * 32, 0, c->cur>>>(w, (const uint8_t*)pool, first, (T*)k_out, (T*)v_out, g.slices, g.rows_each)
     if (c->cfg.dtype == GHD_F32) { if (c->cfg.d_head == 64) GHD_READ(float, 64); else GHD_READ(float, 128); }
     else { if (c->cfg.d_head == 64) GHD_READ(__half, 64); else GHD_READ(__half, 128); }
