@@ -450,7 +450,7 @@ RowGrid row_grid(const ghd_ctx* c, int n_rows, int jobs, int resident) {
     RowGrid g;
     int64_t s = want / n_rows;
     g.slices = (int)(s < 1 ? 1 : (s > jobs ? jobs : s));
-    g.rows_each = (int)((n_rows + 4 * want - 1) / (4 * want));
+    g.rows_each = (int)((n_rows + want - 1) / want);
     const int64_t warps = ((int64_t)n_rows + g.rows_each - 1) / g.rows_each * g.slices;
     g.blocks = (int)((warps + ROW_WARPS - 1) / ROW_WARPS);
     return g;
