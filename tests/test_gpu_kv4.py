@@ -844,3 +844,73 @@ def test_commit_of_long_paths_that_overlap_themselves(ghd, dtype, d):
     ghd.ghd_sync_status(su.ctx)
     assert su.kv_len.cpu().tolist() == okv4.commit(host, su.table, lens, su.start, paths) == [22, 10, 171]
     assert np.array_equal(su.dpool.cpu().numpy(), host[0].data.reshape(-1))
+
+
+@pytest.mark.parametrize("dtype", ["f16", "f32"])
+def test_a_long_call_is_its_pieces(ghd, dtype):
+    """12,000 rows of five sequences appended and read at once (a warp has several rows, and queries and keys of each) against a
+    call for every 300 of them: queries, pool and rows read equal to the bit; queries in place too."""
+    import torch
+    H, Hk, d, R, n = 4, 2, 64, 32, 12000
+    ctx = make_ctx(ghd, H, d, dtype)
+    r = np.random.RandomState(101)
+    cnt = np.array([5000, 0, 1, 6000, 999])
+    start = np.concatenate(([0], np.cumsum(cnt)))
+    lens = np.array([3, 7, 0, 40, 100])
+    pages = -(-(lens + cnt) // R)
+    table = np.zeros((5, pages.max()), np.int32)
+    order = r.permutation(pages.sum())
+    for s in range(5):
+        table[s, :pages[s]] = order[pages[:s].sum():pages[: s + 1].sum()]
+    T = torch.float16 if dtype == "f16" else torch.float32
+    gen = torch.Generator(device="cuda").manual_seed(5)
+    x = torch.randn(n, (H + 2 * Hk) * d, device="cuda", generator=gen).to(T)
+    pos = dev(r.randint(0, 5000, n).astype(np.int32))
+    q, k, v = (t.contiguous() for t in x.split((H * d, Hk * d, Hk * d), 1))
+    kv = ghd.Kv4Cache(dev(table), dev(lens.astype(np.int32)), R, Hk, int(pages.sum()))
+    whole = ghd.ghd_kv4_pool(ctx, kv)[0]
+    all_rows = dev(start.astype(np.int32))
+    qa = ghd.ghd_kv4_append(ctx, kv, ghd.Kv4Rows(all_rows, n, pos=pos), whole, q, k, v)
+    ka, va = ghd.ghd_kv4_read(ctx, kv, whole, all_rows, n)
+    parts, qb, kb, vb = torch.zeros_like(whole), torch.empty_like(qa), torch.empty_like(ka), torch.empty_like(va)
+    for s in range(5):
+        for i in range(0, cnt[s], 300):
+            m = min(300, cnt[s] - i)
+            at = slice(start[s] + i, start[s] + i + m)
+            one = ghd.Kv4Cache(dev(table[s:s + 1]), dev(np.array([lens[s] + i], np.int32)), R, Hk, int(pages.sum()))
+            few = dev(np.array([0, m], np.int32))
+            qb[at] = ghd.ghd_kv4_append(ctx, one, ghd.Kv4Rows(few, m, pos=pos[at].contiguous()), parts, q[at], k[at], v[at])
+            kb[at], vb[at] = ghd.ghd_kv4_read(ctx, one, parts, few, m)
+    ghd.ghd_sync_status(ctx)
+    for a, b in ((qa, qb), (whole, parts), (ka, kb), (va, vb)):
+        assert bool((a == b).all())
+    qc = q.clone()
+    ghd.ghd_kv4_append(ctx, kv, ghd.Kv4Rows(all_rows, n, pos=pos), whole, qc, k, v, q_out=qc)
+    assert bool((qc == qa).all()) and bool((whole == parts).all())
+    ghd.ghd_sync_status(ctx)
+
+
+def test_commit_of_more_layers_than_one_launch_takes(ghd):
+    import torch
+    su = Setup(ghd, 2, 1, 64, "f16", 16, [20, 3], [6, 5], 47)
+    L = 70
+    pools = torch.from_numpy(su.r.randint(0, 256, (L, su.dpool.numel())).astype(np.uint8)).cuda()
+    host = [okv4.Pool(su.pool.data.shape[0], 1, 16, 64, "f16", data=p.cpu().numpy().reshape(su.pool.data.shape)) for p in pools]
+    paths = [(2, [0, 3, 5]), (1, [0, 4])]
+    res = np.zeros((2, 514), np.int32)
+    for s, (m, nodes) in enumerate(paths):
+        res[s, 0], res[s, 1], res[s, 2:3 + m] = m, m + 1, nodes
+    ghd.ghd_kv4_commit(su.ctx, su.kv, ghd.Kv4Rows(dev(su.start), su.n), pools, dev(res))
+    ghd.ghd_sync_status(su.ctx)
+    assert su.kv_len.cpu().tolist() == okv4.commit(host, su.table, [20, 3], su.start, paths)
+    assert np.array_equal(pools.cpu().numpy(), np.stack([h.data.reshape(-1) for h in host]))
+
+
+def test_keys_that_the_rotation_takes_below_the_range(ghd):
+    su = Setup(ghd, 2, 1, 128, "f16", 16, [0], [3], 49)
+    k = su.r.randn(3, 128).astype(np.float16)
+    k[1, :64], k[1, 64:] = -60000, 60000                            # by 0.75 radians: -60000 (cos + sin) = -84800
+    ghd.ghd_kv4_append(su.ctx, su.kv, ghd.Kv4Rows(dev(su.start), 3, pos=dev(np.ones(3, np.int32))), su.dpool, None, dev(k), dev(su.r.randn(3, 128).astype(np.float16)))
+    kb, vb = (x.float().cpu().numpy() for x in ghd.ghd_kv4_read(su.ctx, su.kv, su.dpool, dev(su.start), 3))
+    ghd.ghd_sync_status(su.ctx)
+    assert np.isneginf(kb[1]).all() and np.isfinite(kb[[0, 2]]).all() and np.isfinite(vb).all()
