@@ -35,10 +35,6 @@ template <typename T> __device__ __forceinline__ float to_f(T v);
 template <> __device__ __forceinline__ float to_f<float>(float v) { return v; }
 template <> __device__ __forceinline__ float to_f<__half>(__half v) { return __half2float(v); }
 
-template <typename T> __device__ __forceinline__ float2 load_params(const uint8_t* p);        // (scale, min)
-template <> __device__ __forceinline__ float2 load_params<__half>(const uint8_t* p) { return __half22float2(__ldg(reinterpret_cast<const __half2*>(p))); }
-template <> __device__ __forceinline__ float2 load_params<float>(const uint8_t* p) { return __ldg(reinterpret_cast<const float2*>(p)); }
-
 template <typename T> __device__ __forceinline__ void store4(T* p, float a, float b, float c, float d);
 template <> __device__ __forceinline__ void store4<float>(float* p, float a, float b, float c, float d) { *reinterpret_cast<float4*>(p) = make_float4(a, b, c, d); }
 template <> __device__ __forceinline__ void store4<__half>(__half* p, float a, float b, float c, float d) {
