@@ -161,7 +161,7 @@ constexpr int APPEND_RESIDENT = 16;     // warps of k_kv4_append on an SM at a t
 // channels from 16 j on.  What the next two jobs read is asked for ahead.  The row's angles (64-bit sincos, D / 2 of them) are
 // shared out over the lanes and passed round by shuffles.
 // One row of 32 heads takes 4.0 us, a launch and a chain of loads; 2048 rows, 32 heads on 8, 12.6.  8 ragged prompts of up to 2048 rows
-// (q in and out, k and v in, codes out: 277 MB) take 75 us, 3.7 TB/s, of which the queries are 37; 16 warps an SM (125 registers) wait
+// (q in and out, k and v in, codes out: 277 MB) take 74 us, 3.7 TB/s, of which the queries are 37; 16 warps an SM (126 registers) wait
 // for loads and for one another's results.  More warps with spills: 79 us when this took 85, but one row 5.2 instead of 4.3; quotients
 // in paired instructions: slower.  32 bits instead of 64 for the rotation or the angles would save 2 us.
 template <typename T, int D>
