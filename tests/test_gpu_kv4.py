@@ -914,3 +914,16 @@ def test_keys_that_the_rotation_takes_below_the_range(ghd):
     kb, vb = (x.float().cpu().numpy() for x in ghd.ghd_kv4_read(su.ctx, su.kv, su.dpool, dev(su.start), 3))
     ghd.ghd_sync_status(su.ctx)
     assert np.isneginf(kb[1]).all() and np.isfinite(kb[[0, 2]]).all() and np.isfinite(vb).all()
+
+
+def test_broadcast_rows_are_refused_before_a_launch(ghd):
+    import torch
+    su = Setup(ghd, 4, 2, 64, "f16", 16, [4], [2], 62)
+    rows = ghd.Kv4Rows(dev(su.start), 2)
+    q, k = torch.zeros((2, 256), dtype=torch.float16, device="cuda"), torch.zeros((2, 128), dtype=torch.float16, device="cuda")
+    before, launches = su.dpool.clone(), ghd.ghd_launch_count(su.ctx)
+    for args in ((q[:1].expand(2, 256), k, k), (q, k[:1].expand(2, 128), k[:1].expand(2, 128)), (None, k, k[:1].expand(2, 128))):
+        with pytest.raises(ghd.GhdError) as e:
+            ghd.ghd_kv4_append(su.ctx, su.kv, rows, su.dpool, *args)
+        assert e.value.name == "GHD_EINVAL"
+    assert ghd.ghd_launch_count(su.ctx) == launches and bool((su.dpool == before).all())

@@ -244,3 +244,24 @@ def test_going_on_to_the_next_item_is_the_search_for_it(lay, seed):
         p = lambda a: a.ctypes.data_as(C.c_void_p)  # noqa: E731
         n = lay.walk(S, p(start), p(ln), int(start[-1]), C.c_longlong(4000), heads, group, rows, 128, lead, ctas)
         assert n >= 0 and (n > 0) == (start[-1] > 0)
+
+
+def _host_ctx(dtype="f16"):
+    """What the checks of a call's tensors look at, for tensors on the host (device -1)."""
+    import types
+    import torch
+    return types.SimpleNamespace(dtype=torch.float16 if dtype == "f16" else torch.float32, dev=-1)
+
+
+def test_rows_that_overlap_are_refused():
+    """A broadcast row has stride 0: the call would take it for contiguous rows and read behind it."""
+    import torch
+    import paper_2505_23219_b200 as ghd
+    from paper_2505_23219_b200 import binding
+    x = torch.zeros((1, 256), dtype=torch.float16)
+    for bad in (x.expand(64, 256), torch.zeros(64 * 256, dtype=torch.float16).as_strided((64, 256), (128, 1)), torch.zeros(400, dtype=torch.float16).as_strided((2, 256), (8, 1))):
+        with pytest.raises(ghd.GhdError, match="overlap"):
+            binding._kv4_strided(_host_ctx(), bad, bad.shape[0], 256, "k")
+    wide = torch.zeros((64, 768), dtype=torch.float16)
+    for at in (0, 256, 512):
+        assert binding._kv4_strided(_host_ctx(), wide[:, at:at + 256], 64, 256, "k") == (wide.data_ptr() + 2 * at, 768)
