@@ -457,12 +457,13 @@ def _kv4_pool(ctx: Ctx, kv: Kv4Cache, pool):
 
 
 def _kv4_strided(ctx: Ctx, t, n: int, width: int, what: str):
-    """Rows of `width` elements, contiguous inside a row and apart from one another -> (pointer, row stride)."""
+    """Rows of `width` elements, contiguous inside a row and apart from one another -> (pointer, row stride; 0 for a single row,
+    whose stride says nothing)."""
     if t.dim() != 2 or t.shape[0] < n or t.shape[1] != width or t.stride(1) != 1 or t.dtype != ctx.dtype or t.get_device() != ctx.dev:
         raise GhdError(1, f"{what}: want {ctx.dtype} [{n}][{width}] with contiguous rows on cuda:{ctx.dev}, got {tuple(t.shape)} {t.dtype} on {t.device}")
     if n > 1 and t.stride(0) < width:       # a broadcast row has stride 0, which the call takes for rows one behind the other
         raise GhdError(1, f"{what}: rows of {width} elements overlap (row stride {t.stride(0)})")
-    return t.data_ptr(), t.stride(0)
+    return t.data_ptr(), t.stride(0) if n > 1 else 0
 
 
 def ghd_kv4_append(ctx: Ctx, kv: Kv4Cache, rows: Kv4Rows, pool, q, k, v, q_out=None):

@@ -927,3 +927,22 @@ def test_broadcast_rows_are_refused_before_a_launch(ghd):
             ghd.ghd_kv4_append(su.ctx, su.kv, rows, su.dpool, *args)
         assert e.value.name == "GHD_EINVAL"
     assert ghd.ghd_launch_count(su.ctx) == launches and bool((su.dpool == before).all())
+
+
+@pytest.mark.parametrize("dtype", ["f16", "f32"])
+def test_append_of_one_row_takes_any_row_stride(ghd, dtype):
+    """q of one row in a wider buffer, rotated in place; k a transposed column; v a column block: as contiguous copies give."""
+    import torch
+    H, Hk, d = 4, 2, 64
+    su = Setup(ghd, H, Hk, d, dtype, 16, [9], [1], 63, garbage=False)
+    rows = ghd.Kv4Rows(dev(su.start), 1)
+    q, k, v = (dev(su.r.randn(1, w * d).astype(su.np_t)) for w in (H, Hk, Hk))
+    want_pool = su.dpool.clone()
+    want_q = ghd.ghd_kv4_append(su.ctx, su.kv, rows, want_pool, q, k, v)
+    wide = torch.zeros((1, 1024), dtype=q.dtype, device="cuda")
+    wide[:, 256:512], wide[:, 512:640] = q, v
+    qi = wide[:, 256:512]
+    got = ghd.ghd_kv4_append(su.ctx, su.kv, rows, su.dpool, qi, k.reshape(Hk * d, 1).clone().t(), wide[:, 512:640], q_out=qi)
+    ghd.ghd_sync_status(su.ctx)
+    assert got.data_ptr() == qi.data_ptr() and bool((qi == want_q).all()) and bool((su.dpool == want_pool).all())
+    assert not wide[:, :256].any() and bool((wide[:, 512:640] == v).all()) and not wide[:, 640:].any()

@@ -265,3 +265,12 @@ def test_rows_that_overlap_are_refused():
     wide = torch.zeros((64, 768), dtype=torch.float16)
     for at in (0, 256, 512):
         assert binding._kv4_strided(_host_ctx(), wide[:, at:at + 256], 64, 256, "k") == (wide.data_ptr() + 2 * at, 768)
+
+
+def test_the_stride_of_a_single_row_says_nothing():
+    import torch
+    from paper_2505_23219_b200 import binding
+    wide = torch.zeros((5, 768), dtype=torch.float16)
+    column = torch.zeros((256, 1), dtype=torch.float16)
+    for x in (wide[:1, :256], wide[3:4, 256:512], wide[:, 512:], column.t(), wide[:1, :256].expand(4, 256)):
+        assert binding._kv4_strided(_host_ctx(), x, 1, 256, "k") == (x.data_ptr(), 0)
