@@ -208,35 +208,43 @@ def _need(t, dtype, what: str, numel: int, dev: int | None = None):
     return t.data_ptr()
 
 
-class Kv4Cache:
+class _Description:
+    """Holds tensors beside the struct with their pointers, and does not change: an attribute that was set to another tensor would
+    free the one that the struct still points to.  (The constructors fill __dict__ in one go.)"""
+
+    def __setattr__(self, name, value):
+        raise AttributeError(f"{type(self).__name__}.{name} is fixed: write into its tensors, or make another {type(self).__name__}")
+
+    def __delattr__(self, name):
+        raise AttributeError(f"{type(self).__name__}.{name} is fixed")
+
+
+class Kv4Cache(_Description):
     """Paging of a 4-bit cache: page_table int32 [n_seqs][max_pages], kv_len int32 [n_seqs] (device tensors; the pools of
-    the layers come with each call).  The tensors are read when a kernel runs and have to stay alive until then."""
+    the layers come with each call).  The tensors are read when a kernel runs and have to stay alive until then; their contents may
+    change, the description may not."""
 
     def __init__(self, page_table, kv_len, page_rows: int, n_kv_heads: int, n_pages: int):
-        self.page_table, self.kv_len = page_table, kv_len
         if page_table.dim() != 2:
             raise GhdError(1, "kv4: page_table is not [n_seqs][max_pages]")
         n_seqs, max_pages = page_table.shape
-        table = _need(page_table, torch.int32, "page_table", 0)
-        self.dev = page_table.get_device()
-        self.n_seqs, self.n_kv_heads, self.n_rows = n_seqs, n_kv_heads, n_pages * n_kv_heads * page_rows
-        self.c = _Kv4(n_seqs, n_pages, page_rows, max_pages, n_kv_heads, table, _need(kv_len, torch.int32, "kv_len", n_seqs, self.dev))
-        self.ref = C.byref(self.c)
+        table, dev = _need(page_table, torch.int32, "page_table", 0), page_table.get_device()
+        c = _Kv4(n_seqs, n_pages, page_rows, max_pages, n_kv_heads, table, _need(kv_len, torch.int32, "kv_len", n_seqs, dev))
+        self.__dict__.update(page_table=page_table, kv_len=kv_len, dev=dev, n_seqs=n_seqs, n_kv_heads=n_kv_heads, n_rows=n_pages * n_kv_heads * page_rows,
+                             c=c, ref=C.byref(c))
 
 
-class Kv4Rows:
+class Kv4Rows(_Description):
     """The new rows of a call: row_start int32 [n_seqs + 1]; optional pos int32 [n_rows]; optional mask int64
     [n_rows][words], bit j of row i = the sequence's new row j is visible to it (device tensors)."""
 
     def __init__(self, row_start, n_rows: int, pos=None, mask=None):
-        self.row_start, self.n_rows, self.pos, self.mask = row_start, int(n_rows), pos, mask
-        start = _need(row_start, torch.int32, "row_start", 2)
-        self.n_starts = row_start.numel()
-        self.dev = row_start.get_device()
+        n_rows = int(n_rows)
+        start, dev = _need(row_start, torch.int32, "row_start", 2), row_start.get_device()
         words = 0 if mask is None else int(mask.shape[-1])
-        self.c = _Kv4Rows(self.n_rows, words, start, None if pos is None else _need(pos, torch.int32, "pos", self.n_rows, self.dev),
-                          None if mask is None else _need(mask, torch.int64, "mask", self.n_rows * words, self.dev))
-        self.ref = C.byref(self.c)
+        c = _Kv4Rows(n_rows, words, start, None if pos is None else _need(pos, torch.int32, "pos", n_rows, dev),
+                     None if mask is None else _need(mask, torch.int64, "mask", n_rows * words, dev))
+        self.__dict__.update(row_start=row_start, n_rows=n_rows, pos=pos, mask=mask, n_starts=row_start.numel(), dev=dev, c=c, ref=C.byref(c))
 
 
 class Tree:

@@ -274,3 +274,32 @@ def test_the_stride_of_a_single_row_says_nothing():
     column = torch.zeros((256, 1), dtype=torch.float16)
     for x in (wide[:1, :256], wide[3:4, 256:512], wide[:, 512:], column.t(), wide[:1, :256].expand(4, 256)):
         assert binding._kv4_strided(_host_ctx(), x, 1, 256, "k") == (x.data_ptr(), 0)
+
+
+@pytest.fixture
+def host_binding(monkeypatch):
+    """The binding with descriptions of tensors on the host."""
+    from paper_2505_23219_b200 import binding
+
+    def need(t, dtype, what, numel, dev=None):
+        assert t.dtype is dtype and t.numel() >= numel
+        return t.data_ptr()
+    monkeypatch.setattr(binding, "_need", need)
+    return binding
+
+
+def test_descriptions_keep_the_tensors_they_point_to(host_binding):
+    """The struct has the pointers from the start: another tensor, or another size, needs another description."""
+    import torch
+    i32 = lambda *s: torch.zeros(s, dtype=torch.int32)  # noqa: E731
+    kv = host_binding.Kv4Cache(i32(2, 4), i32(2), 16, 2, 8)
+    rows = host_binding.Kv4Rows(i32(3), 4, pos=i32(4), mask=torch.zeros((4, 1), dtype=torch.int64))
+    for x, names in ((kv, ("kv_len", "page_table", "n_seqs", "n_kv_heads", "n_rows", "dev", "c", "ref")), (rows, ("row_start", "pos", "mask", "n_rows", "n_starts", "dev", "c", "ref"))):
+        for name in names:
+            with pytest.raises(AttributeError):
+                setattr(x, name, i32(2))
+            with pytest.raises(AttributeError):
+                delattr(x, name)
+    kv.kv_len[1] = 7                                            # contents are the caller's
+    assert kv.c.kv_len == kv.kv_len.data_ptr() and kv.c.page_table == kv.page_table.data_ptr()
+    assert (rows.c.row_start, rows.c.pos, rows.c.mask) == (rows.row_start.data_ptr(), rows.pos.data_ptr(), rows.mask.data_ptr())
