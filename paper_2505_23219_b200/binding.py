@@ -208,6 +208,13 @@ def _need(t, dtype, what: str, numel: int, dev: int | None = None):
     return t.data_ptr()
 
 
+def _int32(**numbers):
+    """Refuses numbers that the struct could not hold: ctypes would cut them off, and sizes be checked against other numbers."""
+    for what, x in numbers.items():
+        if not -2**31 <= x < 2**31:
+            raise GhdError(1, f"kv4: {what} = {x} is outside 32 bits")
+
+
 class _Description:
     """Holds tensors beside the struct with their pointers, and does not change: an attribute that was set to another tensor would
     free the one that the struct still points to.  (The constructors fill __dict__ in one go.)"""
@@ -228,6 +235,7 @@ class Kv4Cache(_Description):
         if page_table.dim() != 2:
             raise GhdError(1, "kv4: page_table is not [n_seqs][max_pages]")
         n_seqs, max_pages = page_table.shape
+        _int32(page_rows=page_rows, n_kv_heads=n_kv_heads, n_pages=n_pages)
         table, dev = _need(page_table, torch.int32, "page_table", 0), page_table.get_device()
         c = _Kv4(n_seqs, n_pages, page_rows, max_pages, n_kv_heads, table, _need(kv_len, torch.int32, "kv_len", n_seqs, dev))
         self.__dict__.update(page_table=page_table, kv_len=kv_len, dev=dev, n_seqs=n_seqs, n_kv_heads=n_kv_heads, n_rows=n_pages * n_kv_heads * page_rows,
@@ -240,6 +248,7 @@ class Kv4Rows(_Description):
 
     def __init__(self, row_start, n_rows: int, pos=None, mask=None):
         n_rows = int(n_rows)
+        _int32(n_rows=n_rows)
         start, dev = _need(row_start, torch.int32, "row_start", 2), row_start.get_device()
         words = 0 if mask is None else int(mask.shape[-1])
         c = _Kv4Rows(n_rows, words, start, None if pos is None else _need(pos, torch.int32, "pos", n_rows, dev),

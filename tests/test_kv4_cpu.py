@@ -303,3 +303,16 @@ def test_descriptions_keep_the_tensors_they_point_to(host_binding):
     kv.kv_len[1] = 7                                            # contents are the caller's
     assert kv.c.kv_len == kv.kv_len.data_ptr() and kv.c.page_table == kv.page_table.data_ptr()
     assert (rows.c.row_start, rows.c.pos, rows.c.mask) == (rows.row_start.data_ptr(), rows.pos.data_ptr(), rows.mask.data_ptr())
+
+
+def test_numbers_beyond_the_struct_are_refused(host_binding):
+    """Cut off to 32 bits they would be others: 8 - 2^32 pages are 8 for the kernels and none for the check of the pool's size."""
+    import torch
+    table, lens, start = torch.zeros((2, 4), dtype=torch.int32), torch.zeros(2, dtype=torch.int32), torch.zeros(3, dtype=torch.int32)
+    for args in ((16, 2, 8 - 2**32), (16, 2 - 2**32, 8), (16 - 2**32, 2, 8), (16, 2, 2**31), (2**32 + 16, 2, 8)):
+        with pytest.raises(host_binding.GhdError, match="32 bits"):
+            host_binding.Kv4Cache(table, lens, *args)
+    for n in (2**32 + 4, 2**31, -2**31 - 1):
+        with pytest.raises(host_binding.GhdError, match="32 bits"):
+            host_binding.Kv4Rows(start, n)
+    assert host_binding.Kv4Cache(table, lens, 16, 2, 8).c.n_pages == 8 and host_binding.Kv4Rows(start, -1).c.n_rows == -1      # (the calls refuse that)
