@@ -228,8 +228,8 @@ class _Description:
 
 class Kv4Cache(_Description):
     """Paging of a 4-bit cache: page_table int32 [n_seqs][max_pages], kv_len int32 [n_seqs] (device tensors; the pools of
-    the layers come with each call).  The tensors are read when a kernel runs and have to stay alive until then; their contents may
-    change, the description may not."""
+    the layers come with each call).  The kernels run on the context's stream, whichever is the current one: tensors have to be
+    ready there, and to stay alive until the kernels have run.  Their contents may change, the description may not."""
 
     def __init__(self, page_table, kv_len, page_rows: int, n_kv_heads: int, n_pages: int):
         if page_table.dim() != 2:
@@ -298,6 +298,7 @@ class Ctx:
         with torch.cuda.device(self.device):
             self.dev = torch.cuda.current_device()
             self.stream = torch.cuda.current_stream(self.device)
+            self.raw_stream = self.stream.cuda_stream
             st = self.lib.ghd_create(C.byref(cfg.c), C.c_void_p(self.stream.cuda_stream), C.byref(self.handle))
             if st != 0:
                 raise GhdError(st, "ghd_create")
@@ -452,13 +453,24 @@ def ghd_tree_fill_tokens(ctx: Ctx, cand, result, level, rank, tokens=None):
     return tokens
 
 
+def _kv4_made(ctx: Ctx, make, *args, **kw):
+    """A tensor that a call makes for its result: on the context's stream, where the kernels write it.  Made on another current
+    stream, its fill (or what still runs there on the memory that it gets) could come after the kernels."""
+    if torch._C._cuda_getCurrentRawStream(ctx.dev) == ctx.raw_stream:
+        return make(*args, **kw)
+    with torch.cuda.stream(ctx.stream):
+        t = make(*args, **kw)
+    t.record_stream(torch.cuda.current_stream(ctx.device))          # where the caller is going to use it
+    return t
+
+
 def ghd_kv4_pool_bytes(ctx: Ctx, kv: Kv4Cache) -> int:
     return int(ctx.lib.ghd_kv4_pool_bytes(ctx.handle, C.byref(kv.c)))
 
 
 def ghd_kv4_pool(ctx: Ctx, kv: Kv4Cache, n_layers: int = 1):
     """A zeroed pool per layer, uint8 [n_layers][bytes]."""
-    return torch.zeros((n_layers, ghd_kv4_pool_bytes(ctx, kv)), dtype=torch.uint8, device=ctx.device)
+    return _kv4_made(ctx, torch.zeros, (n_layers, ghd_kv4_pool_bytes(ctx, kv)), dtype=torch.uint8, device=ctx.device)
 
 
 def _kv4_match(ctx: Ctx, kv: Kv4Cache, rows: Kv4Rows):
@@ -498,7 +510,7 @@ def ghd_kv4_append(ctx: Ctx, kv: Kv4Cache, rows: Kv4Rows, pool, q, k, v, q_out=N
         width = ctx.n_heads * ctx.d_head
         qp, qld = _kv4_strided(ctx, q, n, width, "q")
         if q_out is None:
-            q_out = ctx.blank.new_empty((n, width))
+            q_out = _kv4_made(ctx, ctx.blank.new_empty, (n, width))
         op = _need(q_out, ctx.dtype, "q_out", n * width, ctx.dev)
     ctx._check(ctx.lib.ghd_kv4_append(ctx.handle, kv.ref, rows.ref, at, qp, qld, kp, vp, kld, op))
     return q_out
@@ -510,7 +522,7 @@ def ghd_kv4_attention(ctx: Ctx, kv: Kv4Cache, rows: Kv4Rows, pool, q, out=None):
     _kv4_match(ctx, kv, rows)
     at = _kv4_pool(ctx, kv, pool)
     qp = _need(q, ctx.dtype, "q", numel, ctx.dev)
-    out = torch.zeros_like(q) if out is None else out
+    out = _kv4_made(ctx, torch.zeros_like, q) if out is None else out
     ctx._check(ctx.lib.ghd_kv4_attention(ctx.handle, kv.ref, rows.ref, at, qp, _need(out, ctx.dtype, "out", numel, ctx.dev)))
     return out
 
@@ -524,12 +536,12 @@ def ghd_kv4_read(ctx: Ctx, kv: Kv4Cache, pool, row_start, n_rows: int, first=Non
     if rows.n_rows < 0:
         raise GhdError(1, "kv4_read: negative n_rows")
     if k_out is None:
-        k_out = ctx.blank.new_empty(shape)
+        k_out = _kv4_made(ctx, ctx.blank.new_empty, shape)
         kp = k_out.data_ptr()
     else:
         kp = _need(k_out, ctx.dtype, "k_out", shape[0] * shape[1], ctx.dev)
     if v_out is None:
-        v_out = torch.empty_like(k_out) if k_out.shape == shape else ctx.blank.new_empty(shape)
+        v_out = _kv4_made(ctx, torch.empty_like, k_out) if k_out.shape == shape else _kv4_made(ctx, ctx.blank.new_empty, shape)
         vp = v_out.data_ptr()
     else:
         vp = _need(v_out, ctx.dtype, "v_out", shape[0] * shape[1], ctx.dev)

@@ -946,3 +946,46 @@ def test_append_of_one_row_takes_any_row_stride(ghd, dtype):
     ghd.ghd_sync_status(su.ctx)
     assert got.data_ptr() == qi.data_ptr() and bool((qi == want_q).all()) and bool((su.dpool == want_pool).all())
     assert not wide[:, :256].any() and bool((wide[:, 512:640] == v).all()) and not wide[:, 640:].any()
+
+
+@pytest.mark.parametrize("dtype", ["f16", "f32"])
+def test_outputs_made_under_another_current_stream_are_the_kernels(ghd, dtype):
+    """The context's kernels run on its own stream.  A call under another current stream, busy with a long kernel and then with
+    writes to memory that is free again, gives what it gives under the context's."""
+    import torch
+    H, Hk, d = 4, 2, 64
+    su = Setup(ghd, H, Hk, d, dtype, 16, [40, 7], [5, 3], 64, garbage=False)
+    rows = ghd.Kv4Rows(dev(su.start), su.n)
+    q, k, v = (dev(su.r.randn(su.n, w * d).astype(su.np_t)) for w in (H, Hk, Hk))
+    pool0, other = su.dpool.clone(), torch.cuda.Stream()
+
+    def busy(*shapes):                                          # writes that come late, to memory that the next such tensor gets
+        if torch.cuda.current_stream() == su.ctx.stream:
+            return
+        for t in [torch.empty(s, dtype=q.dtype, device="cuda") for s in shapes]:
+            torch.cuda._sleep(20_000_000)
+            t.fill_(9.0)
+
+    def calls():
+        busy(q.shape)
+        qr = ghd.ghd_kv4_append(su.ctx, su.kv, rows, su.dpool, q, k, v)
+        busy(q.shape)
+        out = ghd.ghd_kv4_attention(su.ctx, su.kv, rows, su.dpool, q)
+        busy(k.shape, k.shape)
+        kb, vb = ghd.ghd_kv4_read(su.ctx, su.kv, su.dpool, rows.row_start, su.n)
+        busy()
+        torch.cuda._sleep(20_000_000)
+        pool = ghd.ghd_kv4_pool(su.ctx, su.kv, 2)
+        ghd.ghd_kv4_append(su.ctx, su.kv, rows, pool[1], None, k, v)
+        return [qr, out, kb, vb, pool]
+
+    want = [x.clone() for x in calls()]
+    torch.cuda.synchronize()
+    assert all(bool(x.any()) for x in want)
+    su.dpool.copy_(pool0)
+    torch.cuda.synchronize()
+    with torch.cuda.stream(other):
+        got = calls()
+    torch.cuda.synchronize()
+    for a, b in zip(got, want):
+        assert a.shape == b.shape and bool((a.view(torch.uint8) == b.view(torch.uint8)).all())
