@@ -297,7 +297,7 @@ ghd_status ghd_tree_fill_tokens(ghd_ctx *ctx, const int32_t *cand_dev, const ghd
  * page_table[s * max_pages + t / R].  Pages may be shared by sequences as long as nobody writes to them.
  * The lengths live on the device: no call reads them on the host, so steps can be recorded into one CUDA graph.
  * A length, row number or page id outside its range is skipped by the kernel that meets it (such keys count as not
- * visible) and recorded in the status word: ghd_sync_status -> GHD_ENOSPACE (rows beyond the page table) or GHD_EINVAL
+ * visible) and recorded: ghd_sync_status -> GHD_ENOSPACE (rows beyond the page table) or GHD_EINVAL
  * (a page id outside [0, n_pages)). */
 typedef struct ghd_kv4 {
     int32_t n_seqs;             /* 1 .. GHD_MAX_SEQS                                             */
@@ -392,7 +392,9 @@ ghd_status ghd_tree_attention_static(void *cuda_stream, int32_t dtype, int32_t n
                                      char *err_buf, size_t err_len);
 
 /* Synchronises the stream and returns GHD_OK, GHD_ECUDA (with the CUDA error kept
- * for ghd_last_error) or GHD_ETIMEOUT when a kernel's bounded wait expired. */
+ * for ghd_last_error), GHD_ETIMEOUT when a kernel's bounded wait expired (what the kernels
+ * left half done in the workspace is cleared), or else what they found wrong with lengths,
+ * rows or pages on the device (GHD_ENOSPACE, GHD_EINVAL).  Reported once. */
 ghd_status ghd_sync_status(ghd_ctx *ctx);
 const char *ghd_status_str(ghd_status s);
 const char *ghd_last_error(const ghd_ctx *ctx);

@@ -194,7 +194,7 @@ __global__ void __launch_bounds__(WARPS * 32, Narrow<T, D, NT>::BLOCKS) k_attn_k
                 pbase = lch;
                 pages = lch + (lane >> 1) < lend && key < lkeys ? __ldg(w.table + (size_t)lseq * w.max_pages + (key >> w.shift)) : -1;
                 if ((unsigned)pages >= (unsigned)w.n_pages) {
-                    if (lch + (lane >> 1) < lend && key < lkeys) atomicCAS(w.status, DEV_OK, DEV_KV4_PAGE);
+                    if (lch + (lane >> 1) < lend && key < lkeys) atomicCAS(w.input_status, DEV_OK, DEV_KV4_PAGE);
                     pages = -1;                                                      // such keys are not visible
                 }
             }

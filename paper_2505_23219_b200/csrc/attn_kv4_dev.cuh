@@ -90,7 +90,7 @@ __device__ __forceinline__ int64_t unit_sums(const Kv4View& w, const Kv4Tiling& 
 #pragma unroll 1
     for (int s = s0; s < s0 + each && s < w.n_seqs; ++s) {
         const Kv4Seq q = kv4_load_seq(w, s);
-        if (q.bad) atomicCAS(w.status, DEV_OK, DEV_KV4_ROWS);
+        if (q.bad) atomicCAS(w.input_status, DEV_OK, DEV_KV4_ROWS);
         const int64_t u = (int64_t)t.heads * kv4_head_units(t, q);
         sums[s] = u;
         mine += u;

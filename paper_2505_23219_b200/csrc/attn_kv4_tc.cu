@@ -297,7 +297,7 @@ __global__ void __launch_bounds__(THREADS, 1) k_attn_kv4_tc(const __grid_constan
 #pragma unroll
                 for (int h = 0; h < 2; ++h) {
                     if ((unsigned)page[h] < (unsigned)w.n_pages) there |= 1u << h;
-                    else if (key0 + 16 * h < lkeys) atomicCAS(w.status, DEV_OK, DEV_KV4_PAGE);
+                    else if (key0 + 16 * h < lkeys) atomicCAS(w.input_status, DEV_OK, DEV_KV4_PAGE);
                 }
                 if (which == 0) sm->groups[n & (GROUP_SLOTS - 1)][quad] = (uint8_t)there;
                 if (there) mbar_expect_tx(full, (there == 3u ? 2u : 1u) * 16 * (ROW + (which ? 0 : 8)));

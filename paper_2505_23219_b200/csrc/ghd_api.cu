@@ -25,6 +25,7 @@ size_t carve_workspace(ghd_ctx* c, char* base) {
     const size_t raw_cols = (3 * d > 2 * f) ? 3 * d : 2 * f;
     c->status = (int*)take(256);
     c->kv_len_word = c->status ? c->status + 16 : nullptr;       // same 256-byte block, its own 64-byte line
+    c->input_status = c->status ? c->status + 32 : nullptr;      // likewise
     c->counters = (int*)take(sizeof(int) * 4096);
     for (int b = 0; b < 2; ++b) c->ssq[b] = (float*)take(sizeof(float) * SSQ_MAX_TILES * SSQ_PITCH);
     c->xres = (float*)take(N * d * 4);
@@ -594,26 +595,22 @@ ghd_status ghd_sync_status(ghd_ctx* c) {
     if (!c) return GHD_EINVAL;
     if (cudaStreamSynchronize(c->stream) != cudaSuccess) return check_cuda(c, "stream synchronize");
     if (!c->ws) return GHD_OK;
-    int st = 0;
-    if (cudaMemcpy(&st, c->status, sizeof(int), cudaMemcpyDeviceToHost) != cudaSuccess) return check_cuda(c, "status read");
-    if (st == DEV_KV_RANGE) {
-        snprintf(c->err, sizeof(c->err), "the cache length on the device left [0, max_kv_len - n]");
-        cudaMemset(c->status, 0, sizeof(int));
-        return GHD_ENOSPACE;
-    }
-    if (st == DEV_KV4_ROWS || st == DEV_KV4_PAGE) {
-        snprintf(c->err, sizeof(c->err), st == DEV_KV4_ROWS ? "paged cache: a row beyond the page table, or a length or row start out of order"
-                                                            : "paged cache: a page id outside the pool");
-        cudaMemset(c->status, 0, sizeof(int));
-        return st == DEV_KV4_ROWS ? GHD_ENOSPACE : GHD_EINVAL;
-    }
-    if (st != DEV_OK) {
+    int words[64];                                             // the block of the status words
+    if (cudaMemcpy(words, c->status, sizeof(words), cudaMemcpyDeviceToHost) != cudaSuccess) return check_cuda(c, "status read");
+    const int st = words[0], in = words[c->input_status - c->status];
+    if (st != DEV_OK) {                                        // (goes before what the inputs did: results are missing, counters may be left over)
         snprintf(c->err, sizeof(c->err), "device wait expired (code %d)", st);
-        int keep = 0;                                          // the cache length survives the clean-up
-        cudaMemcpy(&keep, c->kv_len_word, sizeof(int), cudaMemcpyDeviceToHost);
-        cudaMemset(c->status, 0, 256 + sizeof(int) * 4096);   // status word and tile arrival counters
-        cudaMemcpy(c->kv_len_word, &keep, sizeof(int), cudaMemcpyHostToDevice);
+        cudaMemsetAsync(c->status, 0, sizeof(int), c->stream);                   // (the cache length beside it stays)
+        cudaMemsetAsync(c->input_status, 0, sizeof(int), c->stream);
+        cudaMemsetAsync(c->counters, 0, sizeof(int) * 4096, c->stream);          // tile arrival counters
         return GHD_ETIMEOUT;
+    }
+    if (in != DEV_OK) {
+        snprintf(c->err, sizeof(c->err), in == DEV_KV_RANGE   ? "the cache length on the device left [0, max_kv_len - n]"
+                                         : in == DEV_KV4_ROWS ? "paged cache: a row beyond the page table, or a length or row start out of order"
+                                                              : "paged cache: a page id outside the pool");
+        cudaMemsetAsync(c->input_status, 0, sizeof(int), c->stream);
+        return in == DEV_KV4_PAGE ? GHD_EINVAL : GHD_ENOSPACE;
     }
     return GHD_OK;
 }

@@ -14,8 +14,10 @@
 
 namespace ghd {
 
-// Device status word values (first failure wins).
-enum : int { DEV_OK = 0, DEV_TIMEOUT_TMA = 1, DEV_TIMEOUT_MMA = 2, DEV_TIMEOUT_EPI = 3, DEV_TIMEOUT_TMEM = 4, DEV_TIMEOUT_GRID = 5, DEV_KV_RANGE = 6, DEV_KV4_ROWS = 7, DEV_KV4_PAGE = 8 };
+// Values of the two device status words (in each the first failure wins).  status: a wait that ran out; input_status: device data
+// out of range, which the kernels skip and run on.  Apart, so that neither hides the other.
+enum : int { DEV_OK = 0, DEV_TIMEOUT_TMA = 1, DEV_TIMEOUT_MMA = 2, DEV_TIMEOUT_EPI = 3, DEV_TIMEOUT_TMEM = 4, DEV_TIMEOUT_GRID = 5 };
+enum : int { DEV_KV_RANGE = 6, DEV_KV4_ROWS = 7, DEV_KV4_PAGE = 8 };
 
 // Epilogues of the projection GEMMs.
 enum Epilogue : int {
@@ -103,7 +105,7 @@ struct ghd_ctx {
     int h_ssq;        // which of them describes hbuf (-1: hbuf is already normalised)
     float* logits;    // float [max_nodes][vocab]
     float* mlogits;   // float [8][vocab] logits of the drafting heads
-    int* status;      // device status word
+    int *status, *input_status;      // device status words: waits that ran out, data out of range
     int* kv_len_word; // device word with the cache length (calls given GHD_KV_LEN_DEVICE read it)
     int kv_len_hint;  // what the host last wrote there: sizes launches whose grid depends on the length
     int max_splits;

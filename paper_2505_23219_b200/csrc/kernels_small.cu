@@ -26,7 +26,7 @@ struct CooPtrArg { uint16_t ptr[GHD_MAX_NODES + 1]; };
 constexpr int TREE_NODES_PER_BLOCK = 8;
 
 // Length of the cache for a tree kernel: the host's value, or the device word (clamped into the cache; a word
-// outside [0, max_kv_len - n] is recorded in the status word by the kernel's first thread).
+// outside [0, max_kv_len - n] is recorded in the inputs' status word by the kernel's first thread).
 __device__ __forceinline__ int tree_kv_len(int host, const int* dev, int max_kv_len, int n, int* status, bool reporter) {
     if (dev && reporter) {
         const int raw = __ldcg(dev);
@@ -129,7 +129,7 @@ void launch_tree_build(ghd_ctx* c, const int32_t* parent_host, ghd_tree* t) {
     t->nnz = cp.ptr[t->n];
     k_tree_build<<<(t->n + TREE_NODES_PER_BLOCK - 1) / TREE_NODES_PER_BLOCK, 256, 0, c->cur>>>(pa, cp, t->n, t->n_words, t->kv_len, c->cfg.d_head,
                                                      (double)c->cfg.rope_theta, t->mask, t->parent, t->depth,
-                                                     t->pos, t->rope, t->coo_ptr, t->coo_col, kv_len_dev_of(c, t), c->cfg.max_kv_len, c->status);
+                                                     t->pos, t->rope, t->coo_ptr, t->coo_col, kv_len_dev_of(c, t), c->cfg.max_kv_len, c->input_status);
     c->launches++;
 }
 
@@ -146,7 +146,7 @@ void launch_tree_from_mask(ghd_ctx* c, ghd_tree* t, bool have_depth, const uint6
     k_tree_from_mask<<<1, GHD_MAX_NODES, 0, c->cur>>>(cp, t->n, t->n_words, t->kv_len, c->cfg.d_head,
                                                          (double)c->cfg.rope_theta, have_depth ? 1 : 0, t->mask,
                                                          t->depth, t->pos, t->rope, t->coo_ptr, t->coo_col, kv_len_dev_of(c, t),
-                                                         c->cfg.max_kv_len, c->status);
+                                                         c->cfg.max_kv_len, c->input_status);
     c->launches++;
 }
 

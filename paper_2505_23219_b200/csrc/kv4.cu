@@ -146,7 +146,7 @@ __device__ __forceinline__ void find_owner(const Kv4View& w, int row, bool lengt
     o.end = row + 1;
     if (seq >= 0) {
         o.q = lengths ? kv4_load_seq(w, seq) : kv4_seq(__ldg(w.row_start + seq), __ldg(w.row_start + seq + 1), w.n_rows, 0, 0x7fffffffll);
-        if (o.q.bad && lane == 0) atomicCAS(w.status, DEV_OK, DEV_KV4_ROWS);
+        if (o.q.bad && lane == 0) atomicCAS(w.input_status, DEV_OK, DEV_KV4_ROWS);
         if (row < o.q.row0 || row >= o.q.row0 + o.q.n) o.seq = -1;      // starts out of order
         else o.end = o.q.row0 + o.q.n;
     }
@@ -331,7 +331,7 @@ __global__ void __launch_bounds__(ROW_WARPS * 32) k_kv4_read(const __grid_consta
         if (o.seq < 0) continue;
         const int64_t slot = (int64_t)(first ? __ldg(first + o.seq) : o.q.len) + (row - o.q.row0);
         if (slot < 0 || slot >= kv4_capacity(w)) {
-            if (lane == 0) atomicCAS(w.status, DEV_OK, DEV_KV4_ROWS);
+            if (lane == 0) atomicCAS(w.input_status, DEV_OK, DEV_KV4_ROWS);
             continue;
         }
         const int page = kv4_page(w, o.seq, (int)slot);
@@ -398,7 +398,7 @@ __global__ void __launch_bounds__(32) k_kv4_commit(const __grid_constant__ Kv4Vi
         for (int k = 0; k < COMMIT_ROWS; ++k) {
             const int j = j0 + k;
             const bool moves = src[k] > j && src[k] < sq.n_new;
-            if (src[k] != j && !moves) atomicCAS(w.status, DEV_OK, DEV_KV4_ROWS);
+            if (src[k] != j && !moves) atomicCAS(w.input_status, DEV_OK, DEV_KV4_ROWS);
             pf[k] = moves ? kv4_page(w, s, sq.len + src[k]) : -1;
             pt[k] = moves ? kv4_page(w, s, sq.len + j) : -1;
         }
@@ -427,14 +427,14 @@ __global__ void k_kv4_advance(Kv4View w, int32_t* kv_len, const ghd_accept_resul
     const int s = blockIdx.x * blockDim.x + threadIdx.x;
     if (s >= w.n_seqs) return;
     const Kv4Seq sq = kv4_seq(w.row_start[s], w.row_start[s + 1], w.n_rows, kv_len[s], kv4_capacity(w));
-    if (sq.bad) atomicCAS(w.status, DEV_OK, DEV_KV4_ROWS);
+    if (sq.bad) atomicCAS(w.input_status, DEV_OK, DEV_KV4_ROWS);
     if (sq.n <= 0) return;
     int add = sq.n_new;
     if (results) {
         int m = results[s].n_matched;
         if (m < 0) m = 0;
         if (m > GHD_MAX_NODES - 1) m = GHD_MAX_NODES - 1;
-        if (m + 1 > sq.n_new) atomicCAS(w.status, DEV_OK, DEV_KV4_ROWS);
+        if (m + 1 > sq.n_new) atomicCAS(w.input_status, DEV_OK, DEV_KV4_ROWS);
         else add = m + 1;
     }
     kv_len[s] = sq.len + add;
@@ -493,7 +493,7 @@ Kv4View kv4_view(const ghd_ctx* c, const ghd_kv4* kv, const ghd_kv4_rows* rows) 
     w.shift = kv->page_rows == 16 ? 4 : kv->page_rows == 32 ? 5 : kv->page_rows == 64 ? 6 : 7;
     w.heads = kv->n_kv_heads; w.d_head = c->cfg.d_head;
     w.block = kv4_block_bytes(kv->page_rows, c->cfg.d_head, c->cfg.dtype == GHD_F32 ? 4 : 2);
-    w.status = c->status;
+    w.status = c->status; w.input_status = c->input_status;
     return w;
 }
 

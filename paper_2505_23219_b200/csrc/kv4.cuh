@@ -12,7 +12,7 @@ struct Kv4View {
     const int32_t* row_start;
     int n_seqs, n_pages, shift, max_pages, n_rows, heads, d_head;      // page_rows = 1 << shift; heads of K and V
     uint32_t block;                                                    // bytes of one head's rows of a page
-    int* status;
+    int *status, *input_status;                                        // waits that ran out; lengths, rows and pages out of range
 };
 
 #ifdef __CUDACC__
@@ -24,7 +24,7 @@ __device__ __forceinline__ Kv4Seq kv4_load_seq(const Kv4View& w, int s) {
 __device__ __forceinline__ int kv4_page(const Kv4View& w, int seq, int row) {
     const int p = __ldg(w.table + (size_t)seq * w.max_pages + (row >> w.shift));
     if ((unsigned)p < (unsigned)w.n_pages) return p;
-    atomicCAS(w.status, DEV_OK, DEV_KV4_PAGE);
+    atomicCAS(w.input_status, DEV_OK, DEV_KV4_PAGE);
     return -1;
 }
 __device__ __forceinline__ size_t kv4_block_at(const Kv4View& w, int page, int head) { return ((size_t)page * w.heads + head) * w.block; }

@@ -989,3 +989,31 @@ def test_outputs_made_under_another_current_stream_are_the_kernels(ghd, dtype):
     torch.cuda.synchronize()
     for a, b in zip(got, want):
         assert a.shape == b.shape and bool((a.view(torch.uint8) == b.view(torch.uint8)).all())
+
+
+def test_a_bad_page_does_not_hide_a_wait_that_ran_out(ghd):
+    """A bad page id is reported, and the kernel runs on.  A wait that runs out after that has to be reported too, and what it left
+    in the workspace (arrival counters) be cleared.  The wait is played by the words that it would have left."""
+    import torch
+    su = Setup(ghd, 2, 2, 64, "f16", 16, [1500], [2], 65, garbage=False)
+    rows = ghd.Kv4Rows(dev(su.start), 2)
+    q = dev(su.r.randn(2, 128).astype(np.float16))
+    good = ghd.ghd_kv4_attention(su.ctx, su.kv, rows, su.dpool, q).clone()
+    ghd.ghd_sync_status(su.ctx)
+    first = int(su.kv.page_table[0, 0])
+    su.kv.page_table[0, 0] = -1
+    ghd.ghd_kv4_attention(su.ctx, su.kv, rows, su.dpool, q)
+    su.kv.page_table[0, 0] = first
+    words = su.ctx.workspace[:256 + 4 * 4096].view(torch.int32)       # status words, then the counters
+    words[:1] = torch.where(words[:1] == 0, 3, words[:1])             # a kernel records it where nothing stands
+    words[64:] = 5
+    with pytest.raises(ghd.GhdError) as e:
+        ghd.ghd_sync_status(su.ctx)
+    assert e.value.name == "GHD_ETIMEOUT"
+    ghd.ghd_sync_status(su.ctx)                                       # reported once
+    assert not words.any()
+    assert bool((ghd.ghd_kv4_attention(su.ctx, su.kv, rows, su.dpool, q) == good).all())
+    su.kv.page_table[0, 0] = -1
+    ghd.ghd_kv4_attention(su.ctx, su.kv, rows, su.dpool, q)
+    with pytest.raises(ghd.GhdError, match="page id"):
+        ghd.ghd_sync_status(su.ctx)
