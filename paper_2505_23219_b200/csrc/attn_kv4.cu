@@ -9,8 +9,12 @@
 // Keys are the M side of both products: S^T [16 keys x 8 rows] = K Q^T and O^T [16 channels x 8 rows] = V^T P^T
 // (mma.sync m16n8k16), so one to eight rows cost one n-tile.  The lanes' channels are permuted so that a lane's codes are
 // consecutive bytes of a row; nibbles become operands in registers.  A warp takes 32 keys of every chunk of 128 and keeps
-// its own running reference (raised when a score exceeds it by 2^2: p * scale then fits half for every scale) and sums;
-// the warps meet in shared memory.
+// its own running reference (raised when a score exceeds it by 2^2) and sums; the warps meet in shared memory.
+//
+// Half range: p * scale is the operand of the second product, rounded to half's 11 bits.  V's scales are multiplied by a power of
+// two, lowered when a visible key's scale passes 2^13 of it and then chosen so that the largest lies in [2^10, 2^11): p <= 2^2 keeps the
+// operand below 2^15, and weights down to 2^-24 of the reference's keep all bits at the largest scale.  (Without the power,
+// p * scale of small values and of keys far below the top fell below half's normal range.)
 //
 // Work is dealt by device-side lengths: all chunks of all (sequence, head, row tile) items are numbered and each CTA takes
 // an equal run of them (kv4_layout.h), so ragged batches and single long sequences fill the device alike.  An item cut by
@@ -34,6 +38,8 @@ namespace {
 
 constexpr int WARPS = 4, WKEYS = 32, CHUNK = WKEYS * WARPS;      // a warp takes 32 keys of every chunk
 constexpr float RAISE = 2.f;
+constexpr float VS_TOP = 0x1p13f;      // largest of V's scales times their power of two
+constexpr int VS_EXP = 10;             // exponent of the largest one where the power is chosen
 constexpr int LEAD = 4;          // an item's fixed cost in chunks (one token of 32 heads over 2048 and 16384 rows: 2: 11.6 and 28.4 us, 3: 11.2 and 27.3, 4: 11.3 and 27.0)
 
 using namespace kv4;
@@ -132,6 +138,7 @@ template <typename T, int D, int NT>
 __global__ void __launch_bounds__(WARPS * 32, Narrow<T, D, NT>::BLOCKS) k_attn_kv4(const __grid_constant__ Kv4AttnParams p) {
     using N = Narrow<T, D, NT>;
     using O_ = Op<T>;
+    constexpr bool HALF = sizeof(T) == 2;
     constexpr int RT = N::RT, KW = N::KW, VW = N::VW, KS = N::KS, MT = N::MT, TERMS = O_::TERMS, XO = N::XO, es = N::ES;
     extern __shared__ __align__(16) uint8_t smem[];
     __shared__ int64_t scratch[32];
@@ -267,6 +274,7 @@ __global__ void __launch_bounds__(WARPS * 32, Narrow<T, D, NT>::BLOCKS) k_attn_k
         float o[MT][NT][4];
         float base[NT][2], l[NT][2], ms[NT][2];
         uint32_t none = (1u << 2 * NT) - 1u;
+        float vmul = HALF ? 0x1p34f : 1.f;                              // power of two of V's scales (half's smallest, 2^-24, has VS_EXP so)
 #pragma unroll
         for (int nt = 0; nt < NT; ++nt) {
 #pragma unroll
@@ -338,8 +346,15 @@ __global__ void __launch_bounds__(WARPS * 32, Narrow<T, D, NT>::BLOCKS) k_attn_k
                             top = fmaxf(top, v);
                         }
                 }
+            float vs[2][2];                                             // V's scales of keys (z, h)
+#pragma unroll
+            for (int z = 0; z < 2; ++z)
+#pragma unroll
+                for (int h = 0; h < 2; ++h) vs[z][h] = param_of<T>(st + N::VP_AT, 16 * z + ka + 8 * h).x;
             bool over = none != 0u || top > RAISE;                      // (a row's first keys may have had no page)
+            if (HALF) over = over || fmaxf(fmaxf(vs[0][0], vs[0][1]), fmaxf(vs[1][0], vs[1][1])) * vmul > VS_TOP;
             uint32_t vis = 0xffffffffu;                                 // bit 8 nt + 4 z + e: score s[z][nt][e] counts
+            auto seen = [&](int z, int h) { return (vis & (NT == 2 ? 0x303u : 3u) << (4 * z + 2 * h)) != 0u; };      // key (z, h), by a row of this lane
             if (__builtin_expect(!all, 0)) {
                 // a lane looks up the warp's 32 keys for one of the tile's rows; the others get the word by shuffle
                 uint32_t word = sees(p, it.q, (it.tile * RT + min(lane, RT - 1)) / p.group, key0 - it.q.len);
@@ -361,8 +376,28 @@ __global__ void __launch_bounds__(WARPS * 32, Narrow<T, D, NT>::BLOCKS) k_attn_k
                                 over = over || v > ((none >> (2 * nt + e)) & 1u ? -INFINITY : RAISE);
                             }
                     }
+                if (HALF)                                               // what nobody sees, and what lies behind the rows, has no say in the power
+#pragma unroll
+                    for (int z = 0; z < 2; ++z)
+#pragma unroll
+                        for (int h = 0; h < 2; ++h) over = over || (seen(z, h) && vs[z][h] * vmul > VS_TOP);
             }
             if (__any_sync(0xffffffffu, over)) {
+                float fv = 1.f;
+                if (HALF) {
+                    float vx = 0.f;
+#pragma unroll
+                    for (int z = 0; z < 2; ++z)
+#pragma unroll
+                        for (int h = 0; h < 2; ++h) if (seen(z, h) && vs[z][h] <= 65504.f) vx = fmaxf(vx, vs[z][h]);
+#pragma unroll
+                    for (int x = 1; x < 32; x <<= 1) vx = fmaxf(vx, __shfl_xor_sync(0xffffffffu, vx, x));
+                    if (vx * vmul >= (float)(2 << VS_EXP)) {
+                        const float vnew = __uint_as_float((uint32_t)(254 + VS_EXP - (int)(__float_as_uint(vx) >> 23)) << 23);
+                        fv = vnew / vmul;
+                        vmul = vnew;
+                    }
+                }
 #pragma unroll
                 for (int nt = 0; nt < NT; ++nt)
 #pragma unroll
@@ -372,17 +407,19 @@ __global__ void __launch_bounds__(WARPS * 32, Narrow<T, D, NT>::BLOCKS) k_attn_k
                         up = fmaxf(up, __shfl_xor_sync(0xffffffffu, up, 8));
                         up = fmaxf(up, __shfl_xor_sync(0xffffffffu, up, 16));
                         const bool had = !((none >> (2 * nt + e)) & 1u);
+                        float f = 1.f;
                         if (up > (had ? 0.f : -INFINITY)) {             // the new reference is `up` above the base
-                            const float f = had ? ex2(-up) : 0.f;
+                            f = had ? ex2(-up) : 0.f;
                             none &= ~(1u << (2 * nt + e));
                             base[nt][e] += up;
                             l[nt][e] *= f;
                             ms[nt][e] *= f;
 #pragma unroll
                             for (int z = 0; z < 2; ++z) { s[z][nt][e] -= up; s[z][nt][e + 2] -= up; }
-#pragma unroll
-                            for (int mt = 0; mt < MT; ++mt) { o[mt][nt][e] *= f; o[mt][nt][e + 2] *= f; }
                         }
+                        f *= fv;
+#pragma unroll
+                        for (int mt = 0; mt < MT; ++mt) { o[mt][nt][e] *= f; o[mt][nt][e + 2] *= f; }
                     }
             }
             uint32_t bp[2][NT][TERMS][2];
@@ -391,7 +428,7 @@ __global__ void __launch_bounds__(WARPS * 32, Narrow<T, D, NT>::BLOCKS) k_attn_k
 #pragma unroll
                 for (int z = 0; z < 2; ++z) {
                     const float2 vp0 = param_of<T>(st + N::VP_AT, 16 * z + ka), vp1 = param_of<T>(st + N::VP_AT, 16 * z + ka + 8);
-                    const float vm0 = fmaf(8.f, vp0.x, vp0.y), vm1 = fmaf(8.f, vp1.x, vp1.y);
+                    const float vm0 = fmaf(8.f, vp0.x, vp0.y), vm1 = fmaf(8.f, vp1.x, vp1.y), vs0 = HALF ? vs[z][0] * vmul : vs[z][0], vs1 = HALF ? vs[z][1] * vmul : vs[z][1];
 #pragma unroll
                     for (int nt = 0; nt < NT; ++nt) {
                         float ps[4];
@@ -399,7 +436,7 @@ __global__ void __launch_bounds__(WARPS * 32, Narrow<T, D, NT>::BLOCKS) k_attn_k
                         for (int e = 0; e < 4; ++e) {
                             const float pe = ex2(s[z][nt][e]);
                             l[nt][e & 1] += pe;
-                            ps[e] = pe * (e < 2 ? vp0.x : vp1.x);
+                            ps[e] = pe * (e < 2 ? vs0 : vs1);
                             if (PLAIN || ((vis >> (8 * nt + 4 * z + e)) & 1u)) ms[nt][e & 1] = fmaf(pe, e < 2 ? vm0 : vm1, ms[nt][e & 1]);
                             else ps[e] = 0.f;                           // by selection: what a key holds stays out of rows that do not see it
                         }
@@ -448,6 +485,7 @@ __global__ void __launch_bounds__(WARPS * 32, Narrow<T, D, NT>::BLOCKS) k_attn_k
         }
 
         // ---- the warps' sums meet
+        const float vinv = 1.f / vmul;
 #pragma unroll
         for (int nt = 0; nt < NT; ++nt)
 #pragma unroll
@@ -460,7 +498,7 @@ __global__ void __launch_bounds__(WARPS * 32, Narrow<T, D, NT>::BLOCKS) k_attn_k
                 if (g == 0) { xm[warp * RT + rl] = (none >> (2 * nt + e)) & 1u ? -INFINITY : base[nt][e]; xl[warp * RT + rl] = a; xs[warp * RT + rl] = b; }
 #pragma unroll
                 for (int mt = 0; mt < MT; mt += 2)
-                    *reinterpret_cast<float4*>(xo + (warp * RT + rl) * XO + g * (D / 8) + 2 * mt) = make_float4(o[mt][nt][e], o[mt][nt][e + 2], o[mt + 1][nt][e], o[mt + 1][nt][e + 2]);
+                    *reinterpret_cast<float4*>(xo + (warp * RT + rl) * XO + g * (D / 8) + 2 * mt) = make_float4(o[mt][nt][e] * vinv, o[mt][nt][e + 2] * vinv, o[mt + 1][nt][e] * vinv, o[mt + 1][nt][e + 2] * vinv);
             }
         __syncthreads();
         const int64_t c0 = kv4_cta_of(it.first, per), c1 = kv4_cta_of(it.first + it.chunks - 1, per);      // CTAs that share the item

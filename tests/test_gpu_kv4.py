@@ -1017,3 +1017,58 @@ def test_a_bad_page_does_not_hide_a_wait_that_ran_out(ghd):
     ghd.ghd_kv4_attention(su.ctx, su.kv, rows, su.dpool, q)
     with pytest.raises(ghd.GhdError, match="page id"):
         ghd.ghd_sync_status(su.ctx)
+
+
+SINKS = [(1, 1, 1), (1, 1, 9), (1, 4, 3), (2, 1, 40), (2, 4, 17)]       # kernel, query heads a key head, new rows
+
+
+@pytest.mark.parametrize("behind", [9.0, 13.0], ids=["9 below", "13 below"])
+@pytest.mark.parametrize("size", [1e-3, 1e-2, 0.1])
+@pytest.mark.parametrize("path,g,n", SINKS)
+@pytest.mark.parametrize("d", [64, 128])
+def test_small_weights_keep_their_bits(ghd, d, path, g, n, size, behind):
+    """One key has nearly all the weight and values of 0; the others, `behind` nats below it, make the output.  Queries have one
+    channel that is not 0, so scores are sums of three exact products.
+
+    Bound of an element, with the weights of the oracle: each weight times scale is rounded to half (2^-11) and its score and exponential
+    are off by 2^-18 at most (scores below 32 in powers of two, in 32 bits: a few times 2^-19 each), times |code - 8|; the middles
+    min + 8 scale are off by 2^-18 likewise; sums of L terms in 32 bits (2^-23 each, tensor cores may truncate), taken relative to the sum
+    of their sizes; output half a step of half, 2^-25 below the normal range.  A weight rounded below half's normal range is off by
+    up to half of itself: far above this bound."""
+    import torch
+    H, Hk, L = g, 1, 2048
+    r = np.random.RandomState(100 * n + d)
+    su = Setup(ghd, H, Hk, d, "f16", 64, [0], [1], 17, spare=0, garbage=False)
+    n_pages = (L + n + 63) // 64
+    pool = okv4.Pool(n_pages, Hk, 64, d, "f16")
+    table = r.permutation(n_pages).astype(np.int32)[None]
+    q = np.zeros((n, H, d), np.float16)
+    q[:, :, 0] = 8.0
+    top = int(r.randint(0, L))
+    scale = 1.0 if d == 64 else 1.5
+    step = 8.0 * scale / np.sqrt(d)                            # nats of one code of channel 0
+    score = 15 - np.rint((behind + r.rand(L + n) * 1.5) / step)
+    assert 0 <= score.min() and score.max() < 8
+    for t in range(L + n):
+        page, row = okv4.slots(table, 64, 0, t)
+        c = r.randint(0, 16, d)
+        c[0] = 15 if t == top else int(score[t])
+        pool.put(0, page, row, 0, c.astype(np.uint8), scale, -2.0)
+        pool.put(1, page, row, 0, *okv4.quantise((r.randn(d) * size * (t != top)).astype(np.float32), "f16"))
+    on_path(ghd, su.ctx, path)
+    kv = ghd.Kv4Cache(dev(table), dev(np.array([L], np.int32)), 64, Hk, n_pages)
+    out = ghd.ghd_kv4_attention(su.ctx, kv, ghd.Kv4Rows(dev(np.array([0, n], np.int32)), n), dev(pool.data.reshape(-1)), dev(q.reshape(n, -1)))
+    ghd.ghd_sync_status(su.ctx)
+    got = out.double().cpu().numpy().reshape(n, H, d)
+    K, V = okv4.rows(pool, table, 0, 0, L + n)
+    par = np.array([pool.params(1, *okv4.slots(table, 64, 0, t), 0).astype(np.float64) for t in range(L + n)])
+    code = (V[:, 0] - par[:, 1:]) / np.where(par[:, :1] == 0, 1.0, par[:, :1])
+    for i in range(n):
+        see = np.arange(L + n) <= L + i
+        w = np.exp(K[see, 0, 0] * 8.0 / np.sqrt(d) - (K[see, 0, 0] * 8.0 / np.sqrt(d)).max())
+        w /= w.sum()
+        assert w[top] > 0.5
+        part, middle = par[see, :1] * np.abs(code[see] - 8), np.abs(par[see, 1:] + 8 * par[see, :1])
+        want = w @ V[see, 0]
+        tol = w @ (part * (2.0 ** -11 + 2.0 ** -18 + L * 2.0 ** -23) + middle * (2.0 ** -18 + L * 2.0 ** -23)) + np.maximum(2.0 ** -11 * np.abs(want), 2.0 ** -25)
+        assert (np.abs(got[i] - want) <= tol).all(), (i, float((np.abs(got[i] - want) / tol).max()))
