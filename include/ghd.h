@@ -290,7 +290,7 @@ ghd_status ghd_tree_fill_tokens(ghd_ctx *ctx, const int32_t *cand_dev, const ghd
  *   min = T(lowest x), scale = T((highest - lowest) / 15), code = (x - min) / scale rounded to the nearest (ties to
  *   even) and held in [0, 15], 0 when scale is 0; the code stands for min + scale * code.
  * A row with a NaN or an infinity reads back as NaN throughout, one whose lowest value is below T's range (which the
- * rotation can do to keys) as minus infinity.
+ * rotation can do to keys) as minus infinity; either way a row of attention that sees it gets NaN.
  * A pool (one per layer) is dev bytes [n_pages][n_kv_heads][block], 16-byte aligned; with R = page_rows a block is
  *   K codes [R][d_head / 2] | V codes [R][d_head / 2] | K {scale, min} T [R][2] | V {scale, min} T [R][2],
  * channel 2b in the low half of byte b, channel 2b + 1 in the high half.  Row t of sequence s is row t mod R of page

@@ -336,7 +336,9 @@ __global__ void __launch_bounds__(WARPS * 32, Narrow<T, D, NT>::BLOCKS) k_attn_k
 #pragma unroll
                 for (int h = 0; h < 2; ++h) {
                     const float2 kp = param_of<T>(st + N::P_AT, 16 * z + ka + 8 * h);
-                    const float ks = kp.x * sl2, km = fmaf(8.f, kp.x, kp.y) * sl2;
+                    // km - km: 0, or NaN for a minimum that the rotation took to -inf (the key reads as -inf throughout, and a product of
+                    // that with a query is no number; -inf times the queries' sum would drop the key, or not, by the sum's sign)
+                    const float km = fmaf(8.f, kp.x, kp.y) * sl2, ks = fmaf(kp.x, sl2, HALF ? km - km : 0.f);
 #pragma unroll
                     for (int nt = 0; nt < NT; ++nt)
 #pragma unroll

@@ -346,7 +346,8 @@ __global__ void __launch_bounds__(THREADS, 1) k_attn_kv4_tc(const __grid_constan
                 asm volatile("ld.shared.u32 %0, [%1];" : "=r"(kr) : "r"(at) : "memory");
                 asm volatile("ld.shared.u32 %0, [%1];" : "=r"(vr) : "r"(at + 4 * UNIT) : "memory");
                 const float2 kf = __half22float2(*reinterpret_cast<const __half2*>(&kr)), vf = __half22float2(*reinterpret_cast<const __half2*>(&vr));
-                sm->par[i & (PAR_SLOTS - 1)][quad * 32 + lane] = make_float4(kf.x * sl2, fmaf(8.f, kf.x, kf.y) * sl2, vf.x, fmaf(8.f, vf.x, vf.y));
+                const float km = fmaf(8.f, kf.x, kf.y) * sl2;             // (km - km: NaN for a key of -inf, as in attn_kv4.cu)
+                sm->par[i & (PAR_SLOTS - 1)][quad * 32 + lane] = make_float4(fmaf(kf.x, sl2, km - km), km, vf.x, fmaf(8.f, vf.x, vf.y));
             }
             tc_fence_after();
             uint32_t to = which == 0 ? tmem + SH::T_K + b * ROW + ((uint32_t)(quad * 32) << 16) : vt0 + b * SH::V_BYTES;

@@ -1072,3 +1072,39 @@ def test_small_weights_keep_their_bits(ghd, d, path, g, n, size, behind):
         want = w @ V[see, 0]
         tol = w @ (part * (2.0 ** -11 + 2.0 ** -18 + L * 2.0 ** -23) + middle * (2.0 ** -18 + L * 2.0 ** -23)) + np.maximum(2.0 ** -11 * np.abs(want), 2.0 ** -25)
         assert (np.abs(got[i] - want) <= tol).all(), (i, float((np.abs(got[i] - want) / tol).max()))
+
+
+@pytest.mark.parametrize("dtype,d,path,g,n", [("f16", 128, 1, 2, 3), ("f16", 64, 1, 1, 12), ("f16", 128, 2, 1, 40), ("f16", 64, 2, 2, 20)])
+def test_rows_that_see_a_key_of_minus_infinity_get_nan(ghd, dtype, d, path, g, n):
+    """The rotation takes cache row 70 and, in another sequence, new row 1 below half's range: they read back as -inf, whose product
+    with a query is no number, whatever the sign of the query's sum.  Rows that do not see them are what they are without them."""
+    Hk, R = 2, 32
+    H = g * Hk
+    su = Setup(ghd, H, Hk, d, dtype, R, [90, 50], [n, n], 19, garbage=False)
+    on_path(ghd, su.ctx, path)
+    for s, t in ((0, 70), (1, 51)):
+        page, row = okv4.slots(su.table, R, s, t)
+        for h in range(Hk):
+            su.pool.put(0, page, row, h, su.pool.codes(0, page, row, h), 7000.0, -np.inf)
+    su.dpool.copy_(dev(su.pool.data.reshape(-1)))
+    vis = [np.ones((n, n), bool), np.ones((n, n), bool)]
+    vis[1][2:, 1] = np.arange(2, n) % 2 == 0                           # some rows behind new row 1 do not see it
+    mask = np.zeros((2 * n, 64), np.uint8)
+    mask[:n, :n], mask[n:, :n] = vis[0], vis[1]
+    words = np.packbits(mask, axis=1, bitorder="little").view(np.int64)
+    q = su.r.randn(2 * n, H, d).astype(su.np_t)
+    q[::2] += np.float16(0.5)                                           # sums of both signs, channels of both signs in every row
+    q[1::2] -= np.float16(0.5)
+    assert (q.min(-1) < 0).all() and (q.max(-1) > 0).all() and (q.astype(np.float64).sum(-1) > 0).any() and (q.astype(np.float64).sum(-1) < 0).any()
+    out = ghd.ghd_kv4_attention(su.ctx, su.kv, ghd.Kv4Rows(dev(su.start), 2 * n, mask=dev(words)), su.dpool, dev(q.reshape(2 * n, -1)))
+    ghd.ghd_sync_status(su.ctx)
+    got = out.double().cpu().numpy().reshape(2 * n, H, d)
+    with np.errstate(all="ignore"):
+        collect(su)
+        want = okv4.attention(su.pool, su.table, su.lens, su.start, vis, q)
+    bad = np.ones(2 * n, bool)
+    bad[n] = False                                                      # new row 0 comes before it
+    bad[n:] &= np.tril(vis[1])[:, 1]
+    assert np.isnan(want[bad]).all() and np.isfinite(want[~bad]).all() and (n <= 3 or (~bad).sum() > 2)
+    assert np.isnan(got[bad]).all()
+    assert (np.abs(got - want)[~bad] <= attention_tolerance(su, q)(want)[~bad]).all()
