@@ -513,7 +513,7 @@ ghd_status ghd_kv4_append(ghd_ctx* c, const ghd_kv4* kv, const ghd_kv4_rows* row
                           const void* v, int64_t kv_ld, void* q_out) {
     if (!c) return GHD_EINVAL;
     ghd_status st = check_kv4(c, kv, rows);
-    if (st != GHD_OK) return st;
+    if (st != GHD_OK || rows->n_rows == 0) return st;               // (no rows: their buffers may be null)
     const ghd_model_cfg& m = c->cfg;
     const int D = m.d_head;
     if (!pool || !k || !v || (!q != !q_out)) return fail(c, GHD_EINVAL, "kv4_append: null pool, k or v, or only one of q and q_out");
@@ -523,7 +523,6 @@ ghd_status ghd_kv4_append(ghd_ctx* c, const ghd_kv4* kv, const ghd_kv4_rows* row
         return fail(c, GHD_EINVAL, "kv4_append: a leading dimension below the row's width, or not a multiple of 8");
     if (!aligned16(pool) || !aligned16(q) || !aligned16(k) || !aligned16(v) || !aligned16(q_out)) return fail(c, GHD_EINVAL, "kv4_append: pointers must be 16-byte aligned");
     if (q == q_out && q && q_ld != (int64_t)m.n_heads * D) return fail(c, GHD_EINVAL, "kv4_append: q_out may be q only when q is contiguous");
-    if (rows->n_rows == 0) return GHD_OK;
     OnDevice dev(c);
     RopeFreq fr;
     memcpy(fr.f, c->rope_freq, sizeof(fr.f));
@@ -546,11 +545,10 @@ ghd_status ghd_kv4_append(ghd_ctx* c, const ghd_kv4* kv, const ghd_kv4_rows* row
 ghd_status ghd_kv4_attention(ghd_ctx* c, const ghd_kv4* kv, const ghd_kv4_rows* rows, const void* pool, const void* q, void* out) {
     if (!c) return GHD_EINVAL;
     ghd_status st = check_kv4(c, kv, rows);
-    if (st != GHD_OK) return st;
+    if (st != GHD_OK || rows->n_rows == 0) return st;               // (no rows: their buffers may be null)
     if (!pool || !q || !out) return fail(c, GHD_EINVAL, "kv4_attention: null pool, q or out");
     if (!aligned16(pool) || !aligned16(q) || !aligned16(out)) return fail(c, GHD_EINVAL, "kv4_attention: pointers must be 16-byte aligned");
     if (q == out) return fail(c, GHD_EINVAL, "kv4_attention: out may not be q");
-    if (rows->n_rows == 0) return GHD_OK;
     OnDevice dev(c);
     c->entry_fresh = c->opt_chain_calls ? 0 : 1;
     st = launch_attn_kv4(c, kv4_view(c, kv, rows), rows, pool, q, out);
@@ -560,11 +558,10 @@ ghd_status ghd_kv4_attention(ghd_ctx* c, const ghd_kv4* kv, const ghd_kv4_rows* 
 ghd_status ghd_kv4_read(ghd_ctx* c, const ghd_kv4* kv, const ghd_kv4_rows* rows, const void* pool, const int32_t* first, void* k_out, void* v_out) {
     if (!c) return GHD_EINVAL;
     ghd_status st = check_kv4(c, kv, rows);
-    if (st != GHD_OK) return st;
+    if (st != GHD_OK || rows->n_rows == 0) return st;               // (no rows: their buffers may be null)
     if (!pool || (!k_out && !v_out)) return fail(c, GHD_EINVAL, "kv4_read: null pool, or neither output");
     if (!aligned16(pool) || !aligned16(k_out) || !aligned16(v_out) || ((uintptr_t)first & 3)) return fail(c, GHD_EINVAL, "kv4_read: pointers must be 16-byte aligned (first: 4)");
     if (k_out == v_out) return fail(c, GHD_EINVAL, "kv4_read: k_out and v_out are the same");
-    if (rows->n_rows == 0) return GHD_OK;
     OnDevice dev(c);
     const Kv4View w = kv4_view(c, kv, rows);
     const int hpw = 32 / (c->cfg.d_head / 8);

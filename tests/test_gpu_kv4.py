@@ -1108,3 +1108,20 @@ def test_rows_that_see_a_key_of_minus_infinity_get_nan(ghd, dtype, d, path, g, n
     assert np.isnan(want[bad]).all() and np.isfinite(want[~bad]).all() and (n <= 3 or (~bad).sum() > 2)
     assert np.isnan(got[bad]).all()
     assert (np.abs(got - want)[~bad] <= attention_tolerance(su, q)(want)[~bad]).all()
+
+
+@pytest.mark.parametrize("dtype", ["f16", "f32"])
+def test_calls_without_rows_take_buffers_without_elements(ghd, dtype):
+    """A step in which no sequence has a new row: tensors of no rows have no memory, and the calls do nothing."""
+    import torch
+    su = Setup(ghd, 4, 2, 64, dtype, 16, [20, 3], [0, 0], 66, garbage=False)
+    e = lambda *s, t=su.ctx.cfg.torch_dtype: torch.empty(s, dtype=t, device="cuda")  # noqa: E731
+    rows = ghd.Kv4Rows(dev(su.start), 0, pos=e(0, t=torch.int32), mask=e(0, 1, t=torch.int64))
+    before, launches = su.dpool.clone(), ghd.ghd_launch_count(su.ctx)
+    assert ghd.ghd_kv4_append(su.ctx, su.kv, rows, su.dpool, e(0, 256), e(0, 128), e(0, 128)).shape == (0, 256)
+    assert ghd.ghd_kv4_append(su.ctx, su.kv, rows, su.dpool, None, e(0, 128), e(0, 128)) is None
+    assert ghd.ghd_kv4_attention(su.ctx, su.kv, rows, su.dpool, e(0, 256)).shape == (0, 256)
+    assert [x.shape for x in ghd.ghd_kv4_read(su.ctx, su.kv, su.dpool, rows.row_start, 0)] == [(0, 128), (0, 128)]
+    ghd.ghd_kv4_commit(su.ctx, su.kv, rows, None)
+    ghd.ghd_sync_status(su.ctx)
+    assert ghd.ghd_launch_count(su.ctx) == launches and bool((su.dpool == before).all()) and su.kv_len.cpu().tolist() == [20, 3]
