@@ -323,7 +323,7 @@ typedef struct ghd_kv4_rows {
     const uint64_t *mask;       /* dev [n_rows][mask_words] or NULL                               */
 } ghd_kv4_rows;
 
-/* Bytes of one pool (0 for a description that the calls refuse). */
+/* Bytes of one pool (0 for sizes that the calls refuse; the pointers are not looked at). */
 size_t ghd_kv4_pool_bytes(const ghd_ctx *ctx, const ghd_kv4 *kv);
 
 /* Appends the new rows (Sec. II-A): rotates q and k by the rows' positions (angles in 64 bits, rotate-half pairing,

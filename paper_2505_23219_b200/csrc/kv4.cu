@@ -468,13 +468,23 @@ struct OnDevice {
 
 bool aligned16(const void* p) { return ((uintptr_t)p & 15) == 0; }
 
+// What is wrong with the sizes of a cache: a status and a reason.
+struct Kv4Fault {
+    ghd_status status;
+    const char* what;
+};
+Kv4Fault size_fault(const ghd_ctx* c, const ghd_kv4* kv) {
+    if (kv->n_seqs < 1 || kv->n_seqs > GHD_MAX_SEQS) return {GHD_EINVAL, "kv4: n_seqs outside [1, GHD_MAX_SEQS]"};
+    if (kv->page_rows != 16 && kv->page_rows != 32 && kv->page_rows != 64 && kv->page_rows != 128) return {GHD_EINVAL, "kv4: page_rows is not 16, 32, 64 or 128"};
+    if (kv->n_pages < 1 || kv->max_pages < 1 || (int64_t)kv->max_pages * kv->page_rows > (1ll << 30)) return {GHD_EINVAL, "kv4: bad page counts"};
+    if (kv->n_kv_heads < 1 || c->cfg.n_heads % kv->n_kv_heads) return {GHD_ESHAPE, "kv4: n_kv_heads does not divide n_heads"};
+    return {GHD_OK, ""};
+}
+
 ghd_status check_kv4(ghd_ctx* c, const ghd_kv4* kv, const ghd_kv4_rows* rows) {
     if (!kv || !rows) return fail(c, GHD_EINVAL, "kv4: null description");
-    if (kv->n_seqs < 1 || kv->n_seqs > GHD_MAX_SEQS) return fail(c, GHD_EINVAL, "kv4: n_seqs outside [1, GHD_MAX_SEQS]");
-    if (kv->page_rows != 16 && kv->page_rows != 32 && kv->page_rows != 64 && kv->page_rows != 128)
-        return fail(c, GHD_EINVAL, "kv4: page_rows is not 16, 32, 64 or 128");
-    if (kv->n_pages < 1 || kv->max_pages < 1 || (int64_t)kv->max_pages * kv->page_rows > (1ll << 30)) return fail(c, GHD_EINVAL, "kv4: bad page counts");
-    if (kv->n_kv_heads < 1 || c->cfg.n_heads % kv->n_kv_heads) return fail(c, GHD_ESHAPE, "kv4: n_kv_heads does not divide n_heads");
+    const Kv4Fault f = size_fault(c, kv);
+    if (f.status != GHD_OK) return fail(c, f.status, f.what);
     if (!kv->page_table || !kv->kv_len || !rows->row_start) return fail(c, GHD_EINVAL, "kv4: null page table, lengths or row starts");
     if ((((uintptr_t)kv->page_table | (uintptr_t)kv->kv_len | (uintptr_t)rows->row_start | (uintptr_t)rows->pos) & 3) || ((uintptr_t)rows->mask & 7))
         return fail(c, GHD_EINVAL, "kv4: a table, length, row start, position or mask that is not aligned to its type");
@@ -504,8 +514,7 @@ using namespace ghd;
 extern "C" {
 
 size_t ghd_kv4_pool_bytes(const ghd_ctx* c, const ghd_kv4* kv) {
-    if (!c || !kv || kv->n_pages < 1 || kv->n_kv_heads < 1 || c->cfg.n_heads % kv->n_kv_heads ||
-        (kv->page_rows != 16 && kv->page_rows != 32 && kv->page_rows != 64 && kv->page_rows != 128)) return 0;
+    if (!c || !kv || size_fault(c, kv).status != GHD_OK) return 0;
     return (size_t)kv->n_pages * kv->n_kv_heads * kv4_block_bytes(kv->page_rows, c->cfg.d_head, c->cfg.dtype == GHD_F32 ? 4 : 2);
 }
 

@@ -1125,3 +1125,14 @@ def test_calls_without_rows_take_buffers_without_elements(ghd, dtype):
     ghd.ghd_kv4_commit(su.ctx, su.kv, rows, None)
     ghd.ghd_sync_status(su.ctx)
     assert ghd.ghd_launch_count(su.ctx) == launches and bool((su.dpool == before).all()) and su.kv_len.cpu().tolist() == [20, 3]
+
+
+def test_a_cache_that_the_calls_refuse_has_no_pool(ghd):
+    import torch
+    su = Setup(ghd, 4, 2, 64, "f16", 16, [4], [2], 67, garbage=False)
+    z = lambda *s: torch.zeros(s, dtype=torch.int32, device="cuda")  # noqa: E731
+    good = ghd.ghd_kv4_pool_bytes(su.ctx, ghd.Kv4Cache(z(1024, 2), z(1024), 128, 2, 3))
+    assert good == 3 * 2 * okv4.block_bytes(128, 64, "f16")
+    for table, args in ((z(1025, 2), (128, 2, 3)), (z(0, 2), (128, 2, 3)), (z(2, 0), (128, 2, 3)), (z(1, (1 << 23) + 1), (128, 2, 3)), (z(2, 2), (24, 2, 3)), (z(2, 2), (128, 3, 3)),
+                        (z(2, 2), (128, 0, 3)), (z(2, 2), (128, 2, 0)), (z(2, 2), (128, 2, -1))):
+        assert ghd.ghd_kv4_pool_bytes(su.ctx, ghd.Kv4Cache(table, z(table.shape[0]), *args)) == 0, (tuple(table.shape), args)
