@@ -527,24 +527,30 @@ def ghd_kv4_attention(ctx: Ctx, kv: Kv4Cache, rows: Kv4Rows, pool, q, out=None):
     return out
 
 
-def ghd_kv4_read(ctx: Ctx, kv: Kv4Cache, pool, row_start, n_rows: int, first=None, k_out=None, v_out=None):
-    """Cache rows first[s] + i (first None: the new rows' places) in the storage type -> (k, v) [n_rows][n_kv_heads * d_head]."""
+def ghd_kv4_read(ctx: Ctx, kv: Kv4Cache, pool, row_start, n_rows: int, first=None, k_out=None, v_out=None, keys: bool = True, values: bool = True):
+    """Cache rows first[s] + i (first None: the new rows' places) in the storage type -> (k, v) [n_rows][n_kv_heads * d_head], None for
+    the one that is not asked for."""
     rows = Kv4Rows(row_start, n_rows)
     _kv4_match(ctx, kv, rows)
     at = _kv4_pool(ctx, kv, pool)
     shape = (rows.n_rows, kv.n_kv_heads * ctx.d_head)
     if rows.n_rows < 0:
         raise GhdError(1, "kv4_read: negative n_rows")
-    if k_out is None:
-        k_out = _kv4_made(ctx, ctx.blank.new_empty, shape)
-        kp = k_out.data_ptr()
-    else:
-        kp = _need(k_out, ctx.dtype, "k_out", shape[0] * shape[1], ctx.dev)
-    if v_out is None:
-        v_out = _kv4_made(ctx, torch.empty_like, k_out) if k_out.shape == shape else _kv4_made(ctx, ctx.blank.new_empty, shape)
-        vp = v_out.data_ptr()
-    else:
-        vp = _need(v_out, ctx.dtype, "v_out", shape[0] * shape[1], ctx.dev)
+    if (k_out is not None and not keys) or (v_out is not None and not values):
+        raise GhdError(1, "kv4_read: an output for what is not asked for")
+    kp = vp = None
+    if keys:
+        if k_out is None:
+            k_out = _kv4_made(ctx, ctx.blank.new_empty, shape)
+            kp = k_out.data_ptr()
+        else:
+            kp = _need(k_out, ctx.dtype, "k_out", shape[0] * shape[1], ctx.dev)
+    if values:
+        if v_out is None:
+            v_out = _kv4_made(ctx, torch.empty_like, k_out) if keys and k_out.shape == shape else _kv4_made(ctx, ctx.blank.new_empty, shape)
+            vp = v_out.data_ptr()
+        else:
+            vp = _need(v_out, ctx.dtype, "v_out", shape[0] * shape[1], ctx.dev)
     st = ctx.lib.ghd_kv4_read(ctx.handle, kv.ref, rows.ref, at, None if first is None else _need(first, torch.int32, "first", kv.n_seqs, ctx.dev), kp, vp)
     if st:
         ctx._check(st)

@@ -1136,3 +1136,21 @@ def test_a_cache_that_the_calls_refuse_has_no_pool(ghd):
     for table, args in ((z(1025, 2), (128, 2, 3)), (z(0, 2), (128, 2, 3)), (z(2, 0), (128, 2, 3)), (z(1, (1 << 23) + 1), (128, 2, 3)), (z(2, 2), (24, 2, 3)), (z(2, 2), (128, 3, 3)),
                         (z(2, 2), (128, 0, 3)), (z(2, 2), (128, 2, 0)), (z(2, 2), (128, 2, -1))):
         assert ghd.ghd_kv4_pool_bytes(su.ctx, ghd.Kv4Cache(table, z(table.shape[0]), *args)) == 0, (tuple(table.shape), args)
+
+
+@pytest.mark.parametrize("dtype,d", [("f16", 128), ("f32", 64)])
+def test_keys_alone_or_values_alone_are_read(ghd, dtype, d):
+    import torch
+    su = Setup(ghd, 2, 2, d, dtype, 16, [40, 0, 9], [1, 1, 1], 68)
+    start, first, n = dev(np.array([0, 5, 5, 12], np.int32)), dev(np.array([30, 0, 2], np.int32)), 12
+    k, v = ghd.ghd_kv4_read(su.ctx, su.kv, su.dpool, start, n, first=first)
+    only_k, no_v = ghd.ghd_kv4_read(su.ctx, su.kv, su.dpool, start, n, first=first, values=False)
+    no_k, only_v = ghd.ghd_kv4_read(su.ctx, su.kv, su.dpool, start, n, first=first, keys=False)
+    ghd.ghd_sync_status(su.ctx)
+    assert no_v is None and no_k is None and bool((only_k == k).all()) and bool((only_v == v).all())
+    out = torch.zeros_like(v)
+    assert ghd.ghd_kv4_read(su.ctx, su.kv, su.dpool, start, n, first=first, v_out=out, keys=False)[1] is out and bool((out == v).all())
+    for kw in (dict(keys=False, values=False), dict(keys=False, k_out=out), dict(values=False, v_out=out)):
+        with pytest.raises(ghd.GhdError) as e:
+            ghd.ghd_kv4_read(su.ctx, su.kv, su.dpool, start, n, first=first, **kw)
+        assert e.value.name == "GHD_EINVAL"
