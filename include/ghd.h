@@ -187,7 +187,9 @@ typedef enum ghd_path {
     GHD_PATH_ATTN_TC = 2,     /* tcgen05 tree attention                               */
     GHD_PATH_ATTN_SIMT = 3,   /* CUDA-core tree attention                             */
     GHD_PATH_ATTN_COO = 4,    /* sparse part gathered from the coordinate index        */
-    GHD_PATH_GEMM_PAIR = 5    /* tcgen05 projection on CTA pairs (counted besides GEMM_TILE) */
+    GHD_PATH_GEMM_PAIR = 5,   /* tcgen05 projection on CTA pairs (counted besides GEMM_TILE) */
+    GHD_PATH_KV4_ROWS = 6,    /* attention over the 4-bit cache, tiles of at most 16 query rows */
+    GHD_PATH_KV4_TC = 7       /* attention over the 4-bit cache, tcgen05                */
 } ghd_path;
 int64_t ghd_path_count(const ghd_ctx *ctx, int32_t path);
 

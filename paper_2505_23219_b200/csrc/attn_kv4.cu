@@ -565,6 +565,7 @@ ghd_status launch_narrow(ghd_ctx* c, Kv4AttnParams& p) {
     p.ctas = c->sm_count * N::BLOCKS;
     const size_t have = (size_t)c->sm_count * 2 * 256 * 128;             // floats of the tile scratch (carve_workspace)
     if ((size_t)p.ctas * 2 * N::SLOT > have || p.ctas > 4096) return fail(c, GHD_ENOSPACE, "kv4_attention: workspace too small");
+    c->path_count[GHD_PATH_KV4_ROWS]++;
     launch_k(c, false, k_attn_kv4<T, D, NT>, dim3(p.ctas), dim3(WARPS * 32), smem, p);
     return GHD_OK;
 }

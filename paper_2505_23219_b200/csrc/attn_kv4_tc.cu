@@ -804,6 +804,7 @@ ghd_status launch_tc(ghd_ctx* c, Kv4AttnParams& p) {
         c->attr_kv4 |= 1u << VARIANT;
     }
     p.ctas = c->sm_count;
+    c->path_count[GHD_PATH_KV4_TC]++;
     launch_k(c, false, k_attn_kv4_tc<D>, dim3(p.ctas), dim3(THREADS), smem_bytes<D>(p.w.n_seqs), p);
     return GHD_OK;
 }

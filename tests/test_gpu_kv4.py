@@ -1154,3 +1154,20 @@ def test_keys_alone_or_values_alone_are_read(ghd, dtype, d):
         with pytest.raises(ghd.GhdError) as e:
             ghd.ghd_kv4_read(su.ctx, su.kv, su.dpool, start, n, first=first, **kw)
         assert e.value.name == "GHD_EINVAL"
+
+
+@pytest.mark.parametrize("dtype", ["f16", "f32"])
+def test_which_kernel_ran_is_counted(ghd, dtype):
+    """Few rows take the kernel of narrow tiles, many in half mode the tcgen05 kernel, and the option picks one of the two."""
+    ctx = make_ctx(ghd, 4, 64, dtype)
+    few, many = (Setup(ghd, 4, 4, 64, dtype, 16, [30], [n], 69, garbage=False) for n in (1, 100))
+    want = [0, 0]
+    for path in (0, 1, 2):
+        for su, tc in ((few, path == 2), (many, path == 2 or (path == 0 and dtype == "f16"))):
+            if path == 2 and dtype == "f32":                    # refused: nothing runs
+                continue
+            on_path(ghd, ctx, path)
+            ghd.ghd_kv4_attention(ctx, su.kv, ghd.Kv4Rows(dev(su.start), su.n), su.dpool, dev(su.r.randn(su.n, 256).astype(su.np_t)))
+            want[tc] += 1
+            assert [ghd.ghd_path_count(ctx, p) for p in (ghd.PATH_KV4_ROWS, ghd.PATH_KV4_TC)] == want
+    ghd.ghd_sync_status(ctx)
