@@ -584,9 +584,13 @@ ghd_status launch_attn_kv4(ghd_ctx* c, const Kv4View& w, const ghd_kv4_rows* row
     const int64_t avg = ((int64_t)rows->n_rows * p.group + w.n_seqs - 1) / w.n_seqs;      // query rows of a sequence and head, on average
     if (m.dtype == GHD_F32) {
         if (c->opt_attn_path == 2) return fail(c, GHD_EUNSUPPORTED, "kv4_attention: the tcgen05 kernel takes GHD_F16 only");
-        // Two tiles of eight rows at a time where there are many (5 sequences over 2048 keys; 28 heads on 4: 2 x 7 rows 15 us in ones, 22 in
-        // twos; 8 x 7: 20 and 24; 16 x 7: 31 and 33; 88 x 7: 130 and 106; 32 heads, 88 rows: 133 and 121).
-        if (avg > 64) return m.d_head == 64 ? launch_narrow<float, 64, 2>(c, p) : launch_narrow<float, 128, 2>(c, p);
+        // Two tiles of eight rows at a time unpack a key half as often and leave half as many items to deal: with more than 128 rows, or
+        // more than 64 and tiles for two SMs of three.  1 and 5 sequences over 512 and 4096 keys, ones / twos in us: 28 heads on 4 of 128,
+        // 112 rows 16 / 18, 26 / 30, 24 / 25, 59 / 53; up to 252 rows 24 / 23, 46 / 41, 36 / 32, 86 / 76; 32 heads, 80 rows 27 / 27, 81 / 72,
+        // 55 / 53, 179 / 154; 8 heads of 64, 48 rows 12 / 13, 17 / 20, 17 / 17, 32 / 29.  Over 280 such calls (9 to 640 rows) 1 % above the
+        // better of the two on average, 44 % at worst (65 rows of 32 heads over 512 keys: 18.5 / 26.7).
+        const int64_t tiles = (avg + 15) / 16 * w.heads * w.n_seqs;
+        if (avg > 128 || (avg > 64 && 3 * tiles > 2 * (int64_t)c->sm_count)) return m.d_head == 64 ? launch_narrow<float, 64, 2>(c, p) : launch_narrow<float, 128, 2>(c, p);
         return m.d_head == 64 ? launch_narrow<float, 64, 1>(c, p) : launch_narrow<float, 128, 1>(c, p);
     }
     // The tcgen05 kernel for tiles of many rows.  Up to 32 rows two tiles of this file's kernel start sooner and cost a key no more (8

@@ -1171,3 +1171,12 @@ def test_which_kernel_ran_is_counted(ghd, dtype):
             want[tc] += 1
             assert [ghd.ghd_path_count(ctx, p) for p in (ghd.PATH_KV4_ROWS, ghd.PATH_KV4_TC)] == want
     ghd.ghd_sync_status(ctx)
+
+
+@pytest.mark.parametrize("tree", [True, False], ids=["tree", "causal"])
+@pytest.mark.parametrize("H,Hk,d,R,lens,cnt", [(4, 1, 64, 16, [100, 0], [45, 31]), (2, 1, 128, 32, [77], [90]), (24, 24, 128, 16, [33, 0], [90, 70]), (40, 20, 64, 64, [20], [44])])
+def test_two_tiles_at_a_time_in_float_mode(ghd, H, Hk, d, R, lens, cnt, tree):
+    """More than 128 rows a key head, or more than 64 and many heads."""
+    su = Setup(ghd, H, Hk, d, "f32", R, lens, cnt, 37 * H + R + len(lens), behind=3)
+    vis, words = su.trees() if tree else ([np.ones((n, n), bool) for n in cnt], None)
+    check_attention(ghd, su, vis, words)
