@@ -1180,3 +1180,26 @@ def test_two_tiles_at_a_time_in_float_mode(ghd, H, Hk, d, R, lens, cnt, tree):
     su = Setup(ghd, H, Hk, d, "f32", R, lens, cnt, 37 * H + R + len(lens), behind=3)
     vis, words = su.trees() if tree else ([np.ones((n, n), bool) for n in cnt], None)
     check_attention(ghd, su, vis, words)
+
+
+@pytest.mark.parametrize("path", [0, 1, 2], ids=["auto", "rows", "tcgen05"])
+@pytest.mark.parametrize("H,Hk,d,R,lens,cnt", [
+    (2, 1, 128, 64, [0], [700]),                                        # a prompt
+    (2, 2, 64, 16, [300, 0], [1, 513]),                                 # a prompt beside a token
+    (2, 2, 128, 32, [200] + [40 + 7 * i for i in range(31)], [256] + [1] * 31),      # a wide tree beside tokens
+    (4, 1, 64, 128, [130, 5, 1000, 0], [300, 1, 0, 33]),
+])
+def test_long_prompts_and_batches_of_unlike_sequences(ghd, H, Hk, d, R, lens, cnt, path):
+    su = Setup(ghd, H, Hk, d, "f16", R, lens, cnt, 41 * H + R + len(lens), behind=2)
+    on_path(ghd, su.ctx, path)
+    if cnt[0] == 256:
+        vis, words = su.trees()
+    else:
+        vis, words = [np.ones((n, n), bool) for n in cnt], None
+    check_attention(ghd, su, vis, words)
+
+
+@pytest.mark.parametrize("H,Hk,d,lens,cnt", [(2, 1, 128, [0], [600]), (2, 2, 64, [300, 0], [1, 290])])
+def test_long_prompts_in_float_mode(ghd, H, Hk, d, lens, cnt):
+    su = Setup(ghd, H, Hk, d, "f32", 32, lens, cnt, 43 * H + len(lens), behind=2)
+    check_attention(ghd, su, [np.ones((n, n), bool) for n in cnt], None)
