@@ -329,7 +329,8 @@ typedef struct ghd_kv4_rows {
 size_t ghd_kv4_pool_bytes(const ghd_ctx *ctx, const ghd_kv4 *kv);
 
 /* Appends the new rows (Sec. II-A): rotates q and k by the rows' positions (angles in 64 bits, rotate-half pairing,
- * cfg.rope_theta), quantises k and v and writes them to cache rows kv_len[s] + i.  kv_len is not changed.
+ * cfg.rope_theta), quantises k and v and writes them to cache rows kv_len[s] + i.  kv_len is not changed.  Keys, and
+ * GHD_F32's queries, are rotated in 64 bits; GHD_F16's queries in 32, then rounded to half.
  *   q: dev T [n_rows][n_heads * d_head], rows q_ld elements apart; q_out: dev T [n_rows][n_heads * d_head], contiguous
  *   (may be q itself when q_ld is n_heads * d_head); both NULL: keys and values only.  k, v: dev T
  *   [n_rows][n_kv_heads * d_head], rows kv_ld elements apart (q, k and v may be column blocks of one projection).

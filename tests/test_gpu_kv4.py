@@ -1203,3 +1203,22 @@ def test_long_prompts_and_batches_of_unlike_sequences(ghd, H, Hk, d, R, lens, cn
 def test_long_prompts_in_float_mode(ghd, H, Hk, d, lens, cnt):
     su = Setup(ghd, H, Hk, d, "f32", 32, lens, cnt, 43 * H + len(lens), behind=2)
     check_attention(ghd, su, [np.ones((n, n), bool) for n in cnt], None)
+
+
+@pytest.mark.parametrize("H,Hk,d,n", [(4, 4, 64, 1), (28, 4, 128, 3), (32, 32, 128, 200), (8, 8, 64, 700)])
+def test_float_queries_are_rotated_in_64_bits_and_rounded_once(ghd, H, Hk, d, n):
+    """Half a step of the result, and what differs between two ways to the angle in 64 bits: positions below 2^18 times a frequency
+    that two functions may round apart, 2^18 * 2^-51 with the products of the angle, and 2^-51 for sine, cosine and the two sums."""
+    r = np.random.RandomState(d + n)
+    ctx = make_ctx(ghd, H, d, "f32")
+    R, pages = 64, (n + 63) // 64
+    kv = ghd.Kv4Cache(dev(np.arange(pages, dtype=np.int32)[None]), dev(np.zeros(1, np.int32)), R, Hk, pages)
+    q, k = r.randn(n, H, d).astype(np.float32), r.randn(n, Hk * d).astype(np.float32)
+    pos = r.randint(0, 1 << 18, n).astype(np.int32)
+    got = ghd.ghd_kv4_append(ctx, kv, ghd.Kv4Rows(dev(np.array([0, n], np.int32)), n, pos=dev(pos)), ghd.ghd_kv4_pool(ctx, kv)[0], dev(q.reshape(n, -1)), dev(k), dev(k))
+    ghd.ghd_sync_status(ctx)
+    got = got.double().cpu().numpy().reshape(n, H, d)
+    want = np.stack([okv4.rotate(q[i].astype(np.float64), pos[i], THETA) for i in range(n)])
+    amp = np.abs(q.astype(np.float64))
+    amp = amp + np.concatenate([amp[..., d // 2:], amp[..., : d // 2]], -1)
+    assert (np.abs(got - want) <= 2.0 ** -24 * np.abs(want) + 2.0 ** -32 * amp).all()
