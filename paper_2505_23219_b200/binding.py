@@ -10,6 +10,7 @@ from pathlib import Path
 
 import numpy as np
 import torch
+from torch._C import _cuda_getCurrentRawStream as _raw_stream
 
 from . import build as _build
 
@@ -209,16 +210,12 @@ def _need(t, dtype, what: str, numel: int, dev: int | None = None):
     return t.data_ptr()
 
 
-def _int32(**numbers):
-    """Refuses numbers that the struct could not hold: ctypes would cut them off, and sizes be checked against other numbers."""
-    for what, x in numbers.items():
-        if not -2**31 <= x < 2**31:
-            raise GhdError(1, f"kv4: {what} = {x} is outside 32 bits")
+_INT = 0x80000000      # numbers outside [-_INT, _INT) are refused: ctypes would cut them off, and sizes be checked against others
 
 
 class _Description:
     """Holds tensors beside the struct with their pointers, and does not change: an attribute that was set to another tensor would
-    free the one that the struct still points to.  (The constructors fill __dict__ in one go.)"""
+    free the one that the struct still points to.  (The constructors write to __dict__.)"""
 
     def __setattr__(self, name, value):
         raise AttributeError(f"{type(self).__name__}.{name} is fixed: write into its tensors, or make another {type(self).__name__}")
@@ -236,11 +233,13 @@ class Kv4Cache(_Description):
         if page_table.dim() != 2:
             raise GhdError(1, "kv4: page_table is not [n_seqs][max_pages]")
         n_seqs, max_pages = page_table.shape
-        _int32(page_rows=page_rows, n_kv_heads=n_kv_heads, n_pages=n_pages)
+        if not (-_INT <= page_rows < _INT and -_INT <= n_kv_heads < _INT and -_INT <= n_pages < _INT):
+            raise GhdError(1, f"kv4: page_rows {page_rows}, n_kv_heads {n_kv_heads} or n_pages {n_pages} is outside 32 bits")
         table, dev = _need(page_table, torch.int32, "page_table", 0), page_table.get_device()
         c = _Kv4(n_seqs, n_pages, page_rows, max_pages, n_kv_heads, table, _need(kv_len, torch.int32, "kv_len", n_seqs, dev))
-        self.__dict__.update(page_table=page_table, kv_len=kv_len, dev=dev, n_seqs=n_seqs, n_kv_heads=n_kv_heads, n_rows=n_pages * n_kv_heads * page_rows,
-                             c=c, ref=C.byref(c))
+        own = self.__dict__
+        own["page_table"], own["kv_len"], own["dev"], own["n_seqs"], own["n_kv_heads"] = page_table, kv_len, dev, n_seqs, n_kv_heads
+        own["n_rows"], own["c"], own["ref"] = n_pages * n_kv_heads * page_rows, c, C.byref(c)
 
 
 class Kv4Rows(_Description):
@@ -249,12 +248,15 @@ class Kv4Rows(_Description):
 
     def __init__(self, row_start, n_rows: int, pos=None, mask=None):
         n_rows = int(n_rows)
-        _int32(n_rows=n_rows)
+        if not -_INT <= n_rows < _INT:
+            raise GhdError(1, f"kv4: n_rows {n_rows} is outside 32 bits")
         start, dev = _need(row_start, torch.int32, "row_start", 2), row_start.get_device()
         words = 0 if mask is None else int(mask.shape[-1])
         c = _Kv4Rows(n_rows, words, start, None if pos is None else _need(pos, torch.int32, "pos", n_rows, dev),
                      None if mask is None else _need(mask, torch.int64, "mask", n_rows * words, dev))
-        self.__dict__.update(row_start=row_start, n_rows=n_rows, pos=pos, mask=mask, n_starts=row_start.numel(), dev=dev, c=c, ref=C.byref(c))
+        own = self.__dict__
+        own["row_start"], own["n_rows"], own["pos"], own["mask"] = row_start, n_rows, pos, mask
+        own["n_starts"], own["dev"], own["c"], own["ref"] = row_start.numel(), dev, c, C.byref(c)
 
 
 class Tree:
@@ -454,14 +456,17 @@ def ghd_tree_fill_tokens(ctx: Ctx, cand, result, level, rank, tokens=None):
     return tokens
 
 
-def _kv4_made(ctx: Ctx, make, *args, **kw):
-    """A tensor that a call makes for its result: on the context's stream, where the kernels write it.  Made on another current
-    stream, its fill (or what still runs there on the memory that it gets) could come after the kernels."""
-    if torch._C._cuda_getCurrentRawStream(ctx.dev) == ctx.raw_stream:
-        return make(*args, **kw)
+def _kv4_here(ctx: Ctx) -> bool:
+    """Whether the current stream is the context's.  The tensors that a call makes for its results are made on the context's, where
+    the kernels write them: made on another, their fill (or what still runs there on the memory that they get) could come after."""
+    return _raw_stream(ctx.dev) == ctx.raw_stream
+
+
+def _kv4_there(ctx: Ctx, make, *args, **kw):
+    """make(...) under the context's stream, for use on the current one."""
     with torch.cuda.stream(ctx.stream):
         t = make(*args, **kw)
-    t.record_stream(torch.cuda.current_stream(ctx.device))          # where the caller is going to use it
+    t.record_stream(torch.cuda.current_stream(ctx.device))
     return t
 
 
@@ -471,7 +476,10 @@ def ghd_kv4_pool_bytes(ctx: Ctx, kv: Kv4Cache) -> int:
 
 def ghd_kv4_pool(ctx: Ctx, kv: Kv4Cache, n_layers: int = 1):
     """A zeroed pool per layer, uint8 [n_layers][bytes]."""
-    return _kv4_made(ctx, torch.zeros, (n_layers, ghd_kv4_pool_bytes(ctx, kv)), dtype=torch.uint8, device=ctx.device)
+    shape = (n_layers, ghd_kv4_pool_bytes(ctx, kv))
+    if _kv4_here(ctx):
+        return torch.zeros(shape, dtype=torch.uint8, device=ctx.device)
+    return _kv4_there(ctx, torch.zeros, shape, dtype=torch.uint8, device=ctx.device)
 
 
 def _kv4_match(ctx: Ctx, kv: Kv4Cache, rows: Kv4Rows):
@@ -511,7 +519,7 @@ def ghd_kv4_append(ctx: Ctx, kv: Kv4Cache, rows: Kv4Rows, pool, q, k, v, q_out=N
         width = ctx.n_heads * ctx.d_head
         qp, qld = _kv4_strided(ctx, q, n, width, "q")
         if q_out is None:
-            q_out = _kv4_made(ctx, ctx.blank.new_empty, (n, width))
+            q_out = ctx.blank.new_empty((n, width)) if _kv4_here(ctx) else _kv4_there(ctx, ctx.blank.new_empty, (n, width))
         op = _need(q_out, ctx.dtype, "q_out", n * width, ctx.dev)
     ctx._check(ctx.lib.ghd_kv4_append(ctx.handle, kv.ref, rows.ref, at, qp, qld, kp, vp, kld, op))
     return q_out
@@ -523,7 +531,8 @@ def ghd_kv4_attention(ctx: Ctx, kv: Kv4Cache, rows: Kv4Rows, pool, q, out=None):
     _kv4_match(ctx, kv, rows)
     at = _kv4_pool(ctx, kv, pool)
     qp = _need(q, ctx.dtype, "q", numel, ctx.dev)
-    out = _kv4_made(ctx, torch.zeros_like, q) if out is None else out
+    if out is None:
+        out = torch.zeros_like(q) if _kv4_here(ctx) else _kv4_there(ctx, torch.zeros_like, q)
     ctx._check(ctx.lib.ghd_kv4_attention(ctx.handle, kv.ref, rows.ref, at, qp, _need(out, ctx.dtype, "out", numel, ctx.dev)))
     return out
 
@@ -534,24 +543,27 @@ def ghd_kv4_read(ctx: Ctx, kv: Kv4Cache, pool, row_start, n_rows: int, first=Non
     rows = Kv4Rows(row_start, n_rows)
     _kv4_match(ctx, kv, rows)
     at = _kv4_pool(ctx, kv, pool)
-    shape = (rows.n_rows, kv.n_kv_heads * ctx.d_head)
-    if rows.n_rows < 0:
+    n, width = rows.n_rows, kv.n_kv_heads * ctx.d_head
+    if n < 0:
         raise GhdError(1, "kv4_read: negative n_rows")
-    if (k_out is not None and not keys) or (v_out is not None and not values):
-        raise GhdError(1, "kv4_read: an output for what is not asked for")
+    shape = (n, width)
     kp = vp = None
-    if keys:
-        if k_out is None:
-            k_out = _kv4_made(ctx, ctx.blank.new_empty, shape)
-            kp = k_out.data_ptr()
+    here = _raw_stream(ctx.dev) == ctx.raw_stream
+    if k_out is not None:
+        kp = _need(k_out, ctx.dtype, "k_out", n * width, ctx.dev)
+    elif keys:
+        k_out = ctx.blank.new_empty(shape) if here else _kv4_there(ctx, ctx.blank.new_empty, shape)
+        kp = k_out.data_ptr()
+    if v_out is not None:
+        vp = _need(v_out, ctx.dtype, "v_out", n * width, ctx.dev)
+    elif values:
+        if here:
+            v_out = torch.empty_like(k_out) if kp and k_out.shape == shape else ctx.blank.new_empty(shape)      # (the like of a tensor is made sooner)
         else:
-            kp = _need(k_out, ctx.dtype, "k_out", shape[0] * shape[1], ctx.dev)
-    if values:
-        if v_out is None:
-            v_out = _kv4_made(ctx, torch.empty_like, k_out) if keys and k_out.shape == shape else _kv4_made(ctx, ctx.blank.new_empty, shape)
-            vp = v_out.data_ptr()
-        else:
-            vp = _need(v_out, ctx.dtype, "v_out", shape[0] * shape[1], ctx.dev)
+            v_out = _kv4_there(ctx, ctx.blank.new_empty, shape)
+        vp = v_out.data_ptr()
+    if (kp and not keys) or (vp and not values):
+        raise GhdError(1, "kv4_read: an output for what is not asked for")
     st = ctx.lib.ghd_kv4_read(ctx.handle, kv.ref, rows.ref, at, None if first is None else _need(first, torch.int32, "first", kv.n_seqs, ctx.dev), kp, vp)
     if st:
         ctx._check(st)
