@@ -341,7 +341,10 @@ ghd_status ghd_kv4_append(ghd_ctx *ctx, const ghd_kv4 *kv, const ghd_kv4_rows *r
 /* Attention of the new rows over the cache (ghd_tree_attention over pages and 4 bits): row i of sequence s sees cache
  * rows [0, kv_len[s]) and the new rows its mask shows, which ghd_kv4_append has already written.
  * q (rotated), out: dev T [n_rows][n_heads * d_head], 16-byte aligned, not the same memory.  The partial sums lie in the
- * context's workspace: calls of one context, graphs recorded from it included, run one after another. */
+ * context's workspace: calls of one context, graphs recorded from it included, run one after another.
+ * Scores, weights and sums have 32 bits; in the product with V's codes a weight times V's scale has half's 11 bits (GHD_F16) or 24
+ * (GHD_F32, queries too).  The kernel is picked by n_rows / n_seqs: a long prompt or tree and many single tokens are done sooner in
+ * a call each. */
 ghd_status ghd_kv4_attention(ghd_ctx *ctx, const ghd_kv4 *kv, const ghd_kv4_rows *rows, const void *pool, const void *q, void *out);
 
 /* Reads rows back: row i of sequence s is cache row first[s] + i (first: dev [n_seqs], NULL = kv_len), min + scale * code

@@ -5,7 +5,7 @@
 //   K        four warps: one thread per key unpacks its 4-bit row in registers and stores it to tensor memory, from where
 //            the first product takes its A operand - the unpacked keys never touch shared memory;
 //   V        four warps unpack V rows into a swizzled shared-memory tile (A operand of the second product, M-major);
-//   softmax  warps read S^T in the 16x256b fragment form: a thread holds 4 keys x 4 (or 8) query rows, so a key's
+//   softmax  warps read S^T in the 16x256b fragment form: a thread holds 4 keys x 8 query rows, so a key's
 //            scales and minima are a few registers and a row's running sums one each; weights times V's scale go to
 //            shared memory by stmatrix as the B operand of the second product;
 //   one warp each issues the first and the second product, and works out the CTA's items ahead of
@@ -14,12 +14,12 @@
 // queries are stored in that order, and the output's lanes are read back through it.
 //
 // Half range: weights are taken against a reference that is raised when a score passes it by 2^8, and V's scales are
-// divided by 2^e, e raised when a scale passes 2^7 of it, so the operand stays below 2^15.  Raising either rescales O^T
+// divided by 2^e, e raised when a scale passes 2^7 of it, so the operand (11 bits, as in attn_kv4.cu) stays below 2^15.  Raising either rescales O^T
 // in place (rare after the first unit); the 128 threads that share query rows agree on it by one barrier a unit.
 //
 // Work is dealt as in attn_kv4.cu, one CTA an SM.
 //
-// What it costs.  8 ragged trees of up to 64 nodes over up to 8192 rows, 32 heads (148 MB, 30 GFLOP): 120 us; one tree of 256 nodes over
+// What it costs.  8 ragged trees of up to 64 nodes over up to 8192 rows, 32 heads (148 MB, 30 GFLOP): 122 us; one tree of 256 nodes over
 // 4096 rows, 40 heads (22 GFLOP): 83 us.  A unit of 128 keys x 64 rows takes about 2700 clocks where its products take 900 and its
 // exponentials 500: the softmax warps' chain (in clocks: scores 550, agreement on references 270, fetch of the next scores 700, wait
 // for a P buffer 350 though it is free, weights 900, hand-over 250), at 2 instructions an SM a clock; K and V are two units ahead.  A unit
@@ -46,8 +46,8 @@ constexpr int N = 64;                          // query rows of a tile; tiles of
 constexpr int SOFT = 256, CONV = 256;          // threads of the softmax and of the unpacking warps
 constexpr int PARTS = SOFT / 128;              // 128 threads (one a key of four) share query rows, as pairs of blocks of eight: pair part, part + PARTS, ...
 constexpr int THREADS = SOFT + CONV + 128, SW = SOFT / 32, CW = SW + CONV / 32;      // first unpacking warp, first of the others
-// registers a thread after the split by warpgroups, within those launched with
 static_assert(N / 8 / PARTS == 4, "a lane of eight ends up with one of 4 + 4 blocks' sums");
+// registers a thread after the split by warpgroups, within those launched with
 constexpr int REGS_LAUNCH = 96, REGS_SOFT = 152, REGS_CONV = 56, REGS_ISSUE = 56;
 static_assert(SOFT * REGS_SOFT + CONV * REGS_CONV + 128 * REGS_ISSUE <= THREADS * REGS_LAUNCH && THREADS * REGS_LAUNCH <= 65536, "register split");
 constexpr float RAISE = 8.f;

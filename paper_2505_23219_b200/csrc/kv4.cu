@@ -161,10 +161,11 @@ constexpr int APPEND_RESIDENT = 16;     // warps of k_kv4_append on an SM at a t
 // the pairs t = 8 j .. 8 j + 7 with both halves (K, q), so the rotation needs no exchange and its codes are two words; of V the 16
 // channels from 16 j on.  What the next two jobs read is asked for ahead.  The row's angles (64-bit sincos, D / 2 of them) are
 // shared out over the lanes and passed round by shuffles.
-// One row of 32 heads takes 4.0 us, a launch and a chain of loads; 2048 rows, 32 heads on 8, 12.6.  8 ragged prompts of up to 2048 rows
-// (q in and out, k and v in, codes out: 277 MB) take 74 us, 3.7 TB/s, of which the queries are 37; 16 warps an SM (126 registers) wait
-// for loads and for one another's results.  More warps with spills: 79 us when this took 85, but one row 5.2 instead of 4.3; quotients
-// in paired instructions: slower.  32 bits instead of 64 for the rotation or the angles would save 2 us.
+// One row of 32 heads takes 4.6 us, a launch and a chain of loads; 2048 rows, 32 heads on 8 (44 MB), 15.6 from DRAM, 12.6 from the L2.
+// 8 ragged prompts of up to 2048 rows (q in and out, k and v in, codes out: 298 MB) take 74 us, 4.0 TB/s; k and v alone 39; 16 warps an
+// SM (126 registers) wait for loads and for one another's results.  More warps with spills: 79 us when this took 85, but one row 5.2
+// instead of 4.3; quotients in paired instructions: slower.  32 bits instead of 64 for the keys' rotation or the angles would save 2 us.
+// Float (582 MB): 107 us, 5.4 TB/s.
 template <typename T, int D>
 __global__ void __launch_bounds__(ROW_WARPS * 32, APPEND_RESIDENT / ROW_WARPS) k_kv4_append(const __grid_constant__ Kv4View w, const __grid_constant__ RopeFreq fr, uint8_t* __restrict__ pool,
                                                                const int32_t* __restrict__ pos, const T* q, int64_t q_ld, const T* __restrict__ k,
@@ -318,7 +319,8 @@ __device__ __forceinline__ void decode8(uint32_t c, RowPar<__half> f, __half* y)
 
 // A warp takes a row and every `slices`-th of its jobs: K and V of HPW heads, D / 8 lanes each; a lane decodes eight channels of
 // both (4 bytes in, 16 or 32 out).  AHEAD jobs' loads are under way together.  The bytes written bound it when there are many rows:
-// 8 sequences of up to 2048 rows, 32 heads (177 MB): 36 us, 4.8 TB/s (59 us with codes converted to 32 bits one by one).  13 rows: 2.6 us.
+// 8 sequences of up to 2048 rows, 32 heads (177 MB): 37 us, 4.8 TB/s (59 us with codes converted to 32 bits one by one); float (319 MB)
+// 86 us, 3.7 TB/s.  13 rows: 2.7 us.
 template <typename T, int D>
 __global__ void __launch_bounds__(ROW_WARPS * 32) k_kv4_read(const __grid_constant__ Kv4View w, const uint8_t* __restrict__ pool, const int32_t* __restrict__ first,
                                                              T* __restrict__ k_out, T* __restrict__ v_out, int slices, int rows_each) {
@@ -374,7 +376,7 @@ __global__ void __launch_bounds__(ROW_WARPS * 32) k_kv4_read(const __grid_consta
 // Block = one (pool, sequence, head); a lane owns one piece of a row: 16 bytes of K or V codes, or the scale and minimum
 // of K or V.  Lanes own disjoint pieces: no synchronisation.  Eight rows of the path are read together and then written: what a
 // call costs is the latency of node, page and piece, one behind the other (16 sequences, paths of 5, 8 layers, both launches:
-// 6.2 us row by row, 5.0 so).  Accepted nodes rise and nodes[j] >= j, so no row is written before it has been read.
+// 6.2 us row by row, 5.1 so; 32 layers of 16 sequences 7.2).  Accepted nodes rise and nodes[j] >= j, so no row is written before it has been read.
 constexpr int COMMIT_POOLS = 64, COMMIT_ROWS = 8;
 struct CommitPools { uint8_t* p[COMMIT_POOLS]; };
 
@@ -446,7 +448,7 @@ __global__ void k_kv4_advance(Kv4View w, int32_t* kv_len, const ghd_accept_resul
 
 // Warps of a call over rows; `resident`: those that an SM holds at a time.  Few rows: their jobs are dealt to several warps
 // (slices) until the device is full once, and no further, since every warp of a row works out its angles (append with four
-// times as many: 512 / 1024 / 2048 rows of 32 heads on 8 took 11.6 / 20.0 / 23.1 us, now 8.2 / 10.0 / 12.6).  Many rows: a warp takes
+// times as many: 512 / 1024 / 2048 rows of 32 heads on 8 took 11.6 / 20.0 / 23.1 us where they take 6.6 / 8.4 / 12.6).  Many rows: a warp takes
 // several in turn, whose sequence it then looks up once.
 struct RowGrid { int slices, rows_each, blocks; };
 RowGrid row_grid(const ghd_ctx* c, int n_rows, int jobs, int resident) {
@@ -543,8 +545,8 @@ ghd_status ghd_kv4_append(ghd_ctx* c, const ghd_kv4* kv, const ghd_kv4_rows* row
     const int hpw = 32 / (D / 16);
     const int q_jobs = (m.n_heads + hpw - 1) / hpw, kv_jobs = 2 * ((kv->n_kv_heads + hpw - 1) / hpw);
     const RowGrid g = row_grid(c, rows->n_rows, q ? q_jobs : kv_jobs, APPEND_RESIDENT);
-    // Blocks of their own for the queries while all fit the device at once (one row 4.0 us, 64 rows 4.7); else a warp does both, with
-    // one set of angles (512 / 1024 rows of 32 heads on 8: 8.2 / 9.9 us apart, 6.5 / 8.6 together).
+    // Blocks of their own for the queries while all fit the device at once (one row 4.6 us, 64 rows 4.5); else a warp does both, with
+    // one set of angles (512 / 1024 rows of 32 heads on 8: 8.2 / 9.9 us apart, 6.6 / 8.4 together).
     const bool apart = q && 2 * (int64_t)rows->n_rows * q_jobs <= (int64_t)c->sm_count * APPEND_RESIDENT;
     const dim3 grid(g.blocks, apart ? 2 : 1);
 #define GHD_APPEND(T, DH) k_kv4_append<T, DH><<<grid, ROW_WARPS * 32, 0, c->cur>>>(w, fr, (uint8_t*)pool, rows->pos, (const T*)q, q_ld, (const T*)k, (const T*)v, kv_ld, (T*)q_out, m.n_heads, g.slices, g.rows_each)
