@@ -9,12 +9,13 @@
 // Keys are the M side of both products: S^T [16 keys x 8 rows] = K Q^T and O^T [16 channels x 8 rows] = V^T P^T
 // (mma.sync m16n8k16), so one to eight rows cost one n-tile.  The lanes' channels are permuted so that a lane's codes are
 // consecutive bytes of a row; nibbles become operands in registers.  A warp takes 32 keys of every chunk of 128 and keeps
-// its own running reference (raised when a score exceeds it by 2^2) and sums; the warps meet in shared memory.
+// its own running reference and sums; the warps meet in shared memory.
 //
-// Half range: p * scale is the operand of the second product, rounded to half's 11 bits.  V's scales are multiplied by a power of
-// two, lowered when a visible key's scale passes 2^13 of it and then chosen so that the largest lies in [2^10, 2^11): p <= 2^2 keeps the
-// operand below 2^15, and weights down to 2^-24 of the reference's keep all bits at the largest scale.  (Without the power,
-// p * scale of small values and of keys far below the top fell below half's normal range.)
+// Half range: p * scale is the operand of the second product, rounded to half's 11 bits.  So a row's reference goes by score + log2(scale) of
+// the keys that it sees: it is raised when that passes 2^15 of it, and then lies 2^10 below the largest product, so products
+// down to 2^-24 of the largest keep all bits, whatever the values' size, and no key has a say in rows that do not see it.  p itself
+// stays below 2^40, within 32 bits.  (With references by the scores alone, p * scale of small values and of keys far below the
+// top fell below half's normal range.)  Float: by the scores alone, raised by more than 2^2.
 //
 // Work is dealt by device-side lengths: all chunks of all (sequence, head, row tile) items are numbered and each CTA takes
 // an equal run of them (kv4_layout.h), so ragged batches and single long sequences fill the device alike.  An item cut by
@@ -42,9 +43,6 @@ namespace ghd {
 namespace {
 
 constexpr int WARPS = 4, WKEYS = 32, CHUNK = WKEYS * WARPS;      // a warp takes 32 keys of every chunk
-constexpr float RAISE = 2.f;
-constexpr float VS_TOP = 0x1p13f;      // largest of V's scales times their power of two
-constexpr int VS_EXP = 10;             // exponent of the largest one where the power is chosen
 constexpr int LEAD = 4;          // an item's fixed cost in chunks (one token of 32 heads over 2048 and 16384 rows: 2: 11.3 and 28.9 us, 3: 11.3 and 28.3, 4: 11.6 and 27.3)
 
 using namespace kv4;
@@ -144,6 +142,7 @@ __global__ void __launch_bounds__(WARPS * 32, Narrow<T, D, NT>::BLOCKS) k_attn_k
     using N = Narrow<T, D, NT>;
     using O_ = Op<T>;
     constexpr bool HALF = sizeof(T) == 2;
+    constexpr float RAISE = HALF ? 15.f : 2.f, TOP = HALF ? 10.f : 0.f;      // where a reference is raised, and what lies above a new one
     constexpr int RT = N::RT, KW = N::KW, VW = N::VW, KS = N::KS, MT = N::MT, TERMS = O_::TERMS, XO = N::XO, es = N::ES;
     extern __shared__ __align__(16) uint8_t smem[];
     __shared__ int64_t scratch[32];
@@ -279,7 +278,6 @@ __global__ void __launch_bounds__(WARPS * 32, Narrow<T, D, NT>::BLOCKS) k_attn_k
         float o[MT][NT][4];
         float base[NT][2], l[NT][2], ms[NT][2];
         uint32_t none = (1u << 2 * NT) - 1u;
-        float vmul = HALF ? 0x1p34f : 1.f;                              // power of two of V's scales (half's smallest, 2^-24, has VS_EXP so)
 #pragma unroll
         for (int nt = 0; nt < NT; ++nt) {
 #pragma unroll
@@ -335,11 +333,14 @@ __global__ void __launch_bounds__(WARPS * 32, Narrow<T, D, NT>::BLOCKS) k_attn_k
                 }
             }
             // scores in powers of two, less the base
-            float top = -INFINITY;
+            float top = -INFINITY, vs[2][2], lv[2][2] = {};              // V's scales of keys (z, h), and what they add to a product
+            auto product = [&](int z, int h, float v) { return HALF ? v + lv[z][h] : v; };
 #pragma unroll
             for (int z = 0; z < 2; ++z)
 #pragma unroll
                 for (int h = 0; h < 2; ++h) {
+                    vs[z][h] = param_of<T>(st + N::VP_AT, 16 * z + ka + 8 * h).x;
+                    lv[z][h] = HALF ? scale_bits(vs[z][h]) : 0.f;
                     const float2 kp = param_of<T>(st + N::P_AT, 16 * z + ka + 8 * h);
                     // km - km: 0, or NaN for a minimum that the rotation took to -inf (the key reads as -inf throughout, and a product of
                     // that with a query is no number; -inf times the queries' sum would drop the key, or not, by the sum's sign)
@@ -350,18 +351,11 @@ __global__ void __launch_bounds__(WARPS * 32, Narrow<T, D, NT>::BLOCKS) k_attn_k
                         for (int e = 0; e < 2; ++e) {
                             float& v = s[z][nt][2 * h + e];
                             v = fmaf(ks, v, fmaf(km, qs[nt][e], -base[nt][e]));
-                            top = fmaxf(top, v);
+                            top = fmaxf(top, product(z, h, v));
                         }
                 }
-            float vs[2][2];                                             // V's scales of keys (z, h)
-#pragma unroll
-            for (int z = 0; z < 2; ++z)
-#pragma unroll
-                for (int h = 0; h < 2; ++h) vs[z][h] = param_of<T>(st + N::VP_AT, 16 * z + ka + 8 * h).x;
             bool over = none != 0u || top > RAISE;                      // (a row's first keys may have had no page)
-            if (HALF) over = over || fmaxf(fmaxf(vs[0][0], vs[0][1]), fmaxf(vs[1][0], vs[1][1])) * vmul > VS_TOP;
             uint32_t vis = 0xffffffffu;                                 // bit 8 nt + 4 z + e: score s[z][nt][e] counts
-            auto seen = [&](int z, int h) { return (vis & (NT == 2 ? 0x303u : 3u) << (4 * z + 2 * h)) != 0u; };      // key (z, h), by a row of this lane
             if (__builtin_expect(!all, 0)) {
                 // a lane looks up the warp's 32 keys for one of the tile's rows; the others get the word by shuffle
                 uint32_t word = sees(p, it.q, (it.tile * RT + min(lane, RT - 1)) / p.group, key0 - it.q.len);
@@ -380,53 +374,32 @@ __global__ void __launch_bounds__(WARPS * 32, Narrow<T, D, NT>::BLOCKS) k_attn_k
                                 float& v = s[z][nt][2 * h + e];
                                 if ((b >> (16 * z + 8 * h)) & 1u) vis |= 1u << (8 * nt + 4 * z + 2 * h + e);
                                 else v = -INFINITY;
-                                over = over || v > ((none >> (2 * nt + e)) & 1u ? -INFINITY : RAISE);
+                                over = over || product(z, h, v) > ((none >> (2 * nt + e)) & 1u ? -INFINITY : RAISE);
                             }
                     }
-                if (HALF)                                               // what nobody sees, and what lies behind the rows, has no say in the power
-#pragma unroll
-                    for (int z = 0; z < 2; ++z)
-#pragma unroll
-                        for (int h = 0; h < 2; ++h) over = over || (seen(z, h) && vs[z][h] * vmul > VS_TOP);
             }
             if (__any_sync(0xffffffffu, over)) {
-                float fv = 1.f;
-                if (HALF) {
-                    float vx = 0.f;
-#pragma unroll
-                    for (int z = 0; z < 2; ++z)
-#pragma unroll
-                        for (int h = 0; h < 2; ++h) if (seen(z, h) && vs[z][h] <= 65504.f) vx = fmaxf(vx, vs[z][h]);
-#pragma unroll
-                    for (int x = 1; x < 32; x <<= 1) vx = fmaxf(vx, __shfl_xor_sync(0xffffffffu, vx, x));
-                    if (vx * vmul >= (float)(2 << VS_EXP)) {
-                        const float vnew = __uint_as_float((uint32_t)(254 + VS_EXP - (int)(__float_as_uint(vx) >> 23)) << 23);
-                        fv = vnew / vmul;
-                        vmul = vnew;
-                    }
-                }
 #pragma unroll
                 for (int nt = 0; nt < NT; ++nt)
 #pragma unroll
                     for (int e = 0; e < 2; ++e) {
-                        float up = fmaxf(fmaxf(s[0][nt][e], s[0][nt][e + 2]), fmaxf(s[1][nt][e], s[1][nt][e + 2]));
+                        float up = fmaxf(fmaxf(product(0, 0, s[0][nt][e]), product(0, 1, s[0][nt][e + 2])), fmaxf(product(1, 0, s[1][nt][e]), product(1, 1, s[1][nt][e + 2])));
                         up = fmaxf(up, __shfl_xor_sync(0xffffffffu, up, 4));
                         up = fmaxf(up, __shfl_xor_sync(0xffffffffu, up, 8));
                         up = fmaxf(up, __shfl_xor_sync(0xffffffffu, up, 16));
+                        up -= TOP;
                         const bool had = !((none >> (2 * nt + e)) & 1u);
-                        float f = 1.f;
                         if (up > (had ? 0.f : -INFINITY)) {             // the new reference is `up` above the base
-                            f = had ? ex2(-up) : 0.f;
+                            const float f = had ? ex2(-up) : 0.f;
                             none &= ~(1u << (2 * nt + e));
                             base[nt][e] += up;
                             l[nt][e] *= f;
                             ms[nt][e] *= f;
 #pragma unroll
                             for (int z = 0; z < 2; ++z) { s[z][nt][e] -= up; s[z][nt][e + 2] -= up; }
-                        }
-                        f *= fv;
 #pragma unroll
-                        for (int mt = 0; mt < MT; ++mt) { o[mt][nt][e] *= f; o[mt][nt][e + 2] *= f; }
+                            for (int mt = 0; mt < MT; ++mt) { o[mt][nt][e] *= f; o[mt][nt][e + 2] *= f; }
+                        }
                     }
             }
             uint32_t bp[2][NT][TERMS][2];
@@ -435,7 +408,7 @@ __global__ void __launch_bounds__(WARPS * 32, Narrow<T, D, NT>::BLOCKS) k_attn_k
 #pragma unroll
                 for (int z = 0; z < 2; ++z) {
                     const float2 vp0 = param_of<T>(st + N::VP_AT, 16 * z + ka), vp1 = param_of<T>(st + N::VP_AT, 16 * z + ka + 8);
-                    const float vm0 = fmaf(8.f, vp0.x, vp0.y), vm1 = fmaf(8.f, vp1.x, vp1.y), vs0 = HALF ? vs[z][0] * vmul : vs[z][0], vs1 = HALF ? vs[z][1] * vmul : vs[z][1];
+                    const float vm0 = fmaf(8.f, vp0.x, vp0.y), vm1 = fmaf(8.f, vp1.x, vp1.y);
 #pragma unroll
                     for (int nt = 0; nt < NT; ++nt) {
                         float ps[4];
@@ -443,7 +416,7 @@ __global__ void __launch_bounds__(WARPS * 32, Narrow<T, D, NT>::BLOCKS) k_attn_k
                         for (int e = 0; e < 4; ++e) {
                             const float pe = ex2(s[z][nt][e]);
                             l[nt][e & 1] += pe;
-                            ps[e] = pe * (e < 2 ? vs0 : vs1);
+                            ps[e] = pe * vs[z][e >> 1];
                             if (PLAIN || ((vis >> (8 * nt + 4 * z + e)) & 1u)) ms[nt][e & 1] = fmaf(pe, e < 2 ? vm0 : vm1, ms[nt][e & 1]);
                             else ps[e] = 0.f;                           // by selection: what a key holds stays out of rows that do not see it
                         }
@@ -492,7 +465,6 @@ __global__ void __launch_bounds__(WARPS * 32, Narrow<T, D, NT>::BLOCKS) k_attn_k
         }
 
         // ---- the warps' sums meet
-        const float vinv = 1.f / vmul;
 #pragma unroll
         for (int nt = 0; nt < NT; ++nt)
 #pragma unroll
@@ -505,7 +477,7 @@ __global__ void __launch_bounds__(WARPS * 32, Narrow<T, D, NT>::BLOCKS) k_attn_k
                 if (g == 0) { xm[warp * RT + rl] = (none >> (2 * nt + e)) & 1u ? -INFINITY : base[nt][e]; xl[warp * RT + rl] = a; xs[warp * RT + rl] = b; }
 #pragma unroll
                 for (int mt = 0; mt < MT; mt += 2)
-                    *reinterpret_cast<float4*>(xo + (warp * RT + rl) * XO + g * (D / 8) + 2 * mt) = make_float4(o[mt][nt][e] * vinv, o[mt][nt][e + 2] * vinv, o[mt + 1][nt][e] * vinv, o[mt + 1][nt][e + 2] * vinv);
+                    *reinterpret_cast<float4*>(xo + (warp * RT + rl) * XO + g * (D / 8) + 2 * mt) = make_float4(o[mt][nt][e], o[mt][nt][e + 2], o[mt + 1][nt][e], o[mt + 1][nt][e + 2]);
             }
         __syncthreads();
         const int64_t c0 = kv4_cta_of(it.first, per), c1 = kv4_cta_of(it.first + it.chunks - 1, per);      // CTAs that share the item

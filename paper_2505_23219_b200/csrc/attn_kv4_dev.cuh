@@ -31,6 +31,14 @@ __device__ __forceinline__ float ex2(float x) {
     return y;
 }
 
+// What a scale of V adds, in powers of two, to the operand of the second product: its logarithm, held at that of half's smallest number.
+// A scale that is no finite half makes its rows NaN whatever the reference, and has no say in it.
+__device__ __forceinline__ float scale_bits(float s) {
+    float y;
+    asm("lg2.approx.ftz.f32 %0, %1;" : "=f"(y) : "f"(s));
+    return s <= 65504.f ? fmaxf(y, -24.f) : -24.f;
+}
+
 template <typename T> __device__ __forceinline__ float to_f(T v);
 template <> __device__ __forceinline__ float to_f<float>(float v) { return v; }
 template <> __device__ __forceinline__ float to_f<__half>(__half v) { return __half2float(v); }

@@ -13,9 +13,9 @@
 // O^T stays in tensor memory over all keys of an item.  Nibbles come out of a word in the order 0 4 1 5 2 6 3 7; the
 // queries are stored in that order, and the output's lanes are read back through it.
 //
-// Half range: weights are taken against a reference that is raised when a score passes it by 2^8, and V's scales are
-// divided by 2^e, e raised when a scale passes 2^7 of it, so the operand (11 bits, as in attn_kv4.cu) stays below 2^15.  Raising either rescales O^T
-// in place (rare after the first unit); the 128 threads that share query rows agree on it by one barrier a unit.
+// Half range: as in attn_kv4.cu a row's reference goes by score + log2(V's scale) of the keys that it sees, so that the operand (11 bits)
+// stays below 2^15; it is raised when that passes 2^15 of it, and then lies 2^7 below the largest.  Raising rescales O^T in place
+// (rare after the first unit); the 128 threads that share query rows agree on it by one barrier a unit.
 //
 // Work is dealt as in attn_kv4.cu, one CTA an SM.
 //
@@ -50,7 +50,7 @@ static_assert(N / 8 / PARTS == 4, "a lane of eight ends up with one of 4 + 4 blo
 // registers a thread after the split by warpgroups, within those launched with
 constexpr int REGS_LAUNCH = 96, REGS_SOFT = 152, REGS_CONV = 56, REGS_ISSUE = 56;
 static_assert(SOFT * REGS_SOFT + CONV * REGS_CONV + 128 * REGS_ISSUE <= THREADS * REGS_LAUNCH && THREADS * REGS_LAUNCH <= 65536, "register split");
-constexpr float RAISE = 8.f;
+constexpr float RAISE = 15.f, TOP = 7.f;       // where a reference is raised, and what lies above a new one
 constexpr int LEAD = 4;                        // an item's fixed cost in units (8 ragged trees: 3: 124 us, 4: 120, 5: 120, 6: 122; one of 64 nodes over 512 rows: 20.5, 20.5, 21.9, 22.0)
 // What the softmax warps need of a unit's keys is ready when its keys are.  The K warps are two units ahead of the first
 // product, that is two ahead of the scores being fetched, and those one ahead of what the softmax warps work on: five in use.
@@ -86,7 +86,6 @@ struct Ctrl {
     float4 par[PAR_SLOTS][UNIT];     // by unit and key: K's scale and middle (min + 8 scale) times log2(e) / sqrt(d_head), V's scale and middle
     alignas(4) uint8_t groups[GROUP_SLOTS][4];      // which of a quarter's two groups of 16 keys have a page, by unit
     alignas(16) int rowix[2][N];               // row of q and out, in d_head elements, of the query rows of an item and the next
-    float vmax[PARTS][4];            // largest of V's scales of a unit, by part and warp
     int64_t scratch[32];
     int64_t sums[1];                 // [n_seqs + 1]
 };
@@ -478,7 +477,6 @@ __global__ void __launch_bounds__(THREADS, 1) k_attn_kv4_tc(const __grid_constan
         // `neg`: less what a row's scores are taken against, its reference, or 0 while it has none (its bit 2 j + e of `none`)
         float2 l[NB], ms[NB], neg[NB];
         uint32_t none = 0u;
-        float vmul = 0x1p24f;                                             // 2^-e of V's scales
         // Pass n finishes item n - 1 and begins item n: its queries are in place, and its first scores on the way, before the sums of
         // the one before go out.  (Shared words are double: a warp that is still writing sums out meets others in the next item.)
 #pragma unroll 1
@@ -556,7 +554,6 @@ __global__ void __launch_bounds__(THREADS, 1) k_attn_kv4_tc(const __grid_constan
             const int64_t c0 = kv4_cta_of(last.first, per), c1 = kv4_cta_of(last.first + last.chunks - 1, per);
             const bool whole = c0 == c1;
             float* slot = p.part + ((size_t)blockIdx.x * 2 + ((int64_t)blockIdx.x == c0 ? 1 : 0)) * ((size_t)N * (D + 2));
-            const float vinv = 1.f / vmul;                                // (of this part's rows: the same in its four warps)
             // lane m of the accumulator is channel (m & ~7) | {0 4 1 5 2 6 3 7}[m & 7]; a row's channels of this quarter are one store of the warp
             const int chn = quad * 32 + ((lane & ~7) | ((lane & 1) * 4) | ((lane & 7) >> 1));
             if (quad * 32 < D) {
@@ -575,12 +572,12 @@ __global__ void __launch_bounds__(THREADS, 1) k_attn_kv4_tc(const __grid_constan
                         __half* out = (__half*)p.out + chn;
 #pragma unroll
                         for (int x = 0; x < 8; ++x)
-                            if (x < left) out[(size_t)ix[x] * D] = __float2half_rn(fmaf(__uint_as_float(o[x]), vinv, tm[x].z) * tm[x].y);
+                            if (x < left) out[(size_t)ix[x] * D] = __float2half_rn((__uint_as_float(o[x]) + tm[x].z) * tm[x].y);
                     } else {
                         float* out = slot + r0 * D + chn;
 #pragma unroll
                         for (int x = 0; x < 8; ++x)
-                            if (x < left) __stcg(out + x * D, fmaf(__uint_as_float(o[x]), vinv, tm[x].z));
+                            if (x < left) __stcg(out + x * D, __uint_as_float(o[x]) + tm[x].z);
                     }
                 }
             }
@@ -599,7 +596,6 @@ __global__ void __launch_bounds__(THREADS, 1) k_attn_kv4_tc(const __grid_constan
             }
             if (!go) break;
             none = 0u;                                                    // (no bits for blocks without rows)
-            vmul = 0x1p24f;
 #pragma unroll
             for (int j = 0; j < NB; ++j) {
                 l[j] = ms[j] = neg[j] = make_float2(0.f, 0.f);
@@ -627,11 +623,12 @@ __global__ void __launch_bounds__(THREADS, 1) k_attn_kv4_tc(const __grid_constan
 #pragma unroll 1
             for (int k = 0; k < it.take; ++k, ++i) {
                 const int b = i & 1, key0 = (it.chunk0 + k) * UNIT + quad * 32 + g;
-                float ks[4], km[4], vs[4], vm[4];
+                float ks[4], km[4], vs[4], vm[4], lv[4];                  // (lv: what V's scale adds to a product)
 #pragma unroll
                 for (int x = 0; x < 4; ++x) {
                     const float4 f = sm->par[i & (PAR_SLOTS - 1)][quad * 32 + g + 8 * x];
                     ks[x] = f.x; km[x] = f.y; vs[x] = f.z; vm[x] = f.w;
+                    lv[x] = scale_bits(f.z);
                 }
                 const uint32_t groups = *reinterpret_cast<const uint32_t*>(sm->groups[i & (GROUP_SLOTS - 1)]);
                 const bool all = (it.chunk0 + k + 1) * UNIT <= it.q.len && groups == 0x03030303u;      // every key of the unit is visible to every row
@@ -647,7 +644,8 @@ __global__ void __launch_bounds__(THREADS, 1) k_attn_kv4_tc(const __grid_constan
                         const float2 v = fma2(both(ks[x]), dot, fma2(both(km[x]), qq, neg[j]));
                         sc[j][x][0] = v.x;
                         sc[j][x][1] = v.y;
-                        tj = fmaxf(tj, fmaxf(sc[j][x][0], sc[j][x][1]));
+                        const float2 pr = add2(v, both(lv[x]));
+                        tj = fmaxf(tj, fmaxf(pr.x, pr.y));
                     }
                     if (col8(j) < cols) top = fmaxf(top, tj);             // (blocks behind the tile's rows hold anything)
                 }
@@ -660,9 +658,6 @@ __global__ void __launch_bounds__(THREADS, 1) k_attn_kv4_tc(const __grid_constan
                     vis = 0u;
                     over = k == 0;
 #pragma unroll
-                    for (int x = 0; x < 4; ++x)                           // what lies behind the rows has no say in the exponent
-                        if (key0 + 8 * x >= it.keys || !((groups >> (8 * quad + (x >> 1))) & 1u)) vs[x] = 0.f;
-#pragma unroll
                     for (int j = 0; j < NB; ++j)
 #pragma unroll
                         for (int e = 0; e < 2; ++e) {
@@ -672,40 +667,30 @@ __global__ void __launch_bounds__(THREADS, 1) k_attn_kv4_tc(const __grid_constan
                                 const bool ok = (w32 >> (8 * x)) & 1u;
                                 if (ok) vis |= 1u << (8 * j + 4 * e + x);
                                 else sc[j][x][e] = -INFINITY;
-                                over = over || (col8(j) < cols && sc[j][x][e] > ((none >> (2 * j + e)) & 1u ? -INFINITY : RAISE));
+                                over = over || (col8(j) < cols && sc[j][x][e] + lv[x] > ((none >> (2 * j + e)) & 1u ? -INFINITY : RAISE));
                             }
                         }
                 }
-                over = over || fmaxf(fmaxf(vs[0], vs[1]), fmaxf(vs[2], vs[3])) * vmul > 128.f;
-                // Where one of the 128 threads of these rows finds a score too far above (and in an item's first unit), they agree
+                // Where one of the 128 threads of these rows finds a product too far above (and in an item's first unit), they agree
                 // on new references.
                 if (__builtin_expect(part_any(part, over), 0)) {
 #pragma unroll
                     for (int j = 0; j < NB; ++j)
 #pragma unroll
                         for (int e = 0; e < 2; ++e) {
-                            float m = fmaxf(fmaxf(sc[j][0][e], sc[j][1][e]), fmaxf(sc[j][2][e], sc[j][3][e]));
+                            float m = fmaxf(fmaxf(sc[j][0][e] + lv[0], sc[j][1][e] + lv[1]), fmaxf(sc[j][2][e] + lv[2], sc[j][3][e] + lv[3]));
 #pragma unroll
                             for (int sh = 4; sh < 32; sh <<= 1) m = fmaxf(m, __shfl_xor_sync(0xffffffffu, m, sh));
                             if (g == 0) sm->x[quad][col8(j) + 2 * t + e] = m;
                         }
-                    float vx = 0.f;
-#pragma unroll
-                    for (int x = 0; x < 4; ++x) if (vs[x] <= 65504.f) vx = fmaxf(vx, vs[x]);
-#pragma unroll
-                    for (int sh = 4; sh < 32; sh <<= 1) vx = fmaxf(vx, __shfl_xor_sync(0xffffffffu, vx, sh));
-                    if (lane == 0) sm->vmax[part][quad] = vx;
                     part_sync(part);
-                    vx = fmaxf(fmaxf(sm->vmax[part][0], sm->vmax[part][1]), fmaxf(sm->vmax[part][2], sm->vmax[part][3]));
-                    const float vnew = vx * vmul > 1.f ? exp2f(-ceilf(log2f(vx))) : vmul, fv = vnew / vmul;
-                    vmul = vnew;
 #pragma unroll
                     for (int j = 0; j < NB; ++j)
 #pragma unroll
                         for (int e = 0; e < 2; ++e) {
                             const int rl = col8(j) + 2 * t + e;
                             const bool had = !((none >> (2 * j + e)) & 1u);
-                            const float up = fmaxf(fmaxf(sm->x[0][rl], sm->x[1][rl]), fmaxf(sm->x[2][rl], sm->x[3][rl]));
+                            const float up = fmaxf(fmaxf(sm->x[0][rl], sm->x[1][rl]), fmaxf(sm->x[2][rl], sm->x[3][rl])) - TOP;
                             float f = 1.f;
                             if (up > (had ? 0.f : -INFINITY)) {           // the new reference is `up` above the base
                                 f = had ? ex2(-up) : 0.f;
@@ -716,7 +701,7 @@ __global__ void __launch_bounds__(THREADS, 1) k_attn_kv4_tc(const __grid_constan
 #pragma unroll
                                 for (int x = 0; x < 4; ++x) sc[j][x][e] -= up;
                             }
-                            if (quad == 0 && g == 0) sm->fac[rl] = f * fv;
+                            if (quad == 0 && g == 0) sm->fac[rl] = f;
                         }
                     part_sync(part);
                     if (k > 0) {
@@ -747,8 +732,6 @@ __global__ void __launch_bounds__(THREADS, 1) k_attn_kv4_tc(const __grid_constan
                 const bool more = k + 1 < it.take;
                 if (more) fetch(i + 1);
                 if (i >= 2) wait(smem_u32(&sm->p_empty[b]), ((i >> 1) - 1) & 1, looks, w.status, DEV_TIMEOUT_EPI);
-#pragma unroll
-                for (int x = 0; x < 4; ++x) vs[x] *= vmul;
                 // (one straight run of instructions for the units that matter, where nothing is masked and every block has rows)
                 auto weights = [&](auto plain) {
                     constexpr bool PLAIN = decltype(plain)::value;

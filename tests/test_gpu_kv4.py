@@ -1222,3 +1222,41 @@ def test_float_queries_are_rotated_in_64_bits_and_rounded_once(ghd, H, Hk, d, n)
     amp = np.abs(q.astype(np.float64))
     amp = amp + np.concatenate([amp[..., d // 2:], amp[..., : d // 2]], -1)
     assert (np.abs(got - want) <= 2.0 ** -24 * np.abs(want) + 2.0 ** -32 * amp).all()
+
+
+@pytest.mark.parametrize("own", [False, True], ids=["by nobody", "by themselves"])
+@pytest.mark.parametrize("path,H,Hk,n", [(1, 2, 2, 5), (1, 4, 2, 9), (2, 2, 2, 40), (2, 4, 2, 33)])
+def test_values_of_keys_that_a_row_does_not_see_cost_it_no_precision(ghd, path, H, Hk, n, own):
+    """New rows 1 and n - 2 are seen by no row, or by themselves alone, and have the largest values there are; all others are near
+    0.001.  All scores are equal, so the bound is that of the weights alone: 2^-11 for the weight times scale, 2^-18 for the exponential
+    and 32-bit sums of fewer than 128 terms, against codes of at most 8; output half a step of half, 2^-25 below the normal range."""
+    d, L = 128, 60
+    big = (1, n - 2)
+    su = Setup(ghd, H, Hk, d, "f16", 32, [L], [n], 21, garbage=False)
+    on_path(ghd, su.ctx, path)
+    part = middle = 0.0
+    for t in range(L + n):
+        page, row = okv4.slots(su.table, 32, 0, t)
+        for h in range(Hk):
+            c, s, m = okv4.quantise((su.r.randn(d) * (25000.0 if t - L in big else 1e-3)).clip(-65000, 65000).astype(np.float32), "f16")
+            su.pool.put(1, page, row, h, c, s, m)
+            if t - L not in big:
+                part, middle = max(part, 8 * float(s)), max(middle, abs(float(m) + 8 * float(s)))
+    su.dpool.copy_(dev(su.pool.data.reshape(-1)))
+    vis = [np.ones((n, n), bool)]
+    for i in big:
+        vis[0][:, i] = False
+        vis[0][i, i] = own
+    mask = np.zeros((n, 64), np.uint8)
+    mask[:, :n] = vis[0]
+    words = np.packbits(mask, axis=1, bitorder="little").view(np.int64)
+    q = np.zeros((n, H, d), np.float16)
+    out = ghd.ghd_kv4_attention(su.ctx, su.kv, ghd.Kv4Rows(dev(su.start), n, mask=dev(words)), su.dpool, dev(q.reshape(n, -1)))
+    ghd.ghd_sync_status(su.ctx)
+    got = out.double().cpu().numpy().reshape(n, H, d)
+    want = okv4.attention(su.pool, su.table, su.lens, su.start, vis, q)
+    tol = part * (2.0 ** -11 + 2.0 ** -15) + middle * 2.0 ** -15 + np.maximum(2.0 ** -11 * np.abs(want), 2.0 ** -25)
+    small = np.ones(n, bool)
+    small[list(big)] = not own
+    assert (np.abs(got - want) <= tol)[small].all(), float((np.abs(got - want) / tol)[small].max())
+    assert np.isfinite(got).all() and (small.all() or (np.abs(got - want) <= 2.0 ** -9 * np.abs(want).max())[~small].all())
