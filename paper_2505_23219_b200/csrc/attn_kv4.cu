@@ -22,11 +22,10 @@
 // a run's border leaves partial sums; the last of its CTAs to arrive adds them in CTA order (the result does not
 // depend on who was last).  Float contexts split q and p * scale into three bfloat16 terms (24 bits).
 //
-// What it costs.  One token over 2048 rows of 32 heads (8.9 MB): 11.6 us, a chain of latencies (in clocks, of 21000: lengths and prefix
+// What it costs.  One token over 2048 rows of 32 heads (8.9 MB): 11.5 us, a chain of latencies (in clocks, of 21000: lengths and prefix
 // sums 2300, item 2000, page ids and first rows 2200, queries 1200, two chunks 4000, sums 1500, arrival 2000, merge 2500); over 16384 rows
 // 27 us, 2.6 TB/s.  One token each of 32 ragged sequences of up to 8192 rows, 32 heads on 8 (174.5 MB): 54 us, 3.2 TB/s.  That is
-// instructions: 710 a warp for 32 keys, all included (9 for a word of eight codes, 32 words a lane; the products are 32; V's power of two
-// 30), 2.2 an SM a clock out of 12 warps (161 registers a thread).  Four CTAs an SM spill, deeper rings take CTAs away.
+// instructions: 700 a warp for 32 keys, all included (9 for a word of eight codes, 32 words a lane; the products are 32), 2.2 an SM a clock out of 12 warps (161 registers a thread).  Four CTAs an SM spill, deeper rings take CTAs away.
 //
 // Rounding.  Scores, exponentials (ex2.approx: 2 units of 2^-23), weights, sums and the middles' sums are 32 bits.  Half: the weight
 // times scale has 11 bits in the second product, so that a key costs one product and not two; it adds about 1e-4 of the output's size
@@ -43,7 +42,7 @@ namespace ghd {
 namespace {
 
 constexpr int WARPS = 4, WKEYS = 32, CHUNK = WKEYS * WARPS;      // a warp takes 32 keys of every chunk
-constexpr int LEAD = 4;          // an item's fixed cost in chunks (one token of 32 heads over 2048 and 16384 rows: 2: 11.3 and 28.9 us, 3: 11.3 and 28.3, 4: 11.6 and 27.3)
+constexpr int LEAD = 4;          // an item's fixed cost in chunks (one token of 32 heads over 2048 and 16384 rows: 2: 11.1 and 28.8 us, 3: 11.0 and 28.0, 4: 11.5 and 27.1)
 
 using namespace kv4;
 
@@ -129,7 +128,7 @@ struct Narrow {
     static constexpr int ES = (int)sizeof(T), ROW = D / 2;     // bytes of a scale, of a packed row
     // a warp's stage: K rows, V rows, K and V (scale, min) of 32 keys, and which of the two groups of 16 have a page
     static constexpr int V_AT = WKEYS * ROW, P_AT = 2 * WKEYS * ROW, VP_AT = P_AT + 2 * WKEYS * ES, FLAG_AT = VP_AT + 2 * WKEYS * ES, STAGE = FLAG_AT + 16;
-    static constexpr int STAGES = 2;                           // (32 ragged sequences: 54 us; three stages 55, four 81: fewer CTAs fit)
+    static constexpr int STAGES = 2;                           // (32 ragged sequences: 54 us; three stages 56, four 81: fewer CTAs fit)
     static constexpr int XO = D + 4;                           // floats between rows of the exchange buffer
     static constexpr int SMEM = WARPS * STAGES * STAGE + WARPS * RT * (XO + 3) * 4 + WARPS * (D + 2) * 4;
     static constexpr int BLOCKS = NT == 1 && sizeof(T) == 2 ? (D == 64 ? 4 : 3) : 2;      // CTAs an SM
@@ -571,12 +570,12 @@ ghd_status launch_attn_kv4(ghd_ctx* c, const Kv4View& w, const ghd_kv4_rows* row
         return m.d_head == 64 ? launch_narrow<float, 64, 1>(c, p) : launch_narrow<float, 128, 1>(c, p);
     }
     // The tcgen05 kernel for tiles of many rows.  Up to 32 rows two tiles of this file's kernel start sooner and cost a key as much (8
-    // sequences, 32 heads, 32 rows over 0 / 512 / 2048 / 8192 keys: 19 / 30 / 57 / 102 us here, 21 / 30 / 54 / 103 there).  Up to 64 rows
-    // they do while its tiles leave half of the SMs free (32 tiles over 256 / 2048 keys: 15 / 19 us here, 18 / 25 there; but 128 tiles over
-    // 1024 / 4096: 24 / 41 here, 23 / 33 there).  128 rows, 32 heads over 512 / 1024 / 2048 keys: 27 / 35 / 47 here, 24 / 27 / 34 there.
+    // sequences, 32 heads, 32 rows over 0 / 512 / 2048 / 8192 keys: 18 / 28 / 54 / 97 us here, 20 / 31 / 54 / 104 there).  Up to 64 rows
+    // they do while its tiles leave half of the SMs free (32 tiles over 256 / 2048 keys: 15 / 18 us here, 18 / 25 there; but 128 tiles over
+    // 1024 / 4096: 23 / 38 here, 22 / 33 there).  128 rows, 32 heads over 512 / 1024 / 2048 keys: 26 / 32 / 43 here, 24 / 27 / 34 there.
     // The rows of a sequence are known on the device alone, so all rules go by the average, rows behind the last sequence included.  Where
     // sequences are unlike, one call takes longer than one for each kind (32 heads on 8: a tree of 256 nodes beside 63 tokens over up to
-    // 4096 rows 201 us, apart 73 + 57; a prompt of 2048 rows beside 31 tokens 349, apart 258 + 32).
+    // 4096 rows 190 us, apart 74 + 56; a prompt of 2048 rows beside 31 tokens 353, apart 260 + 32).
     const int64_t tiles = (avg + 15) / 16 * w.heads * w.n_seqs;
     if (c->opt_attn_path == 2 || (c->opt_attn_path == 0 && avg > 32 && (avg > 64 || 2 * tiles > c->sm_count))) return launch_attn_kv4_tc(c, p);
     if (m.d_head == 64) return avg <= 8 ? launch_narrow<__half, 64, 1>(c, p) : launch_narrow<__half, 64, 2>(c, p);

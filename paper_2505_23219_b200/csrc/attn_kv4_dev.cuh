@@ -146,7 +146,7 @@ __device__ __forceinline__ int arrive_at(int* counter) {
 
 // Adds the partial sums that CTAs c0 .. c1 left of one item, in that order, and writes its rows.  A warp takes RB rows at a
 // time (the lanes hold D / 32 channels each) and KB contributors of each: what the merge costs is the latency of its loads
-// and, in short calls, the fetch of its instructions (KB = 16 for RB = 1: 12.0 us instead of 11.6 for one token).  With few rows several warps share the contributors and meet in `xch`,
+// and, in short calls, the fetch of its instructions (KB = 16 for RB = 1: 11.8 us instead of 11.5 for one token).  With few rows several warps share the contributors and meet in `xch`,
 // floats [warps][D + 2].  `sync` is a barrier of the NW warps that take part.
 template <typename T, int D, int RB, typename Sync>
 __device__ __forceinline__ void merge_item(const Kv4AttnParams& p, const Kv4Item& it, int tile_rows, int rows, int64_t c0, int64_t c1, int warp, int nw, float* xch, Sync sync) {
