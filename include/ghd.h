@@ -360,6 +360,83 @@ ghd_status ghd_kv4_read(ghd_ctx *ctx, const ghd_kv4 *kv, const ghd_kv4_rows *row
 ghd_status ghd_kv4_commit(ghd_ctx *ctx, const ghd_kv4 *kv, const ghd_kv4_rows *rows, void *const *pools, int32_t n_layers,
                           const ghd_accept_result *results_dev);
 
+/* ---- Matrices in microscaled 4-bit floating point --------------------------------------------------------------------
+ * (Paper Sec. I / II-A: a decode step loads every weight once and is bound by that; with 17 bits for four weights it loads
+ * 27 % of the bytes.)
+ *
+ * 32 elements along k share a scale 2^E; an element is a sign and one of 0, 0.5, 1, 1.5, 2, 3, 4, 6 (two bits of exponent, one of
+ * mantissa) times it.  Quantising: E = floor(log2(largest magnitude)) - 2, at least -127, and x / 2^E rounded to the nearest of these
+ * (ties to the even code) and held within +-6.  32 elements with a NaN or an infinity among them are NaN throughout.
+ * A matrix [m][k] lies in tiles of 128 x 128, m and k rounded up; with kt = ceil(k / 128) tile (i, j) is number i * kt + j:
+ *   codes:  dev bytes [tiles][128 rows][64], 32-byte aligned; element 2b of a row in the low half of byte b, 2b + 1 in the high half;
+ *           a code is the sign in bit 3 over the number of the magnitude in the list above;
+ *   scales: dev bytes [tiles][512], 16-byte aligned: E + 127 of row r, elements 32 q .. 32 q + 31 at (r mod 32) * 16 + (r / 32) * 4 + q;
+ *           255 stands for NaN.
+ * Elements past m and k have code 0; ghd_mx4_quantize writes them (with scale byte 0).  At most 2^20 rows, 2^20 columns, 2^34 elements. */
+typedef struct ghd_mx4 {
+    int32_t m, k;
+    void *codes, *scales;
+} ghd_mx4;
+
+/* Bytes of the two buffers (0 for sizes that the calls refuse). */
+size_t ghd_mx4_code_bytes(int32_t m, int32_t k);
+size_t ghd_mx4_scale_bytes(int32_t m, int32_t k);
+
+/* x: dev T [m][k], rows ld elements apart (0: contiguous), any alignment of T -> w's codes and scales. */
+ghd_status ghd_mx4_quantize(ghd_ctx *ctx, const void *x, int64_t ld, const ghd_mx4 *w);
+/* The values that w stands for, rounded once to T: out dev T [m][k], rows ld elements apart (0: contiguous). */
+ghd_status ghd_mx4_read(ghd_ctx *ctx, const ghd_mx4 *w, void *out, int64_t ld);
+
+/* ghd_linear with such a matrix: y float [n][m] = x T [n][k] * w[m][k]^T, x's rows x_ld elements apart (0: contiguous).
+ * 1 <= n <= max_nodes, k at most the larger of d_model and d_ffn (GHD_ENOSPACE). */
+ghd_status ghd_mx4_linear(ghd_ctx *ctx, const void *x, int64_t x_ld, const ghd_mx4 *w, int32_t n, float *y);
+/* ghd_gate_up with two: u T [n][m] = SiLU(h Wg^T) * (h Wu^T), both [m][k]; h dev T [n][k], rows h_ld elements apart (0: contiguous). */
+ghd_status ghd_mx4_gate_up(ghd_ctx *ctx, const void *h, int64_t h_ld, const ghd_mx4 *w_gate, const ghd_mx4 *w_up, int32_t n, void *u);
+
+/* ---- Drafting and verifying by sampling --------------------------------------------------------------------------------
+ * (Paper Sec. II-C: drafts are verified against what the target model would have said.  ghd_accept does so for its most likely token;
+ * these calls for tokens drawn from its distribution, which they leave exactly as it is whatever the drafter.)
+ * The distribution of a row of logits (float [cfg.vocab]) is softmax(logits / temperature); -inf leaves a token out (top-k or
+ * nucleus filters are such logits).  Random numbers are the caller's, float in [0, 1) (others are held to that); weights and sums are
+ * worked out in 64 bits.  A row with a NaN or +inf, or with nothing but -inf, is none: ghd_sync_status -> GHD_EINVAL. */
+
+/* Candidates: for each of n_rows rows of logits (the heads of one sequence, or of many) n_draws tokens drawn without replacement.
+ * Draw j is the first token t whose running sum of the weights not drawn yet exceeds uniforms[row][j] times their total; -1 once nothing
+ * is left, in a row without a distribution, and from n_draws on.  uniforms: dev float [n_rows][GHD_MAX_TOPK], cand: dev int32
+ * [n_rows][GHD_MAX_TOPK] (as ghd_medusa_draft leaves them), 1 <= n_draws <= GHD_MAX_TOPK. */
+ghd_status ghd_draft_sample(ghd_ctx *ctx, const float *logits, int32_t n_rows, float temperature, int32_t n_draws, const float *uniforms,
+                            int32_t *cand);
+
+/* The trees of n_seqs sequences behind one another: sequence s has rows row_start[s] .. row_start[s + 1] - 1, at most GHD_MAX_NODES;
+ * its row 0 is the root.  All dev pointers. */
+typedef struct ghd_sampled {
+    int32_t n_seqs;                 /* 1 .. GHD_MAX_SEQS                                                       */
+    int32_t n_rows;                 /* rows of the buffers                                                    */
+    const int32_t *row_start;       /* [n_seqs + 1], not falling; NULL: one sequence of n_rows rows           */
+    const int32_t *parent;          /* [n_rows]: number in the sequence, below the row's own; -1 for the root */
+    const int32_t *tokens;          /* [n_rows] drafted tokens; a child whose token is outside [0, vocab) is passed over */
+    const float *logits;            /* [n_rows][vocab] of the target model                                    */
+    const float *uniforms;          /* [n_rows]: of a child its test's, of the root the last token's          */
+    const int32_t *draft_row;       /* [n_rows]: row of draft_logits that the children of a row were drawn from, -1: they were not drawn; NULL: none was */
+    const float *draft_logits;      /* [n_draft][vocab], NULL with draft_row                                   */
+    int32_t n_draft;
+    float temperature, draft_temperature;
+} ghd_sampled;
+
+/* Verification.  From the root on, with P the distribution of the node and Q that of its draft row, the node's children are tested in
+ * the order of their rows, which is that of their draws from Q without replacement:
+ *   x is accepted if u Q(x) < P(x); otherwise P becomes max(P - Q, 0) over its sum, and Q becomes Q without x over its sum.
+ *   A token that Q does not hold (any more) is passed over.  Children that were not drawn are accepted if u < P(x); otherwise P
+ *   becomes P without x over its sum.
+ * The walk goes on from the first accepted child.  Where there is none, the last token is the first one whose running sum of P exceeds
+ * the root's random number times the total.  Tokens so emitted are distributed as if drawn from the target one by one.
+ * results_dev[s] as ghd_accept's: nodes the accepted path, tokens[j] the token of nodes[j + 1], tokens[n_matched] the one drawn last
+ * (0 at a node without a distribution); entries behind these are -1.  A sequence without rows gets n_emitted 0 and no nodes.
+ * Starts out of order, more than GHD_MAX_NODES rows (such a sequence is taken as empty) or a parent that is none (the row is passed
+ * over): ghd_sync_status -> GHD_ETREE; a draft row from n_draft on (taken as -1): GHD_EINVAL.  At a node whose draft row has no distribution no
+ * child is accepted. */
+ghd_status ghd_accept_sampled(ghd_ctx *ctx, const ghd_sampled *rows, ghd_accept_result *results_dev);
+
 /* Building blocks of the layer, exposed for unit tests (same kernels the layer uses).
  * ghd_linear: y float [n][m] = x T[n][k] * w T[m][k]^T.
  * ghd_gate_up: u T [n][d_ffn] = SiLU(h Wg^T) * (h Wu^T) for h T [n][d_model], w_gate_up T [2*d_ffn][d_model]
@@ -400,7 +477,7 @@ ghd_status ghd_tree_attention_static(void *cuda_stream, int32_t dtype, int32_t n
 /* Synchronises the stream and returns GHD_OK, GHD_ECUDA (with the CUDA error kept
  * for ghd_last_error), GHD_ETIMEOUT when a kernel's bounded wait expired (what the kernels
  * left half done in the workspace is cleared), or else what they found wrong with lengths,
- * rows or pages on the device (GHD_ENOSPACE, GHD_EINVAL).  Reported once. */
+ * rows, pages, trees or logits on the device (GHD_ENOSPACE, GHD_EINVAL, GHD_ETREE).  Reported once. */
 ghd_status ghd_sync_status(ghd_ctx *ctx);
 const char *ghd_status_str(ghd_status s);
 const char *ghd_last_error(const ghd_ctx *ctx);

@@ -20,6 +20,8 @@ __all__ = [
     "ghd_verify_step", "ghd_accept", "ghd_linear", "ghd_rmsnorm", "ghd_tree_attention", "ghd_argmax",
     "ghd_sync_status", "ghd_launch_count", "pack_mask", "ghd_copy_hidden", "ghd_gate_up", "ghd_tree_attention_static", "ghd_path_count", "ghd_kv_commit", "ghd_medusa_draft", "ghd_tree_fill_tokens",
     "Kv4Cache", "Kv4Rows", "ghd_kv4_pool_bytes", "ghd_kv4_pool", "ghd_kv4_append", "ghd_kv4_attention", "ghd_kv4_read", "ghd_kv4_commit", "GHD_MAX_SEQS",
+    "Mx4", "ghd_mx4", "ghd_mx4_quantize", "ghd_mx4_read", "ghd_mx4_linear", "ghd_mx4_gate_up", "ghd_mx4_code_bytes", "ghd_mx4_scale_bytes",
+    "SampledRows", "ghd_draft_sample", "ghd_accept_sampled",
     "ghd_kv_len_set", "ghd_kv_len_get", "KV_LEN_DEVICE", "MedusaWeights", "GHD_MAX_TOPK",
     "PATH_GEMM_TILE", "PATH_GEMM_SIMT", "PATH_ATTN_TC", "PATH_ATTN_SIMT", "PATH_ATTN_COO", "PATH_GEMM_PAIR", "PATH_KV4_ROWS", "PATH_KV4_TC", "OPT_GEMM_PAIR", "OPT_ATTN_ROWS", "OPT_GEMM_SKEW", "OPT_ATTN_SMALL",
     "GHD_F32", "GHD_F16", "GHD_MAX_NODES", "OPT_GEMM_PATH", "OPT_ATTN_SPLITS", "OPT_ATTN_PATH", "OPT_GRAPH",
@@ -47,6 +49,8 @@ EXPORTS = [
     "ghd_tree_attention_static", "ghd_path_count", "ghd_kv_commit", "ghd_kv_len_set", "ghd_kv_len_get",
     "ghd_medusa_draft", "ghd_tree_fill_tokens", "ghd_copy_hidden", "ghd_gate_up",
     "ghd_kv4_pool_bytes", "ghd_kv4_append", "ghd_kv4_attention", "ghd_kv4_read", "ghd_kv4_commit",
+    "ghd_mx4_code_bytes", "ghd_mx4_scale_bytes", "ghd_mx4_quantize", "ghd_mx4_read", "ghd_mx4_linear", "ghd_mx4_gate_up",
+    "ghd_draft_sample", "ghd_accept_sampled",
 ]
 
 
@@ -95,6 +99,16 @@ class _Kv4Rows(C.Structure):
     _fields_ = [("n_rows", C.c_int32), ("mask_words", C.c_int32), ("row_start", C.c_void_p), ("pos", C.c_void_p), ("mask", C.c_void_p)]
 
 
+class _Mx4(C.Structure):
+    _fields_ = [("m", C.c_int32), ("k", C.c_int32), ("codes", C.c_void_p), ("scales", C.c_void_p)]
+
+
+class _Sampled(C.Structure):
+    _fields_ = [("n_seqs", C.c_int32), ("n_rows", C.c_int32)] + \
+               [(k, C.c_void_p) for k in ("row_start", "parent", "tokens", "logits", "uniforms", "draft_row", "draft_logits")] + \
+               [("n_draft", C.c_int32), ("temperature", C.c_float), ("draft_temperature", C.c_float)]
+
+
 _LIB = None
 
 
@@ -137,6 +151,14 @@ def load_library(path: str | Path | None = None):
         "ghd_kv4_attention": ([vp, C.POINTER(_Kv4), C.POINTER(_Kv4Rows), vp, vp, vp], C.c_int),
         "ghd_kv4_read": ([vp, C.POINTER(_Kv4), C.POINTER(_Kv4Rows), vp, vp, vp, vp], C.c_int),
         "ghd_kv4_commit": ([vp, C.POINTER(_Kv4), C.POINTER(_Kv4Rows), vp, i32, vp], C.c_int),
+        "ghd_mx4_code_bytes": ([i32, i32], C.c_size_t),
+        "ghd_mx4_scale_bytes": ([i32, i32], C.c_size_t),
+        "ghd_mx4_quantize": ([vp, vp, C.c_int64, C.POINTER(_Mx4)], C.c_int),
+        "ghd_mx4_read": ([vp, C.POINTER(_Mx4), vp, C.c_int64], C.c_int),
+        "ghd_mx4_linear": ([vp, vp, C.c_int64, C.POINTER(_Mx4), i32, vp], C.c_int),
+        "ghd_mx4_gate_up": ([vp, vp, C.c_int64, C.POINTER(_Mx4), C.POINTER(_Mx4), i32, vp], C.c_int),
+        "ghd_draft_sample": ([vp, vp, i32, C.c_float, i32, vp, vp], C.c_int),
+        "ghd_accept_sampled": ([vp, C.POINTER(_Sampled), vp], C.c_int),
         "ghd_sync_status": ([vp], C.c_int),
         "ghd_status_str": ([C.c_int], C.c_char_p),
         "ghd_last_error": ([vp], C.c_char_p),
@@ -257,6 +279,55 @@ class Kv4Rows(_Description):
         own = self.__dict__
         own["row_start"], own["n_rows"], own["pos"], own["mask"] = row_start, n_rows, pos, mask
         own["n_starts"], own["dev"], own["c"], own["ref"] = row_start.numel(), dev, c, C.byref(c)
+
+
+class Mx4(_Description):
+    """A matrix [m][k] in microscaled 4-bit floating point: uint8 device tensors with its codes and scales (any shape with the bytes that
+    ghd_mx4_code_bytes and ghd_mx4_scale_bytes give; ghd_mx4 makes them)."""
+
+    def __init__(self, codes, scales, m: int, k: int):
+        if not (0 < m < _INT and 0 < k < _INT):
+            raise GhdError(1, f"mx4: m {m} or k {k} is outside [1, 2^31)")
+        lib = load_library()
+        nc, ns = lib.ghd_mx4_code_bytes(m, k), lib.ghd_mx4_scale_bytes(m, k)
+        if not nc:
+            raise GhdError(2, f"mx4: a matrix of {m} x {k}")
+        c = _Mx4(m, k, _need(codes, torch.uint8, "codes", nc), _need(scales, torch.uint8, "scales", ns, codes.get_device()))
+        own = self.__dict__
+        own["codes"], own["scales"], own["m"], own["k"], own["dev"], own["c"], own["ref"] = codes, scales, m, k, codes.get_device(), c, C.byref(c)
+
+
+class SampledRows(_Description):
+    """The drafted trees of n_seqs sequences with their target logits: parent, tokens int32 [n_rows], logits float [n_rows][vocab], uniforms
+    float [n_rows]; row_start int32 [n_seqs + 1] (None: one sequence); where candidates were drawn, draft_row int32 [n_rows] and
+    draft_logits float [n_draft][vocab] (device tensors, whose contents may change)."""
+
+    def __init__(self, parent, tokens, logits, uniforms, row_start=None, temperature: float = 1.0, draft_row=None, draft_logits=None,
+                 draft_temperature: float = 1.0):
+        if parent.dim() != 1 or logits.dim() != 2 or logits.shape[0] < parent.shape[0]:
+            raise GhdError(1, "sampled: parent is not [n_rows], or logits not [n_rows][vocab]")
+        n, (_, vocab) = parent.shape[0], logits.shape
+        at = _need(parent, torch.int32, "parent", 0)
+        dev = parent.get_device()
+        if (draft_row is None) != (draft_logits is None):
+            raise GhdError(1, "sampled: give both draft_row and draft_logits or neither")
+        n_draft = 0
+        if draft_row is not None:
+            if draft_logits.dim() != 2 or draft_logits.shape[1] != vocab:
+                raise GhdError(1, "sampled: draft_logits is not [n_draft][vocab]")
+            n_draft = draft_logits.shape[0]
+        n_seqs = 1 if row_start is None else row_start.numel() - 1
+        if not (n < _INT and n_seqs < _INT and n_draft < _INT):
+            raise GhdError(1, "sampled: more than 2^31 rows")
+        c = _Sampled(n_seqs, n, None if row_start is None else _need(row_start, torch.int32, "row_start", 2, dev), at,
+                     _need(tokens, torch.int32, "tokens", n, dev), _need(logits, torch.float32, "logits", n * vocab, dev),
+                     _need(uniforms, torch.float32, "uniforms", n, dev),
+                     None if draft_row is None else _need(draft_row, torch.int32, "draft_row", n, dev),
+                     None if draft_row is None else _need(draft_logits, torch.float32, "draft_logits", n_draft * vocab, dev),
+                     n_draft, temperature, draft_temperature)
+        own = self.__dict__
+        own["tensors"] = (parent, tokens, logits, uniforms, row_start, draft_row, draft_logits)
+        own["n_seqs"], own["vocab"], own["dev"], own["c"], own["ref"] = n_seqs, vocab, dev, c, C.byref(c)
 
 
 class Tree:
@@ -578,6 +649,114 @@ def ghd_kv4_commit(ctx: Ctx, kv: Kv4Cache, rows: Kv4Rows, pools, results=None):
     arr = (C.c_void_p * max(len(ptrs), 1))(*ptrs)
     ctx._check(ctx.lib.ghd_kv4_commit(ctx.handle, kv.ref, rows.ref, arr, len(ptrs),
                                       None if results is None else _need(results, torch.int32, "results", kv.n_seqs * (2 + 2 * GHD_MAX_NODES), ctx.dev)))
+
+
+def _make(ctx: Ctx, shape, dtype):
+    """An empty tensor for a result, made on the context's stream."""
+    if _kv4_here(ctx):
+        return torch.empty(shape, dtype=dtype, device=ctx.device)
+    return _kv4_there(ctx, torch.empty, shape, dtype=dtype, device=ctx.device)
+
+
+def ghd_mx4_code_bytes(m: int, k: int) -> int:
+    return int(load_library().ghd_mx4_code_bytes(m, k))
+
+
+def ghd_mx4_scale_bytes(m: int, k: int) -> int:
+    return int(load_library().ghd_mx4_scale_bytes(m, k))
+
+
+def ghd_mx4(ctx: Ctx, m: int, k: int) -> Mx4:
+    """Room for a matrix [m][k] (its contents are anything until ghd_mx4_quantize has run)."""
+    nc = ghd_mx4_code_bytes(m, k)
+    if not nc:
+        raise GhdError(2, f"mx4: a matrix of {m} x {k}")
+    return Mx4(_make(ctx, (nc,), torch.uint8), _make(ctx, (ghd_mx4_scale_bytes(m, k),), torch.uint8), m, k)
+
+
+def _mx4_here(ctx: Ctx, w: Mx4):
+    if w.dev != ctx.dev:
+        raise GhdError(1, f"mx4: a matrix on cuda:{w.dev}, the context is on cuda:{ctx.dev}")
+
+
+def _mx4_rows(ctx: Ctx, t, n: int, k: int, what: str):
+    """Rows of k elements, contiguous inside a row and apart from one another -> (pointer, row stride)."""
+    if t.dim() != 2 or t.shape[0] != n or t.shape[1] != k or (k > 1 and t.stride(1) != 1) or t.dtype != ctx.dtype or t.get_device() != ctx.dev:
+        raise GhdError(1, f"{what}: want {ctx.dtype} [{n}][{k}] with contiguous rows on cuda:{ctx.dev}, got {tuple(t.shape)} {t.dtype} on {t.device}")
+    if n > 1 and t.stride(0) < k:
+        raise GhdError(1, f"{what}: rows of {k} elements overlap (row stride {t.stride(0)})")
+    return t.data_ptr(), t.stride(0) if n > 1 else 0
+
+
+def ghd_mx4_quantize(ctx: Ctx, x, w: Mx4 | None = None) -> Mx4:
+    """x [m][k] (rows may be strided) in 4 bits, into w or a new one."""
+    if x.dim() != 2:
+        raise GhdError(1, "mx4_quantize: x is not [m][k]")
+    if w is None:
+        w = ghd_mx4(ctx, *x.shape)
+    _mx4_here(ctx, w)
+    at, ld = _mx4_rows(ctx, x, w.m, w.k, "x")
+    ctx._check(ctx.lib.ghd_mx4_quantize(ctx.handle, at, ld, w.ref))
+    return w
+
+
+def ghd_mx4_read(ctx: Ctx, w: Mx4, out=None):
+    """-> the values that w stands for, [m][k] (out's rows may be strided)."""
+    _mx4_here(ctx, w)
+    if out is None:
+        out = _make(ctx, (w.m, w.k), ctx.dtype)
+    at, ld = _mx4_rows(ctx, out, w.m, w.k, "out")
+    ctx._check(ctx.lib.ghd_mx4_read(ctx.handle, w.ref, at, ld))
+    return out
+
+
+def ghd_mx4_linear(ctx: Ctx, x, w: Mx4, y=None):
+    """y float [n][m] = x [n][k] (rows may be strided) w^T."""
+    _mx4_here(ctx, w)
+    n = x.shape[0]
+    at, ld = _mx4_rows(ctx, x, n, w.k, "x")
+    if y is None:
+        y = _make(ctx, (n, w.m), torch.float32)
+    ctx._check(ctx.lib.ghd_mx4_linear(ctx.handle, at, ld, w.ref, n, _need(y, torch.float32, "y", n * w.m, ctx.dev)))
+    return y
+
+
+def ghd_mx4_gate_up(ctx: Ctx, h, w_gate: Mx4, w_up: Mx4, u=None):
+    """u [n][m] = SiLU(h w_gate^T) * (h w_up^T) (h's rows may be strided)."""
+    _mx4_here(ctx, w_gate)
+    _mx4_here(ctx, w_up)
+    n = h.shape[0]
+    at, ld = _mx4_rows(ctx, h, n, w_gate.k, "h")
+    if u is None:
+        u = _make(ctx, (n, w_gate.m), ctx.dtype)
+    ctx._check(ctx.lib.ghd_mx4_gate_up(ctx.handle, at, ld, w_gate.ref, w_up.ref, n, _need(u, ctx.dtype, "u", n * w_gate.m, ctx.dev)))
+    return u
+
+
+def ghd_draft_sample(ctx: Ctx, logits, uniforms, n_draws: int, temperature: float = 1.0, cand=None):
+    """Tokens drawn without replacement from each row of logits float [n_rows][vocab] with uniforms float [n_rows][GHD_MAX_TOPK]
+    -> int32 [n_rows][GHD_MAX_TOPK], -1 from n_draws on."""
+    if logits.dim() != 2 or logits.shape[1] != ctx.cfg.c.vocab:
+        raise GhdError(1, f"draft_sample: logits are not [n_rows][{ctx.cfg.c.vocab}]")
+    n = logits.shape[0]
+    if not (n < _INT and -_INT <= n_draws < _INT):
+        raise GhdError(1, "draft_sample: n_rows or n_draws is outside 32 bits")
+    if cand is None:
+        cand = _make(ctx, (n, GHD_MAX_TOPK), torch.int32)
+    ctx._check(ctx.lib.ghd_draft_sample(ctx.handle, _need(logits, torch.float32, "logits", 0, ctx.dev), n, temperature, n_draws,
+                                        _need(uniforms, torch.float32, "uniforms", n * GHD_MAX_TOPK, ctx.dev),
+                                        _need(cand, torch.int32, "cand", n * GHD_MAX_TOPK, ctx.dev)))
+    return cand
+
+
+def ghd_accept_sampled(ctx: Ctx, rows: SampledRows, out=None):
+    """-> int32 [n_seqs][514], a ghd_accept_result for every sequence: [n_matched, n_emitted, nodes[256], tokens[256]]."""
+    if rows.dev != ctx.dev or rows.vocab != ctx.cfg.c.vocab:
+        raise GhdError(1, f"accept_sampled: {rows.vocab} logits a row on cuda:{rows.dev}, the context has {ctx.cfg.c.vocab} on cuda:{ctx.dev}")
+    if out is None:
+        out = _make(ctx, (rows.n_seqs, 2 + 2 * GHD_MAX_NODES), torch.int32)
+    ctx._check(ctx.lib.ghd_accept_sampled(ctx.handle, rows.ref, _need(out, torch.int32, "out", rows.n_seqs * (2 + 2 * GHD_MAX_NODES), ctx.dev)))
+    return out
 
 
 def ghd_linear(ctx: Ctx, x, w, y=None):

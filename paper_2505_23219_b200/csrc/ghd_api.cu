@@ -606,11 +606,19 @@ ghd_status ghd_sync_status(ghd_ctx* c) {
         return GHD_ETIMEOUT;
     }
     if (in != DEV_OK) {
-        snprintf(c->err, sizeof(c->err), in == DEV_KV_RANGE   ? "the cache length on the device left [0, max_kv_len - n]"
-                                         : in == DEV_KV4_ROWS ? "paged cache: a row beyond the page table, or a length or row start out of order"
-                                                              : "paged cache: a page id outside the pool");
+        const char* what = "paged cache: a page id outside the pool";
+        ghd_status code = GHD_EINVAL;
+        switch (in) {
+            case DEV_KV_RANGE: what = "the cache length on the device left [0, max_kv_len - n]"; code = GHD_ENOSPACE; break;
+            case DEV_KV4_ROWS: what = "paged cache: a row beyond the page table, or a length or row start out of order"; code = GHD_ENOSPACE; break;
+            case DEV_SAMPLE_TREE: what = "sampling: row starts out of order, more than 256 nodes, or a bad parent"; code = GHD_ETREE; break;
+            case DEV_SAMPLE_DRAFT: what = "sampling: a draft row from n_draft on"; break;
+            case DEV_SAMPLE_DIST: what = "sampling: a row of logits without a distribution (NaN, +inf, or nothing but -inf)"; break;
+            default: break;
+        }
+        snprintf(c->err, sizeof(c->err), "%s", what);
         cudaMemsetAsync(c->input_status, 0, sizeof(int), c->stream);
-        return in == DEV_KV4_PAGE ? GHD_EINVAL : GHD_ENOSPACE;
+        return code;
     }
     return GHD_OK;
 }

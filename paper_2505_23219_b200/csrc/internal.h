@@ -17,7 +17,7 @@ namespace ghd {
 // Values of the two device status words (in each the first failure wins).  status: a wait that ran out; input_status: device data
 // out of range, which the kernels skip and run on.  Apart, so that neither hides the other.
 enum : int { DEV_OK = 0, DEV_TIMEOUT_TMA = 1, DEV_TIMEOUT_MMA = 2, DEV_TIMEOUT_EPI = 3, DEV_TIMEOUT_TMEM = 4, DEV_TIMEOUT_GRID = 5 };
-enum : int { DEV_KV_RANGE = 6, DEV_KV4_ROWS = 7, DEV_KV4_PAGE = 8 };
+enum : int { DEV_KV_RANGE = 6, DEV_KV4_ROWS = 7, DEV_KV4_PAGE = 8, DEV_SAMPLE_TREE = 9, DEV_SAMPLE_DRAFT = 10, DEV_SAMPLE_DIST = 11 };
 
 // Epilogues of the projection GEMMs.
 enum Epilogue : int {

@@ -1,0 +1,307 @@
+"""Drafting and verifying by sampling on the GPU against the double-precision oracle (oracle/sampling.py)."""
+import math
+
+import numpy as np
+import pytest
+
+from oracle import sampling as osam
+
+pytestmark = pytest.mark.gpu
+
+
+@pytest.fixture(scope="module")
+def ghd():
+    import paper_2505_23219_b200 as g
+    return g
+
+
+_CTX = {}
+
+
+def ctx_for(ghd, vocab):
+    if vocab not in _CTX:
+        _CTX[vocab] = ghd.ghd_create(ghd.ModelCfg(512, 4, 128, 512, vocab, 1, 512, 16, "f16"))
+    return _CTX[vocab]
+
+
+def dev(a):
+    import torch
+    return torch.from_numpy(np.ascontiguousarray(a)).cuda()
+
+
+def logits_of(r, rows, vocab, strong=3.0):
+    x = r.randn(rows, vocab) * 1.5
+    k = max(1, min(20, vocab // 4))
+    for i in range(rows):
+        x[i, r.choice(vocab, k, replace=False)] += strong + 6 * r.rand(k)
+    return x.astype(np.float32)
+
+
+# ------------------------------------------------------------------ candidates
+@pytest.mark.parametrize("vocab", [1, 2, 31, 32, 33, 100, 1000, 4097, 32000, 100003])
+@pytest.mark.parametrize("rows", [1, 5, 40, 200])
+def test_draw(ghd, vocab, rows):
+    if rows * vocab > 4e6:
+        rows = max(1, 4000000 // vocab)
+    r = np.random.RandomState(vocab + rows)
+    logits, u = logits_of(r, rows, vocab), r.rand(rows, 16).astype(np.float32)
+    draws, temp = 1 + (vocab + rows) % 16, [0.5, 0.8, 1.0, 1.7][rows % 4]
+    got = ghd.ghd_draft_sample(ctx_for(ghd, vocab), dev(logits), dev(u), draws, temp).cpu().numpy()
+    ghd.ghd_sync_status(ctx_for(ghd, vocab))
+    for i in range(rows):
+        assert np.array_equal(got[i], osam.draw(logits[i], temp, draws, u[i])), i
+
+
+def test_draw_at_the_ends(ghd):
+    """Numbers at and outside the ends of [0, 1), masked tokens, rows that run out of tokens, extreme logits."""
+    V = 300
+    r = np.random.RandomState(1)
+    ctx = ctx_for(ghd, V)
+    logits = logits_of(r, 10, V)
+    logits[1, :] = -np.inf
+    logits[1, [5, 250, 299]] = [0.0, 1.0, -2.0]                   # three tokens for sixteen draws
+    logits[2, :] = -np.inf
+    logits[2, 299] = -3e38
+    logits[3, :] = 3e38
+    logits[4, :] = 0.0
+    logits[4, 17] = 1e30                                          # one token has it all, the others round to nothing
+    logits[5, :] = np.where(np.arange(V) % 2, -np.inf, 1.0)
+    logits[6, :] = 0.0                                            # equal tokens
+    u = r.rand(10, 16).astype(np.float32)
+    u[0, :6] = [0.0, 1.0, -1.0, 2.0, np.nan, np.nextafter(np.float32(1), np.float32(0))]
+    u[5, ::2], u[5, 1::2] = 0.0, 1.0
+    got = ghd.ghd_draft_sample(ctx, dev(logits), dev(u), 16, 1.0).cpu().numpy()
+    ghd.ghd_sync_status(ctx)
+    for i in range(10):
+        assert np.array_equal(got[i], osam.draw(logits[i], 1.0, 16, u[i])), i
+    assert sorted(got[1, :3]) == [5, 250, 299] and (got[1, 3:] == -1).all() and (got[4, 1:] == -1).all()
+
+
+@pytest.mark.parametrize("bad", ["nan", "inf", "none"])
+def test_draw_from_what_is_no_distribution(ghd, bad):
+    V = 5000
+    ctx = ctx_for(ghd, V)
+    r = np.random.RandomState(3)
+    logits, u = logits_of(r, 4, V), r.rand(4, 16).astype(np.float32)
+    if bad == "nan":
+        logits[2, 4321] = np.nan
+    elif bad == "inf":
+        logits[2, 77] = np.inf
+    else:
+        logits[2] = -np.inf
+    got = ghd.ghd_draft_sample(ctx, dev(logits), dev(u), 5, 1.0).cpu().numpy()
+    with pytest.raises(ghd.GhdError, match="distribution"):
+        ghd.ghd_sync_status(ctx)
+    ghd.ghd_sync_status(ctx)                                      # reported once
+    assert (got[2] == -1).all()
+    for i in (0, 1, 3):
+        assert np.array_equal(got[i], osam.draw(logits[i], 1.0, 5, u[i]))
+
+
+# ------------------------------------------------------------------ verification
+def random_parents(r, n, wide):
+    return [-1] + [int(r.randint(max(0, (i - 1) // wide), max(1, (i + 1) // 2))) for i in range(1, n)]
+
+
+class Batch:
+    """Trees of several sequences; nodes of one depth share draws from their level's draft row."""
+
+    def __init__(self, r, cnt, vocab, temp, drawn, noise=0.7, share=1.0, wide=4):
+        self.cnt, self.vocab, self.temp, self.drawn = cnt, vocab, temp, drawn
+        parent, tokens, drow, logits, draft = [], [], [], [], []
+        for n in cnt:
+            p = random_parents(r, n, wide) if n else []
+            depth = [0] * n
+            for i in range(1, n):
+                depth[i] = depth[p[i]] + 1
+            deep = max(depth) if n else 0
+            base = len(draft)
+            rows = logits_of(r, deep + 1, vocab, 5.0)
+            draft.extend(rows)
+            kids = np.bincount([x for x in p if x >= 0], minlength=1).max() if n > 1 else 1
+            cand = []
+            for d in range(deep + 1):
+                w = osam.distribution(rows[d], temp).copy()
+                if drawn:
+                    c = [int(x) for x in r.choice(vocab, min(kids, int((w > 0).sum())), replace=False, p=w)]
+                else:
+                    c = [int(x) for x in np.argsort(-rows[d], kind="stable")[:kids]]
+                cand.append(c + [-1] * (kids - len(c)))
+            seen = {}
+            for i in range(n):
+                parent.append(p[i])
+                rank = seen.get(p[i], 0)
+                seen[p[i]] = rank + 1
+                tokens.append(cand[depth[i] - 1][rank] if i else 7 % vocab)
+                drow.append(base + depth[i])
+                logits.append(share * rows[depth[i]] + noise * r.randn(vocab))
+        self.start = np.concatenate(([0], np.cumsum(cnt))).astype(np.int32)
+        self.n = int(self.start[-1])
+        self.parent, self.tokens, self.drow = np.array(parent, np.int32), np.array(tokens, np.int32), np.array(drow, np.int32)
+        self.logits = np.array(logits, np.float32).reshape(self.n, vocab)
+        self.draft = np.array(draft, np.float32).reshape(-1, vocab)
+        self.u = r.rand(self.n).astype(np.float32)
+
+    def rows(self, ghd, **kw):
+        more = dict(draft_row=dev(self.drow), draft_logits=dev(self.draft), draft_temperature=self.temp) if self.drawn else {}
+        args = dict(row_start=dev(self.start), temperature=self.temp, **more)
+        args.update(kw)
+        return ghd.SampledRows(dev(self.parent), dev(self.tokens), dev(self.logits), dev(self.u), **args)
+
+    def check(self, got, only=None):
+        longest = 0
+        for s, n in enumerate(self.cnt):
+            a, b = self.start[s], self.start[s] + n
+            nodes, toks = osam.verify(self.parent[a:b], self.tokens[a:b], self.logits[a:b], self.u[a:b], self.temp,
+                                      self.drow[a:b] if self.drawn else None, self.draft, self.temp)
+            want = np.full(514, -1, np.int32)
+            want[0], want[1] = max(0, len(nodes) - 1), len(nodes)
+            want[2:2 + len(nodes)], want[258:258 + len(toks)] = nodes, toks
+            assert np.array_equal(got[s], want), (s, got[s][:8], want[:8], got[s][258:264], want[258:264])
+            longest = max(longest, len(nodes) - 1)
+        return longest
+
+
+@pytest.mark.parametrize("drawn", [True, False])
+@pytest.mark.parametrize("cnt,vocab", [([1], 50), ([2], 1), ([7], 33), ([64], 32000), ([256], 1000), ([5, 0, 1, 30], 100), ([20] * 20, 997), ([3] * 200, 64),
+                                       ([40, 17, 64, 9], 4099), ([12, 12], 70001)])
+@pytest.mark.parametrize("temp", [0.6, 1.0])
+def test_verify(ghd, drawn, cnt, vocab, temp):
+    r = np.random.RandomState(len(cnt) * 100 + cnt[0] + vocab + 3 * drawn)
+    b = Batch(r, cnt, vocab, temp, drawn)
+    ctx = ctx_for(ghd, vocab)
+    rows = b.rows(ghd)
+    got = ghd.ghd_accept_sampled(ctx, rows)
+    again = ghd.ghd_accept_sampled(ctx, rows)
+    ghd.ghd_sync_status(ctx)
+    b.check(got.cpu().numpy())
+    assert (got == again).all()
+
+
+@pytest.mark.parametrize("noise,share", [(0.0, 1.0), (0.05, 1.0), (2.0, 0.5), (1.0, 0.0)])
+def test_verify_of_near_and_far_drafters(ghd, noise, share):
+    """A draft distribution that is the target's (all accepted), nearly (differences cancel), or has nothing to do with it."""
+    r = np.random.RandomState(int(noise * 100) + 7)
+    b = Batch(r, [30] * 24, 2000, 1.0, True, noise=noise, share=share)
+    ctx = ctx_for(ghd, 2000)
+    longest = b.check(ghd.ghd_accept_sampled(ctx, b.rows(ghd)).cpu().numpy())
+    assert longest >= 3 if share == 1.0 else longest >= 0
+    ghd.ghd_sync_status(ctx)
+
+
+def test_verify_of_wide_nodes_and_repeated_tokens(ghd):
+    """Every node hangs on the root; siblings repeat, lie outside the vocabulary, or have no probability in either distribution."""
+    V = 400
+    ctx = ctx_for(ghd, V)
+    r = np.random.RandomState(11)
+    for drawn in (True, False):
+        b = Batch(r, [200, 200, 200, 200], V, 1.0, drawn)
+        b.parent[:] = np.tile([-1] + [0] * 199, 4)
+        b.tokens[:] = r.randint(0, V, 800)
+        b.tokens[r.choice(800, 60, replace=False)] = [-1, V, 2**31 - 1] * 20
+        b.logits[:, r.choice(V, 150, replace=False)] = -np.inf
+        b.draft[:, r.choice(V, 150, replace=False)] = -np.inf
+        b.u[:] = np.where(r.rand(800) < 0.7, 0.999, b.u)
+        b.u[[0, 200]] = [0.0, 1.0]
+        b.check(ghd.ghd_accept_sampled(ctx, b.rows(ghd)).cpu().numpy())
+        ghd.ghd_sync_status(ctx)
+
+
+def test_verify_mixes_drawn_and_other_children(ghd):
+    V = 600
+    ctx = ctx_for(ghd, V)
+    r = np.random.RandomState(12)
+    b = Batch(r, [50] * 10, V, 0.9, True)
+    b.drow[r.choice(500, 200, replace=False)] = -1
+    b.check(ghd.ghd_accept_sampled(ctx, b.rows(ghd)).cpu().numpy())
+    one = ghd.SampledRows(*(dev(x[:50]) for x in (b.parent, b.tokens, b.logits, b.u)), temperature=0.9, draft_row=dev(b.drow[:50]), draft_logits=dev(b.draft), draft_temperature=0.9)
+    assert (ghd.ghd_accept_sampled(ctx, one)[0] == ghd.ghd_accept_sampled(ctx, b.rows(ghd))[0]).all()
+
+
+def test_temperatures_of_target_and_drafter(ghd):
+    V = 800
+    ctx = ctx_for(ghd, V)
+    r = np.random.RandomState(13)
+    b = Batch(r, [40] * 8, V, 1.0, True)
+    got = ghd.ghd_accept_sampled(ctx, b.rows(ghd, temperature=0.7, draft_temperature=1.4)).cpu().numpy()
+    for s in range(8):
+        a, e = b.start[s], b.start[s + 1]
+        nodes, toks = osam.verify(b.parent[a:e], b.tokens[a:e], b.logits[a:e], b.u[a:e], 0.7, b.drow[a:e], b.draft, 1.4)
+        assert list(got[s, 2:2 + len(nodes)]) == nodes and list(got[s, 258:258 + len(toks)]) == toks
+
+
+def test_bad_rows_are_recorded(ghd):
+    V = 500
+    ctx = ctx_for(ghd, V)
+    r = np.random.RandomState(14)
+    for what, status in [("start", "GHD_ETREE"), ("many", "GHD_ETREE"), ("parent", "GHD_ETREE"), ("draft", "GHD_EINVAL"), ("target nan", "distribution"), ("draft nan", "distribution")]:
+        b = Batch(r, [20, 20, 20], V, 1.0, True)
+        start = b.start.copy()
+        if what == "start":
+            start[1], start[2] = 40, 20                            # sequence 1 runs backwards, 0 and 2 have 40 rows
+        if what == "many":
+            b = Batch(r, [20, 250, 20], V, 1.0, True)
+            start = np.array([0, 0, 270, 290], np.int32)
+        if what == "parent":
+            b.parent[25], b.parent[40] = 9, 3                      # a child before its parent; a root with one
+        if what == "draft":
+            b.drow[20] = len(b.draft)
+        if what == "target nan":
+            b.logits[20, 3] = np.nan
+        if what == "draft nan":
+            b.draft[b.drow[20], 3] = np.inf
+        got = ghd.ghd_accept_sampled(ctx, b.rows(ghd, row_start=dev(start))).cpu().numpy()
+        with pytest.raises(ghd.GhdError, match=status):
+            ghd.ghd_sync_status(ctx)
+        ghd.ghd_sync_status(ctx)
+        if what == "start":
+            assert got[1, 1] == 0 and (got[1, 2:] == -1).all()
+            continue
+        if what == "many":
+            assert list(got[:2, 1]) == [0, 0]
+            a, e = 270, 290
+            nodes, toks = osam.verify(b.parent[a:e], b.tokens[a:e], b.logits[a:e], b.u[a:e], 1.0, b.drow[a:e], b.draft, 1.0)
+            assert list(got[2, 2:2 + len(nodes)]) == nodes and list(got[2, 258:258 + len(toks)]) == toks
+            continue
+        if what == "parent":
+            b.parent[25] = -1                                      # (passed over: nobody's child)
+        b.check(got)
+
+
+def test_refusals(ghd):
+    import torch
+    V = 100
+    ctx = ctx_for(ghd, V)
+    r = np.random.RandomState(15)
+    b = Batch(r, [5, 5], V, 1.0, True)
+    lg, u = dev(b.logits), torch.rand(10, 16, device="cuda")
+    for temp in (0.0, -1.0, math.nan, math.inf):
+        with pytest.raises(ghd.GhdError, match="temperature"):
+            ghd.ghd_draft_sample(ctx, lg, u, 3, temp)
+        with pytest.raises(ghd.GhdError, match="temperature"):
+            ghd.ghd_accept_sampled(ctx, b.rows(ghd, temperature=temp))
+        with pytest.raises(ghd.GhdError, match="temperature"):
+            ghd.ghd_accept_sampled(ctx, b.rows(ghd, draft_temperature=temp))
+    for draws in (0, 17, -1):
+        with pytest.raises(ghd.GhdError, match="n_draws"):
+            ghd.ghd_draft_sample(ctx, lg, u, draws)
+    with pytest.raises(ghd.GhdError, match="logits"):
+        ghd.ghd_draft_sample(ctx, lg[:, :99], u, 3)
+    with pytest.raises(ghd.GhdError, match="uniforms"):
+        ghd.ghd_draft_sample(ctx, lg, u[:9], 3)
+    with pytest.raises(ghd.GhdError, match="both"):
+        b.rows(ghd, draft_logits=None)
+    with pytest.raises(ghd.GhdError, match="logits a row"):
+        ghd.ghd_accept_sampled(ctx_for(ghd, 50), b.rows(ghd))
+    with pytest.raises(ghd.GhdError, match="n_seqs"):
+        ghd.ghd_accept_sampled(ctx, b.rows(ghd, row_start=torch.zeros(1026, dtype=torch.int32, device="cuda")))
+    with pytest.raises(ghd.GhdError, match="out"):
+        ghd.ghd_accept_sampled(ctx, b.rows(ghd), out=torch.zeros(1, 514, dtype=torch.int32, device="cuda"))
+    big = Batch(r, [1], V, 1.0, False)
+    n = 257
+    rows = ghd.SampledRows(torch.zeros(n, dtype=torch.int32, device="cuda"), torch.zeros(n, dtype=torch.int32, device="cuda"), torch.zeros(n, V, device="cuda"), torch.zeros(n, device="cuda"))
+    with pytest.raises(ghd.GhdError, match="256"):
+        ghd.ghd_accept_sampled(ctx, rows)
+    assert (ghd.ghd_draft_sample(ctx, lg[:0], u[:0], 3).shape == (0, 16))
+    ghd.ghd_sync_status(ctx)
+    assert big.n == 1
