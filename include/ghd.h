@@ -388,7 +388,8 @@ ghd_status ghd_mx4_quantize(ghd_ctx *ctx, const void *x, int64_t ld, const ghd_m
 ghd_status ghd_mx4_read(ghd_ctx *ctx, const ghd_mx4 *w, void *out, int64_t ld);
 
 /* ghd_linear with such a matrix: y float [n][m] = x T [n][k] * w[m][k]^T, x's rows x_ld elements apart (0: contiguous).
- * 1 <= n <= max_nodes, k at most the larger of d_model and d_ffn (GHD_ENOSPACE). */
+ * Products and sums have 32 bits: of 32 elements of x what is below 2^-27 (GHD_F32: 2^-37, and 2^-136) of the largest is rounded, and
+ * a row with a NaN or an infinity gives NaN throughout.  1 <= n <= max_nodes, k at most the larger of d_model and d_ffn (GHD_ENOSPACE). */
 ghd_status ghd_mx4_linear(ghd_ctx *ctx, const void *x, int64_t x_ld, const ghd_mx4 *w, int32_t n, float *y);
 /* ghd_gate_up with two: u T [n][m] = SiLU(h Wg^T) * (h Wu^T), both [m][k]; h dev T [n][k], rows h_ld elements apart (0: contiguous). */
 ghd_status ghd_mx4_gate_up(ghd_ctx *ctx, const void *h, int64_t h_ld, const ghd_mx4 *w_gate, const ghd_mx4 *w_up, int32_t n, void *u);

@@ -6,6 +6,7 @@
 #include <new>
 
 #include "internal.h"
+#include "mx4.cuh"
 
 namespace ghd {
 
@@ -39,6 +40,7 @@ size_t carve_workspace(ghd_ctx* c, char* base) {
     c->gemm_part = (float*)take((size_t)c->sm_count * 2 * 256 * 128 * 4);
     c->logits = (float*)take(N * (size_t)m.vocab * 4);
     c->mlogits = (float*)take((size_t)GHD_MAX_DRAFT_HEADS * m.vocab * 4);
+    c->mx4_terms = (uint8_t*)take(mx4_terms_bytes(m));
     return off;
 }
 
@@ -256,7 +258,7 @@ ghd_status ghd_create(const ghd_model_cfg* cfg, void* cuda_stream, ghd_ctx** out
     c->h_ssq = -1;
     c->kv_len_hint = 0;
     c->entry_fresh = c->opt_chain_calls ? 0 : 1;
-    c->attr_gemm = c->attr_attn = c->attr_attn_small = false;
+    c->attr_gemm = c->attr_attn = c->attr_attn_small = c->attr_mx4 = false;
     c->attr_kv4 = 0u;
     c->launches = 0;
     memset(c->path_count, 0, sizeof(c->path_count));

@@ -105,6 +105,7 @@ struct ghd_ctx {
     int h_ssq;        // which of them describes hbuf (-1: hbuf is already normalised)
     float* logits;    // float [max_nodes][vocab]
     float* mlogits;   // float [8][vocab] logits of the drafting heads
+    uint8_t* mx4_terms;   // e4m3 terms of the rows of x and their scales (products with 4-bit matrices)
     int *status, *input_status;      // device status words: waits that ran out, data out of range
     int* kv_len_word; // device word with the cache length (calls given GHD_KV_LEN_DEVICE read it)
     int kv_len_hint;  // what the host last wrote there: sizes launches whose grid depends on the length
@@ -112,7 +113,7 @@ struct ghd_ctx {
     ghd::PendingPartials pending;   // projection output not yet folded into xres
     // bookkeeping
     int entry_fresh;          // 1 until the first launch of a public call: that launch is fully serialised (see launch_k)
-    bool attr_gemm, attr_attn, attr_attn_small;  // dynamic shared memory limits raised on this context's device
+    bool attr_gemm, attr_attn, attr_attn_small, attr_mx4;  // dynamic shared memory limits raised on this context's device
     unsigned attr_kv4;        // ... of the 4-bit cache's attention kernels, a bit each
     int64_t launches;
     int64_t path_count[8];   // launches per kernel family (ghd_path)

@@ -1,0 +1,527 @@
+// Product with matrices in microscaled 4-bit floating point on the 5th-generation tensor cores (sm_100a): y[n][m] = x[n][k] w[m][k]^T.
+//
+// tcgen05.mma of kind::mxf8f6f4 multiplies 4-bit elements with 8-bit ones as they are, each 32 along k with a power-of-two scale
+// on either side.  x has 16 or 32 bits, so 32 elements of it are split into TERMS sums of e4m3 numbers: with 2^e <= largest < 2^(e+1)
+// the first term is x / 2^(e-7) rounded to e4m3 (4 significant bits, at most 256), the next 2^5 times what is left, and so on.  A term
+// leaves at most 2^-4 of its element, so three of them hold the 11 bits of a half and five the 24 of a float, exactly but for what is
+// below 2^-27 (2^-37) of the largest of the 32.  The terms of a row are neighbouring columns of one MMA (N = TERMS * rows), so
+// that a weight is read once for all; the epilogue adds them.
+//
+// As in the half-precision projection, 128 rows of w are the M of an MMA, the columns of x its N; a unit is one tile of 128 rows (MT = 1)
+// or two (MT = 2: two neighbours that share the loads of x, or a gate tile with its up tile), and the flattened (unit, k-step) space is cut
+// into equal ranges, one per CTA.  Units that several CTAs share are summed from their partial sums in the workspace, in the order of
+// the CTAs, each contributor finishing a slice once all have arrived (a bounded wait; every CTA is resident).
+//
+// The tensor cores cut off what they add below 2^-24 of the running sum, always towards zero, so a sum of 4096 loses 1.3e-6 of itself:
+// accumulators are taken out every CHUNK k-steps and added up in registers with rounding (6.5e-7 over 2048, measured).
+#include <cuda.h>
+#include <cuda_fp8.h>
+
+#include <cstdio>
+
+#include "mx4.cuh"
+#include "tc_common.cuh"
+
+namespace ghd {
+
+namespace {
+
+using namespace mx4;
+using namespace tc;
+
+constexpr int THREADS = 320;            // producer warp, MMA warp, eight epilogue warps
+constexpr int MAX_STAGES = 10;
+constexpr int CHUNK = 16;               // k-steps of 128 that one accumulator takes
+constexpr int MAX_UNITS_SHARED = 1024;  // counters: arrivals in the first half of this many, departures in the second
+constexpr int A_BYTES = TILE * TILE;    // a tile of 4-bit elements in shared memory, a byte each
+constexpr int SF_BYTES = 512;           // scales of 128 rows and 128 columns
+
+struct Mx4Params {
+    int n, m, kt;                       // rows of x, rows of w, k-steps (tiles along k)
+    int tiles;                          // tiles of 128 rows of w
+    int per_group, groups, cols;        // rows of x are worked on in groups of per_group: cols = TERMS * per_group, up to a multiple of 16
+    int sf_atoms;                       // ceil(cols / 128)
+    int units, stages;                  // units: row units * groups, groups of one row unit behind one another
+    long long total;                    // units * kt
+    const uint8_t *scales, *scales2;    // of w, of the second matrix
+    const uint8_t* x_scales;
+    float* part;                        // [CTA][2][MT * per_group][128]
+    int* counters;
+    int* status;
+    void* out;
+};
+
+struct Smem {
+    uint64_t full[MAX_STAGES], empty[MAX_STAGES];
+    uint64_t acc_full, acc_empty, drain;
+    uint32_t tmem_base;
+    int abort_flag;
+};
+
+__device__ __forceinline__ void bulk_load(uint32_t dst, const void* src, uint32_t bytes, uint32_t bar, uint64_t policy) {
+    asm volatile("cp.async.bulk.shared::cluster.global.mbarrier::complete_tx::bytes.L2::cache_hint [%0], [%1], %2, [%3], %4;"
+                 ::"r"(dst), "l"(src), "r"(bytes), "r"(bar), "l"(policy) : "memory");
+}
+
+// scales of 128 rows: 32 rows of 16 bytes, 8 of them 128 bytes apart, no swizzle
+__device__ __forceinline__ uint64_t smem_desc_scales(uint32_t addr) {
+    return (uint64_t)((addr & 0x3FFFFu) >> 4) | (uint64_t)(128 >> 4) << 32 | (uint64_t)1 << 46;
+}
+__device__ __forceinline__ void copy_scales(uint32_t tmem, uint32_t smem) {       // to four columns, the same in all four quarters of the lanes
+    asm volatile("tcgen05.cp.cta_group::1.32x128b.warpx4 [%0], %1;" ::"r"(tmem), "l"(smem_desc_scales(smem)) : "memory");
+}
+// kind::mxf8f6f4: A e2m1 (5), B e4m3 (0), scales e8m0, D float, M = 128; byte q of the scale words belongs to the q-th 32 of 128 columns
+__device__ __forceinline__ uint32_t instr_desc_mx(int cols, int q) {
+    return 5u << 7 | (uint32_t)(cols >> 3) << 17 | 1u << 23 | (uint32_t)(TILE >> 4) << 24 | (uint32_t)q << 29 | (uint32_t)q << 4;
+}
+__device__ __forceinline__ void mma_mx(uint32_t d, uint64_t a, uint64_t b, uint32_t idesc, uint32_t sfa, uint32_t sfb, uint32_t accumulate) {
+    asm volatile(
+        "{\n\t.reg .pred p;\n\t"
+        "setp.ne.b32 p, %6, 0;\n\t"
+        "tcgen05.mma.cta_group::1.kind::mxf8f6f4.block_scale.scale_vec::1X [%0], %1, %2, %3, [%4], [%5], p;\n\t}"
+        ::"r"(d), "l"(a), "l"(b), "r"(idesc), "r"(sfa), "r"(sfb), "r"(accumulate) : "memory");
+}
+__device__ __forceinline__ void ld8(uint32_t taddr, uint32_t* r) {                // 8 columns of this warp's 32 lanes; not there until ld_wait
+    asm volatile("tcgen05.ld.sync.aligned.32x32b.x8.b32 {%0, %1, %2, %3, %4, %5, %6, %7}, [%8];"
+                 : "=r"(r[0]), "=r"(r[1]), "=r"(r[2]), "=r"(r[3]), "=r"(r[4]), "=r"(r[5]), "=r"(r[6]), "=r"(r[7]) : "r"(taddr) : "memory");
+}
+__device__ __forceinline__ void ld_wait8(uint32_t* r) {
+    asm volatile("tcgen05.wait::ld.sync.aligned;"
+                 : "+r"(r[0]), "+r"(r[1]), "+r"(r[2]), "+r"(r[3]), "+r"(r[4]), "+r"(r[5]), "+r"(r[6]), "+r"(r[7])::"memory");
+}
+// barrier of the epilogue warps that tells whether all of them are well: they take the same way out
+__device__ __forceinline__ bool epi_all(bool ok) {
+    uint32_t r;
+    asm volatile("{\n\t.reg .pred p, q;\n\tsetp.ne.b32 p, %1, 0;\n\tbar.red.and.pred q, 1, 256, p;\n\tselp.u32 %0, 1, 0, q;\n\t}" : "=r"(r) : "r"((uint32_t)ok) : "memory");
+    return r != 0;
+}
+
+// ---------------------------------------------------------------- x -> terms
+template <typename T> constexpr int TERMS = sizeof(T) == 2 ? 3 : 5;
+template <typename T> constexpr int GROUP = sizeof(T) == 2 ? 64 : 32;             // rows of x that one pass over w takes at most
+
+template <typename T>
+__global__ void __launch_bounds__(256) k_mx4_terms(const T* __restrict__ x, int64_t ld, int n, int k, bool wide, int kt, int per_group, int cols, int sf_atoms,
+                                                   uint2* __restrict__ terms, uint32_t* __restrict__ scales) {
+    constexpr int P = TERMS<T>;
+    pdl_trigger();
+    const int lane = threadIdx.x & 31, w = blockIdx.x * 8 + (threadIdx.x >> 5), per_row = (kt + 1) / 2;
+    const int i = w / per_row, c0 = (w - i * per_row) * 256 + lane * 8, tk = c0 / TILE;
+    if (i >= n || tk >= kt) return;                              // (16 lanes to a k-step: they leave together)
+    const uint32_t mask = 0xffffu << (lane & 16);
+    float v[8];
+    load8(x + i * ld, c0, k, wide, v);
+    float top = 0.f;
+#pragma unroll
+    for (int e = 0; e < 8; ++e) top = max_nan(top, fabsf(v[e]));
+    top = max_nan(top, __shfl_xor_sync(mask, top, 1));
+    top = max_nan(top, __shfl_xor_sync(mask, top, 2));
+    uint32_t field = (__float_as_uint(top) >> 23) & 255u;
+    const bool none = field == 255u;
+    field = max(field, 7u + 5u * (P - 1));                       // (so that the last term's scale is one)
+    const float unit = __uint_as_float((261u - field) << 23);    // 2^(7 - e)
+#pragma unroll
+    for (int e = 0; e < 8; ++e) v[e] = none ? 0.f : v[e] * unit;
+    // Floats from 1.9375 x 2^127 up would round to 2^128: their first term stays at 240 and leaves up to 16, so the next one's factor is 2^4.
+    const bool high = sizeof(T) == 4 && field == 254u;
+    const int g = i / per_group, col0 = (i - g * per_group) * P;
+    const size_t step = (size_t)g * kt + tk;
+#pragma unroll
+    for (int p = 0; p < P; ++p) {
+        uint32_t r[2];
+#pragma unroll
+        for (int q = 0; q < 2; ++q) {
+            const float most = p == 0 && high ? 240.f : 448.f;
+            float h[4];
+#pragma unroll
+            for (int e = 0; e < 4; ++e) h[e] = fminf(fmaxf(v[4 * q + e], -most), most);
+            const __nv_fp8x2_storage_t a = __nv_cvt_float2_to_fp8x2(make_float2(h[0], h[1]), __NV_SATFINITE, __NV_E4M3);
+            const __nv_fp8x2_storage_t b = __nv_cvt_float2_to_fp8x2(make_float2(h[2], h[3]), __NV_SATFINITE, __NV_E4M3);
+            r[q] = (uint32_t)a | (uint32_t)b << 16;
+            const float2 f0 = __half22float2(__half2(__nv_cvt_fp8x2_to_halfraw2(a, __NV_E4M3))), f1 = __half22float2(__half2(__nv_cvt_fp8x2_to_halfraw2(b, __NV_E4M3)));
+            const float f[4] = {f0.x, f0.y, f1.x, f1.y};
+#pragma unroll
+            for (int e = 0; e < 4; ++e) v[4 * q + e] = (v[4 * q + e] - f[e]) * (p == 0 && high ? 16.f : 32.f);
+        }
+        const int col = col0 + p;
+        terms[(step * cols + col) * 16 + (lane & 15)] = make_uint2(r[0], r[1]);
+        uint32_t s = (none ? 255u : field - 7u - 5u * p + (high && p ? 1u : 0u)) << (8 * ((lane >> 2) & 3));
+        s |= __shfl_xor_sync(mask, s, 4);
+        s |= __shfl_xor_sync(mask, s, 8);
+        if ((lane & 15) == 0) scales[(step * sf_atoms + col / TILE) * (SF_BYTES / 4) + scale_at(col % TILE, 0) / 4] = s;
+    }
+}
+
+// ---------------------------------------------------------------- product
+template <int P, int MT, bool GATE>
+__global__ void __launch_bounds__(THREADS, 1)
+k_mx4_gemm(const __grid_constant__ CUtensorMap tm_w, const __grid_constant__ CUtensorMap tm_w2, const __grid_constant__ CUtensorMap tm_x, const Mx4Params p) {
+    static_assert(!GATE || MT == 2, "a gate tile and its up tile");
+    extern __shared__ uint8_t smem_raw[];
+    const uint32_t raw_addr = smem_u32(smem_raw);
+    uint8_t* tiles = smem_raw + ((1024u - (raw_addr & 1023u)) & 1023u);
+    const uint32_t tiles_addr = smem_u32(tiles);
+    // a stage: MT weight tiles | columns of x | scales of the tiles | scales of x
+    const uint32_t b_off = MT * A_BYTES, sa_off = b_off + (uint32_t)p.cols * TILE, sb_off = sa_off + MT * SF_BYTES;
+    const uint32_t stage_bytes = (sb_off + (uint32_t)p.sf_atoms * SF_BYTES + 1023u) & ~1023u;
+    const uint32_t x_bytes = (uint32_t)p.cols * TILE + (uint32_t)p.sf_atoms * SF_BYTES;
+    Smem* sm = reinterpret_cast<Smem*>(tiles + (size_t)p.stages * stage_bytes);
+
+    const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31, cta = blockIdx.x, ctas = gridDim.x;
+    const long long it_beg = p.total * cta / ctas, it_end = p.total * (cta + 1) / ctas;
+    const int my_iters = (int)(it_end - it_beg);
+    const int prefill = my_iters < p.stages ? my_iters : p.stages;
+    const int unit0 = (int)(it_beg / p.kt), kc0 = (int)(it_beg - (long long)unit0 * p.kt);
+    // tiles of a unit: the two of a pair, or one behind which there is none
+    auto tiles_of = [&](int unit) { return GATE || MT == 1 ? MT : (unit / p.groups) * MT + 1 < p.tiles ? 2 : 1; };
+    auto load_w = [&](uint32_t stage, int unit, int kc, uint32_t bar, uint64_t pol) {
+        const int ru = unit / p.groups, nt = tiles_of(unit);
+        mbar_expect_tx(bar, (uint32_t)nt * (TILE_CODES + SF_BYTES) + x_bytes);      // (the 4-bit tiles count as they lie in memory)
+        const uint32_t at = tiles_addr + stage * stage_bytes;
+#pragma unroll
+        for (int t = 0; t < MT; ++t) {
+            if (t >= nt) break;
+            const long long tile = (long long)(GATE ? ru : ru * MT + t) * p.kt + kc;
+            tma_load_2d(at + t * A_BYTES, GATE && t ? &tm_w2 : &tm_w, 0, (int)(tile * TILE), bar, pol);
+            bulk_load(at + sa_off + t * SF_BYTES, (GATE && t ? p.scales2 : p.scales) + tile * TILE_SCALES, SF_BYTES, bar, pol);
+        }
+    };
+    auto load_x = [&](uint32_t stage, int unit, int kc, uint32_t bar, uint64_t pol) {
+        const int step = (unit % p.groups) * p.kt + kc;
+        const uint32_t at = tiles_addr + stage * stage_bytes;
+        tma_load_2d(at + b_off, &tm_x, 0, step * p.cols, bar, pol);
+        bulk_load(at + sb_off, p.x_scales + (size_t)step * p.sf_atoms * SF_BYTES, (uint32_t)p.sf_atoms * SF_BYTES, bar, pol);
+    };
+
+    if (threadIdx.x == 32) {
+        asm volatile("prefetch.tensormap [%0];" ::"l"(&tm_w) : "memory");
+        asm volatile("prefetch.tensormap [%0];" ::"l"(&tm_x) : "memory");
+    }
+    if (threadIdx.x == 0) {
+        for (int s = 0; s < p.stages; ++s) { mbar_init(smem_u32(&sm->full[s]), 1); mbar_init(smem_u32(&sm->empty[s]), 1); }
+        mbar_init(smem_u32(&sm->acc_full), 1);
+        mbar_init(smem_u32(&sm->acc_empty), 8);
+        mbar_init(smem_u32(&sm->drain), 1);
+        sm->abort_flag = 0;
+        asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
+        // weights do not depend on the kernel before: the ring's first ones are on their way during set-up
+        uint64_t pol;
+        asm volatile("createpolicy.fractional.L2::evict_first.b64 %0, 1.0;" : "=l"(pol));
+        for (int i = 0, unit = unit0, kc = kc0; i < prefill; ++i) {
+            load_w(i, unit, kc, smem_u32(&sm->full[i]), pol);
+            if (++kc == p.kt) { kc = 0; ++unit; }
+        }
+    }
+    if (warp == 1) {
+        asm volatile("tcgen05.alloc.cta_group::1.sync.aligned.shared::cta.b32 [%0], 512;" ::"r"(smem_u32(&sm->tmem_base)) : "memory");
+        asm volatile("tcgen05.relinquish_alloc_permit.cta_group::1.sync.aligned;" ::: "memory");
+    }
+    tc_fence_before();
+    __syncthreads();
+    tc_fence_after();
+    const uint32_t tmem = sm->tmem_base;
+    volatile int* abort_flag = &sm->abort_flag;
+
+    if (warp == 0) {
+        if (lane == 0) {
+            uint64_t pol_stream, pol_keep;
+            asm volatile("createpolicy.fractional.L2::evict_first.b64 %0, 1.0;" : "=l"(pol_stream));
+            asm volatile("createpolicy.fractional.L2::evict_last.b64 %0, 1.0;" : "=l"(pol_keep));
+            if (p.groups > 1) asm volatile("createpolicy.fractional.L2::evict_normal.b64 %0, 1.0;" : "=l"(pol_stream));     // read again by the next group
+            int unit = unit0, kc = kc0, issued = 0;
+            uint32_t stage = 0, phase = 0;
+            bool ok = true;
+            pdl_wait();                                        // x's terms belong to the kernel before until now
+            for (; issued < prefill; ++issued) {
+                load_x(issued, unit, kc, smem_u32(&sm->full[issued]), pol_keep);
+                if (++kc == p.kt) { kc = 0; ++unit; }
+            }
+            if (prefill == p.stages) phase = 1; else stage = (uint32_t)prefill;
+            for (int i = prefill; i < my_iters; ++i) {
+                ok = mbar_wait(smem_u32(&sm->empty[stage]), phase ^ 1, abort_flag, p.status, DEV_TIMEOUT_TMA);
+                if (!ok) break;
+                const uint32_t full = smem_u32(&sm->full[stage]);
+                load_w(stage, unit, kc, full, pol_stream);
+                load_x(stage, unit, kc, full, pol_keep);
+                ++issued;
+                if (++stage == (uint32_t)p.stages) { stage = 0; phase ^= 1; }
+                if (++kc == p.kt) { kc = 0; ++unit; }
+            }
+            if (!ok) {                                         // nothing may be in flight when the CTA ends
+                const int inflight = issued < p.stages ? issued : p.stages;
+                for (int q = 0; q < inflight; ++q) {
+                    if (stage == 0) { stage = p.stages - 1; phase ^= 1; } else --stage;
+                    for (uint32_t spin = 0; spin < SPIN_LIMIT && !mbar_try(smem_u32(&sm->full[stage]), phase); ++spin) __nanosleep(64);
+                }
+            }
+        }
+    } else if (warp == 1) {
+        if (lane == 0) {
+            // columns of tensor memory: the accumulators, then the scales of every stage (written again only after the MMAs of the
+            // stage's last use are through, which the ring makes sure of)
+            const uint32_t sf_cols = 4u * (MT + p.sf_atoms), sf0 = tmem + (uint32_t)(MT * p.cols);
+            uint32_t stage = 0, phase = 0, chunks = 0;
+            bool ok = true;
+            int unit = unit0, kc = kc0;
+            for (int i = 0; i < my_iters && ok;) {
+                int take = min(min(p.kt - kc, CHUNK), my_iters - i);
+                if (chunks > 0) ok = mbar_wait(smem_u32(&sm->acc_empty), (chunks - 1) & 1, abort_flag, p.status, DEV_TIMEOUT_TMEM);
+                if (!ok) break;
+                tc_fence_after();
+                const int nt = tiles_of(unit);
+                for (int s = 0; s < take; ++s) {
+                    ok = mbar_wait(smem_u32(&sm->full[stage]), phase, abort_flag, p.status, DEV_TIMEOUT_MMA);
+                    if (!ok) break;
+                    tc_fence_after();
+                    const uint32_t at = tiles_addr + stage * stage_bytes, sfa = sf0 + stage * sf_cols, sfb = sfa + 4 * MT;
+#pragma unroll
+                    for (int t = 0; t < MT; ++t)
+                        if (t < nt) copy_scales(sfa + 4 * t, at + sa_off + t * SF_BYTES);
+                    for (int a = 0; a < p.sf_atoms; ++a) copy_scales(sfb + 4 * a, at + sb_off + a * SF_BYTES);
+                    const uint64_t bdesc = smem_desc_sw128(at + b_off);
+#pragma unroll
+                    for (int t = 0; t < MT; ++t) {
+                        if (t >= nt) break;
+                        const uint64_t adesc = smem_desc_sw128(at + t * A_BYTES);
+#pragma unroll
+                        for (int q = 0; q < 4; ++q)
+                            mma_mx(tmem + t * p.cols, adesc + q * 2, bdesc + q * 2, instr_desc_mx(p.cols, q), sfa + 4 * t, sfb, s > 0 || q > 0);
+                    }
+                    tc_commit(smem_u32(&sm->empty[stage]));
+                    if (++stage == (uint32_t)p.stages) { stage = 0; phase ^= 1; }
+                }
+                if (!ok) break;
+                tc_commit(smem_u32(&sm->acc_full));
+                ++chunks;
+                i += take;
+                kc += take;
+                if (kc == p.kt) { kc = 0; ++unit; }
+            }
+            if (!ok) {                                         // no MMA may run when the tensor memory goes
+                tc_commit(smem_u32(&sm->drain));
+                for (uint32_t spin = 0; spin < SPIN_LIMIT && !mbar_try(smem_u32(&sm->drain), 0); ++spin) __nanosleep(64);
+            }
+        }
+    } else {
+        // Epilogue warps 2 .. 9: the lanes of a warp are 32 rows of w; the first four warps take the first half of the rows of x, the others
+        // the second, in eights.
+        constexpr int NODES = (P == 3 ? 64 : 32) / 2;
+        const int quad = warp & 3, grp = (warp - 2) >> 2, row = quad * 32 + lane, et = threadIdx.x - 64;
+        const size_t slot = (size_t)MT * p.per_group * TILE;
+        const int half = ((p.per_group + 15) / 16) * 8, j0 = grp * half;
+        float acc[MT][NODES];
+        uint32_t chunks = 0;
+        bool ok = true, waited = false;
+        int unit = unit0, kc = kc0, split_unit[2], n_split = 0;
+        float* y = (float*)p.out;
+        using T = typename std::conditional<P == 3, __half, float>::type;
+        T* u = (T*)p.out;
+        auto silu = [](float g, float up) { return __fdividef(g * up, 1.f + exp2f(-1.4426950408889634f * g)); };
+        for (int i = 0; i < my_iters && ok;) {
+            const int first = kc, end = min(p.kt, kc + my_iters - i), g = unit % p.groups, ru = unit / p.groups;
+            const int rows_here = min(p.per_group, p.n - g * p.per_group), mine = max(0, min(half, rows_here - j0));
+            for (int c = first; c < end && ok; c += CHUNK) {
+                const bool fresh = c == first;
+                ok = epi_all(mbar_wait(smem_u32(&sm->acc_full), chunks & 1, abort_flag, p.status, DEV_TIMEOUT_EPI));
+                if (!ok) break;
+                tc_fence_after();
+#pragma unroll
+                for (int t = 0; t < MT; ++t)
+#pragma unroll
+                    for (int e = 0; e < NODES; e += 8)
+                        if (e < mine) {
+                            uint32_t r[8 * P];
+                            const uint32_t at = tmem + t * p.cols + P * (j0 + e) + ((uint32_t)(quad * 32) << 16);
+#pragma unroll
+                            for (int q = 0; q < P; ++q) ld8(at + 8 * q, r + 8 * q);
+#pragma unroll
+                            for (int q = 0; q < P; ++q) ld_wait8(r + 8 * q);
+#pragma unroll
+                            for (int j = 0; j < 8; ++j) {
+                                float v = __uint_as_float(r[P * j + P - 1]);
+#pragma unroll
+                                for (int q = P - 2; q >= 0; --q) v += __uint_as_float(r[P * j + q]);
+                                acc[t][e + j] = fresh ? v : acc[t][e + j] + v;
+                            }
+                        }
+                tc_fence_before();
+                __syncwarp();
+                if (lane == 0) mbar_arrive(smem_u32(&sm->acc_empty));
+                ++chunks;
+            }
+            if (!ok) break;
+            if (!waited) { pdl_wait(); waited = true; }        // outputs and partial sums belong to the kernel before until now
+            if (first == 0 && end == p.kt) {
+#pragma unroll
+                for (int t = 0; t < (GATE ? 1 : MT); ++t) {
+                    const int f = (GATE ? ru : ru * MT + t) * TILE + row;
+#pragma unroll
+                    for (int e = 0; e < NODES; ++e)
+                        if (e < mine && f < p.m) {
+                            const size_t at = (size_t)(g * p.per_group + j0 + e) * p.m + f;
+                            if constexpr (GATE) u[at] = from_f<T>(silu(acc[0][e], acc[1][e]));
+                            else y[at] = acc[t][e];
+                        }
+                }
+            } else {
+                float* mine_at = p.part + ((size_t)cta * 2 + (i == 0 ? 0 : 1)) * slot;
+#pragma unroll
+                for (int t = 0; t < MT; ++t)
+#pragma unroll
+                    for (int e = 0; e < NODES; ++e)
+                        if (e < mine) __stcg(mine_at + ((size_t)t * p.per_group + j0 + e) * TILE + row, acc[t][e]);
+                epi_all(true);
+                if (et == 0) atom_add_acq_rel_gpu(p.counters + (int)((((long long)unit * p.kt + 1) * ctas - 1) / p.total), 1);
+                split_unit[n_split++] = unit;
+            }
+            i += end - first;
+            kc = end;
+            if (kc == p.kt) { kc = 0; ++unit; }
+        }
+        // The slices of this CTA's shared units: at most the first and the last of its range.
+        for (int q = 0; q < n_split && ok; ++q) {
+            const int un = split_unit[q], g = un % p.groups, ru = un / p.groups, nt = tiles_of(un);
+            const long long s0 = (long long)un * p.kt;
+            const int c0 = (int)(((s0 + 1) * ctas - 1) / p.total), cnt = (int)(((s0 + p.kt) * ctas - 1) / p.total) - c0 + 1;
+            if (et == 0) {
+                uint32_t spin = 0;
+                while (ld_acquire_gpu(p.counters + c0) != cnt) {
+                    if (++spin >= SPIN_LIMIT || *abort_flag) { *abort_flag = 1; atomicCAS(p.status, DEV_OK, DEV_TIMEOUT_GRID); ok = false; break; }
+                    __nanosleep(spin > 64 ? 64 : 20);
+                }
+            }
+            ok = epi_all(ok);
+            if (!ok) break;
+            // the first contributor's sums are in its second slot if the unit is not the first of its range
+            const int slot_first = p.total * c0 / ctas < s0 ? 1 : 0;
+            const int rows_here = min(p.per_group, p.n - g * p.per_group), vecs = (GATE ? 1 : nt) * rows_here * (TILE / 4);
+            const int lo = (int)((long long)vecs * (cta - c0) / cnt), hi = (int)((long long)vecs * (cta - c0 + 1) / cnt);
+            for (int v = lo + et; v < hi; v += 256) {
+                const int r4 = (v % (TILE / 4)) * 4, col = v / (TILE / 4), t = col / rows_here, j = col - t * rows_here;
+                float4 sum[GATE ? 2 : 1];
+#pragma unroll
+                for (int h = 0; h < (GATE ? 2 : 1); ++h) {
+                    const size_t off = ((size_t)(t + h) * p.per_group + j) * TILE + r4;
+                    float4 a = make_float4(0.f, 0.f, 0.f, 0.f);
+                    for (int c = 0; c < cnt; c += 4) {
+                        float4 b[4];
+#pragma unroll
+                        for (int d = 0; d < 4; ++d)
+                            b[d] = c + d < cnt ? __ldcg(reinterpret_cast<const float4*>(p.part + ((size_t)(c0 + c + d) * 2 + (c + d == 0 ? slot_first : 0)) * slot + off)) : make_float4(0.f, 0.f, 0.f, 0.f);
+#pragma unroll
+                        for (int d = 0; d < 4; ++d) { a.x += b[d].x; a.y += b[d].y; a.z += b[d].z; a.w += b[d].w; }
+                    }
+                    sum[h] = a;
+                }
+                const float s[4] = {sum[0].x, sum[0].y, sum[0].z, sum[0].w};
+                const int f = (GATE ? ru : ru * MT + t) * TILE + r4;
+                const size_t at = (size_t)(g * p.per_group + j) * p.m + f;
+                if constexpr (GATE) {
+                    const float up[4] = {sum[GATE ? 1 : 0].x, sum[GATE ? 1 : 0].y, sum[GATE ? 1 : 0].z, sum[GATE ? 1 : 0].w};
+#pragma unroll
+                    for (int e = 0; e < 4; ++e)
+                        if (f + e < p.m) u[at + e] = from_f<T>(silu(s[e], up[e]));
+                } else {
+#pragma unroll
+                    for (int e = 0; e < 4; ++e)
+                        if (f + e < p.m) y[at + e] = s[e];
+                }
+            }
+            epi_all(true);
+            if (et == 0 && atom_add_acq_rel_gpu(p.counters + MAX_UNITS_SHARED + c0, 1) == cnt - 1) {
+                p.counters[c0] = 0;                              // everybody has passed the wait: ready for the next launch
+                p.counters[MAX_UNITS_SHARED + c0] = 0;
+            }
+        }
+    }
+    tc_fence_before();
+    __syncthreads();
+    if (warp == 1) {
+        tc_fence_after();
+        asm volatile("tcgen05.dealloc.cta_group::1.sync.aligned.b32 %0, 512;" ::"r"(tmem) : "memory");
+    }
+}
+
+// ---------------------------------------------------------------- host side
+struct Groups { int per, groups, cols, atoms; };
+Groups groups_of(int n, int terms, int most) {
+    Groups g;
+    g.groups = (n + most - 1) / most;
+    g.per = (n + g.groups - 1) / g.groups;
+    g.groups = (n + g.per - 1) / g.per;
+    g.cols = (terms * g.per + 15) / 16 * 16;
+    g.atoms = (g.cols + TILE - 1) / TILE;
+    return g;
+}
+
+template <typename T>
+ghd_status go(ghd_ctx* c, const T* x, int64_t ld, bool wide, const ghd_mx4* w, const ghd_mx4* w2, int n, void* out) {
+    constexpr int P = TERMS<T>;
+    const Groups g = groups_of(n, P, GROUP<T>);
+    Mx4Params p{};
+    p.n = n; p.m = w->m;
+    p.kt = (w->k + TILE - 1) / TILE;
+    p.tiles = (w->m + TILE - 1) / TILE;
+    p.per_group = g.per; p.groups = g.groups; p.cols = g.cols; p.sf_atoms = g.atoms;
+    // two tiles share the columns of x as soon as these are more bytes than a tile (64 a row)
+    const int mt = w2 || g.cols > 64 ? 2 : 1;
+    p.units = (w2 ? p.tiles : (p.tiles + mt - 1) / mt) * g.groups;
+    p.total = (long long)p.units * p.kt;
+    const size_t stage = ((size_t)mt * (A_BYTES + SF_BYTES) + (size_t)g.cols * TILE + (size_t)g.atoms * SF_BYTES + 1023) / 1024 * 1024;
+    p.stages = (int)((227 * 1024 - 1024 - sizeof(Smem)) / stage);
+    if (p.stages > MAX_STAGES) p.stages = MAX_STAGES;
+    const int sf_room = (512 - mt * g.cols) / (4 * (mt + g.atoms));
+    if (p.stages > sf_room) p.stages = sf_room;
+    p.scales = (const uint8_t*)w->scales;
+    p.scales2 = w2 ? (const uint8_t*)w2->scales : nullptr;
+    uint8_t* terms = c->mx4_terms;
+    uint8_t* x_scales = terms + (size_t)g.groups * p.kt * g.cols * TILE;
+    p.x_scales = x_scales;
+    p.part = c->gemm_part;
+    p.counters = c->counters;
+    p.status = c->status;
+    p.out = out;
+    CUtensorMap tw, tw2, tx;
+    const uint64_t rows = (uint64_t)p.tiles * p.kt * TILE;
+    if (!tmap_bytes(c, w->codes, rows, TILE, true, &tw) || (w2 && !tmap_bytes(c, w2->codes, rows, TILE, true, &tw2)) ||
+        !tmap_bytes(c, terms, (uint64_t)g.groups * p.kt * g.cols, (uint32_t)g.cols, false, &tx))
+        return fail(c, GHD_ECUDA, "mx4: tensor map encoding failed");
+    if (!w2) tw2 = tw;
+    if (!c->attr_mx4) {
+        const void* kernels[] = {(const void*)k_mx4_gemm<3, 1, false>, (const void*)k_mx4_gemm<3, 2, false>, (const void*)k_mx4_gemm<3, 2, true>,
+                                 (const void*)k_mx4_gemm<5, 1, false>, (const void*)k_mx4_gemm<5, 2, false>, (const void*)k_mx4_gemm<5, 2, true>};
+        for (const void* f : kernels)
+            if (cudaFuncSetAttribute(f, cudaFuncAttributeMaxDynamicSharedMemorySize, 227 * 1024) != cudaSuccess) return check_cuda(c, "mx4: shared memory");
+        c->attr_mx4 = true;
+    }
+    const int warps = n * ((p.kt + 1) / 2);
+    launch_k(c, false, k_mx4_terms<T>, (warps + 7) / 8, 256, 0, x, ld, n, (int)w->k, wide, p.kt, g.per, g.cols, g.atoms, (uint2*)terms, (uint32_t*)x_scales);
+    int ctas = c->sm_count < MAX_UNITS_SHARED ? c->sm_count : MAX_UNITS_SHARED;
+    if (ctas > p.total) ctas = (int)p.total;
+    const size_t smem = 1024 + p.stages * stage + sizeof(Smem);
+    if (w2) launch_k(c, true, k_mx4_gemm<P, 2, true>, ctas, THREADS, smem, tw, tw2, tx, p);
+    else if (mt == 2) launch_k(c, true, k_mx4_gemm<P, 2, false>, ctas, THREADS, smem, tw, tw2, tx, p);
+    else launch_k(c, true, k_mx4_gemm<P, 1, false>, ctas, THREADS, smem, tw, tw2, tx, p);
+    return GHD_OK;
+}
+
+}  // namespace
+
+size_t mx4_terms_bytes(const ghd_model_cfg& m) {
+    const int terms = m.dtype == GHD_F32 ? TERMS<float> : TERMS<__half>, most = m.dtype == GHD_F32 ? GROUP<float> : GROUP<__half>;
+    const size_t kt = ((m.d_model > m.d_ffn ? m.d_model : m.d_ffn) + TILE - 1) / TILE;
+    size_t best = 0;                                             // (n rows can take more than n + 1)
+    for (int n = 1; n <= m.max_nodes; ++n) {
+        const Groups g = groups_of(n, terms, most);
+        const size_t b = (size_t)g.groups * kt * ((size_t)g.cols * TILE + (size_t)g.atoms * SF_BYTES);
+        if (b > best) best = b;
+    }
+    return best;
+}
+
+ghd_status launch_mx4_product(ghd_ctx* c, const void* x, int64_t ld, bool wide, const ghd_mx4* w, const ghd_mx4* w2, int n, void* out) {
+    c->entry_fresh = 1;
+    return c->cfg.dtype == GHD_F32 ? go(c, (const float*)x, ld, wide, w, w2, n, out) : go(c, (const __half*)x, ld, wide, w, w2, n, out);
+}
+
+}  // namespace ghd

@@ -240,4 +240,8 @@ bool tmap_slabs(ghd_ctx* c, const void* ptr, uint64_t rows, uint64_t cols, uint3
 bool tmap_planes_slabs(ghd_ctx* c, const void* ptr, uint64_t planes, uint64_t rows_alloc, uint64_t rows, uint64_t cols,
                        uint32_t box_rows, CUtensorMap* out);
 
+// Rows of 128 elements of one byte, or of 4 bits (packed in memory, 8 bytes in every 16 in shared memory: what tcgen05.mma takes
+// for 4-bit operands next to 8-bit ones; the barrier counts the bytes in memory); a box of box_rows rows.
+bool tmap_bytes(ghd_ctx* c, const void* ptr, uint64_t rows, uint32_t box_rows, bool fp4, CUtensorMap* out);
+
 }  // namespace ghd

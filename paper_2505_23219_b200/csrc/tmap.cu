@@ -100,4 +100,23 @@ bool tmap_planes_slabs(ghd_ctx* c, const void* ptr, uint64_t planes, uint64_t ro
     return true;
 }
 
+bool tmap_bytes(ghd_ctx* c, const void* ptr, uint64_t rows, uint32_t box_rows, bool fp4, CUtensorMap* out) {
+    const TmapKey key{ptr, rows, 128, fp4 ? 4u : 8u, 0x6d78ull << 48, box_rows, 128};
+    if (cached(c, key, out)) return true;
+    EncodeTiledFn fn = encode_fn();
+    if (!fn) return false;
+    cuuint64_t dims[2] = {128, rows};
+    cuuint64_t strides[1] = {fp4 ? 64u : 128u};
+    cuuint32_t box[2] = {128, box_rows};
+    cuuint32_t estr[2] = {1, 1};
+    CUtensorMap tm;
+    if (fn(&tm, fp4 ? CU_TENSOR_MAP_DATA_TYPE_16U4_ALIGN16B : CU_TENSOR_MAP_DATA_TYPE_UINT8, 2, const_cast<void*>(ptr), dims, strides, box, estr,
+           CU_TENSOR_MAP_INTERLEAVE_NONE, CU_TENSOR_MAP_SWIZZLE_128B, CU_TENSOR_MAP_L2_PROMOTION_L2_256B,
+           CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE) != CUDA_SUCCESS)
+        return false;
+    remember(c, key, tm);
+    *out = tm;
+    return true;
+}
+
 }  // namespace ghd
