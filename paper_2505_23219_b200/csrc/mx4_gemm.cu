@@ -8,9 +8,11 @@
 // that a weight is read once for all; the epilogue adds them.
 //
 // As in the half-precision projection, 128 rows of w are the M of an MMA, the columns of x its N; a unit is one tile of 128 rows (MT = 1)
-// or two (MT = 2: two neighbours that share the loads of x, or a gate tile with its up tile), and the flattened (unit, k-step) space is cut
-// into equal ranges, one per CTA.  Units that several CTAs share are summed from their partial sums in the workspace, in the order of
-// the CTAs, each contributor finishing a slice once all have arrived (a bounded wait; every CTA is resident).
+// or two (MT = 2: two neighbours that share the loads of x, or a gate tile with its up tile).  Where there are fewer than half as many
+// units as SMs, a cluster of CTAs shares each, a part of k to every CTA, and adds up through distributed shared memory.
+// Otherwise the flattened (unit, k-step) space is cut into equal ranges, one per CTA: whoever has the first k-step of a unit finishes
+// it, with its own sums in registers, as the last of its range; the others have come to it first and left their sums in the workspace (a
+// bounded wait makes sure; every CTA is resident).  Both add in the order of k.
 //
 // The tensor cores cut off what they add below 2^-24 of the running sum, always towards zero, so a sum of 4096 loses 1.3e-6 of itself:
 // accumulators are taken out every CHUNK k-steps and added up in registers with rounding (6.5e-7 over 2048, measured).
@@ -32,7 +34,8 @@ using namespace tc;
 constexpr int THREADS = 320;            // producer warp, MMA warp, eight epilogue warps
 constexpr int MAX_STAGES = 10;
 constexpr int CHUNK = 16;               // k-steps of 128 that one accumulator takes
-constexpr int MAX_UNITS_SHARED = 1024;  // counters: arrivals in the first half of this many, departures in the second
+constexpr int MAX_WORKERS = 1024;       // CTAs at most: each has an arrival counter
+constexpr int MAX_SPLIT = 8;            // CTAs of a cluster
 constexpr int A_BYTES = TILE * TILE;    // a tile of 4-bit elements in shared memory, a byte each
 constexpr int SF_BYTES = 512;           // scales of 128 rows and 128 columns
 
@@ -42,10 +45,11 @@ struct Mx4Params {
     int per_group, groups, cols;        // rows of x are worked on in groups of per_group: cols = TERMS * per_group, up to a multiple of 16
     int sf_atoms;                       // ceil(cols / 128)
     int units, stages;                  // units: row units * groups, groups of one row unit behind one another
+    int split;                          // CTAs (a cluster) to a unit; 1: ranges of the flattened space
     long long total;                    // units * kt
     const uint8_t *scales, *scales2;    // of w, of the second matrix
     const uint8_t* x_scales;
-    float* part;                        // [CTA][2][MT * per_group][128]
+    float* part;                        // [CTA][MT * per_group][128]: sums of its first unit, if that began in another CTA's range
     int* counters;
     int* status;
     void* out;
@@ -95,6 +99,13 @@ __device__ __forceinline__ bool epi_all(bool ok) {
     asm volatile("{\n\t.reg .pred p, q;\n\tsetp.ne.b32 p, %1, 0;\n\tbar.red.and.pred q, 1, 256, p;\n\tselp.u32 %0, 1, 0, q;\n\t}" : "=r"(r) : "r"((uint32_t)ok) : "memory");
     return r != 0;
 }
+
+__device__ __forceinline__ float4 ld_cluster(uint32_t addr) {
+    float4 v;
+    asm volatile("ld.shared::cluster.v4.f32 {%0, %1, %2, %3}, [%4];" : "=f"(v.x), "=f"(v.y), "=f"(v.z), "=f"(v.w) : "r"(addr) : "memory");
+    return v;
+}
+__device__ __forceinline__ float silu_times(float g, float up) { return __fdividef(g * up, 1.f + exp2f(-1.4426950408889634f * g)); }
 
 // ---------------------------------------------------------------- x -> terms
 template <typename T> constexpr int TERMS = sizeof(T) == 2 ? 3 : 5;
@@ -168,29 +179,49 @@ k_mx4_gemm(const __grid_constant__ CUtensorMap tm_w, const __grid_constant__ CUt
     Smem* sm = reinterpret_cast<Smem*>(tiles + (size_t)p.stages * stage_bytes);
 
     const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31, cta = blockIdx.x, ctas = gridDim.x;
-    const long long it_beg = p.total * cta / ctas, it_end = p.total * (cta + 1) / ctas;
-    const int my_iters = (int)(it_end - it_beg);
+    int unit0, kc0, my_iters;
+    if (p.split > 1) {
+        const int rank = cta % p.split;
+        unit0 = cta / p.split;
+        kc0 = p.kt * rank / p.split;
+        my_iters = p.kt * (rank + 1) / p.split - kc0;
+    } else {
+        const long long beg = p.total * cta / ctas;
+        unit0 = (int)(beg / p.kt);
+        kc0 = (int)(beg - (long long)unit0 * p.kt);
+        my_iters = (int)(p.total * (cta + 1) / ctas - beg);
+    }
     const int prefill = my_iters < p.stages ? my_iters : p.stages;
-    const int unit0 = (int)(it_beg / p.kt), kc0 = (int)(it_beg - (long long)unit0 * p.kt);
     // tiles of a unit: the two of a pair, or one behind which there is none
-    auto tiles_of = [&](int unit) { return GATE || MT == 1 ? MT : (unit / p.groups) * MT + 1 < p.tiles ? 2 : 1; };
-    auto load_w = [&](uint32_t stage, int unit, int kc, uint32_t bar, uint64_t pol) {
-        const int ru = unit / p.groups, nt = tiles_of(unit);
-        mbar_expect_tx(bar, (uint32_t)nt * (TILE_CODES + SF_BYTES) + x_bytes);      // (the 4-bit tiles count as they lie in memory)
+    auto tiles_of = [&](int ru) { return GATE || MT == 1 ? MT : ru * MT + 1 < p.tiles ? 2 : 1; };
+    // Walks the k-steps of this CTA (divisions once a unit: they cost the loading thread as much as the loads of a step).
+    struct Cursor { int unit, kc, nt, xstep; long long tile; };
+    auto enter = [&](Cursor& c) {
+        const int ru = c.unit / p.groups;
+        c.nt = tiles_of(ru);
+        c.tile = (long long)(GATE ? ru : ru * MT) * p.kt + c.kc;
+        c.xstep = (c.unit - ru * p.groups) * p.kt + c.kc;
+    };
+    auto step = [&](Cursor& c) {
+        ++c.tile;
+        ++c.xstep;
+        if (++c.kc == p.kt) { c.kc = 0; ++c.unit; enter(c); }
+    };
+    auto load_w = [&](uint32_t stage, const Cursor& c, uint32_t bar, uint64_t pol) {
+        mbar_expect_tx(bar, (uint32_t)c.nt * (TILE_CODES + SF_BYTES) + x_bytes);      // (the 4-bit tiles count as they lie in memory)
         const uint32_t at = tiles_addr + stage * stage_bytes;
 #pragma unroll
         for (int t = 0; t < MT; ++t) {
-            if (t >= nt) break;
-            const long long tile = (long long)(GATE ? ru : ru * MT + t) * p.kt + kc;
+            if (t >= c.nt) break;
+            const long long tile = c.tile + (GATE ? 0 : t * p.kt);
             tma_load_2d(at + t * A_BYTES, GATE && t ? &tm_w2 : &tm_w, 0, (int)(tile * TILE), bar, pol);
             bulk_load(at + sa_off + t * SF_BYTES, (GATE && t ? p.scales2 : p.scales) + tile * TILE_SCALES, SF_BYTES, bar, pol);
         }
     };
-    auto load_x = [&](uint32_t stage, int unit, int kc, uint32_t bar, uint64_t pol) {
-        const int step = (unit % p.groups) * p.kt + kc;
+    auto load_x = [&](uint32_t stage, const Cursor& c, uint32_t bar, uint64_t pol) {
         const uint32_t at = tiles_addr + stage * stage_bytes;
-        tma_load_2d(at + b_off, &tm_x, 0, step * p.cols, bar, pol);
-        bulk_load(at + sb_off, p.x_scales + (size_t)step * p.sf_atoms * SF_BYTES, (uint32_t)p.sf_atoms * SF_BYTES, bar, pol);
+        tma_load_2d(at + b_off, &tm_x, 0, c.xstep * p.cols, bar, pol);
+        bulk_load(at + sb_off, p.x_scales + (size_t)c.xstep * p.sf_atoms * SF_BYTES, (uint32_t)p.sf_atoms * SF_BYTES, bar, pol);
     };
 
     if (threadIdx.x == 32) {
@@ -207,10 +238,9 @@ k_mx4_gemm(const __grid_constant__ CUtensorMap tm_w, const __grid_constant__ CUt
         // weights do not depend on the kernel before: the ring's first ones are on their way during set-up
         uint64_t pol;
         asm volatile("createpolicy.fractional.L2::evict_first.b64 %0, 1.0;" : "=l"(pol));
-        for (int i = 0, unit = unit0, kc = kc0; i < prefill; ++i) {
-            load_w(i, unit, kc, smem_u32(&sm->full[i]), pol);
-            if (++kc == p.kt) { kc = 0; ++unit; }
-        }
+        Cursor c{unit0, kc0};
+        enter(c);
+        for (int i = 0; i < prefill; ++i, step(c)) load_w(i, c, smem_u32(&sm->full[i]), pol);
     }
     if (warp == 1) {
         asm volatile("tcgen05.alloc.cta_group::1.sync.aligned.shared::cta.b32 [%0], 512;" ::"r"(smem_u32(&sm->tmem_base)) : "memory");
@@ -221,6 +251,7 @@ k_mx4_gemm(const __grid_constant__ CUtensorMap tm_w, const __grid_constant__ CUt
     tc_fence_after();
     const uint32_t tmem = sm->tmem_base;
     volatile int* abort_flag = &sm->abort_flag;
+    float* sums = reinterpret_cast<float*>(tiles);              // a CTA's sums of a unit that a cluster shares
 
     if (warp == 0) {
         if (lane == 0) {
@@ -228,24 +259,23 @@ k_mx4_gemm(const __grid_constant__ CUtensorMap tm_w, const __grid_constant__ CUt
             asm volatile("createpolicy.fractional.L2::evict_first.b64 %0, 1.0;" : "=l"(pol_stream));
             asm volatile("createpolicy.fractional.L2::evict_last.b64 %0, 1.0;" : "=l"(pol_keep));
             if (p.groups > 1) asm volatile("createpolicy.fractional.L2::evict_normal.b64 %0, 1.0;" : "=l"(pol_stream));     // read again by the next group
-            int unit = unit0, kc = kc0, issued = 0;
+            int issued = 0;
             uint32_t stage = 0, phase = 0;
             bool ok = true;
+            Cursor c{unit0, kc0};
+            enter(c);
             pdl_wait();                                        // x's terms belong to the kernel before until now
-            for (; issued < prefill; ++issued) {
-                load_x(issued, unit, kc, smem_u32(&sm->full[issued]), pol_keep);
-                if (++kc == p.kt) { kc = 0; ++unit; }
-            }
+            for (; issued < prefill; ++issued, step(c)) load_x(issued, c, smem_u32(&sm->full[issued]), pol_keep);
             if (prefill == p.stages) phase = 1; else stage = (uint32_t)prefill;
             for (int i = prefill; i < my_iters; ++i) {
                 ok = mbar_wait(smem_u32(&sm->empty[stage]), phase ^ 1, abort_flag, p.status, DEV_TIMEOUT_TMA);
                 if (!ok) break;
                 const uint32_t full = smem_u32(&sm->full[stage]);
-                load_w(stage, unit, kc, full, pol_stream);
-                load_x(stage, unit, kc, full, pol_keep);
+                load_w(stage, c, full, pol_stream);
+                load_x(stage, c, full, pol_keep);
+                step(c);
                 ++issued;
                 if (++stage == (uint32_t)p.stages) { stage = 0; phase ^= 1; }
-                if (++kc == p.kt) { kc = 0; ++unit; }
             }
             if (!ok) {                                         // nothing may be in flight when the CTA ends
                 const int inflight = issued < p.stages ? issued : p.stages;
@@ -268,7 +298,7 @@ k_mx4_gemm(const __grid_constant__ CUtensorMap tm_w, const __grid_constant__ CUt
                 if (chunks > 0) ok = mbar_wait(smem_u32(&sm->acc_empty), (chunks - 1) & 1, abort_flag, p.status, DEV_TIMEOUT_TMEM);
                 if (!ok) break;
                 tc_fence_after();
-                const int nt = tiles_of(unit);
+                const int nt = tiles_of(unit / p.groups);
                 for (int s = 0; s < take; ++s) {
                     ok = mbar_wait(smem_u32(&sm->full[stage]), phase, abort_flag, p.status, DEV_TIMEOUT_MMA);
                     if (!ok) break;
@@ -312,11 +342,10 @@ k_mx4_gemm(const __grid_constant__ CUtensorMap tm_w, const __grid_constant__ CUt
         float acc[MT][NODES];
         uint32_t chunks = 0;
         bool ok = true, waited = false;
-        int unit = unit0, kc = kc0, split_unit[2], n_split = 0;
+        int unit = unit0, kc = kc0;
         float* y = (float*)p.out;
         using T = typename std::conditional<P == 3, __half, float>::type;
         T* u = (T*)p.out;
-        auto silu = [](float g, float up) { return __fdividef(g * up, 1.f + exp2f(-1.4426950408889634f * g)); };
         for (int i = 0; i < my_iters && ok;) {
             const int first = kc, end = min(p.kt, kc + my_iters - i), g = unit % p.groups, ru = unit / p.groups;
             const int rows_here = min(p.per_group, p.n - g * p.per_group), mine = max(0, min(half, rows_here - j0));
@@ -351,7 +380,51 @@ k_mx4_gemm(const __grid_constant__ CUtensorMap tm_w, const __grid_constant__ CUt
             }
             if (!ok) break;
             if (!waited) { pdl_wait(); waited = true; }        // outputs and partial sums belong to the kernel before until now
-            if (first == 0 && end == p.kt) {
+            const bool whole = first == 0 && end == p.kt;
+            if (!whole && p.split > 1) {
+                // everything that was loaded has been read: the ring's memory takes the sums
+#pragma unroll
+                for (int t = 0; t < MT; ++t)
+#pragma unroll
+                    for (int e = 0; e < NODES; ++e)
+                        if (e < mine) sums[(t * p.per_group + j0 + e) * TILE + row] = acc[t][e];
+            } else if (first != 0) {
+                float* at = p.part + (size_t)cta * slot + row;
+#pragma unroll
+                for (int t = 0; t < MT; ++t)
+#pragma unroll
+                    for (int e = 0; e < NODES; ++e)
+                        if (e < mine) __stcg(at + (t * p.per_group + j0 + e) * TILE, acc[t][e]);
+                epi_all(true);
+                if (et == 0) atom_add_acq_rel_gpu(p.counters + (int)((((long long)unit * p.kt + 1) * ctas - 1) / p.total), 1);
+            } else {
+                if (!whole) {
+                    // the ones behind this CTA: those whose ranges reach into the unit
+                    const int others = (int)((((long long)unit * p.kt + p.kt) * ctas - 1) / p.total) - cta;
+                    if (et == 0) {
+                        uint32_t spin = 0;
+                        while (ld_acquire_gpu(p.counters + cta) != others) {
+                            if (++spin >= SPIN_LIMIT || *abort_flag) { *abort_flag = 1; atomicCAS(p.status, DEV_OK, DEV_TIMEOUT_GRID); ok = false; break; }
+                            __nanosleep(spin > 64 ? 64 : 20);
+                        }
+                        p.counters[cta] = 0;                     // ready for the next launch
+                    }
+                    ok = epi_all(ok);
+                    if (!ok) break;
+                    for (int o = 1; o <= others; ++o) {
+                        const float* at = p.part + (size_t)(cta + o) * slot + row;
+#pragma unroll
+                        for (int t = 0; t < MT; ++t)
+#pragma unroll
+                            for (int e = 0; e < NODES; e += 16) {
+                                float v[16];
+#pragma unroll
+                                for (int j = 0; j < 16; ++j) v[j] = e + j < mine ? __ldcg(at + (t * p.per_group + j0 + e + j) * TILE) : 0.f;
+#pragma unroll
+                                for (int j = 0; j < 16; ++j) acc[t][e + j] += v[j];
+                            }
+                    }
+                }
 #pragma unroll
                 for (int t = 0; t < (GATE ? 1 : MT); ++t) {
                     const int f = (GATE ? ru : ru * MT + t) * TILE + row;
@@ -359,80 +432,56 @@ k_mx4_gemm(const __grid_constant__ CUtensorMap tm_w, const __grid_constant__ CUt
                     for (int e = 0; e < NODES; ++e)
                         if (e < mine && f < p.m) {
                             const size_t at = (size_t)(g * p.per_group + j0 + e) * p.m + f;
-                            if constexpr (GATE) u[at] = from_f<T>(silu(acc[0][e], acc[1][e]));
+                            if constexpr (GATE) u[at] = from_f<T>(silu_times(acc[0][e], acc[1][e]));
                             else y[at] = acc[t][e];
                         }
                 }
-            } else {
-                float* mine_at = p.part + ((size_t)cta * 2 + (i == 0 ? 0 : 1)) * slot;
-#pragma unroll
-                for (int t = 0; t < MT; ++t)
-#pragma unroll
-                    for (int e = 0; e < NODES; ++e)
-                        if (e < mine) __stcg(mine_at + ((size_t)t * p.per_group + j0 + e) * TILE + row, acc[t][e]);
-                epi_all(true);
-                if (et == 0) atom_add_acq_rel_gpu(p.counters + (int)((((long long)unit * p.kt + 1) * ctas - 1) / p.total), 1);
-                split_unit[n_split++] = unit;
             }
             i += end - first;
             kc = end;
             if (kc == p.kt) { kc = 0; ++unit; }
         }
-        // The slices of this CTA's shared units: at most the first and the last of its range.
-        for (int q = 0; q < n_split && ok; ++q) {
-            const int un = split_unit[q], g = un % p.groups, ru = un / p.groups, nt = tiles_of(un);
-            const long long s0 = (long long)un * p.kt;
-            const int c0 = (int)(((s0 + 1) * ctas - 1) / p.total), cnt = (int)(((s0 + p.kt) * ctas - 1) / p.total) - c0 + 1;
-            if (et == 0) {
-                uint32_t spin = 0;
-                while (ld_acquire_gpu(p.counters + c0) != cnt) {
-                    if (++spin >= SPIN_LIMIT || *abort_flag) { *abort_flag = 1; atomicCAS(p.status, DEV_OK, DEV_TIMEOUT_GRID); ok = false; break; }
-                    __nanosleep(spin > 64 ? 64 : 20);
-                }
+    }
+    if (p.split > 1) {
+        // Every CTA of the cluster finishes a slice of the unit's sums; one that gave up takes part in the barriers only.
+        __syncwarp();
+        cluster_sync_all();
+        using T = typename std::conditional<P == 3, __half, float>::type;
+        const int rank = cta % p.split, ru = unit0 / p.groups, g = unit0 - ru * p.groups, nt = tiles_of(ru);
+        const int rows_here = min(p.per_group, p.n - g * p.per_group), vecs = (GATE ? 1 : nt) * rows_here * (TILE / 4);
+        const int lo = vecs * rank / p.split, hi = *abort_flag ? 0 : vecs * (rank + 1) / p.split;
+        const uint32_t base = smem_u32(sums);
+        for (int v = lo + (int)threadIdx.x; v < hi; v += THREADS) {
+            const int r4 = (v % (TILE / 4)) * 4, col = v / (TILE / 4), t = !GATE && MT == 2 && col >= rows_here ? 1 : 0, j = col - t * rows_here;
+            float4 sum[GATE ? 2 : 1];
+#pragma unroll
+            for (int h = 0; h < (GATE ? 2 : 1); ++h) {
+                const uint32_t off = base + (uint32_t)(((t + h) * p.per_group + j) * TILE + r4) * 4;
+                float4 b[MAX_SPLIT];
+#pragma unroll
+                for (int d = 0; d < MAX_SPLIT; ++d)
+                    if (d < p.split) b[d] = ld_cluster(mapa_shared(off, d));
+                float4 a = b[0];
+#pragma unroll
+                for (int d = 1; d < MAX_SPLIT; ++d)
+                    if (d < p.split) { a.x += b[d].x; a.y += b[d].y; a.z += b[d].z; a.w += b[d].w; }
+                sum[h] = a;
             }
-            ok = epi_all(ok);
-            if (!ok) break;
-            // the first contributor's sums are in its second slot if the unit is not the first of its range
-            const int slot_first = p.total * c0 / ctas < s0 ? 1 : 0;
-            const int rows_here = min(p.per_group, p.n - g * p.per_group), vecs = (GATE ? 1 : nt) * rows_here * (TILE / 4);
-            const int lo = (int)((long long)vecs * (cta - c0) / cnt), hi = (int)((long long)vecs * (cta - c0 + 1) / cnt);
-            for (int v = lo + et; v < hi; v += 256) {
-                const int r4 = (v % (TILE / 4)) * 4, col = v / (TILE / 4), t = col / rows_here, j = col - t * rows_here;
-                float4 sum[GATE ? 2 : 1];
+            const float s[4] = {sum[0].x, sum[0].y, sum[0].z, sum[0].w};
+            const int f = (GATE ? ru : ru * MT + t) * TILE + r4;
+            const size_t at = (size_t)(g * p.per_group + j) * p.m + f;
+            if constexpr (GATE) {
+                const float up[4] = {sum[GATE ? 1 : 0].x, sum[GATE ? 1 : 0].y, sum[GATE ? 1 : 0].z, sum[GATE ? 1 : 0].w};
 #pragma unroll
-                for (int h = 0; h < (GATE ? 2 : 1); ++h) {
-                    const size_t off = ((size_t)(t + h) * p.per_group + j) * TILE + r4;
-                    float4 a = make_float4(0.f, 0.f, 0.f, 0.f);
-                    for (int c = 0; c < cnt; c += 4) {
-                        float4 b[4];
+                for (int e = 0; e < 4; ++e)
+                    if (f + e < p.m) ((T*)p.out)[at + e] = from_f<T>(silu_times(s[e], up[e]));
+            } else {
 #pragma unroll
-                        for (int d = 0; d < 4; ++d)
-                            b[d] = c + d < cnt ? __ldcg(reinterpret_cast<const float4*>(p.part + ((size_t)(c0 + c + d) * 2 + (c + d == 0 ? slot_first : 0)) * slot + off)) : make_float4(0.f, 0.f, 0.f, 0.f);
-#pragma unroll
-                        for (int d = 0; d < 4; ++d) { a.x += b[d].x; a.y += b[d].y; a.z += b[d].z; a.w += b[d].w; }
-                    }
-                    sum[h] = a;
-                }
-                const float s[4] = {sum[0].x, sum[0].y, sum[0].z, sum[0].w};
-                const int f = (GATE ? ru : ru * MT + t) * TILE + r4;
-                const size_t at = (size_t)(g * p.per_group + j) * p.m + f;
-                if constexpr (GATE) {
-                    const float up[4] = {sum[GATE ? 1 : 0].x, sum[GATE ? 1 : 0].y, sum[GATE ? 1 : 0].z, sum[GATE ? 1 : 0].w};
-#pragma unroll
-                    for (int e = 0; e < 4; ++e)
-                        if (f + e < p.m) u[at + e] = from_f<T>(silu(s[e], up[e]));
-                } else {
-#pragma unroll
-                    for (int e = 0; e < 4; ++e)
-                        if (f + e < p.m) y[at + e] = s[e];
-                }
-            }
-            epi_all(true);
-            if (et == 0 && atom_add_acq_rel_gpu(p.counters + MAX_UNITS_SHARED + c0, 1) == cnt - 1) {
-                p.counters[c0] = 0;                              // everybody has passed the wait: ready for the next launch
-                p.counters[MAX_UNITS_SHARED + c0] = 0;
+                for (int e = 0; e < 4; ++e)
+                    if (f + e < p.m) ((float*)p.out)[at + e] = s[e];
             }
         }
+        cluster_sync_all();                                      // nobody leaves while its sums are being read
     }
     tc_fence_before();
     __syncthreads();
@@ -496,12 +545,23 @@ ghd_status go(ghd_ctx* c, const T* x, int64_t ld, bool wide, const ghd_mx4* w, c
     }
     const int warps = n * ((p.kt + 1) / 2);
     launch_k(c, false, k_mx4_terms<T>, (warps + 7) / 8, 256, 0, x, ld, n, (int)w->k, wide, p.kt, g.per, g.cols, g.atoms, (uint2*)terms, (uint32_t*)x_scales);
-    int ctas = c->sm_count < MAX_UNITS_SHARED ? c->sm_count : MAX_UNITS_SHARED;
+    int ctas = c->sm_count < MAX_WORKERS ? c->sm_count : MAX_WORKERS;
+    p.split = 1;
+    if (p.units * 2 <= ctas) {
+        p.split = ctas / p.units;
+        if (p.split > MAX_SPLIT) p.split = MAX_SPLIT;
+        if (p.split > p.kt) p.split = p.kt;
+        ctas = p.units * p.split;
+    } else if (p.units < ctas) {
+        // ranges of (q - 1) / q of a unit: each holds the border between two units, and nobody's range lies within one
+        for (int q = 2; q <= 64; ++q)
+            if ((long long)p.units * q % (q - 1) == 0 && (long long)p.units * q / (q - 1) <= ctas) { ctas = p.units * q / (q - 1); break; }
+    }
     if (ctas > p.total) ctas = (int)p.total;
     const size_t smem = 1024 + p.stages * stage + sizeof(Smem);
-    if (w2) launch_k(c, true, k_mx4_gemm<P, 2, true>, ctas, THREADS, smem, tw, tw2, tx, p);
-    else if (mt == 2) launch_k(c, true, k_mx4_gemm<P, 2, false>, ctas, THREADS, smem, tw, tw2, tx, p);
-    else launch_k(c, true, k_mx4_gemm<P, 1, false>, ctas, THREADS, smem, tw, tw2, tx, p);
+    if (w2) launch_kc(c, true, p.split, k_mx4_gemm<P, 2, true>, ctas, THREADS, smem, tw, tw2, tx, p);
+    else if (mt == 2) launch_kc(c, true, p.split, k_mx4_gemm<P, 2, false>, ctas, THREADS, smem, tw, tw2, tx, p);
+    else launch_kc(c, true, p.split, k_mx4_gemm<P, 1, false>, ctas, THREADS, smem, tw, tw2, tx, p);
     return GHD_OK;
 }
 
