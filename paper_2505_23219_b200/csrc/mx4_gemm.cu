@@ -31,7 +31,7 @@ namespace {
 using namespace mx4;
 using namespace tc;
 
-constexpr int THREADS = 320;            // producer warp, MMA warp, eight epilogue warps
+constexpr int THREADS = 352;            // weights' loads, MMAs, eight epilogue warps, x's loads
 constexpr int MAX_STAGES = 10;
 constexpr int CHUNK = 16;               // k-steps of 128 that one accumulator takes
 constexpr int MAX_WORKERS = 1024;       // CTAs at most: each has an arrival counter
@@ -45,6 +45,7 @@ struct Mx4Params {
     int per_group, groups, cols;        // rows of x are worked on in groups of per_group: cols = TERMS * per_group, up to a multiple of 16
     int sf_atoms;                       // ceil(cols / 128)
     int units, stages;                  // units: row units * groups, groups of one row unit behind one another
+    int ks;                             // k-steps of a stage at most (fewer at the end of a range or a unit)
     int split;                          // CTAs (a cluster) to a unit; 1: ranges of the flattened space
     long long total;                    // units * kt
     const uint8_t *scales, *scales2;    // of w, of the second matrix
@@ -54,6 +55,9 @@ struct Mx4Params {
     int* status;
     void* out;
 };
+
+// one k-step and, behind it, ks of them in one box: of w, of the second matrix, of the terms of x
+struct Mx4Maps { CUtensorMap w[2], w2[2], x[2]; };
 
 struct Smem {
     uint64_t full[MAX_STAGES], empty[MAX_STAGES];
@@ -71,8 +75,13 @@ __device__ __forceinline__ void bulk_load(uint32_t dst, const void* src, uint32_
 __device__ __forceinline__ uint64_t smem_desc_scales(uint32_t addr) {
     return (uint64_t)((addr & 0x3FFFFu) >> 4) | (uint64_t)(128 >> 4) << 32 | (uint64_t)1 << 46;
 }
-__device__ __forceinline__ void copy_scales(uint32_t tmem, uint32_t smem) {       // to four columns, the same in all four quarters of the lanes
-    asm volatile("tcgen05.cp.cta_group::1.32x128b.warpx4 [%0], %1;" ::"r"(tmem), "l"(smem_desc_scales(smem)) : "memory");
+__device__ __forceinline__ void copy_scales(uint32_t tmem, uint64_t desc) {       // to four columns, the same in all four quarters of the lanes
+    asm volatile("tcgen05.cp.cta_group::1.32x128b.warpx4 [%0], %1;" ::"r"(tmem), "l"(desc) : "memory");
+}
+__device__ __forceinline__ bool elect_one() {
+    uint32_t r;
+    asm volatile("{\n\t.reg .pred p;\n\telect.sync _|p, 0xffffffff;\n\tselp.u32 %0, 1, 0, p;\n\t}" : "=r"(r));
+    return r != 0;
 }
 // kind::mxf8f6f4: A e2m1 (5), B e4m3 (0), scales e8m0, D float, M = 128; byte q of the scale words belongs to the q-th 32 of 128 columns
 __device__ __forceinline__ uint32_t instr_desc_mx(int cols, int q) {
@@ -166,16 +175,16 @@ __global__ void __launch_bounds__(256) k_mx4_terms(const T* __restrict__ x, int6
 // ---------------------------------------------------------------- product
 template <int P, int MT, bool GATE>
 __global__ void __launch_bounds__(THREADS, 1)
-k_mx4_gemm(const __grid_constant__ CUtensorMap tm_w, const __grid_constant__ CUtensorMap tm_w2, const __grid_constant__ CUtensorMap tm_x, const Mx4Params p) {
+k_mx4_gemm(const __grid_constant__ Mx4Maps maps, const Mx4Params p) {
     static_assert(!GATE || MT == 2, "a gate tile and its up tile");
     extern __shared__ uint8_t smem_raw[];
     const uint32_t raw_addr = smem_u32(smem_raw);
     uint8_t* tiles = smem_raw + ((1024u - (raw_addr & 1023u)) & 1023u);
     const uint32_t tiles_addr = smem_u32(tiles);
-    // a stage: MT weight tiles | columns of x | scales of the tiles | scales of x
-    const uint32_t b_off = MT * A_BYTES, sa_off = b_off + (uint32_t)p.cols * TILE, sb_off = sa_off + MT * SF_BYTES;
-    const uint32_t stage_bytes = (sb_off + (uint32_t)p.sf_atoms * SF_BYTES + 1023u) & ~1023u;
-    const uint32_t x_bytes = (uint32_t)p.cols * TILE + (uint32_t)p.sf_atoms * SF_BYTES;
+    // a stage: weight tiles [MT][ks] | columns of x [ks] | scales of the tiles [MT][ks] | scales of x [ks]
+    const uint32_t x_tile = (uint32_t)p.cols * TILE, x_sf = (uint32_t)p.sf_atoms * SF_BYTES;
+    const uint32_t b_off = MT * p.ks * A_BYTES, sa_off = b_off + p.ks * x_tile, sb_off = sa_off + MT * p.ks * SF_BYTES;
+    const uint32_t stage_bytes = (sb_off + p.ks * x_sf + 1023u) & ~1023u;
     Smem* sm = reinterpret_cast<Smem*>(tiles + (size_t)p.stages * stage_bytes);
 
     const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31, cta = blockIdx.x, ctas = gridDim.x;
@@ -191,43 +200,55 @@ k_mx4_gemm(const __grid_constant__ CUtensorMap tm_w, const __grid_constant__ CUt
         kc0 = (int)(beg - (long long)unit0 * p.kt);
         my_iters = (int)(p.total * (cta + 1) / ctas - beg);
     }
-    const int prefill = my_iters < p.stages ? my_iters : p.stages;
     // tiles of a unit: the two of a pair, or one behind which there is none
     auto tiles_of = [&](int ru) { return GATE || MT == 1 ? MT : ru * MT + 1 < p.tiles ? 2 : 1; };
-    // Walks the k-steps of this CTA (divisions once a unit: they cost the loading thread as much as the loads of a step).
-    struct Cursor { int unit, kc, nt, xstep; long long tile; };
+    // Walks the stages of this CTA (divisions once a unit: they cost a loading thread as much as the loads of a stage).
+    struct Cursor { int unit, kc, left, take, nt, xstep; long long tile; };
     auto enter = [&](Cursor& c) {
         const int ru = c.unit / p.groups;
         c.nt = tiles_of(ru);
         c.tile = (long long)(GATE ? ru : ru * MT) * p.kt + c.kc;
         c.xstep = (c.unit - ru * p.groups) * p.kt + c.kc;
     };
-    auto step = [&](Cursor& c) {
-        ++c.tile;
-        ++c.xstep;
-        if (++c.kc == p.kt) { c.kc = 0; ++c.unit; enter(c); }
+    auto size = [&](Cursor& c) { c.take = min(p.ks, min(p.kt - c.kc, c.left)); };
+    auto begin = [&] {
+        Cursor c{unit0, kc0, my_iters};
+        enter(c);
+        size(c);
+        return c;
     };
-    auto load_w = [&](uint32_t stage, const Cursor& c, uint32_t bar, uint64_t pol) {
-        mbar_expect_tx(bar, (uint32_t)c.nt * (TILE_CODES + SF_BYTES) + x_bytes);      // (the 4-bit tiles count as they lie in memory)
-        const uint32_t at = tiles_addr + stage * stage_bytes;
+    auto step = [&](Cursor& c) {
+        c.tile += c.take;
+        c.xstep += c.take;
+        c.left -= c.take;
+        if ((c.kc += c.take) == p.kt) { c.kc = 0; ++c.unit; enter(c); }
+        size(c);
+    };
+    auto load_w = [&](uint32_t stage, const Cursor& c, uint64_t pol) {
+        const uint32_t at = tiles_addr + stage * stage_bytes, bar = smem_u32(&sm->full[stage]);
+        mbar_expect_tx(bar, (uint32_t)c.take * ((uint32_t)c.nt * (TILE_CODES + SF_BYTES) + x_tile + x_sf));     // (the 4-bit tiles count as they lie in memory)
 #pragma unroll
         for (int t = 0; t < MT; ++t) {
             if (t >= c.nt) break;
             const long long tile = c.tile + (GATE ? 0 : t * p.kt);
-            tma_load_2d(at + t * A_BYTES, GATE && t ? &tm_w2 : &tm_w, 0, (int)(tile * TILE), bar, pol);
-            bulk_load(at + sa_off + t * SF_BYTES, (GATE && t ? p.scales2 : p.scales) + tile * TILE_SCALES, SF_BYTES, bar, pol);
+            tma_load_2d(at + t * p.ks * A_BYTES, GATE && t ? &maps.w2[c.take - 1] : &maps.w[c.take - 1], 0, (int)(tile * TILE), bar, pol);
         }
     };
-    auto load_x = [&](uint32_t stage, const Cursor& c, uint32_t bar, uint64_t pol) {
-        const uint32_t at = tiles_addr + stage * stage_bytes;
-        tma_load_2d(at + b_off, &tm_x, 0, c.xstep * p.cols, bar, pol);
-        bulk_load(at + sb_off, p.x_scales + (size_t)c.xstep * p.sf_atoms * SF_BYTES, (uint32_t)p.sf_atoms * SF_BYTES, bar, pol);
+    auto load_x = [&](uint32_t stage, const Cursor& c, uint64_t pol) {
+        const uint32_t at = tiles_addr + stage * stage_bytes, bar = smem_u32(&sm->full[stage]);
+        tma_load_2d(at + b_off, &maps.x[c.take - 1], 0, c.xstep * p.cols, bar, pol);
+        bulk_load(at + sb_off, p.x_scales + (size_t)c.xstep * x_sf, c.take * x_sf, bar, pol);
+    };
+    auto load_scales = [&](uint32_t stage, const Cursor& c, uint64_t pol) {
+        const uint32_t at = tiles_addr + stage * stage_bytes, bar = smem_u32(&sm->full[stage]);
+#pragma unroll
+        for (int t = 0; t < MT; ++t) {
+            if (t >= c.nt) break;
+            const long long tile = c.tile + (GATE ? 0 : t * p.kt);
+            bulk_load(at + sa_off + t * p.ks * SF_BYTES, (GATE && t ? p.scales2 : p.scales) + tile * TILE_SCALES, c.take * SF_BYTES, bar, pol);
+        }
     };
 
-    if (threadIdx.x == 32) {
-        asm volatile("prefetch.tensormap [%0];" ::"l"(&tm_w) : "memory");
-        asm volatile("prefetch.tensormap [%0];" ::"l"(&tm_x) : "memory");
-    }
     if (threadIdx.x == 0) {
         for (int s = 0; s < p.stages; ++s) { mbar_init(smem_u32(&sm->full[s]), 1); mbar_init(smem_u32(&sm->empty[s]), 1); }
         mbar_init(smem_u32(&sm->acc_full), 1);
@@ -235,12 +256,6 @@ k_mx4_gemm(const __grid_constant__ CUtensorMap tm_w, const __grid_constant__ CUt
         mbar_init(smem_u32(&sm->drain), 1);
         sm->abort_flag = 0;
         asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
-        // weights do not depend on the kernel before: the ring's first ones are on their way during set-up
-        uint64_t pol;
-        asm volatile("createpolicy.fractional.L2::evict_first.b64 %0, 1.0;" : "=l"(pol));
-        Cursor c{unit0, kc0};
-        enter(c);
-        for (int i = 0; i < prefill; ++i, step(c)) load_w(i, c, smem_u32(&sm->full[i]), pol);
     }
     if (warp == 1) {
         asm volatile("tcgen05.alloc.cta_group::1.sync.aligned.shared::cta.b32 [%0], 512;" ::"r"(smem_u32(&sm->tmem_base)) : "memory");
@@ -254,26 +269,18 @@ k_mx4_gemm(const __grid_constant__ CUtensorMap tm_w, const __grid_constant__ CUt
     float* sums = reinterpret_cast<float*>(tiles);              // a CTA's sums of a unit that a cluster shares
 
     if (warp == 0) {
+        // Weights do not depend on the kernel before: the ring's first ones are under way before the terms of x are there.
         if (lane == 0) {
-            uint64_t pol_stream, pol_keep;
-            asm volatile("createpolicy.fractional.L2::evict_first.b64 %0, 1.0;" : "=l"(pol_stream));
-            asm volatile("createpolicy.fractional.L2::evict_last.b64 %0, 1.0;" : "=l"(pol_keep));
-            if (p.groups > 1) asm volatile("createpolicy.fractional.L2::evict_normal.b64 %0, 1.0;" : "=l"(pol_stream));     // read again by the next group
-            int issued = 0;
+            uint64_t pol;
+            asm volatile("createpolicy.fractional.L2::evict_first.b64 %0, 1.0;" : "=l"(pol));
+            if (p.groups > 1) asm volatile("createpolicy.fractional.L2::evict_normal.b64 %0, 1.0;" : "=l"(pol));     // read again by the next group
             uint32_t stage = 0, phase = 0;
+            int issued = 0;
             bool ok = true;
-            Cursor c{unit0, kc0};
-            enter(c);
-            pdl_wait();                                        // x's terms belong to the kernel before until now
-            for (; issued < prefill; ++issued, step(c)) load_x(issued, c, smem_u32(&sm->full[issued]), pol_keep);
-            if (prefill == p.stages) phase = 1; else stage = (uint32_t)prefill;
-            for (int i = prefill; i < my_iters; ++i) {
-                ok = mbar_wait(smem_u32(&sm->empty[stage]), phase ^ 1, abort_flag, p.status, DEV_TIMEOUT_TMA);
+            for (Cursor c = begin(); c.left > 0; step(c)) {
+                if (issued >= p.stages) ok = mbar_wait(smem_u32(&sm->empty[stage]), phase ^ 1, abort_flag, p.status, DEV_TIMEOUT_TMA);
                 if (!ok) break;
-                const uint32_t full = smem_u32(&sm->full[stage]);
-                load_w(stage, c, full, pol_stream);
-                load_x(stage, c, full, pol_keep);
-                step(c);
+                load_w(stage, c, pol);
                 ++issued;
                 if (++stage == (uint32_t)p.stages) { stage = 0; phase ^= 1; }
             }
@@ -285,53 +292,81 @@ k_mx4_gemm(const __grid_constant__ CUtensorMap tm_w, const __grid_constant__ CUt
                 }
             }
         }
-    } else if (warp == 1) {
+    } else if (warp == 10) {
+        // A thread takes 65 ns to start a copy, so that one could not keep up with the memory: this one starts the other half of them.
         if (lane == 0) {
-            // columns of tensor memory: the accumulators, then the scales of every stage (written again only after the MMAs of the
-            // stage's last use are through, which the ring makes sure of)
-            const uint32_t sf_cols = 4u * (MT + p.sf_atoms), sf0 = tmem + (uint32_t)(MT * p.cols);
-            uint32_t stage = 0, phase = 0, chunks = 0;
+            uint64_t pol, pol_keep;
+            asm volatile("createpolicy.fractional.L2::evict_first.b64 %0, 1.0;" : "=l"(pol));
+            if (p.groups > 1) asm volatile("createpolicy.fractional.L2::evict_normal.b64 %0, 1.0;" : "=l"(pol));
+            asm volatile("createpolicy.fractional.L2::evict_last.b64 %0, 1.0;" : "=l"(pol_keep));
+            uint32_t stage = 0, phase = 0;
+            int issued = 0;
             bool ok = true;
-            int unit = unit0, kc = kc0;
-            for (int i = 0; i < my_iters && ok;) {
-                int take = min(min(p.kt - kc, CHUNK), my_iters - i);
-                if (chunks > 0) ok = mbar_wait(smem_u32(&sm->acc_empty), (chunks - 1) & 1, abort_flag, p.status, DEV_TIMEOUT_TMEM);
+            pdl_wait();                                        // x's terms belong to the kernel before until now
+            for (Cursor c = begin(); c.left > 0; step(c)) {
+                if (issued >= p.stages) ok = mbar_wait(smem_u32(&sm->empty[stage]), phase ^ 1, abort_flag, p.status, DEV_TIMEOUT_TMA);
                 if (!ok) break;
-                tc_fence_after();
-                const int nt = tiles_of(unit / p.groups);
-                for (int s = 0; s < take; ++s) {
-                    ok = mbar_wait(smem_u32(&sm->full[stage]), phase, abort_flag, p.status, DEV_TIMEOUT_MMA);
-                    if (!ok) break;
-                    tc_fence_after();
-                    const uint32_t at = tiles_addr + stage * stage_bytes, sfa = sf0 + stage * sf_cols, sfb = sfa + 4 * MT;
-#pragma unroll
-                    for (int t = 0; t < MT; ++t)
-                        if (t < nt) copy_scales(sfa + 4 * t, at + sa_off + t * SF_BYTES);
-                    for (int a = 0; a < p.sf_atoms; ++a) copy_scales(sfb + 4 * a, at + sb_off + a * SF_BYTES);
-                    const uint64_t bdesc = smem_desc_sw128(at + b_off);
-#pragma unroll
-                    for (int t = 0; t < MT; ++t) {
-                        if (t >= nt) break;
-                        const uint64_t adesc = smem_desc_sw128(at + t * A_BYTES);
-#pragma unroll
-                        for (int q = 0; q < 4; ++q)
-                            mma_mx(tmem + t * p.cols, adesc + q * 2, bdesc + q * 2, instr_desc_mx(p.cols, q), sfa + 4 * t, sfb, s > 0 || q > 0);
-                    }
-                    tc_commit(smem_u32(&sm->empty[stage]));
-                    if (++stage == (uint32_t)p.stages) { stage = 0; phase ^= 1; }
-                }
-                if (!ok) break;
-                tc_commit(smem_u32(&sm->acc_full));
-                ++chunks;
-                i += take;
-                kc += take;
-                if (kc == p.kt) { kc = 0; ++unit; }
-            }
-            if (!ok) {                                         // no MMA may run when the tensor memory goes
-                tc_commit(smem_u32(&sm->drain));
-                for (uint32_t spin = 0; spin < SPIN_LIMIT && !mbar_try(smem_u32(&sm->drain), 0); ++spin) __nanosleep(64);
+                load_x(stage, c, pol_keep);
+                load_scales(stage, c, pol);
+                ++issued;
+                if (++stage == (uint32_t)p.stages) { stage = 0; phase ^= 1; }
             }
         }
+    } else if (warp == 1) {
+        // The whole warp walks along, one lane issues: values that all lanes share sit in uniform registers, where the instructions take
+        // their operands (from one lane's registers each MMA took 200 cycles to issue, N = 48 needs 46).
+        // Columns of tensor memory: the accumulators, then the scales of every stage (written again only after the MMAs of the stage's last
+        // use are through, which the ring makes sure of).
+        const bool leader = elect_one();
+        const uint32_t sf_step = 4u * (MT + p.sf_atoms), sf0 = tmem + (uint32_t)(MT * p.cols), idesc = instr_desc_mx(p.cols, 0);
+        uint32_t stage = 0, phase = 0, chunks = 0;
+        int in_chunk = 0;
+        bool ok = true;
+        for (Cursor c = begin(); c.left > 0;) {
+            if (in_chunk == 0 && chunks > 0) ok = mbar_wait(smem_u32(&sm->acc_empty), (chunks - 1) & 1, abort_flag, p.status, DEV_TIMEOUT_TMEM);
+            if (!__all_sync(0xffffffffu, ok)) { ok = false; break; }
+            ok = mbar_wait(smem_u32(&sm->full[stage]), phase, abort_flag, p.status, DEV_TIMEOUT_MMA);
+            if (!__all_sync(0xffffffffu, ok)) { ok = false; break; }
+            tc_fence_after();
+            const uint32_t at = tiles_addr + stage * stage_bytes;
+            const int unit = c.unit, take = c.take, nt = c.nt;
+            const uint32_t acc0 = in_chunk > 0;
+            in_chunk += take;
+            step(c);
+            const bool last = in_chunk == CHUNK || c.unit != unit || c.left == 0;
+            if (leader) {
+                uint64_t adesc = smem_desc_sw128(at), bdesc = smem_desc_sw128(at + b_off), sad = smem_desc_scales(at + sa_off), sbd = smem_desc_scales(at + sb_off);
+                uint32_t sfa = sf0 + stage * p.ks * sf_step;
+                for (int s = 0; s < take; ++s) {
+                    const uint32_t sfb = sfa + 4 * MT;
+                    copy_scales(sfa, sad);
+                    if (MT == 2 && nt == 2) copy_scales(sfa + 4, sad + (p.ks * SF_BYTES >> 4));
+                    copy_scales(sfb, sbd);
+                    if (p.sf_atoms == 2) copy_scales(sfb + 4, sbd + (SF_BYTES >> 4));
+#pragma unroll
+                    for (int q = 0; q < 4; ++q) mma_mx(tmem, adesc + q * 2, bdesc + q * 2, idesc + q * 0x20000010u, sfa, sfb, q > 0 ? 1u : s > 0 ? 1u : acc0);
+                    if (MT == 2 && nt == 2)
+#pragma unroll
+                        for (int q = 0; q < 4; ++q)
+                            mma_mx(tmem + p.cols, adesc + (p.ks * A_BYTES >> 4) + q * 2, bdesc + q * 2, idesc + q * 0x20000010u, sfa + 4, sfb, q > 0 ? 1u : s > 0 ? 1u : acc0);
+                    adesc += A_BYTES >> 4;
+                    bdesc += x_tile >> 4;
+                    sad += SF_BYTES >> 4;
+                    sbd += x_sf >> 4;
+                    sfa += sf_step;
+                }
+                tc_commit(smem_u32(&sm->empty[stage]));
+                if (last) tc_commit(smem_u32(&sm->acc_full));
+            }
+            __syncwarp();
+            if (last) { ++chunks; in_chunk = 0; }
+            if (++stage == (uint32_t)p.stages) { stage = 0; phase ^= 1; }
+        }
+        if (!ok && leader) {                                   // no MMA may run when the tensor memory goes
+            tc_commit(smem_u32(&sm->drain));
+            for (uint32_t spin = 0; spin < SPIN_LIMIT && !mbar_try(smem_u32(&sm->drain), 0); ++spin) __nanosleep(64);
+        }
+        __syncwarp();
     } else {
         // Epilogue warps 2 .. 9: the lanes of a warp are 32 rows of w; the first four warps take the first half of the rows of x, the others
         // the second, in eights.
@@ -516,10 +551,11 @@ ghd_status go(ghd_ctx* c, const T* x, int64_t ld, bool wide, const ghd_mx4* w, c
     const int mt = w2 || g.cols > 64 ? 2 : 1;
     p.units = (w2 ? p.tiles : (p.tiles + mt - 1) / mt) * g.groups;
     p.total = (long long)p.units * p.kt;
-    const size_t stage = ((size_t)mt * (A_BYTES + SF_BYTES) + (size_t)g.cols * TILE + (size_t)g.atoms * SF_BYTES + 1023) / 1024 * 1024;
+    p.ks = mt == 1 ? 2 : 1;                                      // (2 * cols rows of x are one box then)
+    const size_t stage = (p.ks * ((size_t)mt * (A_BYTES + SF_BYTES) + (size_t)g.cols * TILE + (size_t)g.atoms * SF_BYTES) + 1023) / 1024 * 1024;
     p.stages = (int)((227 * 1024 - 1024 - sizeof(Smem)) / stage);
     if (p.stages > MAX_STAGES) p.stages = MAX_STAGES;
-    const int sf_room = (512 - mt * g.cols) / (4 * (mt + g.atoms));
+    const int sf_room = (512 - mt * g.cols) / (4 * p.ks * (mt + g.atoms));
     if (p.stages > sf_room) p.stages = sf_room;
     p.scales = (const uint8_t*)w->scales;
     p.scales2 = w2 ? (const uint8_t*)w2->scales : nullptr;
@@ -530,17 +566,32 @@ ghd_status go(ghd_ctx* c, const T* x, int64_t ld, bool wide, const ghd_mx4* w, c
     p.counters = c->counters;
     p.status = c->status;
     p.out = out;
-    CUtensorMap tw, tw2, tx;
+    Mx4Maps maps;
     const uint64_t rows = (uint64_t)p.tiles * p.kt * TILE;
-    if (!tmap_bytes(c, w->codes, rows, TILE, true, &tw) || (w2 && !tmap_bytes(c, w2->codes, rows, TILE, true, &tw2)) ||
-        !tmap_bytes(c, terms, (uint64_t)g.groups * p.kt * g.cols, (uint32_t)g.cols, false, &tx))
-        return fail(c, GHD_ECUDA, "mx4: tensor map encoding failed");
-    if (!w2) tw2 = tw;
+    for (int q = 0; q < p.ks; ++q)
+        if (!tmap_bytes(c, w->codes, rows, TILE * (q + 1), true, &maps.w[q]) || !tmap_bytes(c, (w2 ? w2 : w)->codes, rows, TILE * (q + 1), true, &maps.w2[q]) ||
+            !tmap_bytes(c, terms, (uint64_t)g.groups * p.kt * g.cols, (uint32_t)(g.cols * (q + 1)), false, &maps.x[q]))
+            return fail(c, GHD_ECUDA, "mx4: tensor map encoding failed");
+    for (int q = p.ks; q < 2; ++q) { maps.w[q] = maps.w[0]; maps.w2[q] = maps.w2[0]; maps.x[q] = maps.x[0]; }
     if (!c->attr_mx4) {
         const void* kernels[] = {(const void*)k_mx4_gemm<3, 1, false>, (const void*)k_mx4_gemm<3, 2, false>, (const void*)k_mx4_gemm<3, 2, true>,
                                  (const void*)k_mx4_gemm<5, 1, false>, (const void*)k_mx4_gemm<5, 2, false>, (const void*)k_mx4_gemm<5, 2, true>};
         for (const void* f : kernels)
             if (cudaFuncSetAttribute(f, cudaFuncAttributeMaxDynamicSharedMemorySize, 227 * 1024) != cudaSuccess) return check_cuda(c, "mx4: shared memory");
+        // clusters that the device holds at a time (they do not straddle its groups of SMs): fewer than SMs / size for the larger ones
+        for (int k = 2; k <= MAX_SPLIT; ++k) {
+            cudaLaunchConfig_t cfg = {};
+            cfg.gridDim = dim3(k);
+            cfg.blockDim = dim3(THREADS);
+            cfg.dynamicSmemBytes = 227 * 1024;
+            cudaLaunchAttribute attr;
+            attr.id = cudaLaunchAttributeClusterDimension;
+            attr.val.clusterDim.x = (unsigned)k;
+            attr.val.clusterDim.y = attr.val.clusterDim.z = 1;
+            cfg.attrs = &attr;
+            cfg.numAttrs = 1;
+            if (cudaOccupancyMaxActiveClusters(&c->mx4_clusters[k], k_mx4_gemm<P, 1, false>, &cfg) != cudaSuccess) return check_cuda(c, "mx4: clusters");
+        }
         c->attr_mx4 = true;
     }
     const int warps = n * ((p.kt + 1) / 2);
@@ -548,9 +599,8 @@ ghd_status go(ghd_ctx* c, const T* x, int64_t ld, bool wide, const ghd_mx4* w, c
     int ctas = c->sm_count < MAX_WORKERS ? c->sm_count : MAX_WORKERS;
     p.split = 1;
     if (p.units * 2 <= ctas) {
-        p.split = ctas / p.units;
-        if (p.split > MAX_SPLIT) p.split = MAX_SPLIT;
-        if (p.split > p.kt) p.split = p.kt;
+        for (int k = 2; k <= MAX_SPLIT && k <= p.kt; ++k)
+            if (c->mx4_clusters[k] >= p.units) p.split = k;
         ctas = p.units * p.split;
     } else if (p.units < ctas) {
         // ranges of (q - 1) / q of a unit: each holds the border between two units, and nobody's range lies within one
@@ -559,9 +609,10 @@ ghd_status go(ghd_ctx* c, const T* x, int64_t ld, bool wide, const ghd_mx4* w, c
     }
     if (ctas > p.total) ctas = (int)p.total;
     const size_t smem = 1024 + p.stages * stage + sizeof(Smem);
-    if (w2) launch_kc(c, true, p.split, k_mx4_gemm<P, 2, true>, ctas, THREADS, smem, tw, tw2, tx, p);
-    else if (mt == 2) launch_kc(c, true, p.split, k_mx4_gemm<P, 2, false>, ctas, THREADS, smem, tw, tw2, tx, p);
-    else launch_kc(c, true, p.split, k_mx4_gemm<P, 1, false>, ctas, THREADS, smem, tw, tw2, tx, p);
+    if (p.stages < 2 || p.stages * stage < (size_t)mt * g.per * TILE * sizeof(float)) return fail(c, GHD_EUNSUPPORTED, "mx4: no room for a ring of stages");
+    if (w2) launch_kc(c, true, p.split, k_mx4_gemm<P, 2, true>, ctas, THREADS, smem, maps, p);
+    else if (mt == 2) launch_kc(c, true, p.split, k_mx4_gemm<P, 2, false>, ctas, THREADS, smem, maps, p);
+    else launch_kc(c, true, p.split, k_mx4_gemm<P, 1, false>, ctas, THREADS, smem, maps, p);
     return GHD_OK;
 }
 
