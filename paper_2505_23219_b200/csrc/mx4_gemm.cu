@@ -14,8 +14,9 @@
 // it, with its own sums in registers, as the last of its range; the others have come to it first and left their sums in the workspace (a
 // bounded wait makes sure; every CTA is resident).  Both add in the order of k.
 //
-// The tensor cores cut off what they add below 2^-24 of the running sum, always towards zero, so a sum of 4096 loses 1.3e-6 of itself:
-// accumulators are taken out every CHUNK k-steps and added up in registers with rounding (6.5e-7 over 2048, measured).
+// The tensor cores cut off what they add below 2^-24 of the running sum, so that long sums lose more than rounded ones (relative error of 4096 terms: 4e-8 for
+// normal weights, 1.3e-6 for scales that differ by 2^20, measured):
+// accumulators are taken out every CHUNK k-steps and added up in registers with rounding.
 #include <cuda.h>
 #include <cuda_fp8.h>
 
@@ -33,7 +34,7 @@ using namespace tc;
 
 constexpr int THREADS = 352;            // weights' loads, MMAs, eight epilogue warps, x's loads
 constexpr int MAX_STAGES = 10;
-constexpr int CHUNK = 16;               // k-steps of 128 that one accumulator takes
+constexpr int CHUNK = 64;               // k-steps of 128 that one accumulator takes
 constexpr int MAX_WORKERS = 1024;       // CTAs at most: each has an arrival counter
 constexpr int MAX_SPLIT = 8;            // CTAs of a cluster
 constexpr int A_BYTES = TILE * TILE;    // a tile of 4-bit elements in shared memory, a byte each
@@ -45,7 +46,6 @@ struct Mx4Params {
     int per_group, groups, cols;        // rows of x are worked on in groups of per_group: cols = TERMS * per_group, up to a multiple of 16
     int sf_atoms;                       // ceil(cols / 128)
     int units, stages;                  // units: row units * groups, groups of one row unit behind one another
-    int ks;                             // k-steps of a stage at most (fewer at the end of a range or a unit)
     int split;                          // CTAs (a cluster) to a unit; 1: ranges of the flattened space
     long long total;                    // units * kt
     const uint8_t *scales, *scales2;    // of w, of the second matrix
@@ -87,11 +87,19 @@ __device__ __forceinline__ bool elect_one() {
 __device__ __forceinline__ uint32_t instr_desc_mx(int cols, int q) {
     return 5u << 7 | (uint32_t)(cols >> 3) << 17 | 1u << 23 | (uint32_t)(TILE >> 4) << 24 | (uint32_t)q << 29 | (uint32_t)q << 4;
 }
-__device__ __forceinline__ void mma_mx(uint32_t d, uint64_t a, uint64_t b, uint32_t idesc, uint32_t sfa, uint32_t sfb, uint32_t accumulate) {
+// the four MMAs of a k-step (32 columns of 128 each), in one statement so that their operands differ by constants only
+__device__ __forceinline__ void mma_step(uint32_t d, uint64_t a, uint64_t b, uint32_t idesc, uint32_t sfa, uint32_t sfb, uint32_t accumulate) {
     asm volatile(
-        "{\n\t.reg .pred p;\n\t"
+        "{\n\t.reg .pred p, t;\n\t.reg .b64 a1, a2, a3, b1, b2, b3;\n\t.reg .b32 i1, i2, i3;\n\t"
         "setp.ne.b32 p, %6, 0;\n\t"
-        "tcgen05.mma.cta_group::1.kind::mxf8f6f4.block_scale.scale_vec::1X [%0], %1, %2, %3, [%4], [%5], p;\n\t}"
+        "setp.ne.b32 t, 1, 0;\n\t"
+        "add.s64 a1, %1, 2;\n\tadd.s64 a2, %1, 4;\n\tadd.s64 a3, %1, 6;\n\t"
+        "add.s64 b1, %2, 2;\n\tadd.s64 b2, %2, 4;\n\tadd.s64 b3, %2, 6;\n\t"
+        "add.u32 i1, %3, 0x20000010;\n\tadd.u32 i2, %3, 0x40000020;\n\tadd.u32 i3, %3, 0x60000030;\n\t"
+        "tcgen05.mma.cta_group::1.kind::mxf8f6f4.block_scale.scale_vec::1X [%0], %1, %2, %3, [%4], [%5], p;\n\t"
+        "tcgen05.mma.cta_group::1.kind::mxf8f6f4.block_scale.scale_vec::1X [%0], a1, b1, i1, [%4], [%5], t;\n\t"
+        "tcgen05.mma.cta_group::1.kind::mxf8f6f4.block_scale.scale_vec::1X [%0], a2, b2, i2, [%4], [%5], t;\n\t"
+        "tcgen05.mma.cta_group::1.kind::mxf8f6f4.block_scale.scale_vec::1X [%0], a3, b3, i3, [%4], [%5], t;\n\t}"
         ::"r"(d), "l"(a), "l"(b), "r"(idesc), "r"(sfa), "r"(sfb), "r"(accumulate) : "memory");
 }
 __device__ __forceinline__ void ld8(uint32_t taddr, uint32_t* r) {                // 8 columns of this warp's 32 lanes; not there until ld_wait
@@ -177,14 +185,15 @@ template <int P, int MT, bool GATE>
 __global__ void __launch_bounds__(THREADS, 1)
 k_mx4_gemm(const __grid_constant__ Mx4Maps maps, const Mx4Params p) {
     static_assert(!GATE || MT == 2, "a gate tile and its up tile");
+    constexpr int KS = MT == 1 ? 2 : 1;                        // k-steps of a stage at most (fewer at the end of a range or a unit)
     extern __shared__ uint8_t smem_raw[];
     const uint32_t raw_addr = smem_u32(smem_raw);
     uint8_t* tiles = smem_raw + ((1024u - (raw_addr & 1023u)) & 1023u);
     const uint32_t tiles_addr = smem_u32(tiles);
     // a stage: weight tiles [MT][ks] | columns of x [ks] | scales of the tiles [MT][ks] | scales of x [ks]
     const uint32_t x_tile = (uint32_t)p.cols * TILE, x_sf = (uint32_t)p.sf_atoms * SF_BYTES;
-    const uint32_t b_off = MT * p.ks * A_BYTES, sa_off = b_off + p.ks * x_tile, sb_off = sa_off + MT * p.ks * SF_BYTES;
-    const uint32_t stage_bytes = (sb_off + p.ks * x_sf + 1023u) & ~1023u;
+    const uint32_t b_off = MT * KS * A_BYTES, sa_off = b_off + KS * x_tile, sb_off = sa_off + MT * KS * SF_BYTES;
+    const uint32_t stage_bytes = (sb_off + KS * x_sf + 1023u) & ~1023u;
     Smem* sm = reinterpret_cast<Smem*>(tiles + (size_t)p.stages * stage_bytes);
 
     const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31, cta = blockIdx.x, ctas = gridDim.x;
@@ -210,7 +219,7 @@ k_mx4_gemm(const __grid_constant__ Mx4Maps maps, const Mx4Params p) {
         c.tile = (long long)(GATE ? ru : ru * MT) * p.kt + c.kc;
         c.xstep = (c.unit - ru * p.groups) * p.kt + c.kc;
     };
-    auto size = [&](Cursor& c) { c.take = min(p.ks, min(p.kt - c.kc, c.left)); };
+    auto size = [&](Cursor& c) { c.take = min(KS, min(p.kt - c.kc, c.left)); };
     auto begin = [&] {
         Cursor c{unit0, kc0, my_iters};
         enter(c);
@@ -231,7 +240,7 @@ k_mx4_gemm(const __grid_constant__ Mx4Maps maps, const Mx4Params p) {
         for (int t = 0; t < MT; ++t) {
             if (t >= c.nt) break;
             const long long tile = c.tile + (GATE ? 0 : t * p.kt);
-            tma_load_2d(at + t * p.ks * A_BYTES, GATE && t ? &maps.w2[c.take - 1] : &maps.w[c.take - 1], 0, (int)(tile * TILE), bar, pol);
+            tma_load_2d(at + t * KS * A_BYTES, GATE && t ? &maps.w2[c.take - 1] : &maps.w[c.take - 1], 0, (int)(tile * TILE), bar, pol);
         }
     };
     auto load_x = [&](uint32_t stage, const Cursor& c, uint64_t pol) {
@@ -245,7 +254,7 @@ k_mx4_gemm(const __grid_constant__ Mx4Maps maps, const Mx4Params p) {
         for (int t = 0; t < MT; ++t) {
             if (t >= c.nt) break;
             const long long tile = c.tile + (GATE ? 0 : t * p.kt);
-            bulk_load(at + sa_off + t * p.ks * SF_BYTES, (GATE && t ? p.scales2 : p.scales) + tile * TILE_SCALES, c.take * SF_BYTES, bar, pol);
+            bulk_load(at + sa_off + t * KS * SF_BYTES, (GATE && t ? p.scales2 : p.scales) + tile * TILE_SCALES, c.take * SF_BYTES, bar, pol);
         }
     };
 
@@ -329,31 +338,24 @@ k_mx4_gemm(const __grid_constant__ Mx4Maps maps, const Mx4Params p) {
             if (!__all_sync(0xffffffffu, ok)) { ok = false; break; }
             tc_fence_after();
             const uint32_t at = tiles_addr + stage * stage_bytes;
-            const int unit = c.unit, take = c.take, nt = c.nt;
+            const int unit = c.unit, take = c.take;
             const uint32_t acc0 = in_chunk > 0;
             in_chunk += take;
             step(c);
             const bool last = in_chunk == CHUNK || c.unit != unit || c.left == 0;
             if (leader) {
-                uint64_t adesc = smem_desc_sw128(at), bdesc = smem_desc_sw128(at + b_off), sad = smem_desc_scales(at + sa_off), sbd = smem_desc_scales(at + sb_off);
-                uint32_t sfa = sf0 + stage * p.ks * sf_step;
-                for (int s = 0; s < take; ++s) {
-                    const uint32_t sfb = sfa + 4 * MT;
-                    copy_scales(sfa, sad);
-                    if (MT == 2 && nt == 2) copy_scales(sfa + 4, sad + (p.ks * SF_BYTES >> 4));
-                    copy_scales(sfb, sbd);
-                    if (p.sf_atoms == 2) copy_scales(sfb + 4, sbd + (SF_BYTES >> 4));
+                const uint64_t adesc = smem_desc_sw128(at), bdesc = smem_desc_sw128(at + b_off), sad = smem_desc_scales(at + sa_off), sbd = smem_desc_scales(at + sb_off);
+                const uint32_t sf = sf0 + stage * KS * sf_step;
 #pragma unroll
-                    for (int q = 0; q < 4; ++q) mma_mx(tmem, adesc + q * 2, bdesc + q * 2, idesc + q * 0x20000010u, sfa, sfb, q > 0 ? 1u : s > 0 ? 1u : acc0);
-                    if (MT == 2 && nt == 2)
-#pragma unroll
-                        for (int q = 0; q < 4; ++q)
-                            mma_mx(tmem + p.cols, adesc + (p.ks * A_BYTES >> 4) + q * 2, bdesc + q * 2, idesc + q * 0x20000010u, sfa + 4, sfb, q > 0 ? 1u : s > 0 ? 1u : acc0);
-                    adesc += A_BYTES >> 4;
-                    bdesc += x_tile >> 4;
-                    sad += SF_BYTES >> 4;
-                    sbd += x_sf >> 4;
-                    sfa += sf_step;
+                for (int s = 0; s < KS; ++s) {
+                    if (s > 0 && s >= take) break;
+                    const uint32_t sfa = sf + s * sf_step, sfb = sfa + 4 * MT;
+                    copy_scales(sfa, sad + s * (SF_BYTES >> 4));
+                    if (MT == 2) copy_scales(sfa + 4, sad + ((KS + s) * SF_BYTES >> 4));      // (of a tile that is not there: what the ring holds)
+                    copy_scales(sfb, sbd + s * (x_sf >> 4));
+                    if (p.sf_atoms == 2) copy_scales(sfb + 4, sbd + s * (x_sf >> 4) + (SF_BYTES >> 4));
+                    mma_step(tmem, adesc + s * (A_BYTES >> 4), bdesc + s * (x_tile >> 4), idesc, sfa, sfb, s > 0 ? 1u : acc0);
+                    if (MT == 2) mma_step(tmem + p.cols, adesc + ((KS + s) * A_BYTES >> 4), bdesc + s * (x_tile >> 4), idesc, sfa + 4, sfb, s > 0 ? 1u : acc0);
                 }
                 tc_commit(smem_u32(&sm->empty[stage]));
                 if (last) tc_commit(smem_u32(&sm->acc_full));
@@ -551,11 +553,11 @@ ghd_status go(ghd_ctx* c, const T* x, int64_t ld, bool wide, const ghd_mx4* w, c
     const int mt = w2 || g.cols > 64 ? 2 : 1;
     p.units = (w2 ? p.tiles : (p.tiles + mt - 1) / mt) * g.groups;
     p.total = (long long)p.units * p.kt;
-    p.ks = mt == 1 ? 2 : 1;                                      // (2 * cols rows of x are one box then)
-    const size_t stage = (p.ks * ((size_t)mt * (A_BYTES + SF_BYTES) + (size_t)g.cols * TILE + (size_t)g.atoms * SF_BYTES) + 1023) / 1024 * 1024;
+    const int ks = mt == 1 ? 2 : 1;                              // as in the kernel (2 * cols rows of x are one box then)
+    const size_t stage = (ks * ((size_t)mt * (A_BYTES + SF_BYTES) + (size_t)g.cols * TILE + (size_t)g.atoms * SF_BYTES) + 1023) / 1024 * 1024;
     p.stages = (int)((227 * 1024 - 1024 - sizeof(Smem)) / stage);
     if (p.stages > MAX_STAGES) p.stages = MAX_STAGES;
-    const int sf_room = (512 - mt * g.cols) / (4 * p.ks * (mt + g.atoms));
+    const int sf_room = (512 - mt * g.cols) / (4 * ks * (mt + g.atoms));
     if (p.stages > sf_room) p.stages = sf_room;
     p.scales = (const uint8_t*)w->scales;
     p.scales2 = w2 ? (const uint8_t*)w2->scales : nullptr;
@@ -568,11 +570,11 @@ ghd_status go(ghd_ctx* c, const T* x, int64_t ld, bool wide, const ghd_mx4* w, c
     p.out = out;
     Mx4Maps maps;
     const uint64_t rows = (uint64_t)p.tiles * p.kt * TILE;
-    for (int q = 0; q < p.ks; ++q)
+    for (int q = 0; q < ks; ++q)
         if (!tmap_bytes(c, w->codes, rows, TILE * (q + 1), true, &maps.w[q]) || !tmap_bytes(c, (w2 ? w2 : w)->codes, rows, TILE * (q + 1), true, &maps.w2[q]) ||
             !tmap_bytes(c, terms, (uint64_t)g.groups * p.kt * g.cols, (uint32_t)(g.cols * (q + 1)), false, &maps.x[q]))
             return fail(c, GHD_ECUDA, "mx4: tensor map encoding failed");
-    for (int q = p.ks; q < 2; ++q) { maps.w[q] = maps.w[0]; maps.w2[q] = maps.w2[0]; maps.x[q] = maps.x[0]; }
+    for (int q = ks; q < 2; ++q) { maps.w[q] = maps.w[0]; maps.w2[q] = maps.w2[0]; maps.x[q] = maps.x[0]; }
     if (!c->attr_mx4) {
         const void* kernels[] = {(const void*)k_mx4_gemm<3, 1, false>, (const void*)k_mx4_gemm<3, 2, false>, (const void*)k_mx4_gemm<3, 2, true>,
                                  (const void*)k_mx4_gemm<5, 1, false>, (const void*)k_mx4_gemm<5, 2, false>, (const void*)k_mx4_gemm<5, 2, true>};
