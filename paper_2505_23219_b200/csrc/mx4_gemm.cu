@@ -32,7 +32,8 @@ namespace {
 using namespace mx4;
 using namespace tc;
 
-constexpr int THREADS = 352;            // weights' loads, MMAs, eight epilogue warps, x's loads
+constexpr int THREADS = 384;            // weights' loads, MMAs, eight epilogue warps, x's loads, weights to the L2
+constexpr int AHEAD = 192 * 1024;       // bytes of weights that a CTA has on their way from memory to the L2
 constexpr int MAX_STAGES = 10;
 constexpr int CHUNK = 64;               // k-steps of 128 that one accumulator takes
 constexpr int MAX_WORKERS = 1024;       // CTAs at most: each has an arrival counter
@@ -48,7 +49,8 @@ struct Mx4Params {
     int units, stages;                  // units: row units * groups, groups of one row unit behind one another
     int split;                          // CTAs (a cluster) to a unit; 1: ranges of the flattened space
     long long total;                    // units * kt
-    const uint8_t *scales, *scales2;    // of w, of the second matrix
+    const uint8_t *codes, *codes2;      // of w, of the second matrix
+    const uint8_t *scales, *scales2;
     const uint8_t* x_scales;
     float* part;                        // [CTA][MT * per_group][128]: sums of its first unit, if that began in another CTA's range
     int* counters;
@@ -64,11 +66,16 @@ struct Smem {
     uint64_t acc_full, acc_empty, drain;
     uint32_t tmem_base;
     int abort_flag;
+    volatile int loaded;                // k-steps whose loads have been started
 };
 
 __device__ __forceinline__ void bulk_load(uint32_t dst, const void* src, uint32_t bytes, uint32_t bar, uint64_t policy) {
     asm volatile("cp.async.bulk.shared::cluster.global.mbarrier::complete_tx::bytes.L2::cache_hint [%0], [%1], %2, [%3], %4;"
                  ::"r"(dst), "l"(src), "r"(bytes), "r"(bar), "l"(policy) : "memory");
+}
+
+__device__ __forceinline__ void prefetch_l2(const void* src, uint32_t bytes) {
+    asm volatile("cp.async.bulk.prefetch.L2.global [%0], %1;" ::"l"(src), "r"(bytes) : "memory");
 }
 
 // scales of 128 rows: 32 rows of 16 bytes, 8 of them 128 bytes apart, no swizzle
@@ -264,6 +271,7 @@ k_mx4_gemm(const __grid_constant__ Mx4Maps maps, const Mx4Params p) {
         mbar_init(smem_u32(&sm->acc_empty), 8);
         mbar_init(smem_u32(&sm->drain), 1);
         sm->abort_flag = 0;
+        sm->loaded = 0;
         asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
     }
     if (warp == 1) {
@@ -290,6 +298,7 @@ k_mx4_gemm(const __grid_constant__ Mx4Maps maps, const Mx4Params p) {
                 if (issued >= p.stages) ok = mbar_wait(smem_u32(&sm->empty[stage]), phase ^ 1, abort_flag, p.status, DEV_TIMEOUT_TMA);
                 if (!ok) break;
                 load_w(stage, c, pol);
+                sm->loaded = my_iters - c.left + c.take;
                 ++issued;
                 if (++stage == (uint32_t)p.stages) { stage = 0; phase ^= 1; }
             }
@@ -321,48 +330,71 @@ k_mx4_gemm(const __grid_constant__ Mx4Maps maps, const Mx4Params p) {
                 if (++stage == (uint32_t)p.stages) { stage = 0; phase ^= 1; }
             }
         }
+    } else if (warp == 11) {
+        // Memory answers after 1.5 us, in which the ring (4-bit elements take a byte in it) holds too little: the weights are brought to
+        // the L2 first, AHEAD bytes before their loads.
+        if (lane == 0) {
+            constexpr int STEPS = AHEAD / (MT * TILE_CODES);
+            int asked = 0;
+            for (Cursor c = begin(); c.left > 0; step(c)) {
+                while (asked - sm->loaded > STEPS && !*abort_flag) __nanosleep(100);
+                if (*abort_flag) break;
+#pragma unroll
+                for (int t = 0; t < MT; ++t) {
+                    if (t >= c.nt) break;
+                    const long long tile = c.tile + (GATE ? 0 : t * p.kt);
+                    prefetch_l2((GATE && t ? p.codes2 : p.codes) + tile * TILE_CODES, c.take * TILE_CODES);
+                    prefetch_l2((GATE && t ? p.scales2 : p.scales) + tile * TILE_SCALES, c.take * TILE_SCALES);
+                }
+                asked += c.take;
+            }
+        }
     } else if (warp == 1) {
         // The whole warp walks along, one lane issues: values that all lanes share sit in uniform registers, where the instructions take
-        // their operands (from one lane's registers each MMA took 200 cycles to issue, N = 48 needs 46).
+        // their operands (from one lane's registers each MMA took 200 cycles to issue, N = 48 needs 46).  What lies between two stages' MMAs
+        // is idle time of the tensor cores, so there is little.
         // Columns of tensor memory: the accumulators, then the scales of every stage (written again only after the MMAs of the stage's last
         // use are through, which the ring makes sure of).
-        const bool leader = elect_one();
+        const uint32_t leader = elect_one();
         const uint32_t sf_step = 4u * (MT + p.sf_atoms), sf0 = tmem + (uint32_t)(MT * p.cols), idesc = instr_desc_mx(p.cols, 0);
-        uint32_t stage = 0, phase = 0, chunks = 0;
-        int in_chunk = 0;
+        const uint64_t a0 = smem_desc_sw128(tiles_addr), b0 = smem_desc_sw128(tiles_addr + b_off);
+        const uint64_t sa0 = smem_desc_scales(tiles_addr + sa_off), sb0 = smem_desc_scales(tiles_addr + sb_off);
+        uint32_t stage = 0, phase = 0;
         bool ok = true;
-        for (Cursor c = begin(); c.left > 0;) {
-            if (in_chunk == 0 && chunks > 0) ok = mbar_wait(smem_u32(&sm->acc_empty), (chunks - 1) & 1, abort_flag, p.status, DEV_TIMEOUT_TMEM);
-            if (!__all_sync(0xffffffffu, ok)) { ok = false; break; }
-            ok = mbar_wait(smem_u32(&sm->full[stage]), phase, abort_flag, p.status, DEV_TIMEOUT_MMA);
-            if (!__all_sync(0xffffffffu, ok)) { ok = false; break; }
-            tc_fence_after();
-            const uint32_t at = tiles_addr + stage * stage_bytes;
-            const int unit = c.unit, take = c.take;
-            const uint32_t acc0 = in_chunk > 0;
-            in_chunk += take;
-            step(c);
-            const bool last = in_chunk == CHUNK || c.unit != unit || c.left == 0;
-            if (leader) {
-                const uint64_t adesc = smem_desc_sw128(at), bdesc = smem_desc_sw128(at + b_off), sad = smem_desc_scales(at + sa_off), sbd = smem_desc_scales(at + sb_off);
-                const uint32_t sf = sf0 + stage * KS * sf_step;
+        auto wait = [&](uint32_t bar, uint32_t parity, int code) {
+            if (!__all_sync(0xffffffffu, mbar_try(bar, parity))) ok = __all_sync(0xffffffffu, mbar_wait(bar, parity, abort_flag, p.status, code));
+            return ok;
+        };
+        for (int left = my_iters, kc = kc0, chunk = 0; left > 0; ++chunk) {
+            const int take = min(min(p.kt - kc, left), CHUNK);
+            if (chunk > 0 && !wait(smem_u32(&sm->acc_empty), (chunk - 1) & 1, DEV_TIMEOUT_TMEM)) break;
+            for (int k = take; k > 0; k -= KS) {
+                if (!wait(smem_u32(&sm->full[stage]), phase, DEV_TIMEOUT_MMA)) break;
+                tc_fence_after();
+                if (leader) {
+                    const uint64_t at = stage * (stage_bytes >> 4);
+                    const uint32_t sf = sf0 + stage * (KS * sf_step);
 #pragma unroll
-                for (int s = 0; s < KS; ++s) {
-                    if (s > 0 && s >= take) break;
-                    const uint32_t sfa = sf + s * sf_step, sfb = sfa + 4 * MT;
-                    copy_scales(sfa, sad + s * (SF_BYTES >> 4));
-                    if (MT == 2) copy_scales(sfa + 4, sad + ((KS + s) * SF_BYTES >> 4));      // (of a tile that is not there: what the ring holds)
-                    copy_scales(sfb, sbd + s * (x_sf >> 4));
-                    if (p.sf_atoms == 2) copy_scales(sfb + 4, sbd + s * (x_sf >> 4) + (SF_BYTES >> 4));
-                    mma_step(tmem, adesc + s * (A_BYTES >> 4), bdesc + s * (x_tile >> 4), idesc, sfa, sfb, s > 0 ? 1u : acc0);
-                    if (MT == 2) mma_step(tmem + p.cols, adesc + ((KS + s) * A_BYTES >> 4), bdesc + s * (x_tile >> 4), idesc, sfa + 4, sfb, s > 0 ? 1u : acc0);
+                    for (int s = 0; s < KS; ++s) {
+                        if (s > 0 && s >= k) break;
+                        const uint32_t sfa = sf + s * sf_step, sfb = sfa + 4 * MT, acc = s > 0 ? 1u : (uint32_t)(k < take);
+                        copy_scales(sfa, sa0 + at + s * (SF_BYTES >> 4));
+                        if (MT == 2) copy_scales(sfa + 4, sa0 + at + ((KS + s) * SF_BYTES >> 4));      // (of a tile that is not there: what the ring holds)
+                        copy_scales(sfb, sb0 + at + s * (x_sf >> 4));
+                        if (p.sf_atoms == 2) copy_scales(sfb + 4, sb0 + at + s * (x_sf >> 4) + (SF_BYTES >> 4));
+                        mma_step(tmem, a0 + at + s * (A_BYTES >> 4), b0 + at + s * (x_tile >> 4), idesc, sfa, sfb, acc);
+                        if (MT == 2) mma_step(tmem + p.cols, a0 + at + ((KS + s) * A_BYTES >> 4), b0 + at + s * (x_tile >> 4), idesc, sfa + 4, sfb, acc);
+                    }
+                    tc_commit(smem_u32(&sm->empty[stage]));
                 }
-                tc_commit(smem_u32(&sm->empty[stage]));
-                if (last) tc_commit(smem_u32(&sm->acc_full));
+                __syncwarp();
+                if (++stage == (uint32_t)p.stages) { stage = 0; phase ^= 1; }
             }
+            if (!ok) break;
+            if (leader) tc_commit(smem_u32(&sm->acc_full));
             __syncwarp();
-            if (last) { ++chunks; in_chunk = 0; }
-            if (++stage == (uint32_t)p.stages) { stage = 0; phase ^= 1; }
+            left -= take;
+            if ((kc += take) == p.kt) kc = 0;
         }
         if (!ok && leader) {                                   // no MMA may run when the tensor memory goes
             tc_commit(smem_u32(&sm->drain));
@@ -388,7 +420,8 @@ k_mx4_gemm(const __grid_constant__ Mx4Maps maps, const Mx4Params p) {
             const int rows_here = min(p.per_group, p.n - g * p.per_group), mine = max(0, min(half, rows_here - j0));
             for (int c = first; c < end && ok; c += CHUNK) {
                 const bool fresh = c == first;
-                ok = epi_all(mbar_wait(smem_u32(&sm->acc_full), chunks & 1, abort_flag, p.status, DEV_TIMEOUT_EPI));
+                // (one warp asks the barrier: eight of them asking took a third of the MMA warp's issue slots)
+                ok = epi_all(warp != 2 || mbar_wait(smem_u32(&sm->acc_full), chunks & 1, abort_flag, p.status, DEV_TIMEOUT_EPI));
                 if (!ok) break;
                 tc_fence_after();
 #pragma unroll
@@ -559,6 +592,8 @@ ghd_status go(ghd_ctx* c, const T* x, int64_t ld, bool wide, const ghd_mx4* w, c
     if (p.stages > MAX_STAGES) p.stages = MAX_STAGES;
     const int sf_room = (512 - mt * g.cols) / (4 * ks * (mt + g.atoms));
     if (p.stages > sf_room) p.stages = sf_room;
+    p.codes = (const uint8_t*)w->codes;
+    p.codes2 = w2 ? (const uint8_t*)w2->codes : nullptr;
     p.scales = (const uint8_t*)w->scales;
     p.scales2 = w2 ? (const uint8_t*)w2->scales : nullptr;
     uint8_t* terms = c->mx4_terms;
