@@ -258,7 +258,7 @@ ghd_status ghd_create(const ghd_model_cfg* cfg, void* cuda_stream, ghd_ctx** out
     c->h_ssq = -1;
     c->kv_len_hint = 0;
     c->entry_fresh = c->opt_chain_calls ? 0 : 1;
-    c->attr_gemm = c->attr_attn = c->attr_attn_small = c->attr_mx4 = false;
+    c->attr_gemm = c->attr_attn = c->attr_attn_small = c->attr_mx4 = c->attr_sampling = false;
     c->attr_kv4 = 0u;
     c->launches = 0;
     memset(c->path_count, 0, sizeof(c->path_count));

@@ -113,7 +113,7 @@ struct ghd_ctx {
     ghd::PendingPartials pending;   // projection output not yet folded into xres
     // bookkeeping
     int entry_fresh;          // 1 until the first launch of a public call: that launch is fully serialised (see launch_k)
-    bool attr_gemm, attr_attn, attr_attn_small, attr_mx4;  // dynamic shared memory limits raised on this context's device
+    bool attr_gemm, attr_attn, attr_attn_small, attr_mx4, attr_sampling;  // dynamic shared memory limits raised on this context's device
     int mx4_clusters[9];      // clusters of 2 .. 8 CTAs of a product with 4-bit matrices that the device holds at a time
     unsigned attr_kv4;        // ... of the 4-bit cache's attention kernels, a bit each
     int64_t launches;
