@@ -1,14 +1,16 @@
 // Sampling from logits with given random numbers: candidates drawn without replacement, and the verification of drafted
 // tokens against the target's probabilities.
 //
-// A row of logits is one distribution, w_s = exp((l_s - max) / temperature), in 64 bits: a token is decided by where a random
+// A row of logits is one distribution, w_s = exp(l_s / temperature) up to a factor, in 64 bits: a token is decided by where a random
 // number falls between running sums of up to 2^17 weights, whose borders 32 bits would move.
 //
-// The tokens lie in segments of 256 (32 lanes with 8 neighbours each; more in vocabularies above 2^20), the segments in equal
-// shares over the CTAs of a cluster, in order.  One pass over a row leaves the weight of every segment, relative to the segment's largest
-// logit until the row's is known: what the CTAs have to know of each other (a maximum, a sum) goes through distributed shared memory,
-// one cluster barrier for each exchange.  Where a random number falls is then looked up over the CTAs, over a CTA's segments, over the
-// lanes of one segment and over a lane's tokens, so that only one segment's weights are worked out again.
+// The tokens lie in segments of 256 (32 lanes with 8 neighbours each), the segments in equal shares over the CTAs of a cluster, in
+// order.  One pass over a row leaves the weight of every segment.  Weights are powers of two, 2^(l log2(e) / temperature - ref) with a
+// whole number ref that is at least the largest exponent of the segment, so that sums with unlike references are added exactly but for
+// the addition, by shifting exponents, and no second pass or exponential is needed once the row's largest logit is known.  What the CTAs
+// have to know of each other goes through distributed shared memory, one cluster barrier for each exchange.  Where a random number
+// falls is looked up over the CTAs, over a CTA's segments, over the lanes of one segment and over a lane's tokens, so that only one
+// segment's weights are worked out again.
 #include <cfloat>
 #include <cstdio>
 
@@ -21,19 +23,18 @@ namespace {
 
 constexpr int THREADS = 512, WARPS = THREADS / 32;
 constexpr int MAX_CLUSTER = 8;
-constexpr int MAX_SEGS = 4096;                  // of a row
-constexpr int RUN = 8;                          // tokens of a lane worked on together
+constexpr int RUN = 8, SEG = 32 * RUN;          // tokens of a lane, of a segment
+constexpr int MAX_VOCAB = 1 << 20;
 constexpr int VALUES = 4;                       // doubles that one exchange carries
 
 struct Shared {
     double box[2][MAX_CLUSTER][VALUES];         // exchanges, by turns: what the CTAs of the cluster have sent
-    double part[2][WARPS][2];                   // largest logit and weight of every warp's segments, of two rows
+    double part[2][WARPS][2];                   // reference and weight of every warp's segments, of two rows
     double mine[VALUES];                        // what this CTA sends
     double share[MAX_CLUSTER];                  // weights of the CTAs' shares of the row
     uint32_t child[GHD_MAX_NODES / 32];         // children of the node, a bit each
     int32_t parent[GHD_MAX_NODES];
     int32_t gone[GHD_MAX_NODES];                // tokens that are not in the distribution any more
-    int32_t token;
 };
 
 __device__ __forceinline__ void send(double* p, uint32_t rank, double v) {
@@ -44,6 +45,11 @@ __device__ __forceinline__ void send(double* p, uint32_t rank, double v) {
 __device__ __forceinline__ double warp_sum(double v) {
 #pragma unroll
     for (int o = 16; o; o >>= 1) v += __shfl_xor_sync(0xffffffffu, v, o);
+    return v;
+}
+__device__ __forceinline__ double warp_max(double v) {
+#pragma unroll
+    for (int o = 16; o; o >>= 1) v = fmax(v, __shfl_xor_sync(0xffffffffu, v, o));
     return v;
 }
 __device__ __forceinline__ float warp_max(float v) {
@@ -61,15 +67,33 @@ __device__ __forceinline__ double warp_scan(double v, int lane) {
     return v;
 }
 
-// exp(l * scale - z), the product rounded before the difference: equal logits are equally likely however large they are
-__device__ __forceinline__ double weight(float l, double scale, double z) { return exp(__dsub_rn(__dmul_rn((double)l, scale), z)); }
+// 2^n of a whole number n <= 0; 0 below -1000.  1 where n is NaN: the difference of two references that are both infinite.
+__device__ __forceinline__ double pow2_whole(double n) {
+    if (!(n < 0.0)) return 1.0;
+    return n < -1000.0 ? 0.0 : __hiloint2double((1023 + (int)n) << 20, 0);
+}
+// 2^y of y <= 0, 0 below -1000, NaN of NaN: 2^n 2^f with the nearest whole n, and the series of e^(f ln 2), whose first term left out is below
+// 2^-52 for |f| <= 1/2.  (The library's function takes any argument and twice the instructions.)
+__device__ __forceinline__ double pow2(double y) {
+    constexpr double LN2 = 0.693147180559945309417, MAGIC = 6755399441055744.0;        // 1.5 * 2^52: adding it rounds to a whole number
+    constexpr double C[13] = {1.0, 1.0, 1.0 / 2, 1.0 / 6, 1.0 / 24, 1.0 / 120, 1.0 / 720, 1.0 / 5040, 1.0 / 40320, 1.0 / 362880, 1.0 / 3628800, 1.0 / 39916800, 1.0 / 479001600};
+    const double x = fmax(y, -1001.0);                          // (fmax drops a NaN; it comes back below)
+    const double t = x + MAGIC, g = (x - (t - MAGIC)) * LN2;
+    double r = C[12];
+#pragma unroll
+    for (int i = 11; i >= 0; --i) r = fma(r, g, C[i]);
+    r *= __hiloint2double((1023 + __double2loint(t)) << 20, 0);
+    return y >= -1000.0 ? r : y < -1000.0 ? 0.0 : y;
+}
+// The product is rounded before the difference: equal logits are equally likely however large they are.
+__device__ __forceinline__ double weight(float l, double scale, double ref) { return pow2(__dsub_rn(__dmul_rn((double)l, scale), ref)); }
 
-// One row's distribution: exp(l * scale - max) / sum, scale = 1 / temperature.
+// One row's distribution: 2^(l * scale - ref) / sum, scale = log2(e) / temperature.
 struct Dist {
     const float* row;
-    double scale, max, inv_sum;
+    double scale, ref, inv_sum;
     bool ok;
-    __device__ __forceinline__ double of(float l) const { return weight(l, scale, max) * inv_sum; }
+    __device__ __forceinline__ double of(float l) const { return weight(l, scale, ref) * inv_sum; }
     __device__ __forceinline__ double at(int t) const { return of(__ldg(row + t)); }
 };
 
@@ -78,19 +102,20 @@ struct Team {
     Shared* s;
     double* seg;                                // [own segments] weights
     int rank, size, turn, warp, lane;
-    int vocab, run, wide;                       // tokens of a lane in a segment (a multiple of RUN); rows on 16-byte boundaries
+    int vocab, wide;                            // rows on 16-byte boundaries
     int seg0, segs;                             // own segments
 
-    __device__ Team(Shared* sm, double* weights, int vocab_, int run_, int cluster) : s(sm), seg(weights), size(cluster), turn(0), vocab(vocab_), run(run_) {
+    __device__ Team(Shared* sm, double* weights, int vocab_, int cluster) : s(sm), seg(weights), size(cluster), turn(0), vocab(vocab_) {
         rank = cluster > 1 ? (int)tc::cluster_ctarank() : 0;
         warp = threadIdx.x >> 5;
         lane = threadIdx.x & 31;
         wide = vocab % 4 == 0;
-        const int n = (vocab + 32 * run - 1) / (32 * run);
-        seg0 = (int)((long long)n * rank / cluster);
-        segs = (int)((long long)n * (rank + 1) / cluster) - seg0;
+        const int n = (vocab + SEG - 1) / SEG;
+        seg0 = n * rank / cluster;
+        segs = n * (rank + 1) / cluster - seg0;
         if (cluster > 1) tc::cluster_sync_all();                   // everybody's shared memory is there
     }
+    __device__ __forceinline__ int first_of(int sg) const { return sg * SEG + lane * RUN; }       // this lane's first token of a segment
     // RUN tokens from t on, -inf past the row's end
     __device__ __forceinline__ void load(const float* __restrict__ row, int t, float (&x)[RUN]) const {
         if (wide && t + RUN <= vocab) {
@@ -104,7 +129,6 @@ struct Team {
             for (int i = 0; i < RUN; ++i) x[i] = t + i < vocab ? __ldg(row + t + i) : -INFINITY;
         }
     }
-    __device__ __forceinline__ int first_of(int sg) const { return (sg * 32 + lane) * run; }       // this lane's first token of a segment
     // mine[0 .. n) of every CTA, to be read from the returned box by everyone: one barrier of the cluster.
     // The box of the exchange before is still being read; the one before that has been left by everybody.
     __device__ double (*exchange(int n))[VALUES] {
@@ -130,94 +154,79 @@ struct Team {
     }
 };
 
-// Maximum and sum of a row p and, if q.row is given, of a second one.  seg[] is left with p's weights (not divided by the sum),
+// The weights of a segment's tokens in this lane, x past the vocabulary and -inf being nothing
+__device__ __forceinline__ double sum_of(const float (&x)[RUN], double scale, double ref) {
+    double w[RUN];
+#pragma unroll
+    for (int e = 0; e < RUN; ++e) w[e] = x[e] == -INFINITY ? 0.0 : weight(x[e], scale, ref);
+    return ((w[0] + w[1]) + (w[2] + w[3])) + ((w[4] + w[5]) + (w[6] + w[7]));
+}
+
+// Reference and sum of a row p and, if q.row is given, of a second one.  seg[] is left with p's weights (not divided by the sum),
 // share[] has every CTA's part of p's sum.
 __device__ void measure(Team& m, Dist& p, Dist& q) {
     const int n = q.row ? 2 : 1;
+    double ref[2] = {-INFINITY, -INFINITY}, all[2] = {0.0, 0.0};
 #pragma unroll 1
-    for (int i = n - 1; i >= 0; --i) {
-        const float* row = i ? q.row : p.row;
-        const double scale = i ? q.scale : p.scale;
-        // of the warp's segments: the largest logit so far, and the weight relative to it
-        float top = -INFINITY;
-        double all = 0.0;
-#pragma unroll 1
-        for (int g = m.warp; g < m.segs; g += WARPS) {
-            float high = -INFINITY;
-            double sum = 0.0;
-#pragma unroll 1
-            for (int c = 0; c < m.run; c += RUN) {
-                float x[RUN];
-                m.load(row, m.first_of(m.seg0 + g) + c, x);
-                float now = x[0];
+    for (int g = m.warp; g < m.segs; g += WARPS) {
+        float x[2][RUN];
+        m.load(p.row, m.first_of(m.seg0 + g), x[0]);
+        if (n == 2) m.load(q.row, m.first_of(m.seg0 + g), x[1]);
 #pragma unroll
-                for (int e = 1; e < RUN; ++e) now = fmaxf(now, x[e]);
-                now = fmaxf(high, warp_max(now));                              // (a NaN is left out of the maximum, and makes the sum one)
-                const double z = (double)now * scale;
-                double add = 0.0;
+        for (int i = 0; i < 2; ++i) {
+            if (i == 1 && n == 1) break;
+            const double scale = i ? q.scale : p.scale;
+            float top = x[i][0];
 #pragma unroll
-                for (int e = 0; e < RUN; ++e) add += x[e] == -INFINITY ? 0.0 : weight(x[e], scale, z);
-                sum = (high == -INFINITY ? sum : sum * weight(high, scale, z)) + warp_sum(add);
-                high = now;
-            }
-            if (i == 0 && m.lane == 0) m.seg[g] = sum;
-            if (i == 0 && m.lane == 0) m.seg[m.segs + g] = (double)high * scale;
-            const float now = fmaxf(top, high);
-            const double z = (double)now * scale;
-            all = (top == -INFINITY ? all : all * weight(top, scale, z)) + (high == -INFINITY ? sum : sum * weight(high, scale, z));
-            top = now;
+            for (int e = 1; e < RUN; ++e) top = fmaxf(top, x[i][e]);
+            const double r = ceil(__dmul_rn((double)warp_max(top), scale));        // (a NaN is left out of the maximum, and makes the sum one)
+            const double sum = warp_sum(sum_of(x[i], scale, r));
+            if (i == 0 && m.lane == 0) { m.seg[g] = sum; m.seg[m.segs + g] = r; }
+            const double both = fmax(ref[i], r);
+            all[i] = all[i] * pow2_whole(ref[i] - both) + sum * pow2_whole(r - both);
+            ref[i] = both;
         }
-        if (m.lane == 0) { m.s->part[i][m.warp][0] = (double)top * scale; m.s->part[i][m.warp][1] = all; }
     }
+    if (m.lane < n) { m.s->part[m.lane][m.warp][0] = m.lane ? ref[1] : ref[0]; m.s->part[m.lane][m.warp][1] = m.lane ? all[1] : all[0]; }
     __syncthreads();
     if (m.warp < n) {                                            // the warps' results of row `warp`
-        double best = m.lane < WARPS ? m.s->part[m.warp][m.lane][0] : -INFINITY;
-        const double a = best, b = m.lane < WARPS ? m.s->part[m.warp][m.lane][1] : 0.0;
-#pragma unroll
-        for (int o = 16; o; o >>= 1) best = fmax(best, __shfl_xor_sync(0xffffffffu, best, o));
-        const double all = warp_sum(a == -INFINITY ? b : b * exp(a - best));       // (b is 0 or NaN where there is no maximum)
-        if (m.lane == 0) { m.s->mine[2 * m.warp] = best; m.s->mine[2 * m.warp + 1] = all; }
+        const double r = m.lane < WARPS ? m.s->part[m.warp][m.lane][0] : -INFINITY, x = m.lane < WARPS ? m.s->part[m.warp][m.lane][1] : 0.0;
+        const double both = warp_max(r), sum = warp_sum(x * pow2_whole(r - both));
+        if (m.lane == 0) { m.s->mine[2 * m.warp] = both; m.s->mine[2 * m.warp + 1] = sum; }
     }
     double (*box)[VALUES] = m.exchange(2 * n);
-    const int r = m.lane < m.size ? m.lane : 0;
-#pragma unroll 1
-    for (int i = 0; i < n; ++i) {
-        const double a = box[r][2 * i], b = box[r][2 * i + 1];
-        double best = a;
 #pragma unroll
-        for (int o = 16; o; o >>= 1) best = fmax(best, __shfl_xor_sync(0xffffffffu, best, o));
-        double share = m.lane < m.size ? (a == -INFINITY ? b : b * exp(a - best)) : 0.0;
-        double sum = 0.0;
-        for (int k = 0; k < m.size; ++k) sum += __shfl_sync(0xffffffffu, share, k);
+    for (int i = 0; i < 2; ++i) {
+        if (i == 1 && n == 1) break;
+        double both = -INFINITY, sum = 0.0;
+        for (int r = 0; r < m.size; ++r) both = fmax(both, box[r][2 * i]);
+        for (int r = 0; r < m.size; ++r) {
+            const double x = box[r][2 * i + 1] * pow2_whole(box[r][2 * i] - both);
+            if (i == 0 && threadIdx.x == 0) m.s->share[r] = x;
+            sum += x;
+        }
         Dist& d = i ? q : p;
-        d.max = best;
+        d.ref = both;
         d.inv_sum = 1.0 / sum;
-        d.ok = best > -INFINITY && best < INFINITY && sum < INFINITY;
-        if (i == 0 && m.warp == 0 && m.lane < m.size) m.s->share[m.lane] = share;
+        d.ok = both > -INFINITY && both < INFINITY && sum < INFINITY;
     }
-    for (int g = threadIdx.x; g < m.segs; g += THREADS) {
-        const double z = m.seg[m.segs + g];
-        m.seg[g] = z == -INFINITY ? 0.0 : m.seg[g] * exp(z - p.max);
-    }
+    for (int g = threadIdx.x; g < m.segs; g += THREADS) m.seg[g] *= pow2_whole(m.seg[m.segs + g] - p.ref);
     __syncthreads();
 }
 
-// The weights w(logit of p, logit of q, token) of every own segment into seg[], of the CTAs' shares into share[] -> the total.
+// The weights w(logit of p, logit of q) of every own segment into seg[], of the CTAs' shares into share[] -> the total.
 template <typename W>
 __device__ double total_of(Team& m, const float* p, const float* q, W w) {
     double all = 0.0;
 #pragma unroll 1
     for (int g = m.warp; g < m.segs; g += WARPS) {
+        float x[RUN], y[RUN];
+        const int t = m.first_of(m.seg0 + g);
+        m.load(p, t, x);
+        m.load(q, t, y);
         double sum = 0.0;
-#pragma unroll 1
-        for (int c = 0; c < m.run; c += RUN) {
-            float x[RUN], y[RUN];
-            const int t = m.first_of(m.seg0 + g) + c;
-            m.load(p, t, x);
-            if (q) m.load(q, t, y);
 #pragma unroll
-            for (int e = 0; e < RUN; ++e) sum += t + e < m.vocab ? w(x[e], q ? y[e] : 0.f, t + e) : 0.0;
-        }
+        for (int e = 0; e < RUN; ++e) sum += w(x[e], y[e]);
         sum = warp_sum(sum);
         if (m.lane == 0) m.seg[g] = sum;
         all += sum;
@@ -247,57 +256,61 @@ __device__ bool own_share(Team& m, double target, double& before) {
     return owner == m.rank;
 }
 
-// One warp: the first token whose running sum, `before` and seg[] in front, exceeds the target; weights as in total_of.  All lanes get it.
-template <typename W>
-__device__ int look_up(Team& m, double before, double target, const float* p, const float* q, W w) {
-    // the segment
-    int found = -1, held = -1;
-    double start = before, held_start = before;
-#pragma unroll 1
-    for (int g0 = 0; g0 < m.segs && found < 0; g0 += 32) {
-        const double x = g0 + m.lane < m.segs ? m.seg[g0 + m.lane] : 0.0;
-        const double run = before + warp_scan(x, m.lane);
-        const uint32_t over = __ballot_sync(0xffffffffu, x > 0.0 && run > target), some = __ballot_sync(0xffffffffu, x > 0.0);
-        if (some) {
-            const int k = 31 - __clz(some);
-            held = g0 + k;
-            held_start = __shfl_sync(0xffffffffu, run - x, k);
-        }
-        if (over) {
-            const int k = __ffs(over) - 1;
-            found = g0 + k;
-            start = __shfl_sync(0xffffffffu, run - x, k);
-        }
-        before = __shfl_sync(0xffffffffu, run, 31);
-    }
-    if (found < 0) { found = held; start = held_start; }
-    if (found < 0) return -1;
-    // the lane, and the token
-    double sum = 0.0;
-    const int t0 = m.first_of(m.seg0 + found);
-    auto weigh = [&](auto f) {
-#pragma unroll 1
-        for (int c = 0; c < m.run; c += RUN) {
-            float x[RUN], y[RUN];
-            m.load(p, t0 + c, x);
-            if (q) m.load(q, t0 + c, y);
-#pragma unroll
-            for (int e = 0; e < RUN; ++e) f(t0 + c + e, t0 + c + e < m.vocab ? w(x[e], q ? y[e] : 0.f, t0 + c + e) : 0.0);
-        }
-    };
-    weigh([&](int, double x) { sum += x; });
-    const double run = start + warp_scan(sum, m.lane);
+// One warp: the lane in whose sums the target falls, `before` lying in front of them all -> that lane, the last one with weight where
+// rounding leaves none, -1 where there is no weight; start: what lies before that lane.
+__device__ int lane_of(double sum, double before, double target, int lane, double& start) {
+    const double run = before + warp_scan(sum, lane);
     const uint32_t over = __ballot_sync(0xffffffffu, sum > 0.0 && run > target), some = __ballot_sync(0xffffffffu, sum > 0.0);
     if (!some) return -1;
     const int k = over ? __ffs(over) - 1 : 31 - __clz(some);
-    double at = run - sum;
+    start = __shfl_sync(0xffffffffu, run - sum, k);
+    return k;
+}
+// One warp: the segment of seg[0 .. n) in which the target falls.  A lane has `per` neighbouring segments, which weigh `sum` together.
+__device__ int segment_of(const double* seg, int n, int per, double sum, double before, double target, int lane, double& start) {
+    const int k = lane_of(sum, before, target, lane, start);
+    if (k < 0) return -1;
+    int found = -1, last = -1;
+    double run = start, last_start = start;
+    for (int g = k * per; g < min(n, (k + 1) * per); ++g) {      // (all lanes walk the owner's)
+        const double x = seg[g];
+        if (x > 0.0) { last = g; last_start = run; }
+        if (x > 0.0 && run + x > target) { found = g; break; }
+        run += x;
+    }
+    start = found < 0 ? last_start : run;
+    return found < 0 ? last : found;
+}
+// One warp: the token, from the weights w of the segment's tokens in this lane.  All lanes get it.
+__device__ int token_of(const double (&w)[RUN], int t0, double before, double target, int lane) {
+    double sum = 0.0, start;
+#pragma unroll
+    for (int e = 0; e < RUN; ++e) sum += w[e];
+    const int k = lane_of(sum, before, target, lane, start);
+    if (k < 0) return -1;
     int token = -1, last = -1;
-    weigh([&](int t, double x) {
-        at += x;
-        if (x > 0.0) last = t;
-        if (token < 0 && x > 0.0 && at > target) token = t;
-    });
+    double run = start;
+#pragma unroll
+    for (int e = 0; e < RUN; ++e) {
+        run += w[e];
+        if (w[e] > 0.0) last = t0 + e;
+        if (token < 0 && w[e] > 0.0 && run > target) token = t0 + e;
+    }
     return __shfl_sync(0xffffffffu, token < 0 ? last : token, k);
+}
+// what a lane's neighbouring segments weigh
+__device__ __forceinline__ double lane_sum(const double* seg, int n, int per, int lane) {
+    double sum = 0.0;
+    for (int g = lane * per; g < min(n, (lane + 1) * per); ++g) sum += seg[g];
+    return sum;
+}
+// tokens that are gone have no weight
+__device__ __forceinline__ void without(double (&w)[RUN], int t0, const int32_t* gone, int n) {
+    for (int g = 0; g < n; ++g) {
+        const int d = gone[g] - t0;
+#pragma unroll
+        for (int e = 0; e < RUN; ++e) w[e] = d == e ? 0.0 : w[e];
+    }
 }
 
 // seg[] and share[] after measure(), without the tokens gone[0 .. n) -> the total
@@ -305,23 +318,19 @@ __device__ double total_without(Team& m, const Dist& p, int n) {
     __syncthreads();
 #pragma unroll 1
     for (int i = m.warp; i < n; i += WARPS) {
-        const int g = m.s->gone[i] / (32 * m.run) - m.seg0;
+        const int g = m.s->gone[i] / SEG - m.seg0;
         bool first = g >= 0 && g < m.segs;                       // one warp to a segment, that of the first of its tokens
-        for (int k = 0; k < i && first; ++k) first = m.s->gone[k] / (32 * m.run) - m.seg0 != g;
+        for (int k = 0; k < i && first; ++k) first = m.s->gone[k] / SEG - m.seg0 != g;
         if (!first) continue;
-        double sum = 0.0;
-#pragma unroll 1
-        for (int c = 0; c < m.run; c += RUN) {
-            float x[RUN];
-            const int t = m.first_of(m.seg0 + g) + c;
-            m.load(p.row, t, x);
+        float x[RUN];
+        double w[RUN], sum = 0.0;
+        const int t0 = m.first_of(m.seg0 + g);
+        m.load(p.row, t0, x);
 #pragma unroll
-            for (int e = 0; e < RUN; ++e) {
-                double y = t + e < m.vocab ? p.of(x[e]) : 0.0;
-                for (int k = 0; k < n; ++k) y = m.s->gone[k] == t + e ? 0.0 : y;
-                sum += y;
-            }
-        }
+        for (int e = 0; e < RUN; ++e) w[e] = p.of(x[e]);
+        without(w, t0, m.s->gone, n);
+#pragma unroll
+        for (int e = 0; e < RUN; ++e) sum += w[e];
         sum = warp_sum(sum);
         if (m.lane == 0) m.seg[g] = sum;
     }
@@ -339,60 +348,53 @@ __device__ double total_without(Team& m, const Dist& p, int n) {
 __device__ __forceinline__ double unit(float u) { return (double)fminf(fmaxf(u, 0.f), 0x1.fffffep-1f); }
 
 // ---------------------------------------------------------------- candidates
-// The CTA in whose share a draw falls is not the same every time, but what it takes to find the token is one segment's logits: when the
-// shares are known the first CTA gets all segments' weights and draws alone, with one warp.
-__global__ void __launch_bounds__(THREADS) k_draft_sample(const float* __restrict__ logits, int vocab, int run, int cluster, double scale, int draws,
+// When the row has been measured its first CTA gets all segments' weights and draws alone, with one warp: what it takes to find a token
+// is one segment's logits.
+__global__ void __launch_bounds__(THREADS) k_draft_sample(const float* __restrict__ logits, int vocab, int cluster, double scale, int draws,
                                                           const float* __restrict__ uniforms, int32_t* __restrict__ cand, int* status) {
     extern __shared__ double weights[];
     __shared__ Shared sm;
-    Team m(&sm, weights, vocab, run, cluster);
+    Team m(&sm, weights, vocab, cluster);
     const int row = blockIdx.x / cluster;
     Dist p{logits + (size_t)row * vocab, scale, 0.0, 1.0, false}, none{};
     measure(m, p, none);
-    const int n = (vocab + 32 * run - 1) / (32 * run);
     if (cluster > 1) {
-        // (in the first CTA the room behind its own segments is free by now: measure's last barrier)
-        tc::cluster_sync_all();
+        tc::cluster_sync_all();                                // (the first CTA's room behind its own segments is free)
         if (m.rank > 0)
             for (int g = threadIdx.x; g < m.segs; g += THREADS) send(weights + m.seg0 + g, 0, weights[g]);
         tc::cluster_sync_all();
     }
     if (m.rank > 0 || m.warp > 0) return;
-    m.segs = n;
     if (!p.ok && m.lane == 0) atomicCAS(status, DEV_OK, DEV_SAMPLE_DIST);
     p.inv_sum = 1.0;                                           // the weights as they are
-    int out = -1, n_gone = 0;
+    const int n = (vocab + SEG - 1) / SEG, per = (n + 31) / 32;
+    const float u = m.lane < draws ? __ldg(uniforms + (size_t)row * GHD_MAX_TOPK + m.lane) : 0.f;
+    double mine = lane_sum(weights, n, per, m.lane);
+    int out = -1;
 #pragma unroll 1
     for (int j = 0; j < draws && p.ok; ++j) {
-        double total = 0.0;
-        for (int g = m.lane; g < n; g += 32) total += weights[g];
-        total = warp_sum(total);
-        if (!(total > 0.0)) break;                             // nothing is left
-        auto w = [&](float l, float, int t) {
-            double x = p.of(l);
-            for (int g = 0; g < n_gone; ++g) x = sm.gone[g] == t ? 0.0 : x;
-            return x;
-        };
-        const int t = look_up(m, 0.0, unit(__ldg(uniforms + (size_t)row * GHD_MAX_TOPK + j)) * total, p.row, nullptr, w);
+        const double target = unit(__shfl_sync(0xffffffffu, u, j)) * warp_sum(mine);
+        double start;
+        const int sg = segment_of(weights, n, per, mine, 0.0, target, m.lane, start);
+        if (sg < 0) break;                                     // nothing is left
+        float x[RUN];
+        double w[RUN], sum = 0.0;
+        const int t0 = m.first_of(sg);
+        m.load(p.row, t0, x);
+#pragma unroll
+        for (int e = 0; e < RUN; ++e) w[e] = p.of(x[e]);
+        without(w, t0, sm.gone, j);
+        const int t = token_of(w, t0, start, target, m.lane);
         if (t < 0) break;
         if (m.lane == j) out = t;
-        if (m.lane == 0) sm.gone[n_gone] = t;
-        ++n_gone;
-        __syncwarp();
+        if (m.lane == 0) sm.gone[j] = t;
         // the segment's weight without it
-        const int sg = t / (32 * run);
-        double sum = 0.0;
-#pragma unroll 1
-        for (int c = 0; c < run; c += RUN) {
-            float x[RUN];
-            const int t0 = m.first_of(sg) + c;
-            m.load(p.row, t0, x);
 #pragma unroll
-            for (int e = 0; e < RUN; ++e) sum += t0 + e < vocab ? w(x[e], 0.f, t0 + e) : 0.0;
-        }
+        for (int e = 0; e < RUN; ++e) sum += t - t0 == e ? 0.0 : w[e];
         sum = warp_sum(sum);
         if (m.lane == 0) weights[sg] = sum;
         __syncwarp();
+        if (m.lane == sg / per) mine = lane_sum(weights, n, per, m.lane);
     }
     if (m.lane < GHD_MAX_TOPK) cand[(size_t)row * GHD_MAX_TOPK + m.lane] = out;
 }
@@ -404,10 +406,10 @@ __global__ void __launch_bounds__(THREADS) k_draft_sample(const float* __restric
 // beta_{j+1} = beta_j + c_j W_j, and c_j = 1 / (1 - Q(rejected)).  A rejected token has u Q_j >= P_j, u < 1, so P_{j+1} gives it
 // nothing, and so do all later ones: beta only grows.  So two numbers are kept instead of two distributions, and a rejection costs
 // one sum over the vocabulary.  Candidates that nobody drew have Q = 1 at themselves: P_{j+1} is P_j without x.
-__global__ void __launch_bounds__(THREADS) k_accept_sampled(ghd_sampled a, int vocab, int run, int cluster, ghd_accept_result* __restrict__ results, int* status) {
+__global__ void __launch_bounds__(THREADS) k_accept_sampled(ghd_sampled a, int vocab, double scale, double draft_scale, int cluster, ghd_accept_result* __restrict__ results, int* status) {
     extern __shared__ double weights[];
     __shared__ Shared sm;
-    Team m(&sm, weights, vocab, run, cluster);
+    Team m(&sm, weights, vocab, cluster);
     const int seq = blockIdx.x / cluster;
     ghd_accept_result* out = results + seq;
     const bool writes = m.rank == 0 && threadIdx.x == 0;
@@ -442,18 +444,14 @@ __global__ void __launch_bounds__(THREADS) k_accept_sampled(ghd_sampled a, int v
             record(DEV_SAMPLE_DRAFT);
             drawn = -1;
         }
-        Dist p{a.logits + (size_t)(first + node) * vocab, 1.0 / (double)a.temperature, 0.0, 1.0, false}, q{};
-        if (any && drawn >= 0) { q.row = a.draft_logits + (size_t)drawn * vocab; q.scale = 1.0 / (double)a.draft_temperature; }
+        Dist p{a.logits + (size_t)(first + node) * vocab, scale, 0.0, 1.0, false}, q{};
+        if (any && drawn >= 0) { q.row = a.draft_logits + (size_t)drawn * vocab; q.scale = draft_scale; }
         measure(m, p, q);
         if (!p.ok || (q.row && !q.ok)) record(DEV_SAMPLE_DIST);
         double beta = 0.0, W = 1.0, rejected = 0.0;
         int n_gone = 0, next = -1;
         bool fresh = false;                                    // seg[] and share[] are of the weights as they are, their total is W
-        auto left = [&](float lp, float lq, int t) {
-            const double x = p.of(lp);
-            if (q.row) return fmax(x - beta * q.of(lq), 0.0);
-            return x;
-        };
+        auto left = [&](float lp, float lq) { return fmax(p.of(lp) - beta * q.of(lq), 0.0); };
         if (p.ok && (!q.row || q.ok))
             for (int word = 0; word < GHD_MAX_NODES / 32 && next < 0; ++word)
                 for (uint32_t bits = sm.child[word]; bits; bits &= bits - 1) {
@@ -492,31 +490,37 @@ __global__ void __launch_bounds__(THREADS) k_accept_sampled(ghd_sampled a, int v
                 // those with a token that is gone weighed again.
                 if (fresh && !(W > 0.0)) {
                     beta = 0.0;
-                    fresh = false;
                     W = total_of(m, p.row, q.row, left);
-                    fresh = true;
                 }
                 double total = W;
                 if (!fresh) {
                     p.inv_sum = 1.0;
-                    if (n_gone == 0 || q.row) {
-                        total = 0.0;
-                        for (int r = 0; r < m.size; ++r) total += m.s->share[r];
-                        n_gone = 0;
-                    } else {
+                    if (q.row) n_gone = 0;
+                    if (n_gone > 0) {
                         total = total_without(m, p, n_gone);
+                    } else {
+                        total = 0.0;
+                        for (int r = 0; r < m.size; ++r) total += sm.share[r];
                     }
                 }
                 const double target = unit(__ldg(a.uniforms + first)) * total;
-                double before;
+                double before, start;
                 if (own_share(m, target, before) && m.warp == 0) {
-                    auto w = [&](float lp, float lq, int t) {
-                        if (q.row && fresh) return left(lp, lq, t);
-                        double x = p.of(lp);
-                        for (int g = 0; g < n_gone; ++g) x = sm.gone[g] == t ? 0.0 : x;
-                        return x;
-                    };
-                    const int t = look_up(m, before, target, p.row, fresh ? q.row : nullptr, w);
+                    const int per = (m.segs + 31) / 32, sg = segment_of(m.seg, m.segs, per, lane_sum(m.seg, m.segs, per, m.lane), before, target, m.lane, start);
+                    float x[RUN], y[RUN];
+                    double w[RUN];
+                    const int t0 = m.first_of(m.seg0 + max(sg, 0));
+                    m.load(p.row, t0, x);
+                    if (fresh) {
+                        m.load(q.row, t0, y);
+#pragma unroll
+                        for (int e = 0; e < RUN; ++e) w[e] = left(x[e], y[e]);
+                    } else {
+#pragma unroll
+                        for (int e = 0; e < RUN; ++e) w[e] = p.of(x[e]);
+                        without(w, t0, sm.gone, n_gone);
+                    }
+                    const int t = token_of(w, t0, start, target, m.lane);
                     if (m.lane == 0) out->tokens[depth] = t;
                 }
             }
@@ -537,23 +541,24 @@ __global__ void __launch_bounds__(THREADS) k_accept_sampled(ghd_sampled a, int v
     if (cluster > 1) tc::cluster_sync_all();
 }
 
-// CTAs to a row: as many as leave each of them a SM of its own and four segments to every warp's one
+// CTAs to a row: as many as leave each of them a SM of its own and four segments
 int cluster_for(const ghd_ctx* c, int rows, int vocab) {
     int k = MAX_CLUSTER;
-    while (k > 1 && ((int64_t)k * rows > c->sm_count || vocab < 1024 * k)) k >>= 1;
+    while (k > 1 && ((int64_t)k * rows > c->sm_count || vocab < 4 * SEG * k)) k >>= 1;
     return k;
 }
-int run_for(int vocab) { return RUN * (int)(((int64_t)vocab + MAX_SEGS * 32 * RUN - 1) / (MAX_SEGS * 32 * RUN)); }
-// room for a CTA's segments twice over (measure), and in a row's first CTA for all of them
-size_t room_for(int vocab, int run, int cluster) {
-    const size_t n = ((size_t)vocab + 32 * run - 1) / (32 * run), own = (n + cluster - 1) / cluster;
+// room for a CTA's segments twice over (weights and references), and in a row's first CTA for the weights of all
+size_t room_for(int vocab, int cluster) {
+    const size_t n = ((size_t)vocab + SEG - 1) / SEG, own = (n + cluster - 1) / cluster;
     return sizeof(double) * (2 * own > n ? 2 * own : n);
 }
+// log2(e) / temperature
+double scale_of(float temperature) { return 1.44269504088896340736 / (double)temperature; }
 
-ghd_status raise_room(ghd_ctx* c) {              // (a CTA with all of 4096 segments takes 64 KB)
+ghd_status raise_room(ghd_ctx* c) {              // (a CTA with all segments of the largest vocabulary takes 64 KB)
     if (c->attr_sampling) return GHD_OK;
-    if (cudaFuncSetAttribute(k_draft_sample, cudaFuncAttributeMaxDynamicSharedMemorySize, 2 * MAX_SEGS * (int)sizeof(double)) != cudaSuccess ||
-        cudaFuncSetAttribute(k_accept_sampled, cudaFuncAttributeMaxDynamicSharedMemorySize, 2 * MAX_SEGS * (int)sizeof(double)) != cudaSuccess)
+    if (cudaFuncSetAttribute(k_draft_sample, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)room_for(MAX_VOCAB, 1)) != cudaSuccess ||
+        cudaFuncSetAttribute(k_accept_sampled, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)room_for(MAX_VOCAB, 1)) != cudaSuccess)
         return check_cuda(c, "sampling: shared memory");
     c->attr_sampling = true;
     return GHD_OK;
@@ -571,15 +576,15 @@ ghd_status ghd_draft_sample(ghd_ctx* c, const float* logits, int32_t n_rows, flo
     if (!c) return GHD_EINVAL;
     if (n_rows < 0 || n_draws < 1 || n_draws > GHD_MAX_TOPK) return fail(c, GHD_EINVAL, "draft_sample: negative n_rows, or n_draws outside [1, 16]");
     if (!(temperature > 0.f) || !(temperature <= FLT_MAX)) return fail(c, GHD_EINVAL, "draft_sample: temperature is not a positive number");
+    if (c->cfg.vocab > MAX_VOCAB) return fail(c, GHD_ESHAPE, "draft_sample: a vocabulary above 2^20");
     if (n_rows == 0) return GHD_OK;
     if (n_rows > (1 << 24)) return fail(c, GHD_EINVAL, "draft_sample: more than 2^24 rows");
     if (!logits || !uniforms || !cand) return fail(c, GHD_EINVAL, "draft_sample: null pointer");
     if (!c->ws) return fail(c, GHD_ENOSPACE, "no workspace set");
     const int k = cluster_for(c, n_rows, c->cfg.vocab);
-    const int run = run_for(c->cfg.vocab);
     ghd_status s = raise_room(c);
     if (s != GHD_OK) return s;
-    launch_kc(c, false, k, k_draft_sample, n_rows * k, THREADS, room_for(c->cfg.vocab, run, k), logits, c->cfg.vocab, run, k, 1.0 / (double)temperature, n_draws, uniforms, cand, c->input_status);
+    launch_kc(c, false, k, k_draft_sample, n_rows * k, THREADS, room_for(c->cfg.vocab, k), logits, c->cfg.vocab, k, scale_of(temperature), n_draws, uniforms, cand, c->input_status);
     return check_cuda(c, "draft_sample");
 }
 
@@ -589,16 +594,16 @@ ghd_status ghd_accept_sampled(ghd_ctx* c, const ghd_sampled* a, ghd_accept_resul
     if (!a->row_start && a->n_seqs != 1) return fail(c, GHD_EINVAL, "accept_sampled: several sequences without row_start");
     if (!a->row_start && a->n_rows > GHD_MAX_NODES) return fail(c, GHD_ETREE, "accept_sampled: a tree of more than 256 nodes");
     if (!(a->temperature > 0.f) || !(a->temperature <= FLT_MAX)) return fail(c, GHD_EINVAL, "accept_sampled: temperature is not a positive number");
+    if (c->cfg.vocab > MAX_VOCAB) return fail(c, GHD_ESHAPE, "accept_sampled: a vocabulary above 2^20");
     if (!results_dev || (a->n_rows > 0 && (!a->parent || !a->tokens || !a->logits || !a->uniforms))) return fail(c, GHD_EINVAL, "accept_sampled: null pointer");
     if ((a->draft_row == nullptr) != (a->draft_logits == nullptr)) return fail(c, GHD_EINVAL, "accept_sampled: give both draft_row and draft_logits or neither");
     if (a->draft_row && (a->n_draft < 1 || !(a->draft_temperature > 0.f) || !(a->draft_temperature <= FLT_MAX)))
         return fail(c, GHD_EINVAL, "accept_sampled: no draft rows, or a draft temperature that is not a positive number");
     if (!c->ws) return fail(c, GHD_ENOSPACE, "no workspace set");
     const int k = cluster_for(c, a->n_seqs, c->cfg.vocab);
-    const int run = run_for(c->cfg.vocab);
     ghd_status s = raise_room(c);
     if (s != GHD_OK) return s;
-    launch_kc(c, false, k, k_accept_sampled, a->n_seqs * k, THREADS, room_for(c->cfg.vocab, run, k), *a, c->cfg.vocab, run, k, results_dev, c->input_status);
+    launch_kc(c, false, k, k_accept_sampled, a->n_seqs * k, THREADS, room_for(c->cfg.vocab, k), *a, c->cfg.vocab, scale_of(a->temperature), a->draft_row ? scale_of(a->draft_temperature) : 0.0, k, results_dev, c->input_status);
     return check_cuda(c, "accept_sampled");
 }
 
