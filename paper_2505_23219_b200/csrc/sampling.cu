@@ -35,6 +35,7 @@ struct Shared {
     uint32_t child[GHD_MAX_NODES / 32];         // children of the node, a bit each
     int32_t parent[GHD_MAX_NODES];
     int32_t gone[GHD_MAX_NODES];                // tokens that are not in the distribution any more
+    double roots[32];
 };
 
 __device__ __forceinline__ void send(double* p, uint32_t rank, double v) {
@@ -72,28 +73,44 @@ __device__ __forceinline__ double pow2_whole(double n) {
     if (!(n < 0.0)) return 1.0;
     return n < -1000.0 ? 0.0 : __hiloint2double((1023 + (int)n) << 20, 0);
 }
-// 2^y of y <= 0, 0 below -1000, NaN of NaN: 2^n 2^f with the nearest whole n, and the series of e^(f ln 2), whose first term left out is below
-// 2^-52 for |f| <= 1/2.  (The library's function takes any argument and twice the instructions.)
-__device__ __forceinline__ double pow2(double y) {
-    constexpr double LN2 = 0.693147180559945309417, MAGIC = 6755399441055744.0;        // 1.5 * 2^52: adding it rounds to a whole number
-    constexpr double C[13] = {1.0, 1.0, 1.0 / 2, 1.0 / 6, 1.0 / 24, 1.0 / 120, 1.0 / 720, 1.0 / 5040, 1.0 / 40320, 1.0 / 362880, 1.0 / 3628800, 1.0 / 39916800, 1.0 / 479001600};
-    const double x = fmax(y, -1001.0);                          // (fmax drops a NaN; it comes back below)
-    const double t = x + MAGIC, g = (x - (t - MAGIC)) * LN2;
-    double r = C[12];
-#pragma unroll
-    for (int i = 11; i >= 0; --i) r = fma(r, g, C[i]);
-    r *= __hiloint2double((1023 + __double2loint(t)) << 20, 0);
+// 2^(j / 32), rounded
+__constant__ double ROOTS[32] = {
+    1.0, 1.0218971486541166, 1.0442737824274138, 1.0671404006768237,
+    1.0905077326652577, 1.1143867425958924, 1.1387886347566916, 1.1637248587775775,
+    1.189207115002721, 1.215247359980469, 1.241857812073484, 1.2690509571917332,
+    1.2968395546510096, 1.3252366431597413, 1.3542555469368927, 1.383909881963832,
+    1.4142135623730951, 1.4451808069770467, 1.4768261459394993, 1.5091644275934228,
+    1.5422108254079407, 1.5759808451078865, 1.6104903319492543, 1.645755478153965,
+    1.681792830507429, 1.718619298122478, 1.7562521603732995, 1.7947090750031072,
+    1.8340080864093424, 1.8741676341103, 1.9152065613971474, 1.9571441241754002,
+};
+// 2^y of y <= 0, 0 below -1000, NaN of NaN.  Table-driven, after Tang (ACM TOMS 15, 1989): y = n / 32 + f with the nearest whole n, 2^(n / 32)
+// from the table (in shared memory) and the exponent, and the series of e^(f ln 2), whose first term left out is below 2^-48 for |f| <= 1/64: the
+// borders between tokens move by that.  (The library's function takes any argument and more than twice the instructions.)
+__device__ __forceinline__ double pow2(double y, const double* roots) {
+    constexpr double LN2 = 0.693147180559945309417, MAGIC = 6755399441055744.0 / 32;        // 1.5 * 2^52 / 32: adding it rounds to a whole 32nd
+    constexpr double C1 = LN2, C2 = LN2 * LN2 / 2, C3 = LN2 * LN2 * LN2 / 6, C4 = LN2 * LN2 * LN2 * LN2 / 24, C5 = LN2 * LN2 * LN2 * LN2 * LN2 / 120;
+    const double t = y + MAGIC, f = y - (t - MAGIC);
+    const int n = __double2loint(t);
+    const double root = roots[n & 31];
+    double r = fma(C5, f, C4);
+    r = fma(r, f, C3);
+    r = fma(r, f, C2);
+    r = fma(r, f, C1);
+    r = fma(r * f, root, root);
+    r = __hiloint2double(__double2hiint(r) + (n >> 5 << 20), __double2loint(r));
     return y >= -1000.0 ? r : y < -1000.0 ? 0.0 : y;
 }
 // The product is rounded before the difference: equal logits are equally likely however large they are.
-__device__ __forceinline__ double weight(float l, double scale, double ref) { return pow2(__dsub_rn(__dmul_rn((double)l, scale), ref)); }
+__device__ __forceinline__ double weight(float l, double scale, double ref, const double* roots) { return pow2(__dsub_rn(__dmul_rn((double)l, scale), ref), roots); }
 
 // One row's distribution: 2^(l * scale - ref) / sum, scale = log2(e) / temperature.
 struct Dist {
     const float* row;
     double scale, ref, inv_sum;
     bool ok;
-    __device__ __forceinline__ double of(float l) const { return weight(l, scale, ref) * inv_sum; }
+    const double* roots;
+    __device__ __forceinline__ double of(float l) const { return weight(l, scale, ref, roots) * inv_sum; }
     __device__ __forceinline__ double at(int t) const { return of(__ldg(row + t)); }
 };
 
@@ -113,7 +130,9 @@ struct Team {
         const int n = (vocab + SEG - 1) / SEG;
         seg0 = n * rank / cluster;
         segs = n * (rank + 1) / cluster - seg0;
+        if (threadIdx.x < 32) s->roots[threadIdx.x] = ROOTS[threadIdx.x];
         if (cluster > 1) tc::cluster_sync_all();                   // everybody's shared memory is there
+        else __syncthreads();
     }
     __device__ __forceinline__ int first_of(int sg) const { return sg * SEG + lane * RUN; }       // this lane's first token of a segment
     // RUN tokens from t on, -inf past the row's end
@@ -154,11 +173,12 @@ struct Team {
     }
 };
 
-// The weights of a segment's tokens in this lane, x past the vocabulary and -inf being nothing
-__device__ __forceinline__ double sum_of(const float (&x)[RUN], double scale, double ref) {
+// The weights of a segment's tokens in this lane: 0 of -inf, whatever the reference
+__device__ __forceinline__ double sum_of(const float (&x)[RUN], double scale, double ref, const double* roots) {
     double w[RUN];
+    ref = ref == -INFINITY ? 0.0 : ref;
 #pragma unroll
-    for (int e = 0; e < RUN; ++e) w[e] = x[e] == -INFINITY ? 0.0 : weight(x[e], scale, ref);
+    for (int e = 0; e < RUN; ++e) w[e] = weight(x[e], scale, ref, roots);
     return ((w[0] + w[1]) + (w[2] + w[3])) + ((w[4] + w[5]) + (w[6] + w[7]));
 }
 
@@ -180,7 +200,7 @@ __device__ void measure(Team& m, Dist& p, Dist& q) {
 #pragma unroll
             for (int e = 1; e < RUN; ++e) top = fmaxf(top, x[i][e]);
             const double r = ceil(__dmul_rn((double)warp_max(top), scale));        // (a NaN is left out of the maximum, and makes the sum one)
-            const double sum = warp_sum(sum_of(x[i], scale, r));
+            const double sum = warp_sum(sum_of(x[i], scale, r, p.roots));
             if (i == 0 && m.lane == 0) { m.seg[g] = sum; m.seg[m.segs + g] = r; }
             const double both = fmax(ref[i], r);
             all[i] = all[i] * pow2_whole(ref[i] - both) + sum * pow2_whole(r - both);
@@ -356,7 +376,7 @@ __global__ void __launch_bounds__(THREADS) k_draft_sample(const float* __restric
     __shared__ Shared sm;
     Team m(&sm, weights, vocab, cluster);
     const int row = blockIdx.x / cluster;
-    Dist p{logits + (size_t)row * vocab, scale, 0.0, 1.0, false}, none{};
+    Dist p{logits + (size_t)row * vocab, scale, 0.0, 1.0, false, sm.roots}, none{};
     measure(m, p, none);
     if (cluster > 1) {
         tc::cluster_sync_all();                                // (the first CTA's room behind its own segments is free)
@@ -444,8 +464,8 @@ __global__ void __launch_bounds__(THREADS) k_accept_sampled(ghd_sampled a, int v
             record(DEV_SAMPLE_DRAFT);
             drawn = -1;
         }
-        Dist p{a.logits + (size_t)(first + node) * vocab, scale, 0.0, 1.0, false}, q{};
-        if (any && drawn >= 0) { q.row = a.draft_logits + (size_t)drawn * vocab; q.scale = draft_scale; }
+        Dist p{a.logits + (size_t)(first + node) * vocab, scale, 0.0, 1.0, false, sm.roots}, q{};
+        if (any && drawn >= 0) { q.row = a.draft_logits + (size_t)drawn * vocab; q.scale = draft_scale; q.roots = sm.roots; }
         measure(m, p, q);
         if (!p.ok || (q.row && !q.ok)) record(DEV_SAMPLE_DIST);
         double beta = 0.0, W = 1.0, rejected = 0.0;
