@@ -34,6 +34,9 @@ struct Shared {
     double share[MAX_CLUSTER];                  // weights of the CTAs' shares of the row
     uint32_t child[GHD_MAX_NODES / 32];         // children of the node, a bit each
     int32_t parent[GHD_MAX_NODES];
+    int32_t token[GHD_MAX_NODES], draft[GHD_MAX_NODES];      // of the nodes: drafted token, draft row
+    float uniform[GHD_MAX_NODES];
+    double of_p[GHD_MAX_NODES], of_q[GHD_MAX_NODES];          // of the children of the node: their tokens' probabilities
     int32_t gone[GHD_MAX_NODES];                // tokens that are not in the distribution any more
     double roots[32];
 };
@@ -111,7 +114,6 @@ struct Dist {
     bool ok;
     const double* roots;
     __device__ __forceinline__ double of(float l) const { return weight(l, scale, ref, roots) * inv_sum; }
-    __device__ __forceinline__ double at(int t) const { return of(__ldg(row + t)); }
 };
 
 // This CTA's share of a row, and what the cluster has agreed on so far.
@@ -165,9 +167,10 @@ struct Team {
     }
     // what every CTA has sent as its share's weight -> the total
     __device__ double add_shares(double (*box)[VALUES]) {
-        double sum = 0.0;
-        for (int r = 0; r < size; ++r) sum += box[r][0];
-        if (threadIdx.x < (unsigned)size) s->share[threadIdx.x] = box[threadIdx.x][0];
+        double sum = lane % MAX_CLUSTER < size ? box[lane % MAX_CLUSTER][0] : 0.0;
+        if (threadIdx.x < (unsigned)size) s->share[threadIdx.x] = sum;
+#pragma unroll
+        for (int o = 1; o < MAX_CLUSTER; o <<= 1) sum += __shfl_xor_sync(0xffffffffu, sum, o);
         __syncthreads();
         return sum;
     }
@@ -215,16 +218,19 @@ __device__ void measure(Team& m, Dist& p, Dist& q) {
         if (m.lane == 0) { m.s->mine[2 * m.warp] = both; m.s->mine[2 * m.warp + 1] = sum; }
     }
     double (*box)[VALUES] = m.exchange(2 * n);
+    // every warp adds up what the CTAs have sent, a CTA to each of eight lanes
+    const int c = m.lane % MAX_CLUSTER;
 #pragma unroll
     for (int i = 0; i < 2; ++i) {
         if (i == 1 && n == 1) break;
-        double both = -INFINITY, sum = 0.0;
-        for (int r = 0; r < m.size; ++r) both = fmax(both, box[r][2 * i]);
-        for (int r = 0; r < m.size; ++r) {
-            const double x = box[r][2 * i + 1] * pow2_whole(box[r][2 * i] - both);
-            if (i == 0 && threadIdx.x == 0) m.s->share[r] = x;
-            sum += x;
-        }
+        const double r = c < m.size ? box[c][2 * i] : -INFINITY;
+        double both = r, sum = c < m.size ? box[c][2 * i + 1] : 0.0;
+#pragma unroll
+        for (int o = 1; o < MAX_CLUSTER; o <<= 1) both = fmax(both, __shfl_xor_sync(0xffffffffu, both, o));
+        sum *= pow2_whole(r - both);
+        if (i == 0 && threadIdx.x < (unsigned)m.size) m.s->share[threadIdx.x] = sum;
+#pragma unroll
+        for (int o = 1; o < MAX_CLUSTER; o <<= 1) sum += __shfl_xor_sync(0xffffffffu, sum, o);
         Dist& d = i ? q : p;
         d.ref = both;
         d.inv_sum = 1.0 / sum;
@@ -448,6 +454,9 @@ __global__ void __launch_bounds__(THREADS) k_accept_sampled(ghd_sampled a, int v
         const bool bad = i < n && (i == 0 ? p != -1 : p < 0 || p >= i);
         if (bad && m.rank == 0) atomicCAS(status, DEV_OK, DEV_SAMPLE_TREE);
         sm.parent[i] = bad ? -1 : p;
+        sm.token[i] = i < n ? __ldg(a.tokens + first + i) : -1;
+        sm.uniform[i] = i < n ? __ldg(a.uniforms + first + i) : 0.f;
+        sm.draft[i] = i < n && a.draft_row ? __ldg(a.draft_row + first + i) : -1;
     }
     __syncthreads();
     int node = 0, depth = 0;
@@ -459,15 +468,24 @@ __global__ void __launch_bounds__(THREADS) k_accept_sampled(ghd_sampled a, int v
         __syncthreads();
         bool any = false;
         for (int i = 0; i < GHD_MAX_NODES / 32; ++i) any |= sm.child[i] != 0;
-        int drawn = a.draft_row ? __ldg(a.draft_row + first + node) : -1;
+        int drawn = sm.draft[node];
         if (drawn >= a.n_draft) {
             record(DEV_SAMPLE_DRAFT);
             drawn = -1;
         }
         Dist p{a.logits + (size_t)(first + node) * vocab, scale, 0.0, 1.0, false, sm.roots}, q{};
         if (any && drawn >= 0) { q.row = a.draft_logits + (size_t)drawn * vocab; q.scale = draft_scale; q.roots = sm.roots; }
+        // the children's logits are on their way while the rows are measured
+        const int mine = threadIdx.x < GHD_MAX_NODES && (sm.child[m.warp % (GHD_MAX_NODES / 32)] >> m.lane & 1) ? sm.token[threadIdx.x] : -1;
+        const bool look = mine >= 0 && mine < vocab;
+        const float lp = look ? __ldg(p.row + mine) : 0.f, lq = look && q.row ? __ldg(q.row + mine) : 0.f;
         measure(m, p, q);
         if (!p.ok || (q.row && !q.ok)) record(DEV_SAMPLE_DIST);
+        if (threadIdx.x < GHD_MAX_NODES) {
+            sm.of_p[threadIdx.x] = look ? p.of(lp) : 0.0;
+            sm.of_q[threadIdx.x] = look && q.row ? q.of(lq) : 0.0;
+        }
+        __syncthreads();
         double beta = 0.0, W = 1.0, rejected = 0.0;
         int n_gone = 0, next = -1;
         bool fresh = false;                                    // seg[] and share[] are of the weights as they are, their total is W
@@ -475,11 +493,11 @@ __global__ void __launch_bounds__(THREADS) k_accept_sampled(ghd_sampled a, int v
         if (p.ok && (!q.row || q.ok))
             for (int word = 0; word < GHD_MAX_NODES / 32 && next < 0; ++word)
                 for (uint32_t bits = sm.child[word]; bits; bits &= bits - 1) {
-                    const int c = 32 * word + __ffs(bits) - 1, x = __ldg(a.tokens + first + c);
+                    const int c = 32 * word + __ffs(bits) - 1, x = sm.token[c];
                     if (x < 0 || x >= vocab) continue;
-                    const double u = unit(__ldg(a.uniforms + first + c)), px = p.at(x);
+                    const double u = unit(sm.uniform[c]), px = sm.of_p[c];
                     if (q.row) {
-                        const double qx = q.at(x);
+                        const double qx = sm.of_q[c];
                         bool before = false;                   // a token that was rejected already is not drawn again
                         for (int g = 0; g < n_gone; ++g) before |= sm.gone[g] == x;
                         if (!(qx > 0.0) || before) continue;
@@ -523,7 +541,7 @@ __global__ void __launch_bounds__(THREADS) k_accept_sampled(ghd_sampled a, int v
                         for (int r = 0; r < m.size; ++r) total += sm.share[r];
                     }
                 }
-                const double target = unit(__ldg(a.uniforms + first)) * total;
+                const double target = unit(sm.uniform[0]) * total;
                 double before, start;
                 if (own_share(m, target, before) && m.warp == 0) {
                     const int per = (m.segs + 31) / 32, sg = segment_of(m.seg, m.segs, per, lane_sum(m.seg, m.segs, per, m.lane), before, target, m.lane, start);
@@ -547,7 +565,7 @@ __global__ void __launch_bounds__(THREADS) k_accept_sampled(ghd_sampled a, int v
             break;
         }
         if (writes) {
-            out->tokens[depth] = __ldg(a.tokens + first + next);
+            out->tokens[depth] = sm.token[next];
             out->nodes[depth + 1] = next;
         }
         ++depth;
