@@ -400,7 +400,7 @@ ghd_status ghd_mx4_gate_up(ghd_ctx *ctx, const void *h, int64_t h_ld, const ghd_
  * The distribution of a row of logits (float [cfg.vocab]) is softmax(logits / temperature); -inf leaves a token out (top-k or
  * nucleus filters are such logits).  Random numbers are the caller's, float in [0, 1) (others are held to that); weights and sums are
  * worked out in 64 bits.  A row with a NaN or +inf, or with nothing but -inf, is none: ghd_sync_status -> GHD_EINVAL.
- * cfg.vocab up to 2^20 (GHD_ESHAPE). */
+ * cfg.vocab up to 2^20 (GHD_ESHAPE), temperatures in (0, 2^64]. */
 
 /* Candidates: for each of n_rows rows of logits (the heads of one sequence, or of many) n_draws tokens drawn without replacement.
  * Draw j is the first token t whose running sum of the weights not drawn yet exceeds uniforms[row][j] times their total; -1 once nothing

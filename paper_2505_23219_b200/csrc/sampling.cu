@@ -11,7 +11,6 @@
 // have to know of each other goes through distributed shared memory, one cluster barrier for each exchange.  Where a random number
 // falls is looked up over the CTAs, over a CTA's segments, over the lanes of one segment and over a lane's tokens, so that only one
 // segment's weights are worked out again.
-#include <cfloat>
 #include <cstdio>
 
 #include "internal.h"
@@ -21,7 +20,7 @@ namespace ghd {
 
 namespace {
 
-constexpr int THREADS = 512, WARPS = THREADS / 32;
+constexpr int THREADS = 256, WARPS = THREADS / 32;
 constexpr int MAX_CLUSTER = 8;
 constexpr int RUN = 8, SEG = 32 * RUN;          // tokens of a lane, of a segment
 constexpr int MAX_VOCAB = 1 << 20;
@@ -46,6 +45,7 @@ __device__ __forceinline__ void send(double* p, uint32_t rank, double v) {
     asm volatile("st.shared::cluster.f64 [%0], %1;" ::"r"(at), "d"(v) : "memory");
 }
 
+__device__ __forceinline__ float max_nan(float a, float b) { float r; asm("max.NaN.f32 %0, %1, %2;" : "=f"(r) : "f"(a), "f"(b)); return r; }
 __device__ __forceinline__ double warp_sum(double v) {
 #pragma unroll
     for (int o = 16; o; o >>= 1) v += __shfl_xor_sync(0xffffffffu, v, o);
@@ -58,7 +58,7 @@ __device__ __forceinline__ double warp_max(double v) {
 }
 __device__ __forceinline__ float warp_max(float v) {
 #pragma unroll
-    for (int o = 16; o; o >>= 1) v = fmaxf(v, __shfl_xor_sync(0xffffffffu, v, o));
+    for (int o = 16; o; o >>= 1) v = max_nan(v, __shfl_xor_sync(0xffffffffu, v, o));
     return v;
 }
 // inclusive running sums over the lanes
@@ -87,7 +87,7 @@ __constant__ double ROOTS[32] = {
     1.681792830507429, 1.718619298122478, 1.7562521603732995, 1.7947090750031072,
     1.8340080864093424, 1.8741676341103, 1.9152065613971474, 1.9571441241754002,
 };
-// 2^y of y <= 0, 0 below -1000, NaN of NaN.  Table-driven, after Tang (ACM TOMS 15, 1989): y = n / 32 + f with the nearest whole n, 2^(n / 32)
+// 2^y of y <= 0, 0 below -1000.  Table-driven, after Tang (ACM TOMS 15, 1989): y = n / 32 + f with the nearest whole n, 2^(n / 32)
 // from the table (in shared memory) and the exponent, and the series of e^(f ln 2), whose first term left out is below 2^-48 for |f| <= 1/64: the
 // borders between tokens move by that.  (The library's function takes any argument and more than twice the instructions.)
 __device__ __forceinline__ double pow2(double y, const double* roots) {
@@ -102,10 +102,16 @@ __device__ __forceinline__ double pow2(double y, const double* roots) {
     r = fma(r, f, C1);
     r = fma(r * f, root, root);
     r = __hiloint2double(__double2hiint(r) + (n >> 5 << 20), __double2loint(r));
-    return y >= -1000.0 ? r : y < -1000.0 ? 0.0 : y;
+    return y >= -1000.0 ? r : 0.0;
+}
+// A float as a double by its bits (the conversion has a quarter of the other instructions' rate): numbers below 2^-126 come out below
+// 2^-126, infinities as 2^128, which is as good for weights (a temperature is at most 2^64); NaN is found by the row's maximum.
+__device__ __forceinline__ double widen(float l) {
+    const uint32_t b = __float_as_uint(l);
+    return __hiloint2double((int)((b & 0x80000000u) | ((b & 0x7fffffffu) >> 3) + 0x38000000u), (int)(b << 29));
 }
 // The product is rounded before the difference: equal logits are equally likely however large they are.
-__device__ __forceinline__ double weight(float l, double scale, double ref, const double* roots) { return pow2(__dsub_rn(__dmul_rn((double)l, scale), ref), roots); }
+__device__ __forceinline__ double weight(float l, double scale, double ref, const double* roots) { return pow2(__dsub_rn(__dmul_rn(widen(l), scale), ref), roots); }
 
 // One row's distribution: 2^(l * scale - ref) / sum, scale = log2(e) / temperature.
 struct Dist {
@@ -201,8 +207,10 @@ __device__ void measure(Team& m, Dist& p, Dist& q) {
             const double scale = i ? q.scale : p.scale;
             float top = x[i][0];
 #pragma unroll
-            for (int e = 1; e < RUN; ++e) top = fmaxf(top, x[i][e]);
-            const double r = ceil(__dmul_rn((double)warp_max(top), scale));        // (a NaN is left out of the maximum, and makes the sum one)
+            for (int e = 1; e < RUN; ++e) top = max_nan(top, x[i][e]);
+            const float high = warp_max(top);
+            // NaN and infinity are kept apart from all numbers: a reference that no number gives
+            const double r = high < INFINITY ? ceil(__dmul_rn((double)high, scale)) : INFINITY;
             const double sum = warp_sum(sum_of(x[i], scale, r, p.roots));
             if (i == 0 && m.lane == 0) { m.seg[g] = sum; m.seg[m.segs + g] = r; }
             const double both = fmax(ref[i], r);
@@ -376,7 +384,7 @@ __device__ __forceinline__ double unit(float u) { return (double)fminf(fmaxf(u, 
 // ---------------------------------------------------------------- candidates
 // When the row has been measured its first CTA gets all segments' weights and draws alone, with one warp: what it takes to find a token
 // is one segment's logits.
-__global__ void __launch_bounds__(THREADS) k_draft_sample(const float* __restrict__ logits, int vocab, int cluster, double scale, int draws,
+__global__ void __launch_bounds__(THREADS, 4) k_draft_sample(const float* __restrict__ logits, int vocab, int cluster, double scale, int draws,
                                                           const float* __restrict__ uniforms, int32_t* __restrict__ cand, int* status) {
     extern __shared__ double weights[];
     __shared__ Shared sm;
@@ -432,7 +440,7 @@ __global__ void __launch_bounds__(THREADS) k_draft_sample(const float* __restric
 // beta_{j+1} = beta_j + c_j W_j, and c_j = 1 / (1 - Q(rejected)).  A rejected token has u Q_j >= P_j, u < 1, so P_{j+1} gives it
 // nothing, and so do all later ones: beta only grows.  So two numbers are kept instead of two distributions, and a rejection costs
 // one sum over the vocabulary.  Candidates that nobody drew have Q = 1 at themselves: P_{j+1} is P_j without x.
-__global__ void __launch_bounds__(THREADS) k_accept_sampled(ghd_sampled a, int vocab, double scale, double draft_scale, int cluster, ghd_accept_result* __restrict__ results, int* status) {
+__global__ void __launch_bounds__(THREADS, 2) k_accept_sampled(ghd_sampled a, int vocab, double scale, double draft_scale, int cluster, ghd_accept_result* __restrict__ results, int* status) {
     extern __shared__ double weights[];
     __shared__ Shared sm;
     Team m(&sm, weights, vocab, cluster);
@@ -579,11 +587,10 @@ __global__ void __launch_bounds__(THREADS) k_accept_sampled(ghd_sampled a, int v
     if (cluster > 1) tc::cluster_sync_all();
 }
 
-// CTAs to a row: as many as leave each of them a SM of its own and four segments
-int cluster_for(const ghd_ctx* c, int rows, int vocab) {
-    int k = MAX_CLUSTER;
-    while (k > 1 && ((int64_t)k * rows > c->sm_count || vocab < 4 * SEG * k)) k >>= 1;
-    return k;
+// CTAs to a row: as many as leave each of them room beside the others (`held` to a SM) and four segments
+int cluster_for(const ghd_ctx* c, int rows, int vocab, int held) {
+    const int64_t k = (int64_t)held * c->sm_count / rows, most = vocab / (4 * SEG);
+    return (int)(k < 1 || most < 1 ? 1 : k > most ? (most > MAX_CLUSTER ? MAX_CLUSTER : most) : k > MAX_CLUSTER ? MAX_CLUSTER : k);
 }
 // room for a CTA's segments twice over (weights and references), and in a row's first CTA for the weights of all
 size_t room_for(int vocab, int cluster) {
@@ -613,13 +620,13 @@ extern "C" {
 ghd_status ghd_draft_sample(ghd_ctx* c, const float* logits, int32_t n_rows, float temperature, int32_t n_draws, const float* uniforms, int32_t* cand) {
     if (!c) return GHD_EINVAL;
     if (n_rows < 0 || n_draws < 1 || n_draws > GHD_MAX_TOPK) return fail(c, GHD_EINVAL, "draft_sample: negative n_rows, or n_draws outside [1, 16]");
-    if (!(temperature > 0.f) || !(temperature <= FLT_MAX)) return fail(c, GHD_EINVAL, "draft_sample: temperature is not a positive number");
+    if (!(temperature > 0.f) || !(temperature <= 0x1p64f)) return fail(c, GHD_EINVAL, "draft_sample: temperature outside (0, 2^64]");
     if (c->cfg.vocab > MAX_VOCAB) return fail(c, GHD_ESHAPE, "draft_sample: a vocabulary above 2^20");
     if (n_rows == 0) return GHD_OK;
     if (n_rows > (1 << 24)) return fail(c, GHD_EINVAL, "draft_sample: more than 2^24 rows");
     if (!logits || !uniforms || !cand) return fail(c, GHD_EINVAL, "draft_sample: null pointer");
     if (!c->ws) return fail(c, GHD_ENOSPACE, "no workspace set");
-    const int k = cluster_for(c, n_rows, c->cfg.vocab);
+    const int k = cluster_for(c, n_rows, c->cfg.vocab, 4);
     ghd_status s = raise_room(c);
     if (s != GHD_OK) return s;
     launch_kc(c, false, k, k_draft_sample, n_rows * k, THREADS, room_for(c->cfg.vocab, k), logits, c->cfg.vocab, k, scale_of(temperature), n_draws, uniforms, cand, c->input_status);
@@ -631,14 +638,14 @@ ghd_status ghd_accept_sampled(ghd_ctx* c, const ghd_sampled* a, ghd_accept_resul
     if (a->n_seqs < 1 || a->n_seqs > GHD_MAX_SEQS || a->n_rows < 0) return fail(c, GHD_EINVAL, "accept_sampled: n_seqs outside [1, 1024] or negative n_rows");
     if (!a->row_start && a->n_seqs != 1) return fail(c, GHD_EINVAL, "accept_sampled: several sequences without row_start");
     if (!a->row_start && a->n_rows > GHD_MAX_NODES) return fail(c, GHD_ETREE, "accept_sampled: a tree of more than 256 nodes");
-    if (!(a->temperature > 0.f) || !(a->temperature <= FLT_MAX)) return fail(c, GHD_EINVAL, "accept_sampled: temperature is not a positive number");
+    if (!(a->temperature > 0.f) || !(a->temperature <= 0x1p64f)) return fail(c, GHD_EINVAL, "accept_sampled: temperature outside (0, 2^64]");
     if (c->cfg.vocab > MAX_VOCAB) return fail(c, GHD_ESHAPE, "accept_sampled: a vocabulary above 2^20");
     if (!results_dev || (a->n_rows > 0 && (!a->parent || !a->tokens || !a->logits || !a->uniforms))) return fail(c, GHD_EINVAL, "accept_sampled: null pointer");
     if ((a->draft_row == nullptr) != (a->draft_logits == nullptr)) return fail(c, GHD_EINVAL, "accept_sampled: give both draft_row and draft_logits or neither");
-    if (a->draft_row && (a->n_draft < 1 || !(a->draft_temperature > 0.f) || !(a->draft_temperature <= FLT_MAX)))
-        return fail(c, GHD_EINVAL, "accept_sampled: no draft rows, or a draft temperature that is not a positive number");
+    if (a->draft_row && (a->n_draft < 1 || !(a->draft_temperature > 0.f) || !(a->draft_temperature <= 0x1p64f)))
+        return fail(c, GHD_EINVAL, "accept_sampled: no draft rows, or a draft temperature outside (0, 2^64]");
     if (!c->ws) return fail(c, GHD_ENOSPACE, "no workspace set");
-    const int k = cluster_for(c, a->n_seqs, c->cfg.vocab);
+    const int k = cluster_for(c, a->n_seqs, c->cfg.vocab, 2);
     ghd_status s = raise_room(c);
     if (s != GHD_OK) return s;
     launch_kc(c, false, k, k_accept_sampled, a->n_seqs * k, THREADS, room_for(c->cfg.vocab, k), *a, c->cfg.vocab, scale_of(a->temperature), a->draft_row ? scale_of(a->draft_temperature) : 0.0, k, results_dev, c->input_status);
