@@ -40,6 +40,7 @@ size_t carve_workspace(ghd_ctx* c, char* base) {
     c->gemm_part = (float*)take((size_t)c->sm_count * 2 * 256 * 128 * 4);
     c->logits = (float*)take(N * (size_t)m.vocab * 4);
     c->mlogits = (float*)take((size_t)GHD_MAX_DRAFT_HEADS * m.vocab * 4);
+    c->sample_segs = take((size_t)SAMPLE_SEGS * 16);
     c->mx4_terms = (uint8_t*)take(mx4_terms_bytes(m));
     return off;
 }

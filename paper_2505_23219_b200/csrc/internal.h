@@ -29,6 +29,7 @@ enum Epilogue : int {
     EPI_RESID_NORM = 5,   // xres += acc; xg T [n][m] = xres * gain (not yet divided by the rms); per-tile sums of squares
 };
 
+constexpr int SAMPLE_SEGS = 48 * 1024;     // segments of 256 logits that a sampled acceptance weighs ahead of its walk at most
 constexpr int SSQ_PITCH = GHD_MAX_NODES;   // floats per 128-feature tile in a sum-of-squares buffer
 constexpr int SSQ_MAX_TILES = 64;
 
@@ -105,6 +106,7 @@ struct ghd_ctx {
     int h_ssq;        // which of them describes hbuf (-1: hbuf is already normalised)
     float* logits;    // float [max_nodes][vocab]
     float* mlogits;   // float [8][vocab] logits of the drafting heads
+    void* sample_segs;    // {weight, reference} of the segments of logits' rows (SAMPLE_SEGS of them)
     uint8_t* mx4_terms;   // e4m3 terms of the rows of x and their scales (products with 4-bit matrices)
     int *status, *input_status;      // device status words: waits that ran out, data out of range
     int* kv_len_word; // device word with the cache length (calls given GHD_KV_LEN_DEVICE read it)

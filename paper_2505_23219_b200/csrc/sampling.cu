@@ -191,6 +191,17 @@ __device__ __forceinline__ double sum_of(const float (&x)[RUN], double scale, do
     return ((w[0] + w[1]) + (w[2] + w[3])) + ((w[4] + w[5]) + (w[6] + w[7]));
 }
 
+// One warp: weight of a segment and its reference, from this lane's logits
+__device__ __forceinline__ double segment_sum(const float (&x)[RUN], double scale, const double* roots, double& ref) {
+    float top = x[0];
+#pragma unroll
+    for (int e = 1; e < RUN; ++e) top = max_nan(top, x[e]);
+    top = warp_max(top);
+    // NaN and infinity are kept apart from all numbers: a reference that no number gives
+    ref = top < INFINITY ? ceil(__dmul_rn((double)top, scale)) : INFINITY;
+    return warp_sum(sum_of(x, scale, ref, roots));
+}
+
 // Reference and sum of a row p and, if q.row is given, of a second one.  seg[] is left with p's weights (not divided by the sum),
 // share[] has every CTA's part of p's sum.
 __device__ void measure(Team& m, Dist& p, Dist& q) {
@@ -204,14 +215,8 @@ __device__ void measure(Team& m, Dist& p, Dist& q) {
 #pragma unroll
         for (int i = 0; i < 2; ++i) {
             if (i == 1 && n == 1) break;
-            const double scale = i ? q.scale : p.scale;
-            float top = x[i][0];
-#pragma unroll
-            for (int e = 1; e < RUN; ++e) top = max_nan(top, x[i][e]);
-            const float high = warp_max(top);
-            // NaN and infinity are kept apart from all numbers: a reference that no number gives
-            const double r = high < INFINITY ? ceil(__dmul_rn((double)high, scale)) : INFINITY;
-            const double sum = warp_sum(sum_of(x[i], scale, r, p.roots));
+            double r;
+            const double sum = segment_sum(x[i], i ? q.scale : p.scale, p.roots, r);
             if (i == 0 && m.lane == 0) { m.seg[g] = sum; m.seg[m.segs + g] = r; }
             const double both = fmax(ref[i], r);
             all[i] = all[i] * pow2_whole(ref[i] - both) + sum * pow2_whole(r - both);
@@ -347,8 +352,8 @@ __device__ __forceinline__ void without(double (&w)[RUN], int t0, const int32_t*
     }
 }
 
-// seg[] and share[] after measure(), without the tokens gone[0 .. n) -> the total
-__device__ double total_without(Team& m, const Dist& p, int n) {
+// seg[] after measure(), without the tokens gone[0 .. n)
+__device__ void weigh_again(Team& m, const Dist& p, int n) {
     __syncthreads();
 #pragma unroll 1
     for (int i = m.warp; i < n; i += WARPS) {
@@ -369,6 +374,9 @@ __device__ double total_without(Team& m, const Dist& p, int n) {
         if (m.lane == 0) m.seg[g] = sum;
     }
     __syncthreads();
+}
+// share[] from seg[] -> the total
+__device__ double total_again(Team& m) {
     if (m.warp == 0) {
         double sum = 0.0;
         for (int g = m.lane; g < m.segs; g += 32) sum += m.seg[g];
@@ -376,6 +384,44 @@ __device__ double total_without(Team& m, const Dist& p, int n) {
         if (m.lane == 0) m.s->mine[0] = sum;
     }
     return m.add_shares(m.exchange(1));
+}
+
+// Reference and sum of one row (or two) whose segments k_row_segments has weighed: every CTA for itself.
+__device__ void collect(Team& m, int n_segs, const double2* sp, const double2* sq, Dist& p, Dist& q) {
+    const int n = q.row ? 2 : 1;
+    double ref[2] = {-INFINITY, -INFINITY}, sum[2] = {0.0, 0.0};
+    for (int g = threadIdx.x; g < n_segs; g += THREADS) {
+        const double2 v[2] = {sp[g], n == 2 ? sq[g] : make_double2(0.0, -INFINITY)};
+#pragma unroll
+        for (int i = 0; i < 2; ++i) {
+            const double both = fmax(ref[i], v[i].y);
+            sum[i] = sum[i] * pow2_whole(ref[i] - both) + v[i].x * pow2_whole(v[i].y - both);
+            ref[i] = both;
+        }
+    }
+    const int c = m.lane % WARPS;
+#pragma unroll
+    for (int i = 0; i < 2; ++i) {
+        if (i == 1 && n == 1) break;
+        const double both = warp_max(ref[i]), all = warp_sum(sum[i] * pow2_whole(ref[i] - both));
+        if (m.lane == 0) { m.s->part[i][m.warp][0] = both; m.s->part[i][m.warp][1] = all; }
+    }
+    __syncthreads();
+#pragma unroll
+    for (int i = 0; i < 2; ++i) {
+        if (i == 1 && n == 1) break;
+        const double r = m.s->part[i][c][0];
+        double both = r, all = m.s->part[i][c][1];
+#pragma unroll
+        for (int o = 1; o < WARPS; o <<= 1) both = fmax(both, __shfl_xor_sync(0xffffffffu, both, o));
+        all *= pow2_whole(r - both);
+#pragma unroll
+        for (int o = 1; o < WARPS; o <<= 1) all += __shfl_xor_sync(0xffffffffu, all, o);
+        Dist& d = i ? q : p;
+        d.ref = both;
+        d.inv_sum = 1.0 / all;
+        d.ok = both > -INFINITY && both < INFINITY && all < INFINITY;
+    }
 }
 
 // random numbers are held in [0, 1 - 2^-24]
@@ -440,7 +486,29 @@ __global__ void __launch_bounds__(THREADS, 4) k_draft_sample(const float* __rest
 // beta_{j+1} = beta_j + c_j W_j, and c_j = 1 / (1 - Q(rejected)).  A rejected token has u Q_j >= P_j, u < 1, so P_{j+1} gives it
 // nothing, and so do all later ones: beta only grows.  So two numbers are kept instead of two distributions, and a rejection costs
 // one sum over the vocabulary.  Candidates that nobody drew have Q = 1 at themselves: P_{j+1} is P_j without x.
-__global__ void __launch_bounds__(THREADS, 2) k_accept_sampled(ghd_sampled a, int vocab, double scale, double draft_scale, int cluster, ghd_accept_result* __restrict__ results, int* status) {
+// The segments' weights and references of all rows, of the targets and behind them of the drafts, a warp to a segment.  With few trees
+// the walk below knows its rows one after the other only, and most SMs would wait; weighing all rows first costs less than it saves.
+__global__ void __launch_bounds__(THREADS, 4) k_row_segments(const float* __restrict__ logits, const float* __restrict__ draft, int n_rows, int n_draft, int vocab, double scale,
+                                                             double draft_scale, double2* __restrict__ out) {
+    __shared__ Shared sm;
+    pdl_trigger();
+    Team m(&sm, nullptr, vocab, 1);
+    const int n = m.segs, total = (n_rows + n_draft) * n;
+    for (int t = blockIdx.x * WARPS + m.warp; t < total; t += gridDim.x * WARPS) {
+        const int row = t / n, g = t - row * n;
+        const bool target = row < n_rows;
+        float x[RUN];
+        m.load(target ? logits + (size_t)row * vocab : draft + (size_t)(row - n_rows) * vocab, m.first_of(g), x);
+        double ref;
+        const double sum = segment_sum(x, target ? scale : draft_scale, sm.roots, ref);
+        if (m.lane == 0) out[t] = make_double2(sum, ref);
+    }
+}
+
+// READY: k_row_segments has run.
+template <bool READY>
+__global__ void __launch_bounds__(THREADS, 2) k_accept_sampled(ghd_sampled a, int vocab, double scale, double draft_scale, int cluster, const double2* __restrict__ ready,
+                                                               ghd_accept_result* __restrict__ results, int* status) {
     extern __shared__ double weights[];
     __shared__ Shared sm;
     Team m(&sm, weights, vocab, cluster);
@@ -467,6 +535,8 @@ __global__ void __launch_bounds__(THREADS, 2) k_accept_sampled(ghd_sampled a, in
         sm.draft[i] = i < n && a.draft_row ? __ldg(a.draft_row + first + i) : -1;
     }
     __syncthreads();
+    const int n_segs = (vocab + SEG - 1) / SEG;
+    if (READY) pdl_wait();
     int node = 0, depth = 0;
     while (n > 0) {
         if (threadIdx.x < GHD_MAX_NODES) {
@@ -487,7 +557,8 @@ __global__ void __launch_bounds__(THREADS, 2) k_accept_sampled(ghd_sampled a, in
         const int mine = threadIdx.x < GHD_MAX_NODES && (sm.child[m.warp % (GHD_MAX_NODES / 32)] >> m.lane & 1) ? sm.token[threadIdx.x] : -1;
         const bool look = mine >= 0 && mine < vocab;
         const float lp = look ? __ldg(p.row + mine) : 0.f, lq = look && q.row ? __ldg(q.row + mine) : 0.f;
-        measure(m, p, q);
+        if (READY) collect(m, n_segs, ready + (size_t)(first + node) * n_segs, ready + (size_t)(a.n_rows + max(drawn, 0)) * n_segs, p, q);
+        else measure(m, p, q);
         if (!p.ok || (q.row && !q.ok)) record(DEV_SAMPLE_DIST);
         if (threadIdx.x < GHD_MAX_NODES) {
             sm.of_p[threadIdx.x] = look ? p.of(lp) : 0.0;
@@ -542,8 +613,19 @@ __global__ void __launch_bounds__(THREADS, 2) k_accept_sampled(ghd_sampled a, in
                 if (!fresh) {
                     p.inv_sum = 1.0;
                     if (q.row) n_gone = 0;
-                    if (n_gone > 0) {
-                        total = total_without(m, p, n_gone);
+                    if (READY) {
+                        if (m.rank != 0) break;
+                        // the first CTA has all of the row
+                        m.size = 1;
+                        m.seg0 = 0;
+                        m.segs = n_segs;
+                        const double2* row = ready + (size_t)(first + node) * n_segs;
+                        for (int g = threadIdx.x; g < n_segs; g += THREADS) m.seg[g] = row[g].x * pow2_whole(row[g].y - p.ref);
+                    }
+                    if (n_gone > 0) weigh_again(m, p, n_gone);
+                    if (READY) __syncthreads();
+                    if (READY || n_gone > 0) {
+                        total = total_again(m);
                     } else {
                         total = 0.0;
                         for (int r = 0; r < m.size; ++r) total += sm.share[r];
@@ -584,7 +666,7 @@ __global__ void __launch_bounds__(THREADS, 2) k_accept_sampled(ghd_sampled a, in
         out->n_matched = depth;
         out->n_emitted = n > 0 ? depth + 1 : 0;
     }
-    if (cluster > 1) tc::cluster_sync_all();
+    if (cluster > 1) tc::cluster_sync_all();                   // nobody leaves while others may write to its shared memory
 }
 
 // CTAs to a row: as many as leave each of them room beside the others (`held` to a SM) and four segments
@@ -603,7 +685,8 @@ double scale_of(float temperature) { return 1.44269504088896340736 / (double)tem
 ghd_status raise_room(ghd_ctx* c) {              // (a CTA with all segments of the largest vocabulary takes 64 KB)
     if (c->attr_sampling) return GHD_OK;
     if (cudaFuncSetAttribute(k_draft_sample, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)room_for(MAX_VOCAB, 1)) != cudaSuccess ||
-        cudaFuncSetAttribute(k_accept_sampled, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)room_for(MAX_VOCAB, 1)) != cudaSuccess)
+        cudaFuncSetAttribute(k_accept_sampled<true>, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)room_for(MAX_VOCAB, 1)) != cudaSuccess ||
+        cudaFuncSetAttribute(k_accept_sampled<false>, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)room_for(MAX_VOCAB, 1)) != cudaSuccess)
         return check_cuda(c, "sampling: shared memory");
     c->attr_sampling = true;
     return GHD_OK;
@@ -648,7 +731,18 @@ ghd_status ghd_accept_sampled(ghd_ctx* c, const ghd_sampled* a, ghd_accept_resul
     const int k = cluster_for(c, a->n_seqs, c->cfg.vocab, 2);
     ghd_status s = raise_room(c);
     if (s != GHD_OK) return s;
-    launch_kc(c, false, k, k_accept_sampled, a->n_seqs * k, THREADS, room_for(c->cfg.vocab, k), *a, c->cfg.vocab, scale_of(a->temperature), a->draft_row ? scale_of(a->draft_temperature) : 0.0, k, results_dev, c->input_status);
+    c->entry_fresh = 1;
+    const double scale = scale_of(a->temperature), draft_scale = a->draft_row ? scale_of(a->draft_temperature) : 0.0;
+    const size_t room = room_for(c->cfg.vocab, k);
+    const int64_t segs = ((int64_t)a->n_rows + (a->draft_row ? a->n_draft : 0)) * ((c->cfg.vocab + SEG - 1) / SEG);
+    if (segs > 0 && segs <= SAMPLE_SEGS) {
+        const int64_t most = 4 * c->sm_count, ctas = (segs + WARPS - 1) / WARPS;
+        launch_k(c, false, k_row_segments, (int)(ctas < most ? ctas : most), THREADS, 0, a->logits, a->draft_logits, a->n_rows, a->draft_row ? a->n_draft : 0, c->cfg.vocab, scale, draft_scale,
+                 (double2*)c->sample_segs);
+        launch_kc(c, true, k, k_accept_sampled<true>, a->n_seqs * k, THREADS, room, *a, c->cfg.vocab, scale, draft_scale, k, (const double2*)c->sample_segs, results_dev, c->input_status);
+    } else {
+        launch_kc(c, false, k, k_accept_sampled<false>, a->n_seqs * k, THREADS, room, *a, c->cfg.vocab, scale, draft_scale, k, (const double2*)nullptr, results_dev, c->input_status);
+    }
     return check_cuda(c, "accept_sampled");
 }
 
