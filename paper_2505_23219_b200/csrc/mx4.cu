@@ -10,40 +10,65 @@ namespace {
 using namespace mx4;
 
 // ---------------------------------------------------------------- quantise, read back
-// A warp takes 256 columns of a row at a time, 8 to a lane, so that four lanes have the 32 elements of a scale.
-constexpr int ROWS_PER_CTA = 32;
+// Both are bound by memory; a lane has eight elements of a row (read) or sixteen (quantise: two lanes to a scale), and the loads of ROWS
+// neighbouring rows go out together.
+constexpr int ROWS = 4, ROWS_PER_CTA = 8 * ROWS;      // rows of a warp
+
+// largest magnitude of sixteen elements, NaN if one is
+template <typename T> __device__ __forceinline__ float top_of(const T (&t)[16]);
+template <> __device__ __forceinline__ float top_of<float>(const float (&t)[16]) {
+    float a = fabsf(t[0]);
+#pragma unroll
+    for (int e = 1; e < 16; ++e) a = max_nan(a, fabsf(t[e]));
+    return a;
+}
+template <> __device__ __forceinline__ float top_of<__half>(const __half (&t)[16]) {
+    const __half2* h = reinterpret_cast<const __half2*>(t);
+    __half2 a = __habs2(h[0]);
+#pragma unroll
+    for (int e = 1; e < 8; ++e) a = __hmax2_nan(a, __habs2(h[e]));
+    return max_nan(__low2float(a), __high2float(a));
+}
 
 template <typename T>
-__global__ void __launch_bounds__(256) k_mx4_quantize(const T* __restrict__ x, int64_t ld, int m, int k, bool wide, uint32_t* __restrict__ codes, uint32_t* __restrict__ scales) {
+__global__ void __launch_bounds__(256) k_mx4_quantize(const T* __restrict__ x, int64_t ld, int m, int k, bool wide, uint2* __restrict__ codes, uint32_t* __restrict__ scales) {
     const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5, kt = (k + TILE - 1) / TILE;
-    const int c0 = blockIdx.x * 256 + lane * 8, tile_k = c0 / TILE;
-    if (c0 - lane * 8 + (lane & 16) * 8 >= kt * TILE) return;      // (16 lanes to a tile: they leave together)
-    for (int i = warp; i < ROWS_PER_CTA; i += 8) {
-        const int row = blockIdx.y * ROWS_PER_CTA + i;
-        float v[8];
-        if (row < m) load8(x + row * ld, c0, k, wide, v);
-        else {
+    const int c0 = blockIdx.x * 512 + lane * 16, tile_k = c0 / TILE;
+    if (tile_k >= kt) return;                                      // (8 lanes to a tile: they leave together)
+    const uint32_t mask = 0xffu << (lane & 24);
+    const int row0 = blockIdx.y * ROWS_PER_CTA + warp * ROWS;
+    alignas(16) T t[ROWS][16];
 #pragma unroll
-            for (int e = 0; e < 8; ++e) v[e] = 0.f;
+    for (int i = 0; i < ROWS; ++i) {
+        const T* row = x + (row0 + i) * ld;
+        if (row0 + i < m && wide && c0 + 16 <= k) {
+#pragma unroll
+            for (int j = 0; j < (int)sizeof(T); ++j) reinterpret_cast<uint4*>(t[i])[j] = __ldg(reinterpret_cast<const uint4*>(row + c0) + j);
+        } else {
+#pragma unroll
+            for (int e = 0; e < 16; ++e) t[i][e] = row0 + i < m && c0 + e < k ? row[c0 + e] : T(0.f);
         }
-        const uint32_t mask = 0xffffu << (lane & 16);
-        float top = 0.f;
+    }
 #pragma unroll
-        for (int e = 0; e < 8; ++e) top = max_nan(top, fabsf(v[e]));
+    for (int i = 0; i < ROWS; ++i) {
+        float top = top_of<T>(t[i]);
         top = max_nan(top, __shfl_xor_sync(mask, top, 1));
-        top = max_nan(top, __shfl_xor_sync(mask, top, 2));
         // exponent field of the largest magnitude less 2: floor(log2) - 2 + 127, and 255 for infinity and NaN
         const uint32_t field = (__float_as_uint(top) >> 23) & 255u;
         const uint32_t byte = field == 255u ? 255u : field > 2u ? field - 2u : 0u;
-        const float inv = __uint_as_float((254u - byte) << 23);     // 2^(127 - byte): at most 2^127, and 2^-125 at least
+        const float inv = byte == 255u ? 0.f : __uint_as_float((254u - byte) << 23);     // 2^(127 - byte): at most 2^127, and 2^-125 at least
+        float v[2][8];
 #pragma unroll
-        for (int e = 0; e < 8; ++e) v[e] = byte == 255u ? 0.f : v[e] * inv;
+        for (int e = 0; e < 16; ++e) v[e / 8][e % 8] = to_f<T>(t[i][e]) * inv;
+        uint2 c = make_uint2(codes_of(v[0]), codes_of(v[1]));
+        if (byte == 255u) c = make_uint2(0u, 0u);
+        const int row = row0 + i;
         const size_t tile = (size_t)(row / TILE) * kt + tile_k;
-        codes[tile * (TILE_CODES / 4) + (row % TILE) * (TILE / 8) + (lane & 15)] = codes_of(v);
-        uint32_t s = byte << (8 * ((lane >> 2) & 3));
+        codes[tile * (TILE_CODES / 8) + (row % TILE) * (TILE / 16) + (lane & 7)] = c;
+        uint32_t s = byte << (8 * ((lane >> 1) & 3));
+        s |= __shfl_xor_sync(mask, s, 2);
         s |= __shfl_xor_sync(mask, s, 4);
-        s |= __shfl_xor_sync(mask, s, 8);
-        if ((lane & 15) == 0) scales[tile * (TILE_SCALES / 4) + scale_at(row % TILE, 0) / 4] = s;
+        if ((lane & 7) == 0) scales[tile * (TILE_SCALES / 4) + scale_at(row % TILE, 0) / 4] = s;
     }
 }
 
@@ -52,13 +77,21 @@ __global__ void __launch_bounds__(256) k_mx4_read(const uint32_t* __restrict__ c
     const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5, kt = (k + TILE - 1) / TILE;
     const int c0 = blockIdx.x * 256 + lane * 8;
     if (c0 >= k) return;
-    for (int i = warp; i < ROWS_PER_CTA; i += 8) {
-        const int row = blockIdx.y * ROWS_PER_CTA + i;
-        if (row >= m) return;
+    uint32_t codes8[ROWS], words[ROWS];
+#pragma unroll
+    for (int i = 0; i < ROWS; ++i) {
+        const int row = min((int)blockIdx.y * ROWS_PER_CTA + warp * ROWS + i, m - 1);
         const size_t tile = (size_t)(row / TILE) * kt + c0 / TILE;
+        codes8[i] = __ldg(codes + tile * (TILE_CODES / 4) + (row % TILE) * (TILE / 8) + (lane & 15));
+        words[i] = __ldg(scales + tile * (TILE_SCALES / 4) + scale_at(row % TILE, 0) / 4);
+    }
+#pragma unroll
+    for (int i = 0; i < ROWS; ++i) {
+        const int row = blockIdx.y * ROWS_PER_CTA + warp * ROWS + i;
+        if (row >= m) return;
         float v[8];
-        levels_of(__ldg(codes + tile * (TILE_CODES / 4) + (row % TILE) * (TILE / 8) + (lane & 15)), v);
-        const float s = pow2_of(__ldg(scales + tile * (TILE_SCALES / 4) + scale_at(row % TILE, 0) / 4) >> (8 * ((lane >> 2) & 3)) & 255u);
+        levels_of(codes8[i], v);
+        const float s = pow2_of(words[i] >> (8 * ((lane >> 2) & 3)) & 255u);
 #pragma unroll
         for (int e = 0; e < 8; ++e) v[e] *= s;
         store8(out + row * ld, c0, k, wide, v);
@@ -120,10 +153,10 @@ ghd_status ghd_mx4_quantize(ghd_ctx* c, const void* x, int64_t ld, const ghd_mx4
     if (!c) return GHD_EINVAL;
     ghd_status s;
     if ((s = check_matrix(c, w)) != GHD_OK || (s = check_rows(c, x, &ld, w->k, "mx4_quantize: null x")) != GHD_OK) return s;
-    const dim3 grid((w->k + 255) / 256, (w->m + TILE - 1) / TILE * (TILE / ROWS_PER_CTA));
+    const dim3 grid((w->k + 511) / 512, (w->m + TILE - 1) / TILE * (TILE / ROWS_PER_CTA));
     const bool wide = wide_rows(c, x, ld);
-    if (c->cfg.dtype == GHD_F32) launch_k(c, false, k_mx4_quantize<float>, grid, 256, 0, (const float*)x, ld, w->m, w->k, wide, (uint32_t*)w->codes, (uint32_t*)w->scales);
-    else launch_k(c, false, k_mx4_quantize<__half>, grid, 256, 0, (const __half*)x, ld, w->m, w->k, wide, (uint32_t*)w->codes, (uint32_t*)w->scales);
+    if (c->cfg.dtype == GHD_F32) launch_k(c, false, k_mx4_quantize<float>, grid, 256, 0, (const float*)x, ld, w->m, w->k, wide, (uint2*)w->codes, (uint32_t*)w->scales);
+    else launch_k(c, false, k_mx4_quantize<__half>, grid, 256, 0, (const __half*)x, ld, w->m, w->k, wide, (uint2*)w->codes, (uint32_t*)w->scales);
     return check_cuda(c, "mx4_quantize");
 }
 

@@ -33,7 +33,7 @@ using namespace mx4;
 using namespace tc;
 
 constexpr int THREADS = 384;            // weights' loads, MMAs, eight epilogue warps, x's loads, weights to the L2
-constexpr int AHEAD = 192 * 1024;       // bytes of weights that a CTA has on their way from memory to the L2
+constexpr int AHEAD = 32 * 1024;        // bytes of weights that a CTA has asked the L2 for beyond its loads (192 KB: 2 us more for 16 rows of an lm_head, whose first loads wait)
 constexpr int MAX_STAGES = 10;
 constexpr int CHUNK = 64;               // k-steps of 128 that one accumulator takes
 constexpr int MAX_WORKERS = 1024;       // CTAs at most: each has an arrival counter
