@@ -37,7 +37,7 @@ struct Shared {
     float uniform[GHD_MAX_NODES];
     double of_p[GHD_MAX_NODES], of_q[GHD_MAX_NODES];          // of the children of the node: their tokens' probabilities
     int32_t gone[GHD_MAX_NODES];                // tokens that are not in the distribution any more
-    double roots[32];
+    double roots[16];
 };
 
 __device__ __forceinline__ void send(double* p, uint32_t rank, double v) {
@@ -76,33 +76,31 @@ __device__ __forceinline__ double pow2_whole(double n) {
     if (!(n < 0.0)) return 1.0;
     return n < -1000.0 ? 0.0 : __hiloint2double((1023 + (int)n) << 20, 0);
 }
-// 2^(j / 32), rounded
-__constant__ double ROOTS[32] = {
-    1.0, 1.0218971486541166, 1.0442737824274138, 1.0671404006768237,
-    1.0905077326652577, 1.1143867425958924, 1.1387886347566916, 1.1637248587775775,
-    1.189207115002721, 1.215247359980469, 1.241857812073484, 1.2690509571917332,
-    1.2968395546510096, 1.3252366431597413, 1.3542555469368927, 1.383909881963832,
-    1.4142135623730951, 1.4451808069770467, 1.4768261459394993, 1.5091644275934228,
-    1.5422108254079407, 1.5759808451078865, 1.6104903319492543, 1.645755478153965,
-    1.681792830507429, 1.718619298122478, 1.7562521603732995, 1.7947090750031072,
-    1.8340080864093424, 1.8741676341103, 1.9152065613971474, 1.9571441241754002,
+// 2^(j / 16), rounded
+__constant__ double ROOTS[16] = {
+    1.0, 1.0442737824274138, 1.0905077326652577, 1.1387886347566916,
+    1.189207115002721, 1.241857812073484, 1.2968395546510096, 1.3542555469368927,
+    1.4142135623730951, 1.4768261459394993, 1.5422108254079407, 1.6104903319492543,
+    1.681792830507429, 1.7562521603732995, 1.8340080864093424, 1.9152065613971474,
 };
-// 2^y of y <= 0, 0 below -1000.  Table-driven, after Tang (ACM TOMS 15, 1989): y = n / 32 + f with the nearest whole n, 2^(n / 32)
-// from the table (in shared memory) and the exponent, and the series of e^(f ln 2), whose first term left out is below 2^-48 for |f| <= 1/64: the
-// borders between tokens move by that.  (The library's function takes any argument and more than twice the instructions.)
+// 2^y of y <= 0, 0 below -1000.  Table-driven, after Tang (ACM TOMS 15, 1989): y = n / 16 + f with the nearest whole n, 2^(n / 16) from
+// the table (in shared memory, a pair of banks to each entry) and the exponent, and the series of e^(f ln 2), whose first term left out is below
+// 2^-50 for |f| <= 1/32: the borders between tokens move by that.  (The library's function takes any argument and about twice the
+// instructions; 64-bit ones are what bounds the calls with many rows.)
 __device__ __forceinline__ double pow2(double y, const double* roots) {
-    constexpr double LN2 = 0.693147180559945309417, MAGIC = 6755399441055744.0 / 32;        // 1.5 * 2^52 / 32: adding it rounds to a whole 32nd
-    constexpr double C1 = LN2, C2 = LN2 * LN2 / 2, C3 = LN2 * LN2 * LN2 / 6, C4 = LN2 * LN2 * LN2 * LN2 / 24, C5 = LN2 * LN2 * LN2 * LN2 * LN2 / 120;
+    constexpr double L = 0.693147180559945309417, MAGIC = 6755399441055744.0 / 16;         // 1.5 * 2^52 / 16: adding it rounds to a whole 16th
+    constexpr double C1 = L, C2 = L * L / 2, C3 = L * L * L / 6, C4 = L * L * L * L / 24, C5 = L * L * L * L * L / 120, C6 = L * L * L * L * L * L / 720;
     const double t = y + MAGIC, f = y - (t - MAGIC);
     const int n = __double2loint(t);
-    const double root = roots[n & 31];
-    double r = fma(C5, f, C4);
+    const double root = roots[n & 15];
+    double r = fma(C6, f, C5);
+    r = fma(r, f, C4);
     r = fma(r, f, C3);
     r = fma(r, f, C2);
     r = fma(r, f, C1);
     r = fma(r * f, root, root);
-    r = __hiloint2double(__double2hiint(r) + (n >> 5 << 20), __double2loint(r));
-    return y >= -1000.0 ? r : 0.0;
+    r = __hiloint2double(__double2hiint(r) + (n >> 4 << 20), __double2loint(r));
+    return (uint32_t)__double2hiint(y) > 0xc08f4000u ? 0.0 : r;      // (below -1000, by its bits)
 }
 // A float as a double by its bits (the conversion has a quarter of the other instructions' rate): numbers below 2^-126 come out below
 // 2^-126, infinities as 2^128, which is as good for weights (a temperature is at most 2^64); NaN is found by the row's maximum.
@@ -138,7 +136,7 @@ struct Team {
         const int n = (vocab + SEG - 1) / SEG;
         seg0 = n * rank / cluster;
         segs = n * (rank + 1) / cluster - seg0;
-        if (threadIdx.x < 32) s->roots[threadIdx.x] = ROOTS[threadIdx.x];
+        if (threadIdx.x < 16) s->roots[threadIdx.x] = ROOTS[threadIdx.x];
         if (cluster > 1) tc::cluster_sync_all();                   // everybody's shared memory is there
         else __syncthreads();
     }
