@@ -389,7 +389,8 @@ ghd_status ghd_mx4_read(ghd_ctx *ctx, const ghd_mx4 *w, void *out, int64_t ld);
 
 /* ghd_linear with such a matrix: y float [n][m] = x T [n][k] * w[m][k]^T, x's rows x_ld elements apart (0: contiguous).
  * Products and sums have 32 bits: of 32 elements of x what is below 2^-27 (GHD_F32: 2^-37, and 2^-136) of the largest is rounded, and
- * a row with a NaN or an infinity gives NaN throughout.  1 <= n <= max_nodes, k at most the larger of d_model and d_ffn (GHD_ENOSPACE). */
+ * a row with a NaN or an infinity gives NaN throughout.  1 <= n <= max_nodes, k at most the larger of d_model and d_ffn (GHD_ENOSPACE).
+ * Intermediate results lie in the context's workspace: calls of one context, graphs recorded from it included, run one after another. */
 ghd_status ghd_mx4_linear(ghd_ctx *ctx, const void *x, int64_t x_ld, const ghd_mx4 *w, int32_t n, float *y);
 /* ghd_gate_up with two: u T [n][m] = SiLU(h Wg^T) * (h Wu^T), both [m][k]; h dev T [n][k], rows h_ld elements apart (0: contiguous). */
 ghd_status ghd_mx4_gate_up(ghd_ctx *ctx, const void *h, int64_t h_ld, const ghd_mx4 *w_gate, const ghd_mx4 *w_up, int32_t n, void *u);
@@ -436,7 +437,7 @@ typedef struct ghd_sampled {
  * (0 at a node without a distribution); entries behind these are -1.  A sequence without rows gets n_emitted 0 and no nodes.
  * Starts out of order, more than GHD_MAX_NODES rows (such a sequence is taken as empty) or a parent that is none (the row is passed
  * over): ghd_sync_status -> GHD_ETREE; a draft row from n_draft on (taken as -1): GHD_EINVAL.  At a node whose draft row has no distribution no
- * child is accepted. */
+ * child is accepted.  Intermediate results of trees of few rows lie in the context's workspace (see ghd_mx4_linear). */
 ghd_status ghd_accept_sampled(ghd_ctx *ctx, const ghd_sampled *rows, ghd_accept_result *results_dev);
 
 /* Building blocks of the layer, exposed for unit tests (same kernels the layer uses).

@@ -242,6 +242,70 @@ def test_nan_and_infinity_stay_in_their_rows(ghd, dtype):
     assert (np.abs(y[rest] - X @ W.T) <= product_bound(X, W, k))[:, keep].all()
 
 
+def test_streams_graphs_and_a_shared_workspace(ghd):
+    """Calls of many shapes one after the other through one workspace; a context on its own stream; calls recorded and replayed with other inputs."""
+    import torch
+    r = np.random.RandomState(21)
+    side = torch.cuda.Stream()
+    with torch.cuda.stream(side):
+        ctx = make_ctx(ghd, "f16", 2048, 200)
+    shapes = [(1, 300, 2048), (200, 513, 640), (3, 4096, 128), (64, 128, 1000), (33, 2000, 2048), (1, 1, 1)]
+    held = [random_held(ghd, r, m, k) for _, m, k in shapes]
+    xs = [r.randn(n, k).astype(np.float16) for n, _, k in shapes]
+    dx = [dev(x) for x in xs]
+    torch.cuda.synchronize()
+    ys = [ghd.ghd_mx4_linear(ctx, x, w[0]) for x, w in zip(dx, held)]        # (asked for on the default stream)
+    side.synchronize()
+    for (n, m, k), x, w, y in zip(shapes, xs, held, ys):
+        check_product(x, w[1], w[2], m, k, y.cpu().numpy())
+    outs = [torch.zeros_like(y) for y in ys]
+    torch.cuda.synchronize()
+    g = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(g, stream=side):
+        for x, w, y in zip(dx, held, outs):
+            ghd.ghd_mx4_linear(ctx, x, w[0], y=y)
+    xs = [r.randn(*x.shape).astype(np.float16) for x in xs]
+    for t, x in zip(dx, xs):
+        t.copy_(dev(x))
+    torch.cuda.synchronize()
+    for _ in range(2):
+        with torch.cuda.stream(side):
+            g.replay()
+    side.synchronize()
+    for (n, m, k), x, w, y in zip(shapes, xs, held, outs):
+        check_product(x, w[1], w[2], m, k, y.cpu().numpy())
+    ghd.ghd_sync_status(ctx)
+
+
+def test_outputs_end_where_they_should(ghd):
+    """Nothing behind the output is written, whatever the last tile holds."""
+    import torch
+    r = np.random.RandomState(22)
+    for dtype in ("f16", "f32"):
+        for n, m, k in [(1, 1, 5), (5, 129, 300), (40, 383, 128), (100, 130, 256)]:
+            ctx = make_ctx(ghd, dtype, k, n)
+            w, codes, scales = random_held(ghd, r, m, k, 118, 124)
+            x = (r.randn(n, k) * 0.3).astype(np_t(dtype))
+            y = torch.full((n * m + 64,), 7.0, device="cuda")
+            ghd.ghd_mx4_linear(ctx, dev(x), w, y=y)
+            u = torch.full((n * m + 64,), 7.0, dtype=ctx.dtype, device="cuda")
+            ghd.ghd_mx4_gate_up(ctx, dev(x), w, w, u=u)
+            ghd.ghd_sync_status(ctx)
+            assert (y[n * m:] == 7.0).all() and (u[n * m:] == 7.0).all()
+            check_product(x, codes, scales, m, k, y[:n * m].view(n, m).cpu().numpy())
+
+
+@pytest.mark.parametrize("m,k", [(20000, 128), (128, 8192), (9000, 1152)])
+def test_linear_of_many_units_and_long_sums(ghd, m, k):
+    r = np.random.RandomState(m + k)
+    for n in (7, 50):
+        ctx = make_ctx(ghd, "f16", k, n)
+        w, codes, scales = random_held(ghd, r, m, k)
+        x = r.randn(n, k).astype(np.float16)
+        check_product(x, codes, scales, m, k, ghd.ghd_mx4_linear(ctx, dev(x), w).cpu().numpy())
+        ghd.ghd_sync_status(ctx)
+
+
 def test_refusals(ghd):
     import torch
     ctx = make_ctx(ghd, "f16", 512, 16)

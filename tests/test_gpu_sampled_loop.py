@@ -1,0 +1,118 @@
+"""Decoding by sampling with drafting heads held in 4 bits: heads -> candidates -> tree -> verify -> acceptance -> commit, step after step,
+every acceptance checked against the double-precision oracle on the logits that the step produced."""
+import numpy as np
+import pytest
+
+import oracle
+import workloads as wl
+from oracle import mx4 as omx
+from oracle import sampling as osam
+
+pytestmark = pytest.mark.gpu
+
+SHAPE = wl.scaled(wl.TINY, name="sampled", d_model=512, n_heads=4, d_head=128, d_ffn=1408, vocab=1500, n_layers=2, dtype="f16")
+HEADS, TEMP, DRAFT_TEMP = 3, 0.9, 1.1
+# node -> parent, level, rank among its parent's children (the candidates of a level in the order of their draws)
+PARENT = [-1, 0, 0, 0, 1, 1, 2, 4, 4, 6, 7]
+
+
+def dev(a):
+    import torch
+    return torch.from_numpy(np.ascontiguousarray(a)).cuda()
+
+
+@pytest.fixture(scope="module")
+def ghd():
+    import paper_2505_23219_b200 as g
+    return g
+
+
+def test_decode_loop(ghd):
+    import torch
+    n, L, steps = len(PARENT), 40, 5
+    level, rank, seen = [0] * n, [0] * n, {}
+    for i in range(1, n):
+        level[i], rank[i] = level[PARENT[i]] + 1, seen.get(PARENT[i], 0)
+        seen[PARENT[i]] = rank[i] + 1
+    Lmax = L + n * (steps + 1)
+    head = wl.head_weights(SHAPE, 5)
+    head["lm_head"] = (head["lm_head"].astype(np.float32) * 6).astype(np.float16)        # logits a few units apart
+    ctx = ghd.ghd_create(ghd.ModelCfg(SHAPE.d_model, SHAPE.n_heads, SHAPE.d_head, SHAPE.d_ffn, SHAPE.vocab, SHAPE.n_layers, Lmax, 16, "f16", SHAPE.rms_eps, SHAPE.rope_theta))
+    weights = ghd.ModelWeights(dev(head["embed"]), [ghd.LayerWeights(**{k: dev(w[k]) for k in ghd.LayerWeights.FIELDS}) for w in
+                               (wl.layer_weights(SHAPE, 5, l) for l in range(SHAPE.n_layers))], dev(head["rms_final"]), dev(head["lm_head"]))
+    caches = [wl.kv_cache(SHAPE, 5, l, L, Lmax) for l in range(SHAPE.n_layers)]
+    kvs = [ghd.KvLayer(dev(k), dev(v), ghd.KV_LEN_DEVICE) for k, v in caches]
+    ghd.ghd_kv_len_set(ctx, L)
+    tree = ghd.ghd_tree_build(ctx, PARENT, ghd.KV_LEN_DEVICE)
+    r = np.random.RandomState(8)
+    # the heads are the model's own lm_head behind a small layer, in 4 bits: drafts that are right now and then
+    w1 = [ghd.ghd_mx4_quantize(ctx, dev((r.randn(512, 512) * 0.01).astype(np.float16))) for _ in range(HEADS)]
+    w2 = ghd.ghd_mx4_quantize(ctx, weights.lm_head)
+    codes, scales = w2.codes.cpu().numpy(), w2.scales.cpu().numpy()
+    lv, rk = dev(np.array(level, np.int32)), dev(np.array(rank, np.int32))
+    drow = dev(np.array([l if l < HEADS else -1 for l in level], np.int32))
+    tokens = dev(wl.draft_tokens(PARENT, SHAPE.vocab, 9).astype(np.int32))
+    draft = torch.zeros(HEADS, SHAPE.vocab, device="cuda")
+    draft_row = None                                             # the first step's candidates were not drawn
+    emitted, accepted = [], 0
+    for step in range(steps):
+        logits, amax = ghd.ghd_verify_step(ctx, weights, kvs, tree, tokens)
+        u = torch.rand(n, device="cuda")
+        more = {} if draft_row is None else dict(draft_row=draft_row, draft_logits=draft, draft_temperature=DRAFT_TEMP)
+        res = ghd.ghd_accept_sampled(ctx, ghd.SampledRows(tree.parent[:n], tokens, logits, u, temperature=TEMP, **more))
+        nodes, toks = osam.verify(PARENT, tokens.cpu().numpy(), logits.cpu().numpy(), u.cpu().numpy(), TEMP, None if draft_row is None else draft_row.cpu().numpy(),
+                                  draft.cpu().numpy(), DRAFT_TEMP)
+        got = res[0].cpu().numpy()
+        assert got[0] == len(nodes) - 1 and list(got[2:2 + len(nodes)]) == nodes and list(got[258:258 + len(toks)]) == toks
+        emitted += toks
+        accepted += len(nodes) - 1
+        before = ghd.ghd_kv_len_get(ctx)
+        ghd.ghd_kv_commit(ctx, kvs, ghd.KV_LEN_DEVICE, res[0])
+        assert ghd.ghd_kv_len_get(ctx) == before + len(nodes)
+        # next candidates: the heads at the last accepted node
+        hidden = ghd.ghd_copy_hidden(ctx, n)[nodes[-1]:nodes[-1] + 1]
+        h = ghd.ghd_rmsnorm(ctx, hidden.contiguous(), weights.rms_final)
+        for k in range(HEADS):
+            a = ghd.ghd_mx4_linear(ctx, h, w1[k])
+            y = (h.float() + a * torch.sigmoid(a)).half()
+            ghd.ghd_mx4_linear(ctx, y, w2, y=draft[k:k + 1])
+            want = omx.product(y.cpu().numpy(), codes, scales, SHAPE.vocab, 512)
+            assert np.abs(draft[k].cpu().numpy() - want[0]).max() <= 2.0 ** -15 * np.abs(want).max()
+        uc = torch.rand(HEADS, 16, device="cuda")
+        cand = ghd.ghd_draft_sample(ctx, draft, uc, 3, DRAFT_TEMP)
+        for k in range(HEADS):
+            assert np.array_equal(cand[k].cpu().numpy(), osam.draw(draft[k].cpu().numpy(), DRAFT_TEMP, 3, uc[k].cpu().numpy()))
+        full = torch.full((max(level) + 1, 16), 0, dtype=torch.int32, device="cuda")
+        full[:HEADS] = cand
+        tokens = ghd.ghd_tree_fill_tokens(ctx, full, res[0], lv, rk)
+        draft_row = drow
+        tree = ghd.ghd_tree_build(ctx, PARENT, ghd.KV_LEN_DEVICE, tree)
+        assert int(tokens[0]) == toks[-1]
+    ghd.ghd_sync_status(ctx)
+    assert len(emitted) == accepted + steps and all(0 <= t < SHAPE.vocab for t in emitted)
+
+
+def test_oracle_is_the_one_of_greedy_acceptance_when_cold(ghd):
+    """Near temperature 0 the sampled acceptance of candidates that were not drawn is the greedy one."""
+    import torch
+    r = np.random.RandomState(12)
+    V, n = 600, 30
+    ctx = ghd.ghd_create(ghd.ModelCfg(512, 4, 128, 512, V, 1, 512, 32, "f16"))
+    for seed in range(5):
+        parent = wl.random_tree(n, 5, 40 + seed, max_children=4)
+        logits = r.randn(n, V).astype(np.float32)
+        amax = logits.argmax(1).astype(np.int32)
+        # siblings unlike each other, half of the nodes' first children right
+        tokens = np.zeros(n, np.int32)
+        kids = {}
+        for i in range(1, n):
+            k = kids.get(parent[i], 0)
+            kids[parent[i]] = k + 1
+            tokens[i] = amax[parent[i]] if k == 0 and r.rand() < 0.7 else (amax[parent[i]] + 1 + k) % V
+        tree = ghd.ghd_tree_build(ctx, parent, 10)
+        greedy = ghd.ghd_accept(ctx, tree, dev(tokens), dev(amax)).cpu().numpy()
+        cold = ghd.ghd_accept_sampled(ctx, ghd.SampledRows(tree.parent[:n], dev(tokens), dev(logits), torch.rand(n, device="cuda"), temperature=1e-4))[0].cpu().numpy()
+        m = cold[0]
+        assert greedy[0] >= m and list(cold[258:259 + m]) == [amax[x] for x in cold[2:3 + m]]
+        want = oracle.accept(parent, tokens, amax)
+        assert want[0] == greedy[0] == m

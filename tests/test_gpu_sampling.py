@@ -207,6 +207,110 @@ def test_verify_of_wide_nodes_and_repeated_tokens(ghd):
         ghd.ghd_sync_status(ctx)
 
 
+@pytest.mark.parametrize("cnt,vocab", [([64], 100), ([256, 0, 1], 250), ([9] * 60, 300), ([30] * 7, 513)])
+def test_verify_row_by_row(ghd, cnt, vocab):
+    """Where there are too many rows to weigh them all ahead of the walk (draft rows that nobody uses make them many here)."""
+    import torch
+    r = np.random.RandomState(vocab)
+    for drawn in (True, False):
+        b = Batch(r, cnt, vocab, 0.8, True)
+        if not drawn:
+            b.drow[:] = -1
+        rest = torch.zeros(49152, vocab, device="cuda")
+        got = ghd.ghd_accept_sampled(ctx_for(ghd, vocab), b.rows(ghd, draft_logits=torch.cat((dev(b.draft), rest))))
+        ghd.ghd_sync_status(ctx_for(ghd, vocab))
+        b.check(got.cpu().numpy())
+        assert (got == ghd.ghd_accept_sampled(ctx_for(ghd, vocab), b.rows(ghd))).all()
+
+
+def test_verify_of_many_rows(ghd):
+    r = np.random.RandomState(31)
+    V = 6000
+    for drawn in (True, False):
+        b = Batch(r, [150] * 14 + [3], V, 1.0, drawn)
+        b.check(ghd.ghd_accept_sampled(ctx_for(ghd, V), b.rows(ghd)).cpu().numpy())
+    ghd.ghd_sync_status(ctx_for(ghd, V))
+
+
+def test_largest_vocabulary(ghd):
+    import torch
+    r = np.random.RandomState(32)
+    V = 1 << 20
+    ctx = ghd.ghd_create(ghd.ModelCfg(512, 4, 128, 512, V, 1, 512, 1, "f16"))
+    b = Batch(r, [4], V, 1.0, True)
+    b.check(ghd.ghd_accept_sampled(ctx, b.rows(ghd)).cpu().numpy())
+    u = r.rand(2, 16).astype(np.float32)
+    got = ghd.ghd_draft_sample(ctx, dev(b.logits[:2]), dev(u), 3).cpu().numpy()
+    for i in range(2):
+        assert np.array_equal(got[i], osam.draw(b.logits[i], 1.0, 3, u[i]))
+    ghd.ghd_sync_status(ctx)
+    big = ghd.ghd_create(ghd.ModelCfg(512, 4, 128, 512, V + 1, 1, 512, 1, "f16"))
+    with pytest.raises(ghd.GhdError, match="GHD_ESHAPE"):
+        ghd.ghd_draft_sample(big, torch.zeros(1, V + 1, device="cuda"), torch.zeros(1, 16, device="cuda"), 1)
+
+
+def test_extreme_temperatures_and_logits(ghd):
+    """Cold: the largest token; hot: all alike; logits near the ends of their type."""
+    V = 700
+    ctx = ctx_for(ghd, V)
+    r = np.random.RandomState(33)
+    logits, u = logits_of(r, 6, V), r.rand(6, 16).astype(np.float32)
+    logits[4] = np.where(r.rand(V) < 0.5, 3.4e38, -3.4e38)
+    logits[5] = r.randn(V) * 1e-40
+    for temp in (1e-30, 1e-3, 1e10, 2.0 ** 64):
+        got = ghd.ghd_draft_sample(ctx, dev(logits), dev(u), 1, temp).cpu().numpy()
+        ghd.ghd_sync_status(ctx)
+        for i in range(6):
+            if temp == 1e-30 and i < 4:
+                assert got[i, 0] == logits[i].argmax()
+            elif i == 4 and temp < 1e30:
+                assert logits[4, got[4, 0]] > 0
+            else:
+                assert got[i, 0] == osam.draw(logits[i], temp, 1, u[i])[0]
+
+
+def test_streams_and_graphs(ghd):
+    """A context on its own stream, results asked for on another; calls recorded once and replayed with other inputs."""
+    import torch
+    V = 2000
+    r = np.random.RandomState(34)
+    side = torch.cuda.Stream()
+    with torch.cuda.stream(side):
+        ctx = ghd.ghd_create(ghd.ModelCfg(512, 4, 128, 512, V, 1, 512, 16, "f16"))
+    b, b2 = Batch(r, [40] * 3, V, 1.0, True), Batch(r, [40] * 3, V, 1.0, True)
+    rows = b.rows(ghd)
+    torch.cuda.synchronize()
+    got = ghd.ghd_accept_sampled(ctx, rows)                    # (from the default stream)
+    side.synchronize()
+    b.check(got.cpu().numpy())
+    u = torch.rand(3, 16, device="cuda")
+    lg = dev(b.logits[:3])
+    torch.cuda.synchronize()
+    cand, out = torch.empty(3, 16, dtype=torch.int32, device="cuda"), torch.empty(3, 514, dtype=torch.int32, device="cuda")
+    g = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(g, stream=side):
+        ghd.ghd_accept_sampled(ctx, rows, out=out)
+        ghd.ghd_draft_sample(ctx, lg, u, 5, cand=cand)
+    for t, a in zip(rows.tensors, (b2.parent, b2.tokens, b2.logits, b2.u, b2.start, b2.drow, None)):
+        if a is not None:
+            t.copy_(dev(a))
+    if rows.tensors[6].shape[0] == b2.draft.shape[0]:
+        rows.tensors[6].copy_(dev(b2.draft))
+    else:
+        b2.draft = rows.tensors[6].cpu().numpy()
+        b2.drow = np.minimum(b2.drow, len(b2.draft) - 1)
+        rows.tensors[5].copy_(dev(b2.drow))
+    lg.copy_(dev(b2.logits[:3]))
+    torch.cuda.synchronize()
+    with torch.cuda.stream(side):
+        g.replay()
+    side.synchronize()
+    b2.check(out.cpu().numpy())
+    for i in range(3):
+        assert np.array_equal(cand[i].cpu().numpy(), osam.draw(b2.logits[i], 1.0, 5, u[i].cpu().numpy()))
+    ghd.ghd_sync_status(ctx)
+
+
 def test_verify_mixes_drawn_and_other_children(ghd):
     V = 600
     ctx = ctx_for(ghd, V)
@@ -266,6 +370,19 @@ def test_bad_rows_are_recorded(ghd):
         if what == "parent":
             b.parent[25] = -1                                      # (passed over: nobody's child)
         b.check(got)
+
+
+def test_nothing_to_do(ghd):
+    import torch
+    V = 100
+    ctx = ctx_for(ghd, V)
+    i32 = lambda *a: torch.tensor(a, dtype=torch.int32, device="cuda")  # noqa: E731
+    none = torch.empty(0, V, device="cuda")
+    for start in (None, i32(0, 0, 0)):
+        rows = ghd.SampledRows(i32(), i32(), none, torch.empty(0, device="cuda"), row_start=start)
+        got = ghd.ghd_accept_sampled(ctx, rows).cpu().numpy()
+        assert (got[:, :2] == 0).all() and (got[:, 2:] == -1).all()
+    ghd.ghd_sync_status(ctx)
 
 
 def test_refusals(ghd):
