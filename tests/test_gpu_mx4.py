@@ -295,7 +295,7 @@ def test_outputs_end_where_they_should(ghd):
             check_product(x, codes, scales, m, k, y[:n * m].view(n, m).cpu().numpy())
 
 
-@pytest.mark.parametrize("m,k", [(20000, 128), (128, 8192), (9000, 1152)])
+@pytest.mark.parametrize("m,k", [(20000, 128), (128, 8192), (9000, 1152), (12928, 640), (25600, 384)])
 def test_linear_of_many_units_and_long_sums(ghd, m, k):
     r = np.random.RandomState(m + k)
     for n in (7, 50):
