@@ -67,6 +67,7 @@ struct Smem {
     uint32_t tmem_base;
     int abort_flag;
     volatile int loaded;                // k-steps whose loads have been started
+    volatile int others_in;             // the other CTAs' sums of the unit that this one finishes are in the workspace
 };
 
 __device__ __forceinline__ void bulk_load(uint32_t dst, const void* src, uint32_t bytes, uint32_t bar, uint64_t policy) {
@@ -272,6 +273,7 @@ k_mx4_gemm(const __grid_constant__ Mx4Maps maps, const Mx4Params p) {
         mbar_init(smem_u32(&sm->drain), 1);
         sm->abort_flag = 0;
         sm->loaded = 0;
+        sm->others_in = 0;
         asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
     }
     if (warp == 1) {
@@ -328,6 +330,19 @@ k_mx4_gemm(const __grid_constant__ Mx4Maps maps, const Mx4Params p) {
                 load_scales(stage, c, pol);
                 ++issued;
                 if (++stage == (uint32_t)p.stages) { stage = 0; phase ^= 1; }
+            }
+            // All is on its way: this thread looks out for the others' sums, so that the epilogue need not ask the memory.
+            const long long end = (long long)unit0 * p.kt + kc0 + my_iters, first = (end - 1) / p.kt * p.kt;
+            if (ok && p.split == 1 && end < first + p.kt && first >= end - my_iters) {
+                const int others = (int)(((first + p.kt) * ctas - 1) / p.total) - cta;
+                uint32_t spin = 0;
+                while (ld_acquire_gpu(p.counters + cta) != others) {
+                    if (++spin >= SPIN_LIMIT || *abort_flag) { *abort_flag = 1; atomicCAS(p.status, DEV_OK, DEV_TIMEOUT_GRID); break; }
+                    __nanosleep(spin > 64 ? 64 : 20);
+                }
+                p.counters[cta] = 0;                             // ready for the next launch
+                __threadfence_block();
+                sm->others_in = 1;
             }
         }
     } else if (warp == 11) {
@@ -472,27 +487,22 @@ k_mx4_gemm(const __grid_constant__ Mx4Maps maps, const Mx4Params p) {
                     // the ones behind this CTA: those whose ranges reach into the unit
                     const int others = (int)((((long long)unit * p.kt + p.kt) * ctas - 1) / p.total) - cta;
                     if (et == 0) {
-                        uint32_t spin = 0;
-                        while (ld_acquire_gpu(p.counters + cta) != others) {
-                            if (++spin >= SPIN_LIMIT || *abort_flag) { *abort_flag = 1; atomicCAS(p.status, DEV_OK, DEV_TIMEOUT_GRID); ok = false; break; }
-                            __nanosleep(spin > 64 ? 64 : 20);
-                        }
-                        p.counters[cta] = 0;                     // ready for the next launch
+                        while (!sm->others_in && !*abort_flag) __nanosleep(20);       // (the loading thread's wait is bounded, or it has given up)
+                        ok = !*abort_flag;
+                        __threadfence_block();
                     }
                     ok = epi_all(ok);
                     if (!ok) break;
                     for (int o = 1; o <= others; ++o) {
                         const float* at = p.part + (size_t)(cta + o) * slot + row;
 #pragma unroll
-                        for (int t = 0; t < MT; ++t)
+                        for (int t = 0; t < MT; ++t) {
+                            float v[NODES];                      // all of a tile's are on their way together
 #pragma unroll
-                            for (int e = 0; e < NODES; e += 16) {
-                                float v[16];
+                            for (int e = 0; e < NODES; ++e) v[e] = e < mine ? __ldcg(at + (t * p.per_group + j0 + e) * TILE) : 0.f;
 #pragma unroll
-                                for (int j = 0; j < 16; ++j) v[j] = e + j < mine ? __ldcg(at + (t * p.per_group + j0 + e + j) * TILE) : 0.f;
-#pragma unroll
-                                for (int j = 0; j < 16; ++j) acc[t][e + j] += v[j];
-                            }
+                            for (int e = 0; e < NODES; ++e) acc[t][e] += v[e];
+                        }
                     }
                 }
 #pragma unroll
