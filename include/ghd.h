@@ -420,7 +420,7 @@ typedef struct ghd_sampled {
     const int32_t *tokens;          /* [n_rows] drafted tokens; a child whose token is outside [0, vocab) is passed over */
     const float *logits;            /* [n_rows][vocab] of the target model                                    */
     const float *uniforms;          /* [n_rows]: of a child its test's, of the root the last token's          */
-    const int32_t *draft_row;       /* [n_rows]: row of draft_logits that the children of a row were drawn from, -1: they were not drawn; NULL: none was */
+    const int32_t *draft_row;       /* [n_rows]: row of draft_logits that the children of a row were drawn from, below 0: they were not drawn; NULL: none was */
     const float *draft_logits;      /* [n_draft][vocab], NULL with draft_row                                   */
     int32_t n_draft;
     float temperature, draft_temperature;
@@ -436,7 +436,7 @@ typedef struct ghd_sampled {
  * results_dev[s] as ghd_accept's: nodes the accepted path, tokens[j] the token of nodes[j + 1], tokens[n_matched] the one drawn last
  * (0 at a node without a distribution); entries behind these are -1.  A sequence without rows gets n_emitted 0 and no nodes.
  * Starts out of order, more than GHD_MAX_NODES rows (such a sequence is taken as empty) or a parent that is none (the row is passed
- * over): ghd_sync_status -> GHD_ETREE; a draft row from n_draft on (taken as -1): GHD_EINVAL.  At a node whose draft row has no distribution no
+ * over): ghd_sync_status -> GHD_ETREE; a node with children whose draft row is n_draft or above (taken as -1): GHD_EINVAL.  At a node whose draft row has no distribution no
  * child is accepted.  Intermediate results of trees of few rows lie in the context's workspace (see ghd_mx4_linear). */
 ghd_status ghd_accept_sampled(ghd_ctx *ctx, const ghd_sampled *rows, ghd_accept_result *results_dev);
 

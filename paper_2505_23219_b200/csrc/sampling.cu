@@ -14,7 +14,7 @@
 //
 // What bounds it: chains of latencies.  10 draws from 5 rows of 32000: 23 us, 2 for each draw (where it falls, the segment's logits from
 // the L2, two running sums over 32 lanes, the segment's weight again); 4 draws from 320 rows 36 us, 19 of them the pass over the rows at 1.4 instructions a cycle.
-// A tree: 12 us when nothing was drawn, about 1 a level and 3 a rejected draw (28 with three of these); 48 trees of 64 nodes, row by row, 33.
+// A tree: 14 us when nothing was drawn, about 1 a level and 3 a rejected draw (28 with three of these); 48 trees of 64 nodes, row by row, 33.
 #include <cstdio>
 
 #include "internal.h"
@@ -129,14 +129,14 @@ struct Team {
     Shared* s;
     double* seg;                                // [own segments] weights
     int rank, size, turn, warp, lane;
-    int vocab, wide;                            // rows on 16-byte boundaries
+    int vocab;
+    bool wide;                                  // all rows on 16-byte boundaries
     int seg0, segs;                             // own segments
 
-    __device__ Team(Shared* sm, double* weights, int vocab_, int cluster) : s(sm), seg(weights), size(cluster), turn(0), vocab(vocab_) {
+    __device__ Team(Shared* sm, double* weights, int vocab_, bool wide_, int cluster) : s(sm), seg(weights), size(cluster), turn(0), vocab(vocab_), wide(wide_) {
         rank = cluster > 1 ? (int)tc::cluster_ctarank() : 0;
         warp = threadIdx.x >> 5;
         lane = threadIdx.x & 31;
-        wide = vocab % 4 == 0;
         const int n = (vocab + SEG - 1) / SEG;
         seg0 = n * rank / cluster;
         segs = n * (rank + 1) / cluster - seg0;
@@ -432,11 +432,11 @@ __device__ __forceinline__ double unit(float u) { return (double)fminf(fmaxf(u, 
 // ---------------------------------------------------------------- candidates
 // When the row has been measured its first CTA gets all segments' weights and draws alone, with one warp: what it takes to find a token
 // is one segment's logits.
-__global__ void __launch_bounds__(THREADS, 4) k_draft_sample(const float* __restrict__ logits, int vocab, int cluster, double scale, int draws,
+__global__ void __launch_bounds__(THREADS, 4) k_draft_sample(const float* __restrict__ logits, int vocab, bool wide, int cluster, double scale, int draws,
                                                           const float* __restrict__ uniforms, int32_t* __restrict__ cand, int* status) {
     extern __shared__ double weights[];
     __shared__ Shared sm;
-    Team m(&sm, weights, vocab, cluster);
+    Team m(&sm, weights, vocab, wide, cluster);
     const int row = blockIdx.x / cluster;
     Dist p{logits + (size_t)row * vocab, scale, 0.0, 1.0, false, sm.roots}, none{};
     measure(m, p, none);
@@ -490,11 +490,11 @@ __global__ void __launch_bounds__(THREADS, 4) k_draft_sample(const float* __rest
 // one sum over the vocabulary.  Candidates that nobody drew have Q = 1 at themselves: P_{j+1} is P_j without x.
 // The segments' weights and references of all rows, of the targets and behind them of the drafts, a warp to a segment.  With few trees
 // the walk below knows its rows one after the other only, and most SMs would wait; weighing all rows first costs less than it saves.
-__global__ void __launch_bounds__(THREADS, 4) k_row_segments(const float* __restrict__ logits, const float* __restrict__ draft, int n_rows, int n_draft, int vocab, double scale,
+__global__ void __launch_bounds__(THREADS, 4) k_row_segments(const float* __restrict__ logits, const float* __restrict__ draft, int n_rows, int n_draft, int vocab, bool wide, double scale,
                                                              double draft_scale, double2* __restrict__ out) {
     __shared__ Shared sm;
     pdl_trigger();
-    Team m(&sm, nullptr, vocab, 1);
+    Team m(&sm, nullptr, vocab, wide, 1);
     const int n = m.segs, total = (n_rows + n_draft) * n;
     for (int t = blockIdx.x * WARPS + m.warp; t < total; t += gridDim.x * WARPS) {
         const int row = t / n, g = t - row * n;
@@ -509,11 +509,11 @@ __global__ void __launch_bounds__(THREADS, 4) k_row_segments(const float* __rest
 
 // READY: k_row_segments has run.
 template <bool READY>
-__global__ void __launch_bounds__(THREADS, 2) k_accept_sampled(ghd_sampled a, int vocab, double scale, double draft_scale, int cluster, const double2* __restrict__ ready,
+__global__ void __launch_bounds__(THREADS, 2) k_accept_sampled(ghd_sampled a, int vocab, bool wide, double scale, double draft_scale, int cluster, const double2* __restrict__ ready,
                                                                ghd_accept_result* __restrict__ results, int* status) {
     extern __shared__ double weights[];
     __shared__ Shared sm;
-    Team m(&sm, weights, vocab, cluster);
+    Team m(&sm, weights, vocab, wide, cluster);
     const int seq = blockIdx.x / cluster;
     ghd_accept_result* out = results + seq;
     const bool writes = m.rank == 0 && threadIdx.x == 0;
@@ -549,7 +549,7 @@ __global__ void __launch_bounds__(THREADS, 2) k_accept_sampled(ghd_sampled a, in
         bool any = false;
         for (int i = 0; i < GHD_MAX_NODES / 32; ++i) any |= sm.child[i] != 0;
         int drawn = sm.draft[node];
-        if (drawn >= a.n_draft) {
+        if (any && drawn >= a.n_draft) {
             record(DEV_SAMPLE_DRAFT);
             drawn = -1;
         }
@@ -681,6 +681,8 @@ size_t room_for(int vocab, int cluster) {
     const size_t n = ((size_t)vocab + SEG - 1) / SEG, own = (n + cluster - 1) / cluster;
     return sizeof(double) * (2 * own > n ? 2 * own : n);
 }
+// rows of four logits at a time (a null pointer is as good as any)
+bool wide_rows(const ghd_ctx* c, const float* rows) { return c->cfg.vocab % 4 == 0 && ((uintptr_t)rows & 15) == 0; }
 // log2(e) / temperature
 double scale_of(float temperature) { return 1.44269504088896340736 / (double)temperature; }
 
@@ -714,7 +716,7 @@ ghd_status ghd_draft_sample(ghd_ctx* c, const float* logits, int32_t n_rows, flo
     const int k = cluster_for(c, n_rows, c->cfg.vocab, 4);
     ghd_status s = raise_room(c);
     if (s != GHD_OK) return s;
-    launch_kc(c, false, k, k_draft_sample, n_rows * k, THREADS, room_for(c->cfg.vocab, k), logits, c->cfg.vocab, k, scale_of(temperature), n_draws, uniforms, cand, c->input_status);
+    launch_kc(c, false, k, k_draft_sample, n_rows * k, THREADS, room_for(c->cfg.vocab, k), logits, c->cfg.vocab, wide_rows(c, logits), k, scale_of(temperature), n_draws, uniforms, cand, c->input_status);
     return check_cuda(c, "draft_sample");
 }
 
@@ -736,14 +738,15 @@ ghd_status ghd_accept_sampled(ghd_ctx* c, const ghd_sampled* a, ghd_accept_resul
     c->entry_fresh = 1;
     const double scale = scale_of(a->temperature), draft_scale = a->draft_row ? scale_of(a->draft_temperature) : 0.0;
     const size_t room = room_for(c->cfg.vocab, k);
+    const bool wide = wide_rows(c, a->logits) && wide_rows(c, a->draft_logits);
     const int64_t segs = ((int64_t)a->n_rows + (a->draft_row ? a->n_draft : 0)) * ((c->cfg.vocab + SEG - 1) / SEG);
     if (segs > 0 && segs <= SAMPLE_SEGS) {
         const int64_t most = 4 * c->sm_count, ctas = (segs + WARPS - 1) / WARPS;
-        launch_k(c, false, k_row_segments, (int)(ctas < most ? ctas : most), THREADS, 0, a->logits, a->draft_logits, a->n_rows, a->draft_row ? a->n_draft : 0, c->cfg.vocab, scale, draft_scale,
+        launch_k(c, false, k_row_segments, (int)(ctas < most ? ctas : most), THREADS, 0, a->logits, a->draft_logits, a->n_rows, a->draft_row ? a->n_draft : 0, c->cfg.vocab, wide, scale, draft_scale,
                  (double2*)c->sample_segs);
-        launch_kc(c, true, k, k_accept_sampled<true>, a->n_seqs * k, THREADS, room, *a, c->cfg.vocab, scale, draft_scale, k, (const double2*)c->sample_segs, results_dev, c->input_status);
+        launch_kc(c, true, k, k_accept_sampled<true>, a->n_seqs * k, THREADS, room, *a, c->cfg.vocab, wide, scale, draft_scale, k, (const double2*)c->sample_segs, results_dev, c->input_status);
     } else {
-        launch_kc(c, false, k, k_accept_sampled<false>, a->n_seqs * k, THREADS, room, *a, c->cfg.vocab, scale, draft_scale, k, (const double2*)nullptr, results_dev, c->input_status);
+        launch_kc(c, false, k, k_accept_sampled<false>, a->n_seqs * k, THREADS, room, *a, c->cfg.vocab, wide, scale, draft_scale, k, (const double2*)nullptr, results_dev, c->input_status);
     }
     return check_cuda(c, "accept_sampled");
 }

@@ -277,6 +277,42 @@ def test_streams_graphs_and_a_shared_workspace(ghd):
     ghd.ghd_sync_status(ctx)
 
 
+def test_first_call_of_a_context_is_recorded(ghd):
+    import torch
+    r = np.random.RandomState(23)
+    side = torch.cuda.Stream()
+    with torch.cuda.stream(side):
+        ctx = make_ctx(ghd, "f16", 512, 32)
+    w, codes, scales = random_held(ghd, r, 300, 500)
+    x, y = r.randn(20, 500).astype(np.float16), torch.empty(20, 300, device="cuda")
+    dx = dev(x)
+    torch.cuda.synchronize()
+    g = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(g, stream=side):
+        ghd.ghd_mx4_linear(ctx, dx, w, y=y)
+    with torch.cuda.stream(side):
+        g.replay()
+    side.synchronize()
+    check_product(x, codes, scales, 300, 500, y.cpu().numpy())
+
+
+@pytest.mark.parametrize("lo,hi,e", [(240, 255, -110), (0, 20, 100), (60, 70, 60), (200, 254, -127)])
+def test_scales_far_from_one(ghd, lo, hi, e):
+    """Large scales with small x and the other way round: the products are ordinary numbers."""
+    r = np.random.RandomState(lo)
+    n, m, k = 9, 140, 300
+    ctx = make_ctx(ghd, "f32", k, n)
+    w, codes, scales = random_held(ghd, r, m, k, lo, hi)
+    x = np.ldexp(r.randn(n, k), e).astype(np.float32)
+    y = ghd.ghd_mx4_linear(ctx, dev(x), w).cpu().numpy()
+    X, W = x.astype(np.float64), omx.values(codes, scales, m, k)
+    # besides product_bound's: an element of x may be off by 2^-137, half of the least number that a term and its scale hold
+    bound = product_bound(X, W, k) + 2.0 ** -137 * np.abs(W).sum(1)[None, :]
+    want = X @ W.T
+    fine = np.abs(want) + bound < 3e38
+    assert fine.all() and (np.abs(y - want) <= bound).all(), f"{(np.abs(y - want) / bound).max()} of the bound"
+
+
 def test_outputs_end_where_they_should(ghd):
     """Nothing behind the output is written, whatever the last tile holds."""
     import torch

@@ -372,6 +372,63 @@ def test_bad_rows_are_recorded(ghd):
         b.check(got)
 
 
+@pytest.mark.parametrize("vocab", [400, 402])
+def test_rows_off_the_16_byte_boundaries(ghd, vocab):
+    """Logits anywhere in a buffer, in both ways through the calls."""
+    import torch
+    r = np.random.RandomState(41)
+    ctx = ctx_for(ghd, vocab)
+    b = Batch(r, [30] * 3, vocab, 1.0, True)
+    lazy = np.concatenate((b.draft, np.zeros((49152 // (vocab // 256 + 1) + 1, vocab), np.float32)))
+    for off in (1, 2, 3):
+        def at(x):
+            t = torch.zeros(x.size + off, device="cuda")
+            t[off:] = dev(x.reshape(-1))
+            return t[off:].view(x.shape)
+        for draft in (b.draft, lazy):
+            rows = ghd.SampledRows(dev(b.parent), dev(b.tokens), at(b.logits), at(b.u), row_start=dev(b.start), draft_row=dev(b.drow), draft_logits=at(draft))
+            b.check(ghd.ghd_accept_sampled(ctx, rows).cpu().numpy())
+        u = r.rand(5, 16).astype(np.float32)
+        got = ghd.ghd_draft_sample(ctx, at(b.logits[:5]), at(u), 7).cpu().numpy()
+        for i in range(5):
+            assert np.array_equal(got[i], osam.draw(b.logits[i], 1.0, 7, u[i]))
+    ghd.ghd_sync_status(ctx)
+
+
+def test_draft_rows_of_leaves_are_not_looked_at(ghd):
+    V = 300
+    ctx = ctx_for(ghd, V)
+    b = Batch(np.random.RandomState(42), [30] * 6, V, 1.0, True)
+    for s in range(6):
+        for i in range(30):
+            if i not in b.parent[30 * s:30 * s + 30]:
+                b.drow[30 * s + i] = 10 ** 9
+    got = ghd.ghd_accept_sampled(ctx, b.rows(ghd)).cpu().numpy()
+    ghd.ghd_sync_status(ctx)
+    b.drow[b.drow == 10 ** 9] = -1
+    b.check(got)
+
+
+def test_first_call_of_a_context_is_recorded(ghd):
+    import torch
+    V = 900
+    r = np.random.RandomState(43)
+    side = torch.cuda.Stream()
+    with torch.cuda.stream(side):
+        ctx = ghd.ghd_create(ghd.ModelCfg(512, 4, 128, 512, V, 1, 512, 16, "f16"))
+    b = Batch(r, [40] * 3, V, 1.0, True)
+    rows = b.rows(ghd)
+    out = torch.empty(3, 514, dtype=torch.int32, device="cuda")
+    torch.cuda.synchronize()
+    g = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(g, stream=side):
+        ghd.ghd_accept_sampled(ctx, rows, out=out)
+    with torch.cuda.stream(side):
+        g.replay()
+    side.synchronize()
+    b.check(out.cpu().numpy())
+
+
 def test_nothing_to_do(ghd):
     import torch
     V = 100
