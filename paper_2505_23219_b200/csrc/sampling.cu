@@ -297,19 +297,18 @@ __device__ bool own_share(Team& m, double target, double& before) {
     return owner == m.rank;
 }
 
-// One warp: the lane in whose sums the target falls, `before` lying in front of them all -> that lane, the last one with weight where
-// rounding leaves none, -1 where there is no weight; start: what lies before that lane.
-__device__ int lane_of(double sum, double before, double target, int lane, double& start) {
-    const double run = before + warp_scan(sum, lane);
+// One warp: the lane in whose running sum the target falls, the last one with weight where rounding leaves none, -1 where there is no weight;
+// start: what lies before that lane.
+__device__ __forceinline__ int lane_at(double run, double sum, double target, double& start) {
     const uint32_t over = __ballot_sync(0xffffffffu, sum > 0.0 && run > target), some = __ballot_sync(0xffffffffu, sum > 0.0);
     if (!some) return -1;
     const int k = over ? __ffs(over) - 1 : 31 - __clz(some);
     start = __shfl_sync(0xffffffffu, run - sum, k);
     return k;
 }
-// One warp: the segment of seg[0 .. n) in which the target falls.  A lane has `per` neighbouring segments, which weigh `sum` together.
-__device__ int segment_of(const double* seg, int n, int per, double sum, double before, double target, int lane, double& start) {
-    const int k = lane_of(sum, before, target, lane, start);
+__device__ __forceinline__ int lane_of(double sum, double before, double target, int lane, double& start) { return lane_at(before + warp_scan(sum, lane), sum, target, start); }
+// One warp: the segment of seg[0 .. n) in which the target falls.  A lane has `per` neighbouring segments; k: the lane that it falls in.
+__device__ __forceinline__ int segment_at(const double* seg, int n, int per, int k, double target, double& start) {
     if (k < 0) return -1;
     int found = -1, last = -1;
     double run = start, last_start = start;
@@ -321,6 +320,10 @@ __device__ int segment_of(const double* seg, int n, int per, double sum, double 
     }
     start = found < 0 ? last_start : run;
     return found < 0 ? last : found;
+}
+__device__ __forceinline__ int segment_of(const double* seg, int n, int per, double sum, double before, double target, int lane, double& start) {
+    const int k = lane_of(sum, before, target, lane, start);
+    return segment_at(seg, n, per, k, target, start);
 }
 // One warp: the token, from the weights w of the segment's tokens in this lane.  All lanes get it.
 __device__ int token_of(const double (&w)[RUN], int t0, double before, double target, int lane) {
@@ -432,7 +435,10 @@ __device__ __forceinline__ double unit(float u) { return (double)fminf(fmaxf(u, 
 // ---------------------------------------------------------------- candidates
 // When the row has been measured its first CTA gets all segments' weights and draws alone, with one warp: what it takes to find a token
 // is one segment's logits.
-__global__ void __launch_bounds__(THREADS, 4) k_draft_sample(const float* __restrict__ logits, int vocab, bool wide, int cluster, double scale, int draws,
+// HELD: CTAs to a SM.  Four hide more of each other's latencies (1000 rows of 32000, 4 draws each: 73 us against 85), three leave registers for
+// a shorter chain of a draw (5 rows 11.8 us against 13.0, 320 rows 33.7 against 34.8): four from where there are rows for four.
+template <int HELD>
+__global__ void __launch_bounds__(THREADS, HELD) k_draft_sample(const float* __restrict__ logits, int vocab, bool wide, int cluster, double scale, int draws,
                                                           const float* __restrict__ uniforms, int32_t* __restrict__ cand, int* status) {
     extern __shared__ double weights[];
     __shared__ Shared sm;
@@ -455,9 +461,9 @@ __global__ void __launch_bounds__(THREADS, 4) k_draft_sample(const float* __rest
     int out = -1;
 #pragma unroll 1
     for (int j = 0; j < draws && p.ok; ++j) {
-        const double target = unit(__shfl_sync(0xffffffffu, u, j)) * warp_sum(mine);
+        const double run = warp_scan(mine, m.lane), target = unit(__shfl_sync(0xffffffffu, u, j)) * __shfl_sync(0xffffffffu, run, 31);
         double start;
-        const int sg = segment_of(weights, n, per, mine, 0.0, target, m.lane, start);
+        const int k = lane_at(run, mine, target, start), sg = segment_at(weights, n, per, k, target, start);
         if (sg < 0) break;                                     // nothing is left
         float x[RUN];
         double w[RUN], sum = 0.0;
@@ -465,11 +471,15 @@ __global__ void __launch_bounds__(THREADS, 4) k_draft_sample(const float* __rest
         m.load(p.row, t0, x);
 #pragma unroll
         for (int e = 0; e < RUN; ++e) w[e] = p.of(x[e]);
-        without(w, t0, sm.gone, j);
+        // (lane i has drawn token i)
+        for (uint32_t here = __ballot_sync(0xffffffffu, out >= 0 && out / SEG == sg); here; here &= here - 1) {
+            const int d = __shfl_sync(0xffffffffu, out, __ffs(here) - 1) - t0;
+#pragma unroll
+            for (int e = 0; e < RUN; ++e) w[e] = d == e ? 0.0 : w[e];
+        }
         const int t = token_of(w, t0, start, target, m.lane);
         if (t < 0) break;
         if (m.lane == j) out = t;
-        if (m.lane == 0) sm.gone[j] = t;
         // the segment's weight without it
 #pragma unroll
         for (int e = 0; e < RUN; ++e) sum += t - t0 == e ? 0.0 : w[e];
@@ -688,7 +698,8 @@ double scale_of(float temperature) { return 1.44269504088896340736 / (double)tem
 
 ghd_status raise_room(ghd_ctx* c) {              // (a CTA with all segments of the largest vocabulary takes 64 KB)
     if (c->attr_sampling) return GHD_OK;
-    if (cudaFuncSetAttribute(k_draft_sample, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)room_for(MAX_VOCAB, 1)) != cudaSuccess ||
+    if (cudaFuncSetAttribute(k_draft_sample<3>, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)room_for(MAX_VOCAB, 1)) != cudaSuccess ||
+        cudaFuncSetAttribute(k_draft_sample<4>, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)room_for(MAX_VOCAB, 1)) != cudaSuccess ||
         cudaFuncSetAttribute(k_accept_sampled<true>, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)room_for(MAX_VOCAB, 1)) != cudaSuccess ||
         cudaFuncSetAttribute(k_accept_sampled<false>, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)room_for(MAX_VOCAB, 1)) != cudaSuccess)
         return check_cuda(c, "sampling: shared memory");
@@ -713,10 +724,11 @@ ghd_status ghd_draft_sample(ghd_ctx* c, const float* logits, int32_t n_rows, flo
     if (n_rows > (1 << 24)) return fail(c, GHD_EINVAL, "draft_sample: more than 2^24 rows");
     if (!logits || !uniforms || !cand) return fail(c, GHD_EINVAL, "draft_sample: null pointer");
     if (!c->ws) return fail(c, GHD_ENOSPACE, "no workspace set");
-    const int k = cluster_for(c, n_rows, c->cfg.vocab, 4);
+    const bool many = n_rows > 3 * c->sm_count;
+    const int k = cluster_for(c, n_rows, c->cfg.vocab, many ? 4 : 3);
     ghd_status s = raise_room(c);
     if (s != GHD_OK) return s;
-    launch_kc(c, false, k, k_draft_sample, n_rows * k, THREADS, room_for(c->cfg.vocab, k), logits, c->cfg.vocab, wide_rows(c, logits), k, scale_of(temperature), n_draws, uniforms, cand, c->input_status);
+    launch_kc(c, false, k, many ? k_draft_sample<4> : k_draft_sample<3>, n_rows * k, THREADS, room_for(c->cfg.vocab, k), logits, c->cfg.vocab, wide_rows(c, logits), k, scale_of(temperature), n_draws, uniforms, cand, c->input_status);
     return check_cuda(c, "draft_sample");
 }
 
