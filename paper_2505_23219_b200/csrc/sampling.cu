@@ -255,19 +255,32 @@ __device__ void measure(Team& m, Dist& p, Dist& q) {
     __syncthreads();
 }
 
-// The weights w(logit of p, logit of q) of every own segment into seg[], of the CTAs' shares into share[] -> the total.
-template <typename W>
-__device__ double total_of(Team& m, const float* p, const float* q, W w) {
+// What is left of P after rejected draws, max(P - beta Q, 0): the weights of every own segment into seg[], of the CTAs' shares into share[]
+// -> the total.  keep (or null): room for P and Q of the own segments, which `kept` says are there from the rejection before.
+__device__ double total_left(Team& m, const Dist& p, const Dist& q, double beta, double2* keep, bool kept) {
     double all = 0.0;
 #pragma unroll 1
     for (int g = m.warp; g < m.segs; g += WARPS) {
-        float x[RUN], y[RUN];
-        const int t = m.first_of(m.seg0 + g);
-        m.load(p, t, x);
-        m.load(q, t, y);
         double sum = 0.0;
+        double2* at = keep + g * SEG + m.lane;
+        if (keep && kept) {
 #pragma unroll
-        for (int e = 0; e < RUN; ++e) sum += w(x[e], y[e]);
+            for (int e = 0; e < RUN; ++e) {
+                const double2 v = at[e * 32];
+                sum += fmax(v.x - beta * v.y, 0.0);
+            }
+        } else {
+            float x[RUN], y[RUN];
+            const int t = m.first_of(m.seg0 + g);
+            m.load(p.row, t, x);
+            m.load(q.row, t, y);
+#pragma unroll
+            for (int e = 0; e < RUN; ++e) {
+                const double2 v = make_double2(p.of(x[e]), q.of(y[e]));
+                if (keep) at[e * 32] = v;
+                sum += fmax(v.x - beta * v.y, 0.0);
+            }
+        }
         sum = warp_sum(sum);
         if (m.lane == 0) m.seg[g] = sum;
         all += sum;
@@ -440,7 +453,7 @@ __device__ __forceinline__ double unit(float u) { return (double)fminf(fmaxf(u, 
 template <int HELD>
 __global__ void __launch_bounds__(THREADS, HELD) k_draft_sample(const float* __restrict__ logits, int vocab, bool wide, int cluster, double scale, int draws,
                                                           const float* __restrict__ uniforms, int32_t* __restrict__ cand, int* status) {
-    extern __shared__ double weights[];
+    extern __shared__ __align__(16) double weights[];
     __shared__ Shared sm;
     Team m(&sm, weights, vocab, wide, cluster);
     const int row = blockIdx.x / cluster;
@@ -519,11 +532,12 @@ __global__ void __launch_bounds__(THREADS, 4) k_row_segments(const float* __rest
 
 // READY: k_row_segments has run.
 template <bool READY>
-__global__ void __launch_bounds__(THREADS, 2) k_accept_sampled(ghd_sampled a, int vocab, bool wide, double scale, double draft_scale, int cluster, const double2* __restrict__ ready,
+__global__ void __launch_bounds__(THREADS, 2) k_accept_sampled(ghd_sampled a, int vocab, bool wide, double scale, double draft_scale, int cluster, int keep_at, const double2* __restrict__ ready,
                                                                ghd_accept_result* __restrict__ results, int* status) {
-    extern __shared__ double weights[];
+    extern __shared__ __align__(16) double weights[];
     __shared__ Shared sm;
     Team m(&sm, weights, vocab, wide, cluster);
+    double2* keep = keep_at ? reinterpret_cast<double2*>(weights + keep_at) : nullptr;
     const int seq = blockIdx.x / cluster;
     ghd_accept_result* out = results + seq;
     const bool writes = m.rank == 0 && threadIdx.x == 0;
@@ -597,7 +611,7 @@ __global__ void __launch_bounds__(THREADS, 2) k_accept_sampled(ghd_sampled a, in
                         if (u * qx * c_j * W < fmax(px - beta * qx, 0.0)) { next = c; break; }
                         beta += c_j * W;
                         rejected += qx;
-                        W = total_of(m, p.row, q.row, left);
+                        W = total_left(m, p, q, beta, keep, fresh);
                         fresh = true;
                     } else {
                         bool before = false;
@@ -619,7 +633,7 @@ __global__ void __launch_bounds__(THREADS, 2) k_accept_sampled(ghd_sampled a, in
                 // those with a token that is gone weighed again.
                 if (fresh && !(W > 0.0)) {
                     beta = 0.0;
-                    W = total_of(m, p.row, q.row, left);
+                    W = total_left(m, p, q, beta, keep, true);
                 }
                 double total = W;
                 if (!fresh) {
@@ -691,6 +705,9 @@ size_t room_for(int vocab, int cluster) {
     const size_t n = ((size_t)vocab + SEG - 1) / SEG, own = (n + cluster - 1) / cluster;
     return sizeof(double) * (2 * own > n ? 2 * own : n);
 }
+// room for P and Q of a CTA's segments
+size_t keep_for(int vocab, int cluster) { return ((size_t)(vocab + SEG - 1) / SEG + cluster - 1) / cluster * SEG * sizeof(double2); }
+constexpr size_t MAX_ROOM = 96 * 1024;
 // rows of four logits at a time (a null pointer is as good as any)
 bool wide_rows(const ghd_ctx* c, const float* rows) { return c->cfg.vocab % 4 == 0 && ((uintptr_t)rows & 15) == 0; }
 // log2(e) / temperature
@@ -700,8 +717,8 @@ ghd_status raise_room(ghd_ctx* c) {              // (a CTA with all segments of 
     if (c->attr_sampling) return GHD_OK;
     if (cudaFuncSetAttribute(k_draft_sample<3>, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)room_for(MAX_VOCAB, 1)) != cudaSuccess ||
         cudaFuncSetAttribute(k_draft_sample<4>, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)room_for(MAX_VOCAB, 1)) != cudaSuccess ||
-        cudaFuncSetAttribute(k_accept_sampled<true>, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)room_for(MAX_VOCAB, 1)) != cudaSuccess ||
-        cudaFuncSetAttribute(k_accept_sampled<false>, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)room_for(MAX_VOCAB, 1)) != cudaSuccess)
+        cudaFuncSetAttribute(k_accept_sampled<true>, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)MAX_ROOM) != cudaSuccess ||
+        cudaFuncSetAttribute(k_accept_sampled<false>, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)MAX_ROOM) != cudaSuccess)
         return check_cuda(c, "sampling: shared memory");
     c->attr_sampling = true;
     return GHD_OK;
@@ -749,16 +766,20 @@ ghd_status ghd_accept_sampled(ghd_ctx* c, const ghd_sampled* a, ghd_accept_resul
     if (s != GHD_OK) return s;
     c->entry_fresh = 1;
     const double scale = scale_of(a->temperature), draft_scale = a->draft_row ? scale_of(a->draft_temperature) : 0.0;
-    const size_t room = room_for(c->cfg.vocab, k);
+    // P and Q of a node's rows are kept from one rejected draw to the next where two CTAs' worth fits into a SM (trees of 64 nodes over 32000
+    // tokens, kernel us without / with: one 30.7 / 28.3, 48 of them 72.5 / 67.2)
+    const size_t room = (room_for(c->cfg.vocab, k) + 15) / 16 * 16, keeps = keep_for(c->cfg.vocab, k);
+    const bool keep = a->draft_row && room + keeps <= MAX_ROOM;
+    const int keep_at = keep ? (int)(room / sizeof(double)) : 0;
     const bool wide = wide_rows(c, a->logits) && wide_rows(c, a->draft_logits);
     const int64_t segs = ((int64_t)a->n_rows + (a->draft_row ? a->n_draft : 0)) * ((c->cfg.vocab + SEG - 1) / SEG);
     if (segs > 0 && segs <= SAMPLE_SEGS) {
         const int64_t most = 4 * c->sm_count, ctas = (segs + WARPS - 1) / WARPS;
         launch_k(c, false, k_row_segments, (int)(ctas < most ? ctas : most), THREADS, 0, a->logits, a->draft_logits, a->n_rows, a->draft_row ? a->n_draft : 0, c->cfg.vocab, wide, scale, draft_scale,
                  (double2*)c->sample_segs);
-        launch_kc(c, true, k, k_accept_sampled<true>, a->n_seqs * k, THREADS, room, *a, c->cfg.vocab, wide, scale, draft_scale, k, (const double2*)c->sample_segs, results_dev, c->input_status);
+        launch_kc(c, true, k, k_accept_sampled<true>, a->n_seqs * k, THREADS, room + (keep ? keeps : 0), *a, c->cfg.vocab, wide, scale, draft_scale, k, keep_at, (const double2*)c->sample_segs, results_dev, c->input_status);
     } else {
-        launch_kc(c, false, k, k_accept_sampled<false>, a->n_seqs * k, THREADS, room, *a, c->cfg.vocab, wide, scale, draft_scale, k, (const double2*)nullptr, results_dev, c->input_status);
+        launch_kc(c, false, k, k_accept_sampled<false>, a->n_seqs * k, THREADS, room + (keep ? keeps : 0), *a, c->cfg.vocab, wide, scale, draft_scale, k, keep_at, (const double2*)nullptr, results_dev, c->input_status);
     }
     return check_cuda(c, "accept_sampled");
 }

@@ -52,6 +52,15 @@ def test_draw(ghd, vocab, rows):
         assert np.array_equal(got[i], osam.draw(logits[i], temp, draws, u[i])), i
 
 
+def test_draw_from_many_rows(ghd):
+    r = np.random.RandomState(6)
+    for rows, vocab in ((700, 300), (450, 2050)):
+        logits, u = logits_of(r, rows, vocab), r.rand(rows, 16).astype(np.float32)
+        got = ghd.ghd_draft_sample(ctx_for(ghd, vocab), dev(logits), dev(u), 5, 0.9).cpu().numpy()
+        for i in range(rows):
+            assert np.array_equal(got[i], osam.draw(logits[i], 0.9, 5, u[i])), i
+
+
 def test_draw_at_the_ends(ghd):
     """Numbers at and outside the ends of [0, 1), masked tokens, rows that run out of tokens, extreme logits."""
     V = 300
@@ -164,7 +173,7 @@ class Batch:
 
 @pytest.mark.parametrize("drawn", [True, False])
 @pytest.mark.parametrize("cnt,vocab", [([1], 50), ([2], 1), ([7], 33), ([64], 32000), ([256], 1000), ([5, 0, 1, 30], 100), ([20] * 20, 997), ([3] * 200, 64),
-                                       ([40, 17, 64, 9], 4099), ([12, 12], 70001)])
+                                       ([40, 17, 64, 9], 4099), ([12, 12], 70001), ([20] * 40, 33000)])
 @pytest.mark.parametrize("temp", [0.6, 1.0])
 def test_verify(ghd, drawn, cnt, vocab, temp):
     r = np.random.RandomState(len(cnt) * 100 + cnt[0] + vocab + 3 * drawn)
