@@ -12,9 +12,9 @@
 // falls is looked up over the CTAs, over a CTA's segments, over the lanes of one segment and over a lane's tokens, so that only one
 // segment's weights are worked out again.
 //
-// What bounds it: chains of latencies.  10 draws from 5 rows of 32000: 23 us, 2 for each draw (where it falls, the segment's logits from
-// the L2, two running sums over 32 lanes, the segment's weight again); 4 draws from 320 rows 36 us, 19 of them the pass over the rows at 1.4 instructions a cycle.
-// A tree: 14 us when nothing was drawn, about 1 a level and 3 a rejected draw (28 with three of these); 48 trees of 64 nodes, row by row, 33.
+// What bounds it: chains of latencies.  10 draws from 5 rows of 32000: 20 us, 1.75 for each draw (where it falls, the segment's logits from
+// the L2, two running sums over 32 lanes, the segment's weight again); 4 draws from 320 rows 35 us, 19 of them the pass over the rows at 1.4 instructions a cycle.
+// A tree: 14 us when nothing was drawn, about 1 a level and 2 to 3 a rejected draw (28 with three of these); 48 trees of 64 nodes, row by row, 34.
 #include <cstdio>
 
 #include "internal.h"
