@@ -181,6 +181,16 @@ inline cudaError_t launch_k(ghd_ctx* c, bool pdl, void (*kernel)(KArgs...), dim3
     return launch_kc(c, pdl, 1, kernel, grid, block, smem, std::forward<Args>(args)...);
 }
 
+// A call works on its context's device whatever the current one is.
+struct OnDevice {
+    int before;
+    bool moved;
+    explicit OnDevice(const ghd_ctx* c) : before(-1), moved(false) {
+        if (cudaGetDevice(&before) == cudaSuccess && before != c->device) moved = cudaSetDevice(c->device) == cudaSuccess;
+    }
+    ~OnDevice() { if (moved) cudaSetDevice(before); }
+};
+
 ghd_status fail(ghd_ctx* c, ghd_status s, const char* what);      // keeps the message for ghd_last_error
 ghd_status check_cuda(ghd_ctx* c, const char* where);             // status of the launches so far
 size_t carve_workspace(ghd_ctx* c, char* base);   // returns bytes needed; assigns pointers when base != nullptr

@@ -462,16 +462,6 @@ RowGrid row_grid(const ghd_ctx* c, int n_rows, int jobs, int resident) {
     return g;
 }
 
-// A call works on its context's device whatever the current one is.
-struct OnDevice {
-    int before;
-    bool moved;
-    explicit OnDevice(const ghd_ctx* c) : before(-1), moved(false) {
-        if (cudaGetDevice(&before) == cudaSuccess && before != c->device) moved = cudaSetDevice(c->device) == cudaSuccess;
-    }
-    ~OnDevice() { if (moved) cudaSetDevice(before); }
-};
-
 bool aligned16(const void* p) { return ((uintptr_t)p & 15) == 0; }
 
 // What is wrong with the sizes of a cache: a status and a reason.

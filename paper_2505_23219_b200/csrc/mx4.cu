@@ -130,6 +130,7 @@ ghd_status product(ghd_ctx* c, const void* x, int64_t ld, const ghd_mx4* w, cons
     if (n > c->cfg.max_nodes) return fail(c, GHD_ENOSPACE, "mx4: n > max_nodes");
     if (w->k > c->cfg.d_model && w->k > c->cfg.d_ffn) return fail(c, GHD_ENOSPACE, "mx4: k above both d_model and d_ffn");
     if (!c->ws) return fail(c, GHD_ENOSPACE, "no workspace set");
+    OnDevice dev(c);
     if ((s = launch_mx4_product(c, x, ld, wide_rows(c, x, ld), w, w2, n, y)) != GHD_OK) return s;
     return check_cuda(c, w2 ? "mx4_gate_up" : "mx4_linear");
 }
@@ -154,6 +155,7 @@ ghd_status ghd_mx4_quantize(ghd_ctx* c, const void* x, int64_t ld, const ghd_mx4
     if (!c) return GHD_EINVAL;
     ghd_status s;
     if ((s = check_matrix(c, w)) != GHD_OK || (s = check_rows(c, x, &ld, w->k, "mx4_quantize: null x")) != GHD_OK) return s;
+    OnDevice dev(c);
     const dim3 grid((w->k + 511) / 512, (w->m + TILE - 1) / TILE * (TILE / ROWS_PER_CTA));
     const bool wide = wide_rows(c, x, ld);
     if (c->cfg.dtype == GHD_F32) launch_k(c, false, k_mx4_quantize<float>, grid, 256, 0, (const float*)x, ld, w->m, w->k, wide, (uint2*)w->codes, (uint32_t*)w->scales);
@@ -165,6 +167,7 @@ ghd_status ghd_mx4_read(ghd_ctx* c, const ghd_mx4* w, void* out, int64_t ld) {
     if (!c) return GHD_EINVAL;
     ghd_status s;
     if ((s = check_matrix(c, w)) != GHD_OK || (s = check_rows(c, out, &ld, w->k, "mx4_read: null out")) != GHD_OK) return s;
+    OnDevice dev(c);
     const dim3 grid((w->k + 255) / 256, (w->m + ROWS_PER_CTA - 1) / ROWS_PER_CTA);
     const bool wide = wide_rows(c, out, ld);
     if (c->cfg.dtype == GHD_F32) launch_k(c, false, k_mx4_read<float>, grid, 256, 0, (const uint32_t*)w->codes, (const uint32_t*)w->scales, w->m, w->k, (float*)out, ld, wide);

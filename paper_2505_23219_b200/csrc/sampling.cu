@@ -741,6 +741,7 @@ ghd_status ghd_draft_sample(ghd_ctx* c, const float* logits, int32_t n_rows, flo
     if (n_rows > (1 << 24)) return fail(c, GHD_EINVAL, "draft_sample: more than 2^24 rows");
     if (!logits || !uniforms || !cand) return fail(c, GHD_EINVAL, "draft_sample: null pointer");
     if (!c->ws) return fail(c, GHD_ENOSPACE, "no workspace set");
+    OnDevice dev(c);
     const bool many = n_rows > 3 * c->sm_count;
     const int k = cluster_for(c, n_rows, c->cfg.vocab, many ? 4 : 3);
     ghd_status s = raise_room(c);
@@ -761,6 +762,7 @@ ghd_status ghd_accept_sampled(ghd_ctx* c, const ghd_sampled* a, ghd_accept_resul
     if (a->draft_row && (a->n_draft < 1 || !(a->draft_temperature > 0.f) || !(a->draft_temperature <= 0x1p64f)))
         return fail(c, GHD_EINVAL, "accept_sampled: no draft rows, or a draft temperature outside (0, 2^64]");
     if (!c->ws) return fail(c, GHD_ENOSPACE, "no workspace set");
+    OnDevice dev(c);
     const int k = cluster_for(c, a->n_seqs, c->cfg.vocab, 2);
     ghd_status s = raise_room(c);
     if (s != GHD_OK) return s;
