@@ -1,5 +1,7 @@
 // Tensor-map (TMA descriptor) construction, cached per context.
 #include <cstring>
+#include <new>
+#include <utility>
 
 #include "tc_common.cuh"
 
@@ -32,10 +34,14 @@ bool cached(ghd_ctx* c, const TmapKey& key, CUtensorMap* out) {
 }
 
 void remember(ghd_ctx* c, const TmapKey& key, const CUtensorMap& tm) {
-    std::vector<uint64_t> blob(sizeof(CUtensorMap) / 8);
-    memcpy(blob.data(), &tm, sizeof(CUtensorMap));
-    if (c->tmaps->size() > 8192) c->tmaps->clear();
-    (*c->tmaps)[key] = blob;
+    // (a map that memory did not suffice for is made again the next time: no exception may leave a C entry)
+    try {
+        std::vector<uint64_t> blob(sizeof(CUtensorMap) / 8);
+        memcpy(blob.data(), &tm, sizeof(CUtensorMap));
+        if (c->tmaps->size() > 8192) c->tmaps->clear();
+        c->tmaps->emplace(key, std::move(blob));
+    } catch (const std::bad_alloc&) {
+    }
 }
 
 }  // namespace
