@@ -8,7 +8,7 @@
 // that a weight is read once for all; the epilogue adds them.
 //
 // As in the half-precision projection, 128 rows of w are the M of an MMA, the columns of x its N; a unit is one tile of 128 rows (MT = 1)
-// or two (MT = 2: two neighbours that share the loads of x, or a gate tile with its up tile).  Where there are fewer than half as many
+// or two (MT = 2: two neighbours that share the loads of x, or a gate tile with its up tile; which: at the launch below).  Where there are fewer than half as many
 // units as SMs, a cluster of CTAs shares each, a part of k to every CTA, and adds up through distributed shared memory.
 // Otherwise the flattened (unit, k-step) space is cut into equal ranges, one per CTA: whoever has the first k-step of a unit finishes
 // it, with its own sums in registers, as the last of its range; the others have come to it first and left their sums in the workspace (a
@@ -195,11 +195,11 @@ __global__ void __launch_bounds__(256) k_mx4_terms(const T* __restrict__ x, int6
 }
 
 // ---------------------------------------------------------------- product
-template <int P, int MT, bool GATE>
+template <int P, int MT, bool GATE, int KS>
 __global__ void __launch_bounds__(THREADS, 1)
 k_mx4_gemm(const __grid_constant__ Mx4Maps maps, const Mx4Params p) {
     static_assert(!GATE || MT == 2, "a gate tile and its up tile");
-    constexpr int KS = MT == 1 ? 2 : 1;                        // k-steps of a stage at most (fewer at the end of a range or a unit)
+    // KS: k-steps of a stage at most (fewer at the end of a range or a unit)
     extern __shared__ uint8_t smem_raw[];
     const uint32_t raw_addr = smem_u32(smem_raw);
     uint8_t* tiles = smem_raw + ((1024u - (raw_addr & 1023u)) & 1023u);
@@ -589,6 +589,41 @@ Groups groups_of(int n, int terms, int most) {
     return g;
 }
 
+// Raises the kernels' limits of shared memory and finds out how many clusters the device holds, once a context.
+template <int P>
+ghd_status prepare(ghd_ctx* c) {
+    if (c->attr_mx4) return GHD_OK;
+    const void* kernels[] = {(const void*)k_mx4_gemm<P, 1, false, 2>, (const void*)k_mx4_gemm<P, 1, false, 1>, (const void*)k_mx4_gemm<P, 2, false, 1>,
+                             (const void*)k_mx4_gemm<P, 2, true, 1>};       // (a context has one type)
+    for (const void* f : kernels)
+        if (cudaFuncSetAttribute(f, cudaFuncAttributeMaxDynamicSharedMemorySize, 227 * 1024) != cudaSuccess) return check_cuda(c, "mx4: shared memory");
+    // clusters that the device holds at a time (they do not straddle its groups of SMs): fewer than SMs / size for the larger ones
+    for (int k = 2; k <= MAX_SPLIT; ++k) {
+        cudaLaunchConfig_t cfg = {};
+        cfg.gridDim = dim3(k);
+        cfg.blockDim = dim3(THREADS);
+        cfg.dynamicSmemBytes = 227 * 1024;
+        cudaLaunchAttribute attr;
+        attr.id = cudaLaunchAttributeClusterDimension;
+        attr.val.clusterDim.x = (unsigned)k;
+        attr.val.clusterDim.y = attr.val.clusterDim.z = 1;
+        cfg.attrs = &attr;
+        cfg.numAttrs = 1;
+        if (cudaOccupancyMaxActiveClusters(&c->mx4_clusters[k], k_mx4_gemm<P, 1, false, 2>, &cfg) != cudaSuccess) return check_cuda(c, "mx4: clusters");
+    }
+    c->attr_mx4 = true;
+    return GHD_OK;
+}
+
+// CTAs (a cluster) that share a unit where there are fewer than half as many units as SMs; else 1
+int split_of(const ghd_ctx* c, int units, int kt, int sms) {
+    int split = 1;
+    if (units * 2 <= sms)
+        for (int k = 2; k <= MAX_SPLIT && k <= kt; ++k)
+            if (c->mx4_clusters[k] >= units) split = k;
+    return split;
+}
+
 template <typename T>
 ghd_status go(ghd_ctx* c, const T* x, int64_t ld, bool wide, const ghd_mx4* w, const ghd_mx4* w2, int n, void* out) {
     constexpr int P = TERMS<T>;
@@ -598,11 +633,22 @@ ghd_status go(ghd_ctx* c, const T* x, int64_t ld, bool wide, const ghd_mx4* w, c
     p.kt = (w->k + TILE - 1) / TILE;
     p.tiles = (w->m + TILE - 1) / TILE;
     p.per_group = g.per; p.groups = g.groups; p.cols = g.cols; p.sf_atoms = g.atoms;
-    // two tiles share the columns of x as soon as these are more bytes than a tile (64 a row)
-    const int mt = w2 || g.cols > 64 ? 2 : 1;
+    const ghd_status ready = prepare<P>(c);
+    if (ready != GHD_OK) return ready;
+    int ctas = c->sm_count < MAX_WORKERS ? c->sm_count : MAX_WORKERS;
+    // Two tiles share the columns of x as soon as these are more bytes than a tile (64 a row).  Single ones have half as many sums to exchange at
+    // the end, but load x twice as often, which costs 0.1 us a k-step: they are taken where clusters share few k-steps, or where clusters of pairs
+    // would leave many SMs without work.  Kernel us, pairs / single: 64 rows by 1024 x 1024 9.6 / 7.3, 4096 x 4096 13.3 / 10.4, 4096 x 11008 18.1 / 15.9;
+    // not taken: 96 rows by 4096 x 11008 20.8 / 23.3, 24 rows by 5120 x 13824 16.1 / 18.3, 24 rows of floats by 8192 x 4096 11.1 / 12.0.
+    int mt = w2 || g.cols > 64 ? 2 : 1;
+    if (mt == 2 && !w2) {
+        const int one = split_of(c, p.tiles * g.groups, p.kt, ctas), two = split_of(c, (p.tiles + 1) / 2 * g.groups, p.kt, ctas);
+        const int steps = (p.kt + one - 1) / one, pair_steps = (p.kt + two - 1) / two;
+        if (p.tiles * g.groups * 2 <= ctas && (steps * P <= 48 || 2 * steps <= 3 * pair_steps)) mt = 1;
+    }
     p.units = (w2 ? p.tiles : (p.tiles + mt - 1) / mt) * g.groups;
     p.total = (long long)p.units * p.kt;
-    const int ks = mt == 1 ? 2 : 1;                              // as in the kernel (2 * cols rows of x are one box then)
+    const int ks = mt == 1 && g.cols <= 64 ? 2 : 1;              // (ks * cols rows of x are one box)
     const size_t stage = (ks * ((size_t)mt * (A_BYTES + SF_BYTES) + (size_t)g.cols * TILE + (size_t)g.atoms * SF_BYTES) + 1023) / 1024 * 1024;
     p.stages = (int)((227 * 1024 - 1024 - sizeof(Smem)) / stage);
     if (p.stages > MAX_STAGES) p.stages = MAX_STAGES;
@@ -626,34 +672,10 @@ ghd_status go(ghd_ctx* c, const T* x, int64_t ld, bool wide, const ghd_mx4* w, c
             !tmap_bytes(c, terms, (uint64_t)g.groups * p.kt * g.cols, (uint32_t)(g.cols * (q + 1)), false, &maps.x[q]))
             return fail(c, GHD_ECUDA, "mx4: tensor map encoding failed");
     for (int q = ks; q < 2; ++q) { maps.w[q] = maps.w[0]; maps.w2[q] = maps.w2[0]; maps.x[q] = maps.x[0]; }
-    if (!c->attr_mx4) {
-        const void* kernels[] = {(const void*)k_mx4_gemm<3, 1, false>, (const void*)k_mx4_gemm<3, 2, false>, (const void*)k_mx4_gemm<3, 2, true>,
-                                 (const void*)k_mx4_gemm<5, 1, false>, (const void*)k_mx4_gemm<5, 2, false>, (const void*)k_mx4_gemm<5, 2, true>};
-        for (const void* f : kernels)
-            if (cudaFuncSetAttribute(f, cudaFuncAttributeMaxDynamicSharedMemorySize, 227 * 1024) != cudaSuccess) return check_cuda(c, "mx4: shared memory");
-        // clusters that the device holds at a time (they do not straddle its groups of SMs): fewer than SMs / size for the larger ones
-        for (int k = 2; k <= MAX_SPLIT; ++k) {
-            cudaLaunchConfig_t cfg = {};
-            cfg.gridDim = dim3(k);
-            cfg.blockDim = dim3(THREADS);
-            cfg.dynamicSmemBytes = 227 * 1024;
-            cudaLaunchAttribute attr;
-            attr.id = cudaLaunchAttributeClusterDimension;
-            attr.val.clusterDim.x = (unsigned)k;
-            attr.val.clusterDim.y = attr.val.clusterDim.z = 1;
-            cfg.attrs = &attr;
-            cfg.numAttrs = 1;
-            if (cudaOccupancyMaxActiveClusters(&c->mx4_clusters[k], k_mx4_gemm<P, 1, false>, &cfg) != cudaSuccess) return check_cuda(c, "mx4: clusters");
-        }
-        c->attr_mx4 = true;
-    }
     const int warps = n * ((p.kt + 1) / 2);
     launch_k(c, false, k_mx4_terms<T>, (warps + 7) / 8, 256, 0, x, ld, n, (int)w->k, wide, p.kt, g.per, g.cols, g.atoms, (uint2*)terms, (uint32_t*)x_scales);
-    int ctas = c->sm_count < MAX_WORKERS ? c->sm_count : MAX_WORKERS;
-    p.split = 1;
+    p.split = split_of(c, p.units, p.kt, ctas);
     if (p.units * 2 <= ctas) {
-        for (int k = 2; k <= MAX_SPLIT && k <= p.kt; ++k)
-            if (c->mx4_clusters[k] >= p.units) p.split = k;
         ctas = p.units * p.split;
     } else if (p.units < ctas) {
         // ranges of (q - 1) / q of a unit: each holds the border between two units, and nobody's range lies within one
@@ -663,9 +685,10 @@ ghd_status go(ghd_ctx* c, const T* x, int64_t ld, bool wide, const ghd_mx4* w, c
     if (ctas > p.total) ctas = (int)p.total;
     const size_t smem = 1024 + p.stages * stage + sizeof(Smem);
     if (p.stages < 2 || p.stages * stage < (size_t)mt * g.per * TILE * sizeof(float)) return fail(c, GHD_EUNSUPPORTED, "mx4: no room for a ring of stages");
-    if (w2) launch_kc(c, true, p.split, k_mx4_gemm<P, 2, true>, ctas, THREADS, smem, maps, p);
-    else if (mt == 2) launch_kc(c, true, p.split, k_mx4_gemm<P, 2, false>, ctas, THREADS, smem, maps, p);
-    else launch_kc(c, true, p.split, k_mx4_gemm<P, 1, false>, ctas, THREADS, smem, maps, p);
+    if (w2) launch_kc(c, true, p.split, k_mx4_gemm<P, 2, true, 1>, ctas, THREADS, smem, maps, p);
+    else if (mt == 2) launch_kc(c, true, p.split, k_mx4_gemm<P, 2, false, 1>, ctas, THREADS, smem, maps, p);
+    else if (ks == 1) launch_kc(c, true, p.split, k_mx4_gemm<P, 1, false, 1>, ctas, THREADS, smem, maps, p);
+    else launch_kc(c, true, p.split, k_mx4_gemm<P, 1, false, 2>, ctas, THREADS, smem, maps, p);
     return GHD_OK;
 }
 

@@ -170,6 +170,21 @@ def test_linear(ghd, dtype, n, m, k):
     assert (y == again).all()
 
 
+# clusters of single tiles and of pairs, with an odd number of tiles, several groups of rows, one k-step, more CTAs than k-steps
+@pytest.mark.parametrize("dtype", ["f16", "f32"])
+@pytest.mark.parametrize("n,m,k", [(96, 2400, 7000), (24, 2400, 7000), (64, 300, 1100), (22, 9400, 300), (40, 9600, 300), (64, 700, 100), (256, 1100, 130)])
+def test_linear_shared_units(ghd, dtype, n, m, k):
+    r = np.random.RandomState(n * 11 + m + k)
+    ctx = make_ctx(ghd, dtype, k, n)
+    w, codes, scales = random_held(ghd, r, m, k)
+    x = r.randn(n, k).astype(np_t(dtype))
+    y = ghd.ghd_mx4_linear(ctx, dev(x), w)
+    again = ghd.ghd_mx4_linear(ctx, dev(x), w)
+    ghd.ghd_sync_status(ctx)
+    check_product(x, codes, scales, m, k, y.cpu().numpy())
+    assert (y == again).all()
+
+
 @pytest.mark.parametrize("dtype", ["f16", "f32"])
 @pytest.mark.parametrize("n,m,k", [(1, 1, 1), (1, 11008, 512), (16, 130, 100), (33, 300, 384), (64, 512, 1000), (70, 1376, 512), (256, 257, 256)])
 def test_gate_up(ghd, dtype, n, m, k):
