@@ -255,43 +255,59 @@ __device__ void measure(Team& m, Dist& p, Dist& q) {
     __syncthreads();
 }
 
-// What is left of P after rejected draws, max(P - beta Q, 0): the weights of every own segment into seg[], of the CTAs' shares into share[]
-// -> the total.  keep (or null): room for P and Q of the own segments, which `kept` says are there from the rejection before.
-__device__ double total_left(Team& m, const Dist& p, const Dist& q, double beta, double2* keep, bool kept) {
-    double all = 0.0;
+// What is left after rejected draws gone[0 .. n): of P max(P - beta Q, 0), the weights of every own segment into seg[], of the CTAs' shares into
+// share[] -> the total; of Q the sum without these tokens -> rest.  Both are sums over what is left: 1 - Q(rejected) has no right digit where a
+// rejected token holds all but 1e-16 of Q.  keep (or null): room for P and Q of the own segments, which `kept` says are there from the
+// rejection before.
+__device__ double total_left(Team& m, const Dist& p, const Dist& q, double beta, int n, double2* keep, bool kept, double& rest) {
+    double all = 0.0, all_q = 0.0;
 #pragma unroll 1
     for (int g = m.warp; g < m.segs; g += WARPS) {
-        double sum = 0.0;
+        double2 v[RUN];
         double2* at = keep + g * SEG + m.lane;
+        const int t = m.first_of(m.seg0 + g);
         if (keep && kept) {
 #pragma unroll
-            for (int e = 0; e < RUN; ++e) {
-                const double2 v = at[e * 32];
-                sum += fmax(v.x - beta * v.y, 0.0);
-            }
+            for (int e = 0; e < RUN; ++e) v[e] = at[e * 32];
         } else {
             float x[RUN], y[RUN];
-            const int t = m.first_of(m.seg0 + g);
             m.load(p.row, t, x);
             m.load(q.row, t, y);
 #pragma unroll
             for (int e = 0; e < RUN; ++e) {
-                const double2 v = make_double2(p.of(x[e]), q.of(y[e]));
-                if (keep) at[e * 32] = v;
-                sum += fmax(v.x - beta * v.y, 0.0);
+                v[e] = make_double2(p.of(x[e]), q.of(y[e]));
+                if (keep) at[e * 32] = v[e];
             }
+        }
+#pragma unroll 1
+        for (int i = 0; i < n; ++i) {
+            const int d = m.s->gone[i];
+            if (d / SEG != m.seg0 + g) continue;                 // (the whole warp)
+#pragma unroll
+            for (int e = 0; e < RUN; ++e) if (d == t + e) v[e] = make_double2(0.0, 0.0);
+        }
+        double sum = 0.0;
+#pragma unroll
+        for (int e = 0; e < RUN; ++e) {
+            sum += fmax(v[e].x - beta * v[e].y, 0.0);
+            all_q += v[e].y;
         }
         sum = warp_sum(sum);
         if (m.lane == 0) m.seg[g] = sum;
         all += sum;
     }
-    if (m.lane == 0) m.s->part[0][m.warp][0] = all;
+    all_q = warp_sum(all_q);
+    if (m.lane == 0) { m.s->part[0][m.warp][0] = all; m.s->part[0][m.warp][1] = all_q; }
     __syncthreads();
-    if (m.warp == 0) {
-        const double sum = warp_sum(m.lane < WARPS ? m.s->part[0][m.lane][0] : 0.0);
-        if (m.lane == 0) m.s->mine[0] = sum;
+    if (m.warp < 2) {
+        const double sum = warp_sum(m.lane < WARPS ? m.s->part[0][m.lane][m.warp] : 0.0);
+        if (m.lane == 0) m.s->mine[m.warp] = sum;
     }
-    return m.add_shares(m.exchange(1));
+    double (*box)[VALUES] = m.exchange(2);
+    rest = m.lane % MAX_CLUSTER < m.size ? box[m.lane % MAX_CLUSTER][1] : 0.0;
+#pragma unroll
+    for (int o = 1; o < MAX_CLUSTER; o <<= 1) rest += __shfl_xor_sync(0xffffffffu, rest, o);
+    return m.add_shares(box);
 }
 
 // The CTA in whose share u times the total falls (the last one with weight where rounding leaves none) -> whether it is this one, and the
@@ -508,9 +524,10 @@ __global__ void __launch_bounds__(THREADS, HELD) k_draft_sample(const float* __r
 // A walk from the root.  At a node with target distribution P and draft distribution Q its children are looked at in order, with
 // P_1 = P, Q_1 = Q: child x is accepted if u Q_j(x) < P_j(x); otherwise P_{j+1} = max(P_j - Q_j, 0) / its sum and Q_{j+1} = Q_j
 // without x / its sum.  Written out, P_j = max(P - beta_j Q, 0) / W_j with W_j its sum: subtracting Q_j = c_j Q from that gives
-// beta_{j+1} = beta_j + c_j W_j, and c_j = 1 / (1 - Q(rejected)).  A rejected token has u Q_j >= P_j, u < 1, so P_{j+1} gives it
-// nothing, and so do all later ones: beta only grows.  So two numbers are kept instead of two distributions, and a rejection costs
-// one sum over the vocabulary.  Candidates that nobody drew have Q = 1 at themselves: P_{j+1} is P_j without x.
+// beta_{j+1} = beta_j + c_j W_j, and 1 / c_j is the sum of Q without the rejected tokens.  A rejected token has u Q_j >= P_j, u < 1, so
+// P_{j+1} gives it nothing, and so do all later ones: beta only grows (rounding is kept out of it by taking rejected tokens out).  So two
+// numbers are kept instead of two distributions, and a rejection costs one pass over the vocabulary for both sums.  Where P - beta Q
+// is nothing but rounding, P_j stays, without x.  Candidates that nobody drew have Q = 1 at themselves: P_{j+1} is P_j without x.
 // The segments' weights and references of all rows, of the targets and behind them of the drafts, a warp to a segment.  With few trees
 // the walk below knows its rows one after the other only, and most SMs would wait; weighing all rows first costs less than it saves.
 __global__ void __launch_bounds__(THREADS, 4) k_row_segments(const float* __restrict__ logits, const float* __restrict__ draft, int n_rows, int n_draft, int vocab, bool wide, double scale,
@@ -591,7 +608,7 @@ __global__ void __launch_bounds__(THREADS, 2) k_accept_sampled(ghd_sampled a, in
             sm.of_q[threadIdx.x] = look && q.row ? q.of(lq) : 0.0;
         }
         __syncthreads();
-        double beta = 0.0, W = 1.0, rejected = 0.0;
+        double beta = 0.0, W = 1.0, rest = 1.0, rejected = 0.0;      // rest: of Q without the rejected tokens
         int n_gone = 0, next = -1;
         bool fresh = false;                                    // seg[] and share[] are of the weights as they are, their total is W
         auto left = [&](float lp, float lq) { return fmax(p.of(lp) - beta * q.of(lq), 0.0); };
@@ -606,12 +623,15 @@ __global__ void __launch_bounds__(THREADS, 2) k_accept_sampled(ghd_sampled a, in
                         bool before = false;                   // a token that was rejected already is not drawn again
                         for (int g = 0; g < n_gone; ++g) before |= sm.gone[g] == x;
                         if (!(qx > 0.0) || before) continue;
-                        const double c_j = 1.0 / fmax(1.0 - rejected, qx);
-                        if (!(W > 0.0)) break;
-                        if (u * qx * c_j * W < fmax(px - beta * qx, 0.0)) { next = c; break; }
-                        beta += c_j * W;
-                        rejected += qx;
-                        W = total_left(m, p, q, beta, keep, fresh);
+                        const double c_j = 1.0 / fmax(rest, qx);
+                        if (u * (qx * c_j) * W < fmax(px - beta * qx, 0.0)) { next = c; break; }
+                        __syncthreads();
+                        if (threadIdx.x == 0) sm.gone[n_gone] = x;
+                        ++n_gone;
+                        __syncthreads();
+                        const double more = beta + c_j * W, w = total_left(m, p, q, more, n_gone, keep, fresh, rest);
+                        if (w > 0.0) beta = more;
+                        W = w > 0.0 ? w : total_left(m, p, q, beta, n_gone, keep, true, rest);
                         fresh = true;
                     } else {
                         bool before = false;
@@ -619,11 +639,11 @@ __global__ void __launch_bounds__(THREADS, 2) k_accept_sampled(ghd_sampled a, in
                         if (before) continue;
                         if (u * fmax(1.0 - rejected, px) < px) { next = c; break; }
                         rejected += px;
+                        __syncthreads();
+                        if (threadIdx.x == 0) sm.gone[n_gone] = x;
+                        ++n_gone;
+                        __syncthreads();
                     }
-                    __syncthreads();
-                    if (threadIdx.x == 0) sm.gone[n_gone] = x;
-                    ++n_gone;
-                    __syncthreads();
                 }
         if (next < 0) {
             if (!p.ok) {
@@ -631,14 +651,9 @@ __global__ void __launch_bounds__(THREADS, 2) k_accept_sampled(ghd_sampled a, in
             } else {
                 // What is left of P: after rejected draws the weights of the last sum; otherwise P's own segments (not divided by the sum),
                 // those with a token that is gone weighed again.
-                if (fresh && !(W > 0.0)) {
-                    beta = 0.0;
-                    W = total_left(m, p, q, beta, keep, true);
-                }
                 double total = W;
                 if (!fresh) {
                     p.inv_sum = 1.0;
-                    if (q.row) n_gone = 0;
                     if (READY) {
                         if (m.rank != 0) break;
                         // the first CTA has all of the row
@@ -672,8 +687,8 @@ __global__ void __launch_bounds__(THREADS, 2) k_accept_sampled(ghd_sampled a, in
                     } else {
 #pragma unroll
                         for (int e = 0; e < RUN; ++e) w[e] = p.of(x[e]);
-                        without(w, t0, sm.gone, n_gone);
                     }
+                    without(w, t0, sm.gone, n_gone);
                     const int t = token_of(w, t0, start, target, m.lane);
                     if (m.lane == 0) out->tokens[depth] = t;
                 }

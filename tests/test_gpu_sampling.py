@@ -488,3 +488,81 @@ def test_refusals(ghd):
     assert (ghd.ghd_draft_sample(ctx, lg[:0], u[:0], 3).shape == (0, 16))
     ghd.ghd_sync_status(ctx)
     assert big.n == 1
+
+
+# ------------------------------------------------------------------ cold drafters
+# (lead of the likeliest draft token over the others in logits, draft temperature): from a lead that rounding does not see to one in
+# front of which the rest is nothing in 64 bits (40 at 0.05: 800 nats; the others stay clear of the 693 that the calls hold and the 745 that the
+# oracle's exponential holds)
+COLD = [(3, 0.05), (3, 0.5), (8, 0.2), (10, 0.2), (10, 0.25), (16, 0.4), (20, 0.5), (20, 0.1), (30, 0.05), (40, 0.4), (40, 0.05)]
+
+
+def cold_batch(r, seqs, kids, vocab, lead, temp_q):
+    """seqs trees of a root with `kids` children drawn from a draft row with one token far ahead, which the target mostly rejects."""
+    b = Batch(r, [1 + kids] * seqs, vocab, 1.0, False)
+    n = 1 + kids
+    b.parent = np.tile(np.array([-1] + [0] * kids, np.int32), seqs)
+    b.logits = (r.randn(b.n, vocab) * 1.2).astype(np.float32)
+    b.draft = (r.uniform(-0.5, 0.5, (seqs, vocab))).astype(np.float32)
+    top = r.randint(0, vocab, seqs)
+    b.draft[np.arange(seqs), top] += np.float32(lead)
+    b.logits[np.arange(seqs) * n, top] -= np.float32(4)
+    b.drow = np.repeat(np.arange(seqs), n).astype(np.int32)
+    for s in range(seqs):
+        b.tokens[n * s + 1:n * (s + 1)] = osam.draw(b.draft[s], temp_q, kids, r.rand(kids).astype(np.float32))[:kids]
+    # the first child is rejected in most of the trees, the later ones meet any number
+    b.u[1::n] = np.where(r.rand(seqs) < 0.9, np.float32(0.97), b.u[1::n])
+    return b
+
+
+def check_cold(b, got, temp_q):
+    rejected = 0
+    for s, n in enumerate(b.cnt):
+        a, e = b.start[s], b.start[s] + n
+        nodes, toks = osam.verify(b.parent[a:e], b.tokens[a:e], b.logits[a:e], b.u[a:e], 1.0, b.drow[a:e], b.draft, temp_q)
+        assert list(got[s, :2]) == [len(nodes) - 1, len(nodes)] and list(got[s, 2:2 + len(nodes)]) == nodes and list(got[s, 258:258 + len(toks)]) == toks, (s, nodes, toks)
+        rejected += nodes[1:2] != [1]
+    return rejected
+
+
+@pytest.mark.parametrize("lead,temp_q", COLD)
+@pytest.mark.parametrize("vocab,seqs,kids", [(5, 400, 2), (600, 100, 3), (4100, 12, 5), (8000, 150, 4)])
+def test_verify_of_cold_drafters(ghd, lead, temp_q, vocab, seqs, kids):
+    """One draft token holds nearly all of its distribution and is rejected: what is left of it decides, however little that is.
+    All rows weighed ahead and row by row (unused draft rows make them many), with a node's probabilities kept and (8000) worked out again."""
+    import torch
+    r = np.random.RandomState(int(lead * 100 + temp_q * 1000) + vocab + kids)
+    b = cold_batch(r, seqs, kids, vocab, lead, temp_q)
+    ctx = ctx_for(ghd, vocab)
+    more = dict(draft_row=dev(b.drow), draft_temperature=temp_q)
+    got = ghd.ghd_accept_sampled(ctx, b.rows(ghd, draft_logits=dev(b.draft), **more))
+    assert check_cold(b, got.cpu().numpy(), temp_q) > seqs // 2
+    rest = torch.zeros(49152 * 256 // vocab + 1 if vocab > 256 else 49152, vocab, device="cuda")
+    assert (got == ghd.ghd_accept_sampled(ctx, b.rows(ghd, draft_logits=torch.cat((dev(b.draft), rest)), **more))).all()
+    ghd.ghd_sync_status(ctx)
+
+
+@pytest.mark.parametrize("lead,temp_q", [(10, 0.25), (10, 0.2), (16, 0.4), (37, 1.0), (40, 0.05)])
+def test_cold_drafters_leave_the_distribution_as_it_is(ghd, lead, temp_q):
+    """Draws and their verification together: the first token is the target's over many random numbers."""
+    import torch
+    V, seqs, calls = 5, 1024, 40
+    ctx = ctx_for(ghd, V)
+    p = np.array([0.02, 0.10, 0.60, 0.20, 0.08])
+    logits = torch.log(torch.tensor(np.tile(p, (3 * seqs, 1)), device="cuda")).float()
+    draft = torch.tensor([[lead, 0.6, -0.5, -0.2, 0.1]], device="cuda").float().repeat(seqs, 1)
+    g = torch.Generator(device="cuda")
+    g.manual_seed(int(lead * 10 + temp_q * 100))
+    i32 = dict(dtype=torch.int32, device="cuda")
+    parent = torch.tensor([-1, 0, 0] * seqs, **i32)
+    start, drow = torch.arange(0, 3 * seqs + 1, 3, **i32), torch.arange(0, seqs, **i32).repeat_interleave(3)
+    count = torch.zeros(V, device="cuda")
+    for _ in range(calls):
+        cand = ghd.ghd_draft_sample(ctx, draft, torch.rand(seqs, 16, generator=g, device="cuda"), 2, temp_q)
+        tokens = torch.cat((torch.zeros(seqs, 1, **i32), cand[:, :2]), 1).reshape(-1).contiguous()
+        rows = ghd.SampledRows(parent, tokens, logits, torch.rand(3 * seqs, generator=g, device="cuda"), row_start=start, draft_row=drow, draft_logits=draft, draft_temperature=temp_q)
+        first = ghd.ghd_accept_sampled(ctx, rows)[:, 258]
+        count += torch.bincount(first.long(), minlength=V)
+    ghd.ghd_sync_status(ctx)
+    n = seqs * calls
+    assert (np.abs(count.cpu().numpy() / n - p) <= 5 * np.sqrt(p * (1 - p) / n)).all(), count / n
