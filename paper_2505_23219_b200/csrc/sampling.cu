@@ -608,7 +608,7 @@ __global__ void __launch_bounds__(THREADS, 2) k_accept_sampled(ghd_sampled a, in
             sm.of_q[threadIdx.x] = look && q.row ? q.of(lq) : 0.0;
         }
         __syncthreads();
-        double beta = 0.0, W = 1.0, rest = 1.0, rejected = 0.0;      // rest: of Q without the rejected tokens
+        double beta = 0.0, W = 1.0, rest = 1.0;                // rest: of what the children come from (Q, or P if they were not drawn) without the rejected tokens
         int n_gone = 0, next = -1;
         bool fresh = false;                                    // seg[] and share[] are of the weights as they are, their total is W
         auto left = [&](float lp, float lq) { return fmax(p.of(lp) - beta * q.of(lq), 0.0); };
@@ -637,12 +637,16 @@ __global__ void __launch_bounds__(THREADS, 2) k_accept_sampled(ghd_sampled a, in
                         bool before = false;
                         for (int g = 0; g < n_gone; ++g) before |= sm.gone[g] == x;
                         if (before) continue;
-                        if (u * fmax(1.0 - rejected, px) < px) { next = c; break; }
-                        rejected += px;
+                        if (u * fmax(rest, px) < px) { next = c; break; }
+                        rest -= px;
                         __syncthreads();
                         if (threadIdx.x == 0) sm.gone[n_gone] = x;
                         ++n_gone;
                         __syncthreads();
+                        if (rest < 0x1p-10) {                  // the difference loses its digits (random numbers close to one get here)
+                            W = total_left(m, p, p, 0.0, n_gone, nullptr, false, rest);
+                            fresh = true;
+                        }
                     }
                 }
         if (next < 0) {
@@ -680,7 +684,7 @@ __global__ void __launch_bounds__(THREADS, 2) k_accept_sampled(ghd_sampled a, in
                     double w[RUN];
                     const int t0 = m.first_of(m.seg0 + max(sg, 0));
                     m.load(p.row, t0, x);
-                    if (fresh) {
+                    if (fresh && q.row) {
                         m.load(q.row, t0, y);
 #pragma unroll
                         for (int e = 0; e < RUN; ++e) w[e] = left(x[e], y[e]);

@@ -566,3 +566,27 @@ def test_cold_drafters_leave_the_distribution_as_it_is(ghd, lead, temp_q):
     ghd.ghd_sync_status(ctx)
     n = seqs * calls
     assert (np.abs(count.cpu().numpy() / n - p) <= 5 * np.sqrt(p * (1 - p) / n)).all(), count / n
+
+
+@pytest.mark.parametrize("vocab", [5, 700, 9000])
+def test_candidates_that_were_not_drawn_and_hold_nearly_all(ghd, vocab):
+    """Each child holds all but some 1e-7 of what is left of the target and is rejected all the same (its number is close to one): what is
+    left after three of them is less than rounding leaves of 1 - their sum."""
+    r = np.random.RandomState(vocab)
+    ctx, seqs, kids = ctx_for(ghd, vocab), 60, 5
+    b = Batch(r, [1 + kids] * seqs, vocab, 1.0, True)
+    n, most = 1 + kids, np.float32(osam.U_MOST)
+    b.parent = np.tile(np.array([-1] + [0] * kids, np.int32), seqs)
+    b.drow[:] = -1
+    for s in range(seqs):
+        order = r.choice(vocab, 5, replace=False)
+        b.logits[n * s] = -110.0 + r.rand(vocab)
+        b.logits[n * s, order] = -16.0 * np.arange(5)
+        b.tokens[n * s + 1:n * (s + 1)] = order
+        b.u[n * s + 1:n * (s + 1)] = np.where(np.arange(kids) < s % 5, most, r.rand(kids))
+    many = np.concatenate((b.draft, np.zeros((49152 // (vocab // 256 + 1) + 1, vocab), np.float32)))
+    for draft in (b.draft, many):
+        got = ghd.ghd_accept_sampled(ctx, b.rows(ghd, draft_logits=dev(draft))).cpu().numpy()
+        b.check(got)
+    assert {1, 2, 3, 4, 5} <= set(got[:, 3])
+    ghd.ghd_sync_status(ctx)
