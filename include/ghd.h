@@ -400,7 +400,8 @@ ghd_status ghd_mx4_gate_up(ghd_ctx *ctx, const void *h, int64_t h_ld, const ghd_
  * these calls for tokens drawn from its distribution, which they leave exactly as it is whatever the drafter.)
  * The distribution of a row of logits (float [cfg.vocab]) is softmax(logits / temperature); -inf leaves a token out (top-k or
  * nucleus filters are such logits).  Random numbers are the caller's, float in [0, 1) (others are held to that); weights and sums are
- * worked out in 64 bits.  A row with a NaN or +inf, or with nothing but -inf, is none: ghd_sync_status -> GHD_EINVAL.
+ * worked out in 64 bits, which leave out a token with less than 2^-1000 of the least power of two that is not below the likeliest one's
+ * weight (behind it by 693 temperatures).  A row with a NaN or +inf, or with nothing but -inf, is none: ghd_sync_status -> GHD_EINVAL.
  * cfg.vocab up to 2^20 (GHD_ESHAPE), temperatures in (0, 2^64]. */
 
 /* Candidates: for each of n_rows rows of logits (the heads of one sequence, or of many) n_draws tokens drawn without replacement.

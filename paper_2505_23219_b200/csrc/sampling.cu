@@ -204,9 +204,34 @@ __device__ __forceinline__ double segment_sum(const float (&x)[RUN], double scal
     return warp_sum(sum_of(x, scale, ref, roots));
 }
 
+// seg[] from the segments' own weights and references: the weights with the row's reference (not divided by the sum).  A token ends at 2^-1000 of that
+// reference (see pow2), a segment's weight does not: what is below FAR is weighed again token by token, so that a segment has weight exactly where
+// a token of it has.  Above FAR the tokens that end are 2^-60 of their segment.
+constexpr double FAR = -940.0;
+template <typename W, typename R>
+__device__ void row_weights(Team& m, const Dist& p, W weight_of, R ref_of) {
+    bool far = false;
+    for (int g = threadIdx.x; g < m.segs; g += THREADS) {
+        const double d = ref_of(g) - p.ref, w = weight_of(g) * pow2_whole(d);
+        m.seg[g] = w;
+        far |= w > 0.0 && d < FAR;
+    }
+    if (!__syncthreads_or(far)) return;
+#pragma unroll 1
+    for (int g = m.warp; g < m.segs; g += WARPS) {
+        if (!(m.seg[g] > 0.0 && ref_of(g) - p.ref < FAR)) continue;
+        float x[RUN];
+        m.load(p.row, m.first_of(m.seg0 + g), x);
+        const double sum = warp_sum(sum_of(x, p.scale, p.ref, p.roots));
+        if (m.lane == 0) m.seg[g] = sum;
+    }
+    __syncthreads();
+}
+
 // Reference and sum of a row p and, if q.row is given, of a second one.  seg[] is left with p's weights (not divided by the sum),
-// share[] has every CTA's part of p's sum.
-__device__ void measure(Team& m, Dist& p, Dist& q) {
+// share[] has every CTA's part of p's sum.  -> whether a part is below FAR: then the sum of seg[] is right, share[] is not.
+__device__ bool measure(Team& m, Dist& p, Dist& q) {
+    bool far = false;
     const int n = q.row ? 2 : 1;
     double ref[2] = {-INFINITY, -INFINITY}, all[2] = {0.0, 0.0};
 #pragma unroll 1
@@ -243,6 +268,7 @@ __device__ void measure(Team& m, Dist& p, Dist& q) {
 #pragma unroll
         for (int o = 1; o < MAX_CLUSTER; o <<= 1) both = fmax(both, __shfl_xor_sync(0xffffffffu, both, o));
         sum *= pow2_whole(r - both);
+        if (i == 0) far = __any_sync(0xffffffffu, sum > 0.0 && r - both < FAR);
         if (i == 0 && threadIdx.x < (unsigned)m.size) m.s->share[threadIdx.x] = sum;
 #pragma unroll
         for (int o = 1; o < MAX_CLUSTER; o <<= 1) sum += __shfl_xor_sync(0xffffffffu, sum, o);
@@ -251,8 +277,8 @@ __device__ void measure(Team& m, Dist& p, Dist& q) {
         d.inv_sum = 1.0 / sum;
         d.ok = both > -INFINITY && both < INFINITY && sum < INFINITY;
     }
-    for (int g = threadIdx.x; g < m.segs; g += THREADS) m.seg[g] *= pow2_whole(m.seg[m.segs + g] - p.ref);
-    __syncthreads();
+    row_weights(m, p, [&](int g) { return m.seg[g]; }, [&](int g) { return m.seg[m.segs + g]; });
+    return far;
 }
 
 // What is left after rejected draws gone[0 .. n): of P max(P - beta Q, 0), the weights of every own segment into seg[], of the CTAs' shares into
@@ -600,8 +626,9 @@ __global__ void __launch_bounds__(THREADS, 2) k_accept_sampled(ghd_sampled a, in
         const int mine = threadIdx.x < GHD_MAX_NODES && (sm.child[m.warp % (GHD_MAX_NODES / 32)] >> m.lane & 1) ? sm.token[threadIdx.x] : -1;
         const bool look = mine >= 0 && mine < vocab;
         const float lp = look ? __ldg(p.row + mine) : 0.f, lq = look && q.row ? __ldg(q.row + mine) : 0.f;
+        bool far = false;
         if (READY) collect(m, n_segs, ready + (size_t)(first + node) * n_segs, ready + (size_t)(a.n_rows + max(drawn, 0)) * n_segs, p, q);
-        else measure(m, p, q);
+        else far = measure(m, p, q);
         if (!p.ok || (q.row && !q.ok)) record(DEV_SAMPLE_DIST);
         if (threadIdx.x < GHD_MAX_NODES) {
             sm.of_p[threadIdx.x] = look ? p.of(lp) : 0.0;
@@ -665,11 +692,10 @@ __global__ void __launch_bounds__(THREADS, 2) k_accept_sampled(ghd_sampled a, in
                         m.seg0 = 0;
                         m.segs = n_segs;
                         const double2* row = ready + (size_t)(first + node) * n_segs;
-                        for (int g = threadIdx.x; g < n_segs; g += THREADS) m.seg[g] = row[g].x * pow2_whole(row[g].y - p.ref);
+                        row_weights(m, p, [&](int g) { return row[g].x; }, [&](int g) { return row[g].y; });
                     }
                     if (n_gone > 0) weigh_again(m, p, n_gone);
-                    if (READY) __syncthreads();
-                    if (READY || n_gone > 0) {
+                    if (READY || n_gone > 0 || far) {
                         total = total_again(m);
                     } else {
                         total = 0.0;

@@ -590,3 +590,47 @@ def test_candidates_that_were_not_drawn_and_hold_nearly_all(ghd, vocab):
         b.check(got)
     assert {1, 2, 3, 4, 5} <= set(got[:, 3])
     ghd.ghd_sync_status(ctx)
+
+
+# ------------------------------------------------------------------ the ends of what 64 bits hold
+def held(logits, temp):
+    """The calls' reading of logits: a token with less than 2^-1000 of the likeliest one's weight (which is 1 in these tests) is left out."""
+    z = logits.astype(np.float64) / float(np.float32(temp)) / math.log(2)
+    assert z.max() == 0 and not (np.abs(z + 1000) < 0.2).any()
+    return np.where(z < -1000, -np.inf, logits).astype(np.float32)
+
+
+def far(rows, vocab, temp, top, below):
+    """Token `top` alone at the top, the others `below` (binary orders) under it."""
+    z = np.array(below, np.float64) + np.zeros((rows, vocab))
+    z[:, top] = 0
+    return (-z * (math.log(2) * float(np.float32(temp)))).astype(np.float32)
+
+
+@pytest.mark.parametrize("V,top", [(1024, 700), (9000, 8000)])
+@pytest.mark.parametrize("below", [940.5, 985.5, 998.5, 999.5, 1000.5, 1010.5])
+def test_tokens_at_the_end_of_64_bits(ghd, below, V, top):
+    """Segments (and whole CTAs' shares) in front whose tokens are some 2^-1000 of the likeliest: the number 0 takes the first token that has
+    weight, and there is one.  Draws go on into such tokens as long as they have weight."""
+    import torch
+    temp, seqs = 0.01, 3
+    ctx = ctx_for(ghd, V)
+    r = np.random.RandomState(int(below))
+    logits = far(seqs, V, temp, top, below)
+    logits[2, :top] = far(1, top + 1, temp, top, below - 6.25 + 0.5 * r.randint(0, 20, top + 1))[0, :top]      # some have weight, some have none
+    zero = np.zeros((seqs, 16), np.float32)
+    u = np.stack((zero[0], r.rand(16), r.rand(16))).astype(np.float32)
+    for us in (zero, u):
+        got = ghd.ghd_draft_sample(ctx, dev(logits), dev(us), 8, temp).cpu().numpy()
+        for i in range(seqs):
+            assert np.array_equal(got[i], osam.draw(held(logits[i], temp), temp, 8, us[i])), i
+    lazy = torch.zeros(49152 * 256 // V + 1, V, device="cuda")
+    one = np.full(seqs, -1, np.int32)
+    for draft in (lazy[:1], lazy):
+        for u0 in (0.0, 0.5):
+            rows = ghd.SampledRows(dev(one), dev(one), dev(logits), dev(np.full(seqs, u0, np.float32)), row_start=dev(np.arange(seqs + 1, dtype=np.int32)), temperature=temp,
+                                   draft_row=dev(one), draft_logits=draft)
+            res = ghd.ghd_accept_sampled(ctx, rows).cpu().numpy()
+            for i in range(seqs):
+                assert res[i, 258] == osam.first_over(osam.distribution(held(logits[i], temp), temp), u0), (i, u0)
+    ghd.ghd_sync_status(ctx)
