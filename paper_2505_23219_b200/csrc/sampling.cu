@@ -106,22 +106,29 @@ __device__ __forceinline__ double pow2(double y, const double* roots) {
     r = __hiloint2double(__double2hiint(r) + (n >> 4 << 20), __double2loint(r));
     return (uint32_t)__double2hiint(y) > 0xc08f4000u ? 0.0 : r;      // (below -1000, by its bits)
 }
-// A float as a double by its bits (the conversion has a quarter of the other instructions' rate): numbers below 2^-126 come out below
-// 2^-126, infinities as 2^128, which is as good for weights (a temperature is at most 2^64); NaN is found by the row's maximum.
+// A float as a double by its bits (the conversion has a quarter of the other instructions' rate): numbers below 2^-126, zeros among them, come out
+// below 2^-126, infinities as 2^128 (as good for weights: a temperature is at most 2^64); NaN is found by the row's maximum.
+// COLD: temperatures below some 2^-60 bring what is below 2^-126 up to where it counts, and are served by kernels that convert (looking at each
+// logit costs all calls 5 %, at the temperature 2 to 3).
+constexpr double COLD_SCALE = 0x1p60;
+template <bool COLD>
 __device__ __forceinline__ double widen(float l) {
+    if (COLD) return (double)l;
     const uint32_t b = __float_as_uint(l);
     return __hiloint2double((int)((b & 0x80000000u) | ((b & 0x7fffffffu) >> 3) + 0x38000000u), (int)(b << 29));
 }
 // The product is rounded before the difference: equal logits are equally likely however large they are.
-__device__ __forceinline__ double weight(float l, double scale, double ref, const double* roots) { return pow2(__dsub_rn(__dmul_rn(widen(l), scale), ref), roots); }
+template <bool COLD>
+__device__ __forceinline__ double weight(float l, double scale, double ref, const double* roots) { return pow2(__dsub_rn(__dmul_rn(widen<COLD>(l), scale), ref), roots); }
 
 // One row's distribution: 2^(l * scale - ref) / sum, scale = log2(e) / temperature.
+template <bool COLD>
 struct Dist {
     const float* row;
     double scale, ref, inv_sum;
     bool ok;
     const double* roots;
-    __device__ __forceinline__ double of(float l) const { return weight(l, scale, ref, roots) * inv_sum; }
+    __device__ __forceinline__ double of(float l) const { return weight<COLD>(l, scale, ref, roots) * inv_sum; }
 };
 
 // This CTA's share of a row, and what the cluster has agreed on so far.
@@ -185,15 +192,17 @@ struct Team {
 };
 
 // The weights of a segment's tokens in this lane: 0 of -inf, whatever the reference
+template <bool COLD>
 __device__ __forceinline__ double sum_of(const float (&x)[RUN], double scale, double ref, const double* roots) {
     double w[RUN];
     ref = ref == -INFINITY ? 0.0 : ref;
 #pragma unroll
-    for (int e = 0; e < RUN; ++e) w[e] = weight(x[e], scale, ref, roots);
+    for (int e = 0; e < RUN; ++e) w[e] = weight<COLD>(x[e], scale, ref, roots);
     return ((w[0] + w[1]) + (w[2] + w[3])) + ((w[4] + w[5]) + (w[6] + w[7]));
 }
 
 // One warp: weight of a segment and its reference, from this lane's logits
+template <bool COLD>
 __device__ __forceinline__ double segment_sum(const float (&x)[RUN], double scale, const double* roots, double& ref) {
     float top = x[0];
 #pragma unroll
@@ -201,15 +210,15 @@ __device__ __forceinline__ double segment_sum(const float (&x)[RUN], double scal
     top = warp_max(top);
     // NaN and infinity are kept apart from all numbers: a reference that no number gives
     ref = top < INFINITY ? ceil(__dmul_rn((double)top, scale)) : INFINITY;
-    return warp_sum(sum_of(x, scale, ref, roots));
+    return warp_sum(sum_of<COLD>(x, scale, ref, roots));
 }
 
 // seg[] from the segments' own weights and references: the weights with the row's reference (not divided by the sum).  A token ends at 2^-1000 of that
 // reference (see pow2), a segment's weight does not: what is below FAR is weighed again token by token, so that a segment has weight exactly where
 // a token of it has.  Above FAR the tokens that end are 2^-60 of their segment.
 constexpr double FAR = -940.0;
-template <typename W, typename R>
-__device__ void row_weights(Team& m, const Dist& p, W weight_of, R ref_of) {
+template <bool COLD, typename W, typename R>
+__device__ void row_weights(Team& m, const Dist<COLD>& p, W weight_of, R ref_of) {
     bool far = false;
     for (int g = threadIdx.x; g < m.segs; g += THREADS) {
         const double d = ref_of(g) - p.ref, w = weight_of(g) * pow2_whole(d);
@@ -222,7 +231,7 @@ __device__ void row_weights(Team& m, const Dist& p, W weight_of, R ref_of) {
         if (!(m.seg[g] > 0.0 && ref_of(g) - p.ref < FAR)) continue;
         float x[RUN];
         m.load(p.row, m.first_of(m.seg0 + g), x);
-        const double sum = warp_sum(sum_of(x, p.scale, p.ref, p.roots));
+        const double sum = warp_sum(sum_of<COLD>(x, p.scale, p.ref, p.roots));
         if (m.lane == 0) m.seg[g] = sum;
     }
     __syncthreads();
@@ -230,7 +239,8 @@ __device__ void row_weights(Team& m, const Dist& p, W weight_of, R ref_of) {
 
 // Reference and sum of a row p and, if q.row is given, of a second one.  seg[] is left with p's weights (not divided by the sum),
 // share[] has every CTA's part of p's sum.  -> whether a part is below FAR: then the sum of seg[] is right, share[] is not.
-__device__ bool measure(Team& m, Dist& p, Dist& q) {
+template <bool COLD>
+__device__ bool measure(Team& m, Dist<COLD>& p, Dist<COLD>& q) {
     bool far = false;
     const int n = q.row ? 2 : 1;
     double ref[2] = {-INFINITY, -INFINITY}, all[2] = {0.0, 0.0};
@@ -243,7 +253,7 @@ __device__ bool measure(Team& m, Dist& p, Dist& q) {
         for (int i = 0; i < 2; ++i) {
             if (i == 1 && n == 1) break;
             double r;
-            const double sum = segment_sum(x[i], i ? q.scale : p.scale, p.roots, r);
+            const double sum = segment_sum<COLD>(x[i], i ? q.scale : p.scale, p.roots, r);
             if (i == 0 && m.lane == 0) { m.seg[g] = sum; m.seg[m.segs + g] = r; }
             const double both = fmax(ref[i], r);
             all[i] = all[i] * pow2_whole(ref[i] - both) + sum * pow2_whole(r - both);
@@ -272,7 +282,7 @@ __device__ bool measure(Team& m, Dist& p, Dist& q) {
         if (i == 0 && threadIdx.x < (unsigned)m.size) m.s->share[threadIdx.x] = sum;
 #pragma unroll
         for (int o = 1; o < MAX_CLUSTER; o <<= 1) sum += __shfl_xor_sync(0xffffffffu, sum, o);
-        Dist& d = i ? q : p;
+        Dist<COLD>& d = i ? q : p;
         d.ref = both;
         d.inv_sum = 1.0 / sum;
         d.ok = both > -INFINITY && both < INFINITY && sum < INFINITY;
@@ -285,7 +295,8 @@ __device__ bool measure(Team& m, Dist& p, Dist& q) {
 // share[] -> the total; of Q the sum without these tokens -> rest.  Both are sums over what is left: 1 - Q(rejected) has no right digit where a
 // rejected token holds all but 1e-16 of Q.  keep (or null): room for P and Q of the own segments, which `kept` says are there from the
 // rejection before.
-__device__ double total_left(Team& m, const Dist& p, const Dist& q, double beta, int n, double2* keep, bool kept, double& rest) {
+template <bool COLD>
+__device__ double total_left(Team& m, const Dist<COLD>& p, const Dist<COLD>& q, double beta, int n, double2* keep, bool kept, double& rest) {
     double all = 0.0, all_q = 0.0;
 #pragma unroll 1
     for (int g = m.warp; g < m.segs; g += WARPS) {
@@ -413,7 +424,8 @@ __device__ __forceinline__ void without(double (&w)[RUN], int t0, const int32_t*
 }
 
 // seg[] after measure(), without the tokens gone[0 .. n)
-__device__ void weigh_again(Team& m, const Dist& p, int n) {
+template <bool COLD>
+__device__ void weigh_again(Team& m, const Dist<COLD>& p, int n) {
     __syncthreads();
 #pragma unroll 1
     for (int i = m.warp; i < n; i += WARPS) {
@@ -447,7 +459,8 @@ __device__ double total_again(Team& m) {
 }
 
 // Reference and sum of one row (or two) whose segments k_row_segments has weighed: every CTA for itself.
-__device__ void collect(Team& m, int n_segs, const double2* sp, const double2* sq, Dist& p, Dist& q) {
+template <bool COLD>
+__device__ void collect(Team& m, int n_segs, const double2* sp, const double2* sq, Dist<COLD>& p, Dist<COLD>& q) {
     const int n = q.row ? 2 : 1;
     double ref[2] = {-INFINITY, -INFINITY}, sum[2] = {0.0, 0.0};
     for (int g = threadIdx.x; g < n_segs; g += THREADS) {
@@ -477,7 +490,7 @@ __device__ void collect(Team& m, int n_segs, const double2* sp, const double2* s
         all *= pow2_whole(r - both);
 #pragma unroll
         for (int o = 1; o < WARPS; o <<= 1) all += __shfl_xor_sync(0xffffffffu, all, o);
-        Dist& d = i ? q : p;
+        Dist<COLD>& d = i ? q : p;
         d.ref = both;
         d.inv_sum = 1.0 / all;
         d.ok = both > -INFINITY && both < INFINITY && all < INFINITY;
@@ -492,14 +505,14 @@ __device__ __forceinline__ double unit(float u) { return (double)fminf(fmaxf(u, 
 // is one segment's logits.
 // HELD: CTAs to a SM.  Four hide more of each other's latencies (1000 rows of 32000, 4 draws each: 73 us against 85), three leave registers for
 // a shorter chain of a draw (5 rows 11.8 us against 13.0, 320 rows 33.7 against 34.8): four from where there are rows for four.
-template <int HELD>
+template <int HELD, bool COLD>
 __global__ void __launch_bounds__(THREADS, HELD) k_draft_sample(const float* __restrict__ logits, int vocab, bool wide, int cluster, double scale, int draws,
                                                           const float* __restrict__ uniforms, int32_t* __restrict__ cand, int* status) {
     extern __shared__ __align__(16) double weights[];
     __shared__ Shared sm;
     Team m(&sm, weights, vocab, wide, cluster);
     const int row = blockIdx.x / cluster;
-    Dist p{logits + (size_t)row * vocab, scale, 0.0, 1.0, false, sm.roots}, none{};
+    Dist<COLD> p{logits + (size_t)row * vocab, scale, 0.0, 1.0, false, sm.roots}, none{};
     measure(m, p, none);
     if (cluster > 1) {
         tc::cluster_sync_all();                                // (the first CTA's room behind its own segments is free)
@@ -556,6 +569,7 @@ __global__ void __launch_bounds__(THREADS, HELD) k_draft_sample(const float* __r
 // is nothing but rounding, P_j stays, without x.  Candidates that nobody drew have Q = 1 at themselves: P_{j+1} is P_j without x.
 // The segments' weights and references of all rows, of the targets and behind them of the drafts, a warp to a segment.  With few trees
 // the walk below knows its rows one after the other only, and most SMs would wait; weighing all rows first costs less than it saves.
+template <bool COLD>
 __global__ void __launch_bounds__(THREADS, 4) k_row_segments(const float* __restrict__ logits, const float* __restrict__ draft, int n_rows, int n_draft, int vocab, bool wide, double scale,
                                                              double draft_scale, double2* __restrict__ out) {
     __shared__ Shared sm;
@@ -568,13 +582,13 @@ __global__ void __launch_bounds__(THREADS, 4) k_row_segments(const float* __rest
         float x[RUN];
         m.load(target ? logits + (size_t)row * vocab : draft + (size_t)(row - n_rows) * vocab, m.first_of(g), x);
         double ref;
-        const double sum = segment_sum(x, target ? scale : draft_scale, sm.roots, ref);
+        const double sum = segment_sum<COLD>(x, target ? scale : draft_scale, sm.roots, ref);
         if (m.lane == 0) out[t] = make_double2(sum, ref);
     }
 }
 
 // READY: k_row_segments has run.
-template <bool READY>
+template <bool READY, bool COLD>
 __global__ void __launch_bounds__(THREADS, 2) k_accept_sampled(ghd_sampled a, int vocab, bool wide, double scale, double draft_scale, int cluster, int keep_at, const double2* __restrict__ ready,
                                                                ghd_accept_result* __restrict__ results, int* status) {
     extern __shared__ __align__(16) double weights[];
@@ -620,7 +634,7 @@ __global__ void __launch_bounds__(THREADS, 2) k_accept_sampled(ghd_sampled a, in
             record(DEV_SAMPLE_DRAFT);
             drawn = -1;
         }
-        Dist p{a.logits + (size_t)(first + node) * vocab, scale, 0.0, 1.0, false, sm.roots}, q{};
+        Dist<COLD> p{a.logits + (size_t)(first + node) * vocab, scale, 0.0, 1.0, false, sm.roots}, q{};
         if (any && drawn >= 0) { q.row = a.draft_logits + (size_t)drawn * vocab; q.scale = draft_scale; q.roots = sm.roots; }
         // the children's logits are on their way while the rows are measured
         const int mine = threadIdx.x < GHD_MAX_NODES && (sm.child[m.warp % (GHD_MAX_NODES / 32)] >> m.lane & 1) ? sm.token[threadIdx.x] : -1;
@@ -760,11 +774,12 @@ double scale_of(float temperature) { return 1.44269504088896340736 / (double)tem
 
 ghd_status raise_room(ghd_ctx* c) {              // (a CTA with all segments of the largest vocabulary takes 64 KB)
     if (c->attr_sampling) return GHD_OK;
-    if (cudaFuncSetAttribute(k_draft_sample<3>, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)room_for(MAX_VOCAB, 1)) != cudaSuccess ||
-        cudaFuncSetAttribute(k_draft_sample<4>, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)room_for(MAX_VOCAB, 1)) != cudaSuccess ||
-        cudaFuncSetAttribute(k_accept_sampled<true>, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)MAX_ROOM) != cudaSuccess ||
-        cudaFuncSetAttribute(k_accept_sampled<false>, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)MAX_ROOM) != cudaSuccess)
-        return check_cuda(c, "sampling: shared memory");
+    const void* drafts[] = {(const void*)k_draft_sample<3, false>, (const void*)k_draft_sample<4, false>, (const void*)k_draft_sample<4, true>};
+    const void* walks[] = {(const void*)k_accept_sampled<true, false>, (const void*)k_accept_sampled<false, false>, (const void*)k_accept_sampled<true, true>, (const void*)k_accept_sampled<false, true>};
+    for (const void* f : drafts)
+        if (cudaFuncSetAttribute(f, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)room_for(MAX_VOCAB, 1)) != cudaSuccess) return check_cuda(c, "sampling: shared memory");
+    for (const void* f : walks)
+        if (cudaFuncSetAttribute(f, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)MAX_ROOM) != cudaSuccess) return check_cuda(c, "sampling: shared memory");
     c->attr_sampling = true;
     return GHD_OK;
 }
@@ -791,7 +806,9 @@ ghd_status ghd_draft_sample(ghd_ctx* c, const float* logits, int32_t n_rows, flo
     const int k = cluster_for(c, n_rows, c->cfg.vocab, many ? 4 : 3);
     ghd_status s = raise_room(c);
     if (s != GHD_OK) return s;
-    launch_kc(c, false, k, many ? k_draft_sample<4> : k_draft_sample<3>, n_rows * k, THREADS, room_for(c->cfg.vocab, k), logits, c->cfg.vocab, wide_rows(c, logits), k, scale_of(temperature), n_draws, uniforms, cand, c->input_status);
+    const double scale = scale_of(temperature);
+    launch_kc(c, false, k, scale > COLD_SCALE ? k_draft_sample<4, true> : many ? k_draft_sample<4, false> : k_draft_sample<3, false>, n_rows * k, THREADS, room_for(c->cfg.vocab, k), logits, c->cfg.vocab,
+              wide_rows(c, logits), k, scale, n_draws, uniforms, cand, c->input_status);
     return check_cuda(c, "draft_sample");
 }
 
@@ -819,14 +836,15 @@ ghd_status ghd_accept_sampled(ghd_ctx* c, const ghd_sampled* a, ghd_accept_resul
     const bool keep = a->draft_row && room + keeps <= MAX_ROOM;
     const int keep_at = keep ? (int)(room / sizeof(double)) : 0;
     const bool wide = wide_rows(c, a->logits) && wide_rows(c, a->draft_logits);
+    const bool cold = scale > COLD_SCALE || draft_scale > COLD_SCALE;
     const int64_t segs = ((int64_t)a->n_rows + (a->draft_row ? a->n_draft : 0)) * ((c->cfg.vocab + SEG - 1) / SEG);
     if (segs > 0 && segs <= SAMPLE_SEGS) {
         const int64_t most = 4 * c->sm_count, ctas = (segs + WARPS - 1) / WARPS;
-        launch_k(c, false, k_row_segments, (int)(ctas < most ? ctas : most), THREADS, 0, a->logits, a->draft_logits, a->n_rows, a->draft_row ? a->n_draft : 0, c->cfg.vocab, wide, scale, draft_scale,
+        launch_k(c, false, cold ? k_row_segments<true> : k_row_segments<false>, (int)(ctas < most ? ctas : most), THREADS, 0, a->logits, a->draft_logits, a->n_rows, a->draft_row ? a->n_draft : 0, c->cfg.vocab, wide, scale, draft_scale,
                  (double2*)c->sample_segs);
-        launch_kc(c, true, k, k_accept_sampled<true>, a->n_seqs * k, THREADS, room + (keep ? keeps : 0), *a, c->cfg.vocab, wide, scale, draft_scale, k, keep_at, (const double2*)c->sample_segs, results_dev, c->input_status);
+        launch_kc(c, true, k, cold ? k_accept_sampled<true, true> : k_accept_sampled<true, false>, a->n_seqs * k, THREADS, room + (keep ? keeps : 0), *a, c->cfg.vocab, wide, scale, draft_scale, k, keep_at, (const double2*)c->sample_segs, results_dev, c->input_status);
     } else {
-        launch_kc(c, false, k, k_accept_sampled<false>, a->n_seqs * k, THREADS, room + (keep ? keeps : 0), *a, c->cfg.vocab, wide, scale, draft_scale, k, keep_at, (const double2*)nullptr, results_dev, c->input_status);
+        launch_kc(c, false, k, cold ? k_accept_sampled<false, true> : k_accept_sampled<false, false>, a->n_seqs * k, THREADS, room + (keep ? keeps : 0), *a, c->cfg.vocab, wide, scale, draft_scale, k, keep_at, (const double2*)nullptr, results_dev, c->input_status);
     }
     return check_cuda(c, "accept_sampled");
 }

@@ -634,3 +634,43 @@ def test_tokens_at_the_end_of_64_bits(ghd, below, V, top):
             for i in range(seqs):
                 assert res[i, 258] == osam.first_over(osam.distribution(held(logits[i], temp), temp), u0), (i, u0)
     ghd.ghd_sync_status(ctx)
+
+
+@pytest.mark.parametrize("temp", [2.0 ** -149, 2.0 ** -140, 1e-38, 1e-36, 1e-30])
+def test_smallest_temperatures(ghd, temp):
+    """Zeros of both signs are equal and numbers below 2^-126 are what they are, whatever the temperature divides them by."""
+    V = 600
+    ctx = ctx_for(ghd, V)
+    r = np.random.RandomState(35)
+    x = np.full((5, V), -np.inf)
+    x[0, :] = np.where(r.rand(V) < 0.5, 0.0, -0.0)
+    x[1, :] = -1e-3
+    x[1, r.choice(V, 9, replace=False)] = [0.0, -0.0, 0.0, -0.0, 0.0, -0.0, 0.0, -0.0, 0.0]
+    x[2, :] = -np.abs(r.randn(V)) * 3 * temp                                 # (rounded to the numbers that there are)
+    x[3, :] = r.randn(V) * 3 * temp
+    x[4, [3, 300, 599]] = [0.0, temp, 2 * temp]
+    logits, u = x.astype(np.float32), r.rand(5, 16).astype(np.float32)
+    got = ghd.ghd_draft_sample(ctx, dev(logits), dev(u), 8, temp).cpu().numpy()
+    one = np.full(5, -1, np.int32)
+    rows = ghd.SampledRows(dev(one), dev(one), dev(logits), dev(u[:, 9].copy()), row_start=dev(np.arange(6, dtype=np.int32)), temperature=temp)
+    res = ghd.ghd_accept_sampled(ctx, rows).cpu().numpy()
+    ghd.ghd_sync_status(ctx)
+    for i in range(5):
+        assert np.array_equal(got[i], osam.draw(logits[i], temp, 8, u[i])), i
+        assert res[i, 258] == osam.first_over(osam.distribution(logits[i], temp), u[i, 9]), i
+
+
+def test_verify_at_the_smallest_temperatures(ghd):
+    """Trees whose logits and temperatures are both about 1e-37, below 2^-126 in part; in both ways through the call."""
+    import torch
+    V, temp = 700, float(np.float32(1e-37))
+    ctx = ctx_for(ghd, V)
+    for drawn in (True, False):
+        b = Batch(np.random.RandomState(36), [20] * 8, V, 1.0, drawn)
+        b.logits, b.draft, b.temp = (b.logits * temp).astype(np.float32), (b.draft * temp).astype(np.float32), temp
+        assert (np.abs(b.logits) < 2.0 ** -126).any() and (np.abs(b.logits) > 2.0 ** -126).any()
+        b.check(ghd.ghd_accept_sampled(ctx, b.rows(ghd)).cpu().numpy())
+        if drawn:
+            many = torch.cat((dev(b.draft), torch.zeros(49152, V, device="cuda")))
+            b.check(ghd.ghd_accept_sampled(ctx, b.rows(ghd, draft_logits=many)).cpu().numpy())
+    ghd.ghd_sync_status(ctx)
