@@ -136,7 +136,22 @@ __device__ __forceinline__ float4 ld_cluster(uint32_t addr) {
     asm volatile("ld.shared::cluster.v4.f32 {%0, %1, %2, %3}, [%4];" : "=f"(v.x), "=f"(v.y), "=f"(v.z), "=f"(v.w) : "r"(addr) : "memory");
     return v;
 }
-__device__ __forceinline__ float silu_times(float g, float up) { return __fdividef(g * up, 1.f + exp2f(-1.4426950408889634f * g)); }
+// SiLU(g) * up = g s^2 up / (1 + s^2) with s = e^(g/2) for g < 0, g up / (1 + s^2) with s = e^(-g/2) otherwise.  Both sums can have any exponent, so nothing
+// on the way may leave the type's range where the result does not: g * up may, and so may e^-g.  Halves (11 bits) take the faster exponential.
+// Floats take the plain form, rounded four times, down to DEEP, where 1 + e^-g is e^-g to the last bit; below it up is multiplied by e^(g/4)
+// four times (s itself would run out of bits at -174).
+// (g * up / (1 + e^-g) before: 64 rows by 11008 x 4096 23.9 us against 24.4 in halves, 28.7 against 29.4 in floats.)
+constexpr float DEEP = -80.f;
+template <typename T> __device__ __forceinline__ float silu_times(float g, float up);
+template <> __device__ __forceinline__ float silu_times<__half>(float g, float up) {
+    const float s = __expf(-0.5f * fabsf(g)), c = g < 0.f ? s : 1.f;
+    return g * c * up * __fdividef(c, fmaf(s, s, 1.f));
+}
+template <> __device__ __forceinline__ float silu_times<float>(float g, float up) { return __fdividef(g, 1.f + expf(-g)) * up; }
+__device__ __forceinline__ float silu_times_deep(float g, float up) {
+    const float t = expf(0.25f * g);
+    return g * t * up * t * t * t;
+}
 
 // ---------------------------------------------------------------- x -> terms
 template <typename T> constexpr int TERMS = sizeof(T) == 2 ? 3 : 5;
@@ -518,9 +533,20 @@ k_mx4_gemm(const __grid_constant__ Mx4Maps maps, const Mx4Params p) {
                     for (int e = 0; e < NODES; ++e)
                         if (e < mine && f < p.m) {
                             const size_t at = (size_t)(g * p.per_group + j0 + e) * p.m + f;
-                            if constexpr (GATE) u[at] = from_f<T>(silu_times(acc[0][e], acc[1][e]));
+                            if constexpr (GATE) u[at] = from_f<T>(silu_times<T>(acc[0][e], acc[1][e]));
                             else y[at] = acc[t][e];
                         }
+                }
+                if constexpr (GATE && P == 5) {
+                    // (apart, and hardly ever run)
+                    bool deep = false;
+#pragma unroll
+                    for (int e = 0; e < NODES; ++e) deep |= e < mine && acc[0][e] < DEEP;
+                    const int f = ru * TILE + row;
+                    if (deep && f < p.m)
+#pragma unroll
+                        for (int e = 0; e < NODES; ++e)
+                            if (e < mine && acc[0][e] < DEEP) u[(size_t)(g * p.per_group + j0 + e) * p.m + f] = from_f<T>(silu_times_deep(acc[0][e], acc[1][e]));
                 }
             }
             i += end - first;
@@ -560,7 +586,7 @@ k_mx4_gemm(const __grid_constant__ Mx4Maps maps, const Mx4Params p) {
                 const float up[4] = {sum[GATE ? 1 : 0].x, sum[GATE ? 1 : 0].y, sum[GATE ? 1 : 0].z, sum[GATE ? 1 : 0].w};
 #pragma unroll
                 for (int e = 0; e < 4; ++e)
-                    if (f + e < p.m) ((T*)p.out)[at + e] = from_f<T>(silu_times(s[e], up[e]));
+                    if (f + e < p.m) ((T*)p.out)[at + e] = from_f<T>(P == 5 && s[e] < DEEP ? silu_times_deep(s[e], up[e]) : silu_times<T>(s[e], up[e]));
             } else {
 #pragma unroll
                 for (int e = 0; e < 4; ++e)

@@ -388,3 +388,45 @@ def test_refusals(ghd):
     assert ctx.lib.ghd_mx4_linear(ctx.handle, x.data_ptr(), 100, w.ref, 16, x.data_ptr()) == 1          # ld < k
     assert ctx.lib.ghd_mx4_linear(ctx.handle, x.data_ptr() + 1, 0, w.ref, 16, x.data_ptr()) == 1
     ghd.ghd_sync_status(ctx)
+
+
+def picked(cols, k, scale):
+    """A matrix whose row i has `scale` (a power of two) in column cols[i] and nothing else -> codes, scale bytes."""
+    w = np.zeros((len(cols), k))
+    w[np.arange(len(cols)), cols] = scale
+    return omx.quantise(w)
+
+
+@pytest.mark.parametrize("dtype", ["f16", "f32"])
+def test_gate_up_far_from_zero(ghd, dtype):
+    """Strongly negative and positive gates next to large and small up values: finite, and as exact as the functions are."""
+    gates = np.array([-3e4, -1000, -206.5, -180.25, -120, -95.5, -89, -88, -87.25, -81, -80, -79.875, -50, -30, -20, -8, -2, -0.5, 0, 0.5, 3, 20, 89, 200], np.float32)
+    ups = np.array([1.0, -1.0, 3.0], np.float32)
+    n, k = len(gates) * len(ups), 64
+    x = np.zeros((n, k), np_t(dtype))
+    x[:, 0], x[:, 32] = np.repeat(gates, len(ups)), np.tile(ups, len(gates))          # (32 apart: neither is small next to the other)
+    ctx = make_ctx(ghd, dtype, k, n)
+    m, worst = 5, 0.0
+    wide = [(1.0, 2.0 ** 125), (1.0, 2.0 ** 60), (1.0, 1.0), (1.0, 2.0 ** -30)]
+    if dtype == "f32":
+        wide += [(2.0 ** 60, 2.0 ** 60), (2.0 ** 100, 2.0 ** -100)]
+    for a, b in wide:
+        (gc, gs), (uc, us) = picked([0] * m, k, a), picked([32] * m, k, b)
+        u = ghd.ghd_mx4_gate_up(ctx, dev(x), ghd.Mx4(dev(gc), dev(gs), m, k), ghd.Mx4(dev(uc), dev(us), m, k)).cpu().numpy().astype(np.float64)
+        g, up = x[:, 0].astype(np.float64) * a, x[:, 32].astype(np.float64) * b
+        with np.errstate(over="ignore"):
+            want = (g / (1 + np.exp(-g)) * up)[:, None] + np.zeros((n, m))
+        big = 65504.0 if dtype == "f16" else float(np.finfo(np.float32).max)
+        fine = np.abs(want) < big
+        assert np.array_equal(u[~fine], np.where(want > 0, np.inf, -np.inf)[~fine])
+        # Both sums are exact here.  Above -80: the exponential of a float (one unit, 2^-23), a sum, a quotient and a product (2^-24 each).  Below,
+        # 1 + e^-g is e^-g: four factors of the exponential of g / 4 and five products.  At the end half a step of the output, and of its smallest numbers
+        # (which the products before the last pass as well).
+        # (half: its exponential is exp2's, whose argument -1.44 g is rounded: |g| 2^-23 besides, and a quotient of 2 units)
+        err = 14 * 2.0 ** -24 + (2.0 ** -23 * np.abs(np.clip(g, -80, 80))[:, None] + 2.0 ** -22 if dtype == "f16" else 0.0)
+        half, least = (2.0 ** -11, 2.0 ** -24) if dtype == "f16" else (2.0 ** -24, 2.0 ** -149)
+        bound = np.abs(want) * (err + half) + 4 * least
+        assert np.isfinite(u[fine]).all() and (np.abs(u - want)[fine] <= bound[fine]).all(), (a, b, (np.abs(u - want) / bound)[fine].max())
+        worst = max(worst, float((np.abs(u - want) / bound)[fine].max()))
+    ghd.ghd_sync_status(ctx)
+    assert worst <= 1
