@@ -14,9 +14,11 @@
 // it, with its own sums in registers, as the last of its range; the others have come to it first and left their sums in the workspace (a
 // bounded wait makes sure; every CTA is resident).  Both add in the order of k.
 //
-// The tensor cores cut off what they add below 2^-24 of the running sum, so that long sums lose more than rounded ones (relative error of 4096 terms: 4e-8 for
-// normal weights, 1.3e-6 for scales that differ by 2^20, measured):
-// accumulators are taken out every CHUNK k-steps and added up in registers with rounding.
+// The tensor cores cut off a little of each sum they add to, so that long sums of one sign lose more than rounded ones, the more the longer: accumulators
+// are taken out every CHUNK k-steps and added up in registers with rounding.  Relative error of the norm, sums of 4096 to 14336 elements of one sign, for
+// CHUNK 8 / 16 / 32 / 64: 5e-8 / 7e-8 / 1.4e-7 / 1.4e-7 to 3.8e-7; of both signs 4e-8 to 7e-8 with each; a plain float product 5e-7 to 1.6e-6.
+// Time: gate and up of 256 rows by 13824 x 5120 97 / 93 / 91 / 90 us (floats 157 / 151 / 147 / 145), of 64 rows by 11008 x 4096
+// 26.6 / 25.6 / 24.6 / 24.6 (31.5 / 30.1 / 29.4 / 29.4).  16 where five terms hold a float's 24 bits, 32 for halves.
 //
 // What bounds it: with up to 16 rows the memory (16 rows by 32000 x 4096: 20 us of which 11 are streaming at 345 cycles a k-step, the rest
 // set-up and the last unit's end; 68 MB of weights), with 64 and more the MMAs (a stage of eight of 128 x 192 x 32 takes 806 cycles of 768: gate and up of
@@ -41,7 +43,6 @@ using namespace tc;
 constexpr int THREADS = 384;            // weights' loads, MMAs, eight epilogue warps, x's loads, weights to the L2
 constexpr int AHEAD = 32 * 1024;        // bytes of weights that a CTA has asked the L2 for beyond its loads (192 KB: 2 us more for 16 rows of an lm_head, whose first loads wait)
 constexpr int MAX_STAGES = 10;
-constexpr int CHUNK = 64;               // k-steps of 128 that one accumulator takes
 constexpr int MAX_WORKERS = 1024;       // CTAs at most: each has an arrival counter
 constexpr int MAX_SPLIT = 8;            // CTAs of a cluster
 constexpr int A_BYTES = TILE * TILE;    // a tile of 4-bit elements in shared memory, a byte each
@@ -155,6 +156,7 @@ __device__ __forceinline__ float silu_times_deep(float g, float up) {
 
 // ---------------------------------------------------------------- x -> terms
 template <typename T> constexpr int TERMS = sizeof(T) == 2 ? 3 : 5;
+template <int P> constexpr int CHUNK = P == 3 ? 32 : 16;                          // k-steps of 128 that one accumulator takes
 template <typename T> constexpr int GROUP = sizeof(T) == 2 ? 64 : 32;             // rows of x that one pass over w takes at most
 
 template <typename T>
@@ -402,7 +404,7 @@ k_mx4_gemm(const __grid_constant__ Mx4Maps maps, const Mx4Params p) {
             return ok;
         };
         for (int left = my_iters, kc = kc0, chunk = 0; left > 0; ++chunk) {
-            const int take = min(min(p.kt - kc, left), CHUNK);
+            const int take = min(min(p.kt - kc, left), CHUNK<P>);
             if (chunk > 0 && !wait(smem_u32(&sm->acc_empty), (chunk - 1) & 1, DEV_TIMEOUT_TMEM)) break;
             for (int k = take; k > 0; k -= KS) {
                 if (!wait(smem_u32(&sm->full[stage]), phase, DEV_TIMEOUT_MMA)) break;
@@ -454,7 +456,7 @@ k_mx4_gemm(const __grid_constant__ Mx4Maps maps, const Mx4Params p) {
         for (int i = 0; i < my_iters && ok;) {
             const int first = kc, end = min(p.kt, kc + my_iters - i), g = unit % p.groups, ru = unit / p.groups;
             const int rows_here = min(p.per_group, p.n - g * p.per_group), mine = max(0, min(half, rows_here - j0));
-            for (int c = first; c < end && ok; c += CHUNK) {
+            for (int c = first; c < end && ok; c += CHUNK<P>) {
                 const bool fresh = c == first;
                 // (one warp asks the barrier: eight of them asking took a third of the MMA warp's issue slots)
                 ok = epi_all(warp != 2 || mbar_wait(smem_u32(&sm->acc_full), chunks & 1, abort_flag, p.status, DEV_TIMEOUT_EPI));

@@ -430,3 +430,26 @@ def test_gate_up_far_from_zero(ghd, dtype):
         worst = max(worst, float((np.abs(u - want) / bound)[fine].max()))
     ghd.ghd_sync_status(ctx)
     assert worst <= 1
+
+
+@pytest.mark.parametrize("dtype", ["f16", "f32"])
+@pytest.mark.parametrize("k", [4096, 8192, 14336])
+@pytest.mark.parametrize("signs", [1, 2])
+def test_long_sums_lose_little(ghd, dtype, k, signs):
+    """Relative error of the norm over outputs whose whole sum one CTA works out.  An accumulator takes 4 x 32 (halves) or 4 x 16 (floats) sums
+    of 32 products; the running sum is half of the last one on average, and an addition cuts off up to some 2^-28.5 of it on average: for one sign
+    64 (32) x 2^-28.5 = 2^-22.5 (2^-23.5).  Besides, each is rounded, half a unit at most, without a sign.  The bound does not depend on k.
+    For both signs the running sums are short and the cuts have no sign.  (Without x's last term it is above 2^-21.5 in floats.)"""
+    import torch
+    n, m = 16, 19000
+    g = torch.Generator(device="cuda")
+    g.manual_seed(k + signs)
+    ctx = make_ctx(ghd, dtype, k, n)
+    w, x = torch.randn(m, k, generator=g, device="cuda") * 0.05, torch.randn(n, k, generator=g, device="cuda")
+    if signs == 1:
+        w, x = w.abs(), x.abs()
+    held, x = ghd.ghd_mx4_quantize(ctx, w.to(ctx.dtype)), x.to(ctx.dtype)
+    want = x.double() @ ghd.ghd_mx4_read(ctx, held).double().T
+    err = float((ghd.ghd_mx4_linear(ctx, x, held).double() - want).norm() / want.norm())
+    ghd.ghd_sync_status(ctx)
+    assert err <= (2.0 ** -23 if signs == 2 or dtype == "f32" else 2.0 ** -22)

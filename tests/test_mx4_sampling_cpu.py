@@ -123,3 +123,20 @@ def test_descriptions_have_the_header_layout():
     from paper_2505_23219_b200 import binding
     assert C.sizeof(binding._Mx4) == 24 and binding._Mx4.codes.offset == 8
     assert C.sizeof(binding._Sampled) == 80 and binding._Sampled.n_draft.offset == 64 and binding._Sampled.draft_temperature.offset == 72
+
+
+@pytest.mark.parametrize("bits,terms", [(11, 3), (24, 5)])
+def test_terms_hold_every_bit_and_the_last_one_is_needed(bits, terms):
+    """x as a sum of e4m3 numbers, each with 2^5 times what the ones before it left: what the product makes of rows of halves and floats.  One term
+    less shows in the norm of a long sum (2^-23 is what the tests of the product allow there)."""
+    import torch
+    r = np.random.RandomState(bits)
+    x = torch.from_numpy(r.randn(128, 32).astype(np.float16 if bits == 11 else np.float32)).double()
+    top = torch.floor(torch.log2(x.abs().amax(1, keepdim=True)))
+    left, held, after = x * 2.0 ** (7 - top), torch.zeros_like(x), []
+    for p in range(terms):
+        t = left.float().clamp(-448, 448).to(torch.float8_e4m3fn).double()
+        held, left = held + t * 2.0 ** (top - 7 - 5 * p), (left - t) * 32
+        after.append(float((held - x).norm() / x.norm()))
+    assert ((held - x).abs() <= 2.0 ** (top + 1) * 2.0 ** (-27 if bits == 11 else -37)).all()
+    assert after[-2] > 2.0 ** -21.5
