@@ -273,8 +273,9 @@ typedef struct ghd_medusa_weights {
  * result_dev->nodes[n_matched] (read on the device) and writes, for head k, its topk_host[k] best token ids
  * to cand_dev[k * GHD_MAX_TOPK ..] (int32, best first; unused entries -1).  logits_dev: float
  * [n_heads][vocab] or NULL.  Must follow ghd_verify_step on the same context and stream with nothing of this
- * library in between except ghd_accept / ghd_kv_commit.  GHD_EINVAL: null pointer, n_heads or a top-k out of
- * range. */
+ * library in between except ghd_accept, ghd_accept_sampled, ghd_draft_sample, ghd_kv_commit and the calls with
+ * 4-bit matrices (ghd_mx4_*).  Its logits are what ghd_draft_sample draws candidates from.  GHD_EINVAL: null
+ * pointer, n_heads or a top-k out of range. */
 ghd_status ghd_medusa_draft(ghd_ctx *ctx, const ghd_medusa_weights *w, const ghd_accept_result *result_dev,
                             const int32_t *topk_host, int32_t *cand_dev, float *logits_dev);
 

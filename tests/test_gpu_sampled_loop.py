@@ -116,3 +116,64 @@ def test_oracle_is_the_one_of_greedy_acceptance_when_cold(ghd):
         assert greedy[0] >= m and list(cold[258:259 + m]) == [amax[x] for x in cold[2:3 + m]]
         want = oracle.accept(parent, tokens, amax)
         assert want[0] == greedy[0] == m
+
+
+def test_decode_loop_of_the_drafting_heads(ghd):
+    """Step, sampled acceptance, commit, the framework's own heads, draws from their logits, next tree.  What is allowed between the step and the heads
+    (acceptance, draws, products with 4-bit matrices) leaves the heads' input alone: a second context does the step and the heads only."""
+    import torch
+    n, L, steps, K = len(PARENT), 40, 4, 3
+    level, rank, seen = [0] * n, [0] * n, {}
+    for i in range(1, n):
+        level[i], rank[i] = level[PARENT[i]] + 1, seen.get(PARENT[i], 0)
+        seen[PARENT[i]] = rank[i] + 1
+    Lmax = L + n * (steps + 1)
+    head = wl.head_weights(SHAPE, 7)
+    head["lm_head"] = (head["lm_head"].astype(np.float32) * 6).astype(np.float16)
+    r = np.random.RandomState(18)
+    weights = ghd.ModelWeights(dev(head["embed"]), [ghd.LayerWeights(**{k: dev(w[k]) for k in ghd.LayerWeights.FIELDS}) for w in
+                               (wl.layer_weights(SHAPE, 7, l) for l in range(SHAPE.n_layers))], dev(head["rms_final"]), dev(head["lm_head"]))
+    heads = ghd.MedusaWeights(dev((r.randn(K, 512, 512) * 0.01).astype(np.float16)), dev(np.tile(head["lm_head"], (K, 1, 1))))
+    held = ghd.ghd_mx4_quantize(ghd.ghd_create(ghd.ModelCfg(512, 4, 128, 512, 100, 1, 512, 16, "f16")), weights.lm_head)
+    caches = [wl.kv_cache(SHAPE, 7, l, L, Lmax) for l in range(SHAPE.n_layers)]
+    both = []
+    for _ in range(2):
+        ctx = ghd.ghd_create(ghd.ModelCfg(SHAPE.d_model, SHAPE.n_heads, SHAPE.d_head, SHAPE.d_ffn, SHAPE.vocab, SHAPE.n_layers, Lmax, 16, "f16", SHAPE.rms_eps, SHAPE.rope_theta))
+        ghd.ghd_kv_len_set(ctx, L)
+        both.append([ctx, [ghd.KvLayer(dev(k), dev(v), ghd.KV_LEN_DEVICE) for k, v in caches], ghd.ghd_tree_build(ctx, PARENT, ghd.KV_LEN_DEVICE)])
+    (ctx, kvs, tree), (ctx2, kvs2, tree2) = both
+    lv, rk = dev(np.array(level, np.int32)), dev(np.array(rank, np.int32))
+    drow = dev(np.array([l if l < K else -1 for l in level], np.int32))
+    tokens = dev(wl.draft_tokens(PARENT, SHAPE.vocab, 9).astype(np.int32))
+    draft = draft_row = None
+    x = torch.randn(16, 512, device="cuda").half()
+    for step in range(steps):
+        logits, _ = ghd.ghd_verify_step(ctx, weights, kvs, tree, tokens)
+        u = torch.rand(n, device="cuda")
+        more = {} if draft is None else dict(draft_row=draft_row, draft_logits=draft, draft_temperature=DRAFT_TEMP)
+        res = ghd.ghd_accept_sampled(ctx, ghd.SampledRows(tree.parent[:n], tokens, logits, u, temperature=TEMP, **more))
+        nodes, toks = osam.verify(PARENT, tokens.cpu().numpy(), logits.cpu().numpy(), u.cpu().numpy(), TEMP, None if draft is None else draft_row.cpu().numpy(),
+                                  None if draft is None else draft.cpu().numpy(), DRAFT_TEMP)
+        got = res[0].cpu().numpy()
+        assert got[0] == len(nodes) - 1 and list(got[2:2 + len(nodes)]) == nodes and list(got[258:258 + len(toks)]) == toks
+        ghd.ghd_mx4_linear(ctx, x, held)
+        ghd.ghd_mx4_gate_up(ctx, x, held, held)
+        ghd.ghd_draft_sample(ctx, logits, torch.rand(n, 16, device="cuda"), 5)
+        ghd.ghd_kv_commit(ctx, kvs, ghd.KV_LEN_DEVICE, res[0])
+        _, draft = ghd.ghd_medusa_draft(ctx, heads, res[0], [1] * K, want_logits=True)
+        logits2, _ = ghd.ghd_verify_step(ctx2, weights, kvs2, tree2, tokens)
+        _, draft2 = ghd.ghd_medusa_draft(ctx2, heads, res[0], [1] * K, want_logits=True)
+        ghd.ghd_kv_commit(ctx2, kvs2, ghd.KV_LEN_DEVICE, res[0])
+        assert torch.equal(logits, logits2) and torch.equal(draft, draft2)
+        uc = torch.rand(K, 16, device="cuda")
+        cand = ghd.ghd_draft_sample(ctx, draft, uc, 3, DRAFT_TEMP)
+        for k in range(K):
+            assert np.array_equal(cand[k].cpu().numpy(), osam.draw(draft[k].cpu().numpy(), DRAFT_TEMP, 3, uc[k].cpu().numpy()))
+        full = torch.zeros(max(level) + 1, 16, dtype=torch.int32, device="cuda")
+        full[:K] = cand
+        tokens = ghd.ghd_tree_fill_tokens(ctx, full, res[0], lv, rk)
+        assert int(tokens[0]) == toks[-1]
+        draft_row = drow
+        tree, tree2 = ghd.ghd_tree_build(ctx, PARENT, ghd.KV_LEN_DEVICE, tree), ghd.ghd_tree_build(ctx2, PARENT, ghd.KV_LEN_DEVICE, tree2)
+    ghd.ghd_sync_status(ctx)
+    ghd.ghd_sync_status(ctx2)
