@@ -218,7 +218,9 @@ ghd_status ghd_verify_layer(ghd_ctx *ctx, const ghd_layer_weights *w, ghd_kv_lay
 /* The whole verify forward: embedding rows of tokens_dev[n], cfg.n_layers layers
  * (kv[l] is layer l's cache, HOST array), final RMSNorm, lm_head, row argmax
  * (first index among equal maxima).  logits_dev: float [n][vocab] or NULL (then
- * the logits live only in the workspace); argmax_dev: int32 [n]. */
+ * the logits live only in the workspace); argmax_dev: int32 [n].  A token outside
+ * [0, vocab) (a slot without a candidate) is embedded as token 0; neither
+ * acceptance takes its node unless it is the root. */
 ghd_status ghd_verify_step(ghd_ctx *ctx, const ghd_model_weights *w, ghd_kv_layer *kv, const ghd_tree *tree,
                            const int32_t *tokens_dev, float *logits_dev, int32_t *argmax_dev);
 

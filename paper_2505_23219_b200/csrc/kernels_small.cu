@@ -164,10 +164,12 @@ __global__ void k_store_x(const float* __restrict__ xres, T* __restrict__ x, siz
 }
 
 template <typename T>
-__global__ void k_embed(const T* __restrict__ table, const int32_t* __restrict__ tokens, float* __restrict__ xres, int d) {
+__global__ void k_embed(const T* __restrict__ table, const int32_t* __restrict__ tokens, float* __restrict__ xres, int d, int vocab) {
     pdl_wait();
     pdl_trigger();
-    const T* row = table + (size_t)tokens[blockIdx.x] * d;
+    // A slot without a candidate holds -1 (draws that ran out of tokens, say): its node is computed as token 0 and accepted by nobody.
+    const int t = tokens[blockIdx.x];
+    const T* row = table + (size_t)((unsigned)t < (unsigned)vocab ? t : 0) * d;
     for (int cidx = threadIdx.x; cidx < d; cidx += blockDim.x) xres[(size_t)blockIdx.x * d + cidx] = to_f32<T>(row[cidx]);
 }
 
@@ -193,8 +195,8 @@ void launch_store_x(ghd_ctx* c, void* x_out, int n) {
 }
 
 void launch_embed(ghd_ctx* c, const void* embed, const int32_t* tokens, int n) {
-    GHD_DISPATCH_T(c, launch_k(c, true, k_embed<float>, n, 256, 0, (const float*)embed, tokens, c->xres, c->cfg.d_model),
-                   launch_k(c, true, k_embed<__half>, n, 256, 0, (const __half*)embed, tokens, c->xres, c->cfg.d_model));
+    GHD_DISPATCH_T(c, launch_k(c, true, k_embed<float>, n, 256, 0, (const float*)embed, tokens, c->xres, c->cfg.d_model, c->cfg.vocab),
+                   launch_k(c, true, k_embed<__half>, n, 256, 0, (const __half*)embed, tokens, c->xres, c->cfg.d_model, c->cfg.vocab));
 }
 
 // ---------------------------------------------------------------- RMSNorm

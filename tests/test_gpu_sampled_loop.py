@@ -177,3 +177,49 @@ def test_decode_loop_of_the_drafting_heads(ghd):
         tree, tree2 = ghd.ghd_tree_build(ctx, PARENT, ghd.KV_LEN_DEVICE, tree), ghd.ghd_tree_build(ctx2, PARENT, ghd.KV_LEN_DEVICE, tree2)
     ghd.ghd_sync_status(ctx)
     ghd.ghd_sync_status(ctx2)
+
+
+@pytest.mark.parametrize("dtype", ["f16", "f32"])
+def test_slots_without_a_candidate(ghd, dtype):
+    """A drafter with one likely token only: its further draws are -1, and so are the tree's slots that take them.  The step works them out as token 0,
+    the other nodes do not see them, and no acceptance takes them."""
+    import torch
+    shape = wl.scaled(SHAPE, dtype=dtype)
+    n, L = len(PARENT), 30
+    head = wl.head_weights(shape, 9)
+    T = np.float16 if dtype == "f16" else np.float32
+    weights = ghd.ModelWeights(dev(head["embed"]), [ghd.LayerWeights(**{k: dev(w[k]) for k in ghd.LayerWeights.FIELDS}) for w in
+                               (wl.layer_weights(shape, 9, l) for l in range(shape.n_layers))], dev(head["rms_final"]), dev(head["lm_head"]))
+    ctx = ghd.ghd_create(ghd.ModelCfg(shape.d_model, shape.n_heads, shape.d_head, shape.d_ffn, shape.vocab, shape.n_layers, L + n, 16, dtype, shape.rms_eps, shape.rope_theta))
+    caches = [wl.kv_cache(shape, 9, l, L, L + n) for l in range(shape.n_layers)]
+    kvs = [ghd.KvLayer(dev(k.astype(T)), dev(v.astype(T)), L) for k, v in caches]
+    tree = ghd.ghd_tree_build(ctx, PARENT, L)
+    draft = torch.full((3, shape.vocab), -np.inf, device="cuda")
+    draft[0, 40], draft[1, 41], draft[2, [42, 43]] = 1.0, 2.0, 3.0
+    cand = ghd.ghd_draft_sample(ctx, draft, torch.rand(3, 16, device="cuda"), 3)
+    assert (cand[:2, 1:] == -1).all() and (cand[2, 2:] == -1).all() and (cand[:, 0] >= 40).all()
+    level, rank, seen = [0] * n, [0] * n, {}
+    for i in range(1, n):
+        level[i], rank[i] = level[PARENT[i]] + 1, seen.get(PARENT[i], 0)
+        seen[PARENT[i]] = rank[i] + 1
+    cand = torch.cat((cand, torch.full((max(level), 16), -1, dtype=torch.int32, device="cuda")))
+    res = torch.full((514,), -1, dtype=torch.int32, device="cuda")
+    res[0], res[258] = 0, 5
+    tokens = ghd.ghd_tree_fill_tokens(ctx, cand, res, dev(np.array(level, np.int32)), dev(np.array(rank, np.int32)))
+    none = [i for i in range(n) if int(tokens[i]) == -1]
+    assert none and int(tokens[1]) == 40
+    for bad in (-1, shape.vocab, 2 ** 31 - 1, -2 ** 31):
+        t = tokens.clone()
+        t[none] = bad
+        logits, amax = ghd.ghd_verify_step(ctx, weights, kvs, tree, t)
+        zero = t.clone()
+        zero[none] = 0
+        assert torch.equal(logits, ghd.ghd_verify_step(ctx, weights, kvs, tree, zero)[0])
+        drow = dev(np.array([l if l < 3 else -1 for l in level], np.int32))
+        u = torch.rand(n, device="cuda")
+        got = ghd.ghd_accept_sampled(ctx, ghd.SampledRows(tree.parent[:n], t, logits, u, draft_row=drow, draft_logits=draft))[0].cpu().numpy()
+        nodes, toks = osam.verify(PARENT, t.cpu().numpy(), logits.cpu().numpy(), u.cpu().numpy(), 1.0, drow.cpu().numpy(), draft.cpu().numpy(), 1.0)
+        assert list(got[2:2 + len(nodes)]) == nodes and list(got[258:258 + len(toks)]) == toks and not set(nodes) & set(none)
+        greedy = ghd.ghd_accept(ctx, tree, t, amax).cpu().numpy()
+        assert not set(greedy[2:3 + greedy[0]]) & set(none)
+    ghd.ghd_sync_status(ctx)
