@@ -12,7 +12,7 @@
 // units as SMs, a cluster of CTAs shares each, a part of k to every CTA, and adds up through distributed shared memory.
 // Otherwise the flattened (unit, k-step) space is cut into equal ranges, one per CTA: whoever has the first k-step of a unit finishes
 // it, with its own sums in registers, as the last of its range; the others have come to it first and left their sums in the workspace (a
-// bounded wait makes sure; every CTA is resident).  Both add in the order of k.
+// bounded wait makes sure; they have started before it).  Both add in the order of k.
 //
 // The tensor cores cut off a little of each sum they add to, so that long sums of one sign lose more than rounded ones, the more the longer: accumulators
 // are taken out every CHUNK k-steps and added up in registers with rounding.  Relative error of the norm, sums of 4096 to 14336 elements of one sign, for
@@ -227,7 +227,9 @@ k_mx4_gemm(const __grid_constant__ Mx4Maps maps, const Mx4Params p) {
     const uint32_t stage_bytes = (sb_off + KS * x_sf + 1023u) & ~1023u;
     Smem* sm = reinterpret_cast<Smem*>(tiles + (size_t)p.stages * stage_bytes);
 
-    const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31, cta = blockIdx.x, ctas = gridDim.x;
+    // Ranges are dealt from the last one on: a CTA waits for those with the ranges behind its own, which then have started before it, also where a kernel of
+    // another stream holds SMs back.
+    const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31, ctas = gridDim.x, cta = p.split > 1 ? (int)blockIdx.x : ctas - 1 - (int)blockIdx.x;
     int unit0, kc0, my_iters;
     if (p.split > 1) {
         const int rank = cta % p.split;

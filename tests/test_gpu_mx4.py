@@ -453,3 +453,30 @@ def test_long_sums_lose_little(ghd, dtype, k, signs):
     err = float((ghd.ghd_mx4_linear(ctx, x, held).double() - want).norm() / want.norm())
     ghd.ghd_sync_status(ctx)
     assert err <= (2.0 ** -23 if signs == 2 or dtype == "f32" else 2.0 ** -22)
+
+
+@pytest.mark.parametrize("dtype", ["f16", "f32"])
+def test_two_contexts_at_once(ghd, dtype):
+    """Products of two contexts on two streams, each with units that several CTAs share, while a third stream keeps SMs busy by turns."""
+    import torch
+    r = np.random.RandomState(61)
+    shapes, sides, jobs = [(50, 12928, 640), (16, 25600, 384)], [torch.cuda.Stream() for _ in range(3)], []
+    for (n, m, k), side in zip(shapes, sides):
+        with torch.cuda.stream(side):
+            ctx = make_ctx(ghd, dtype, k, n)
+        w, codes, scales = random_held(ghd, r, m, k)
+        x = r.randn(n, k).astype(np_t(dtype))
+        jobs.append((ctx, dev(x), w, x, codes, scales, [torch.empty(n, m, device="cuda") for _ in range(30)]))
+    a = torch.randn(2048, 2048, device="cuda")
+    b = torch.empty_like(a)
+    torch.cuda.synchronize()
+    for i in range(30):
+        for ctx, dx, w, *_, ys in jobs:
+            ghd.ghd_mx4_linear(ctx, dx, w, y=ys[i])
+        with torch.cuda.stream(sides[2]):
+            torch.mul(a, a, out=b)
+    torch.cuda.synchronize()
+    for (n, m, k), (ctx, dx, w, x, codes, scales, ys) in zip(shapes, jobs):
+        ghd.ghd_sync_status(ctx)
+        check_product(x, codes, scales, m, k, ys[0].cpu().numpy())
+        assert all(torch.equal(ys[0], y) for y in ys[1:])
