@@ -317,11 +317,13 @@ __device__ double total_left(Team& m, const Dist<COLD>& p, const Dist<COLD>& q, 
             }
         }
 #pragma unroll 1
-        for (int i = 0; i < n; ++i) {
-            const int d = m.s->gone[i];
-            if (d / SEG != m.seg0 + g) continue;                 // (the whole warp)
+        for (int i = 0; i < n; i += 32) {
+            const int x = i + m.lane < n ? m.s->gone[i + m.lane] : -1;
+            for (uint32_t here = __ballot_sync(0xffffffffu, x >= 0 && x / SEG == m.seg0 + g); here; here &= here - 1) {
+                const int d = __shfl_sync(0xffffffffu, x, __ffs(here) - 1) - t;
 #pragma unroll
-            for (int e = 0; e < RUN; ++e) if (d == t + e) v[e] = make_double2(0.0, 0.0);
+                for (int e = 0; e < RUN; ++e) if (d == e) v[e] = make_double2(0.0, 0.0);
+            }
         }
         double sum = 0.0;
 #pragma unroll
@@ -684,7 +686,7 @@ __global__ void __launch_bounds__(THREADS, 2) k_accept_sampled(ghd_sampled a, in
                         if (threadIdx.x == 0) sm.gone[n_gone] = x;
                         ++n_gone;
                         __syncthreads();
-                        if (rest < 0x1p-10) {                  // the difference loses its digits (random numbers close to one get here)
+                        if (px > 0.0 && rest < 0x1p-10) {      // the difference loses its digits (random numbers close to one get here)
                             W = total_left(m, p, p, 0.0, n_gone, nullptr, false, rest);
                             fresh = true;
                         }
@@ -831,7 +833,7 @@ ghd_status ghd_accept_sampled(ghd_ctx* c, const ghd_sampled* a, ghd_accept_resul
     c->entry_fresh = 1;
     const double scale = scale_of(a->temperature), draft_scale = a->draft_row ? scale_of(a->draft_temperature) : 0.0;
     // P and Q of a node's rows are kept from one rejected draw to the next where two CTAs' worth fits into a SM (trees of 64 nodes over 32000
-    // tokens, kernel us without / with: one 30.7 / 28.3, 48 of them 72.5 / 67.2)
+    // tokens, us without / with: one 30.2 / 28.4, 48 of them 85 / 78)
     const size_t room = (room_for(c->cfg.vocab, k) + 15) / 16 * 16, keeps = keep_for(c->cfg.vocab, k);
     const bool keep = a->draft_row && room + keeps <= MAX_ROOM;
     const int keep_at = keep ? (int)(room / sizeof(double)) : 0;
