@@ -10,9 +10,9 @@ namespace {
 using namespace mx4;
 
 // ---------------------------------------------------------------- quantise, read back
-// Both are bound by memory (27648 x 5120 halves: quantise 54 us, 6.6 TB/s; read back 59 us, 6.0; with eight elements a lane and one row's
-// load at a time quantising took 95: its instructions, shuffles above all, are as many for eight elements as for sixteen).  A lane has eight elements of a row (read) or sixteen (quantise: two lanes to a scale), and the loads of ROWS
-// neighbouring rows go out together.
+// Both are bound by memory (27648 x 5120 halves: quantise 54 us, 6.6 TB/s; read back 59 us, 6.0).  A lane has eight elements of a row to read, sixteen to
+// quantise (two lanes to a scale: instructions, shuffles above all, are as many for eight elements as for sixteen, and eight of them and one
+// row's load at a time took 95 us), and the loads of ROWS neighbouring rows go out together.
 constexpr int ROWS = 4, ROWS_PER_CTA = 8 * ROWS;      // rows of a warp
 
 // largest magnitude of sixteen elements, NaN if one is

@@ -22,7 +22,7 @@
 //
 // What bounds it: with up to 16 rows the memory (16 rows by 32000 x 4096: 20 us of which 11 are streaming at 345 cycles a k-step, the rest
 // set-up and the last unit's end; 68 MB of weights), with 64 and more the MMAs (a stage of eight of 128 x 192 x 32 takes 806 cycles of 768: gate and up of
-// 256 rows by 13824 x 5120 twice, 88 us, 2.5 PFLOP/s of e4m3 products under the power cap).  One row by 4096 x 4096: 7.2 us, half of it in the two launches.
+// 256 rows by 13824 x 5120 twice, 91 us, 2.4 PFLOP/s of e4m3 products under the power cap).  One row by 4096 x 4096: 7.4 us, half of it in the two launches.
 // cta_group::2 would halve x's share of the loads, which do not bound it; kind::f16 with unpacked weights would need twice the
 // shared memory's bandwidth for them.
 #include <cuda.h>

@@ -2,7 +2,7 @@
 // tokens against the target's probabilities.
 //
 // A row of logits is one distribution, w_s = exp(l_s / temperature) up to a factor, in 64 bits: a token is decided by where a random
-// number falls between running sums of up to 2^17 weights, whose borders 32 bits would move.
+// number falls between running sums of up to 2^20 weights, whose borders 32 bits would move.
 //
 // The tokens lie in segments of 256 (32 lanes with 8 neighbours each), the segments in equal shares over the CTAs of a cluster, in
 // order.  One pass over a row leaves the weight of every segment.  Weights are powers of two, 2^(l log2(e) / temperature - ref) with a
@@ -14,7 +14,7 @@
 //
 // What bounds it: chains of latencies.  10 draws from 5 rows of 32000: 20 us, 1.75 for each draw (where it falls, the segment's logits from
 // the L2, two running sums over 32 lanes, the segment's weight again); 4 draws from 320 rows 35 us, 19 of them the pass over the rows at 1.4 instructions a cycle.
-// A tree: 14 us when nothing was drawn, about 1 a level and 2 to 3 a rejected draw (28 with three of these); 48 trees of 64 nodes, row by row, 34.
+// A tree: 15 us when nothing was drawn, about 1 a level and 2 to 3 a rejected draw (28 with three of these); 48 trees of 64 nodes, row by row, 34.
 #include <cstdio>
 
 #include "internal.h"
