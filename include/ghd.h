@@ -432,7 +432,8 @@ typedef struct ghd_sampled {
 
 /* Verification.  From the root on, with P the distribution of the node and Q that of its draft row, the node's children are tested in
  * the order of their rows, which is that of their draws from Q without replacement:
- *   x is accepted if u Q(x) < P(x); otherwise P becomes max(P - Q, 0) over its sum, and Q becomes Q without x over its sum.
+ *   x is accepted if u Q(x) < P(x); otherwise P becomes max(P - Q, 0) over its sum (P without x over its sum where rounding leaves
+ *   nothing of that), and Q becomes Q without x over its sum.
  *   A token that Q does not hold (any more) is passed over.  Children that were not drawn are accepted if u < P(x); otherwise P
  *   becomes P without x over its sum.
  * The walk goes on from the first accepted child.  Where there is none, the last token is the first one whose running sum of P exceeds

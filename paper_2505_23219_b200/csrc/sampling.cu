@@ -14,7 +14,7 @@
 //
 // What bounds it: chains of latencies.  10 draws from 5 rows of 32000: 20 us, 1.75 for each draw (where it falls, the segment's logits from
 // the L2, two running sums over 32 lanes, the segment's weight again); 4 draws from 320 rows 35 us, 19 of them the pass over the rows at 1.4 instructions a cycle.
-// A tree: 15 us when nothing was drawn, about 1 a level and 2 to 3 a rejected draw (28 with three of these); 48 trees of 64 nodes, row by row, 34.
+// A tree: 15 us when nothing was drawn, about 1 a level and 2 to 3 a rejected draw (29 with three of these); 48 trees of 64 nodes, row by row, 34.
 #include <cstdio>
 
 #include "internal.h"
@@ -41,6 +41,7 @@ struct Shared {
     float uniform[GHD_MAX_NODES];
     double of_p[GHD_MAX_NODES], of_q[GHD_MAX_NODES];          // of the children of the node: their tokens' probabilities
     int32_t gone[GHD_MAX_NODES];                // tokens that are not in the distribution any more
+    double taken[GHD_MAX_NODES];                // what rejected draws have taken from P, as multiples of Q
     double roots[16];
 };
 
@@ -128,7 +129,7 @@ struct Dist {
     double scale, ref, inv_sum;
     bool ok;
     const double* roots;
-    __device__ __forceinline__ double of(float l) const { return weight<COLD>(l, scale, ref, roots) * inv_sum; }
+    __device__ __forceinline__ double of(float l) const { return __dmul_rn(weight<COLD>(l, scale, ref, roots), inv_sum); }
 };
 
 // This CTA's share of a row, and what the cluster has agreed on so far.
@@ -291,45 +292,70 @@ __device__ bool measure(Team& m, Dist<COLD>& p, Dist<COLD>& q) {
     return far;
 }
 
-// What is left after rejected draws gone[0 .. n): of P max(P - beta Q, 0), the weights of every own segment into seg[], of the CTAs' shares into
-// share[] -> the total; of Q the sum without these tokens -> rest.  Both are sums over what is left: 1 - Q(rejected) has no right digit where a
-// rejected token holds all but 1e-16 of Q.  keep (or null): room for P and Q of the own segments, which `kept` says are there from the
-// rejection before.
+// What a rejected draw leaves of P at a token.  One rounding, and the same wherever it is worked out: sums and the tokens in them must agree on
+// where there is nothing.
+__device__ __forceinline__ double take(double p, double q, double a) { return fmax(__fma_rn(-a, q, p), 0.0); }
+
+// P and Q of this lane's tokens of segment g
 template <bool COLD>
-__device__ double total_left(Team& m, const Dist<COLD>& p, const Dist<COLD>& q, double beta, int n, double2* keep, bool kept, double& rest) {
+__device__ __forceinline__ void both_of(const Team& m, const Dist<COLD>& p, const Dist<COLD>& q, int g, double (&a)[RUN], double (&b)[RUN]) {
+    float x[RUN], y[RUN];
+    const int t = m.first_of(m.seg0 + g);
+    m.load(p.row, t, x);
+    m.load(q.row, t, y);
+#pragma unroll
+    for (int e = 0; e < RUN; ++e) {
+        a[e] = p.of(x[e]);
+        b[e] = q.of(y[e]);
+    }
+}
+// ... after rejected draws: P less taken[0 .. steps) times Q, one after the other, and Q, both without the tokens gone[0 .. n)
+__device__ __forceinline__ void leave(const Team& m, int g, int steps, int n, double (&a)[RUN], double (&b)[RUN]) {
+#pragma unroll 1
+    for (int i = 0; i < steps; ++i) {
+        const double w = m.s->taken[i];
+#pragma unroll
+        for (int e = 0; e < RUN; ++e) a[e] = take(a[e], b[e], w);
+    }
+#pragma unroll 1
+    for (int i = 0; i < n; i += 32) {
+        const int d = i + m.lane < n ? m.s->gone[i + m.lane] : -1;
+        for (uint32_t here = __ballot_sync(0xffffffffu, d >= 0 && d / SEG == m.seg0 + g); here; here &= here - 1) {
+            const int at = __shfl_sync(0xffffffffu, d, __ffs(here) - 1) - m.first_of(m.seg0 + g);
+#pragma unroll
+            for (int e = 0; e < RUN; ++e) if (at == e) a[e] = b[e] = 0.0;
+        }
+    }
+}
+
+// What is left after rejected draws (see leave): of P the weights of every own segment into seg[], of the CTAs' shares into share[] -> the total;
+// of Q the sum -> rest.  Both are sums over what is left: 1 - Q(rejected) has no right digit where a rejected token holds all but 1e-16 of Q.
+// keep (or null): room for P and Q of the own segments, which `kept` says are there from the rejection before.
+template <bool COLD>
+__device__ double total_left(Team& m, const Dist<COLD>& p, const Dist<COLD>& q, int steps, int n, double2* keep, bool kept, double& rest) {
     double all = 0.0, all_q = 0.0;
 #pragma unroll 1
     for (int g = m.warp; g < m.segs; g += WARPS) {
-        double2 v[RUN];
+        double a[RUN], b[RUN], sum = 0.0;
         double2* at = keep + g * SEG + m.lane;
-        const int t = m.first_of(m.seg0 + g);
         if (keep && kept) {
 #pragma unroll
-            for (int e = 0; e < RUN; ++e) v[e] = at[e * 32];
-        } else {
-            float x[RUN], y[RUN];
-            m.load(p.row, t, x);
-            m.load(q.row, t, y);
-#pragma unroll
             for (int e = 0; e < RUN; ++e) {
-                v[e] = make_double2(p.of(x[e]), q.of(y[e]));
-                if (keep) at[e * 32] = v[e];
+                const double2 v = at[e * 32];
+                a[e] = v.x;
+                b[e] = v.y;
             }
-        }
-#pragma unroll 1
-        for (int i = 0; i < n; i += 32) {
-            const int x = i + m.lane < n ? m.s->gone[i + m.lane] : -1;
-            for (uint32_t here = __ballot_sync(0xffffffffu, x >= 0 && x / SEG == m.seg0 + g); here; here &= here - 1) {
-                const int d = __shfl_sync(0xffffffffu, x, __ffs(here) - 1) - t;
+        } else {
+            both_of(m, p, q, g, a, b);
 #pragma unroll
-                for (int e = 0; e < RUN; ++e) if (d == e) v[e] = make_double2(0.0, 0.0);
-            }
+            for (int e = 0; e < RUN; ++e)
+                if (keep) at[e * 32] = make_double2(a[e], b[e]);
         }
-        double sum = 0.0;
+        leave(m, g, steps, n, a, b);
 #pragma unroll
         for (int e = 0; e < RUN; ++e) {
-            sum += fmax(v[e].x - beta * v[e].y, 0.0);
-            all_q += v[e].y;
+            sum += a[e];
+            all_q += b[e];
         }
         sum = warp_sum(sum);
         if (m.lane == 0) m.seg[g] = sum;
@@ -564,11 +590,12 @@ __global__ void __launch_bounds__(THREADS, HELD) k_draft_sample(const float* __r
 // ---------------------------------------------------------------- verification
 // A walk from the root.  At a node with target distribution P and draft distribution Q its children are looked at in order, with
 // P_1 = P, Q_1 = Q: child x is accepted if u Q_j(x) < P_j(x); otherwise P_{j+1} = max(P_j - Q_j, 0) / its sum and Q_{j+1} = Q_j
-// without x / its sum.  Written out, P_j = max(P - beta_j Q, 0) / W_j with W_j its sum: subtracting Q_j = c_j Q from that gives
-// beta_{j+1} = beta_j + c_j W_j, and 1 / c_j is the sum of Q without the rejected tokens.  A rejected token has u Q_j >= P_j, u < 1, so
-// P_{j+1} gives it nothing, and so do all later ones: beta only grows (rounding is kept out of it by taking rejected tokens out).  So two
-// numbers are kept instead of two distributions, and a rejection costs one pass over the vocabulary for both sums.  Where P - beta Q
-// is nothing but rounding, P_j stays, without x.  Candidates that nobody drew have Q = 1 at themselves: P_{j+1} is P_j without x.
+// without x / its sum.  Neither is divided by its sum here: with p_j = W_j P_j, W_j the sum of p_j, and 1 / c_j the sum of Q without the rejected
+// tokens, Q_j is c_j Q and p_{j+1} = max(p_j - c_j W_j Q, 0).  So a rejection leaves one number a_j = c_j W_j, from which, with the ones before it,
+// a token's p is worked out at any time, and costs one pass over the vocabulary for both sums.  (max(P - (a_1 + .. + a_j) Q, 0) is the same without
+// rounding, but a difference of numbers that agree to ever more digits.)  A rejected token has u Q_j >= P_j, u < 1, so P_{j+1} gives it nothing;
+// it is taken out, so that rounding gives it nothing either.  Where p_j - a_j Q is nothing but rounding, p_j stays, without x.
+// Candidates that nobody drew have Q = 1 at themselves: P_{j+1} is P_j without x.
 // The segments' weights and references of all rows, of the targets and behind them of the drafts, a warp to a segment.  With few trees
 // the walk below knows its rows one after the other only, and most SMs would wait; weighing all rows first costs less than it saves.
 template <bool COLD>
@@ -651,10 +678,9 @@ __global__ void __launch_bounds__(THREADS, 2) k_accept_sampled(ghd_sampled a, in
             sm.of_q[threadIdx.x] = look && q.row ? q.of(lq) : 0.0;
         }
         __syncthreads();
-        double beta = 0.0, W = 1.0, rest = 1.0;                // rest: of what the children come from (Q, or P if they were not drawn) without the rejected tokens
-        int n_gone = 0, next = -1;
+        double W = 1.0, rest = 1.0;                            // rest: of what the children come from (Q, or P if they were not drawn) without the rejected tokens
+        int n_gone = 0, steps = 0, next = -1;
         bool fresh = false;                                    // seg[] and share[] are of the weights as they are, their total is W
-        auto left = [&](float lp, float lq) { return fmax(p.of(lp) - beta * q.of(lq), 0.0); };
         if (p.ok && (!q.row || q.ok))
             for (int word = 0; word < GHD_MAX_NODES / 32 && next < 0; ++word)
                 for (uint32_t bits = sm.child[word]; bits; bits &= bits - 1) {
@@ -667,14 +693,23 @@ __global__ void __launch_bounds__(THREADS, 2) k_accept_sampled(ghd_sampled a, in
                         for (int g = 0; g < n_gone; ++g) before |= sm.gone[g] == x;
                         if (!(qx > 0.0) || before) continue;
                         const double c_j = 1.0 / fmax(rest, qx);
-                        if (u * (qx * c_j) * W < fmax(px - beta * qx, 0.0)) { next = c; break; }
+                        if (u * (qx * c_j) * W < px) { next = c; break; }
+                        const double a_j = c_j * W;
                         __syncthreads();
-                        if (threadIdx.x == 0) sm.gone[n_gone] = x;
+                        if (threadIdx.x == 0) {
+                            sm.gone[n_gone] = x;
+                            sm.taken[steps] = a_j;
+                        }
                         ++n_gone;
+                        ++steps;
                         __syncthreads();
-                        const double more = beta + c_j * W, w = total_left(m, p, q, more, n_gone, keep, fresh, rest);
-                        if (w > 0.0) beta = more;
-                        W = w > 0.0 ? w : total_left(m, p, q, beta, n_gone, keep, true, rest);
+                        W = total_left(m, p, q, steps, n_gone, keep, fresh, rest);
+                        if (W > 0.0) {
+                            if (threadIdx.x < GHD_MAX_NODES) sm.of_p[threadIdx.x] = take(sm.of_p[threadIdx.x], sm.of_q[threadIdx.x], a_j);
+                            __syncthreads();
+                        } else {
+                            W = total_left(m, p, q, --steps, n_gone, keep, true, rest);
+                        }
                         fresh = true;
                     } else {
                         bool before = false;
@@ -687,7 +722,7 @@ __global__ void __launch_bounds__(THREADS, 2) k_accept_sampled(ghd_sampled a, in
                         ++n_gone;
                         __syncthreads();
                         if (px > 0.0 && rest < 0x1p-10) {      // the difference loses its digits (random numbers close to one get here)
-                            W = total_left(m, p, p, 0.0, n_gone, nullptr, false, rest);
+                            W = total_left(m, p, p, 0, n_gone, nullptr, false, rest);
                             fresh = true;
                         }
                     }
@@ -722,20 +757,11 @@ __global__ void __launch_bounds__(THREADS, 2) k_accept_sampled(ghd_sampled a, in
                 double before, start;
                 if (own_share(m, target, before) && m.warp == 0) {
                     const int per = (m.segs + 31) / 32, sg = segment_of(m.seg, m.segs, per, lane_sum(m.seg, m.segs, per, m.lane), before, target, m.lane, start);
-                    float x[RUN], y[RUN];
-                    double w[RUN];
-                    const int t0 = m.first_of(m.seg0 + max(sg, 0));
-                    m.load(p.row, t0, x);
-                    if (fresh && q.row) {
-                        m.load(q.row, t0, y);
-#pragma unroll
-                        for (int e = 0; e < RUN; ++e) w[e] = left(x[e], y[e]);
-                    } else {
-#pragma unroll
-                        for (int e = 0; e < RUN; ++e) w[e] = p.of(x[e]);
-                    }
-                    without(w, t0, sm.gone, n_gone);
-                    const int t = token_of(w, t0, start, target, m.lane);
+                    const int g = max(sg, 0);
+                    double w[RUN], v[RUN];
+                    both_of(m, p, q.row ? q : p, g, w, v);
+                    leave(m, g, steps, n_gone, w, v);
+                    const int t = token_of(w, m.first_of(m.seg0 + g), start, target, m.lane);
                     if (m.lane == 0) out->tokens[depth] = t;
                 }
             }
@@ -833,7 +859,7 @@ ghd_status ghd_accept_sampled(ghd_ctx* c, const ghd_sampled* a, ghd_accept_resul
     c->entry_fresh = 1;
     const double scale = scale_of(a->temperature), draft_scale = a->draft_row ? scale_of(a->draft_temperature) : 0.0;
     // P and Q of a node's rows are kept from one rejected draw to the next where two CTAs' worth fits into a SM (trees of 64 nodes over 32000
-    // tokens, us without / with: one 30.2 / 28.4, 48 of them 85 / 78)
+    // tokens, us without / with: one 31 / 29.5, 48 of them 88 / 81)
     const size_t room = (room_for(c->cfg.vocab, k) + 15) / 16 * 16, keeps = keep_for(c->cfg.vocab, k);
     const bool keep = a->draft_row && room + keeps <= MAX_ROOM;
     const int keep_at = keep ? (int)(room / sizeof(double)) : 0;

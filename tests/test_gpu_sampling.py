@@ -674,3 +674,39 @@ def test_verify_at_the_smallest_temperatures(ghd):
             many = torch.cat((dev(b.draft), torch.zeros(49152, V, device="cuda")))
             b.check(ghd.ghd_accept_sampled(ctx, b.rows(ghd, draft_logits=many)).cpu().numpy())
     ghd.ghd_sync_status(ctx)
+
+
+def improbable_batch(r, seqs, kids, vocab, both):
+    """Drafter and target agree but for some 1e-5: the tokens behind the first one or two (`both`) are all but impossible for the target, and are what the
+    children hold.  Each is rejected, and each time all but some 1e-5 of what was left is taken away."""
+    b = Batch(r, [1 + kids] * seqs, vocab, 1.0, False)
+    n = 1 + kids
+    b.parent = np.tile(np.array([-1] + [0] * kids, np.int32), seqs)
+    b.drow = np.repeat(np.arange(seqs), n).astype(np.int32)
+    b.draft = (np.full((seqs, vocab), -np.inf)).astype(np.float32)
+    b.logits = np.full((b.n, vocab), -60.0, np.float32) - (3 * r.rand(b.n, vocab)).astype(np.float32)
+    for s in range(seqs):
+        order = r.choice(vocab, kids + 4, replace=False)
+        top = order[:1 + both]
+        b.draft[s, order] = -11 - 2 * r.rand(kids + 4)
+        b.draft[s, top] = [0.0, 0.4][:len(top)]
+        b.logits[n * s, top] = [0.0, 0.4 + r.choice([-1e-4, 1e-4])][:len(top)]
+        b.tokens[n * s + 1:n * (s + 1)] = order[2:2 + kids]
+        b.u[n * s + 1:n * (s + 1)] = 0.3 + 0.7 * r.rand(kids)
+    return b
+
+
+@pytest.mark.parametrize("both", [0, 1])
+@pytest.mark.parametrize("vocab,seqs,kids", [(20, 200, 6), (700, 60, 3), (8000, 150, 5)])
+def test_children_that_are_all_but_impossible(ghd, vocab, seqs, kids, both):
+    """What is left of the target shrinks by 1e-5 with each rejection, and keeps its digits; there always is a last token."""
+    import torch
+    r = np.random.RandomState(vocab + kids + both)
+    b = improbable_batch(r, seqs, kids, vocab, both)
+    ctx = ctx_for(ghd, vocab)
+    got = ghd.ghd_accept_sampled(ctx, b.rows(ghd, draft_row=dev(b.drow), draft_logits=dev(b.draft)))
+    rest = torch.zeros(49152 * 256 // vocab + 1 if vocab > 256 else 49152, vocab, device="cuda")
+    assert (got == ghd.ghd_accept_sampled(ctx, b.rows(ghd, draft_row=dev(b.drow), draft_logits=torch.cat((dev(b.draft), rest))))).all()
+    ghd.ghd_sync_status(ctx)
+    assert check_cold(b, got.cpu().numpy(), 1.0) == seqs
+    assert (got[:, 258] >= 0).all()
